@@ -492,6 +492,80 @@ cat_status cat_gram_f32(const void* X, cat_dtype dtype, int64_t n, int64_t d, fl
 cat_status cat_alignment_ceiling_host(const double* sigma_x, const double* sigma_w, int64_t d, double* out3);
 
 /*
+ * Microscaled 4-bit floating point (MXFP4 of the OCP Microscaling Formats specification, v1.0): the number
+ * format that the tensor cores multiply as it is, beside the integer codes above.  Not in the paper, whose
+ * quantizer is the uniform one; the transforms go before it all the same (cat_block_transform's x' = T x and
+ * W' = W T^{-1} are what cat_mx_quantize then takes).
+ *
+ * A row of d values (d a multiple of 32, at most 262144) is
+ *   codes   d/2 bytes: E2M1 codes, value 2j in the low nibble of byte j.  Bit 3 is the sign, bits 0-2 the
+ *           magnitude: 0, 0.5, 1, 1.5, 2, 3, 4, 6;
+ *   scales  cat_mx_scale_pitch(d) bytes: d/32 rounded up to a multiple of 16.  Byte j < d/32 is the scale
+ *           2^(byte - 127) of values 32j .. 32j+31, 255 for NaN; the bytes behind are written as zeros and not
+ *           read for their value.
+ * Quantization of a block of 32 with largest magnitude a: scale byte max(floor(log2 a) + 125, 0) (0 where a = 0),
+ * value / scale to the nearest E2M1 value, ties to the even code, magnitudes above 6 to 6.  A block with an
+ * infinity or a NaN gets the NaN scale and codes 0 (outputs that use it are NaN), and raises the non-finite bit
+ * of the device status word (CAT_ERR_NUMERIC).
+ */
+
+/* cat_mx_scale_pitch -- bytes of a row's scales (0 where d is not a multiple of 32 in the range above). */
+int64_t cat_mx_scale_pitch(int64_t d);
+
+/*
+ * cat_mx_quantize -- x device [n][d] in `dtype` to codes xq [m][d/2] and scales xs [m][pitch].
+ *   rows  NULL (then m == n), or device [m] int32: output row r is x's row rows[r] (experts' tokens, gathered as
+ *         they are quantized).  An index outside [0, n) gives a row of zeros.
+ * Serves activations and weights alike.
+ */
+cat_status cat_mx_quantize(const void* x, cat_dtype dtype, int64_t n, int64_t d, const int32_t* rows, int64_t m,
+                           uint8_t* xq, uint8_t* xs, cat_stream_t stream);
+
+/* cat_mx_dequantize -- the values that codes and scales stand for, device [n][d] in `out_dtype`; exact in both
+ * (NaN under a NaN scale). */
+cat_status cat_mx_dequantize(const uint8_t* xq, const uint8_t* xs, int64_t n, int64_t d, cat_dtype out_dtype, void* out,
+                             cat_stream_t stream);
+
+/* cat_mx_swiglu_quantize -- gu device [n][2d] in `dtype`, a row the gate g and then u: the 4-bit form of
+ * silu(g) u = g / (1 + exp(-g)) u, computed in float32 and rounded once.  For a down projection's input. */
+cat_status cat_mx_swiglu_quantize(const void* gu, cat_dtype dtype, int64_t n, int64_t d, uint8_t* xq, uint8_t* xs,
+                                  cat_stream_t stream);
+
+/*
+ * cat_mx_rmsnorm_quantize -- residual addition, root-mean-square norm and quantization of its output:
+ *   h = x + residual;   v = h / sqrt(mean_i h_i^2 + eps) * weight;   xq, xs = the 4-bit form of v
+ * all in float32; v is of the sum before it is rounded to h's type.
+ *   x, residual  device [n][d] in `dtype`; residual may be NULL (h = x).
+ *   weight       device [d] in `weight_dtype`.
+ *   h            out, device [n][d] in `dtype`; may be x or residual themselves, and may be NULL (not written).
+ * eps >= 0 and finite.
+ */
+cat_status cat_mx_rmsnorm_quantize(const void* x, const void* residual, cat_dtype dtype, const void* weight,
+                                   cat_dtype weight_dtype, int64_t n, int64_t d, float eps, void* h, uint8_t* xq,
+                                   uint8_t* xs, cat_stream_t stream);
+
+/*
+ * cat_mx_linear -- y[t][o] = sum_i x[t][i] W[o][i] of 4-bit operands (n x d and d_out x d), products exact and
+ * summed in float32; y device [n][d_out] in `out_dtype`, rounded once.
+ */
+cat_status cat_mx_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* Wq, const uint8_t* ws, int64_t n, int64_t d,
+                         int64_t d_out, cat_dtype out_dtype, void* y, cat_stream_t stream);
+
+/*
+ * cat_mx_linear_grouped -- the products of experts: rows offsets[e] .. offsets[e+1]-1 of x [m][d] times expert e's
+ * weights.
+ *   Wq, ws    device [experts][d_out][d/2] and [experts][d_out][pitch]; 1 <= experts <= 1024.
+ *   offsets   device [experts + 1] int32, in order, within [0, m]; read on the device, so routing needs no
+ *             synchronization.  Empty groups are fine.  Offsets out of order or out of range are taken as the
+ *             nearest that are not (never read or written out of bounds).
+ *   y         device [m][d_out] in `out_dtype`; rows of no group (before offsets[0], from offsets[experts] on) are
+ *             set to zero.
+ */
+cat_status cat_mx_linear_grouped(const uint8_t* xq, const uint8_t* xs, const uint8_t* Wq, const uint8_t* ws,
+                                 const int32_t* offsets, int64_t experts, int64_t m, int64_t d, int64_t d_out,
+                                 cat_dtype out_dtype, void* y, cat_stream_t stream);
+
+/*
  * cat_device_status -- synchronizes `stream`, then reads and clears the device status word.
  * Returns CAT_OK, CAT_ERR_TIMEOUT (a bounded wait in a kernel gave up and the kernel returned
  * early; its outputs are undefined) or CAT_ERR_NUMERIC (a kernel met a non-finite value; the

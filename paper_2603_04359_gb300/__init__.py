@@ -24,6 +24,8 @@ __all__ = [
     "cat_block_transform", "cat_dequantize_codes", "cat_gemm_f32", "one_sided_sqnr", "cat_set_wait_limit_ns",
     "cat_transform_quantize_act_hd", "cat_fwht_rows", "cat_gram_f32", "cat_alignment_ceiling_host",
     "cat_split_transform", "cat_split_transform_bytes", "cat_transform_quantize_act_split",
+    "cat_mx_scale_pitch", "cat_mx_quantize", "cat_mx_dequantize", "cat_mx_swiglu_quantize", "cat_mx_rmsnorm_quantize",
+    "cat_mx_linear", "cat_mx_linear_grouped",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -90,6 +92,13 @@ def load_library() -> ctypes.CDLL:
         "cat_transform_quantize_act_e8": ([P, I, I64, I64, I32, P, P, P, P, P], I),
         "cat_w4a4_linear_e8": ([P, P, P, P, I64, I64, I64, P, P, P], I),
         "cat_w4a4_linear_sqnr_e8": ([P, P, P, P, I64, I64, I64, P, P, P, P], I),
+        "cat_mx_scale_pitch": ([I64], I64),
+        "cat_mx_quantize": ([P, I, I64, I64, P, I64, P, P, P], I),
+        "cat_mx_dequantize": ([P, P, I64, I64, I, P, P], I),
+        "cat_mx_swiglu_quantize": ([P, I, I64, I64, P, P, P], I),
+        "cat_mx_rmsnorm_quantize": ([P, P, I, P, I, I64, I64, ctypes.c_float, P, P, P, P], I),
+        "cat_mx_linear": ([P, P, P, P, I64, I64, I64, I, P, P], I),
+        "cat_mx_linear_grouped": ([P, P, P, P, P, I64, I64, I64, I64, I, P, P], I),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -618,6 +627,131 @@ def cat_alignment_ceiling_host(sigma_x: np.ndarray, sigma_w: np.ndarray) -> Tupl
     vp = lambda a: a.ctypes.data_as(ctypes.c_void_p)  # noqa: E731
     _check("cat_alignment_ceiling_host", load_library().cat_alignment_ceiling_host(vp(sx), vp(sw), d, vp(out)))
     return float(out[0]), float(out[1]), float(out[2])
+
+
+# ---- microscaled 4-bit floating point (MXFP4): codes uint8 [rows, d / 2], scales uint8 [rows, cat_mx_scale_pitch(d)]
+
+def cat_mx_scale_pitch(d: int) -> int:
+    """Bytes of a row's scales: d / 32 rounded up to a multiple of 16."""
+    return (d + 511) // 512 * 16
+
+
+def _mx_out(xq, xs, m: int, d: int, dev: torch.device) -> Tuple[torch.Tensor, torch.Tensor]:
+    return (_given(xq, "xq", torch.uint8, (m, d // 2), dev),
+            _given(xs, "xs", torch.uint8, (m, cat_mx_scale_pitch(d)), dev))
+
+
+def cat_mx_quantize(x: torch.Tensor, rows: Optional[torch.Tensor] = None, xq: Optional[torch.Tensor] = None,
+                    xs: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The 4-bit form (codes, scales) of x [n, d], or of its rows ``rows`` (int32 [m]; an index outside [0, n) gives a
+    row of zeros).  Activations and weights alike."""
+    _need(x, "x")
+    n, d = x.shape
+    dev = x.device
+    m = n
+    if rows is not None:
+        m = rows.numel()
+        _expect(rows, "rows", torch.int32, (m,), dev)
+    xq, xs = _mx_out(xq, xs, m, d, dev)
+    _check("cat_mx_quantize", load_library().cat_mx_quantize(x.data_ptr(), _dtype(x), n, d, _ptr(rows), m, xq.data_ptr(),
+                                                             xs.data_ptr(), _stream(dev)))
+    return xq, xs
+
+
+def _mx_result(t: Optional[torch.Tensor], name: str, dtype: Optional[torch.dtype], shape: tuple,
+               dev: torch.device) -> torch.Tensor:
+    """An output of either type: of ``dtype``, by default the caller's buffer's own or float32."""
+    if t is not None:
+        _expect(t, name, dtype or t.dtype, shape, dev)
+        return t
+    return torch.empty(shape, dtype=dtype or torch.float32, device=dev)
+
+
+def _mx_codes(q: torch.Tensor, s: torch.Tensor, names: Tuple[str, str], shape: tuple, dev: torch.device) -> int:
+    """Checks codes [*shape, d / 2] and their scales; returns d."""
+    half = q.shape[-1]
+    _expect(q, names[0], torch.uint8, (*shape, half), dev)
+    _expect(s, names[1], torch.uint8, (*shape, (half + 255) // 256 * 16), dev)
+    return 2 * half
+
+
+def cat_mx_dequantize(xq: torch.Tensor, xs: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
+                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that codes [n, d / 2] and scales stand for, [n, d]: float32 (default) or bfloat16, exact in both."""
+    n, dev = xq.shape[0], xq.device
+    d = _mx_codes(xq, xs, ("xq", "xs"), (n,), dev)
+    out = _mx_result(out, "out", out_dtype, (n, d), dev)
+    _check("cat_mx_dequantize", load_library().cat_mx_dequantize(xq.data_ptr(), xs.data_ptr(), n, d, _dtype(out),
+                                                                 out.data_ptr(), _stream(dev)))
+    return out
+
+
+def cat_mx_swiglu_quantize(gu: torch.Tensor, xq: Optional[torch.Tensor] = None,
+                           xs: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The 4-bit form of silu(g) u for gu [n, 2 d] = [g | u]."""
+    _need(gu, "gu")
+    n, d2 = gu.shape
+    dev = gu.device
+    if d2 % 2:
+        raise ValueError(f"gu has {d2} columns, expected an even number")
+    d = d2 // 2
+    xq, xs = _mx_out(xq, xs, n, d, dev)
+    _check("cat_mx_swiglu_quantize", load_library().cat_mx_swiglu_quantize(gu.data_ptr(), _dtype(gu), n, d, xq.data_ptr(),
+                                                                           xs.data_ptr(), _stream(dev)))
+    return xq, xs
+
+
+def cat_mx_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                            h: Optional[torch.Tensor] = None, xq: Optional[torch.Tensor] = None,
+                            xs: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """h = x + residual, and the 4-bit form of h / sqrt(mean(h^2) + eps) * weight: (xq, xs, h).  ``h`` may be x or
+    residual; without a residual it is x and nothing is written but the 4-bit form."""
+    _need(x, "x")
+    n, d = x.shape
+    dev = x.device
+    _need(weight, "weight")
+    _expect(weight, "weight", weight.dtype, (d,), dev)
+    if residual is not None:
+        _expect(residual, "residual", x.dtype, (n, d), dev)
+        h = _given(h, "h", x.dtype, (n, d), dev)
+    elif h is not None:
+        _expect(h, "h", x.dtype, (n, d), dev)
+    xq, xs = _mx_out(xq, xs, n, d, dev)
+    _check("cat_mx_rmsnorm_quantize", load_library().cat_mx_rmsnorm_quantize(
+        x.data_ptr(), _ptr(residual), _dtype(x), weight.data_ptr(), _dtype(weight), n, d, eps, _ptr(h), xq.data_ptr(),
+        xs.data_ptr(), _stream(dev)))
+    return xq, xs, x if h is None else h
+
+
+def cat_mx_linear(xq: torch.Tensor, xs: torch.Tensor, Wq: torch.Tensor, ws: torch.Tensor,
+                  out_dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [n, d_out] = x W^T of 4-bit operands, summed in float32; y is float32 (default) or bfloat16."""
+    n, dev = xq.shape[0], xq.device
+    d_out = Wq.shape[0]
+    d = _mx_codes(xq, xs, ("xq", "xs"), (n,), dev)
+    if _mx_codes(Wq, ws, ("Wq", "ws"), (d_out,), dev) != d:
+        raise ValueError(f"Wq has {Wq.shape[1]} bytes a row, xq has {xq.shape[1]}")
+    y = _mx_result(y, "y", out_dtype, (n, d_out), dev)
+    _check("cat_mx_linear", load_library().cat_mx_linear(xq.data_ptr(), xs.data_ptr(), Wq.data_ptr(), ws.data_ptr(), n, d,
+                                                         d_out, _dtype(y), y.data_ptr(), _stream(dev)))
+    return y
+
+
+def cat_mx_linear_grouped(xq: torch.Tensor, xs: torch.Tensor, Wq: torch.Tensor, ws: torch.Tensor, offsets: torch.Tensor,
+                          out_dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [m, d_out]: rows offsets[e] to offsets[e + 1] of x times expert e's weights (Wq [experts, d_out, d / 2]);
+    offsets int32 [experts + 1] on the device, ragged and empty groups allowed, rows of no group zero."""
+    m, dev = xq.shape[0], xq.device
+    experts, d_out = Wq.shape[0], Wq.shape[1]
+    d = _mx_codes(xq, xs, ("xq", "xs"), (m,), dev)
+    if _mx_codes(Wq, ws, ("Wq", "ws"), (experts, d_out), dev) != d:
+        raise ValueError(f"Wq has {Wq.shape[2]} bytes a row, xq has {xq.shape[1]}")
+    _expect(offsets, "offsets", torch.int32, (experts + 1,), dev)
+    y = _mx_result(y, "y", out_dtype, (m, d_out), dev)
+    _check("cat_mx_linear_grouped", load_library().cat_mx_linear_grouped(
+        xq.data_ptr(), xs.data_ptr(), Wq.data_ptr(), ws.data_ptr(), offsets.data_ptr(), experts, m, d, d_out, _dtype(y),
+        y.data_ptr(), _stream(dev)))
+    return y
 
 
 def cat_set_wait_limit_ns(ns: int) -> None:

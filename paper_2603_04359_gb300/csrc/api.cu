@@ -9,6 +9,7 @@
 
 #include "../../include/cat_w4a4.h"
 #include "common.cuh"
+#include "mx_format.cuh"
 #include "transform_host.h"
 
 namespace cat {
@@ -49,6 +50,16 @@ cudaError_t launch_transform_quantize_dp(const void* x, int dtype, int64_t n, in
 cudaError_t launch_dp_gemm(const uint8_t* x_planes, int DX, const float* sx, const int32_t* zx, const uint8_t* w_planes,
                            int DW, const float* sw, const int32_t* w_rowsum, int64_t n, int64_t d_in, int64_t d_out,
                            float* y, int32_t* acc_out, uint32_t* status, cudaStream_t stream);
+cudaError_t launch_mx_quantize(const void* x, int dtype, int64_t n, int64_t d, const int32_t* rows, int64_t m, int gated,
+                               uint8_t* xq, uint8_t* xs, uint32_t* status, cudaStream_t stream);
+cudaError_t launch_mx_dequantize(const uint8_t* xq, const uint8_t* xs, int64_t n, int64_t d, int dtype, void* out,
+                                 cudaStream_t stream);
+cudaError_t launch_mx_rmsnorm_quantize(const void* x, const void* residual, const void* weight, int dtype,
+                                       int weight_dtype, int64_t n, int64_t d, float eps, void* h, uint8_t* xq, uint8_t* xs,
+                                       uint32_t* status, cudaStream_t stream);
+cudaError_t launch_mx_gemm(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws,
+                           const int32_t* offsets, int64_t experts, int64_t m, int64_t d, int64_t d_out, int out_dtype,
+                           void* y, uint32_t* status, cudaStream_t stream);
 }  // namespace cat
 
 namespace {
@@ -930,4 +941,122 @@ cat_status cat_alignment_ceiling_host(const double* sigma_x, const double* sigma
   if (!cat::alignment_ceiling_host(sigma_x, sigma_w, d, &out3[0], &out3[1], &out3[2]))
     return fail(CAT_ERR_NUMERIC, "Sigma_x is not positive definite");
   return ok();
+}
+
+// ---- microscaled 4-bit floating point
+
+static cat_status check_mx(int64_t n, int64_t d) {
+  if (n < 0) return fail(CAT_ERR_SHAPE, "the number of rows must be >= 0");
+  if (d <= 0 || d % 32 != 0 || d > kMaxDin) return fail(CAT_ERR_SHAPE, "d must be a positive multiple of 32, at most 262144");
+  if (n > 0x7FFFFFFF) return fail(CAT_ERR_SHAPE, "the number of rows must fit in int32");
+  return CAT_OK;
+}
+
+static bool known(cat_dtype t) { return t == CAT_F32 || t == CAT_BF16; }
+
+// What is left of a call whose arguments hold: the device, its status word, the launch.
+template <typename F>
+static cat_status mx_launch(const char* where, F&& f) {
+  cat_status st = check_device();
+  if (st != CAT_OK) return st;
+  cudaError_t e;
+  uint32_t* status = status_word(&e);
+  if (!status) return cuda_fail(e, "status word");
+  if ((e = f(status)) != cudaSuccess) return cuda_fail(e, where);
+  return ok();
+}
+
+int64_t cat_mx_scale_pitch(int64_t d) { return d <= 0 || d % 32 != 0 || d > kMaxDin ? 0 : cat::mx_pitch(d); }
+
+cat_status cat_mx_quantize(const void* x, cat_dtype dtype, int64_t n, int64_t d, const int32_t* rows, int64_t m,
+                           uint8_t* xq, uint8_t* xs, cat_stream_t stream) {
+  if (!known(dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_mx(n, d);
+  if (st != CAT_OK || (st = check_mx(m, d)) != CAT_OK) return st;
+  if (!rows && m != n) return fail(CAT_ERR_SHAPE, "without rows, m must be n");
+  if (m == 0) return ok();
+  if ((n > 0 && !x) || !xq || !xs) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(x) || !aligned16(rows) || !aligned16(xq) || !aligned16(xs))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_quantize launch", [&](uint32_t* status) {
+    return cat::launch_mx_quantize(x, (int)dtype, n, d, rows, m, 0, xq, xs, status, (cudaStream_t)stream);
+  });
+}
+
+cat_status cat_mx_dequantize(const uint8_t* xq, const uint8_t* xs, int64_t n, int64_t d, cat_dtype out_dtype, void* out,
+                             cat_stream_t stream) {
+  if (!known(out_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_mx(n, d);
+  if (st != CAT_OK) return st;
+  if (n == 0) return ok();
+  if (!xq || !xs || !out) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(xq) || !aligned16(xs) || !aligned16(out))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_dequantize launch", [&](uint32_t*) {
+    return cat::launch_mx_dequantize(xq, xs, n, d, (int)out_dtype, out, (cudaStream_t)stream);
+  });
+}
+
+cat_status cat_mx_swiglu_quantize(const void* gu, cat_dtype dtype, int64_t n, int64_t d, uint8_t* xq, uint8_t* xs,
+                                  cat_stream_t stream) {
+  if (!known(dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_mx(n, d);
+  if (st != CAT_OK) return st;
+  if (n == 0) return ok();
+  if (!gu || !xq || !xs) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(gu) || !aligned16(xq) || !aligned16(xs))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_swiglu_quantize launch", [&](uint32_t* status) {
+    return cat::launch_mx_quantize(gu, (int)dtype, n, d, nullptr, n, 1, xq, xs, status, (cudaStream_t)stream);
+  });
+}
+
+cat_status cat_mx_rmsnorm_quantize(const void* x, const void* residual, cat_dtype dtype, const void* weight,
+                                   cat_dtype weight_dtype, int64_t n, int64_t d, float eps, void* h, uint8_t* xq,
+                                   uint8_t* xs, cat_stream_t stream) {
+  if (!known(dtype) || !known(weight_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  if (!(eps >= 0.f) || std::isinf(eps)) return fail(CAT_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+  cat_status st = check_mx(n, d);
+  if (st != CAT_OK) return st;
+  if (n == 0) return ok();
+  if (!x || !weight || !xq || !xs) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(h) || !aligned16(xq) || !aligned16(xs))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_rmsnorm_quantize launch", [&](uint32_t* status) {
+    return cat::launch_mx_rmsnorm_quantize(x, residual, weight, (int)dtype, (int)weight_dtype, n, d, eps, h, xq, xs, status,
+                                           (cudaStream_t)stream);
+  });
+}
+
+cat_status cat_mx_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* Wq, const uint8_t* ws, int64_t n, int64_t d,
+                         int64_t d_out, cat_dtype out_dtype, void* y, cat_stream_t stream) {
+  if (!known(out_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_mx(n, d);
+  if (st != CAT_OK) return st;
+  if (d_out <= 0 || d_out > 0x7FFFFFFF) return fail(CAT_ERR_SHAPE, "d_out must be >= 1 and fit in int32");
+  if (n == 0) return ok();
+  if (!xq || !xs || !Wq || !ws || !y) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(xq) || !aligned16(xs) || !aligned16(Wq) || !aligned16(ws) || !aligned16(y))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_linear launch", [&](uint32_t* status) {
+    return cat::launch_mx_gemm(xq, xs, Wq, ws, nullptr, 1, n, d, d_out, (int)out_dtype, y, status, (cudaStream_t)stream);
+  });
+}
+
+cat_status cat_mx_linear_grouped(const uint8_t* xq, const uint8_t* xs, const uint8_t* Wq, const uint8_t* ws,
+                                 const int32_t* offsets, int64_t experts, int64_t m, int64_t d, int64_t d_out,
+                                 cat_dtype out_dtype, void* y, cat_stream_t stream) {
+  if (!known(out_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_mx(m, d);
+  if (st != CAT_OK) return st;
+  if (experts < 1 || experts > cat::kMxMaxExperts) return fail(CAT_ERR_SHAPE, "experts must be in [1, 1024]");
+  if (d_out <= 0 || d_out > 0x7FFFFFFF / experts) return fail(CAT_ERR_SHAPE, "d_out must be >= 1 and experts * d_out fit in int32");
+  if (m == 0) return ok();
+  if (!xq || !xs || !Wq || !ws || !offsets || !y) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(xq) || !aligned16(xs) || !aligned16(Wq) || !aligned16(ws) || !aligned16(offsets) || !aligned16(y))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_linear_grouped launch", [&](uint32_t* status) {
+    return cat::launch_mx_gemm(xq, xs, Wq, ws, offsets, experts, m, d, d_out, (int)out_dtype, y, status,
+                               (cudaStream_t)stream);
+  });
 }

@@ -1,0 +1,121 @@
+"""The microscaled 4-bit operators without a GPU: the reference's own grid, and what the library refuses."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import mx_reference as R
+import paper_2603_04359_gb300 as cat
+from paper_2603_04359_gb300 import build as catbuild
+from fake_runtime import ensure_built
+
+P, BAD = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10008)
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    ensure_built()
+    return cat.load_library()
+
+
+def test_reference_rounds_to_the_nearest_grid_value():
+    x = np.linspace(-8, 8, 32 * 512).reshape(-1, 32).copy()
+    x[:, 0] = 4.0                                                  # every block's scale is 1
+    x[:, 1:] = np.clip(x[:, 1:], -7.99, 7.99)
+    codes, b = R.quantize(x)
+    assert np.all(b == 127)
+    v = R.values(codes, b)
+    nearest = np.abs(x[..., None] - np.concatenate([R.GRID, -R.GRID])).min(-1)
+    np.testing.assert_array_equal(np.abs(x - v), nearest)
+    ties = np.zeros((1, 32))
+    ties[0, :10] = [4, .25, .75, 1.25, 1.75, 2.5, 3.5, 5, -2.5, 7.9]
+    np.testing.assert_array_equal(R.values(*R.quantize(ties))[0, :10], [4, 0, 1, 1, 2, 2, 4, 4, -2, 6])
+
+
+def test_reference_scales_and_packing():
+    x = np.zeros((5, 544))
+    x[0, 0], x[1, 33], x[2, 64], x[3, 100] = 1.0, 7.9, 2.0 ** -140, np.inf
+    b = R.scale_bytes(x)
+    assert (b[0, 0], b[1, 1], b[2, 2], b[3, 3], b[4, 0]) == (125, 127, 0, 255, 0)
+    codes, b = R.quantize(x)
+    q, s = R.pack(codes, b)
+    assert q.shape == (5, 272) and s.shape == (5, 32) and cat.cat_mx_scale_pitch(544) == 32
+    assert not s[:, 17:].any()
+    again = R.unpack(q, s)
+    np.testing.assert_array_equal(again[0], codes)
+    np.testing.assert_array_equal(again[1], b)
+
+
+def test_scale_pitch(lib):
+    for d in (32, 480, 512, 544, 4096, 14336, 262144):
+        assert lib.cat_mx_scale_pitch(d) == cat.cat_mx_scale_pitch(d) == R.pitch(d) and R.pitch(d) % 16 == 0
+        assert R.pitch(d) >= d // 32
+    for d in (0, -32, 48, 262176):
+        assert lib.cat_mx_scale_pitch(d) == 0
+
+
+def test_refusals(lib):
+    """Invalid calls are refused on the host, before anything touches CUDA."""
+    # (x, dtype, n, d, rows, m, xq, xs, stream)
+    q = lib.cat_mx_quantize
+    assert q(P, 2, 4, 64, None, 4, P, P, None) == 1                 # dtype
+    assert q(P, 0, 4, 48, None, 4, P, P, None) == 2                 # d % 32
+    assert q(P, 0, 4, 0, None, 4, P, P, None) == 2
+    assert q(P, 0, 4, 262176, None, 4, P, P, None) == 2             # too long a row
+    assert q(P, 0, -1, 64, None, -1, P, P, None) == 2
+    assert q(P, 0, 4, 64, None, 5, P, P, None) == 2                 # m without rows
+    assert q(P, 0, 4, 64, P, -1, P, P, None) == 2
+    assert q(P, 0, 1 << 31, 64, None, 1 << 31, P, P, None) == 2
+    assert q(None, 0, 4, 64, None, 4, P, P, None) == 1
+    assert q(P, 0, 4, 64, None, 4, None, P, None) == 1
+    assert q(P, 0, 4, 64, None, 4, P, None, None) == 1
+    for bad in ((BAD, None, P, P), (P, BAD, P, P), (P, None, BAD, P), (P, None, P, BAD)):
+        assert q(bad[0], 0, 4, 64, bad[1], 4, bad[2], bad[3], None) == 3
+    assert q(None, 0, 0, 64, None, 0, None, None, None) == 0        # nothing to do
+    # (xq, xs, n, d, out_dtype, out, stream)
+    dq = lib.cat_mx_dequantize
+    assert dq(P, P, 4, 64, 5, P, None) == 1
+    assert dq(P, P, 4, 40, 0, P, None) == 2
+    assert dq(P, None, 4, 64, 0, P, None) == 1
+    assert dq(P, P, 4, 64, 0, BAD, None) == 3
+    assert dq(None, None, 0, 64, 0, None, None) == 0
+    # (gu, dtype, n, d, xq, xs, stream)
+    g = lib.cat_mx_swiglu_quantize
+    assert g(P, 3, 4, 64, P, P, None) == 1
+    assert g(P, 1, 4, 63, P, P, None) == 2
+    assert g(None, 1, 4, 64, P, P, None) == 1
+    assert g(P, 1, 4, 64, P, BAD, None) == 3
+    assert g(None, 1, 0, 64, None, None, None) == 0
+    # (x, residual, dtype, weight, weight_dtype, n, d, eps, h, xq, xs, stream)
+    r = lib.cat_mx_rmsnorm_quantize
+    assert r(P, P, 2, P, 0, 4, 64, 0.1, P, P, P, None) == 1
+    assert r(P, P, 0, P, 2, 4, 64, 0.1, P, P, P, None) == 1
+    for eps in (-1e-6, NAN, INF):
+        assert r(P, P, 0, P, 0, 4, 64, eps, P, P, P, None) == 1
+    assert r(P, P, 0, P, 0, 4, 16, 0.1, P, P, P, None) == 2
+    assert r(P, P, 0, None, 0, 4, 64, 0.1, P, P, P, None) == 1
+    assert r(P, BAD, 0, P, 0, 4, 64, 0.1, P, P, P, None) == 3
+    assert r(P, P, 0, P, 0, 4, 64, 0.1, BAD, P, P, None) == 3
+    assert r(None, None, 0, None, 0, 0, 64, 0.1, None, None, None, None) == 0
+    # (xq, xs, Wq, ws, n, d, d_out, out_dtype, y, stream)
+    f = lib.cat_mx_linear
+    assert f(P, P, P, P, 4, 64, 8, 2, P, None) == 1
+    assert f(P, P, P, P, 4, 72, 8, 0, P, None) == 2
+    assert f(P, P, P, P, 4, 64, 0, 0, P, None) == 2
+    assert f(P, P, P, P, 4, 64, 1 << 31, 0, P, None) == 2
+    assert f(P, P, P, P, 4, 64, 8, 0, None, None) == 1
+    assert f(P, P, BAD, P, 4, 64, 8, 0, P, None) == 3
+    assert f(None, None, None, None, 0, 64, 8, 0, None, None) == 0
+    # (xq, xs, Wq, ws, offsets, experts, m, d, d_out, out_dtype, y, stream)
+    e = lib.cat_mx_linear_grouped
+    assert e(P, P, P, P, P, 2, 4, 64, 8, 7, P, None) == 1
+    for experts in (0, -1, 1025):
+        assert e(P, P, P, P, P, experts, 4, 64, 8, 0, P, None) == 2
+    assert e(P, P, P, P, P, 1024, 4, 64, 1 << 22, 0, P, None) == 2  # experts x d_out
+    assert e(P, P, P, P, None, 2, 4, 64, 8, 0, P, None) == 1
+    assert e(P, P, P, P, BAD, 2, 4, 64, 8, 0, P, None) == 3
+    assert e(P, P, P, P, P, 2, -4, 64, 8, 0, P, None) == 2
+    assert e(None, None, None, None, None, 2, 0, 64, 8, 0, None, None) == 0
+    f(P, P, P, P, 4, 72, 8, 0, P, None)
+    assert b"multiple of 32" in lib.cat_last_error()
