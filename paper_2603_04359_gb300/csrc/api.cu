@@ -43,6 +43,7 @@ cudaError_t launch_fwht_rows(float* V, int64_t rows, int64_t d, cudaStream_t str
 cudaError_t launch_gram_f32(const void* X, int dtype, int64_t n, int64_t d, float* C, cudaStream_t stream);
 cudaError_t set_decode_wait_limit(uint64_t ns);
 cudaError_t set_dp_wait_limit(uint64_t ns);
+cudaError_t set_mx_wait_limit(uint64_t ns);
 size_t dp_l24_work_bytes(int64_t n);
 cudaError_t launch_transform_quantize_dp(const void* x, int dtype, int64_t n, int64_t d, int k, const float* A, int bits,
                                          int asym, int l24, uint8_t* planes, float* scale, int32_t* zero,
@@ -798,6 +799,7 @@ cat_status cat_set_wait_limit_ns(uint64_t ns) {
   if (st != CAT_OK) return st;
   cudaError_t e = cat::set_decode_wait_limit(v);
   if (e == cudaSuccess) e = cat::set_dp_wait_limit(v);
+  if (e == cudaSuccess) e = cat::set_mx_wait_limit(v);
   if (e != cudaSuccess) return cuda_fail(e, "cat_set_wait_limit_ns");
   return ok();
 }

@@ -1,15 +1,131 @@
-// Products of microscaled 4-bit operands (mx_format.cuh), plain and grouped by expert:
+// Products of microscaled 4-bit operands (mx_format.cuh), plain and grouped by expert, on 5th-generation tensor cores:
 //
 //   y[t, o] = sum over blocks b of 32 channels of 2^(bx + bw - 254) sum_{i in b} c_x[t, i] c_w[o, i]
 //
-// A simple kernel: 64 tokens by 64 channels a CTA, operands widened to float32 in shared memory, four by four outputs
-// a thread, sums in 32 bits.
+// The tensor cores multiply the format as it is stored (tcgen05.mma.kind::mxf4.block_scale, K = 64): codes go from
+// memory to 128B-swizzled shared memory by TMA and are read there, scales go by TMA to shared memory and from there,
+// through registers, to tensor memory, where the MMA reads 2 bytes a row and K = 64.  Sums are float32 in tensor memory.
+//
+// Weights are the M operand and tokens the N operand: M is 128 whatever the call, N any multiple of 8, so a tile fits
+// the tokens there are -- one token of a decode step, an expert's ragged rows -- and the padding is at most 7 of them.
+// A thread of the epilogue holds one channel of many tokens, so a warp's store is 32 neighbouring channels of a token.
+//
+// Two forms of one kernel:
+//   * CG = 2, CTA pairs: a tile is 256 channels by up to 256 tokens, each CTA with its 128 channels and half of the
+//     tokens' codes in shared memory (and all of the tokens' scales in its tensor memory); persistent, one pair a tile;
+//   * CG = 1: 128 channels by up to 128 tokens; K may be cut over the CTAs of a cluster (`split`), whose parts are
+//     exchanged through distributed shared memory and summed in the order of their K, so results do not depend on timing.
+//
+// Warps (512 threads):
+//   0       TMA of codes              1  lane 0 issues the MMAs (CG = 2, odd CTA: forwards stages to the even one)
+//   2       TMA of scales, TMEM       3  (CG = 2, odd CTA: forwards scale slots)
+//   4..7    scales from shared to tensor memory, each to its own 32 lanes (the MMA reads a copy in each)
+//   8..15   epilogue, two warps a lane quadrant, taking 32-token chunks in turn
+// TMEM: accumulators (two where they fit) from column 0, then the scale slots of 512 channels each.  Every wait is
+// bounded; a wait that gives up raises the device status word and all roles drain and exit.
+#include <cstring>
+#include <mutex>
+
+#include "gemm_pair.cuh"
 #include "mx_format.cuh"
+#include "per_device.h"
 
 namespace cat {
 namespace {
 
-constexpr int kTile = 64, kStep = 32;
+constexpr int kThreads = 512;
+constexpr int BM = 128;                     // channels per CTA
+constexpr int BK = 256;                     // values per K step (128 bytes a row)
+constexpr int kChunk = 512;                 // values per scale slot (16 bytes a row)
+constexpr int kMaxStages = 8, kMaxSlots = 4, kRing = 4;
+constexpr int kScaleWarp0 = 4, kScaleWarps = 4, kEpiWarp0 = 8, kEpiWarps = 8;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kStageW = BM * 128;      // 16 KiB of weight codes a stage
+constexpr uint32_t kScalesW = BM * 16;      // 2 KiB of weight scales a ring slot
+// Shared memory: at least half an SM's, as two CTAs would wait for each other's tensor memory.  Clusters take all but
+// 12 KB, whatever they need: a CTA that holds its SM's tensor memory while its cluster waits for another SM's must not
+// share the SM with a CTA of some other kernel of which the same holds (all that use tensor memory need more than 12 KB).
+constexpr size_t kMaxSmem = 215 * 1024, kMinSmem = 120 * 1024;
+
+__device__ uint64_t g_mx_wait_limit = kWaitLimitNs;   // bound of the pipeline waits (cat_set_wait_limit_ns)
+
+struct MxArgs {
+  const int32_t* offsets;                   // grouped: [experts + 1], else null
+  void* y;
+  uint32_t* status;
+  int experts, m, d, d_out;
+  int nt;                                   // most tokens of a tile
+  int bx, bxs;                              // token rows per TMA box: codes, scales
+  int stages, acc_bufs, slots, xcols;       // xcols: TMEM columns of the tokens' scales per 128 channels
+  int split;                                // CTAs that share a tile's K (CG = 1)
+  uint32_t stage_bytes, ring_bytes;
+  uint32_t off_ring, off_red, off_table, off_bars;
+};
+
+struct Bars {
+  uint64_t full[kMaxStages], ready[kMaxStages], empty[kMaxStages];
+  uint64_t sfull[kRing], sempty[kRing];                       // scales in shared memory
+  uint64_t tfull[kMaxSlots], tready[kMaxSlots], tempty[kMaxSlots];   // scales in tensor memory
+  uint64_t acc_full[2], acc_empty[2], mma_done;
+  uint32_t fwd_stage[kMaxStages], fwd_slot[kMaxSlots];        // even CTA: targets of the odd CTA's st.async
+  uint32_t tmem_addr;
+  int abort;
+  int total;                                                  // grouped: tiles of the launch
+};
+
+struct Tile {
+  int w_row;                                // the expert's first row of the weights
+  int o0;                                   // first channel (of the pair)
+  int t0, valid, n;                         // tokens: first row, how many, padded to a multiple of 8 CG
+};
+
+// ---- tensor memory and MMA ---------------------------------------------------------------------
+__device__ __forceinline__ void tmem_st2(uint32_t taddr, uint32_t a, uint32_t b) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(taddr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Instruction descriptor of kind::mxf4: A and B E2M1, K-major, scales E8M0, D fp32, shape M x N.
+__device__ __forceinline__ uint32_t idesc_mxf4(int M, int N) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27);
+}
+// which byte of a scale column's word an MMA's first scale is in (0 or 2), of A and of B
+__device__ __forceinline__ uint32_t idesc_scale_byte(uint32_t id) { return (id << 4) | (id << 29); }
+
+template <int CG>
+__device__ __forceinline__ void mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scale,
+                                         uint32_t b_scale, uint32_t accumulate) {
+  if constexpr (CG == 2)
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %6, 0; "
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p; }" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %6, 0; "
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p; }" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+        : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  if constexpr (CG == 2)
+    mma_commit_pair(bar);
+  else
+    mma_commit(bar);
+}
+
+// a float32 into CTA `rank`'s shared memory at this address's offset
+__device__ __forceinline__ void st_cluster(float* p, uint32_t rank, float v) {
+  uint32_t remote;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v) : "memory");
+}
 
 template <typename T>
 __device__ __forceinline__ T to_out(float v);
@@ -18,99 +134,546 @@ __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// A group's first row and the one past its last: offsets in order within [0, m], whatever the caller's are.
-__device__ __forceinline__ int edge(const int32_t* offsets, int e, int m, int before) {
-  return min(max(offsets[e], before), m);
+// Grouped: one warp fills the table: rows[e], the first row of expert e (rows[experts]: one past the last), and
+// tiles[e], the tiles of the experts before it.  Offsets are taken in order and within [0, m], whatever they are.
+__device__ __forceinline__ void make_table(const MxArgs& a, int* rows, int* tiles, int channel_tiles, int* total) {
+  const int lane = threadIdx.x & 31;
+  int high = 0, sum = 0;                    // the largest offset and the tiles so far
+  for (int e0 = 0; e0 <= a.experts; e0 += 32) {
+    const int e = e0 + lane;
+    int o = e <= a.experts ? min(max(a.offsets[e], 0), a.m) : a.m;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, o, k);
+      if (lane >= k) o = max(o, v);
+    }
+    o = max(o, high);
+    if (e <= a.experts) rows[e] = o;
+    high = __shfl_sync(0xFFFFFFFFu, o, 31);
+  }
+  __syncwarp();
+  for (int e0 = 0; e0 < a.experts; e0 += 32) {
+    const int e = e0 + lane;
+    const int mine = e < a.experts ? (rows[e + 1] - rows[e] + a.nt - 1) / a.nt * channel_tiles : 0;
+    int s = mine;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, s, k);
+      if (lane >= k) s += v;
+    }
+    if (e < a.experts) tiles[e] = sum + s - mine;
+    sum += __shfl_sync(0xFFFFFFFFu, s, 31);
+  }
+  if (lane == 0) {
+    tiles[a.experts] = sum;
+    *total = sum;
+  }
+}
+
+template <int CG, typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+    mx_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
+                   const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmXs,
+                   const __grid_constant__ MxArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = smem + a.off_ring;            // kRing x [weights' scales 128 x 16 B | tokens' scales]
+  float* red = reinterpret_cast<float*>(smem + a.off_red);   // split: [part][token of this CTA's][128 channels]
+  int* rows = reinterpret_cast<int*>(smem + a.off_table);    // grouped: see make_table
+  int* tiles = rows + a.experts + 1;
+  Bars* bars = reinterpret_cast<Bars*>(smem + a.off_bars);
+  volatile int* abort_flag = &bars->abort;
+  T* y = static_cast<T*>(a.y);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank();
+  const int csize = CG == 2 ? 2 : a.split;       // CTAs of a cluster
+  const int cluster = blockIdx.x / csize, clusters = gridDim.x / csize;
+  const int channel_tiles = (a.d_out + CG * BM - 1) / (CG * BM);
+  const int chunks = (a.d + kChunk - 1) / kChunk, steps = (a.d + BK - 1) / BK;
+  // this CTA's share of K, in whole chunks
+  const int c0 = CG == 2 ? 0 : (int)rank * chunks / a.split, c1 = CG == 2 ? chunks : ((int)rank + 1) * chunks / a.split;
+  const int k0 = 2 * c0, k1 = min(2 * c1, steps);
+
+  if (tid == 0) {
+    for (int s = 0; s < a.stages; ++s) {
+      mbar_init(&bars->full[s], 1);
+      mbar_init(&bars->ready[s], 1);
+      mbar_init(&bars->empty[s], 1);
+    }
+    for (int s = 0; s < kRing; ++s) {
+      mbar_init(&bars->sfull[s], 1);
+      mbar_init(&bars->sempty[s], kScaleWarps);
+    }
+    for (int s = 0; s < a.slots; ++s) {
+      mbar_init(&bars->tfull[s], kScaleWarps);
+      mbar_init(&bars->tready[s], kScaleWarps);
+      mbar_init(&bars->tempty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&bars->acc_full[b], 1);
+      mbar_init(&bars->acc_empty[b], CG * kEpiWarps);
+    }
+    mbar_init(&bars->mma_done, 1);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  __syncwarp();
+  pdl_wait_then_release();                       // nothing global or in tensor memory before this
+  const uint64_t lim = g_mx_wait_limit;
+  if (a.offsets && warp == 1) make_table(a, rows, tiles, channel_tiles, &bars->total);
+  if (warp == 2) {
+    if constexpr (CG == 2)
+      tmem_alloc_pair(&bars->tmem_addr, kTmemCols);
+    else
+      tmem_alloc(&bars->tmem_addr, kTmemCols);
+  }
+  tc_fence_before();
+  cluster_sync();                                // barriers, table and TMEM address are there, in the whole cluster
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_addr;
+  const int token_tiles = (a.m + a.nt - 1) / a.nt;
+  const int total = a.offsets ? bars->total : token_tiles * channel_tiles;
+
+  if (a.offsets) {                               // rows of no group
+    const int64_t head = (int64_t)rows[0] * a.d_out, from = (int64_t)rows[a.experts] * a.d_out,
+                  all = (int64_t)a.m * a.d_out;
+    const int64_t stride = (int64_t)gridDim.x * kThreads, first = (int64_t)blockIdx.x * kThreads + tid;
+    for (int64_t i = first; i < head; i += stride) y[i] = to_out<T>(0.f);
+    for (int64_t i = from + first; i < all; i += stride) y[i] = to_out<T>(0.f);
+  }
+
+  // tile u of the launch; e: the caller's place in the table (tiles are asked for in order)
+  auto tile_at = [&](int u, int& e) {
+    Tile t;
+    int begin = 0, end = a.m, tt, ct, n_tiles = token_tiles;
+    if (a.offsets) {
+      while (u >= tiles[e + 1]) ++e;
+      begin = rows[e];
+      end = rows[e + 1];
+      n_tiles = (end - begin + a.nt - 1) / a.nt;
+      tt = (u - tiles[e]) % n_tiles;
+      ct = (u - tiles[e]) / n_tiles;
+    } else {
+      tile_coords(u, token_tiles, channel_tiles, &tt, &ct);
+    }
+    // tiles of equal size, as few as there must be
+    constexpr int kUnit = 8 * CG;
+    const int size = ((end - begin + n_tiles - 1) / n_tiles + kUnit - 1) / kUnit * kUnit;
+    t.w_row = e * a.d_out;
+    t.o0 = ct * CG * BM;
+    t.t0 = begin + tt * size;
+    t.valid = min(size, end - t.t0);             // (may be none, in the last tile)
+    t.n = size;
+    return t;
+  };
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- TMA of codes
+    if (lane == 0) {
+      prefetch_tensormap(&tmW);
+      prefetch_tensormap(&tmX);
+      uint32_t it = 0;
+      bool ok = true;
+      int e = 0;
+      for (int u = cluster; u < total && ok; u += clusters) {
+        const Tile t = tile_at(u, e);
+        const int wrow = t.w_row + t.o0 + (int)(CG == 2 ? rank : 0) * BM;
+        const int mine = t.n / CG, xrow = t.t0 + (CG == 2 ? (int)rank : 0) * mine;
+        const int boxes = (mine + a.bx - 1) / a.bx;
+        const uint32_t bytes = kStageW + (uint32_t)(boxes * a.bx) * 128u;
+        for (int ks = k0; ks < k1; ++ks, ++it) {
+          const uint32_t s = it % a.stages, use = it / a.stages;
+          if (use > 0 && !(ok = mbar_wait_bounded(&bars->empty[s], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
+          uint8_t* dst = smem + s * a.stage_bytes;
+          uint64_t* fb = CG == 2 && rank == 1 ? &bars->ready[s] : &bars->full[s];
+          mbar_arrive_expect_tx(fb, bytes + (CG == 2 && rank == 0 ? 4u : 0u));   // (+ the odd CTA's signal)
+          tma_load_2d(dst, &tmW, ks * (BK / 2), wrow, fb);
+          for (int b = 0; b < boxes; ++b)
+            tma_load_2d(dst + kStageW + (uint32_t)(b * a.bx) * 128u, &tmX, ks * (BK / 2), xrow + b * a.bx, fb);
+        }
+      }
+      // the copies in flight land before the CTA exits (they have, unless a wait gave up)
+      volatile int no_abort = 0;
+      for (uint32_t j = it > (uint32_t)a.stages ? it - a.stages : 0; j < it; ++j)
+        mbar_wait_bounded(CG == 2 && rank == 1 ? &bars->ready[j % a.stages] : &bars->full[j % a.stages],
+                          (j / a.stages) & 1, &no_abort);
+    }
+  } else if (warp == 2) {
+    // ---------------------------------------------------------------- TMA of scales
+    if (lane == 0) {
+      prefetch_tensormap(&tmWs);
+      prefetch_tensormap(&tmXs);
+      uint32_t it = 0;
+      bool ok = true;
+      int e = 0;
+      for (int u = cluster; u < total && ok; u += clusters) {
+        const Tile t = tile_at(u, e);
+        const int wrow = t.w_row + t.o0 + (int)(CG == 2 ? rank : 0) * BM;
+        const int boxes = (t.n + a.bxs - 1) / a.bxs;
+        const uint32_t bytes = kScalesW + (uint32_t)(boxes * a.bxs) * 16u;
+        for (int c = c0; c < c1; ++c, ++it) {
+          const uint32_t s = it % kRing, use = it / kRing;
+          if (use > 0 && !(ok = mbar_wait_bounded(&bars->sempty[s], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
+          uint8_t* dst = ring + s * a.ring_bytes;
+          mbar_arrive_expect_tx(&bars->sfull[s], bytes);
+          tma_load_2d(dst, &tmWs, c * 16, wrow, &bars->sfull[s]);
+          for (int b = 0; b < boxes; ++b)
+            tma_load_2d(dst + kScalesW + (uint32_t)(b * a.bxs) * 16u, &tmXs, c * 16, t.t0 + b * a.bxs, &bars->sfull[s]);
+        }
+      }
+      volatile int no_abort = 0;
+      for (uint32_t j = it > (uint32_t)kRing ? it - kRing : 0; j < it; ++j)
+        mbar_wait_bounded(&bars->sfull[j % kRing], (j / kRing) & 1, &no_abort);
+    }
+  } else if (CG == 2 && rank == 1 && (warp == 1 || warp == 3)) {
+    // ---------------------------------------------------------------- odd CTA: forward stages (1) and scale slots (3)
+    // (an arrive on the even CTA's barrier from the warps that wrote the data would stall them; a thread that waits for
+    // them here carries the signal over with an asynchronous 4-byte store)
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int u = cluster; u < total && ok; u += clusters)
+        for (int j = warp == 1 ? k0 : c0; j < (warp == 1 ? k1 : c1); ++j, ++it) {
+          const uint32_t of = warp == 1 ? a.stages : a.slots, s = it % of;
+          uint64_t* here = warp == 1 ? &bars->ready[s] : &bars->tready[s];
+          if (!(ok = mbar_wait_bounded(here, (it / of) & 1, abort_flag, __LINE__, lim))) break;
+          tc_fence_after();
+          if (warp == 1)
+            st_async_signal(&bars->fwd_stage[s], &bars->full[s], 0);
+          else
+            st_async_signal(&bars->fwd_slot[s], &bars->tfull[s], 0);
+        }
+      if (warp == 1) {                           // the pair's last commits have arrived here too
+        volatile int no_abort = 0;
+        mbar_wait_bounded(&bars->mma_done, 0, &no_abort);
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32, scale0 = tmem + a.acc_bufs * npad;
+      const uint32_t slot_cols = 16u + 4u * a.xcols;
+      uint32_t it = 0, ct = 0, tcount = 0;
+      bool ok = true;
+      int e = 0;
+      for (int u = cluster; u < total && ok; u += clusters, ++tcount) {
+        const Tile t = tile_at(u, e);
+        const uint32_t ab = tcount % a.acc_bufs, use = tcount / a.acc_bufs;
+        const uint32_t acc = tmem + ab * npad, idesc = idesc_mxf4(CG * BM, t.n);
+        if (use > 0 && !(ok = mbar_wait_bounded(&bars->acc_empty[ab], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
+        tc_fence_after();
+        for (int ks = k0; ks < k1; ++ks, ++it) {
+          const uint32_t s = it % a.stages, slot = ct % a.slots;
+          if ((ks & 1) == 0 && !(ok = mbar_wait_bounded(&bars->tfull[slot], (ct / a.slots) & 1, abort_flag, __LINE__, lim))) break;
+          if (!(ok = mbar_wait_bounded(&bars->full[s], (it / a.stages) & 1, abort_flag, __LINE__, lim))) break;
+          tc_fence_after();
+          const uint32_t wbase = smem_u32(smem + s * a.stage_bytes), xbase = wbase + kStageW;
+          const uint32_t sw = scale0 + slot * slot_cols, sx = sw + 16;
+          const int mmas = min(BK / 64, (a.d - ks * BK + 63) / 64);
+#pragma unroll
+          for (int kk = 0; kk < BK / 64; ++kk)
+            if (kk < mmas) {
+              const uint32_t word = (uint32_t)(ks & 1) * 2 + (kk >> 1);   // 128 channels' scales a word
+              mma_mxf4<CG>(acc, sdesc_kmajor_sw128(wbase) + 2 * kk, sdesc_kmajor_sw128(xbase) + 2 * kk,
+                           idesc | idesc_scale_byte(2u * (kk & 1)), sw + 4 * word, sx + a.xcols * word,
+                           ks != k0 || kk != 0 ? 1u : 0u);
+            }
+          commit<CG>(&bars->empty[s]);
+          if ((ks & 1) == 1 || ks == k1 - 1) {
+            commit<CG>(&bars->tempty[slot]);
+            ++ct;
+          }
+        }
+        if (ok) commit<CG>(&bars->acc_full[ab]);
+      }
+      commit<CG>(&bars->mma_done);               // all MMAs complete before TMEM is released
+      volatile int no_abort = 0;
+      mbar_wait_bounded(&bars->mma_done, 0, &no_abort);
+    }
+  } else if (warp >= kScaleWarp0 && warp < kScaleWarp0 + kScaleWarps) {
+    // ---------------------------------------------------------------- scales to tensor memory
+    // Column j of 128 channels' scales holds rows 32 j .. 32 j + 31, a row a lane, its word the scales of 4 blocks; each
+    // quadrant of 32 lanes has a copy.  Rows behind the tile's tokens are whatever shared memory holds: nothing uses them.
+    const uint32_t quad = (uint32_t)(warp & 3) * 32u << 16;
+    const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32, scale0 = tmem + a.acc_bufs * npad + quad;
+    const uint32_t slot_cols = 16u + 4u * a.xcols;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int u = cluster; u < total && ok; u += clusters)
+      for (int c = c0; c < c1; ++c, ++it) {
+        const uint32_t r = it % kRing, slot = it % a.slots, use = it / a.slots;
+        if (!(ok = mbar_wait_bounded(&bars->sfull[r], (it / kRing) & 1, abort_flag, __LINE__, lim))) break;
+        if (use > 0 && !(ok = mbar_wait_bounded(&bars->tempty[slot], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
+        __syncwarp();
+        tc_fence_after();
+        const uint4* src = reinterpret_cast<const uint4*>(ring + r * a.ring_bytes);
+        const uint32_t dst = scale0 + slot * slot_cols;
+        // the last chunk's bytes behind the row's scales: an MMA that covers them multiplies zero codes, so any finite
+        // scale will do
+        const int have = a.d / 32 - c * 16;
+        auto masked = [&](uint4 v) {
+          if (have < 16) {
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int left = have - 4 * i;
+              w[i] = left >= 4 ? w[i] : left <= 0 ? 0u : w[i] & ((1u << (8 * left)) - 1u);
+            }
+            v = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          return v;
+        };
+        {
+          uint4 v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = masked(src[32 * j + lane]);
+          tmem_st4(dst, v[0].x, v[1].x, v[2].x, v[3].x);
+          tmem_st4(dst + 4, v[0].y, v[1].y, v[2].y, v[3].y);
+          tmem_st4(dst + 8, v[0].z, v[1].z, v[2].z, v[3].z);
+          tmem_st4(dst + 12, v[0].w, v[1].w, v[2].w, v[3].w);
+        }
+        for (int p = 0; p < a.xcols; p += 2) {    // 64 tokens at a time
+          const uint4 v0 = masked(src[BM + 32 * p + lane]), v1 = masked(src[BM + 32 * p + 32 + lane]);
+          const uint32_t x = dst + 16 + p;
+          tmem_st2(x, v0.x, v1.x);
+          tmem_st2(x + a.xcols, v0.y, v1.y);
+          tmem_st2(x + 2 * a.xcols, v0.z, v1.z);
+          tmem_st2(x + 3 * a.xcols, v0.w, v1.w);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&bars->sempty[r]);
+          if (CG == 2 && rank == 1)
+            mbar_arrive(&bars->tready[slot]);
+          else if (CG == 2 && warp == kScaleWarp0)
+            mbar_arrive_expect_tx(&bars->tfull[slot], 4u);   // the odd CTA's signal completes the slot
+          else
+            mbar_arrive(&bars->tfull[slot]);
+        }
+      }
+  } else if (warp >= kEpiWarp0) {
+    // ---------------------------------------------------------------- epilogue
+    const int quad = warp & 3, half = (warp - kEpiWarp0) >> 2;
+    const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32;
+    uint32_t tcount = 0;
+    int e = 0;
+    for (int u = cluster; u < total; u += clusters, ++tcount) {
+      const Tile t = tile_at(u, e);
+      const uint32_t ab = tcount % a.acc_bufs;
+      if (!mbar_wait_bounded(&bars->acc_full[ab], (tcount / a.acc_bufs) & 1, abort_flag, __LINE__, lim)) break;
+      __syncwarp();
+      tc_fence_after();
+      const int row = quad * 32 + lane, o = t.o0 + (CG == 2 ? (int)rank * BM : 0) + row;
+      for (int c = half; c * 32 < t.valid; c += 2) {
+        uint32_t r[32];
+        __syncwarp();
+        CAT_TMEM_LD32(tmem + ((uint32_t)(quad * 32) << 16) + ab * npad + c * 32, r);
+        tmem_ld_wait();
+        if (CG == 1 && a.split > 1) {
+          // token t of the tile is summed by CTA t mod split, its t / split-th
+          const int each = (a.nt + a.split - 1) / a.split;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int tok = c * 32 + i;
+            if (tok < t.valid)
+              st_cluster(red + ((size_t)rank * each + tok / a.split) * BM + row, (uint32_t)(tok % a.split),
+                         __uint_as_float(r[i]));
+          }
+        } else if (o < a.d_out) {
+          T* p = y + (size_t)(t.t0 + c * 32) * a.d_out + o;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c * 32 + i < t.valid) p[(size_t)i * a.d_out] = to_out<T>(__uint_as_float(r[i]));
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (CG == 2)
+          mbar_arrive_cluster(&bars->acc_empty[ab], 0);
+        else
+          mbar_arrive(&bars->acc_empty[ab]);
+      }
+    }
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync();                                // MMAs and epilogues are done with TMEM; a split's parts have arrived
+  if (CG == 1 && a.split > 1 && cluster < total && !bars->abort) {
+    int e = 0;
+    const Tile t = tile_at(cluster, e);
+    const int each = (a.nt + a.split - 1) / a.split, o = t.o0 + (tid & (BM - 1));
+    for (int j = tid / BM; j * a.split + (int)rank < t.valid; j += kThreads / BM) {
+      float sum = 0.f;
+      for (int p = 0; p < a.split; ++p) sum += red[((size_t)p * each + j) * BM + (tid & (BM - 1))];
+      if (o < a.d_out) y[(size_t)(t.t0 + j * a.split + (int)rank) * a.d_out + o] = to_out<T>(sum);
+    }
+  }
+  if (bars->abort && tid == 0) report(a.status, timeout_bits(kWhereMxGemm, bars->abort));
+  if (warp == 2) {
+    tc_fence_after();
+    if constexpr (CG == 2)
+      tmem_dealloc_pair(tmem, kTmemCols);
+    else
+      tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiledFn>(p);
+  });
+  return fn;
+}
+
+// Bytes [rows][row_bytes], box [box_rows][box_bytes], out-of-range reads zero.
+bool make_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t row_bytes, int box_rows, int box_bytes) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+  cuuint32_t box[2] = {(cuuint32_t)box_bytes, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int sm_count() {
+  static PerDevice<int> asked;
+  return asked.get([] {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) return 148;
+    return sms;
+  });
+}
+
+struct Call {
+  const uint8_t *xq, *xs, *wq, *ws;
+  const int32_t* offsets;
+  int64_t experts, m, d, d_out;
+  void* y;
+  uint32_t* status;
+  cudaStream_t stream;
+};
+
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+template <int CG, typename T>
+cudaError_t launch_form(const Call& c, int nt, int split) {
+  MxArgs a;
+  memset(&a, 0, sizeof(a));
+  a.offsets = c.offsets;
+  a.y = c.y;
+  a.status = c.status;
+  a.experts = c.offsets ? (int)c.experts : 0;
+  a.m = (int)c.m;
+  a.d = (int)c.d;
+  a.d_out = (int)c.d_out;
+  a.nt = nt;
+  a.split = split;
+  // boxes of a whole tile's tokens, or with groups, whose tiles differ, of up to 64
+  a.bx = c.offsets && nt / CG > 64 ? 64 : nt / CG;
+  a.bxs = c.offsets && nt > 64 ? 64 : nt;
+  a.xcols = 2 * ((nt + 63) / 64);
+  const int npad = (nt + 31) / 32 * 32, slot_cols = 16 + 4 * a.xcols;
+  a.acc_bufs = 2 * npad + 2 * slot_cols <= (int)kTmemCols ? 2 : 1;
+  const int slots = ((int)kTmemCols - a.acc_bufs * npad) / slot_cols;
+  a.slots = slots < kMaxSlots ? slots : kMaxSlots;
+  a.stage_bytes = kStageW + (uint32_t)up(nt / CG, a.bx) * 128u;
+  a.ring_bytes = kScalesW + (uint32_t)up(up(nt, a.bxs), 64) * 16u;
+  const size_t red = split > 1 ? (size_t)split * ((nt + split - 1) / split) * BM * 4 : 0;
+  const size_t table = c.offsets ? up(2 * (c.experts + 1) * 4, 128) : 0;
+  const size_t rest = (size_t)kRing * a.ring_bytes + red + table + sizeof(Bars) + 1024;
+  const int stages = (int)((kMaxSmem - rest) / a.stage_bytes);
+  a.stages = stages < kMaxStages ? stages : kMaxStages;
+  if (a.slots < 2 || a.stages < 2 || nt % (8 * CG) != 0 || a.bx > 256 || a.bxs > 256) return cudaErrorInvalidConfiguration;
+  a.off_ring = a.stages * a.stage_bytes;
+  a.off_red = a.off_ring + kRing * a.ring_bytes;
+  a.off_table = a.off_red + (uint32_t)red;
+  a.off_bars = a.off_table + (uint32_t)table;
+  size_t smem = a.off_bars + sizeof(Bars) + 1024;
+  if (smem < kMinSmem) smem = kMinSmem;
+  if (CG == 2 || split > 1) smem = kMaxSmem;
+
+  CUtensorMap tw, tx, tws, txs;
+  const int64_t pitch = mx_pitch(c.d), wrows = (c.offsets ? c.experts : 1) * c.d_out;
+  if (!make_map(&tw, c.wq, wrows, c.d / 2, BM, 128) || !make_map(&tx, c.xq, c.m, c.d / 2, a.bx, 128) ||
+      !make_map(&tws, c.ws, wrows, pitch, BM, 16) || !make_map(&txs, c.xs, c.m, pitch, a.bxs, 16))
+    return cudaErrorInvalidValue;
+  static PerDevice<cudaError_t> allowed;
+  const cudaError_t attr_err = allowed.get([] { return allow_smem(mx_gemm_kernel<CG, T>, kMaxSmem); });
+  if (attr_err != cudaSuccess) return attr_err;
+
+  // at most this many tiles (with groups the device knows how many)
+  const int64_t token_tiles = (c.m + nt - 1) / nt + (c.offsets ? (c.experts < c.m ? c.experts : c.m) : 0);
+  const int64_t tiles = token_tiles * ((c.d_out + CG * BM - 1) / (CG * BM));
+  const int csize = CG == 2 ? 2 : split;
+  const int64_t resident = sm_count() / csize;
+  const int64_t clusters = split > 1 ? tiles : (tiles < resident ? tiles : resident);   // a split tile has a cluster of its own
+  if (clusters * csize > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+  note_launch();
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)(clusters * csize), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attrs[2];
+  attrs[0] = pdl_attr();
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = csize;
+  attrs[1].val.clusterDim.y = 1;
+  attrs[1].val.clusterDim.z = 1;
+  cfg.attrs = attrs;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, mx_gemm_kernel<CG, T>, tw, tx, tws, txs, a);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) mx_gemm_kernel(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs,
-                                                      const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws,
-                                                      const int32_t* __restrict__ offsets, int experts, int m, int d,
-                                                      int d_out, T* __restrict__ y) {
-  pdl_wait_then_release();
-  // token tile blockIdx.y of the groups' tiles, in order
-  int expert = 0, row0 = 0, row1 = m, tile = blockIdx.y;
-  if (offsets) {
-    int lo = edge(offsets, 0, m, 0), hi = lo;
-    for (expert = 0; expert < experts; ++expert, lo = hi) {
-      hi = edge(offsets, expert + 1, m, lo);
-      const int tiles = (hi - lo + kTile - 1) / kTile;
-      if (tile < tiles) break;
-      tile -= tiles;
-    }
-    if (expert == experts) return;
-    row0 = lo;
-    row1 = hi;
+cudaError_t launch_typed(const Call& c) {
+  const int64_t busy = c.offsets ? (c.experts < c.m ? c.experts : c.m) : 1;   // groups with rows, at most
+  const int64_t rows = (c.m + busy - 1) / busy;                               // rows of a group, on average
+  const bool pair = rows > 128;
+  if (pair) {
+    const int64_t tiles = (rows + 191) / 192;
+    const int nt = c.offsets ? 192 : (int)up((c.m + tiles - 1) / tiles, 16);
+    return launch_form<2, T>(c, nt, 1);
   }
-  row0 += tile * kTile;
-  if (row0 >= row1) return;
-  const int o0 = blockIdx.x * kTile, pitch = (int)mx_pitch(d);
-  wq += (size_t)expert * d_out * (d / 2);
-  ws += (size_t)expert * d_out * pitch;
-  __shared__ float sx[kStep][kTile + 1], sw[kStep][kTile + 1];
-  const int tid = threadIdx.x, tr = tid / 16, tc = tid % 16;
-  float acc[4][4] = {};
-  for (int k = 0; k < d; k += kStep) {
-    // 64 rows x 4 octets an operand, one a thread
-    const int r = tid / 4, oct = tid % 4;
-    uint32_t wx = 0, ww = 0;
-    float fx = 0.f, fw = 0.f;
-    if (row0 + r < row1) {
-      wx = *reinterpret_cast<const uint32_t*>(xq + (size_t)(row0 + r) * (d / 2) + k / 2 + 4 * oct);
-      fx = mx_scale(xs[(size_t)(row0 + r) * pitch + k / 32]);
-    }
-    if (o0 + r < d_out) {
-      ww = *reinterpret_cast<const uint32_t*>(wq + (size_t)(o0 + r) * (d / 2) + k / 2 + 4 * oct);
-      fw = mx_scale(ws[(size_t)(o0 + r) * pitch + k / 32]);
-    }
-    for (int i = 0; i < 8; ++i) {
-      sx[8 * oct + i][r] = mx_code_value((wx >> (4 * i)) & 15u) * fx;
-      sw[8 * oct + i][r] = mx_code_value((ww >> (4 * i)) & 15u) * fw;
-    }
-    __syncthreads();
-#pragma unroll 8
-    for (int i = 0; i < kStep; ++i) {
-      float a[4], b[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        a[j] = sx[i][tr * 4 + j];
-        b[j] = sw[i][tc + 16 * j];
-      }
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(a[p], b[q], acc[p][q]);
-    }
-    __syncthreads();
-  }
-  for (int p = 0; p < 4; ++p)
-    for (int q = 0; q < 4; ++q) {
-      const int t = row0 + tr * 4 + p, o = o0 + tc + 16 * q;
-      if (t < row1 && o < d_out) y[(size_t)t * d_out + o] = to_out<T>(acc[p][q]);
-    }
+  // one CTA a tile; K over the CTAs of a cluster where tiles leave SMs idle
+  const int nt = (int)up(c.offsets ? (c.m < 2 * rows ? c.m : 2 * rows) : c.m, 8);
+  const int n128 = nt < 128 ? nt : 128;
+  const int64_t tiles = busy * ((c.d_out + BM - 1) / BM), chunks = (c.d + kChunk - 1) / kChunk;
+  int split = 1;
+  while (split < 8 && 2 * split * tiles <= sm_count() && 2 * split <= chunks) split *= 2;
+  return launch_form<1, T>(c, n128, split);
 }
 
 }  // namespace
 
+cudaError_t set_mx_wait_limit(uint64_t ns) { return cudaMemcpyToSymbol(g_mx_wait_limit, &ns, sizeof(ns)); }
+
 // offsets == nullptr: one group of all m rows.  Rows that belong to no group are zero.
 cudaError_t launch_mx_gemm(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws,
                            const int32_t* offsets, int64_t experts, int64_t m, int64_t d, int64_t d_out, int out_dtype,
-                           void* y, uint32_t*, cudaStream_t stream) {
-  if (offsets) {
-    const cudaError_t e = cudaMemsetAsync(y, 0, (size_t)m * d_out * (out_dtype == 0 ? 4 : 2), stream);
-    if (e != cudaSuccess) return e;
-  }
-  const int64_t tiles = (m + kTile - 1) / kTile + (offsets ? (experts < m ? experts : m) : 0);
-  const dim3 grid((unsigned)((d_out + kTile - 1) / kTile), (unsigned)tiles, 1);
-  note_launch();
-  if (out_dtype == 0)
-    mx_gemm_kernel<float><<<grid, 256, 0, stream>>>(xq, xs, wq, ws, offsets, (int)experts, (int)m, (int)d, (int)d_out,
-                                                    static_cast<float*>(y));
-  else
-    mx_gemm_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(xq, xs, wq, ws, offsets, (int)experts, (int)m, (int)d,
-                                                            (int)d_out, static_cast<__nv_bfloat16*>(y));
-  return cudaGetLastError();
+                           void* y, uint32_t* status, cudaStream_t stream) {
+  const Call c = {xq, xs, wq, ws, offsets, experts, m, d, d_out, y, status, stream};
+  return out_dtype == 0 ? launch_typed<float>(c) : launch_typed<__nv_bfloat16>(c);
 }
 
 }  // namespace cat
