@@ -73,6 +73,21 @@ struct Bars {
   int total;                                                  // grouped: tiles of the launch
 };
 
+// A place in a ring of buffers and the parity of its round: next() in step with the ring's other side.
+struct Place {
+  uint32_t at = 0, round = 0;
+  __device__ __forceinline__ void next(uint32_t of) {
+    if (++at == of) {
+      at = 0;
+      ++round;
+    }
+  }
+  // waits that follow the ring's fillings (full) or the buffer's release in the round before (free)
+  __device__ __forceinline__ bool first() const { return round == 0; }
+  __device__ __forceinline__ uint32_t full() const { return round & 1; }
+  __device__ __forceinline__ uint32_t free() const { return (round - 1) & 1; }
+};
+
 struct Tile {
   int w_row;                                // the expert's first row of the weights
   int o0;                                   // first channel (of the pair)
@@ -274,6 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       prefetch_tensormap(&tmW);
       prefetch_tensormap(&tmX);
       uint32_t it = 0;
+      Place st;
       bool ok = true;
       int e = 0;
       for (int u = cluster; u < total && ok; u += clusters) {
@@ -282,9 +298,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int mine = t.n / CG, xrow = t.t0 + (CG == 2 ? (int)rank : 0) * mine;
         const int boxes = (mine + a.bx - 1) / a.bx;
         const uint32_t bytes = kStageW + (uint32_t)(boxes * a.bx) * 128u;
-        for (int ks = k0; ks < k1; ++ks, ++it) {
-          const uint32_t s = it % a.stages, use = it / a.stages;
-          if (use > 0 && !(ok = mbar_wait_bounded(&bars->empty[s], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
+        for (int ks = k0; ks < k1; ++ks, ++it, st.next(a.stages)) {
+          const uint32_t s = st.at;
+          if (!st.first() && !(ok = mbar_wait_bounded(&bars->empty[s], st.free(), abort_flag, __LINE__, lim))) break;
           uint8_t* dst = smem + s * a.stage_bytes;
           uint64_t* fb = CG == 2 && rank == 1 ? &bars->ready[s] : &bars->full[s];
           mbar_arrive_expect_tx(fb, bytes + (CG == 2 && rank == 0 ? 4u : 0u));   // (+ the odd CTA's signal)
@@ -331,13 +347,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     // (an arrive on the even CTA's barrier from the warps that wrote the data would stall them; a thread that waits for
     // them here carries the signal over with an asynchronous 4-byte store)
     if (lane == 0) {
-      uint32_t it = 0;
+      Place st;
       bool ok = true;
       for (int u = cluster; u < total && ok; u += clusters)
-        for (int j = warp == 1 ? k0 : c0; j < (warp == 1 ? k1 : c1); ++j, ++it) {
-          const uint32_t of = warp == 1 ? a.stages : a.slots, s = it % of;
+        for (int j = warp == 1 ? k0 : c0; j < (warp == 1 ? k1 : c1); ++j, st.next(warp == 1 ? a.stages : a.slots)) {
+          const uint32_t s = st.at;
           uint64_t* here = warp == 1 ? &bars->ready[s] : &bars->tready[s];
-          if (!(ok = mbar_wait_bounded(here, (it / of) & 1, abort_flag, __LINE__, lim))) break;
+          if (!(ok = mbar_wait_bounded(here, st.full(), abort_flag, __LINE__, lim))) break;
           tc_fence_after();
           if (warp == 1)
             st_async_signal(&bars->fwd_stage[s], &bars->full[s], 0);
@@ -351,41 +367,47 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
+    // The tensor cores wait for this thread wherever its instructions between two MMAs take longer than one, so all that
+    // it needs is worked out ahead and counted on, not divided.
     if (lane == 0) {
       const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32, scale0 = tmem + a.acc_bufs * npad;
-      const uint32_t slot_cols = 16u + 4u * a.xcols;
-      uint32_t it = 0, ct = 0, tcount = 0;
+      const uint32_t slot_cols = 16u + 4u * a.xcols, xcols = a.xcols;
+      const uint64_t wdesc0 = sdesc_kmajor_sw128(smem_u32(smem)), xdesc0 = sdesc_kmajor_sw128(smem_u32(smem) + kStageW);
+      const uint32_t stage16 = a.stage_bytes >> 4;
+      const int last_mmas = (a.d - (steps - 1) * BK + 63) / 64;      // of the row's last K step
+      Place st, sl, ac;
       bool ok = true;
       int e = 0;
-      for (int u = cluster; u < total && ok; u += clusters, ++tcount) {
+      for (int u = cluster; u < total && ok; u += clusters, ac.next(a.acc_bufs)) {
         const Tile t = tile_at(u, e);
-        const uint32_t ab = tcount % a.acc_bufs, use = tcount / a.acc_bufs;
-        const uint32_t acc = tmem + ab * npad, idesc = idesc_mxf4(CG * BM, t.n);
-        if (use > 0 && !(ok = mbar_wait_bounded(&bars->acc_empty[ab], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
-        tc_fence_after();
-        for (int ks = k0; ks < k1; ++ks, ++it) {
-          const uint32_t s = it % a.stages, slot = ct % a.slots;
-          if ((ks & 1) == 0 && !(ok = mbar_wait_bounded(&bars->tfull[slot], (ct / a.slots) & 1, abort_flag, __LINE__, lim))) break;
-          if (!(ok = mbar_wait_bounded(&bars->full[s], (it / a.stages) & 1, abort_flag, __LINE__, lim))) break;
-          tc_fence_after();
-          const uint32_t wbase = smem_u32(smem + s * a.stage_bytes), xbase = wbase + kStageW;
-          const uint32_t sw = scale0 + slot * slot_cols, sx = sw + 16;
-          const int mmas = min(BK / 64, (a.d - ks * BK + 63) / 64);
+        const uint32_t acc = tmem + ac.at * npad, idesc = idesc_mxf4(CG * BM, t.n);
+        if (!ac.first() && !(ok = mbar_wait_bounded(&bars->acc_empty[ac.at], ac.free(), abort_flag, __LINE__, lim))) break;
+        uint32_t more = 0;                         // accumulate (0: the tile's first MMA)
+        for (int ks = k0; ks < k1 && ok; sl.next(a.slots)) {
+          if (!(ok = mbar_wait_bounded(&bars->tfull[sl.at], sl.full(), abort_flag, __LINE__, lim))) break;
+          const uint32_t sw = scale0 + sl.at * slot_cols, sx = sw + 16;
 #pragma unroll
-          for (int kk = 0; kk < BK / 64; ++kk)
-            if (kk < mmas) {
-              const uint32_t word = (uint32_t)(ks & 1) * 2 + (kk >> 1);   // 128 channels' scales a word
-              mma_mxf4<CG>(acc, sdesc_kmajor_sw128(wbase) + 2 * kk, sdesc_kmajor_sw128(xbase) + 2 * kk,
-                           idesc | idesc_scale_byte(2u * (kk & 1)), sw + 4 * word, sx + a.xcols * word,
-                           ks != k0 || kk != 0 ? 1u : 0u);
-            }
-          commit<CG>(&bars->empty[s]);
-          if ((ks & 1) == 1 || ks == k1 - 1) {
-            commit<CG>(&bars->tempty[slot]);
-            ++ct;
+          for (int h = 0; h < 2; ++h) {            // the slot's two K steps
+            if (h == 1 && ks == k1) break;
+            if (!(ok = mbar_wait_bounded(&bars->full[st.at], st.full(), abort_flag, __LINE__, lim))) break;
+            tc_fence_after();
+            const uint64_t wd = wdesc0 + st.at * stage16, xd = xdesc0 + st.at * stage16;
+            const int mmas = ks == steps - 1 ? last_mmas : BK / 64;
+#pragma unroll
+            for (int kk = 0; kk < BK / 64; ++kk)
+              if (kk < mmas) {
+                const uint32_t word = h * 2 + (kk >> 1);             // 128 channels' scales a word
+                mma_mxf4<CG>(acc, wd + 2 * kk, xd + 2 * kk, idesc | idesc_scale_byte(2u * (kk & 1)), sw + 4 * word,
+                             sx + xcols * word, more);
+                more = 1;
+              }
+            commit<CG>(&bars->empty[st.at]);
+            st.next(a.stages);
+            ++ks;
           }
+          if (ok) commit<CG>(&bars->tempty[sl.at]);
         }
-        if (ok) commit<CG>(&bars->acc_full[ab]);
+        if (ok) commit<CG>(&bars->acc_full[ac.at]);
       }
       commit<CG>(&bars->mma_done);               // all MMAs complete before TMEM is released
       volatile int no_abort = 0;
@@ -398,13 +420,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t quad = (uint32_t)(warp & 3) * 32u << 16;
     const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32, scale0 = tmem + a.acc_bufs * npad + quad;
     const uint32_t slot_cols = 16u + 4u * a.xcols;
-    uint32_t it = 0;
+    Place rg, sl;
     bool ok = true;
     for (int u = cluster; u < total && ok; u += clusters)
-      for (int c = c0; c < c1; ++c, ++it) {
-        const uint32_t r = it % kRing, slot = it % a.slots, use = it / a.slots;
-        if (!(ok = mbar_wait_bounded(&bars->sfull[r], (it / kRing) & 1, abort_flag, __LINE__, lim))) break;
-        if (use > 0 && !(ok = mbar_wait_bounded(&bars->tempty[slot], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
+      for (int c = c0; c < c1; ++c, rg.next(kRing), sl.next(a.slots)) {
+        const uint32_t r = rg.at, slot = sl.at;
+        if (!(ok = mbar_wait_bounded(&bars->sfull[r], rg.full(), abort_flag, __LINE__, lim))) break;
+        if (!sl.first() && !(ok = mbar_wait_bounded(&bars->tempty[slot], sl.free(), abort_flag, __LINE__, lim))) break;
         __syncwarp();
         tc_fence_after();
         const uint4* src = reinterpret_cast<const uint4*>(ring + r * a.ring_bytes);
@@ -458,12 +480,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------------------------------------------------------- epilogue
     const int quad = warp & 3, half = (warp - kEpiWarp0) >> 2;
     const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32;
-    uint32_t tcount = 0;
+    Place ac;
     int e = 0;
-    for (int u = cluster; u < total; u += clusters, ++tcount) {
+    for (int u = cluster; u < total; u += clusters, ac.next(a.acc_bufs)) {
       const Tile t = tile_at(u, e);
-      const uint32_t ab = tcount % a.acc_bufs;
-      if (!mbar_wait_bounded(&bars->acc_full[ab], (tcount / a.acc_bufs) & 1, abort_flag, __LINE__, lim)) break;
+      const uint32_t ab = ac.at;
+      if (!mbar_wait_bounded(&bars->acc_full[ab], ac.full(), abort_flag, __LINE__, lim)) break;
       __syncwarp();
       tc_fence_after();
       const int row = quad * 32 + lane, o = t.o0 + (CG == 2 ? (int)rank * BM : 0) + row;
