@@ -37,11 +37,14 @@ constexpr int kThreads = 512;
 constexpr int BM = 128;                     // channels per CTA
 constexpr int BK = 256;                     // values per K step (128 bytes a row)
 constexpr int kChunk = 512;                 // values per scale slot (16 bytes a row)
-constexpr int kMaxStages = 8, kMaxSlots = 4, kRing = 4;
+constexpr int kMaxStages = 8, kMaxSlots = 4;
+// Scales come from memory two slots at a time: a copy's cost goes by its rows, not their bytes, and 384 rows of 16 bytes a
+// slot beside 512 of 128 for its codes kept the copy engine from feeding the MMAs.
+constexpr int kRing = 2, kGroup = 2, kScaleRow = 16 * kGroup;
 constexpr int kScaleWarp0 = 4, kScaleWarps = 4, kEpiWarp0 = 8, kEpiWarps = 8;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kStageW = BM * 128;      // 16 KiB of weight codes a stage
-constexpr uint32_t kScalesW = BM * 16;      // 2 KiB of weight scales a ring slot
+constexpr uint32_t kScalesW = BM * kScaleRow;   // 4 KiB of weight scales a ring slot
 // Shared memory: at least half an SM's, as two CTAs would wait for each other's tensor memory.  Clusters take all but
 // 12 KB, whatever they need: a CTA that holds its SM's tensor memory while its cluster waits for another SM's must not
 // share the SM with a CTA of some other kernel of which the same holds (all that use tensor memory need more than 12 KB).
@@ -95,12 +98,20 @@ struct Tile {
 };
 
 // ---- tensor memory and MMA ---------------------------------------------------------------------
-__device__ __forceinline__ void tmem_st2(uint32_t taddr, uint32_t a, uint32_t b) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(taddr), "r"(a), "r"(b) : "memory");
+// N consecutive columns of this warp's 32 lanes
+template <int N>
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t* v);
+template <>
+__device__ __forceinline__ void tmem_st<8>(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
-__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d)
-               : "memory");
+template <>
+__device__ __forceinline__ void tmem_st<16>(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+template <>
+__device__ __forceinline__ void tmem_st<32>(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -109,6 +120,11 @@ __device__ __forceinline__ uint32_t idesc_mxf4(int M, int N) {
   return (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27);
 }
 // which byte of a scale column's word an MMA's first scale is in (0 or 2), of A and of B
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{ .reg .pred q; elect.sync _|q, 0xFFFFFFFF; selp.u32 %0, 1, 0, q; }" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ uint32_t idesc_scale_byte(uint32_t id) { return (id << 4) | (id << 29); }
 
 template <int CG>
@@ -135,6 +151,40 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
     mma_commit(bar);
 }
 
+// Scales of 32 R rows, row 32 j + lane at src[32 kGroup j], to w[R i + j] = the word of blocks 4 i .. 4 i + 3; bytes from
+// `have` on are zero.
+template <int R>
+__device__ __forceinline__ void load_scales(const uint4* src, int have, uint32_t* w) {
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const uint4 v = src[32 * kGroup * j];
+    w[j] = v.x;
+    w[R + j] = v.y;
+    w[2 * R + j] = v.z;
+    w[3 * R + j] = v.w;
+  }
+  if (have < 16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int left = have - 4 * i;
+      const uint32_t mask = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+      for (int j = 0; j < R; ++j) w[R * i + j] &= mask;
+    }
+  }
+}
+template <int R>
+__device__ __forceinline__ void store_scales(const uint4* src, int have, uint32_t taddr) {
+  uint32_t w[4 * R];
+  load_scales<R>(src, have, w);
+  if constexpr (R == 6) {
+    tmem_st<16>(taddr, w);
+    tmem_st<8>(taddr + 16, w + 16);
+  } else {
+    tmem_st<4 * R>(taddr, w);
+  }
+}
+
 // a float32 into CTA `rank`'s shared memory at this address's offset
 __device__ __forceinline__ void st_cluster(float* p, uint32_t rank, float v) {
   uint32_t remote;
@@ -148,6 +198,12 @@ template <>
 __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Two float32 bit patterns to bf16, the first in the low half.
+__device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 
 // Grouped: one warp fills the table: rows[e], the first row of expert e (rows[experts]: one past the last), and
 // tiles[e], the tiles of the experts before it.  Offsets are taken in order and within [0, m], whatever they are.
@@ -192,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                    const __grid_constant__ MxArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* ring = smem + a.off_ring;            // kRing x [weights' scales 128 x 16 B | tokens' scales]
+  uint8_t* ring = smem + a.off_ring;            // kRing x [weights' scales 128 x 32 B | tokens' scales]
   float* red = reinterpret_cast<float*>(smem + a.off_red);   // split: [part][token of this CTA's][128 channels]
   int* rows = reinterpret_cast<int*>(smem + a.off_table);    // grouped: see make_table
   int* tiles = rows + a.experts + 1;
@@ -200,7 +256,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* abort_flag = &bars->abort;
   T* y = static_cast<T*>(a.y);
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);   // (known to be the same in all lanes)
   const uint32_t rank = cluster_rank();
   const int csize = CG == 2 ? 2 : a.split;       // CTAs of a cluster
   const int cluster = blockIdx.x / csize, clusters = gridDim.x / csize;
@@ -246,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   cluster_sync();                                // barriers, table and TMEM address are there, in the whole cluster
   tc_fence_after();
-  const uint32_t tmem = bars->tmem_addr;
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, bars->tmem_addr, 0);
   const int token_tiles = (a.m + a.nt - 1) / a.nt;
   const int total = a.offsets ? bars->total : token_tiles * channel_tiles;
 
@@ -327,15 +384,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Tile t = tile_at(u, e);
         const int wrow = t.w_row + t.o0 + (int)(CG == 2 ? rank : 0) * BM;
         const int boxes = (t.n + a.bxs - 1) / a.bxs;
-        const uint32_t bytes = kScalesW + (uint32_t)(boxes * a.bxs) * 16u;
-        for (int c = c0; c < c1; ++c, ++it) {
+        const uint32_t bytes = kScalesW + (uint32_t)(boxes * a.bxs * kScaleRow);
+        for (int c = c0; c < c1; c += kGroup, ++it) {
           const uint32_t s = it % kRing, use = it / kRing;
           if (use > 0 && !(ok = mbar_wait_bounded(&bars->sempty[s], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
           uint8_t* dst = ring + s * a.ring_bytes;
           mbar_arrive_expect_tx(&bars->sfull[s], bytes);
           tma_load_2d(dst, &tmWs, c * 16, wrow, &bars->sfull[s]);
           for (int b = 0; b < boxes; ++b)
-            tma_load_2d(dst + kScalesW + (uint32_t)(b * a.bxs) * 16u, &tmXs, c * 16, t.t0 + b * a.bxs, &bars->sfull[s]);
+            tma_load_2d(dst + kScalesW + (uint32_t)(b * a.bxs * kScaleRow), &tmXs, c * 16, t.t0 + b * a.bxs, &bars->sfull[s]);
         }
       }
       volatile int no_abort = 0;
@@ -367,49 +424,56 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
-    // The tensor cores wait for this thread wherever its instructions between two MMAs take longer than one, so all that
-    // it needs is worked out ahead and counted on, not divided.
-    if (lane == 0) {
-      const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32, scale0 = tmem + a.acc_bufs * npad;
-      const uint32_t slot_cols = 16u + 4u * a.xcols, xcols = a.xcols;
-      const uint64_t wdesc0 = sdesc_kmajor_sw128(smem_u32(smem)), xdesc0 = sdesc_kmajor_sw128(smem_u32(smem) + kStageW);
-      const uint32_t stage16 = a.stage_bytes >> 4;
-      const int last_mmas = (a.d - (steps - 1) * BK + 63) / 64;      // of the row's last K step
-      Place st, sl, ac;
-      bool ok = true;
-      int e = 0;
-      for (int u = cluster; u < total && ok; u += clusters, ac.next(a.acc_bufs)) {
-        const Tile t = tile_at(u, e);
-        const uint32_t acc = tmem + ac.at * npad, idesc = idesc_mxf4(CG * BM, t.n);
-        if (!ac.first() && !(ok = mbar_wait_bounded(&bars->acc_empty[ac.at], ac.free(), abort_flag, __LINE__, lim))) break;
-        uint32_t more = 0;                         // accumulate (0: the tile's first MMA)
-        for (int ks = k0; ks < k1 && ok; sl.next(a.slots)) {
-          if (!(ok = mbar_wait_bounded(&bars->tfull[sl.at], sl.full(), abort_flag, __LINE__, lim))) break;
-          const uint32_t sw = scale0 + sl.at * slot_cols, sx = sw + 16;
+    // The tensor cores wait for this warp wherever its instructions between two MMAs take longer than one.  So all lanes
+    // go through the loop (what the MMAs need stays in uniform registers) and one is elected to issue, places are counted,
+    // not divided, and a K step always has its four MMAs: behind the row's end the codes are zeros and the scales finite.
+    const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32, scale0 = tmem + a.acc_bufs * npad;
+    const uint32_t slot_cols = 16u + 4u * a.xcols, xcols = a.xcols;
+    const uint64_t wdesc0 = sdesc_kmajor_sw128(smem_u32(smem)), xdesc0 = sdesc_kmajor_sw128(smem_u32(smem) + kStageW);
+    const uint32_t stage16 = a.stage_bytes >> 4;
+    auto wait = [&](uint64_t* bar, uint32_t parity, int line) {
+      return (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort_flag, line, lim));
+    };
+    Place st, sl, ac;
+    bool ok = true;
+    int e = 0;
+    for (int u = cluster; u < total && ok; u += clusters, ac.next(a.acc_bufs)) {
+      const Tile t = tile_at(u, e);
+      const uint32_t acc = tmem + ac.at * npad, idesc = idesc_mxf4(CG * BM, t.n);
+      if (!ac.first() && !(ok = wait(&bars->acc_empty[ac.at], ac.free(), __LINE__))) break;
+      uint32_t more = 0;                           // accumulate (0: the tile's first MMA)
+      for (int ks = k0; ks < k1 && ok; sl.next(a.slots)) {
+        if (!(ok = wait(&bars->tfull[sl.at], sl.full(), __LINE__))) break;
+        const uint32_t sw = scale0 + sl.at * slot_cols, sx = sw + 16;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {            // the slot's two K steps
-            if (h == 1 && ks == k1) break;
-            if (!(ok = mbar_wait_bounded(&bars->full[st.at], st.full(), abort_flag, __LINE__, lim))) break;
-            tc_fence_after();
+        for (int h = 0; h < 2; ++h) {              // the slot's two K steps
+          if (h == 1 && ks == k1) break;
+          if (!(ok = wait(&bars->full[st.at], st.full(), __LINE__))) break;
+          tc_fence_after();
+          if (elect_one()) {
             const uint64_t wd = wdesc0 + st.at * stage16, xd = xdesc0 + st.at * stage16;
-            const int mmas = ks == steps - 1 ? last_mmas : BK / 64;
 #pragma unroll
-            for (int kk = 0; kk < BK / 64; ++kk)
-              if (kk < mmas) {
-                const uint32_t word = h * 2 + (kk >> 1);             // 128 channels' scales a word
-                mma_mxf4<CG>(acc, wd + 2 * kk, xd + 2 * kk, idesc | idesc_scale_byte(2u * (kk & 1)), sw + 4 * word,
-                             sx + xcols * word, more);
-                more = 1;
-              }
+            for (int kk = 0; kk < BK / 64; ++kk) {
+              const uint32_t word = h * 2 + (kk >> 1);               // 128 channels' scales a word
+              mma_mxf4<CG>(acc, wd + 2 * kk, xd + 2 * kk, idesc | idesc_scale_byte(2u * (kk & 1)), sw + 4 * word,
+                           sx + xcols * word, kk ? 1u : more);
+            }
             commit<CG>(&bars->empty[st.at]);
-            st.next(a.stages);
-            ++ks;
           }
-          if (ok) commit<CG>(&bars->tempty[sl.at]);
+          __syncwarp();
+          more = 1;
+          st.next(a.stages);
+          ++ks;
         }
-        if (ok) commit<CG>(&bars->acc_full[ac.at]);
+        if (ok && elect_one()) commit<CG>(&bars->tempty[sl.at]);
+        __syncwarp();
       }
-      commit<CG>(&bars->mma_done);               // all MMAs complete before TMEM is released
+      if (ok && elect_one()) commit<CG>(&bars->acc_full[ac.at]);
+      __syncwarp();
+    }
+    if (elect_one()) commit<CG>(&bars->mma_done);  // all MMAs complete before TMEM is released
+    __syncwarp();
+    if (lane == 0) {
       volatile int no_abort = 0;
       mbar_wait_bounded(&bars->mma_done, 0, &no_abort);
     }
@@ -423,51 +487,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     Place rg, sl;
     bool ok = true;
     for (int u = cluster; u < total && ok; u += clusters)
-      for (int c = c0; c < c1; ++c, rg.next(kRing), sl.next(a.slots)) {
+      for (int c = c0; c < c1; ++c, sl.next(a.slots)) {
+        const int g = (c - c0) % kGroup;           // which slot of its group's copy
         const uint32_t r = rg.at, slot = sl.at;
-        if (!(ok = mbar_wait_bounded(&bars->sfull[r], rg.full(), abort_flag, __LINE__, lim))) break;
+        if (g == 0 && !(ok = mbar_wait_bounded(&bars->sfull[r], rg.full(), abort_flag, __LINE__, lim))) break;
         if (!sl.first() && !(ok = mbar_wait_bounded(&bars->tempty[slot], sl.free(), abort_flag, __LINE__, lim))) break;
         __syncwarp();
         tc_fence_after();
-        const uint4* src = reinterpret_cast<const uint4*>(ring + r * a.ring_bytes);
+        // row q of the group's scales: kGroup times 16 bytes
+        const uint4* src = reinterpret_cast<const uint4*>(ring + r * a.ring_bytes) + g;
         const uint32_t dst = scale0 + slot * slot_cols;
-        // the last chunk's bytes behind the row's scales: an MMA that covers them multiplies zero codes, so any finite
+        // the last chunk's bytes behind the row's scales: the MMAs that cover them multiply zero codes, so any finite
         // scale will do
         const int have = a.d / 32 - c * 16;
-        auto masked = [&](uint4 v) {
-          if (have < 16) {
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int left = have - 4 * i;
-              w[i] = left >= 4 ? w[i] : left <= 0 ? 0u : w[i] & ((1u << (8 * left)) - 1u);
-            }
-            v = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-          return v;
-        };
-        {
-          uint4 v[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = masked(src[32 * j + lane]);
-          tmem_st4(dst, v[0].x, v[1].x, v[2].x, v[3].x);
-          tmem_st4(dst + 4, v[0].y, v[1].y, v[2].y, v[3].y);
-          tmem_st4(dst + 8, v[0].z, v[1].z, v[2].z, v[3].z);
-          tmem_st4(dst + 12, v[0].w, v[1].w, v[2].w, v[3].w);
+        uint32_t w[16];
+        load_scales<4>(src + kGroup * lane, have, w);
+        switch (a.xcols) {                         // 64 tokens a step
+          case 2: store_scales<2>(src + kGroup * (BM + lane), have, dst + 16); break;
+          case 4: store_scales<4>(src + kGroup * (BM + lane), have, dst + 16); break;
+          case 6: store_scales<6>(src + kGroup * (BM + lane), have, dst + 16); break;
+          default: store_scales<8>(src + kGroup * (BM + lane), have, dst + 16); break;
         }
-        for (int p = 0; p < a.xcols; p += 2) {    // 64 tokens at a time
-          const uint4 v0 = masked(src[BM + 32 * p + lane]), v1 = masked(src[BM + 32 * p + 32 + lane]);
-          const uint32_t x = dst + 16 + p;
-          tmem_st2(x, v0.x, v1.x);
-          tmem_st2(x + a.xcols, v0.y, v1.y);
-          tmem_st2(x + 2 * a.xcols, v0.z, v1.z);
-          tmem_st2(x + 3 * a.xcols, v0.w, v1.w);
-        }
+        tmem_st<16>(dst, w);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
+        const bool last = g == kGroup - 1 || c == c1 - 1;
+        if (last) rg.next(kRing);
         if (lane == 0) {
-          mbar_arrive(&bars->sempty[r]);
+          if (last) mbar_arrive(&bars->sempty[r]);
           if (CG == 2 && rank == 1)
             mbar_arrive(&bars->tready[slot]);
           else if (CG == 2 && warp == kScaleWarp0)
@@ -484,19 +532,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     int e = 0;
     for (int u = cluster; u < total; u += clusters, ac.next(a.acc_bufs)) {
       const Tile t = tile_at(u, e);
-      const uint32_t ab = ac.at;
-      if (!mbar_wait_bounded(&bars->acc_full[ab], ac.full(), abort_flag, __LINE__, lim)) break;
+      if (!mbar_wait_bounded(&bars->acc_full[ac.at], ac.full(), abort_flag, __LINE__, lim)) break;
       __syncwarp();
       tc_fence_after();
       const int row = quad * 32 + lane, o = t.o0 + (CG == 2 ? (int)rank * BM : 0) + row;
-      for (int c = half; c * 32 < t.valid; c += 2) {
-        uint32_t r[32];
-        __syncwarp();
-        CAT_TMEM_LD32(tmem + ((uint32_t)(quad * 32) << 16) + ab * npad + c * 32, r);
-        tmem_ld_wait();
-        if (CG == 1 && a.split > 1) {
-          // token t of the tile is summed by CTA t mod split, its t / split-th
-          const int each = (a.nt + a.split - 1) / a.split;
+      const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + ac.at * npad;
+      if (CG == 1 && a.split > 1) {
+        // this CTA's part of K: token k of the tile is summed by CTA k mod split, its k / split-th
+        const int each = (a.nt + a.split - 1) / a.split;
+        for (int c = half; c * 32 < t.valid; c += 2) {
+          uint32_t r[32];
+          __syncwarp();
+          CAT_TMEM_LD32(acc + c * 32, r);
+          tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const int tok = c * 32 + i;
@@ -504,20 +552,72 @@ __global__ void __launch_bounds__(kThreads, 1)
               st_cluster(red + ((size_t)rank * each + tok / a.split) * BM + row, (uint32_t)(tok % a.split),
                          __uint_as_float(r[i]));
           }
-        } else if (o < a.d_out) {
-          T* p = y + (size_t)(t.t0 + c * 32) * a.d_out + o;
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c * 32 + i < t.valid) p[(size_t)i * a.d_out] = to_out<T>(__uint_as_float(r[i]));
         }
+        break;                                     // (a split tile is its cluster's only one)
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (CG == 2)
-          mbar_arrive_cluster(&bars->acc_empty[ab], 0);
-        else
-          mbar_arrive(&bars->acc_empty[ab]);
+      // The accumulator is read to registers and given back before anything is stored (bf16: all of this warp's part
+      // at once; float32: half of it), so the next tile's MMAs wait for the reads alone.
+      constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;
+      bool held = true;
+#pragma unroll 1
+      for (int c0_ = half; held; c0_ += 2 * kAtOnce) {
+        uint32_t r[kAtOnce][32 * sizeof(T) / 4];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const int c = c0_ + 2 * k;
+          if (c * 32 < t.valid) {
+            uint32_t v[32];
+            __syncwarp();
+            CAT_TMEM_LD32(acc + c * 32, v);
+            tmem_ld_wait();
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) r[k][i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[k][i] = v[i];
+            }
+          }
+        }
+        held = (c0_ + 2 * kAtOnce) * 32 < t.valid;
+        if (!held) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (CG == 2)
+              mbar_arrive_cluster(&bars->acc_empty[ac.at], 0);
+            else
+              mbar_arrive(&bars->acc_empty[ac.at]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const int c = c0_ + 2 * k, left = t.valid - c * 32;     // tokens of this chunk on
+          if (left > 0) {
+            T* p = y + (size_t)(t.t0 + c * 32) * a.d_out;
+            if constexpr (sizeof(T) == 2) {
+              if ((a.d_out & 1) == 0) {
+                // lanes 2j and 2j + 1 have two tokens of a channel each; they trade, for two channels of a token each
+                const int tok = lane & 1;
+                T* q = p + (size_t)tok * a.d_out + (o & ~1);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  const uint32_t mine = r[k][i], other = __shfl_xor_sync(0xFFFFFFFFu, mine, 1);
+                  const uint32_t both = tok ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
+                  if (o < a.d_out && 2 * i + tok < left) *reinterpret_cast<uint32_t*>(q + (size_t)(2 * i) * a.d_out) = both;
+                }
+              } else if (o < a.d_out) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (i < left) p[(size_t)i * a.d_out + o] = __ushort_as_bfloat16((unsigned short)(r[k][i / 2] >> (16 * (i & 1))));
+              }
+            } else if (o < a.d_out) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (i < left) p[(size_t)i * a.d_out + o] = __uint_as_float(r[k][i]);
+            }
+          }
+        }
       }
     }
   }
@@ -618,7 +718,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   const int slots = ((int)kTmemCols - a.acc_bufs * npad) / slot_cols;
   a.slots = slots < kMaxSlots ? slots : kMaxSlots;
   a.stage_bytes = kStageW + (uint32_t)up(nt / CG, a.bx) * 128u;
-  a.ring_bytes = kScalesW + (uint32_t)up(up(nt, a.bxs), 64) * 16u;
+  a.ring_bytes = kScalesW + (uint32_t)up(up(nt, a.bxs), 64) * kScaleRow;
   const size_t red = split > 1 ? (size_t)split * ((nt + split - 1) / split) * BM * 4 : 0;
   const size_t table = c.offsets ? up(2 * (c.experts + 1) * 4, 128) : 0;
   const size_t rest = (size_t)kRing * a.ring_bytes + red + table + sizeof(Bars) + 1024;
@@ -636,7 +736,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   CUtensorMap tw, tx, tws, txs;
   const int64_t pitch = mx_pitch(c.d), wrows = (c.offsets ? c.experts : 1) * c.d_out;
   if (!make_map(&tw, c.wq, wrows, c.d / 2, BM, 128) || !make_map(&tx, c.xq, c.m, c.d / 2, a.bx, 128) ||
-      !make_map(&tws, c.ws, wrows, pitch, BM, 16) || !make_map(&txs, c.xs, c.m, pitch, a.bxs, 16))
+      !make_map(&tws, c.ws, wrows, pitch, BM, kScaleRow) || !make_map(&txs, c.xs, c.m, pitch, a.bxs, kScaleRow))
     return cudaErrorInvalidValue;
   static PerDevice<cudaError_t> allowed;
   const cudaError_t attr_err = allowed.get([] { return allow_smem(mx_gemm_kernel<CG, T>, kMaxSmem); });
@@ -673,8 +773,8 @@ cudaError_t launch_typed(const Call& c) {
   const int64_t rows = (c.m + busy - 1) / busy;                               // rows of a group, on average
   const bool pair = rows > 128;
   if (pair) {
-    const int64_t tiles = (rows + 191) / 192;
-    const int nt = c.offsets ? 192 : (int)up((c.m + tiles - 1) / tiles, 16);
+    const int64_t tiles = (rows + 255) / 256;
+    const int nt = c.offsets ? 256 : (int)up((c.m + tiles - 1) / tiles, 16);
     return launch_form<2, T>(c, nt, 1);
   }
   // one CTA a tile; K over the CTAs of a cluster where tiles leave SMs idle
