@@ -44,6 +44,7 @@ constexpr int kRing = 2, kGroup = 2, kScaleRow = 16 * kGroup;
 constexpr int kScaleWarp0 = 4, kScaleWarps = 4, kEpiWarp0 = 8, kEpiWarps = 8;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kStageW = BM * 128;      // 16 KiB of weight codes a stage
+constexpr uint32_t kStageOut = 8192;        // an epilogue half's outputs on their way: 32 bf16 or 16 float32 tokens
 constexpr uint32_t kScalesW = BM * kScaleRow;   // 4 KiB of weight scales a ring slot
 // Shared memory: at least half an SM's, as two CTAs would wait for each other's tensor memory.  Clusters take all but
 // 12 KB, whatever they need: a CTA that holds its SM's tensor memory while its cluster waits for another SM's must not
@@ -62,7 +63,7 @@ struct MxArgs {
   int stages, acc_bufs, slots, xcols;       // xcols: TMEM columns of the tokens' scales per 128 channels
   int split;                                // CTAs that share a tile's K (CG = 1)
   uint32_t stage_bytes, ring_bytes;
-  uint32_t off_ring, off_red, off_table, off_bars;
+  uint32_t off_ring, off_out, off_red, off_table, off_bars;
 };
 
 struct Bars {
@@ -70,7 +71,7 @@ struct Bars {
   uint64_t sfull[kRing], sempty[kRing];                       // scales in shared memory
   uint64_t tfull[kMaxSlots], tready[kMaxSlots], tempty[kMaxSlots];   // scales in tensor memory
   uint64_t acc_full[2], acc_empty[2], mma_done;
-  uint32_t fwd_stage[kMaxStages], fwd_slot[kMaxSlots];        // even CTA: targets of the odd CTA's st.async
+  uint32_t fwd_stage[kMaxStages], fwd_slot[kMaxSlots], fwd_acc[kEpiWarps];   // even CTA: targets of the odd CTA's st.async
   uint32_t tmem_addr;
   int abort;
   int total;                                                  // grouped: tiles of the launch
@@ -199,6 +200,29 @@ __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// The four warps of an epilogue half, in step.
+__device__ __forceinline__ void epi_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory"); }
+
+__device__ __forceinline__ bool epi_all(int half, bool ok) {
+  uint32_t all;
+  asm volatile(
+      "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; bar.red.and.pred q, %2, 128, p; selp.u32 %0, 1, 0, q; }"
+      : "=r"(all)
+      : "r"((uint32_t)ok), "r"(1 + half)
+      : "memory");
+  return all != 0;
+}
+
+// Value i of a thread's 32: bf16 two to a word, float32 one.
+template <typename T>
+__device__ __forceinline__ T element(const uint32_t* r, int i);
+template <>
+__device__ __forceinline__ float element<float>(const uint32_t* r, int i) { return __uint_as_float(r[i]); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 element<__nv_bfloat16>(const uint32_t* r, int i) {
+  return __ushort_as_bfloat16((unsigned short)(r[i / 2] >> (16 * (i & 1))));
+}
+
 // Two float32 bit patterns to bf16, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
@@ -284,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->acc_full[b], 1);
-      mbar_init(&bars->acc_empty[b], CG * kEpiWarps);
+      mbar_init(&bars->acc_empty[b], kEpiWarps);   // (CG = 2, even CTA: + 4 bytes from each of the odd CTA's warps)
     }
     mbar_init(&bars->mma_done, 1);
     bars->abort = 0;
@@ -476,6 +500,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       volatile int no_abort = 0;
       mbar_wait_bounded(&bars->mma_done, 0, &no_abort);
+      // the odd CTA's last signals have landed before this CTA exits
+      for (uint32_t b = 0; CG == 2 && b < (uint32_t)a.acc_bufs; ++b) {
+        const uint32_t uses = ac.round + (b < ac.at ? 1u : 0u);
+        if (uses > 0) mbar_wait_bounded(&bars->acc_empty[b], (uses - 1) & 1, &no_abort);
+      }
     }
   } else if (warp >= kScaleWarp0 && warp < kScaleWarp0 + kScaleWarps) {
     // ---------------------------------------------------------------- scales to tensor memory
@@ -528,14 +557,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------------------------------------------------------- epilogue
     const int quad = warp & 3, half = (warp - kEpiWarp0) >> 2;
     const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32;
+    constexpr int kVec = 16 / sizeof(T), kStaged = kStageOut / (BM * sizeof(T));   // values of a store, tokens staged at once
+    T* stage = reinterpret_cast<T*>(smem + a.off_out) + half * (kStageOut / sizeof(T));
+    const bool whole = a.d_out % kVec == 0;        // 16 bytes are wholly in or out of a row
     Place ac;
     int e = 0;
     for (int u = cluster; u < total; u += clusters, ac.next(a.acc_bufs)) {
       const Tile t = tile_at(u, e);
-      if (!mbar_wait_bounded(&bars->acc_full[ac.at], ac.full(), abort_flag, __LINE__, lim)) break;
-      __syncwarp();
+      // (the half's warps go on or give up together: they meet at barriers below)
+      if (!epi_all(half, mbar_wait_bounded(&bars->acc_full[ac.at], ac.full(), abort_flag, __LINE__, lim))) break;
       tc_fence_after();
-      const int row = quad * 32 + lane, o = t.o0 + (CG == 2 ? (int)rank * BM : 0) + row;
+      const int row = quad * 32 + lane, o_first = t.o0 + (CG == 2 ? (int)rank * BM : 0);
       const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + ac.at * npad;
       if (CG == 1 && a.split > 1) {
         // this CTA's part of K: token k of the tile is summed by CTA k mod split, its k / split-th
@@ -583,9 +615,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!held) {
           tc_fence_before();
           __syncwarp();
+          // (an arrive on the even CTA's barrier would wait for this warp's stores of the tile before, ~2000 cycles)
           if (lane == 0) {
-            if (CG == 2)
-              mbar_arrive_cluster(&bars->acc_empty[ac.at], 0);
+            if (CG == 2 && rank == 1)
+              st_async_signal(&bars->fwd_acc[warp - kEpiWarp0], &bars->acc_empty[ac.at], 0);
+            else if (CG == 2 && warp == kEpiWarp0)
+              mbar_arrive_expect_tx(&bars->acc_empty[ac.at], 4u * kEpiWarps);
             else
               mbar_arrive(&bars->acc_empty[ac.at]);
           }
@@ -593,29 +628,30 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
           const int c = c0_ + 2 * k, left = t.valid - c * 32;     // tokens of this chunk on
-          if (left > 0) {
-            T* p = y + (size_t)(t.t0 + c * 32) * a.d_out;
-            if constexpr (sizeof(T) == 2) {
-              if ((a.d_out & 1) == 0) {
-                // lanes 2j and 2j + 1 have two tokens of a channel each; they trade, for two channels of a token each
-                const int tok = lane & 1;
-                T* q = p + (size_t)tok * a.d_out + (o & ~1);
+          if (left <= 0) break;
+          T* p = y + (size_t)(t.t0 + c * 32) * a.d_out;
+          if (whole) {
+            // through shared memory: [token][128 channels], then 16 bytes a lane, a token's channels by 128 / kVec lanes
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  const uint32_t mine = r[k][i], other = __shfl_xor_sync(0xFFFFFFFFu, mine, 1);
-                  const uint32_t both = tok ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
-                  if (o < a.d_out && 2 * i + tok < left) *reinterpret_cast<uint32_t*>(q + (size_t)(2 * i) * a.d_out) = both;
-                }
-              } else if (o < a.d_out) {
+            for (int i0 = 0; i0 < 32; i0 += kStaged) {
+              epi_sync(half);                      // the buffer has been read
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (i < left) p[(size_t)i * a.d_out + o] = __ushort_as_bfloat16((unsigned short)(r[k][i / 2] >> (16 * (i & 1))));
+              for (int i = 0; i < kStaged; ++i) stage[i * BM + row] = element<T>(r[k], i0 + i);
+              epi_sync(half);
+              constexpr int kLanes = BM / kVec, kRows = 128 / kLanes;
+              const int v = (tid & 127) % kLanes * kVec, o = o_first + v;
+#pragma unroll
+              for (int i = 0; i < kStaged; i += kRows) {
+                const int tok = i + (tid & 127) / kLanes;
+                if (i0 + tok < left && o < a.d_out)
+                  *reinterpret_cast<uint4*>(p + (size_t)(i0 + tok) * a.d_out + o) =
+                      *reinterpret_cast<const uint4*>(stage + tok * BM + v);
               }
-            } else if (o < a.d_out) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (i < left) p[(size_t)i * a.d_out + o] = __uint_as_float(r[k][i]);
             }
+          } else if (o_first + row < a.d_out) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i < left) p[(size_t)i * a.d_out + o_first + row] = element<T>(r[k], i);
           }
         }
       }
@@ -721,12 +757,13 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   a.ring_bytes = kScalesW + (uint32_t)up(up(nt, a.bxs), 64) * kScaleRow;
   const size_t red = split > 1 ? (size_t)split * ((nt + split - 1) / split) * BM * 4 : 0;
   const size_t table = c.offsets ? up(2 * (c.experts + 1) * 4, 128) : 0;
-  const size_t rest = (size_t)kRing * a.ring_bytes + red + table + sizeof(Bars) + 1024;
+  const size_t rest = (size_t)kRing * a.ring_bytes + 2 * kStageOut + red + table + sizeof(Bars) + 1024;
   const int stages = (int)((kMaxSmem - rest) / a.stage_bytes);
   a.stages = stages < kMaxStages ? stages : kMaxStages;
   if (a.slots < 2 || a.stages < 2 || nt % (8 * CG) != 0 || a.bx > 256 || a.bxs > 256) return cudaErrorInvalidConfiguration;
   a.off_ring = a.stages * a.stage_bytes;
-  a.off_red = a.off_ring + kRing * a.ring_bytes;
+  a.off_out = a.off_ring + kRing * a.ring_bytes;
+  a.off_red = a.off_out + 2 * kStageOut;
   a.off_table = a.off_red + (uint32_t)red;
   a.off_bars = a.off_table + (uint32_t)table;
   size_t smem = a.off_bars + sizeof(Bars) + 1024;
