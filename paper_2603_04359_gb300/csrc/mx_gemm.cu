@@ -61,7 +61,7 @@ struct MxArgs {
   int nt;                                   // most tokens of a tile
   int bx, bxs;                              // token rows per TMA box: codes, scales
   int stages, acc_bufs, slots, xcols;       // xcols: TMEM columns of the tokens' scales per 128 channels
-  int split;                                // CTAs that share a tile's K (CG = 1)
+  int split, split_log;                     // CTAs that share a tile's K (CG = 1), a power of two up to 8, and its logarithm
   uint32_t stage_bytes, ring_bytes;
   uint32_t off_ring, off_out, off_red, off_table, off_bars;
 };
@@ -186,6 +186,10 @@ __device__ __forceinline__ void store_scales(const uint4* src, int have, uint32_
   }
 }
 
+// A cluster barrier in two parts, which orders no memory.
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 // a float32 into CTA `rank`'s shared memory at this address's offset
 __device__ __forceinline__ void st_cluster(float* p, uint32_t rank, float v) {
   uint32_t remote;
@@ -291,6 +295,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int c0 = CG == 2 ? 0 : (int)rank * chunks / a.split, c1 = CG == 2 ? chunks : ((int)rank + 1) * chunks / a.split;
   const int k0 = 2 * c0, k1 = min(2 * c1, steps);
 
+  if (warp == 2 && lane == 0) {                  // (parameters: no need to wait for the kernel before)
+    prefetch_tensormap(&tmW);
+    prefetch_tensormap(&tmX);
+    prefetch_tensormap(&tmWs);
+    prefetch_tensormap(&tmXs);
+  }
   if (tid == 0) {
     for (int s = 0; s < a.stages; ++s) {
       mbar_init(&bars->full[s], 1);
@@ -325,7 +335,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       tmem_alloc(&bars->tmem_addr, kTmemCols);
   }
   tc_fence_before();
-  cluster_sync();                                // barriers, table and TMEM address are there, in the whole cluster
+  if constexpr (CG == 2) {
+    cluster_sync();                              // barriers, table and TMEM address are there, in the whole cluster
+  } else {
+    __syncthreads();
+    cluster_arrive_relaxed();                    // (a split's other CTAs have to be there only when parts are sent)
+  }
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, bars->tmem_addr, 0);
   const int token_tiles = (a.m + a.nt - 1) / a.nt;
@@ -347,15 +362,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (u >= tiles[e + 1]) ++e;
       begin = rows[e];
       end = rows[e + 1];
-      n_tiles = (end - begin + a.nt - 1) / a.nt;
-      tt = (u - tiles[e]) % n_tiles;
-      ct = (u - tiles[e]) / n_tiles;
-    } else {
-      tile_coords(u, token_tiles, channel_tiles, &tt, &ct);
+      u -= tiles[e];
+      if (end - begin > a.nt) n_tiles = (end - begin + a.nt - 1) / a.nt;
+      else n_tiles = 1;
     }
     // tiles of equal size, as few as there must be
     constexpr int kUnit = 8 * CG;
-    const int size = ((end - begin + n_tiles - 1) / n_tiles + kUnit - 1) / kUnit * kUnit;
+    int size = end - begin;
+    tt = 0;
+    ct = u;
+    if (n_tiles > 1) {
+      size = (size + n_tiles - 1) / n_tiles;
+      if (a.offsets) {
+        ct = u / n_tiles;
+        tt = u - ct * n_tiles;
+      } else {
+        tile_coords(u, token_tiles, channel_tiles, &tt, &ct);
+      }
+    }
+    size = (size + kUnit - 1) / kUnit * kUnit;
     t.w_row = e * a.d_out;
     t.o0 = ct * CG * BM;
     t.t0 = begin + tt * size;
@@ -367,8 +392,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA of codes
     if (lane == 0) {
-      prefetch_tensormap(&tmW);
-      prefetch_tensormap(&tmX);
       uint32_t it = 0;
       Place st;
       bool ok = true;
@@ -399,8 +422,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 2) {
     // ---------------------------------------------------------------- TMA of scales
     if (lane == 0) {
-      prefetch_tensormap(&tmWs);
-      prefetch_tensormap(&tmXs);
       uint32_t it = 0;
       bool ok = true;
       int e = 0;
@@ -560,6 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr int kVec = 16 / sizeof(T), kStaged = kStageOut / (BM * sizeof(T));   // values of a store, tokens staged at once
     T* stage = reinterpret_cast<T*>(smem + a.off_out) + half * (kStageOut / sizeof(T));
     const bool whole = a.d_out % kVec == 0;        // 16 bytes are wholly in or out of a row
+    if (CG == 1) cluster_wait();                   // a split's CTAs have all started
     Place ac;
     int e = 0;
     for (int u = cluster; u < total; u += clusters, ac.next(a.acc_bufs)) {
@@ -571,19 +593,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + ac.at * npad;
       if (CG == 1 && a.split > 1) {
         // this CTA's part of K: token k of the tile is summed by CTA k mod split, its k / split-th
-        const int each = (a.nt + a.split - 1) / a.split;
+        const int each = (a.nt + a.split - 1) >> a.split_log;
         for (int c = half; c * 32 < t.valid; c += 2) {
           uint32_t r[32];
           __syncwarp();
           CAT_TMEM_LD32(acc + c * 32, r);
           tmem_ld_wait();
+          float* part = red + ((size_t)rank * each + ((c * 32) >> a.split_log)) * BM + row;   // (split divides 32)
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const int tok = c * 32 + i;
-            if (tok < t.valid)
-              st_cluster(red + ((size_t)rank * each + tok / a.split) * BM + row, (uint32_t)(tok % a.split),
-                         __uint_as_float(r[i]));
-          }
+          for (int i = 0; i < 32; ++i)
+            if (c * 32 + i < t.valid)
+              st_cluster(part + (i >> a.split_log) * BM, (uint32_t)i & (a.split - 1), __uint_as_float(r[i]));
         }
         break;                                     // (a split tile is its cluster's only one)
       }
@@ -660,15 +680,24 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   __syncwarp();
   tc_fence_before();
-  cluster_sync();                                // MMAs and epilogues are done with TMEM; a split's parts have arrived
+  if (CG == 1 && warp < kEpiWarp0) cluster_wait();   // (the epilogue has)
+  // MMAs and epilogues are done with TMEM; a split's parts have arrived
+  if (CG == 1 && a.split > 1) {
+    cluster_sync();
+  } else if (CG == 2) {
+    cluster_arrive_relaxed();                    // (a releasing one would wait for all stores)
+    cluster_wait();
+  } else {
+    __syncthreads();
+  }
   if (CG == 1 && a.split > 1 && cluster < total && !bars->abort) {
     int e = 0;
     const Tile t = tile_at(cluster, e);
-    const int each = (a.nt + a.split - 1) / a.split, o = t.o0 + (tid & (BM - 1));
-    for (int j = tid / BM; j * a.split + (int)rank < t.valid; j += kThreads / BM) {
+    const int each = (a.nt + a.split - 1) >> a.split_log, o = t.o0 + (tid & (BM - 1));
+    for (int j = tid / BM; (j << a.split_log) + (int)rank < t.valid; j += kThreads / BM) {
       float sum = 0.f;
       for (int p = 0; p < a.split; ++p) sum += red[((size_t)p * each + j) * BM + (tid & (BM - 1))];
-      if (o < a.d_out) y[(size_t)(t.t0 + j * a.split + (int)rank) * a.d_out + o] = to_out<T>(sum);
+      if (o < a.d_out) y[(size_t)(t.t0 + (j << a.split_log) + (int)rank) * a.d_out + o] = to_out<T>(sum);
     }
   }
   if (bars->abort && tid == 0) report(a.status, timeout_bits(kWhereMxGemm, bars->abort));
@@ -745,6 +774,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   a.d_out = (int)c.d_out;
   a.nt = nt;
   a.split = split;
+  a.split_log = split == 8 ? 3 : split / 2;
   // boxes of a whole tile's tokens, or with groups, whose tiles differ, of up to 64
   a.bx = c.offsets && nt / CG > 64 ? 64 : nt / CG;
   a.bxs = c.offsets && nt > 64 ? 64 : nt;
