@@ -5,18 +5,29 @@
 // all that is written beside the norm's sum, so the norm's or SwiGLU's 16-bit output never goes through memory.
 //
 // A thread takes 8 consecutive values (16 bytes of bf16), four lanes a block of 32: the block's largest magnitude takes
-// two shuffles, a warp's codes are 128 consecutive bytes and its scales 8.  Magnitudes are compared as integers, their
-// bits without the sign, so a NaN or an infinity is the largest of all and needs no test of its own.
+// two shuffles, a warp's codes are 128 consecutive bytes and its scales 8.  Memory gives an SM 22 bytes a cycle, a warp's
+// 256 bf16 values in 23: what bounds these kernels in practice are the instructions an octet takes (about 200 at first),
+// so bf16 values are compared and scaled two at a time, places are counted on instead of divided, and the row numbers of
+// a gather have a kernel of their own.
 #include "mx_format.cuh"
 
 namespace cat {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kFlatBlocks = 32;  // most blocks an SM of a grid-stride loop
 
 struct Oct {
   float v[8];
 };
+
+__device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+__device__ __forceinline__ __nv_bfloat162 bf16_pair(uint32_t bits) {
+  const uint32_t two = bits | (bits << 16);
+  return *reinterpret_cast<const __nv_bfloat162*>(&two);
+}
 
 __device__ __forceinline__ Oct load_oct(const float* p) {
   const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
@@ -24,14 +35,7 @@ __device__ __forceinline__ Oct load_oct(const float* p) {
 }
 __device__ __forceinline__ Oct load_oct(const __nv_bfloat16* p) {
   const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
-  Oct o;
-  const uint32_t r[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    o.v[2 * i] = __uint_as_float(r[i] << 16);
-    o.v[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
-  }
-  return o;
+  return {{lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)}};
 }
 __device__ __forceinline__ void store_oct(float* p, const Oct& o) {
   reinterpret_cast<float4*>(p)[0] = make_float4(o.v[0], o.v[1], o.v[2], o.v[3]);
@@ -47,15 +51,22 @@ __device__ __forceinline__ void store_oct(__nv_bfloat16* p, const Oct& o) {
   *reinterpret_cast<uint4*>(p) = make_uint4(r[0], r[1], r[2], r[3]);
 }
 
+// The larger magnitude; a NaN is larger than all.
+__device__ __forceinline__ float max_magnitude(float a, float b) {
+  float m;
+  asm("{ .reg .f32 x, y; abs.f32 x, %1; abs.f32 y, %2; max.NaN.f32 %0, x, y; }" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+
 // The 4-bit form of a lane's 8 values of a block of 32 (four neighbouring lanes, all of which call this): the codes
 // and the block's scale byte.
 __device__ __forceinline__ uint32_t quantize_oct(const Oct& o, uint32_t* scale_byte) {
-  uint32_t a = 0u;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(o.v[i]) & 0x7FFFFFFFu);
-  a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-  a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-  const uint32_t b = mx_scale_byte(a);
+  const float m0 = max_magnitude(max_magnitude(o.v[0], o.v[1]), max_magnitude(o.v[2], o.v[3]));
+  const float m1 = max_magnitude(max_magnitude(o.v[4], o.v[5]), max_magnitude(o.v[6], o.v[7]));
+  float a = max_magnitude(m0, m1);
+  a = max_magnitude(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+  a = max_magnitude(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+  const uint32_t b = mx_scale_byte(__float_as_uint(a) & 0x7FFFFFFFu);
   *scale_byte = b;
   if (b == 255u) return 0u;
   const float inv = mx_inverse_scale(b);
@@ -64,11 +75,40 @@ __device__ __forceinline__ uint32_t quantize_oct(const Oct& o, uint32_t* scale_b
   for (int i = 0; i < 8; ++i) v[i] = o.v[i] * inv;
   return mx_pack8(v);
 }
+// The same of 8 bf16 values as they are stored.  Magnitudes are compared as 16-bit integers, two at a time (a NaN is the
+// largest); the scaling is exact in bf16 too (what underflows has the code 0 either way).
+__device__ __forceinline__ uint32_t quantize_oct(const uint4& w, uint32_t* scale_byte) {
+  constexpr uint32_t kMag = 0x7FFF7FFFu;
+  uint32_t a = __vmaxu2(__vmaxu2(w.x & kMag, w.y & kMag), __vmaxu2(w.z & kMag, w.w & kMag));
+  a = __vmaxu2(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+  a = __vmaxu2(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+  const uint32_t b = mx_scale_byte(max(a & 0xFFFF0000u, a << 16));
+  *scale_byte = b;
+  if (b == 255u) return 0u;
+  const __nv_bfloat162 inv = bf16_pair((254u - b) << 7);
+  const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 p = __hmul2_rn(*reinterpret_cast<const __nv_bfloat162*>(&r[i]), inv);
+    const uint32_t q = *reinterpret_cast<const uint32_t*>(&p);
+    v[2 * i] = lo_f32(q);
+    v[2 * i + 1] = hi_f32(q);
+  }
+  return mx_pack8(v);
+}
+
+// silu(g) u: g / (1 + exp(-g)) u.  The reciprocal is within a unit of the last place, 0 of infinity.
+__device__ __forceinline__ float swiglu(float g, float u) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-g)));
+  return g * r * u;
+}
 
 // Writes a lane's codes, and for the block's first lane its scale byte (and the row's pad bytes behind the last).
-__device__ __forceinline__ void store_codes(uint32_t w, uint32_t b, int64_t row, int oct, int octs, uint8_t* xq,
+__device__ __forceinline__ void store_codes(uint32_t w, uint32_t b, int64_t row, int oct, int octs, uint32_t* xq,
                                             uint8_t* xs, int pitch) {
-  reinterpret_cast<uint32_t*>(xq)[row * octs + oct] = w;
+  *xq = w;
   if ((oct & 3) == 0) {
     uint8_t* s = xs + row * pitch + (oct >> 2);
     *s = (uint8_t)b;
@@ -77,54 +117,114 @@ __device__ __forceinline__ void store_codes(uint32_t w, uint32_t b, int64_t row,
   }
 }
 
-// x [n][d] (or its rows `rows`) -> 4-bit form; GATED: x is [n][2 d] = [g | u] and the values are silu(g) u.
-template <typename T, bool GATED>
+// A thread's octets in a grid-stride loop: row and octet counted on, not divided.
+struct Walk {
+  int row, oct;
+  __device__ __forceinline__ Walk(int64_t first, int octs) : row((int)(first / octs)), oct((int)(first - (int64_t)row * octs)) {}
+  __device__ __forceinline__ void next(int step_rows, int step_octs, int octs) {
+    row += step_rows;
+    oct += step_octs;
+    if (oct >= octs) {
+      oct -= octs;
+      ++row;
+    }
+  }
+};
+
+// What a row's octet is made of: x itself, x's row rows[row], or silu(g) u of x [n][2 d] = [g | u].
+enum { kPlain = 0, kRows = 1, kGated = 2 };
+
+template <typename T, int FROM>
 __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const T* __restrict__ x, int64_t n,
                                                                const int32_t* __restrict__ rows, int64_t m, int octs,
-                                                               uint8_t* __restrict__ xq, uint8_t* __restrict__ xs,
-                                                               int pitch, uint32_t* __restrict__ status) {
-  pdl_wait_then_release();
+                                                               int step_rows, int step_octs, uint8_t* __restrict__ xq,
+                                                               uint8_t* __restrict__ xs, int pitch,
+                                                               uint32_t* __restrict__ status) {
   const int64_t total = m * octs, stride = (int64_t)gridDim.x * kThreads;
-  // a whole warp goes on together (the shuffles): the bound is the warp's first octet
-  for (int64_t i0 = (int64_t)blockIdx.x * kThreads + (threadIdx.x & ~31); i0 < total; i0 += stride) {
-    const int64_t i = i0 + (threadIdx.x & 31);
+  int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int lane = threadIdx.x & 31;
+  Walk w(i, octs);
+  pdl_wait_then_release();
+  bool bad = false;
+  // a whole warp goes on together (the shuffles): the bound is its first octet
+  for (; i - lane < total; i += stride, w.next(step_rows, step_octs, octs)) {
     const bool in = i < total;
-    const int64_t row = in ? i / octs : 0;
-    const int oct = in ? (int)(i - row * octs) : 0;
-    const int64_t src = rows && in ? rows[row] : row;
-    Oct o = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-    if (in && src >= 0 && src < n) {
-      if (GATED) {
-        const T* p = x + (src * 2 * octs + oct) * 8;
+    uint32_t b = 0, c;
+    if constexpr (FROM == kGated) {
+      Oct o = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+      if (in) {
+        const T* p = x + ((int64_t)w.row * octs + i) * 8;          // 2 octs a row
         const Oct g = load_oct(p), u = load_oct(p + (int64_t)octs * 8);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o.v[k] = g.v[k] / (1.f + __expf(-g.v[k])) * u.v[k];
+        for (int k = 0; k < 8; ++k) o.v[k] = swiglu(g.v[k], u.v[k]);
+      }
+      c = quantize_oct(o, &b);
+    } else {
+      int64_t src = i;
+      bool have = in;
+      if constexpr (FROM == kRows) {
+        const int64_t row = in ? rows[w.row] : -1;
+        have = row >= 0 && row < n;
+        src = row * octs + w.oct;
+      }
+      if constexpr (sizeof(T) == 2) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (have) v = __ldcs(reinterpret_cast<const uint4*>(x) + src);
+        c = quantize_oct(v, &b);
       } else {
-        o = load_oct(x + (src * octs + oct) * 8);
+        Oct o = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+        if (have) o = load_oct(x + src * 8);
+        c = quantize_oct(o, &b);
       }
     }
-    uint32_t b;
-    const uint32_t w = quantize_oct(o, &b);
-    if (in) store_codes(w, b, row, oct, octs, xq, xs, pitch);
-    if (in && b == 255u) report(status, kStatusNonFinite);
+    if (in) store_codes(c, b, w.row, w.oct, octs, reinterpret_cast<uint32_t*>(xq) + i, xs, pitch);
+    bad |= b == 255u;
   }
+  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
+}
+
+// Two E2M1 codes (nibbles 0 and 1 of c) as bf16 values 2^126 too small, the first in the low half: the code's magnitude
+// bits are a bf16's last exponent bits and first mantissa bit (a subnormal for 0.5).
+__device__ __forceinline__ uint32_t code_pair(uint32_t c) {
+  return ((c & 7u) << 6) | ((c & 0x70u) << 18) | ((c & 8u) << 12) | ((c & 0x80u) << 24);
+}
+// times 2^126, then the scale: each exact, in bf16 too (one factor for both could be out of range)
+__device__ __forceinline__ void dequantize_oct(uint32_t c, uint32_t b, float* out) {
+  const float s = mx_scale(b);
+  Oct o;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t p = code_pair(c >> (8 * k));
+    o.v[2 * k] = lo_f32(p) * 0x1p126f * s;
+    o.v[2 * k + 1] = hi_f32(p) * 0x1p126f * s;
+  }
+  store_oct(out, o);
+}
+__device__ __forceinline__ void dequantize_oct(uint32_t c, uint32_t b, __nv_bfloat16* out) {
+  const __nv_bfloat162 up = bf16_pair((126u + 127u) << 7), s = bf16_pair(b == 255u ? 0x7FFFu : b == 0u ? 0x0040u : b << 7);
+  uint32_t r[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t p = code_pair(c >> (8 * k));
+    const __nv_bfloat162 v = __hmul2_rn(__hmul2_rn(*reinterpret_cast<const __nv_bfloat162*>(&p), up), s);
+    r[k] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+  *reinterpret_cast<uint4*>(out) = make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* __restrict__ xq,
                                                                  const uint8_t* __restrict__ xs, int64_t n, int octs,
-                                                                 int pitch, T* __restrict__ out) {
-  pdl_wait_then_release();
+                                                                 int step_rows, int step_octs, int pitch,
+                                                                 T* __restrict__ out) {
   const int64_t total = n * octs, stride = (int64_t)gridDim.x * kThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += stride) {
-    const int64_t row = i / octs;
-    const int oct = (int)(i - row * octs);
-    const uint32_t w = reinterpret_cast<const uint32_t*>(xq)[i];
-    const float s = mx_scale(xs[row * pitch + (oct >> 2)]);
-    Oct o;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) o.v[k] = mx_code_value((w >> (4 * k)) & 15u) * s;
-    store_oct(out + i * 8, o);
+  int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  Walk w(i, octs);
+  pdl_wait_then_release();
+  for (; i < total; i += stride, w.next(step_rows, step_octs, octs)) {
+    const uint32_t c = __ldcs(reinterpret_cast<const uint32_t*>(xq) + i);
+    const uint32_t b = xs[(int64_t)w.row * pitch + (w.oct >> 2)];
+    dequantize_oct(c, b, out + i * 8);
   }
 }
 
@@ -140,6 +240,7 @@ __global__ void __launch_bounds__(1024) mx_rmsnorm_quantize_kernel(const T* x, c
   __shared__ float part[32];
   pdl_wait_then_release();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  bool bad = false;
   for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
     const int64_t base = row * octs;
     auto sum_of = [&](int oct) {
@@ -195,12 +296,13 @@ __global__ void __launch_bounds__(1024) mx_rmsnorm_quantize_kernel(const T* x, c
       uint32_t b;
       const uint32_t c = quantize_oct(v, &b);
       if (oct < octs) {
-        store_codes(c, b, row, oct, octs, xq, xs, pitch);
-        if (b == 255u) report(status, kStatusNonFinite);
+        store_codes(c, b, row, oct, octs, reinterpret_cast<uint32_t*>(xq) + base + oct, xs, pitch);
+        bad |= b == 255u;
       }
     }
     __syncthreads();                                     // part[] is read before the next row's sums
   }
+  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
 }
 
 int sm_count() {
@@ -223,17 +325,25 @@ cudaError_t launch(void (*kernel)(P...), int64_t blocks, int threads, cudaStream
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
-int64_t flat_blocks(int64_t octets) {
-  const int64_t blocks = (octets + kThreads - 1) / kThreads, cap = (int64_t)sm_count() * 32;
-  return blocks < cap ? blocks : cap;
-}
+// Blocks of a grid-stride loop over octets, and its stride in rows and octets.
+struct Flat {
+  int64_t blocks;
+  int step_rows, step_octs;
+  Flat(int64_t octets, int octs) {
+    const int64_t want = (octets + kThreads - 1) / kThreads, cap = (int64_t)sm_count() * kFlatBlocks;
+    blocks = want < cap ? want : cap;
+    step_rows = (int)(blocks * kThreads / octs);
+    step_octs = (int)(blocks * kThreads % octs);
+  }
+};
 
-template <typename T, bool GATED>
+template <typename T, int FROM>
 cudaError_t quantize(const void* x, int64_t n, int64_t d, const int32_t* rows, int64_t m, uint8_t* xq, uint8_t* xs,
                      uint32_t* status, cudaStream_t stream) {
   const int octs = (int)(d / 8);
-  return launch(mx_quantize_kernel<T, GATED>, flat_blocks(m * octs), kThreads, stream, static_cast<const T*>(x), n, rows, m,
-                octs, xq, xs, (int)mx_pitch(d), status);
+  const Flat f(m * octs, octs);
+  return launch(mx_quantize_kernel<T, FROM>, f.blocks, kThreads, stream, static_cast<const T*>(x), n, rows, m, octs,
+                f.step_rows, f.step_octs, xq, xs, (int)mx_pitch(d), status);
 }
 
 template <typename T, typename W>
@@ -256,23 +366,29 @@ cudaError_t rmsnorm(const void* x, const void* residual, const void* weight, int
 
 }  // namespace
 
+template <typename T>
+static cudaError_t quantize_from(const void* x, int64_t n, int64_t d, const int32_t* rows, int64_t m, int gated, uint8_t* xq,
+                                 uint8_t* xs, uint32_t* status, cudaStream_t stream) {
+  if (gated) return quantize<T, kGated>(x, n, d, rows, m, xq, xs, status, stream);
+  return rows ? quantize<T, kRows>(x, n, d, rows, m, xq, xs, status, stream)
+              : quantize<T, kPlain>(x, n, d, rows, m, xq, xs, status, stream);
+}
+
 cudaError_t launch_mx_quantize(const void* x, int dtype, int64_t n, int64_t d, const int32_t* rows, int64_t m, int gated,
                                uint8_t* xq, uint8_t* xs, uint32_t* status, cudaStream_t stream) {
-  if (dtype == 0)
-    return gated ? quantize<float, true>(x, n, d, rows, m, xq, xs, status, stream)
-                 : quantize<float, false>(x, n, d, rows, m, xq, xs, status, stream);
-  return gated ? quantize<__nv_bfloat16, true>(x, n, d, rows, m, xq, xs, status, stream)
-               : quantize<__nv_bfloat16, false>(x, n, d, rows, m, xq, xs, status, stream);
+  return dtype == 0 ? quantize_from<float>(x, n, d, rows, m, gated, xq, xs, status, stream)
+                    : quantize_from<__nv_bfloat16>(x, n, d, rows, m, gated, xq, xs, status, stream);
 }
 
 cudaError_t launch_mx_dequantize(const uint8_t* xq, const uint8_t* xs, int64_t n, int64_t d, int dtype, void* out,
                                  cudaStream_t stream) {
   const int octs = (int)(d / 8), pitch = (int)mx_pitch(d);
+  const Flat f(n * octs, octs);
   if (dtype == 0)
-    return launch(mx_dequantize_kernel<float>, flat_blocks(n * octs), kThreads, stream, xq, xs, n, octs, pitch,
+    return launch(mx_dequantize_kernel<float>, f.blocks, kThreads, stream, xq, xs, n, octs, f.step_rows, f.step_octs, pitch,
                   static_cast<float*>(out));
-  return launch(mx_dequantize_kernel<__nv_bfloat16>, flat_blocks(n * octs), kThreads, stream, xq, xs, n, octs, pitch,
-                static_cast<__nv_bfloat16*>(out));
+  return launch(mx_dequantize_kernel<__nv_bfloat16>, f.blocks, kThreads, stream, xq, xs, n, octs, f.step_rows, f.step_octs,
+                pitch, static_cast<__nv_bfloat16*>(out));
 }
 
 cudaError_t launch_mx_rmsnorm_quantize(const void* x, const void* residual, const void* weight, int dtype,
