@@ -15,6 +15,7 @@ namespace cat {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWarpOcts = 64;     // rows of a norm up to this have a warp each (8192 x 256 bf16 4.5 us, a CTA each 8.7; x 768 13.5, 12.3)
 constexpr int kFlatBlocks = 32;  // most blocks an SM of a grid-stride loop
 
 struct Oct {
@@ -228,78 +229,182 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* 
   }
 }
 
-// One row a CTA.  h = x + residual in 32 bits, stored in x's type; v = h / sqrt(mean(h^2) + eps) * weight, of the
-// unrounded h; then the 4-bit form of v.  A thread keeps ITEMS octets of h in registers, so the row is read once; with
-// ITEMS = 0 (rows too long for that) it is read again for the second pass, before h is written, so h may be x or residual.
+// ---- h = x + residual in 32 bits, stored in x's type; v = h / sqrt(mean(h^2) + eps) * weight, of the unrounded h; then
+// the 4-bit form of v.  Rows of up to 512 values have a warp each, up to 16384 a CTA each, whose threads hold them in
+// registers (an octet each to 8192, two beyond); with persistent CTAs that load the next row while this one's sum is
+// formed, 8192 x 8192 bf16 takes 82 us (5.3 TB/s), without 93, and 106 with four octets a thread.  Copying rows ahead into
+// shared memory was no faster for 8192 rows of 8192 (83) and slower for all smaller (2048 x 4096 19 us, 13 here).
+// h may be x or residual: a row's values are read by the CTA (warp) that writes them, before it writes.
+
+__device__ __forceinline__ Oct load_weights(const float* p) {
+  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+__device__ __forceinline__ Oct load_weights(const __nv_bfloat16* p) {
+  const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
+  return {{lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)}};
+}
+
+__device__ __forceinline__ void add(Oct& a, const Oct& b) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) a.v[k] += b.v[k];
+}
+__device__ __forceinline__ float squares(const Oct& a, float sum) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum = fmaf(a.v[k], a.v[k], sum);
+  return sum;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+
+struct NormOut {
+  void* h;
+  uint8_t *xq, *xs;
+  int octs, pitch;
+};
+
+// The second half for one octet of a row (whole warps; lanes past the row's end hold nothing): h and the 4-bit form.
+template <typename T, typename W>
+__device__ __forceinline__ bool finish_oct(const NormOut& out, const W* weight, int64_t row, int oct, const Oct& a, float r) {
+  const bool in = oct < out.octs;
+  Oct v = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+  const int64_t at = row * out.octs + oct;
+  if (in) {
+    if (out.h) store_oct(static_cast<T*>(out.h) + at * 8, a);
+    const Oct w = load_weights(weight + (int64_t)oct * 8);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v.v[k] = a.v[k] * r * w.v[k];
+  }
+  uint32_t b;
+  const uint32_t c = quantize_oct(v, &b);
+  if (in) store_codes(c, b, row, oct, out.octs, reinterpret_cast<uint32_t*>(out.xq) + at, out.xs, out.pitch);
+  return in && b == 255u;
+}
+
+// A warp a row of up to 32 ITEMS octets.
 template <typename T, typename W, int ITEMS>
-__global__ void __launch_bounds__(1024) mx_rmsnorm_quantize_kernel(const T* x, const T* residual,
-                                                                   const W* __restrict__ weight, int64_t n, int octs,
-                                                                   float eps, T* h, uint8_t* __restrict__ xq,
-                                                                   uint8_t* __restrict__ xs, int pitch,
-                                                                   uint32_t* __restrict__ status) {
+__global__ void __launch_bounds__(kThreads) mx_rmsnorm_warp_kernel(const T* x, const T* residual,
+                                                                   const W* __restrict__ weight, int64_t n, float eps,
+                                                                   const NormOut out, uint32_t* __restrict__ status) {
+  pdl_wait_then_release();
+  const int lane = threadIdx.x & 31, octs = out.octs;
+  const int64_t stride = (int64_t)gridDim.x * (kThreads / 32);
+  bool bad = false;
+  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); row < n; row += stride) {
+    Oct a[ITEMS];
+    float sq = 0.f;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      const int oct = 32 * j + lane;
+      if (oct < octs) {
+        a[j] = load_oct(x + (row * octs + oct) * 8);
+        if (residual) add(a[j], load_oct(residual + (row * octs + oct) * 8));
+        sq = squares(a[j], sq);
+      }
+    }
+    const float r = 1.f / sqrtf(warp_sum(sq) / (float)(octs * 8) + eps);
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+      if (32 * j < octs) bad |= finish_oct<T>(out, weight, row, 32 * j + lane, a[j], r);
+  }
+  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
+}
+
+// An octet as it is in memory.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldcs(reinterpret_cast<const float4*>(p));
+    b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ Oct oct() const { return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}}; }
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint4 w;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ Oct oct() const {
+    return {{lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)}};
+  }
+};
+
+// A CTA a row, ITEMS octets a thread in registers; the next row's are on their way while this one's sum is formed.
+template <typename T, typename W, int ITEMS>
+__global__ void __launch_bounds__(1024) mx_rmsnorm_row_kernel(const T* x, const T* residual, const W* __restrict__ weight,
+                                                              int64_t n, float eps, const NormOut out,
+                                                              uint32_t* __restrict__ status) {
+  __shared__ float part[2][32];
+  pdl_wait_then_release();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, octs = out.octs;
+  Raw<T> nx[ITEMS], nr[ITEMS];
+  auto load = [&](int64_t row) {
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      const int oct = j * blockDim.x + threadIdx.x;
+      if (row < n && oct < octs) {
+        nx[j].load(x + (row * octs + oct) * 8);
+        if (residual) nr[j].load(residual + (row * octs + oct) * 8);
+      }
+    }
+  };
+  bool bad = false;
+  int turn = 0;
+  load(blockIdx.x);
+  for (int64_t row = blockIdx.x; row < n; row += gridDim.x, turn ^= 1) {
+    Oct a[ITEMS];
+    float sq = 0.f;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      if (j * (int)blockDim.x + (int)threadIdx.x < octs) {
+        a[j] = nx[j].oct();
+        if (residual) add(a[j], nr[j].oct());
+        sq = squares(a[j], sq);
+      }
+    }
+    load(row + gridDim.x);
+    sq = warp_sum(sq);
+    if (lane == 0) part[turn][warp] = sq;
+    __syncthreads();                                     // (part[] has two turns, so one barrier a row will do)
+    const float r = 1.f / sqrtf(warp_sum(lane < warps ? part[turn][lane] : 0.f) / (float)(octs * 8) + eps);
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      const int oct = j * blockDim.x + threadIdx.x;
+      if (oct - lane < octs) bad |= finish_oct<T>(out, weight, row, oct, a[j], r);
+    }
+  }
+  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
+}
+
+// Longer rows are read twice (before h is written).
+template <typename T, typename W>
+__global__ void __launch_bounds__(1024) mx_rmsnorm_long_kernel(const T* x, const T* residual, const W* __restrict__ weight,
+                                                               int64_t n, float eps, const NormOut out,
+                                                               uint32_t* __restrict__ status) {
   __shared__ float part[32];
   pdl_wait_then_release();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, octs = out.octs;
   bool bad = false;
   for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
     const int64_t base = row * octs;
     auto sum_of = [&](int oct) {
       Oct a = load_oct(x + (base + oct) * 8);
-      if (residual) {
-        const Oct r = load_oct(residual + (base + oct) * 8);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) a.v[k] += r.v[k];
-      }
+      if (residual) add(a, load_oct(residual + (base + oct) * 8));
       return a;
     };
-    constexpr int kKept = ITEMS ? ITEMS : 1;
-    const int steps = ITEMS ? ITEMS : (octs + (int)blockDim.x - 1) / (int)blockDim.x;
-    Oct kept[kKept];
     float sq = 0.f;
-    if (ITEMS) {
-#pragma unroll
-      for (int j = 0; j < kKept; ++j) {
-        const int oct = j * blockDim.x + threadIdx.x;
-        if (oct < octs) {
-          kept[j] = sum_of(oct);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) sq = fmaf(kept[j].v[k], kept[j].v[k], sq);
-        }
-      }
-    } else {
-      for (int oct = threadIdx.x; oct < octs; oct += blockDim.x) {
-        const Oct a = sum_of(oct);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sq = fmaf(a.v[k], a.v[k], sq);
-      }
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, d);
+    for (int oct = threadIdx.x; oct < octs; oct += blockDim.x) sq = squares(sum_of(oct), sq);
+    sq = warp_sum(sq);
     if (lane == 0) part[warp] = sq;
     __syncthreads();
-    float all = lane < warps ? part[lane] : 0.f;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, d);
-    const float r = 1.f / sqrtf(all / (float)(octs * 8) + eps);
-#pragma unroll
-    for (int j = 0; j < (ITEMS ? kKept : steps); ++j) {
-      const int oct = j * blockDim.x + threadIdx.x;
-      if (oct - lane >= octs) break;                     // whole warps (the shuffles)
-      Oct v = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-      if (oct < octs) {
-        const Oct a = ITEMS ? kept[ITEMS ? j : 0] : sum_of(oct);
-        if (h) store_oct(h + (base + oct) * 8, a);
-        const Oct w = load_oct(weight + (int64_t)oct * 8);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v.v[k] = a.v[k] * r * w.v[k];
-      }
-      uint32_t b;
-      const uint32_t c = quantize_oct(v, &b);
-      if (oct < octs) {
-        store_codes(c, b, row, oct, octs, reinterpret_cast<uint32_t*>(xq) + base + oct, xs, pitch);
-        bad |= b == 255u;
-      }
-    }
+    const float r = 1.f / sqrtf(warp_sum(lane < warps ? part[lane] : 0.f) / (float)(octs * 8) + eps);
+    for (int oct = threadIdx.x; oct - lane < octs; oct += blockDim.x)
+      bad |= finish_oct<T>(out, weight, row, oct, oct < octs ? sum_of(oct) : Oct{}, r);
     __syncthreads();                                     // part[] is read before the next row's sums
   }
   if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
@@ -347,21 +452,24 @@ cudaError_t quantize(const void* x, int64_t n, int64_t d, const int32_t* rows, i
 }
 
 template <typename T, typename W>
-cudaError_t rmsnorm(const void* x, const void* residual, const void* weight, int64_t n, int64_t d, float eps, void* h,
+cudaError_t rmsnorm(const void* x_, const void* residual_, const void* weight_, int64_t n, int64_t d, float eps, void* h,
                     uint8_t* xq, uint8_t* xs, uint32_t* status, cudaStream_t stream) {
   const int octs = (int)(d / 8);
-  int threads = 32;
-  while (threads < 1024 && threads * (threads < 256 ? 1 : 4) < octs) threads *= 2;
-  const int items = (octs + threads - 1) / threads;
-  auto go = [&](auto kernel) {
-    const int64_t cap = (int64_t)sm_count() * 64;
-    return launch(kernel, n < cap ? n : cap, threads, stream, static_cast<const T*>(x), static_cast<const T*>(residual),
-                  static_cast<const W*>(weight), n, octs, eps, static_cast<T*>(h), xq, xs, (int)mx_pitch(d), status);
-  };
-  if (items == 1) return go(mx_rmsnorm_quantize_kernel<T, W, 1>);
-  if (items == 2) return go(mx_rmsnorm_quantize_kernel<T, W, 2>);
-  if (items <= 4) return go(mx_rmsnorm_quantize_kernel<T, W, 4>);
-  return go(mx_rmsnorm_quantize_kernel<T, W, 0>);
+  const NormOut out = {h, xq, xs, octs, (int)mx_pitch(d)};
+  const T *x = static_cast<const T*>(x_), *residual = static_cast<const T*>(residual_);
+  const W* weight = static_cast<const W*>(weight_);
+  const int64_t sms = sm_count();
+  if (octs <= kWarpOcts) {
+    const int64_t want = (n + kThreads / 32 - 1) / (kThreads / 32), blocks = want < sms * 16 ? want : sms * 16;
+    auto go = [&](auto kernel) { return launch(kernel, blocks, kThreads, stream, x, residual, weight, n, eps, out, status); };
+    return octs <= 32 ? go(mx_rmsnorm_warp_kernel<T, W, 1>) : go(mx_rmsnorm_warp_kernel<T, W, 2>);
+  }
+  const int threads = octs < 1024 ? (octs + 31) / 32 * 32 : 1024;
+  const int64_t most = sms * (2048 / threads), blocks = n < most ? n : most;
+  auto go = [&](auto kernel) { return launch(kernel, blocks, threads, stream, x, residual, weight, n, eps, out, status); };
+  if (octs <= 1024) return go(mx_rmsnorm_row_kernel<T, W, 1>);
+  if (octs <= 2048) return go(mx_rmsnorm_row_kernel<T, W, 2>);
+  return go(mx_rmsnorm_long_kernel<T, W>);
 }
 
 }  // namespace
