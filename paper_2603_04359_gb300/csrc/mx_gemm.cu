@@ -92,6 +92,19 @@ struct Place {
   __device__ __forceinline__ uint32_t free() const { return (round - 1) & 1; }
 };
 
+// A whole warp waits (and knows the outcome to be the same in all lanes).
+__device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int line, uint64_t limit) {
+  return (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort, line, limit));
+}
+// Waits for the last fillings of a ring's buffers, `at` its next place.
+__device__ __forceinline__ void drain(uint64_t* full, Place at, uint32_t of) {
+  volatile int no_abort = 0;
+  for (uint32_t b = 0; b < of; ++b) {
+    const uint32_t fills = at.round + (b < at.at ? 1u : 0u);
+    if (fills > 0) mbar_wait_bounded(&full[b], (fills - 1) & 1, &no_abort);
+  }
+}
+
 struct Tile {
   int w_row;                                // the expert's first row of the weights
   int o0;                                   // first channel (of the pair)
@@ -391,59 +404,55 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA of codes
-    if (lane == 0) {
-      uint32_t it = 0;
-      Place st;
-      bool ok = true;
-      int e = 0;
-      for (int u = cluster; u < total && ok; u += clusters) {
-        const Tile t = tile_at(u, e);
-        const int wrow = t.w_row + t.o0 + (int)(CG == 2 ? rank : 0) * BM;
-        const int mine = t.n / CG, xrow = t.t0 + (CG == 2 ? (int)rank : 0) * mine;
-        const int boxes = (mine + a.bx - 1) / a.bx;
-        const uint32_t bytes = kStageW + (uint32_t)(boxes * a.bx) * 128u;
-        for (int ks = k0; ks < k1; ++ks, ++it, st.next(a.stages)) {
-          const uint32_t s = st.at;
-          if (!st.first() && !(ok = mbar_wait_bounded(&bars->empty[s], st.free(), abort_flag, __LINE__, lim))) break;
-          uint8_t* dst = smem + s * a.stage_bytes;
-          uint64_t* fb = CG == 2 && rank == 1 ? &bars->ready[s] : &bars->full[s];
+    // (here too all lanes go through the loop and one is elected: a copy issued in a branch of lane 0's took ~300 cycles)
+    Place st;
+    bool ok = true;
+    int e = 0;
+    for (int u = cluster; u < total && ok; u += clusters) {
+      const Tile t = tile_at(u, e);
+      const int wrow = t.w_row + t.o0 + (int)(CG == 2 ? rank : 0) * BM;
+      const int mine = t.n / CG, xrow = t.t0 + (CG == 2 ? (int)rank : 0) * mine;
+      const int boxes = mine > a.bx ? (mine + a.bx - 1) / a.bx : 1;
+      const uint32_t bytes = kStageW + (uint32_t)(boxes * a.bx) * 128u;
+      for (int ks = k0; ks < k1; ++ks, st.next(a.stages)) {
+        if (!st.first() && !(ok = all_wait(&bars->empty[st.at], st.free(), abort_flag, __LINE__, lim))) break;
+        uint8_t* dst = smem + st.at * a.stage_bytes;
+        uint64_t* fb = CG == 2 && rank == 1 ? &bars->ready[st.at] : &bars->full[st.at];
+        if (elect_one()) {
           mbar_arrive_expect_tx(fb, bytes + (CG == 2 && rank == 0 ? 4u : 0u));   // (+ the odd CTA's signal)
           tma_load_2d(dst, &tmW, ks * (BK / 2), wrow, fb);
           for (int b = 0; b < boxes; ++b)
             tma_load_2d(dst + kStageW + (uint32_t)(b * a.bx) * 128u, &tmX, ks * (BK / 2), xrow + b * a.bx, fb);
         }
+        __syncwarp();
       }
-      // the copies in flight land before the CTA exits (they have, unless a wait gave up)
-      volatile int no_abort = 0;
-      for (uint32_t j = it > (uint32_t)a.stages ? it - a.stages : 0; j < it; ++j)
-        mbar_wait_bounded(CG == 2 && rank == 1 ? &bars->ready[j % a.stages] : &bars->full[j % a.stages],
-                          (j / a.stages) & 1, &no_abort);
     }
+    // the copies in flight land before the CTA exits (they have, unless a wait gave up)
+    if (lane == 0) drain(CG == 2 && rank == 1 ? bars->ready : bars->full, st, a.stages);
   } else if (warp == 2) {
     // ---------------------------------------------------------------- TMA of scales
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      int e = 0;
-      for (int u = cluster; u < total && ok; u += clusters) {
-        const Tile t = tile_at(u, e);
-        const int wrow = t.w_row + t.o0 + (int)(CG == 2 ? rank : 0) * BM;
-        const int boxes = (t.n + a.bxs - 1) / a.bxs;
-        const uint32_t bytes = kScalesW + (uint32_t)(boxes * a.bxs * kScaleRow);
-        for (int c = c0; c < c1; c += kGroup, ++it) {
-          const uint32_t s = it % kRing, use = it / kRing;
-          if (use > 0 && !(ok = mbar_wait_bounded(&bars->sempty[s], (use - 1) & 1, abort_flag, __LINE__, lim))) break;
-          uint8_t* dst = ring + s * a.ring_bytes;
-          mbar_arrive_expect_tx(&bars->sfull[s], bytes);
-          tma_load_2d(dst, &tmWs, c * 16, wrow, &bars->sfull[s]);
+    Place rg;
+    bool ok = true;
+    int e = 0;
+    for (int u = cluster; u < total && ok; u += clusters) {
+      const Tile t = tile_at(u, e);
+      const int wrow = t.w_row + t.o0 + (int)(CG == 2 ? rank : 0) * BM;
+      const int boxes = t.n > a.bxs ? (t.n + a.bxs - 1) / a.bxs : 1;
+      const uint32_t bytes = kScalesW + (uint32_t)(boxes * a.bxs * kScaleRow);
+      for (int c = c0; c < c1; c += kGroup, rg.next(kRing)) {
+        if (!rg.first() && !(ok = all_wait(&bars->sempty[rg.at], rg.free(), abort_flag, __LINE__, lim))) break;
+        uint8_t* dst = ring + rg.at * a.ring_bytes;
+        uint64_t* fb = &bars->sfull[rg.at];
+        if (elect_one()) {
+          mbar_arrive_expect_tx(fb, bytes);
+          tma_load_2d(dst, &tmWs, c * 16, wrow, fb);
           for (int b = 0; b < boxes; ++b)
-            tma_load_2d(dst + kScalesW + (uint32_t)(b * a.bxs * kScaleRow), &tmXs, c * 16, t.t0 + b * a.bxs, &bars->sfull[s]);
+            tma_load_2d(dst + kScalesW + (uint32_t)(b * a.bxs * kScaleRow), &tmXs, c * 16, t.t0 + b * a.bxs, fb);
         }
+        __syncwarp();
       }
-      volatile int no_abort = 0;
-      for (uint32_t j = it > (uint32_t)kRing ? it - kRing : 0; j < it; ++j)
-        mbar_wait_bounded(&bars->sfull[j % kRing], (j / kRing) & 1, &no_abort);
     }
+    if (lane == 0) drain(bars->sfull, rg, kRing);
   } else if (CG == 2 && rank == 1 && (warp == 1 || warp == 3)) {
     // ---------------------------------------------------------------- odd CTA: forward stages (1) and scale slots (3)
     // (an arrive on the even CTA's barrier from the warps that wrote the data would stall them; a thread that waits for
@@ -476,9 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t slot_cols = 16u + 4u * a.xcols, xcols = a.xcols;
     const uint64_t wdesc0 = sdesc_kmajor_sw128(smem_u32(smem)), xdesc0 = sdesc_kmajor_sw128(smem_u32(smem) + kStageW);
     const uint32_t stage16 = a.stage_bytes >> 4;
-    auto wait = [&](uint64_t* bar, uint32_t parity, int line) {
-      return (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort_flag, line, lim));
-    };
+    auto wait = [&](uint64_t* bar, uint32_t parity, int line) { return all_wait(bar, parity, abort_flag, line, lim); };
     Place st, sl, ac;
     bool ok = true;
     int e = 0;
