@@ -636,45 +636,32 @@ def cat_mx_scale_pitch(d: int) -> int:
     return (d + 511) // 512 * 16
 
 
-# The checks of these calls are one chain of attribute tests over all tensors (a get_device of one CPU tensor is -1); a
-# call that does not pass goes through _expect, which says what is wrong.  Host time of a call: 6 to 8 us, 3 of them in
-# the library and 1.5 for each output allocated here (11 to 16 us with an _expect for each tensor).
+# A call whose arguments are the ordinary ones goes through _mx_calls (csrc/mx_calls.cpp: the same checks and the same
+# entry points, without the interpreter's time); any other through the code behind it here, which takes buffers to write
+# to and says what is wrong with a tensor.
 
-_U8 = torch.uint8
-_empty = torch.empty
+_mx_native = None
+
+
+def _calls():
+    """The compiled calls; fails loudly if they have not been built."""
+    global _mx_native
+    if _mx_native is None:
+        load_library()
+        from . import _mx_calls
+        _mx_native = _mx_calls
+    return _mx_native
 
 
 def _mx_out(xq, xs, m: int, d: int, dev: torch.device) -> Tuple[torch.Tensor, torch.Tensor]:
-    pitch = (d + 511) // 512 * 16
-    return (_empty((m, d >> 1), dtype=_U8, device=dev) if xq is None else _given(xq, "xq", _U8, (m, d // 2), dev),
-            _empty((m, pitch), dtype=_U8, device=dev) if xs is None else _given(xs, "xs", _U8, (m, pitch), dev))
+    return (_given(xq, "xq", torch.uint8, (m, d // 2), dev),
+            _given(xs, "xs", torch.uint8, (m, cat_mx_scale_pitch(d)), dev))
 
 
-def _mx_stream(t: torch.Tensor) -> int:
-    return _stream(t.device) if _raw_stream is None else _raw_stream(t.get_device())
-
-
-def _mx_library() -> ctypes.CDLL:
-    return _lib or load_library()
-
-
-def cat_mx_quantize(x: torch.Tensor, rows: Optional[torch.Tensor] = None, xq: Optional[torch.Tensor] = None,
-                    xs: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """The 4-bit form (codes, scales) of x [n, d], or of its rows ``rows`` (int32 [m]; an index outside [0, n) gives a
-    row of zeros).  Activations and weights alike."""
-    _need(x, "x")
-    n, d = x.shape
-    dev = x.device
-    m = n
-    if rows is not None:
-        m = rows.numel()
-        _expect(rows, "rows", torch.int32, (m,), dev)
-    xq, xs = _mx_out(xq, xs, m, d, dev)
-    st = _mx_library().cat_mx_quantize(x.data_ptr(), _dtype(x), n, d, None if rows is None else rows.data_ptr(), m,
-                                       xq.data_ptr(), xs.data_ptr(), _mx_stream(x))
-    if st:
-        _check("cat_mx_quantize", st)
-    return xq, xs
+def _mx_codes(q: torch.Tensor, s: torch.Tensor, names: Tuple[str, str], shape: tuple, half: int, dev: torch.device) -> None:
+    """Checks codes [*shape, half] and their scales."""
+    _expect(q, names[0], torch.uint8, (*shape, half), dev)
+    _expect(s, names[1], torch.uint8, (*shape, cat_mx_scale_pitch(2 * half)), dev)
 
 
 def _mx_result(t: Optional[torch.Tensor], name: str, dtype: Optional[torch.dtype], shape: tuple,
@@ -683,38 +670,66 @@ def _mx_result(t: Optional[torch.Tensor], name: str, dtype: Optional[torch.dtype
     if t is not None:
         _expect(t, name, dtype or t.dtype, shape, dev)
         return t
-    return _empty(shape, dtype=dtype or torch.float32, device=dev)
+    return torch.empty(shape, dtype=dtype or torch.float32, device=dev)
+
+
+def cat_mx_quantize(x: torch.Tensor, rows: Optional[torch.Tensor] = None, xq: Optional[torch.Tensor] = None,
+                    xs: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The 4-bit form (codes, scales) of x [n, d], or of its rows ``rows`` (int32 [m]; an index outside [0, n) gives a
+    row of zeros).  Activations and weights alike."""
+    if xq is None and xs is None:
+        r = (_mx_native or _calls()).quantize(x, rows)
+        if type(r) is tuple:
+            return r
+        if r is not None:
+            _check("cat_mx_quantize", r)
+    _need(x, "x")
+    n, d = x.shape
+    dev = x.device
+    m = n
+    if rows is not None:
+        m = rows.numel()
+        _expect(rows, "rows", torch.int32, (m,), dev)
+    xq, xs = _mx_out(xq, xs, m, d, dev)
+    _check("cat_mx_quantize", load_library().cat_mx_quantize(_ptr(x), _dtype(x), n, d, _ptr(rows), m, _ptr(xq), _ptr(xs),
+                                                             _stream(dev)))
+    return xq, xs
 
 
 def cat_mx_dequantize(xq: torch.Tensor, xs: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values that codes [n, d / 2] and scales stand for, [n, d]: float32 (default) or bfloat16, exact in both."""
+    if out is None:
+        r = (_mx_native or _calls()).dequantize(xq, xs, out_dtype)
+        if isinstance(r, torch.Tensor):
+            return r
+        if r is not None:
+            _check("cat_mx_dequantize", r)
     n, half = xq.shape
-    dev, pitch = xq.device, (half + 255) // 256 * 16
-    if not (xq.dtype is _U8 is xs.dtype and xs.shape == (n, pitch) and xq.is_contiguous() and xs.is_contiguous()
-            and xq.get_device() == xs.get_device() >= 0):
-        _expect(xq, "xq", _U8, (n, half), dev)
-        _expect(xs, "xs", _U8, (n, pitch), dev)
+    dev = xq.device
+    _mx_codes(xq, xs, ("xq", "xs"), (n,), half, dev)
     out = _mx_result(out, "out", out_dtype, (n, 2 * half), dev)
-    st = _mx_library().cat_mx_dequantize(xq.data_ptr(), xs.data_ptr(), n, 2 * half, _dtype(out), out.data_ptr(),
-                                         _mx_stream(xq))
-    if st:
-        _check("cat_mx_dequantize", st)
+    _check("cat_mx_dequantize", load_library().cat_mx_dequantize(_ptr(xq), _ptr(xs), n, 2 * half, _dtype(out), _ptr(out),
+                                                                 _stream(dev)))
     return out
 
 
 def cat_mx_swiglu_quantize(gu: torch.Tensor, xq: Optional[torch.Tensor] = None,
                            xs: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The 4-bit form of silu(g) u for gu [n, 2 d] = [g | u]."""
+    if xq is None and xs is None:
+        r = (_mx_native or _calls()).swiglu_quantize(gu)
+        if type(r) is tuple:
+            return r
+        if r is not None:
+            _check("cat_mx_swiglu_quantize", r)
     _need(gu, "gu")
     n, d2 = gu.shape
     if d2 % 2:
         raise ValueError(f"gu has {d2} columns, expected an even number")
-    d = d2 // 2
-    xq, xs = _mx_out(xq, xs, n, d, gu.device)
-    st = _mx_library().cat_mx_swiglu_quantize(gu.data_ptr(), _dtype(gu), n, d, xq.data_ptr(), xs.data_ptr(), _mx_stream(gu))
-    if st:
-        _check("cat_mx_swiglu_quantize", st)
+    xq, xs = _mx_out(xq, xs, n, d2 // 2, gu.device)
+    _check("cat_mx_swiglu_quantize", load_library().cat_mx_swiglu_quantize(_ptr(gu), _dtype(gu), n, d2 // 2, _ptr(xq), _ptr(xs),
+                                                                           _stream(gu.device)))
     return xq, xs
 
 
@@ -723,45 +738,44 @@ def cat_mx_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float, r
                             xs: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """h = x + residual, and the 4-bit form of h / sqrt(mean(h^2) + eps) * weight: (xq, xs, h).  ``h`` may be x or
     residual; without a residual it is x and nothing is written but the 4-bit form."""
+    if h is None and xq is None and xs is None:
+        r = (_mx_native or _calls()).rmsnorm_quantize(x, weight, eps, residual)
+        if type(r) is tuple:
+            return r
+        if r is not None:
+            _check("cat_mx_rmsnorm_quantize", r)
     _need(x, "x")
     n, d = x.shape
     dev = x.device
-    if not (weight.shape == (d,) and weight.is_contiguous() and weight.get_device() == x.get_device()):
-        _expect(weight, "weight", weight.dtype, (d,), dev)
+    _expect(weight, "weight", weight.dtype, (d,), dev)
     if residual is not None:
-        if not (residual.dtype is x.dtype and residual.shape == (n, d) and residual.is_contiguous()
-                and residual.get_device() == x.get_device()):
-            _expect(residual, "residual", x.dtype, (n, d), dev)
-        h = _empty((n, d), dtype=x.dtype, device=dev) if h is None else _given(h, "h", x.dtype, (n, d), dev)
+        _expect(residual, "residual", x.dtype, (n, d), dev)
+        h = _given(h, "h", x.dtype, (n, d), dev)
     elif h is not None:
         _expect(h, "h", x.dtype, (n, d), dev)
     xq, xs = _mx_out(xq, xs, n, d, dev)
-    st = _mx_library().cat_mx_rmsnorm_quantize(
-        x.data_ptr(), None if residual is None else residual.data_ptr(), _dtype(x), weight.data_ptr(), _dtype(weight), n, d,
-        eps, None if h is None else h.data_ptr(), xq.data_ptr(), xs.data_ptr(), _mx_stream(x))
-    if st:
-        _check("cat_mx_rmsnorm_quantize", st)
+    _check("cat_mx_rmsnorm_quantize", load_library().cat_mx_rmsnorm_quantize(
+        _ptr(x), _ptr(residual), _dtype(x), _ptr(weight), _dtype(weight), n, d, eps, _ptr(h), _ptr(xq), _ptr(xs), _stream(dev)))
     return xq, xs, x if h is None else h
 
 
 def cat_mx_linear(xq: torch.Tensor, xs: torch.Tensor, Wq: torch.Tensor, ws: torch.Tensor,
                   out_dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [n, d_out] = x W^T of 4-bit operands, summed in float32; y is float32 (default) or bfloat16."""
+    if y is None:
+        r = (_mx_native or _calls()).linear(xq, xs, Wq, ws, out_dtype)
+        if isinstance(r, torch.Tensor):
+            return r
+        if r is not None:
+            _check("cat_mx_linear", r)
     n, half = xq.shape
-    d_out, w_half = Wq.shape
-    dev, pitch = xq.device, (half + 255) // 256 * 16
-    if not (half == w_half and xq.dtype is _U8 is xs.dtype and Wq.dtype is _U8 is ws.dtype and xs.shape == (n, pitch)
-            and ws.shape == (d_out, pitch) and xq.is_contiguous() and xs.is_contiguous() and Wq.is_contiguous()
-            and ws.is_contiguous() and xq.get_device() == xs.get_device() == Wq.get_device() == ws.get_device() >= 0):
-        _expect(xq, "xq", _U8, (n, half), dev)
-        _expect(xs, "xs", _U8, (n, pitch), dev)
-        _expect(Wq, "Wq", _U8, (d_out, half), dev)
-        _expect(ws, "ws", _U8, (d_out, pitch), dev)
+    d_out = Wq.shape[0]
+    dev = xq.device
+    _mx_codes(xq, xs, ("xq", "xs"), (n,), half, dev)
+    _mx_codes(Wq, ws, ("Wq", "ws"), (d_out,), half, dev)
     y = _mx_result(y, "y", out_dtype, (n, d_out), dev)
-    st = _mx_library().cat_mx_linear(xq.data_ptr(), xs.data_ptr(), Wq.data_ptr(), ws.data_ptr(), n, 2 * half, d_out, _dtype(y),
-                                     y.data_ptr(), _mx_stream(xq))
-    if st:
-        _check("cat_mx_linear", st)
+    _check("cat_mx_linear", load_library().cat_mx_linear(_ptr(xq), _ptr(xs), _ptr(Wq), _ptr(ws), n, 2 * half, d_out, _dtype(y),
+                                                         _ptr(y), _stream(dev)))
     return y
 
 
@@ -769,23 +783,21 @@ def cat_mx_linear_grouped(xq: torch.Tensor, xs: torch.Tensor, Wq: torch.Tensor, 
                           out_dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [m, d_out]: rows offsets[e] to offsets[e + 1] of x times expert e's weights (Wq [experts, d_out, d / 2]);
     offsets int32 [experts + 1] on the device, ragged and empty groups allowed, rows of no group zero."""
+    if y is None:
+        r = (_mx_native or _calls()).linear_grouped(xq, xs, Wq, ws, offsets, out_dtype)
+        if isinstance(r, torch.Tensor):
+            return r
+        if r is not None:
+            _check("cat_mx_linear_grouped", r)
     m, half = xq.shape
-    experts, d_out, w_half = Wq.shape
-    dev, pitch = xq.device, (half + 255) // 256 * 16
-    if not (half == w_half and xq.dtype is _U8 is xs.dtype and Wq.dtype is _U8 is ws.dtype and xs.shape == (m, pitch)
-            and ws.shape == (experts, d_out, pitch) and xq.is_contiguous() and xs.is_contiguous() and Wq.is_contiguous()
-            and ws.is_contiguous() and xq.get_device() == xs.get_device() == Wq.get_device() == ws.get_device() >= 0):
-        _expect(xq, "xq", _U8, (m, half), dev)
-        _expect(xs, "xs", _U8, (m, pitch), dev)
-        _expect(Wq, "Wq", _U8, (experts, d_out, half), dev)
-        _expect(ws, "ws", _U8, (experts, d_out, pitch), dev)
+    experts, d_out = Wq.shape[0], Wq.shape[1]
+    dev = xq.device
+    _mx_codes(xq, xs, ("xq", "xs"), (m,), half, dev)
+    _mx_codes(Wq, ws, ("Wq", "ws"), (experts, d_out), half, dev)
     _expect(offsets, "offsets", torch.int32, (experts + 1,), dev)
     y = _mx_result(y, "y", out_dtype, (m, d_out), dev)
-    st = _mx_library().cat_mx_linear_grouped(
-        xq.data_ptr(), xs.data_ptr(), Wq.data_ptr(), ws.data_ptr(), offsets.data_ptr(), experts, m, 2 * half, d_out, _dtype(y),
-        y.data_ptr(), _mx_stream(xq))
-    if st:
-        _check("cat_mx_linear_grouped", st)
+    _check("cat_mx_linear_grouped", load_library().cat_mx_linear_grouped(
+        _ptr(xq), _ptr(xs), _ptr(Wq), _ptr(ws), _ptr(offsets), experts, m, 2 * half, d_out, _dtype(y), _ptr(y), _stream(dev)))
     return y
 
 

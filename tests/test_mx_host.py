@@ -119,3 +119,17 @@ def test_refusals(lib):
     assert e(None, None, None, None, None, 2, 0, 64, 8, 0, None, None) == 0
     f(P, P, P, P, 4, 72, 8, 0, P, None)
     assert b"multiple of 32" in lib.cat_last_error()
+
+
+def test_compiled_calls_leave_other_arguments_to_the_binding(lib):
+    """Tensors that are not on a GPU (or none at all) are not taken: None, and nothing has touched CUDA."""
+    import torch
+    calls = cat._calls()
+    x, u = torch.randn(4, 64), torch.zeros(4, 32, dtype=torch.uint8)
+    assert calls.quantize(x, None) is None and calls.quantize(3, None) is None and calls.swiglu_quantize(x) is None
+    assert calls.rmsnorm_quantize(x, x[0], 1e-5, None) is None and calls.dequantize(u, u, None) is None
+    assert calls.linear(u, u, u, u, None) is None and calls.linear_grouped(u, u, u, u, u, torch.float32) is None
+    with pytest.raises(TypeError):
+        calls.quantize(x)
+    with pytest.raises(ValueError):
+        cat.cat_mx_quantize(x)
