@@ -165,13 +165,15 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
     mma_commit(bar);
 }
 
-// Scales of 32 R rows, row 32 j + lane at src[32 kGroup j], to w[R i + j] = the word of blocks 4 i .. 4 i + 3; bytes from
-// `have` on are zero.
+// Scales of 32 R rows, 16 bytes of row 32 j + lane (half g of its 32), to w[R i + j] = the word of blocks 4 i .. 4 i + 3;
+// bytes from `have` on are zero.  The rows lie with the copy engine's 32-byte swizzle (halves change places in every
+// second four rows), which eight lanes' reads of a half take without bank conflicts.
 template <int R>
-__device__ __forceinline__ void load_scales(const uint4* src, int have, uint32_t* w) {
+__device__ __forceinline__ void load_scales(const uint8_t* src, int lane, int g, int have, uint32_t* w) {
+  const uint8_t* at = src + lane * kScaleRow + ((g ^ (lane >> 2 & 1)) << 4);
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    const uint4 v = src[32 * kGroup * j];
+    const uint4 v = *reinterpret_cast<const uint4*>(at + 32 * kScaleRow * j);
     w[j] = v.x;
     w[R + j] = v.y;
     w[2 * R + j] = v.z;
@@ -188,9 +190,9 @@ __device__ __forceinline__ void load_scales(const uint4* src, int have, uint32_t
   }
 }
 template <int R>
-__device__ __forceinline__ void store_scales(const uint4* src, int have, uint32_t taddr) {
+__device__ __forceinline__ void store_scales(const uint8_t* src, int lane, int g, int have, uint32_t taddr) {
   uint32_t w[4 * R];
-  load_scales<R>(src, have, w);
+  load_scales<R>(src, lane, g, have, w);
   if constexpr (R == 6) {
     tmem_st<16>(taddr, w);
     tmem_st<8>(taddr + 16, w + 16);
@@ -551,19 +553,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!sl.first() && !(ok = mbar_wait_bounded(&bars->tempty[slot], sl.free(), abort_flag, __LINE__, lim))) break;
         __syncwarp();
         tc_fence_after();
-        // row q of the group's scales: kGroup times 16 bytes
-        const uint4* src = reinterpret_cast<const uint4*>(ring + r * a.ring_bytes) + g;
+        const uint8_t* src = ring + r * a.ring_bytes;
         const uint32_t dst = scale0 + slot * slot_cols;
         // the last chunk's bytes behind the row's scales: the MMAs that cover them multiply zero codes, so any finite
         // scale will do
         const int have = a.d / 32 - c * 16;
         uint32_t w[16];
-        load_scales<4>(src + kGroup * lane, have, w);
+        load_scales<4>(src, lane, g, have, w);
         switch (a.xcols) {                         // 64 tokens a step
-          case 2: store_scales<2>(src + kGroup * (BM + lane), have, dst + 16); break;
-          case 4: store_scales<4>(src + kGroup * (BM + lane), have, dst + 16); break;
-          case 6: store_scales<6>(src + kGroup * (BM + lane), have, dst + 16); break;
-          default: store_scales<8>(src + kGroup * (BM + lane), have, dst + 16); break;
+          case 2: store_scales<2>(src + kScalesW, lane, g, have, dst + 16); break;
+          case 4: store_scales<4>(src + kScalesW, lane, g, have, dst + 16); break;
+          case 6: store_scales<6>(src + kScalesW, lane, g, have, dst + 16); break;
+          default: store_scales<8>(src + kScalesW, lane, g, have, dst + 16); break;
         }
         tmem_st<16>(dst, w);
         tmem_st_wait();
@@ -572,13 +573,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool last = g == kGroup - 1 || c == c1 - 1;
         if (last) rg.next(kRing);
         if (lane == 0) {
-          if (last) mbar_arrive(&bars->sempty[r]);
           if (CG == 2 && rank == 1)
             mbar_arrive(&bars->tready[slot]);
           else if (CG == 2 && warp == kScaleWarp0)
             mbar_arrive_expect_tx(&bars->tfull[slot], 4u);   // the odd CTA's signal completes the slot
           else
             mbar_arrive(&bars->tfull[slot]);
+          if (last) mbar_arrive(&bars->sempty[r]);
         }
       }
   } else if (warp >= kEpiWarp0) {
@@ -734,7 +735,7 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// Bytes [rows][row_bytes], box [box_rows][box_bytes], out-of-range reads zero.
+// Bytes [rows][row_bytes], box [box_rows][box_bytes] with a swizzle of its row, out-of-range reads zero.
 bool make_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t row_bytes, int box_rows, int box_bytes) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
@@ -743,7 +744,7 @@ bool make_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t row_b
   cuuint32_t box[2] = {(cuuint32_t)box_bytes, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_32B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
