@@ -783,9 +783,10 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   a.nt = nt;
   a.split = split;
   a.split_log = split == 8 ? 3 : split / 2;
-  // boxes of a whole tile's tokens, or with groups, whose tiles differ, of up to 64
-  a.bx = c.offsets && nt / CG > 64 ? 64 : nt / CG;
-  a.bxs = c.offsets && nt > 64 ? 64 : nt;
+  // boxes of a whole tile's tokens, or with groups, whose tiles differ, of up to 32 a CTA (64 for pairs: many rows)
+  constexpr int kGroupBox = 32 * CG;
+  a.bx = c.offsets && nt / CG > kGroupBox ? kGroupBox : nt / CG;
+  a.bxs = c.offsets && nt > kGroupBox ? kGroupBox : nt;
   a.xcols = 2 * ((nt + 63) / 64);
   const int npad = (nt + 31) / 32 * 32, slot_cols = 16 + 4 * a.xcols;
   a.acc_bufs = 2 * npad + 2 * slot_cols <= (int)kTmemCols ? 2 : 1;
@@ -842,23 +843,68 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   return cudaLaunchKernelEx(&cfg, mx_gemm_kernel<CG, T>, tw, tx, tws, txs, a);
 }
 
+// What a call runs on: pairs or single CTAs, the most tokens of a tile, the CTAs that share a tile's K.
+struct Form {
+  int cg, nt, split;
+};
+
+// The form of least estimated time.  A round of tiles costs its K steps, at least 0.28 us each (a stage's turn) and a little
+// for its tokens, whatever is between 8 and 256 of them; so as few rounds as can be, and in them the narrowest tiles.  With
+// many CTAs a step takes what its bytes do: the weights from memory (6 TB/s), all operands from L2 (16 TB/s).  The
+// constants (us) are fitted to bf16 outputs of 1 to 512 tokens on 4096 -> 6144, 4096 -> 14336, 14336 -> 4096,
+// 4096 -> 4096, 1024 -> 1024 and 2048 -> 640, within 15 % of each time: one token, 4096 -> 6144: K in two 8.1, whole 9.2;
+// 128 tokens, 14336 -> 4096: K in four 14.2, in two (64-wide) 16.0, pairs 20.8; 200, 4096 -> 14336: pairs (one round) 13.0,
+// single CTAs (two) 16.4; 512, 4096 -> 4096: 128-wide 11.0, 256-wide 12.3.
+Form pick_form(int64_t groups, int64_t rows, int64_t d, int64_t d_out) {
+  const int64_t sms = sm_count(), chunks = (d + kChunk - 1) / kChunk;
+  const double steps = (double)((d + BK - 1) / BK);
+  // clusters that are resident at once (a cluster stays within a group of 14 to 22 SMs)
+  const int64_t resident[4] = {sms, sms / 2, sms * 36 / 152, sms * 15 / 152};
+  Form best = {2, 256, 1};
+  double least = 1e30;
+  auto consider = [&](int cg, int split, int64_t at_once) {
+    const int64_t unit = 8 * cg, widest = 128 * cg, channel_tiles = groups * ((d_out + cg * BM - 1) / (cg * BM));
+    const int64_t fewest = (rows + widest - 1) / widest;
+    const int64_t rounds = (fewest * channel_tiles + at_once - 1) / at_once;
+    if (split > 1 && rounds > 1) return;          // (a split tile has a cluster of its own, launched with the others)
+    const int64_t narrow = split > 1 ? 32 : 64, most = (rows + narrow - 1) / narrow;
+    int64_t tiles = rounds * at_once / channel_tiles;
+    tiles = tiles < fewest ? fewest : tiles > most ? (most < fewest ? fewest : most) : tiles;
+    const int64_t nt = up((rows + tiles - 1) / tiles, unit);
+    const double active = (double)(cg * split * (tiles * channel_tiles < at_once ? tiles * channel_tiles : at_once));
+    const double streams = (double)(cg * split * (channel_tiles < at_once ? channel_tiles : at_once));   // of weights
+    const double from_memory = 0.0029 * streams, from_l2 = active * (18.4 + 0.144 * nt / cg) / 16000.0;
+    double step = cg == 1 ? 0.28 + 0.0003 * nt : 0.29 + 0.0002 * nt;
+    step = step < from_memory ? from_memory : step;
+    step = step < from_l2 ? from_l2 : step;
+    double us = rounds * steps / split * step;
+    if (cg == 1)
+      us += 4.0 + 0.004 * nt + (split > 1 ? 0.7 + 0.02 * nt : 0.0);
+    else   // (past 160 tokens there is one accumulator: a tile's MMAs wait for the one before to be read)
+      us += 4.6 + (nt > 160 ? rounds : 1) * (1.2 + 0.004 * nt);
+    if (us < least) {
+      least = us;
+      best = {cg, (int)nt, split};
+    }
+  };
+  consider(1, 1, resident[0]);
+  for (int k = 1; k < 4; ++k)
+    if ((1 << k) <= chunks) consider(1, 1 << k, resident[k]);
+  consider(2, 1, sms / 2);
+  return best;
+}
+
 template <typename T>
 cudaError_t launch_typed(const Call& c) {
-  const int64_t busy = c.offsets ? (c.experts < c.m ? c.experts : c.m) : 1;   // groups with rows, at most
-  const int64_t rows = (c.m + busy - 1) / busy;                               // rows of a group, on average
-  const bool pair = rows > 128;
-  if (pair) {
-    const int64_t tiles = (rows + 255) / 256;
-    const int nt = c.offsets ? 256 : (int)up((c.m + tiles - 1) / tiles, 16);
-    return launch_form<2, T>(c, nt, 1);
+  const int64_t groups = c.offsets ? (c.experts < c.m ? c.experts : c.m) : 1;   // with rows, at most
+  const int64_t rows = (c.m + groups - 1) / groups;                             // of each, on average
+  Form f = pick_form(groups, rows, c.d, c.d_out);
+  if (c.offsets) {
+    // the host knows no group's rows: tiles have room for four times the average (each takes what its group needs)
+    const int64_t room = up(c.m < 4 * rows ? c.m : 4 * rows, 8 * f.cg), widest = 128 * f.cg;
+    f.nt = (int)(room < widest ? room : widest);
   }
-  // one CTA a tile; K over the CTAs of a cluster where tiles leave SMs idle
-  const int nt = (int)up(c.offsets ? (c.m < 2 * rows ? c.m : 2 * rows) : c.m, 8);
-  const int n128 = nt < 128 ? nt : 128;
-  const int64_t tiles = busy * ((c.d_out + BM - 1) / BM), chunks = (c.d + kChunk - 1) / kChunk;
-  int split = 1;
-  while (split < 8 && 2 * split * tiles <= sm_count() && 2 * split <= chunks) split *= 2;
-  return launch_form<1, T>(c, n128, split);
+  return f.cg == 2 ? launch_form<2, T>(c, f.nt, 1) : launch_form<1, T>(c, f.nt, f.split);
 }
 
 }  // namespace
