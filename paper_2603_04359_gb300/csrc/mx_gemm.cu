@@ -74,7 +74,6 @@ struct Bars {
   uint32_t fwd_stage[kMaxStages], fwd_slot[kMaxSlots], fwd_acc[kEpiWarps];   // even CTA: targets of the odd CTA's st.async
   uint32_t tmem_addr;
   int abort;
-  int total;                                                  // grouped: tiles of the launch
 };
 
 // A place in a ring of buffers and the parity of its round: next() in step with the ring's other side.
@@ -248,25 +247,32 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Grouped: one warp fills the table: rows[e], the first row of expert e (rows[experts]: one past the last), and
-// tiles[e], the tiles of the experts before it.  Offsets are taken in order and within [0, m], whatever they are.
-__device__ __forceinline__ void make_table(const MxArgs& a, int* rows, int* tiles, int channel_tiles, int* total) {
-  const int lane = threadIdx.x & 31;
-  int high = 0, sum = 0;                    // the largest offset and the tiles so far
-  for (int e0 = 0; e0 <= a.experts; e0 += 32) {
+// Grouped: all threads fill the table: rows[e], the first row of expert e (rows[experts]: one past the last), and
+// tiles[e], the tiles of the experts before it (tiles[experts]: all).  Offsets are taken in order and within [0, m],
+// whatever they are.  Scans by warps of 32 entries each, then the 32s' totals: one round trip to memory.
+constexpr int kMaxChunks = (int)kMxMaxExperts / 32 + 1;
+__device__ __forceinline__ void make_table(const MxArgs& a, int* rows, int* tiles, int channel_tiles, int* totals) {
+  const int lane = threadIdx.x & 31, first = threadIdx.x & ~31;
+  const int entries = a.experts + 1;
+  for (int e0 = first; e0 < entries; e0 += kThreads) {
     const int e = e0 + lane;
-    int o = e <= a.experts ? min(max(a.offsets[e], 0), a.m) : a.m;
+    int o = e < entries ? min(max(a.offsets[e], 0), a.m) : 0;
 #pragma unroll
     for (int k = 1; k < 32; k <<= 1) {
       const int v = __shfl_up_sync(0xFFFFFFFFu, o, k);
       if (lane >= k) o = max(o, v);
     }
-    o = max(o, high);
-    if (e <= a.experts) rows[e] = o;
-    high = __shfl_sync(0xFFFFFFFFu, o, 31);
+    if (e < entries) rows[e] = o;
+    if (lane == 31) totals[e0 / 32] = o;
   }
-  __syncwarp();
-  for (int e0 = 0; e0 < a.experts; e0 += 32) {
+  __syncthreads();
+  for (int e = threadIdx.x; e < entries; e += kThreads) {
+    int o = rows[e];
+    for (int c = 0; c < e / 32; ++c) o = max(o, totals[c]);
+    rows[e] = o;
+  }
+  __syncthreads();
+  for (int e0 = first; e0 < entries; e0 += kThreads) {
     const int e = e0 + lane;
     const int mine = e < a.experts ? (rows[e + 1] - rows[e] + a.nt - 1) / a.nt * channel_tiles : 0;
     int s = mine;
@@ -275,12 +281,14 @@ __device__ __forceinline__ void make_table(const MxArgs& a, int* rows, int* tile
       const int v = __shfl_up_sync(0xFFFFFFFFu, s, k);
       if (lane >= k) s += v;
     }
-    if (e < a.experts) tiles[e] = sum + s - mine;
-    sum += __shfl_sync(0xFFFFFFFFu, s, 31);
+    if (e < entries) tiles[e] = s - mine;
+    if (lane == 31) totals[kMaxChunks + e0 / 32] = s;
   }
-  if (lane == 0) {
-    tiles[a.experts] = sum;
-    *total = sum;
+  __syncthreads();
+  for (int e = threadIdx.x; e < entries; e += kThreads) {
+    int s = tiles[e];
+    for (int c = 0; c < e / 32; ++c) s += totals[kMaxChunks + c];
+    tiles[e] = s;
   }
 }
 
@@ -342,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   pdl_wait_then_release();                       // nothing global or in tensor memory before this
   const uint64_t lim = g_mx_wait_limit;
-  if (a.offsets && warp == 1) make_table(a, rows, tiles, channel_tiles, &bars->total);
+  if (a.offsets) make_table(a, rows, tiles, channel_tiles, tiles + a.experts + 1);
   if (warp == 2) {
     if constexpr (CG == 2)
       tmem_alloc_pair(&bars->tmem_addr, kTmemCols);
@@ -359,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, bars->tmem_addr, 0);
   const int token_tiles = (a.m + a.nt - 1) / a.nt;
-  const int total = a.offsets ? bars->total : token_tiles * channel_tiles;
+  const int total = a.offsets ? tiles[a.experts] : token_tiles * channel_tiles;
 
   if (a.offsets) {                               // rows of no group
     const int64_t head = (int64_t)rows[0] * a.d_out, from = (int64_t)rows[a.experts] * a.d_out,
@@ -374,7 +382,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     Tile t;
     int begin = 0, end = a.m, tt, ct, n_tiles = token_tiles;
     if (a.offsets) {
-      while (u >= tiles[e + 1]) ++e;
+      for (int last = a.experts - 1; e < last;) {   // the last expert that begins at u or before (the others there are empty)
+        const int mid = (e + last + 1) / 2;
+        if (tiles[mid] <= u) e = mid;
+        else last = mid - 1;
+      }
       begin = rows[e];
       end = rows[e + 1];
       u -= tiles[e];
@@ -795,7 +807,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   a.stage_bytes = kStageW + (uint32_t)up(nt / CG, a.bx) * 128u;
   a.ring_bytes = kScalesW + (uint32_t)up(up(nt, a.bxs), 64) * kScaleRow;
   const size_t red = split > 1 ? (size_t)split * ((nt + split - 1) / split) * BM * 4 : 0;
-  const size_t table = c.offsets ? up(2 * (c.experts + 1) * 4, 128) : 0;
+  const size_t table = c.offsets ? up((2 * (c.experts + 1) + 2 * kMaxChunks) * 4, 128) : 0;
   const size_t rest = (size_t)kRing * a.ring_bytes + 2 * kStageOut + red + table + sizeof(Bars) + 1024;
   const int stages = (int)((kMaxSmem - rest) / a.stage_bytes);
   a.stages = stages < kMaxStages ? stages : kMaxStages;
