@@ -418,12 +418,12 @@ cat_status cat_linear_dp(const uint8_t* x_planes, int32_t bits_x, int32_t asym_x
 
 /*
  * cat_set_wait_limit_ns -- testing aid, no counterpart in the paper.  Sets, on the current device, the
- * bound of the pipeline waits of the weight-streaming W4A4 GEMM (cat_w4a4_linear, n <= 32) and of the
- * digit-plane GEMM (cat_linear_dp); 0 restores the default of 1 s (1e9 ns, also the largest value
+ * bound of the pipeline waits of the weight-streaming W4A4 GEMM (cat_w4a4_linear, n <= 32), of the
+ * digit-plane GEMM (cat_linear_dp) and of the microscaled products (cat_mx_linear, cat_mx_linear_grouped); 0 restores the default of 1 s (1e9 ns, also the largest value
  * accepted).  A wait that exceeds its bound gives up: the kernel drains its copies and MMAs in flight
  * (those waits keep the 1 s bound), frees its tensor memory, returns, and raises CAT_ERR_TIMEOUT in the
- * device status word with the kernel's bit (1 << 11 weight-streaming GEMM, 1 << 13 digit-plane GEMM)
- * and the source line of the first wait that gave up in bits 16..31.  Its outputs are then undefined.
+ * device status word with the kernel's bit (1 << 11 weight-streaming GEMM, 1 << 13 digit-plane GEMM,
+ * 1 << 14 microscaled products) and the source line of the first wait that gave up in bits 16..31.  Its outputs are then undefined.
  * Synchronous (a blocking copy to the device); not for use while those kernels run.
  */
 cat_status cat_set_wait_limit_ns(uint64_t ns);
@@ -497,7 +497,7 @@ cat_status cat_alignment_ceiling_host(const double* sigma_x, const double* sigma
  * quantizer is the uniform one; the transforms go before it all the same (cat_block_transform's x' = T x and
  * W' = W T^{-1} are what cat_mx_quantize then takes).
  *
- * A row of d values (d a multiple of 32, at most 262144) is
+ * Numbers of rows, and experts * d_out, are at most 2^31 - 512.  A row of d values (d a multiple of 32, at most 262144) is
  *   codes   d/2 bytes: E2M1 codes, value 2j in the low nibble of byte j.  Bit 3 is the sign, bits 0-2 the
  *           magnitude: 0, 0.5, 1, 1.5, 2, 3, 4, 6;
  *   scales  cat_mx_scale_pitch(d) bytes: d/32 rounded up to a multiple of 16.  Byte j < d/32 is the scale

@@ -947,10 +947,12 @@ cat_status cat_alignment_ceiling_host(const double* sigma_x, const double* sigma
 
 // ---- microscaled 4-bit floating point
 
+static constexpr int64_t kMaxMxRows = 0x7FFFFE00;   // rows of a tile past the end still have int32 numbers
+
 static cat_status check_mx(int64_t n, int64_t d) {
   if (n < 0) return fail(CAT_ERR_SHAPE, "the number of rows must be >= 0");
   if (d <= 0 || d % 32 != 0 || d > kMaxDin) return fail(CAT_ERR_SHAPE, "d must be a positive multiple of 32, at most 262144");
-  if (n > 0x7FFFFFFF) return fail(CAT_ERR_SHAPE, "the number of rows must fit in int32");
+  if (n > kMaxMxRows) return fail(CAT_ERR_SHAPE, "too many rows (more than 2^31 - 512)");
   return CAT_OK;
 }
 
@@ -1035,7 +1037,7 @@ cat_status cat_mx_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* Wq
   if (!known(out_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
   cat_status st = check_mx(n, d);
   if (st != CAT_OK) return st;
-  if (d_out <= 0 || d_out > 0x7FFFFFFF) return fail(CAT_ERR_SHAPE, "d_out must be >= 1 and fit in int32");
+  if (d_out <= 0 || d_out > kMaxMxRows) return fail(CAT_ERR_SHAPE, "d_out must be in [1, 2^31 - 512]");
   if (n == 0) return ok();
   if (!xq || !xs || !Wq || !ws || !y) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
   if (!aligned16(xq) || !aligned16(xs) || !aligned16(Wq) || !aligned16(ws) || !aligned16(y))
@@ -1052,7 +1054,7 @@ cat_status cat_mx_linear_grouped(const uint8_t* xq, const uint8_t* xs, const uin
   cat_status st = check_mx(m, d);
   if (st != CAT_OK) return st;
   if (experts < 1 || experts > cat::kMxMaxExperts) return fail(CAT_ERR_SHAPE, "experts must be in [1, 1024]");
-  if (d_out <= 0 || d_out > 0x7FFFFFFF / experts) return fail(CAT_ERR_SHAPE, "d_out must be >= 1 and experts * d_out fit in int32");
+  if (d_out <= 0 || d_out > kMaxMxRows / experts) return fail(CAT_ERR_SHAPE, "d_out must be >= 1 and experts * d_out at most 2^31 - 512");
   if (m == 0) return ok();
   if (!xq || !xs || !Wq || !ws || !offsets || !y) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
   if (!aligned16(xq) || !aligned16(xs) || !aligned16(Wq) || !aligned16(ws) || !aligned16(offsets) || !aligned16(y))

@@ -95,12 +95,15 @@ struct Place {
 __device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int line, uint64_t limit) {
   return (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort, line, limit));
 }
-// Waits for the last fillings of a ring's buffers, `at` its next place.
+// Waits for the last fillings of a ring's buffers, `at` its next place: at most kWaitLimitNs in all (after a wait that gave
+// up, a buffer's other signal may never come).
 __device__ __forceinline__ void drain(uint64_t* full, Place at, uint32_t of) {
   volatile int no_abort = 0;
+  const uint64_t t0 = globaltimer_ns();
   for (uint32_t b = 0; b < of; ++b) {
     const uint32_t fills = at.round + (b < at.at ? 1u : 0u);
-    if (fills > 0) mbar_wait_bounded(&full[b], (fills - 1) & 1, &no_abort);
+    const uint64_t spent = globaltimer_ns() - t0;
+    if (fills > 0) mbar_wait_bounded(&full[b], (fills - 1) & 1, &no_abort, 1, spent < kWaitLimitNs ? kWaitLimitNs - spent : 1);
   }
 }
 
@@ -219,6 +222,9 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
 // The four warps of an epilogue half, in step.
+// Named barrier 4: warp 2 has asked for the first scales, warp 0 goes on behind it.
+__device__ __forceinline__ void first_scales_arrive() { asm volatile("bar.arrive 4, 64;" ::: "memory"); }
+__device__ __forceinline__ void first_scales_sync() { asm volatile("bar.sync 4, 64;" ::: "memory"); }
 __device__ __forceinline__ void epi_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory"); }
 
 __device__ __forceinline__ bool epi_all(int half, bool ok) {
@@ -419,6 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA of codes
     // (here too all lanes go through the loop and one is elected: a copy issued in a branch of lane 0's took ~300 cycles)
+    first_scales_sync();                           // copies are made in the order they are asked for, and MMAs need both
     Place st;
     bool ok = true;
     int e = 0;
@@ -445,6 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) drain(CG == 2 && rank == 1 ? bars->ready : bars->full, st, a.stages);
   } else if (warp == 2) {
     // ---------------------------------------------------------------- TMA of scales
+    bool told = false;                             // the codes' warp, that the first are asked for
     Place rg;
     bool ok = true;
     int e = 0;
@@ -464,8 +472,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             tma_load_2d(dst + kScalesW + (uint32_t)(b * a.bxs * kScaleRow), &tmXs, c * 16, t.t0 + b * a.bxs, fb);
         }
         __syncwarp();
+        if (!told) first_scales_arrive();
+        told = true;
       }
     }
+    if (!told) first_scales_arrive();
     if (lane == 0) drain(bars->sfull, rg, kRing);
   } else if (CG == 2 && rank == 1 && (warp == 1 || warp == 3)) {
     // ---------------------------------------------------------------- odd CTA: forward stages (1) and scale slots (3)
@@ -542,11 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       volatile int no_abort = 0;
       mbar_wait_bounded(&bars->mma_done, 0, &no_abort);
-      // the odd CTA's last signals have landed before this CTA exits
-      for (uint32_t b = 0; CG == 2 && b < (uint32_t)a.acc_bufs; ++b) {
-        const uint32_t uses = ac.round + (b < ac.at ? 1u : 0u);
-        if (uses > 0) mbar_wait_bounded(&bars->acc_empty[b], (uses - 1) & 1, &no_abort);
-      }
+      if (CG == 2) drain(bars->acc_empty, ac, a.acc_bufs);   // the odd CTA's last signals have landed
     }
   } else if (warp >= kScaleWarp0 && warp < kScaleWarp0 + kScaleWarps) {
     // ---------------------------------------------------------------- scales to tensor memory

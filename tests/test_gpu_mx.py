@@ -317,6 +317,79 @@ def test_grouped_is_the_linear_of_each_group():
     check_product(y, x, w)
 
 
+def nan_rows(s, rows):
+    s = s.clone()
+    s[rows] = 255
+    return s
+
+
+@pytest.mark.parametrize("counts,d,d_out", [([3, 0, 5, 1], 512, 200), ([300, 20, 500], 1056, 384)])
+def test_grouped_products_use_their_own_rows_alone(counts, d, d_out):
+    """NaN scales in all of the other experts' rows and weights, and in the rows of no group, do not reach a group."""
+    rng = np.random.default_rng(11)
+    m = sum(counts) + 9
+    edges = 4 + np.concatenate([[0], np.cumsum(counts)])
+    xq, xs, x = operand(rng, m, d)
+    wq, ws, w = operand(rng, len(counts) * d_out, d)
+    w, wq, ws = (t.view(len(counts), d_out, -1) for t in (w, wq, ws))
+    for e in range(len(counts)):
+        mine = slice(edges[e], edges[e + 1])
+        others = torch.ones(m, dtype=torch.bool, device=DEV)
+        others[mine] = False
+        other_w = torch.arange(len(counts), device=DEV) != e
+        y = cat.cat_mx_linear_grouped(xq, nan_rows(xs, others), wq, nan_rows(ws, other_w), dev(edges.astype(np.int32)))
+        if counts[e]:
+            check_product(y[mine], x[mine], w[e])
+        assert not y[:4].any() and not y[-5:].any()
+
+
+def test_sizes_past_32_bits():
+    """Outputs, values and codes whose element numbers and byte offsets need more than 32 bits: the last rows are right."""
+    rng = np.random.default_rng(12)
+    n, d, d_out = 70001, 64, 65536
+    xq, xs, _ = operand(rng, n, d)
+    wq, ws, w = operand(rng, d_out, d)
+    y = cat.cat_mx_linear(xq, xs, wq, ws, out_dtype=torch.bfloat16)
+    tail = slice(n - 40, n)
+    check_product(y[tail], cat.cat_mx_dequantize(xq[tail].contiguous(), xs[tail].contiguous()).double(), w)
+    grouped = cat.cat_mx_linear_grouped(xq, xs, wq[None], ws[None], dev(np.array([30, n - 20], dtype=np.int32)),
+                                        out_dtype=torch.bfloat16)
+    assert torch.equal(grouped[n - 40:n - 20], y[n - 40:n - 20]) and not grouped[n - 20:].any() and not grouped[:30].any()
+    del y, grouped
+    n, d = 140001, 32768
+    x = torch.zeros((n, d), dtype=torch.bfloat16, device=DEV)
+    x[-2:] = torch.randn((2, d), device=DEV)
+    xq, xs = cat.cat_mx_quantize(x)
+    same_form(xq[-2:], xs[-2:], *R.quantize(host(x[-2:])))
+    v = cat.cat_mx_dequantize(xq, xs, out_dtype=torch.bfloat16)
+    assert torch.equal(v[-2:], cat.cat_mx_dequantize(xq[-2:].contiguous(), xs[-2:].contiguous(), out_dtype=torch.bfloat16))
+    assert not v[:-2].any()
+    del v
+    hq, hs, h = cat.cat_mx_rmsnorm_quantize(x, torch.ones(d, device=DEV), 1e-5, residual=x)
+    last = cat.cat_mx_rmsnorm_quantize(x[-2:].contiguous(), torch.ones(d, device=DEV), 1e-5, residual=x[-2:].contiguous())
+    assert torch.equal(hq[-2:], last[0]) and torch.equal(hs[-2:], last[1]) and torch.equal(h[-2:], last[2])
+
+
+@pytest.mark.parametrize("n,d,d_out", [(40, 131072, 1024), (16, 65536, 8192), (1000, 65536, 4096)],
+                         ids=["split", "single", "pairs"])
+def test_bounded_wait_gives_up_then_library_recovers(n, d, d_out):
+    """Waits that run out (a bound of 1 ns): the kernel drains, returns and says so; the next call is right."""
+    rng = np.random.default_rng(13)
+    xq, xs, x = operand(rng, n, d)
+    wq, ws, w = operand(rng, d_out, d)
+    assert cat.cat_device_status()[0] == 0
+    try:
+        cat.cat_set_wait_limit_ns(1)
+        cat.cat_mx_linear(xq, xs, wq, ws)
+        st, word = cat.cat_device_status()
+    finally:
+        cat.cat_set_wait_limit_ns(0)
+    assert st == 7 and word & 1 and word & 1 << 14 and word >> 16, hex(word)
+    for _ in range(2):
+        check_product(cat.cat_mx_linear(xq, xs, wq, ws), x, w)
+    assert cat.cat_device_status()[0] == 0
+
+
 def test_on_several_streams():
     """Calls of all kinds on streams of their own, at once."""
     rng = np.random.default_rng(8)

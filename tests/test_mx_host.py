@@ -7,7 +7,7 @@ import pytest
 import mx_reference as R
 import paper_2603_04359_gb300 as cat
 from paper_2603_04359_gb300 import build as catbuild
-from fake_runtime import ensure_built
+from fake_runtime import FakeRuntime, ensure_built
 
 P, BAD = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10008)
 NAN, INF = float("nan"), float("inf")
@@ -133,3 +133,70 @@ def test_compiled_calls_leave_other_arguments_to_the_binding(lib):
         calls.quantize(x)
     with pytest.raises(ValueError):
         cat.cat_mx_quantize(x)
+
+
+A = 0x10 << 40          # an address that holds nothing
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    return FakeRuntime(tmp_path_factory.mktemp("fake_mx"))
+
+
+def form(launch):
+    """pairs or single CTAs, CTAs a cluster."""
+    cg = 2 if "mx_gemm_kernel<2" in launch.kernel else 1
+    return (cg, launch.cluster, launch.grid)
+
+
+@pytest.mark.parametrize("n,d,d_out,cg,cluster,grid", [
+    (1, 4096, 6144, 1, 2, 96), (1, 4096, 4096, 1, 4, 128), (27, 14336, 4096, 1, 4, 128), (16, 4096, 14336, 1, 1, 112),
+    (1, 8192, 28672, 1, 1, 152), (128, 14336, 4096, 1, 4, 128), (200, 4096, 14336, 2, 2, 112), (201, 4096, 6144, 1, 1, 144),
+    (512, 4096, 4096, 1, 1, 128), (2048, 4096, 6144, 2, 2, 152), (8192, 8192, 28672, 2, 2, 152), (1, 256, 256, 1, 1, 2),
+])
+def test_products_take_the_form_of_least_time(fake, n, d, d_out, cg, cluster, grid):
+    """The forms that were measured fastest, on 152 SMs."""
+    launch, = fake.call("cat_mx_linear", A, A, A, A, n, d, d_out, 1, A, None)
+    assert form(launch) == (cg, cluster, grid)
+    # a cluster leaves no room on its SMs for another kernel's CTA with tensor memory of its own
+    assert launch.smem >= (215 if cluster > 1 else 120) * 1024
+
+
+def mx_calls(fake):
+    for dtype in (0, 1):
+        for n, d in ((1, 32), (3, 4096), (5000, 8192), (2, 262144)):
+            yield "cat_mx_quantize", A, dtype, n, d, None, n, A, A, None
+            yield "cat_mx_quantize", A, dtype, n, d, A, 2 * n, A, A, None
+            yield "cat_mx_swiglu_quantize", A, dtype, n, d, A, A, None
+            yield "cat_mx_dequantize", A, A, n, d, dtype, A, None
+            for weight in (0, 1):
+                yield "cat_mx_rmsnorm_quantize", A, A, dtype, A, weight, n, d, 1e-5, A, A, A, None
+        for n, d, d_out in ((1, 32, 1), (1, 4096, 4096), (1, 4096, 1000), (40, 4096, 6144), (300, 1120, 4097), (5000, 14336, 8192)):
+            yield "cat_mx_linear", A, A, A, A, n, d, d_out, dtype, A, None
+            for experts in (1, 7, 1024):
+                yield "cat_mx_linear_grouped", A, A, A, A, A, experts, n, d, d_out, dtype, A, None
+
+
+def test_every_launch_is_allowed_on_every_device(fake):
+    first, second = [], []
+    for found, device in ((first, 2), (second, 6)):
+        fake.device(device)
+        for name, *args in mx_calls(fake):
+            launches = fake.call(name, *args)
+            assert len(launches) == 1, (name, args)                 # one launch a call, without scratch or memsets
+            found += launches
+    fake.device(0)
+    assert [x._replace(device=0) for x in first] == [x._replace(device=0) for x in second]
+    assert {x.device for x in second} == {6}
+
+
+@pytest.mark.parametrize("n,d_out,groups,rows", [(1, 6144, None, [128, 8, 128, 8]), (201, 6144, None, [128, 72, 128, 72]),
+                                                 (8192, 28672, None, [128, 128, 128, 256]), (16, 14336, 8, [128, 8, 128, 8]),
+                                                 (4096, 14336, 8, [128, 64, 128, 64])])
+def test_products_load_the_token_rows_there_are(fake, n, d_out, groups, rows):
+    """Boxes: the weights' codes, the tokens', and the same of the scales."""
+    if groups:
+        fake.call("cat_mx_linear_grouped", A, A, A, A, A, groups, n, 4096, d_out, 1, A, None)
+    else:
+        fake.call("cat_mx_linear", A, A, A, A, n, 4096 if n < 8192 else 8192, d_out, 1, A, None)
+    assert fake.box_rows() == rows
