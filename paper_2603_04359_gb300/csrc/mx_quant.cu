@@ -276,7 +276,7 @@ __device__ __forceinline__ bool finish_oct(const NormOut& out, const W* weight, 
     if (out.h) store_oct(static_cast<T*>(out.h) + at * 8, a);
     const Oct w = load_weights(weight + (int64_t)oct * 8);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v.v[k] = a.v[k] * r * w.v[k];
+    for (int k = 0; k < 8; ++k) v.v[k] = a.v[k] * w.v[k] * r;   // (bf16 times bf16 is mostly exact: one rounding, of the last product)
   }
   uint32_t b;
   const uint32_t c = quantize_oct(v, &b);
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kThreads) mx_rmsnorm_warp_kernel(const T* x, c
         sq = squares(a[j], sq);
       }
     }
-    const float r = 1.f / sqrtf(warp_sum(sq) / (float)(octs * 8) + eps);
+    const float r = __frsqrt_rn(warp_sum(sq) / (float)(octs * 8) + eps);
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j)
       if (32 * j < octs) bad |= finish_oct<T>(out, weight, row, 32 * j + lane, a[j], r);
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(1024) mx_rmsnorm_row_kernel(const T* x, const 
     sq = warp_sum(sq);
     if (lane == 0) part[turn][warp] = sq;
     __syncthreads();                                     // (part[] has two turns, so one barrier a row will do)
-    const float r = 1.f / sqrtf(warp_sum(lane < warps ? part[turn][lane] : 0.f) / (float)(octs * 8) + eps);
+    const float r = __frsqrt_rn(warp_sum(lane < warps ? part[turn][lane] : 0.f) / (float)(octs * 8) + eps);
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
       const int oct = j * blockDim.x + threadIdx.x;
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(1024) mx_rmsnorm_long_kernel(const T* x, const
     sq = warp_sum(sq);
     if (lane == 0) part[warp] = sq;
     __syncthreads();
-    const float r = 1.f / sqrtf(warp_sum(lane < warps ? part[lane] : 0.f) / (float)(octs * 8) + eps);
+    const float r = __frsqrt_rn(warp_sum(lane < warps ? part[lane] : 0.f) / (float)(octs * 8) + eps);
     for (int oct = threadIdx.x; oct - lane < octs; oct += blockDim.x)
       bad |= finish_oct<T>(out, weight, row, oct, oct < octs ? sum_of(oct) : Oct{}, r);
     __syncthreads();                                     // part[] is read before the next row's sums
