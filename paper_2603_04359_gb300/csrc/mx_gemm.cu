@@ -44,12 +44,14 @@ constexpr int kRing = 2, kGroup = 2, kScaleRow = 16 * kGroup;
 constexpr int kScaleWarp0 = 4, kScaleWarps = 4, kEpiWarp0 = 8, kEpiWarps = 8;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kStageW = BM * 128;      // 16 KiB of weight codes a stage
-constexpr uint32_t kStageOut = 8192;        // an epilogue half's outputs on their way: 32 bf16 or 16 float32 tokens
+constexpr uint32_t kStageOut = 4096;        // an epilogue half's outputs on their way: 16 bf16 or 8 float32 tokens
 constexpr uint32_t kScalesW = BM * kScaleRow;   // 4 KiB of weight scales a ring slot
 // Shared memory: at least half an SM's, as two CTAs would wait for each other's tensor memory.  Clusters take all but
 // 12 KB, whatever they need: a CTA that holds its SM's tensor memory while its cluster waits for another SM's must not
-// share the SM with a CTA of some other kernel of which the same holds (all that use tensor memory need more than 12 KB).
-constexpr size_t kMaxSmem = 215 * 1024, kMinSmem = 120 * 1024;
+// share the SM with a CTA of some other kernel of which the same holds (all that use tensor memory need more than 12 KB);
+// those 12 KB let the next call's CTAs come early.  Pairs take those too, for a sixth stage of 256-token tiles
+// (8192 x 8192 -> 28672 561 -> 545 us, 4096 x 14336 -> 4096 86 -> 79).
+constexpr size_t kPairSmem = 227 * 1024, kMaxSmem = 215 * 1024, kMinSmem = 120 * 1024;
 
 __device__ uint64_t g_mx_wait_limit = kWaitLimitNs;   // bound of the pipeline waits (cat_set_wait_limit_ns)
 
@@ -816,7 +818,8 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   const size_t red = split > 1 ? (size_t)split * ((nt + split - 1) / split) * BM * 4 : 0;
   const size_t table = c.offsets ? up((2 * (c.experts + 1) + 2 * kMaxChunks) * 4, 128) : 0;
   const size_t rest = (size_t)kRing * a.ring_bytes + 2 * kStageOut + red + table + sizeof(Bars) + 1024;
-  const int stages = (int)((kMaxSmem - rest) / a.stage_bytes);
+  const size_t most = CG == 2 ? kPairSmem : kMaxSmem;
+  const int stages = (int)((most - rest) / a.stage_bytes);
   a.stages = stages < kMaxStages ? stages : kMaxStages;
   if (a.slots < 2 || a.stages < 2 || nt % (8 * CG) != 0 || a.bx > 256 || a.bxs > 256) return cudaErrorInvalidConfiguration;
   a.off_ring = a.stages * a.stage_bytes;
@@ -826,7 +829,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   a.off_bars = a.off_table + (uint32_t)table;
   size_t smem = a.off_bars + sizeof(Bars) + 1024;
   if (smem < kMinSmem) smem = kMinSmem;
-  if (CG == 2 || split > 1) smem = kMaxSmem;
+  if (CG == 2 || split > 1) smem = most;
 
   CUtensorMap tw, tx, tws, txs;
   const int64_t pitch = mx_pitch(c.d), wrows = (c.offsets ? c.experts : 1) * c.d_out;
@@ -834,7 +837,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
       !make_map(&tws, c.ws, wrows, pitch, BM, kScaleRow) || !make_map(&txs, c.xs, c.m, pitch, a.bxs, kScaleRow))
     return cudaErrorInvalidValue;
   static PerDevice<cudaError_t> allowed;
-  const cudaError_t attr_err = allowed.get([] { return allow_smem(mx_gemm_kernel<CG, T>, kMaxSmem); });
+  const cudaError_t attr_err = allowed.get([] { return allow_smem(mx_gemm_kernel<CG, T>, CG == 2 ? kPairSmem : kMaxSmem); });
   if (attr_err != cudaSuccess) return attr_err;
 
   // at most this many tiles (with groups the device knows how many)
