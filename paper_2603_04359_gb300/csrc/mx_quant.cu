@@ -4,11 +4,10 @@
 // All are bound by the bytes that they move: every input is read once and the 4-bit form (17/32 of a byte a value) is
 // all that is written beside the norm's sum, so the norm's or SwiGLU's 16-bit output never goes through memory.
 //
-// A thread takes 8 consecutive values (16 bytes of bf16), four lanes a block of 32: the block's largest magnitude takes
-// two shuffles, a warp's codes are 128 consecutive bytes and its scales 8.  Memory gives an SM 22 bytes a cycle, a warp's
-// 256 bf16 values in 23: what bounds these kernels in practice are the instructions an octet takes (about 200 at first),
-// so bf16 values are compared and scaled two at a time, places are counted on instead of divided, and the row numbers of
-// a gather have a kernel of their own.
+// Memory gives an SM 22 bytes a cycle, 256 bf16 values in 23 cycles: what bounds these kernels in practice are the
+// instructions a value takes.  So a thread of the flat kernels takes 16 consecutive values in one 32-byte load, two lanes a
+// block of 32, bf16 values are compared and scaled two at a time, places are counted on instead of divided, and the row
+// numbers of a gather have a kernel of their own.  Codes leave 8 bytes a lane, a warp's scales are 16 neighbouring bytes.
 #include "mx_format.cuh"
 
 namespace cat {
@@ -76,29 +75,6 @@ __device__ __forceinline__ uint32_t quantize_oct(const Oct& o, uint32_t* scale_b
   for (int i = 0; i < 8; ++i) v[i] = o.v[i] * inv;
   return mx_pack8(v);
 }
-// The same of 8 bf16 values as they are stored.  Magnitudes are compared as 16-bit integers, two at a time (a NaN is the
-// largest); the scaling is exact in bf16 too (what underflows has the code 0 either way).
-__device__ __forceinline__ uint32_t quantize_oct(const uint4& w, uint32_t* scale_byte) {
-  constexpr uint32_t kMag = 0x7FFF7FFFu;
-  uint32_t a = __vmaxu2(__vmaxu2(w.x & kMag, w.y & kMag), __vmaxu2(w.z & kMag, w.w & kMag));
-  a = __vmaxu2(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-  a = __vmaxu2(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-  const uint32_t b = mx_scale_byte(max(a & 0xFFFF0000u, a << 16));
-  *scale_byte = b;
-  if (b == 255u) return 0u;
-  const __nv_bfloat162 inv = bf16_pair((254u - b) << 7);
-  const uint32_t r[4] = {w.x, w.y, w.z, w.w};
-  float v[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 p = __hmul2_rn(*reinterpret_cast<const __nv_bfloat162*>(&r[i]), inv);
-    const uint32_t q = *reinterpret_cast<const uint32_t*>(&p);
-    v[2 * i] = lo_f32(q);
-    v[2 * i + 1] = hi_f32(q);
-  }
-  return mx_pack8(v);
-}
-
 // silu(g) u: g / (1 + exp(-g)) u.  The reciprocal is within a unit of the last place, 0 of infinity.
 __device__ __forceinline__ float swiglu(float g, float u) {
   float r;
@@ -118,68 +94,165 @@ __device__ __forceinline__ void store_codes(uint32_t w, uint32_t b, int64_t row,
   }
 }
 
-// A thread's octets in a grid-stride loop: row and octet counted on, not divided.
+// ---- the flat kernels: a thread takes half a block, 16 values -------------------------------------------------
+
+// 32 bytes from or to memory, at once where they lie on a 32-byte boundary (`wide`).
+__device__ __forceinline__ void load32(const void* p, bool wide, uint32_t* r) {
+  if (wide) {
+    asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "l"(p)
+                 : "memory");
+  } else {
+    const uint4 a = __ldcs(static_cast<const uint4*>(p)), b = __ldcs(static_cast<const uint4*>(p) + 1);
+    r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w, r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
+  }
+}
+__device__ __forceinline__ void store32(void* p, bool wide, const uint32_t* r) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+  }
+}
+
+// Half a block as it is in memory: 8 words of bf16 pairs, or 16 of float32.
+template <typename T>
+struct Half {
+  static constexpr int kWords = 4 * sizeof(T);
+  uint32_t r[kWords];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) r[i] = 0u;
+  }
+  __device__ __forceinline__ void load(const T* p, bool wide) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 8) load32(reinterpret_cast<const uint32_t*>(p) + i, wide, r + i);
+  }
+  __device__ __forceinline__ float value(int i) const {
+    return sizeof(T) == 4 ? __uint_as_float(r[i]) : i & 1 ? hi_f32(r[i / 2]) : lo_f32(r[i / 2]);
+  }
+};
+
+// The 4-bit form of half a block (two neighbouring lanes, both of which call this): the codes and the block's scale byte.
+__device__ __forceinline__ uint2 quantize_half(const Half<float>& h, uint32_t* scale_byte) {
+  float m[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m[i] = max_magnitude(h.value(i), h.value(i + 8));
+#pragma unroll
+  for (int k = 4; k; k >>= 1)
+#pragma unroll
+    for (int i = 0; i < k; ++i) m[i] = max_magnitude(m[i], m[i + k]);
+  const float a = max_magnitude(m[0], __shfl_xor_sync(0xFFFFFFFFu, m[0], 1));
+  const uint32_t b = mx_scale_byte(__float_as_uint(a) & 0x7FFFFFFFu);
+  *scale_byte = b;
+  if (b == 255u) return make_uint2(0u, 0u);
+  const float inv = mx_inverse_scale(b);
+  float lo[8], hi[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo[i] = h.value(i) * inv;
+    hi[i] = h.value(i + 8) * inv;
+  }
+  return make_uint2(mx_pack8(lo), mx_pack8(hi));
+}
+// bf16 magnitudes are compared as 16-bit integers, two at a time (a NaN is the largest), and scaled two at a time: exact in
+// bf16 too (what underflows has the code 0 either way).
+__device__ __forceinline__ uint2 quantize_half(const Half<__nv_bfloat16>& h, uint32_t* scale_byte) {
+  constexpr uint32_t kMag = 0x7FFF7FFFu;
+  uint32_t m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = __vmaxu2(h.r[i] & kMag, h.r[i + 4] & kMag);
+  uint32_t a = __vmaxu2(__vmaxu2(m[0], m[1]), __vmaxu2(m[2], m[3]));
+  a = __vmaxu2(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+  const uint32_t b = mx_scale_byte(max(a & 0xFFFF0000u, a << 16));
+  *scale_byte = b;
+  if (b == 255u) return make_uint2(0u, 0u);
+  const __nv_bfloat162 inv = bf16_pair((254u - b) << 7);
+  float v[2][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const __nv_bfloat162 p = __hmul2_rn(*reinterpret_cast<const __nv_bfloat162*>(&h.r[i]), inv);
+    const uint32_t q = *reinterpret_cast<const uint32_t*>(&p);
+    v[i / 4][2 * (i & 3)] = lo_f32(q);
+    v[i / 4][2 * (i & 3) + 1] = hi_f32(q);
+  }
+  return make_uint2(mx_pack8(v[0]), mx_pack8(v[1]));
+}
+
+// A thread's halves in a grid-stride loop: row and place in it counted on, not divided.
 struct Walk {
-  int row, oct;
-  __device__ __forceinline__ Walk(int64_t first, int octs) : row((int)(first / octs)), oct((int)(first - (int64_t)row * octs)) {}
-  __device__ __forceinline__ void next(int step_rows, int step_octs, int octs) {
+  int row, half;
+  __device__ __forceinline__ Walk(int64_t first, int halves)
+      : row((int)(first / halves)), half((int)(first - (int64_t)row * halves)) {}
+  __device__ __forceinline__ void next(int step_rows, int step_halves, int halves) {
     row += step_rows;
-    oct += step_octs;
-    if (oct >= octs) {
-      oct -= octs;
+    half += step_halves;
+    if (half >= halves) {
+      half -= halves;
       ++row;
     }
   }
 };
 
-// What a row's octet is made of: x itself, x's row rows[row], or silu(g) u of x [n][2 d] = [g | u].
+// What a row's values are made of: x itself, x's row rows[row], or silu(g) u of x [n][2 d] = [g | u].
 enum { kPlain = 0, kRows = 1, kGated = 2 };
 
 template <typename T, int FROM>
 __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const T* __restrict__ x, int64_t n,
-                                                               const int32_t* __restrict__ rows, int64_t m, int octs,
-                                                               int step_rows, int step_octs, uint8_t* __restrict__ xq,
-                                                               uint8_t* __restrict__ xs, int pitch,
-                                                               uint32_t* __restrict__ status) {
-  const int64_t total = m * octs, stride = (int64_t)gridDim.x * kThreads;
+                                                               const int32_t* __restrict__ rows, int64_t m, int halves,
+                                                               int step_rows, int step_halves, int wide,
+                                                               uint8_t* __restrict__ xq, uint8_t* __restrict__ xs,
+                                                               int pitch, uint32_t* __restrict__ status) {
+  const int64_t total = m * halves, stride = (int64_t)gridDim.x * kThreads;
   int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int lane = threadIdx.x & 31;
-  Walk w(i, octs);
+  Walk w(i, halves);
   pdl_wait_then_release();
   bool bad = false;
-  // a whole warp goes on together (the shuffles): the bound is its first octet
-  for (; i - lane < total; i += stride, w.next(step_rows, step_octs, octs)) {
+  // a whole warp goes on together (the shuffles): the bound is its first half
+  for (; i - lane < total; i += stride, w.next(step_rows, step_halves, halves)) {
     const bool in = i < total;
-    uint32_t b = 0, c;
+    uint32_t b;
+    uint2 c;
     if constexpr (FROM == kGated) {
-      Oct o = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+      Half<float> o;
+      o.zero();
       if (in) {
-        const T* p = x + ((int64_t)w.row * octs + i) * 8;          // 2 octs a row
-        const Oct g = load_oct(p), u = load_oct(p + (int64_t)octs * 8);
+        const T* p = x + ((int64_t)w.row * halves + i) * 16;       // 2 halves a row
+        Half<T> g, u;
+        g.load(p, wide);
+        u.load(p + (int64_t)halves * 16, wide);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o.v[k] = swiglu(g.v[k], u.v[k]);
+        for (int k = 0; k < 16; ++k) o.r[k] = __float_as_uint(swiglu(g.value(k), u.value(k)));
       }
-      c = quantize_oct(o, &b);
+      c = quantize_half(o, &b);
     } else {
       int64_t src = i;
       bool have = in;
       if constexpr (FROM == kRows) {
         const int64_t row = in ? rows[w.row] : -1;
         have = row >= 0 && row < n;
-        src = row * octs + w.oct;
+        src = row * halves + w.half;
       }
-      if constexpr (sizeof(T) == 2) {
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (have) v = __ldcs(reinterpret_cast<const uint4*>(x) + src);
-        c = quantize_oct(v, &b);
-      } else {
-        Oct o = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-        if (have) o = load_oct(x + src * 8);
-        c = quantize_oct(o, &b);
-      }
+      Half<T> v;
+      v.zero();
+      if (have) v.load(x + src * 16, wide);
+      c = quantize_half(v, &b);
     }
-    if (in) store_codes(c, b, w.row, w.oct, octs, reinterpret_cast<uint32_t*>(xq) + i, xs, pitch);
-    bad |= b == 255u;
+    if (in) {
+      reinterpret_cast<uint2*>(xq)[i] = c;
+      if ((w.half & 1) == 0) {                     // the block's scale, and the row's pad bytes behind the last
+        uint8_t* s = xs + (int64_t)w.row * pitch + (w.half >> 1);
+        *s = (uint8_t)b;
+        if (w.half == halves - 2)
+          for (int k = 1; k < pitch - (w.half >> 1); ++k) s[k] = 0;
+      }
+      bad |= b == 255u;
+    }
   }
   if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
 }
@@ -190,42 +263,41 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t c) {
   return ((c & 7u) << 6) | ((c & 0x70u) << 18) | ((c & 8u) << 12) | ((c & 0x80u) << 24);
 }
 // times 2^126, then the scale: each exact, in bf16 too (one factor for both could be out of range)
-__device__ __forceinline__ void dequantize_oct(uint32_t c, uint32_t b, float* out) {
+__device__ __forceinline__ void dequantize_half(const uint2& c, uint32_t b, Half<float>& out) {
   const float s = mx_scale(b);
-  Oct o;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t p = code_pair(c >> (8 * k));
-    o.v[2 * k] = lo_f32(p) * 0x1p126f * s;
-    o.v[2 * k + 1] = hi_f32(p) * 0x1p126f * s;
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t p = code_pair((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
+    out.r[2 * k] = __float_as_uint(lo_f32(p) * 0x1p126f * s);
+    out.r[2 * k + 1] = __float_as_uint(hi_f32(p) * 0x1p126f * s);
   }
-  store_oct(out, o);
 }
-__device__ __forceinline__ void dequantize_oct(uint32_t c, uint32_t b, __nv_bfloat16* out) {
+__device__ __forceinline__ void dequantize_half(const uint2& c, uint32_t b, Half<__nv_bfloat16>& out) {
   const __nv_bfloat162 up = bf16_pair((126u + 127u) << 7), s = bf16_pair(b == 255u ? 0x7FFFu : b == 0u ? 0x0040u : b << 7);
-  uint32_t r[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t p = code_pair(c >> (8 * k));
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t p = code_pair((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
     const __nv_bfloat162 v = __hmul2_rn(__hmul2_rn(*reinterpret_cast<const __nv_bfloat162*>(&p), up), s);
-    r[k] = *reinterpret_cast<const uint32_t*>(&v);
+    out.r[k] = *reinterpret_cast<const uint32_t*>(&v);
   }
-  *reinterpret_cast<uint4*>(out) = make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* __restrict__ xq,
-                                                                 const uint8_t* __restrict__ xs, int64_t n, int octs,
-                                                                 int step_rows, int step_octs, int pitch,
+                                                                 const uint8_t* __restrict__ xs, int64_t n, int halves,
+                                                                 int step_rows, int step_halves, int wide, int pitch,
                                                                  T* __restrict__ out) {
-  const int64_t total = n * octs, stride = (int64_t)gridDim.x * kThreads;
+  const int64_t total = n * halves, stride = (int64_t)gridDim.x * kThreads;
   int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  Walk w(i, octs);
+  Walk w(i, halves);
   pdl_wait_then_release();
-  for (; i < total; i += stride, w.next(step_rows, step_octs, octs)) {
-    const uint32_t c = __ldcs(reinterpret_cast<const uint32_t*>(xq) + i);
-    const uint32_t b = xs[(int64_t)w.row * pitch + (w.oct >> 2)];
-    dequantize_oct(c, b, out + i * 8);
+  for (; i < total; i += stride, w.next(step_rows, step_halves, halves)) {
+    const uint2 c = __ldcs(reinterpret_cast<const uint2*>(xq) + i);
+    const uint32_t b = xs[(int64_t)w.row * pitch + (w.half >> 1)];
+    Half<T> v;
+    dequantize_half(c, b, v);
+#pragma unroll
+    for (int k = 0; k < Half<T>::kWords; k += 8) store32(reinterpret_cast<uint32_t*>(out + i * 16) + k, wide, v.r + k);
   }
 }
 
@@ -430,25 +502,25 @@ cudaError_t launch(void (*kernel)(P...), int64_t blocks, int threads, cudaStream
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
-// Blocks of a grid-stride loop over octets, and its stride in rows and octets.
+// Blocks of a grid-stride loop over `rows` rows of halves, and its stride in rows and halves.
 struct Flat {
+  int halves, step_rows, step_halves;
   int64_t blocks;
-  int step_rows, step_octs;
-  Flat(int64_t octets, int octs) {
-    const int64_t want = (octets + kThreads - 1) / kThreads, cap = (int64_t)sm_count() * kFlatBlocks;
+  Flat(int64_t rows, int64_t d) : halves((int)(d / 16)) {
+    const int64_t want = (rows * halves + kThreads - 1) / kThreads, cap = (int64_t)sm_count() * kFlatBlocks;
     blocks = want < cap ? want : cap;
-    step_rows = (int)(blocks * kThreads / octs);
-    step_octs = (int)(blocks * kThreads % octs);
+    step_rows = (int)(blocks * kThreads / halves);
+    step_halves = (int)(blocks * kThreads % halves);
   }
 };
+int aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
 
 template <typename T, int FROM>
 cudaError_t quantize(const void* x, int64_t n, int64_t d, const int32_t* rows, int64_t m, uint8_t* xq, uint8_t* xs,
                      uint32_t* status, cudaStream_t stream) {
-  const int octs = (int)(d / 8);
-  const Flat f(m * octs, octs);
-  return launch(mx_quantize_kernel<T, FROM>, f.blocks, kThreads, stream, static_cast<const T*>(x), n, rows, m, octs,
-                f.step_rows, f.step_octs, xq, xs, (int)mx_pitch(d), status);
+  const Flat f(m, d);
+  return launch(mx_quantize_kernel<T, FROM>, f.blocks, kThreads, stream, static_cast<const T*>(x), n, rows, m, f.halves,
+                f.step_rows, f.step_halves, aligned32(x), xq, xs, (int)mx_pitch(d), status);
 }
 
 template <typename T, typename W>
@@ -490,13 +562,13 @@ cudaError_t launch_mx_quantize(const void* x, int dtype, int64_t n, int64_t d, c
 
 cudaError_t launch_mx_dequantize(const uint8_t* xq, const uint8_t* xs, int64_t n, int64_t d, int dtype, void* out,
                                  cudaStream_t stream) {
-  const int octs = (int)(d / 8), pitch = (int)mx_pitch(d);
-  const Flat f(n * octs, octs);
+  const int pitch = (int)mx_pitch(d);
+  const Flat f(n, d);
   if (dtype == 0)
-    return launch(mx_dequantize_kernel<float>, f.blocks, kThreads, stream, xq, xs, n, octs, f.step_rows, f.step_octs, pitch,
-                  static_cast<float*>(out));
-  return launch(mx_dequantize_kernel<__nv_bfloat16>, f.blocks, kThreads, stream, xq, xs, n, octs, f.step_rows, f.step_octs,
-                pitch, static_cast<__nv_bfloat16*>(out));
+    return launch(mx_dequantize_kernel<float>, f.blocks, kThreads, stream, xq, xs, n, f.halves, f.step_rows, f.step_halves,
+                  aligned32(out), pitch, static_cast<float*>(out));
+  return launch(mx_dequantize_kernel<__nv_bfloat16>, f.blocks, kThreads, stream, xq, xs, n, f.halves, f.step_rows,
+                f.step_halves, aligned32(out), pitch, static_cast<__nv_bfloat16*>(out));
 }
 
 cudaError_t launch_mx_rmsnorm_quantize(const void* x, const void* residual, const void* weight, int dtype,
