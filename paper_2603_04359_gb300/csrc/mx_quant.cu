@@ -14,12 +14,8 @@ namespace cat {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWarpOcts = 64;     // rows of a norm up to this have a warp each (8192 x 256 bf16 4.5 us, a CTA each 8.7; x 768 13.5, 12.3)
+constexpr int kRowThreads = 512;  // most threads of a norm's CTA
 constexpr int kFlatBlocks = 32;  // most blocks an SM of a grid-stride loop
-
-struct Oct {
-  float v[8];
-};
 
 __device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -29,28 +25,6 @@ __device__ __forceinline__ __nv_bfloat162 bf16_pair(uint32_t bits) {
   return *reinterpret_cast<const __nv_bfloat162*>(&two);
 }
 
-__device__ __forceinline__ Oct load_oct(const float* p) {
-  const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-  return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-}
-__device__ __forceinline__ Oct load_oct(const __nv_bfloat16* p) {
-  const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
-  return {{lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)}};
-}
-__device__ __forceinline__ void store_oct(float* p, const Oct& o) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(o.v[0], o.v[1], o.v[2], o.v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(o.v[4], o.v[5], o.v[6], o.v[7]);
-}
-__device__ __forceinline__ void store_oct(__nv_bfloat16* p, const Oct& o) {
-  uint32_t r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(o.v[2 * i], o.v[2 * i + 1]);
-    r[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  *reinterpret_cast<uint4*>(p) = make_uint4(r[0], r[1], r[2], r[3]);
-}
-
 // The larger magnitude; a NaN is larger than all.
 __device__ __forceinline__ float max_magnitude(float a, float b) {
   float m;
@@ -58,43 +32,12 @@ __device__ __forceinline__ float max_magnitude(float a, float b) {
   return m;
 }
 
-// The 4-bit form of a lane's 8 values of a block of 32 (four neighbouring lanes, all of which call this): the codes
-// and the block's scale byte.
-__device__ __forceinline__ uint32_t quantize_oct(const Oct& o, uint32_t* scale_byte) {
-  const float m0 = max_magnitude(max_magnitude(o.v[0], o.v[1]), max_magnitude(o.v[2], o.v[3]));
-  const float m1 = max_magnitude(max_magnitude(o.v[4], o.v[5]), max_magnitude(o.v[6], o.v[7]));
-  float a = max_magnitude(m0, m1);
-  a = max_magnitude(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-  a = max_magnitude(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-  const uint32_t b = mx_scale_byte(__float_as_uint(a) & 0x7FFFFFFFu);
-  *scale_byte = b;
-  if (b == 255u) return 0u;
-  const float inv = mx_inverse_scale(b);
-  float v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = o.v[i] * inv;
-  return mx_pack8(v);
-}
 // silu(g) u: g / (1 + exp(-g)) u.  The reciprocal is within a unit of the last place, 0 of infinity.
 __device__ __forceinline__ float swiglu(float g, float u) {
   float r;
   asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-g)));
   return g * r * u;
 }
-
-// Writes a lane's codes, and for the block's first lane its scale byte (and the row's pad bytes behind the last).
-__device__ __forceinline__ void store_codes(uint32_t w, uint32_t b, int64_t row, int oct, int octs, uint32_t* xq,
-                                            uint8_t* xs, int pitch) {
-  *xq = w;
-  if ((oct & 3) == 0) {
-    uint8_t* s = xs + row * pitch + (oct >> 2);
-    *s = (uint8_t)b;
-    if (oct == octs - 4)
-      for (int i = 1; i < pitch - (oct >> 2); ++i) s[i] = 0;
-  }
-}
-
-// ---- the flat kernels: a thread takes half a block, 16 values -------------------------------------------------
 
 // 32 bytes from or to memory, at once where they lie on a 32-byte boundary (`wide`).
 __device__ __forceinline__ void load32(const void* p, bool wide, uint32_t* r) {
@@ -183,6 +126,19 @@ __device__ __forceinline__ uint2 quantize_half(const Half<__nv_bfloat16>& h, uin
   return make_uint2(mx_pack8(v[0]), mx_pack8(v[1]));
 }
 
+// Writes half `half` of row `row`: its codes, and for the block's first lane the scale byte (behind the row's last, its pad
+// bytes).
+__device__ __forceinline__ void store_half(const uint2& c, uint32_t b, int row, int half, int halves, uint8_t* xq, uint8_t* xs,
+                                           int pitch) {
+  reinterpret_cast<uint2*>(xq)[(int64_t)row * halves + half] = c;
+  if ((half & 1) == 0) {
+    uint8_t* s = xs + (int64_t)row * pitch + (half >> 1);
+    *s = (uint8_t)b;
+    if (half == halves - 2)
+      for (int k = 1; k < pitch - (half >> 1); ++k) s[k] = 0;
+  }
+}
+
 // A thread's halves in a grid-stride loop: row and place in it counted on, not divided.
 struct Walk {
   int row, half;
@@ -244,13 +200,7 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const T* __restri
       c = quantize_half(v, &b);
     }
     if (in) {
-      reinterpret_cast<uint2*>(xq)[i] = c;
-      if ((w.half & 1) == 0) {                     // the block's scale, and the row's pad bytes behind the last
-        uint8_t* s = xs + (int64_t)w.row * pitch + (w.half >> 1);
-        *s = (uint8_t)b;
-        if (w.half == halves - 2)
-          for (int k = 1; k < pitch - (w.half >> 1); ++k) s[k] = 0;
-      }
+      store_half(c, b, w.row, w.half, halves, xq, xs, pitch);
       bad |= b == 255u;
     }
   }
@@ -301,185 +251,193 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* 
   }
 }
 
-// ---- h = x + residual in 32 bits, stored in x's type; v = h / sqrt(mean(h^2) + eps) * weight, of the unrounded h; then
+// ---- h = x + residual in 32 bits, stored in x's type; v = h weight / sqrt(mean(h^2) + eps), of the unrounded h; then
 // the 4-bit form of v.  Rows of up to 512 values have a warp each, up to 16384 a CTA each, whose threads hold them in
-// registers (an octet each to 8192, two beyond); with persistent CTAs that load the next row while this one's sum is
-// formed, 8192 x 8192 bf16 takes 82 us (5.3 TB/s), without 93, and 106 with four octets a thread.  Copying rows ahead into
-// shared memory was no faster for 8192 rows of 8192 (83) and slower for all smaller (2048 x 4096 19 us, 13 here).
+// registers (half a block each to 8192, two beyond) and load the next row's while this one's sum is formed.  Moves 436 MB
+// in 66 us at 8192 x 8192 bf16 (6.6 TB/s); with 8 values a thread 79, without the loads ahead 93, through shared memory
+// (bulk copies of the next rows) 83.  1024 threads an SM are resident; a grid of more CTAs than that took up to 14 % longer.
 // h may be x or residual: a row's values are read by the CTA (warp) that writes them, before it writes.
 
-__device__ __forceinline__ Oct load_weights(const float* p) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+struct NormArgs {
+  const void *x, *residual, *weight;
+  void* h;
+  uint8_t *xq, *xs;
+  int64_t n;
+  int halves, pitch, wide;                  // wide: x, residual and h lie on 32-byte boundaries
+  float eps;
+  uint32_t* status;
+};
+
+// x and residual of half a block, as they are in memory.
+template <typename T>
+struct Pair {
+  Half<T> x, r;
+  __device__ __forceinline__ void load(const NormArgs& a, int64_t at) {
+    x.load(static_cast<const T*>(a.x) + at * 16, a.wide);
+    if (a.residual) r.load(static_cast<const T*>(a.residual) + at * 16, a.wide);
+  }
+  // the sum, and its squares added to `sq`
+  __device__ __forceinline__ float sum(const NormArgs& a, float (&h)[16], float sq) const {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      h[k] = x.value(k);
+      if (a.residual) h[k] += r.value(k);
+      sq = fmaf(h[k], h[k], sq);
+    }
+    return sq;
+  }
+};
+
+__device__ __forceinline__ void load_weights(const float* p, float (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 v = __ldg(reinterpret_cast<const float4*>(p) + i);
+    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+  }
 }
-__device__ __forceinline__ Oct load_weights(const __nv_bfloat16* p) {
-  const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
-  return {{lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)}};
+__device__ __forceinline__ void load_weights(const __nv_bfloat16* p, float (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      w[8 * i + 2 * k] = lo_f32(r[k]);
+      w[8 * i + 2 * k + 1] = hi_f32(r[k]);
+    }
+  }
+}
+__device__ __forceinline__ void round_half(const float (&h)[16], Half<float>& out) {
+#pragma unroll
+  for (int k = 0; k < 16; ++k) out.r[k] = __float_as_uint(h[k]);
+}
+__device__ __forceinline__ void round_half(const float (&h)[16], Half<__nv_bfloat16>& out) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(h[2 * k], h[2 * k + 1]);
+    out.r[k] = *reinterpret_cast<const uint32_t*>(&v);
+  }
 }
 
-__device__ __forceinline__ void add(Oct& a, const Oct& b) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) a.v[k] += b.v[k];
-}
-__device__ __forceinline__ float squares(const Oct& a, float sum) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) sum = fmaf(a.v[k], a.v[k], sum);
-  return sum;
-}
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   return v;
 }
+__device__ __forceinline__ float row_factor(const NormArgs& a, float sum) {
+  return __frsqrt_rn(sum / (float)(a.halves * 16) + a.eps);
+}
 
-struct NormOut {
-  void* h;
-  uint8_t *xq, *xs;
-  int octs, pitch;
-};
-
-// The second half for one octet of a row (whole warps; lanes past the row's end hold nothing): h and the 4-bit form.
+// The second half of a row's work for half a block (whole warps; lanes past the row's end hold nothing): h and the 4-bit
+// form.  Whether the block is not finite.
 template <typename T, typename W>
-__device__ __forceinline__ bool finish_oct(const NormOut& out, const W* weight, int64_t row, int oct, const Oct& a, float r) {
-  const bool in = oct < out.octs;
-  Oct v = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-  const int64_t at = row * out.octs + oct;
+__device__ __forceinline__ bool finish_half(const NormArgs& a, int64_t row, int half, const float (&h)[16], float r) {
+  const bool in = half < a.halves;
+  Half<float> v;
+  v.zero();
   if (in) {
-    if (out.h) store_oct(static_cast<T*>(out.h) + at * 8, a);
-    const Oct w = load_weights(weight + (int64_t)oct * 8);
+    if (a.h) {
+      Half<T> out;
+      round_half(h, out);
+      uint32_t* p = reinterpret_cast<uint32_t*>(static_cast<T*>(a.h) + (row * a.halves + half) * 16);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v.v[k] = a.v[k] * w.v[k] * r;   // (bf16 times bf16 is mostly exact: one rounding, of the last product)
+      for (int k = 0; k < Half<T>::kWords; k += 8) store32(p + k, a.wide, out.r + k);
+    }
+    float w[16];
+    load_weights(static_cast<const W*>(a.weight) + (int64_t)half * 16, w);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v.r[k] = __float_as_uint(h[k] * w[k] * r);   // (bf16 times bf16 is mostly exact: one rounding, of the last product)
   }
   uint32_t b;
-  const uint32_t c = quantize_oct(v, &b);
-  if (in) store_codes(c, b, row, oct, out.octs, reinterpret_cast<uint32_t*>(out.xq) + at, out.xs, out.pitch);
+  const uint2 c = quantize_half(v, &b);
+  if (in) store_half(c, b, (int)row, half, a.halves, a.xq, a.xs, a.pitch);
   return in && b == 255u;
 }
 
-// A warp a row of up to 32 ITEMS octets.
-template <typename T, typename W, int ITEMS>
-__global__ void __launch_bounds__(kThreads) mx_rmsnorm_warp_kernel(const T* x, const T* residual,
-                                                                   const W* __restrict__ weight, int64_t n, float eps,
-                                                                   const NormOut out, uint32_t* __restrict__ status) {
+// A warp a row of up to 32 halves.
+template <typename T, typename W>
+__global__ void __launch_bounds__(kThreads) mx_rmsnorm_warp_kernel(const __grid_constant__ NormArgs a) {
   pdl_wait_then_release();
-  const int lane = threadIdx.x & 31, octs = out.octs;
+  const int lane = threadIdx.x & 31;
   const int64_t stride = (int64_t)gridDim.x * (kThreads / 32);
   bool bad = false;
-  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); row < n; row += stride) {
-    Oct a[ITEMS];
-    float sq = 0.f;
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-      const int oct = 32 * j + lane;
-      if (oct < octs) {
-        a[j] = load_oct(x + (row * octs + oct) * 8);
-        if (residual) add(a[j], load_oct(residual + (row * octs + oct) * 8));
-        sq = squares(a[j], sq);
-      }
+  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); row < a.n; row += stride) {
+    float h[16], sq = 0.f;
+    if (lane < a.halves) {
+      Pair<T> p;
+      p.load(a, row * a.halves + lane);
+      sq = p.sum(a, h, 0.f);
     }
-    const float r = __frsqrt_rn(warp_sum(sq) / (float)(octs * 8) + eps);
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j)
-      if (32 * j < octs) bad |= finish_oct<T>(out, weight, row, 32 * j + lane, a[j], r);
+    bad |= finish_half<T, W>(a, row, lane, h, row_factor(a, warp_sum(sq)));
   }
-  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
+  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(a.status, kStatusNonFinite);
 }
 
-// An octet as it is in memory.
-template <typename T>
-struct Raw;
-template <>
-struct Raw<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    a = __ldcs(reinterpret_cast<const float4*>(p));
-    b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-  }
-  __device__ __forceinline__ Oct oct() const { return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}}; }
-};
-template <>
-struct Raw<__nv_bfloat16> {
-  uint4 w;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ Oct oct() const {
-    return {{lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)}};
-  }
-};
-
-// A CTA a row, ITEMS octets a thread in registers; the next row's are on their way while this one's sum is formed.
+// A CTA a row, ITEMS halves a thread in registers; the next row's are on their way while this one's sum is formed.
 template <typename T, typename W, int ITEMS>
-__global__ void __launch_bounds__(1024) mx_rmsnorm_row_kernel(const T* x, const T* residual, const W* __restrict__ weight,
-                                                              int64_t n, float eps, const NormOut out,
-                                                              uint32_t* __restrict__ status) {
+__global__ void __launch_bounds__(kRowThreads, sizeof(T) * ITEMS == 2 ? 2 : 1)
+    mx_rmsnorm_row_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float part[2][32];
   pdl_wait_then_release();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, octs = out.octs;
-  Raw<T> nx[ITEMS], nr[ITEMS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  Pair<T> next[ITEMS];
   auto load = [&](int64_t row) {
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
-      const int oct = j * blockDim.x + threadIdx.x;
-      if (row < n && oct < octs) {
-        nx[j].load(x + (row * octs + oct) * 8);
-        if (residual) nr[j].load(residual + (row * octs + oct) * 8);
-      }
+      const int half = j * blockDim.x + threadIdx.x;
+      if (row < a.n && half < a.halves) next[j].load(a, row * a.halves + half);
     }
   };
   bool bad = false;
   int turn = 0;
   load(blockIdx.x);
-  for (int64_t row = blockIdx.x; row < n; row += gridDim.x, turn ^= 1) {
-    Oct a[ITEMS];
-    float sq = 0.f;
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x, turn ^= 1) {
+    float h[ITEMS][16], sq = 0.f;
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-      if (j * (int)blockDim.x + (int)threadIdx.x < octs) {
-        a[j] = nx[j].oct();
-        if (residual) add(a[j], nr[j].oct());
-        sq = squares(a[j], sq);
-      }
-    }
+    for (int j = 0; j < ITEMS; ++j)
+      if (j * (int)blockDim.x + (int)threadIdx.x < a.halves) sq = next[j].sum(a, h[j], sq);
     load(row + gridDim.x);
     sq = warp_sum(sq);
     if (lane == 0) part[turn][warp] = sq;
     __syncthreads();                                     // (part[] has two turns, so one barrier a row will do)
-    const float r = __frsqrt_rn(warp_sum(lane < warps ? part[turn][lane] : 0.f) / (float)(octs * 8) + eps);
+    const float r = row_factor(a, warp_sum(lane < warps ? part[turn][lane] : 0.f));
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
-      const int oct = j * blockDim.x + threadIdx.x;
-      if (oct - lane < octs) bad |= finish_oct<T>(out, weight, row, oct, a[j], r);
+      const int half = j * blockDim.x + threadIdx.x;
+      if (half - lane < a.halves) bad |= finish_half<T, W>(a, row, half, h[j], r);
     }
   }
-  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
+  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(a.status, kStatusNonFinite);
 }
 
 // Longer rows are read twice (before h is written).
 template <typename T, typename W>
-__global__ void __launch_bounds__(1024) mx_rmsnorm_long_kernel(const T* x, const T* residual, const W* __restrict__ weight,
-                                                               int64_t n, float eps, const NormOut out,
-                                                               uint32_t* __restrict__ status) {
+__global__ void __launch_bounds__(kRowThreads) mx_rmsnorm_long_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float part[32];
   pdl_wait_then_release();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, octs = out.octs;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   bool bad = false;
-  for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
-    const int64_t base = row * octs;
-    auto sum_of = [&](int oct) {
-      Oct a = load_oct(x + (base + oct) * 8);
-      if (residual) add(a, load_oct(residual + (base + oct) * 8));
-      return a;
-    };
-    float sq = 0.f;
-    for (int oct = threadIdx.x; oct < octs; oct += blockDim.x) sq = squares(sum_of(oct), sq);
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    float h[16], sq = 0.f;
+    Pair<T> p;
+    for (int half = threadIdx.x; half < a.halves; half += blockDim.x) {
+      p.load(a, row * a.halves + half);
+      sq = p.sum(a, h, sq);
+    }
     sq = warp_sum(sq);
     if (lane == 0) part[warp] = sq;
     __syncthreads();
-    const float r = __frsqrt_rn(warp_sum(lane < warps ? part[lane] : 0.f) / (float)(octs * 8) + eps);
-    for (int oct = threadIdx.x; oct - lane < octs; oct += blockDim.x)
-      bad |= finish_oct<T>(out, weight, row, oct, oct < octs ? sum_of(oct) : Oct{}, r);
+    const float r = row_factor(a, warp_sum(lane < warps ? part[lane] : 0.f));
+    for (int half = threadIdx.x; half - lane < a.halves; half += blockDim.x) {
+      if (half < a.halves) {
+        p.load(a, row * a.halves + half);
+        p.sum(a, h, 0.f);
+      }
+      bad |= finish_half<T, W>(a, row, half, h, r);
+    }
     __syncthreads();                                     // part[] is read before the next row's sums
   }
-  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(status, kStatusNonFinite);
+  if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(a.status, kStatusNonFinite);
 }
 
 int sm_count() {
@@ -524,24 +482,17 @@ cudaError_t quantize(const void* x, int64_t n, int64_t d, const int32_t* rows, i
 }
 
 template <typename T, typename W>
-cudaError_t rmsnorm(const void* x_, const void* residual_, const void* weight_, int64_t n, int64_t d, float eps, void* h,
-                    uint8_t* xq, uint8_t* xs, uint32_t* status, cudaStream_t stream) {
-  const int octs = (int)(d / 8);
-  const NormOut out = {h, xq, xs, octs, (int)mx_pitch(d)};
-  const T *x = static_cast<const T*>(x_), *residual = static_cast<const T*>(residual_);
-  const W* weight = static_cast<const W*>(weight_);
+cudaError_t rmsnorm(const NormArgs& a, cudaStream_t stream) {
   const int64_t sms = sm_count();
-  if (octs <= kWarpOcts) {
-    const int64_t want = (n + kThreads / 32 - 1) / (kThreads / 32), blocks = want < sms * 16 ? want : sms * 16;
-    auto go = [&](auto kernel) { return launch(kernel, blocks, kThreads, stream, x, residual, weight, n, eps, out, status); };
-    return octs <= 32 ? go(mx_rmsnorm_warp_kernel<T, W, 1>) : go(mx_rmsnorm_warp_kernel<T, W, 2>);
+  if (a.halves <= 32) {
+    const int64_t want = (a.n + kThreads / 32 - 1) / (kThreads / 32), blocks = want < sms * 16 ? want : sms * 16;
+    return launch(mx_rmsnorm_warp_kernel<T, W>, blocks, kThreads, stream, a);
   }
-  const int threads = octs < 1024 ? (octs + 31) / 32 * 32 : 1024;
-  const int64_t most = sms * (2048 / threads), blocks = n < most ? n : most;
-  auto go = [&](auto kernel) { return launch(kernel, blocks, threads, stream, x, residual, weight, n, eps, out, status); };
-  if (octs <= 1024) return go(mx_rmsnorm_row_kernel<T, W, 1>);
-  if (octs <= 2048) return go(mx_rmsnorm_row_kernel<T, W, 2>);
-  return go(mx_rmsnorm_long_kernel<T, W>);
+  const int threads = a.halves < kRowThreads ? (a.halves + 31) / 32 * 32 : kRowThreads;
+  const int64_t most = sms * (1024 / threads), blocks = a.n < most ? a.n : most;
+  if (a.halves <= kRowThreads) return launch(mx_rmsnorm_row_kernel<T, W, 1>, blocks, threads, stream, a);
+  if (a.halves <= 2 * kRowThreads) return launch(mx_rmsnorm_row_kernel<T, W, 2>, blocks, threads, stream, a);
+  return launch(mx_rmsnorm_long_kernel<T, W>, blocks, threads, stream, a);
 }
 
 }  // namespace
@@ -575,11 +526,10 @@ cudaError_t launch_mx_rmsnorm_quantize(const void* x, const void* residual, cons
                                        int weight_dtype, int64_t n, int64_t d, float eps, void* h, uint8_t* xq, uint8_t* xs,
                                        uint32_t* status, cudaStream_t stream) {
   using B = __nv_bfloat16;
-  if (dtype == 0)
-    return weight_dtype == 0 ? rmsnorm<float, float>(x, residual, weight, n, d, eps, h, xq, xs, status, stream)
-                             : rmsnorm<float, B>(x, residual, weight, n, d, eps, h, xq, xs, status, stream);
-  return weight_dtype == 0 ? rmsnorm<B, float>(x, residual, weight, n, d, eps, h, xq, xs, status, stream)
-                           : rmsnorm<B, B>(x, residual, weight, n, d, eps, h, xq, xs, status, stream);
+  const NormArgs a = {x, residual, weight, h, xq, xs, n, (int)(d / 16), (int)mx_pitch(d),
+                      aligned32(x) & aligned32(residual) & aligned32(h), eps, status};
+  if (dtype == 0) return weight_dtype == 0 ? rmsnorm<float, float>(a, stream) : rmsnorm<float, B>(a, stream);
+  return weight_dtype == 0 ? rmsnorm<B, float>(a, stream) : rmsnorm<B, B>(a, stream);
 }
 
 }  // namespace cat
