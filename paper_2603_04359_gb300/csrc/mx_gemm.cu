@@ -44,7 +44,7 @@ constexpr int kRing = 2, kGroup = 2, kScaleRow = 16 * kGroup;
 constexpr int kScaleWarp0 = 4, kScaleWarps = 4, kEpiWarp0 = 8, kEpiWarps = 8;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kStageW = BM * 128;      // 16 KiB of weight codes a stage
-constexpr uint32_t kStageOut = 4096;        // an epilogue half's outputs on their way: 16 bf16 or 8 float32 tokens
+constexpr uint32_t kStageOut = 1024;        // an epilogue warp's outputs on their way: 16 bf16 or 8 float32 tokens
 constexpr uint32_t kScalesW = BM * kScaleRow;   // 4 KiB of weight scales a ring slot
 // Shared memory: at least half an SM's, as two CTAs would wait for each other's tensor memory.  Clusters take all but
 // 12 KB, whatever they need: a CTA that holds its SM's tensor memory while its cluster waits for another SM's must not
@@ -223,21 +223,9 @@ __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// The four warps of an epilogue half, in step.
 // Named barrier 4: warp 2 has asked for the first scales, warp 0 goes on behind it.
 __device__ __forceinline__ void first_scales_arrive() { asm volatile("bar.arrive 4, 64;" ::: "memory"); }
 __device__ __forceinline__ void first_scales_sync() { asm volatile("bar.sync 4, 64;" ::: "memory"); }
-__device__ __forceinline__ void epi_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory"); }
-
-__device__ __forceinline__ bool epi_all(int half, bool ok) {
-  uint32_t all;
-  asm volatile(
-      "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; bar.red.and.pred q, %2, 128, p; selp.u32 %0, 1, 0, q; }"
-      : "=r"(all)
-      : "r"((uint32_t)ok), "r"(1 + half)
-      : "memory");
-  return all != 0;
-}
 
 // Value i of a thread's 32: bf16 two to a word, float32 one.
 template <typename T>
@@ -247,6 +235,36 @@ __device__ __forceinline__ float element<float>(const uint32_t* r, int i) { retu
 template <>
 __device__ __forceinline__ __nv_bfloat16 element<__nv_bfloat16>(const uint32_t* r, int i) {
   return __ushort_as_bfloat16((unsigned short)(r[i / 2] >> (16 * (i & 1))));
+}
+
+// A warp's 32 channels of up to 32 tokens (`left` of them), a channel a lane, to rows of y: through shared memory, a few
+// tokens at a time as [token][32 channels], then V bytes a lane, so a token's channels leave in one or two sectors of four
+// lanes' 16 bytes and eight tokens in one instruction.  (Between the four warps of a quadrant each, for whole 256-byte
+// rows, two barriers every 16 tokens took 790 cycles.)
+template <int V, typename T, typename R>
+__device__ __forceinline__ void store_chunk(T* p, int d_out, T* stage, const R& r, int channels, int left) {
+  constexpr int kStaged = kStageOut / (32 * sizeof(T)), kVec = V / sizeof(T), kLanes = 32 / kVec, kTokens = 32 / kLanes;
+  const int lane = threadIdx.x & 31, c = lane % kLanes * kVec;
+  left = c < channels ? left - lane / kLanes : 0;  // (V bytes are wholly in or out of a row)
+  T* to = p + (size_t)(lane / kLanes) * d_out + c;
+  const size_t step = (size_t)kTokens * d_out;
+#pragma unroll
+  for (int i0 = 0; i0 < 32; i0 += kStaged) {
+    __syncwarp();                                  // the tokens before have been read
+#pragma unroll
+    for (int i = 0; i < kStaged; ++i) stage[i * 32 + lane] = element<T>(r, i0 + i);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kStaged; i += kTokens, to += step) {
+      const T* from = stage + i * 32 + lane * kVec;
+      if (i0 + i < left) {
+        if constexpr (V == 16)
+          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+        else
+          *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
+      }
+    }
+  }
 }
 
 // Two float32 bit patterns to bf16, the first in the low half.
@@ -607,16 +625,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------------------------------------------------------- epilogue
     const int quad = warp & 3, half = (warp - kEpiWarp0) >> 2;
     const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32;
-    constexpr int kVec = 16 / sizeof(T), kStaged = kStageOut / (BM * sizeof(T));   // values of a store, tokens staged at once
-    T* stage = reinterpret_cast<T*>(smem + a.off_out) + half * (kStageOut / sizeof(T));
-    const bool whole = a.d_out % kVec == 0;        // 16 bytes are wholly in or out of a row
+    T* stage = reinterpret_cast<T*>(smem + a.off_out + (warp - kEpiWarp0) * kStageOut);
+    const int row_bytes = a.d_out * (int)sizeof(T);   // what a row's address is a multiple of
+    const int vec = row_bytes % 16 == 0 ? 16 : row_bytes % 4 == 0 ? 4 : 2;
     if (CG == 1) cluster_wait();                   // a split's CTAs have all started
     Place ac;
     int e = 0;
     for (int u = cluster; u < total; u += clusters, ac.next(a.acc_bufs)) {
       const Tile t = tile_at(u, e);
-      // (the half's warps go on or give up together: they meet at barriers below)
-      if (!epi_all(half, mbar_wait_bounded(&bars->acc_full[ac.at], ac.full(), abort_flag, __LINE__, lim))) break;
+      if (!mbar_wait_bounded(&bars->acc_full[ac.at], ac.full(), abort_flag, __LINE__, lim)) break;
+      __syncwarp();
       tc_fence_after();
       const int row = quad * 32 + lane, o_first = t.o0 + (CG == 2 ? (int)rank * BM : 0);
       const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + ac.at * npad;
@@ -678,29 +696,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int k = 0; k < kAtOnce; ++k) {
           const int c = c0_ + 2 * k, left = t.valid - c * 32;     // tokens of this chunk on
           if (left <= 0) break;
-          T* p = y + (size_t)(t.t0 + c * 32) * a.d_out;
-          if (whole) {
-            // through shared memory: [token][128 channels], then 16 bytes a lane, a token's channels by 128 / kVec lanes
-#pragma unroll
-            for (int i0 = 0; i0 < 32; i0 += kStaged) {
-              epi_sync(half);                      // the buffer has been read
-#pragma unroll
-              for (int i = 0; i < kStaged; ++i) stage[i * BM + row] = element<T>(r[k], i0 + i);
-              epi_sync(half);
-              constexpr int kLanes = BM / kVec, kRows = 128 / kLanes;
-              const int v = (tid & 127) % kLanes * kVec, o = o_first + v;
-#pragma unroll
-              for (int i = 0; i < kStaged; i += kRows) {
-                const int tok = i + (tid & 127) / kLanes;
-                if (i0 + tok < left && o < a.d_out)
-                  *reinterpret_cast<uint4*>(p + (size_t)(i0 + tok) * a.d_out + o) =
-                      *reinterpret_cast<const uint4*>(stage + tok * BM + v);
-              }
-            }
-          } else if (o_first + row < a.d_out) {
+          T* p = y + (size_t)(t.t0 + c * 32) * a.d_out + o_first + quad * 32;
+          const int channels = a.d_out - o_first - quad * 32;     // of this warp's 32 that there are
+          if (vec == 16)
+            store_chunk<16>(p, a.d_out, stage, r[k], channels, left);
+          else if (vec == 4)
+            store_chunk<4>(p, a.d_out, stage, r[k], channels, left);
+          else if (lane < channels) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (i < left) p[(size_t)i * a.d_out + o_first + row] = element<T>(r[k], i);
+              if (i < left) p[(size_t)i * a.d_out + lane] = element<T>(r[k], i);
           }
         }
       }
@@ -817,14 +822,14 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   a.ring_bytes = kScalesW + (uint32_t)up(up(nt, a.bxs), 64) * kScaleRow;
   const size_t red = split > 1 ? (size_t)split * ((nt + split - 1) / split) * BM * 4 : 0;
   const size_t table = c.offsets ? up((2 * (c.experts + 1) + 2 * kMaxChunks) * 4, 128) : 0;
-  const size_t rest = (size_t)kRing * a.ring_bytes + 2 * kStageOut + red + table + sizeof(Bars) + 1024;
+  const size_t rest = (size_t)kRing * a.ring_bytes + kEpiWarps * kStageOut + red + table + sizeof(Bars) + 1024;
   const size_t most = CG == 2 ? kPairSmem : kMaxSmem;
   const int stages = (int)((most - rest) / a.stage_bytes);
   a.stages = stages < kMaxStages ? stages : kMaxStages;
   if (a.slots < 2 || a.stages < 2 || nt % (8 * CG) != 0 || a.bx > 256 || a.bxs > 256) return cudaErrorInvalidConfiguration;
   a.off_ring = a.stages * a.stage_bytes;
   a.off_out = a.off_ring + kRing * a.ring_bytes;
-  a.off_red = a.off_out + 2 * kStageOut;
+  a.off_red = a.off_out + kEpiWarps * kStageOut;
   a.off_table = a.off_red + (uint32_t)red;
   a.off_bars = a.off_table + (uint32_t)table;
   size_t smem = a.off_bars + sizeof(Bars) + 1024;
