@@ -227,51 +227,136 @@ __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return
 __device__ __forceinline__ void first_scales_arrive() { asm volatile("bar.arrive 4, 64;" ::: "memory"); }
 __device__ __forceinline__ void first_scales_sync() { asm volatile("bar.sync 4, 64;" ::: "memory"); }
 
-// Value i of a thread's 32: bf16 two to a word, float32 one.
-template <typename T>
-__device__ __forceinline__ T element(const uint32_t* r, int i);
-template <>
-__device__ __forceinline__ float element<float>(const uint32_t* r, int i) { return __uint_as_float(r[i]); }
-template <>
-__device__ __forceinline__ __nv_bfloat16 element<__nv_bfloat16>(const uint32_t* r, int i) {
-  return __ushort_as_bfloat16((unsigned short)(r[i / 2] >> (16 * (i & 1))));
-}
-
-// A warp's 32 channels of up to 32 tokens (`left` of them), a channel a lane, to rows of y: through shared memory, a few
-// tokens at a time as [token][32 channels], then V bytes a lane, so a token's channels leave in one or two sectors of four
-// lanes' 16 bytes and eight tokens in one instruction.  (Between the four warps of a quadrant each, for whole 256-byte
-// rows, two barriers every 16 tokens took 790 cycles.)
-template <int V, typename T, typename R>
-__device__ __forceinline__ void store_chunk(T* p, int d_out, T* stage, const R& r, int channels, int left) {
-  constexpr int kStaged = kStageOut / (32 * sizeof(T)), kVec = V / sizeof(T), kLanes = 32 / kVec, kTokens = 32 / kLanes;
-  const int lane = threadIdx.x & 31, c = lane % kLanes * kVec;
-  left = c < channels ? left - lane / kLanes : 0;  // (V bytes are wholly in or out of a row)
-  T* to = p + (size_t)(lane / kLanes) * d_out + c;
-  const size_t step = (size_t)kTokens * d_out;
-#pragma unroll
-  for (int i0 = 0; i0 < 32; i0 += kStaged) {
-    __syncwarp();                                  // the tokens before have been read
-#pragma unroll
-    for (int i = 0; i < kStaged; ++i) stage[i * 32 + lane] = element<T>(r, i0 + i);
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < kStaged; i += kTokens, to += step) {
-      const T* from = stage + i * 32 + lane * kVec;
-      if (i0 + i < left) {
-        if constexpr (V == 16)
-          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
-        else
-          *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
-      }
-    }
-  }
-}
-
 // Two float32 bit patterns to bf16, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+
+// 16 lanes of tensor memory by 32 columns: of each 8 columns g, thread l has lanes l / 4 (v[4 g], v[4 g + 1]) and l / 4 + 8
+// (v[4 g + 2], v[4 g + 3]) at columns 8 g + 2 (l % 4) and the next -- as the rows of stmatrix's 8 x 8 matrices lie.
+__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t row, const uint32_t* r) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(row), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3])
+               : "memory");
+}
+
+// An accumulator chunk (32 tokens of a warp's 32 channels) as a warp keeps it until it is stored, and its way to rows of y
+// (`left` tokens and `channels` channels of it are there).  Rows of 16-byte multiples (WHOLE) go through the warp's part of
+// shared memory, a few tokens at a time as [token][32 channels], and leave 16 bytes a lane; others straight from the
+// registers, a channel a lane, 64 or 128 bytes of a token an instruction (3843 x 2560 -> 3709, bf16: 27.1 us; through shared
+// memory in 2-byte pieces 31.4, in words that straddle them 37.3).  (One part for the four warps of a half, whole
+// 256-byte rows, took two barriers every 16 tokens and 790 cycles; bf16 put in shared memory a value at a time, 500: 521 x
+// 1024 -> 23104 18.0 us, 15.3 here.)
+template <typename T, bool WHOLE>
+struct Kept;
+
+template <bool WHOLE>
+struct Kept<float, WHOLE> {
+  static constexpr int kAtOnce = 2;                // chunks kept at once
+  uint32_t r[32];                                  // lane = channel, a token a word
+  __device__ __forceinline__ void load(uint32_t taddr) {
+    CAT_TMEM_LD32(taddr, r);
+    tmem_ld_wait();
+  }
+  __device__ __forceinline__ void store(float* p, int d_out, uint8_t* stage_, int channels, int left) const {
+    const int lane = threadIdx.x & 31;
+    if constexpr (WHOLE) {
+      constexpr int kStaged = kStageOut / 128;     // 8 tokens, four an instruction
+      float* stage = reinterpret_cast<float*>(stage_);
+      const int c = lane % 8 * 4;
+      left = c < channels ? left - lane / 8 : 0;   // (16 bytes are wholly in or out of a row)
+      float* to = p + (size_t)(lane / 8) * d_out + c;
+      const size_t step = 4 * (size_t)d_out;
+#pragma unroll
+      for (int i0 = 0; i0 < 32; i0 += kStaged) {
+        __syncwarp();                              // the tokens before have been read
+#pragma unroll
+        for (int i = 0; i < kStaged; ++i) stage[i * 32 + lane] = __uint_as_float(r[i0 + i]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kStaged; i += 4, to += step)
+          if (i0 + i < left) *reinterpret_cast<float4*>(to) = *reinterpret_cast<const float4*>(stage + i * 32 + lane * 4);
+      }
+    } else if (lane < channels) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < left) p[(size_t)i * d_out + lane] = __uint_as_float(r[i]);
+    }
+  }
+};
+
+template <>
+struct Kept<__nv_bfloat16, true> {
+  static constexpr int kAtOnce = 4;
+  uint32_t r[16];                                  // word 4 g + m: 8 x 8 values, tokens 8 g .. by channels 8 m ..; a lane has
+                                                   // tokens 2 (lane % 4), + 1 of channel lane / 4
+  __device__ __forceinline__ void load(uint32_t taddr) {
+    uint32_t v[16], u[16];                         // channels 0 .. 15 and 16 .. 31
+    tmem_ld_16x256b_x4(taddr, v);
+    tmem_ld_16x256b_x4(taddr + (16u << 16), u);
+    tmem_ld_wait();
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      r[4 * g] = pack_bf16(v[4 * g], v[4 * g + 1]);
+      r[4 * g + 1] = pack_bf16(v[4 * g + 2], v[4 * g + 3]);
+      r[4 * g + 2] = pack_bf16(u[4 * g], u[4 * g + 1]);
+      r[4 * g + 3] = pack_bf16(u[4 * g + 2], u[4 * g + 3]);
+    }
+  }
+  // A token's four 16-byte pieces lie as piece q at q ^ (token / 2 mod 4): the eight rows of a matrix, and eight lanes'
+  // pieces of two tokens, are in different banks.
+  __device__ __forceinline__ void store(__nv_bfloat16* p, int d_out, uint8_t* stage, int channels, int left) const {
+    static_assert(kStageOut == 16 * 64, "two groups of eight tokens are staged at once");
+    int lane = threadIdx.x & 31;
+    asm volatile("" : "+r"(lane));                 // (addresses made per chunk, not kept across them: registers are short)
+    const int c = lane % 4 * 8;
+    left = c < channels ? left - lane / 4 : 0;
+    __nv_bfloat16* to = p + (size_t)(lane / 4) * d_out + c;
+    const size_t step = 8 * (size_t)d_out;
+    // lane l gives the row of token l % 8 of the matrix of channels 8 (l / 8) .., and takes piece l % 4 of token l / 4
+    const uint32_t row = smem_u32(stage) + (uint32_t)(lane & 7) * 64u + (uint32_t)(((lane >> 3) ^ (lane >> 1 & 3)) << 4);
+    const uint8_t* from = stage + (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3 & 3)) << 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __syncwarp();                                // the tokens before have been read
+#pragma unroll
+      for (int g = 0; g < 2; ++g) stmatrix_x4_trans(row + (uint32_t)g * 512u, r + 8 * h + 4 * g);
+      __syncwarp();
+#pragma unroll
+      for (int g = 0; g < 2; ++g, to += step)
+        if (16 * h + 8 * g < left) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from + g * 512);
+    }
+  }
+};
+
+template <>
+struct Kept<__nv_bfloat16, false> {
+  static constexpr int kAtOnce = 4;
+  uint32_t r[16];                                  // lane = channel, two tokens a word
+  __device__ __forceinline__ void load(uint32_t taddr) {
+    uint32_t v[32];
+    CAT_TMEM_LD32(taddr, v);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* p, int d_out, uint8_t*, int channels, int left) const {
+    const int lane = threadIdx.x & 31;
+    if (lane < channels) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < left) p[(size_t)i * d_out + lane] = __ushort_as_bfloat16((unsigned short)(r[i / 2] >> (16 * (i & 1))));
+    }
+  }
+};
 
 // Grouped: all threads fill the table: rows[e], the first row of expert e (rows[experts]: one past the last), and
 // tiles[e], the tiles of the experts before it (tiles[experts]: all).  Offsets are taken in order and within [0, m],
@@ -318,7 +403,8 @@ __device__ __forceinline__ void make_table(const MxArgs& a, int* rows, int* tile
   }
 }
 
-template <int CG, typename T>
+// WHOLE: rows of y are multiples of 16 bytes.
+template <int CG, typename T, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 1)
     mx_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                    const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmXs,
@@ -625,9 +711,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------------------------------------------------------- epilogue
     const int quad = warp & 3, half = (warp - kEpiWarp0) >> 2;
     const uint32_t npad = (uint32_t)(a.nt + 31) / 32 * 32;
-    T* stage = reinterpret_cast<T*>(smem + a.off_out + (warp - kEpiWarp0) * kStageOut);
-    const int row_bytes = a.d_out * (int)sizeof(T);   // what a row's address is a multiple of
-    const int vec = row_bytes % 16 == 0 ? 16 : row_bytes % 4 == 0 ? 4 : 2;
+    uint8_t* stage = smem + a.off_out + (warp - kEpiWarp0) * kStageOut;
     if (CG == 1) cluster_wait();                   // a split's CTAs have all started
     Place ac;
     int e = 0;
@@ -656,26 +740,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // The accumulator is read to registers and given back before anything is stored (bf16: all of this warp's part
       // at once; float32: half of it), so the next tile's MMAs wait for the reads alone.
-      constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;
+      constexpr int kAtOnce = Kept<T, WHOLE>::kAtOnce;
       bool held = true;
 #pragma unroll 1
       for (int c0_ = half; held; c0_ += 2 * kAtOnce) {
-        uint32_t r[kAtOnce][32 * sizeof(T) / 4];
+        Kept<T, WHOLE> kept[kAtOnce];
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
           const int c = c0_ + 2 * k;
           if (c * 32 < t.valid) {
-            uint32_t v[32];
             __syncwarp();
-            CAT_TMEM_LD32(acc + c * 32, v);
-            tmem_ld_wait();
-            if constexpr (sizeof(T) == 2) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) r[k][i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) r[k][i] = v[i];
-            }
+            kept[k].load(acc + c * 32);
           }
         }
         held = (c0_ + 2 * kAtOnce) * 32 < t.valid;
@@ -698,15 +773,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (left <= 0) break;
           T* p = y + (size_t)(t.t0 + c * 32) * a.d_out + o_first + quad * 32;
           const int channels = a.d_out - o_first - quad * 32;     // of this warp's 32 that there are
-          if (vec == 16)
-            store_chunk<16>(p, a.d_out, stage, r[k], channels, left);
-          else if (vec == 4)
-            store_chunk<4>(p, a.d_out, stage, r[k], channels, left);
-          else if (lane < channels) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i < left) p[(size_t)i * a.d_out + lane] = element<T>(r[k], i);
-          }
+          kept[k].store(p, a.d_out, stage, channels, left);
         }
       }
     }
@@ -795,7 +862,7 @@ struct Call {
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-template <int CG, typename T>
+template <int CG, typename T, bool WHOLE>
 cudaError_t launch_form(const Call& c, int nt, int split) {
   MxArgs a;
   memset(&a, 0, sizeof(a));
@@ -842,7 +909,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
       !make_map(&tws, c.ws, wrows, pitch, BM, kScaleRow) || !make_map(&txs, c.xs, c.m, pitch, a.bxs, kScaleRow))
     return cudaErrorInvalidValue;
   static PerDevice<cudaError_t> allowed;
-  const cudaError_t attr_err = allowed.get([] { return allow_smem(mx_gemm_kernel<CG, T>, CG == 2 ? kPairSmem : kMaxSmem); });
+  const cudaError_t attr_err = allowed.get([] { return allow_smem(mx_gemm_kernel<CG, T, WHOLE>, CG == 2 ? kPairSmem : kMaxSmem); });
   if (attr_err != cudaSuccess) return attr_err;
 
   // at most this many tiles (with groups the device knows how many)
@@ -867,7 +934,7 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   attrs[1].val.clusterDim.z = 1;
   cfg.attrs = attrs;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, mx_gemm_kernel<CG, T>, tw, tx, tws, txs, a);
+  return cudaLaunchKernelEx(&cfg, mx_gemm_kernel<CG, T, WHOLE>, tw, tx, tws, txs, a);
 }
 
 // What a call runs on: pairs or single CTAs, the most tokens of a tile, the CTAs that share a tile's K.
@@ -931,7 +998,9 @@ cudaError_t launch_typed(const Call& c) {
     const int64_t room = up(c.m < 4 * rows ? c.m : 4 * rows, 8 * f.cg), widest = 128 * f.cg;
     f.nt = (int)(room < widest ? room : widest);
   }
-  return f.cg == 2 ? launch_form<2, T>(c, f.nt, 1) : launch_form<1, T>(c, f.nt, f.split);
+  if (c.d_out * (int64_t)sizeof(T) % 16 == 0)
+    return f.cg == 2 ? launch_form<2, T, true>(c, f.nt, 1) : launch_form<1, T, true>(c, f.nt, f.split);
+  return f.cg == 2 ? launch_form<2, T, false>(c, f.nt, 1) : launch_form<1, T, false>(c, f.nt, f.split);
 }
 
 }  // namespace
