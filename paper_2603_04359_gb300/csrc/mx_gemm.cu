@@ -944,20 +944,20 @@ struct Form {
 
 // The form of least estimated time.  A round of tiles costs its K steps, at least 0.28 us each (a stage's turn) and a little
 // for its tokens, whatever is between 8 and 256 of them; so as few rounds as can be, and in them the narrowest tiles.  With
-// many CTAs a step takes what its bytes do: the weights from memory (6 TB/s), all operands from L2 (16 TB/s).  The
-// constants (us) are fitted to bf16 outputs of 1 to 512 tokens on 4096 -> 6144, 4096 -> 14336, 14336 -> 4096,
-// 4096 -> 4096, 1024 -> 1024 and 2048 -> 640, within 15 % of each time: one token, 4096 -> 6144: K in two 8.1, whole 9.2;
-// 128 tokens, 14336 -> 4096: K in four 14.2, in two (64-wide) 16.0, pairs 20.8; 200, 4096 -> 14336: pairs (one round) 13.0,
-// single CTAs (two) 16.4; 512, 4096 -> 4096: 128-wide 11.0, 256-wide 12.3.
+// many CTAs a step takes what its bytes do: the weights from memory (6 TB/s), all operands from L2 (16 TB/s); and a round
+// never takes less than its outputs' way out.  The constants (us) are fitted to bf16 outputs of 1 to 512 tokens on
+// 4096 -> 6144, 4096 -> 14336, 14336 -> 4096, 4096 -> 4096, 1024 -> 1024 and 2048 -> 640, and of 521 to 8192 on K of 256 to
+// 7040, within 15 % of each time: one token, 4096 -> 6144: K in two 7.6, whole 8.6; 128 tokens, 14336 -> 4096: K in four
+// 13.8, in two (64-wide) 15.7, pairs 20.8; 200, 4096 -> 14336: pairs (one round) 12.2, single CTAs (two) 15.5; 512,
+// 4096 -> 4096: 128-wide 10.4, 256-wide 11.8; 3843, 2560 -> 3712: pairs 22.2, single CTAs 25.6.
 Form pick_form(int64_t groups, int64_t rows, int64_t d, int64_t d_out) {
   const int64_t sms = sm_count(), chunks = (d + kChunk - 1) / kChunk;
   const double steps = (double)((d + BK - 1) / BK);
-  // clusters that are resident at once (a cluster stays within a group of 14 to 22 SMs)
-  const int64_t resident[4] = {sms, sms / 2, sms * 36 / 152, sms * 15 / 152};
   Form best = {2, 256, 1};
   double least = 1e30;
-  auto consider = [&](int cg, int split, int64_t at_once) {
-    const int64_t unit = 8 * cg, widest = 128 * cg, channel_tiles = groups * ((d_out + cg * BM - 1) / (cg * BM));
+  // `at_once` clusters are resident (a cluster stays within a group of 14 to 22 SMs)
+  auto consider = [&](int cg, int split, int64_t widest, int64_t at_once) {
+    const int64_t unit = 8 * cg, channel_tiles = groups * ((d_out + cg * BM - 1) / (cg * BM));
     const int64_t fewest = (rows + widest - 1) / widest;
     const int64_t rounds = (fewest * channel_tiles + at_once - 1) / at_once;
     if (split > 1 && rounds > 1) return;          // (a split tile has a cluster of its own, launched with the others)
@@ -971,20 +971,26 @@ Form pick_form(int64_t groups, int64_t rows, int64_t d, int64_t d_out) {
     double step = cg == 1 ? 0.28 + 0.0003 * nt : 0.29 + 0.0002 * nt;
     step = step < from_memory ? from_memory : step;
     step = step < from_l2 ? from_l2 : step;
-    double us = rounds * steps / split * step;
-    if (cg == 1)
-      us += 4.0 + 0.004 * nt + (split > 1 ? 0.7 + 0.02 * nt : 0.0);
-    else   // (past 160 tokens there is one accumulator: a tile's MMAs wait for the one before to be read)
-      us += 4.6 + (nt > 160 ? rounds : 1) * (1.2 + 0.004 * nt);
+    double round = steps / split * step, us = cg == 1 ? 3.6 + 0.004 * nt : 4.6, out = 0.6 + 0.011 * nt;
+    if (cg == 2 && nt > 160) {                    // one accumulator: a tile's MMAs wait for the one before to be read
+      round += 0.8 + 0.002 * nt;
+      out = 0.6 + 0.009 * nt;
+      us += round < out ? out : round;
+    } else {
+      us += round + (cg == 2 ? 1.0 + 0.003 * nt : 0.0);
+    }
+    us += (rounds - 1) * (round < out ? out : round) + (split > 1 ? 1.2 + 0.02 * nt : 0.0);
     if (us < least) {
       least = us;
       best = {cg, (int)nt, split};
     }
   };
-  consider(1, 1, resident[0]);
+  consider(1, 1, 128, sms);
+  const int64_t resident[4] = {0, sms / 2, sms * 36 / 152, sms * 15 / 152};
   for (int k = 1; k < 4; ++k)
-    if ((1 << k) <= chunks) consider(1, 1 << k, resident[k]);
-  consider(2, 1, sms / 2);
+    if ((1 << k) <= chunks) consider(1, 1 << k, 128, resident[k]);
+  consider(2, 1, 256, sms / 2);
+  consider(2, 1, 160, sms / 2);
   return best;
 }
 
