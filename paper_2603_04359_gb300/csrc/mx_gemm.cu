@@ -8,7 +8,7 @@
 //
 // Weights are the M operand and tokens the N operand: M is 128 whatever the call, N any multiple of 8, so a tile fits
 // the tokens there are -- one token of a decode step, an expert's ragged rows -- and the padding is at most 7 of them.
-// A thread of the epilogue holds one channel of many tokens, so a warp's store is 32 neighbouring channels of a token.
+// An accumulator's lane is a channel, so a warp of the epilogue turns 32 channels of a few tokens at a time (`Kept`).
 //
 // Two forms of one kernel:
 //   * CG = 2, CTA pairs: a tile is 256 channels by up to 256 tokens, each CTA with its 128 channels and half of the
@@ -17,7 +17,7 @@
 //     exchanged through distributed shared memory and summed in the order of their K, so results do not depend on timing.
 //
 // Warps (512 threads):
-//   0       TMA of codes              1  lane 0 issues the MMAs (CG = 2, odd CTA: forwards stages to the even one)
+//   0       TMA of codes              1  issues the MMAs (CG = 2, odd CTA: forwards stages to the even one)
 //   2       TMA of scales, TMEM       3  (CG = 2, odd CTA: forwards scale slots)
 //   4..7    scales from shared to tensor memory, each to its own 32 lanes (the MMA reads a copy in each)
 //   8..15   epilogue, two warps a lane quadrant, taking 32-token chunks in turn
@@ -137,12 +137,12 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ uint32_t idesc_mxf4(int M, int N) {
   return (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27);
 }
-// which byte of a scale column's word an MMA's first scale is in (0 or 2), of A and of B
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
   asm volatile("{ .reg .pred q; elect.sync _|q, 0xFFFFFFFF; selp.u32 %0, 1, 0, q; }" : "=r"(p));
   return p != 0;
 }
+// which byte of a scale column's word an MMA's first scale is in (0 or 2), of A and of B
 __device__ __forceinline__ uint32_t idesc_scale_byte(uint32_t id) { return (id << 4) | (id << 29); }
 
 template <int CG>
@@ -489,15 +489,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int64_t i = from + first; i < all; i += stride) y[i] = to_out<T>(0.f);
   }
 
-  // tile u of the launch; e: the caller's place in the table (tiles are asked for in order)
+  // tile u of the launch, for a whole warp; e: the caller's place in the table (tiles are asked for in order)
   auto tile_at = [&](int u, int& e) {
     Tile t;
     int begin = 0, end = a.m, tt, ct, n_tiles = token_tiles;
     if (a.offsets) {
-      for (int last = a.experts - 1; e < last;) {   // the last expert that begins at u or before (the others there are empty)
-        const int mid = (e + last + 1) / 2;
-        if (tiles[mid] <= u) e = mid;
-        else last = mid - 1;
+      // the last expert that begins at u or before (the others there are empty), 32 entries a look (a binary search:
+      // 6000 rows of 64 experts, 1024 -> 768, 14.7 us, 14.2 here)
+      for (int n = 32; n == 32; e += n) {
+        const int next = e + 1 + lane;
+        n = __popc(__ballot_sync(0xFFFFFFFFu, next < a.experts && tiles[next] <= u));
       }
       begin = rows[e];
       end = rows[e + 1];
