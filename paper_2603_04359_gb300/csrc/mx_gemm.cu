@@ -93,6 +93,16 @@ struct Place {
   __device__ __forceinline__ uint32_t free() const { return (round - 1) & 1; }
 };
 
+// Whether a barrier's phase is over, without waiting.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t over;
+  asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+               : "=r"(over)
+               : "r"(smem_u32(bar)), "r"(parity)
+               : "memory");
+  return over != 0;
+}
+
 // A whole warp waits (and knows the outcome to be the same in all lanes).
 __device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int line, uint64_t limit) {
   return (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort, line, limit));
@@ -549,8 +559,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (elect_one()) {
           mbar_arrive_expect_tx(fb, bytes + (CG == 2 && rank == 0 ? 4u : 0u));   // (+ the odd CTA's signal)
           tma_load_2d(dst, &tmW, ks * (BK / 2), wrow, fb);
-          for (int b = 0; b < boxes; ++b)
-            tma_load_2d(dst + kStageW + (uint32_t)(b * a.bx) * 128u, &tmX, ks * (BK / 2), xrow + b * a.bx, fb);
+          tma_load_2d(dst + kStageW, &tmX, ks * (BK / 2), xrow, fb);
+          if (boxes > 1)                           // (a loop for the first box too: 6 % of a pair's K step)
+            for (int b = 1; b < boxes; ++b)
+              tma_load_2d(dst + kStageW + (uint32_t)(b * a.bx) * 128u, &tmX, ks * (BK / 2), xrow + b * a.bx, fb);
         }
         __syncwarp();
       }
@@ -619,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t stage16 = a.stage_bytes >> 4;
     auto wait = [&](uint64_t* bar, uint32_t parity, int line) { return all_wait(bar, parity, abort_flag, line, lim); };
     Place st, sl, ac;
-    bool ok = true;
+    bool ok = true, st_in = false, sl_in = false;   // st_in, sl_in: the next stage, slot has been seen full
     int e = 0;
     for (int u = cluster; u < total && ok; u += clusters, ac.next(a.acc_bufs)) {
       const Tile t = tile_at(u, e);
@@ -627,13 +639,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ac.first() && !(ok = wait(&bars->acc_empty[ac.at], ac.free(), __LINE__))) break;
       uint32_t more = 0;                           // accumulate (0: the tile's first MMA)
       for (int ks = k0; ks < k1 && ok; sl.next(a.slots)) {
-        if (!(ok = wait(&bars->tfull[sl.at], sl.full(), __LINE__))) break;
+        if (!__all_sync(0xFFFFFFFFu, sl_in) && !(ok = wait(&bars->tfull[sl.at], sl.full(), __LINE__))) break;
+        sl_in = false;
         const uint32_t sw = scale0 + sl.at * slot_cols, sx = sw + 16;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {              // the slot's two K steps
           if (h == 1 && ks == k1) break;
-          if (!(ok = wait(&bars->full[st.at], st.full(), __LINE__))) break;
+          if (!__all_sync(0xFFFFFFFFu, st_in) && !(ok = wait(&bars->full[st.at], st.full(), __LINE__))) break;
           tc_fence_after();
+          Place next = st;                         // (the next waits are looked at while these MMAs are issued)
+          next.next(a.stages);
+          st_in = mbar_test(&bars->full[next.at], next.full());
+          if (h == 1) {
+            Place next_sl = sl;
+            next_sl.next(a.slots);
+            sl_in = mbar_test(&bars->tfull[next_sl.at], next_sl.full());
+          }
           if (elect_one()) {
             const uint64_t wd = wdesc0 + st.at * stage16, xd = xdesc0 + st.at * stage16;
 #pragma unroll
