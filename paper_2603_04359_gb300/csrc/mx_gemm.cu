@@ -18,7 +18,7 @@
 //
 // Warps (512 threads):
 //   0       TMA of codes              1  issues the MMAs (CG = 2, odd CTA: forwards stages to the even one)
-//   2       TMA of scales, TMEM       3  (CG = 2, odd CTA: forwards scale slots)
+//   2       TMA of scales             3  TMEM (CG = 2, odd CTA: forwards scale slots)
 //   4..7    scales from shared to tensor memory, each to its own 32 lanes (the MMA reads a copy in each)
 //   8..15   epilogue, two warps a lane quadrant, taking 32-token chunks in turn
 // TMEM: accumulators (two where they fit) from column 0, then the scale slots of 512 channels each.  Every wait is
@@ -61,6 +61,7 @@ struct MxArgs {
   uint32_t* status;
   int experts, m, d, d_out;
   int nt;                                   // most tokens of a tile
+  int channel_tiles, token_tiles;           // tiles along each side (token_tiles: not grouped)
   int bx, bxs;                              // token rows per TMA box: codes, scales
   int stages, acc_bufs, slots, xcols;       // xcols: TMEM columns of the tokens' scales per 128 channels
   int split, split_log;                     // CTAs that share a tile's K (CG = 1), a power of two up to 8, and its logarithm
@@ -236,6 +237,9 @@ __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return
 // Named barrier 4: warp 2 has asked for the first scales, warp 0 goes on behind it.
 __device__ __forceinline__ void first_scales_arrive() { asm volatile("bar.arrive 4, 64;" ::: "memory"); }
 __device__ __forceinline__ void first_scales_sync() { asm volatile("bar.sync 4, 64;" ::: "memory"); }
+
+// Named barrier 5: all but the copies' warps, 0 and 2.
+__device__ __forceinline__ void tmem_there_sync() { asm volatile("bar.sync 5, %0;" ::"n"(kThreads - 64) : "memory"); }
 
 // Two float32 bit patterns to bf16, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
@@ -432,12 +436,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);   // (known to be the same in all lanes)
   const uint32_t rank = cluster_rank();
-  const int csize = CG == 2 ? 2 : a.split;       // CTAs of a cluster
-  const int cluster = blockIdx.x / csize, clusters = gridDim.x / csize;
-  const int channel_tiles = (a.d_out + CG * BM - 1) / (CG * BM);
+  const int csize_log = CG == 2 ? 1 : a.split_log;   // CTAs of a cluster
+  const int cluster = blockIdx.x >> csize_log, clusters = gridDim.x >> csize_log;
+  const int channel_tiles = a.channel_tiles, token_tiles = a.token_tiles;
   const int chunks = (a.d + kChunk - 1) / kChunk, steps = (a.d + BK - 1) / BK;
   // this CTA's share of K, in whole chunks
-  const int c0 = CG == 2 ? 0 : (int)rank * chunks / a.split, c1 = CG == 2 ? chunks : ((int)rank + 1) * chunks / a.split;
+  const int c0 = CG == 2 ? 0 : (int)rank * chunks >> a.split_log, c1 = CG == 2 ? chunks : ((int)rank + 1) * chunks >> a.split_log;
   const int k0 = 2 * c0, k1 = min(2 * c1, steps);
 
   if (warp == 2 && lane == 0) {                  // (parameters: no need to wait for the kernel before)
@@ -469,26 +473,33 @@ __global__ void __launch_bounds__(kThreads, 1)
     bars->abort = 0;
     fence_mbar_init();
   }
-  __syncwarp();
+  if constexpr (CG == 2) {
+    cluster_sync();                              // barriers are there, in the whole cluster
+  } else {
+    __syncthreads();
+    cluster_arrive_relaxed();                    // (a split's other CTAs have to be there only when parts are sent)
+  }
   pdl_wait_then_release();                       // nothing global or in tensor memory before this
   const uint64_t lim = g_mx_wait_limit;
-  if (a.offsets) make_table(a, rows, tiles, channel_tiles, tiles + a.experts + 1);
-  if (warp == 2) {
+  if (a.offsets) {
+    make_table(a, rows, tiles, channel_tiles, tiles + a.experts + 1);
+    __syncthreads();
+  }
+  // The copies start here; the others wait for tensor memory.  (The even CTA's MMAs write the odd one's too: they wait for its
+  // scales, which come after its allocation.)
+  uint32_t tmem = 0;
+  if (warp == 3) {
     if constexpr (CG == 2)
       tmem_alloc_pair(&bars->tmem_addr, kTmemCols);
     else
       tmem_alloc(&bars->tmem_addr, kTmemCols);
   }
-  tc_fence_before();
-  if constexpr (CG == 2) {
-    cluster_sync();                              // barriers, table and TMEM address are there, in the whole cluster
-  } else {
-    __syncthreads();
-    cluster_arrive_relaxed();                    // (a split's other CTAs have to be there only when parts are sent)
+  if (warp != 0 && warp != 2) {
+    tc_fence_before();
+    tmem_there_sync();
+    tc_fence_after();
+    tmem = __shfl_sync(0xFFFFFFFFu, bars->tmem_addr, 0);
   }
-  tc_fence_after();
-  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, bars->tmem_addr, 0);
-  const int token_tiles = (a.m + a.nt - 1) / a.nt;
   const int total = a.offsets ? tiles[a.experts] : token_tiles * channel_tiles;
 
   if (a.offsets) {                               // rows of no group
@@ -824,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   if (bars->abort && tid == 0) report(a.status, timeout_bits(kWhereMxGemm, bars->abort));
-  if (warp == 2) {
+  if (warp == 3) {
     tc_fence_after();
     if constexpr (CG == 2)
       tmem_dealloc_pair(tmem, kTmemCols);
@@ -896,6 +907,8 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   a.d = (int)c.d;
   a.d_out = (int)c.d_out;
   a.nt = nt;
+  a.channel_tiles = (int)((c.d_out + CG * BM - 1) / (CG * BM));
+  a.token_tiles = (int)((c.m + nt - 1) / nt);
   a.split = split;
   a.split_log = split == 8 ? 3 : split / 2;
   // boxes of a whole tile's tokens, or with groups, whose tiles differ, of up to 32 a CTA (64 for pairs: many rows)
