@@ -765,9 +765,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld_wait();
           float* part = red + ((size_t)rank * each + ((c * 32) >> a.split_log)) * BM + row;   // (split divides 32)
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c * 32 + i < t.valid)
-              st_cluster(part + (i >> a.split_log) * BM, (uint32_t)i & (a.split - 1), __uint_as_float(r[i]));
+          for (int i0 = 0; i0 < 32; i0 += 8) {         // (out early: a token's code is 0.2 us if all 32 are passed)
+            if (c * 32 + i0 >= t.valid) break;
+#pragma unroll
+            for (int i = i0; i < i0 + 8; ++i)
+              if (c * 32 + i < t.valid)
+                st_cluster(part + (i >> a.split_log) * BM, (uint32_t)i & (a.split - 1), __uint_as_float(r[i]));
+          }
         }
         break;                                     // (a split tile is its cluster's only one)
       }
