@@ -1,6 +1,6 @@
 // The Python calls of the microscaled 4-bit operators, without the interpreter's part of them: checks of the tensors,
 // outputs from torch's allocator, the current stream and the C entry point.  A decode call's kernels take a few
-// microseconds, so the host's time counts: a product took 10.8 us through ctypes and torch's Python, 4 here.
+// microseconds, so the host's time counts: a product took 10.8 us through ctypes and torch's Python, 3.8 here.
 //
 // A function takes what the Python function of the same operator takes, outputs excepted, and returns its result, or the
 // status of a call that the library refused, or None where the arguments are not the ordinary ones (other types, shapes,
@@ -8,7 +8,10 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -39,9 +42,13 @@ bool out_type(PyObject* o, at::ScalarType* t) {
 cat_stream_t stream_of(const at::Tensor& t) {
   return reinterpret_cast<cat_stream_t>(c10::cuda::getCurrentCUDAStream(t.get_device()).stream());
 }
-at::Tensor bytes(const at::Tensor& like, int64_t rows, int64_t cols) {
-  return at::empty({rows, cols}, like.options().dtype(at::kByte));
+// A new tensor on `like`'s device, from torch's allocator without its dispatcher (0.44 us, 0.81 with it).
+at::Tensor make(const at::Tensor& like, int64_t rows, int64_t cols, at::ScalarType type) {
+  if (like.get_device() != c10::cuda::current_device()) return at::empty({rows, cols}, like.options().dtype(type));
+  return at::detail::empty_generic({rows, cols}, c10::cuda::CUDACachingAllocator::get(),
+                                   c10::DispatchKeySet(c10::DispatchKey::CUDA), type, c10::nullopt);
 }
+at::Tensor bytes(const at::Tensor& like, int64_t rows, int64_t cols) { return make(like, rows, cols, at::kByte); }
 uint8_t* u8(const at::Tensor& t) { return static_cast<uint8_t*>(t.data_ptr()); }
 
 // Codes [.., half] and scales [.., pitch] of one device; the rows' shapes are the caller's to compare.
@@ -117,7 +124,7 @@ PyObject* rmsnorm_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (args[3] != Py_None && (!(r = dense(args[3], 2)) || r->scalar_type() != x->scalar_type() || r->size(0) != n || r->size(1) != d ||
                              r->get_device() != x->get_device()))
     Py_RETURN_NONE;
-  const at::Tensor h = r ? at::empty({n, d}, x->options()) : *x;
+  const at::Tensor h = r ? make(*x, n, d, x->scalar_type()) : *x;
   const at::Tensor xq = bytes(*x, n, d / 2), xs = bytes(*x, n, (d + 511) / 512 * 16);
   const cat_status st = cat_mx_rmsnorm_quantize(x->data_ptr(), r ? r->data_ptr() : nullptr, code(*x), w->data_ptr(), code(*w), n, d,
                                                 (float)eps, r ? h.data_ptr() : nullptr, u8(xq), u8(xs), stream_of(*x));
@@ -133,7 +140,7 @@ PyObject* dequantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   at::ScalarType type;
   if (!form(q, s, q ? q->get_device() : -1) || !out_type(args[2], &type)) Py_RETURN_NONE;
   const int64_t n = q->size(0), d = 2 * q->size(1);
-  const at::Tensor out = at::empty({n, d}, q->options().dtype(type));
+  const at::Tensor out = make(*q, n, d, type);
   const cat_status st = cat_mx_dequantize(u8(*q), u8(*s), n, d, code(out), out.data_ptr(), stream_of(*q));
   return st == CAT_OK ? THPVariable_Wrap(out) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
@@ -148,7 +155,7 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t device = q ? q->get_device() : -1;
   if (!form(q, s, device) || !form(wq, ws, device) || wq->size(1) != q->size(1) || !out_type(args[4], &type)) Py_RETURN_NONE;
   const int64_t n = q->size(0), d_out = wq->size(0);
-  const at::Tensor y = at::empty({n, d_out}, q->options().dtype(type));
+  const at::Tensor y = make(*q, n, d_out, type);
   const cat_status st = cat_mx_linear(u8(*q), u8(*s), u8(*wq), u8(*ws), n, 2 * q->size(1), d_out, code(y), y.data_ptr(), stream_of(*q));
   return st == CAT_OK ? THPVariable_Wrap(y) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
@@ -166,7 +173,7 @@ PyObject* linear_grouped(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       o->size(0) != wq->size(0) + 1 || o->get_device() != device || !out_type(args[5], &type))
     Py_RETURN_NONE;
   const int64_t m = q->size(0), d_out = wq->size(1);
-  const at::Tensor y = at::empty({m, d_out}, q->options().dtype(type));
+  const at::Tensor y = make(*q, m, d_out, type);
   const cat_status st = cat_mx_linear_grouped(u8(*q), u8(*s), u8(*wq), u8(*ws), static_cast<const int32_t*>(o->data_ptr()),
                                               wq->size(0), m, 2 * q->size(1), d_out, code(y), y.data_ptr(), stream_of(*q));
   return st == CAT_OK ? THPVariable_Wrap(y) : PyLong_FromLong(st);
