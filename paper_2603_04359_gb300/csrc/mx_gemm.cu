@@ -765,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld_wait();
           float* part = red + ((size_t)rank * each + ((c * 32) >> a.split_log)) * BM + row;   // (split divides 32)
 #pragma unroll
-          for (int i0 = 0; i0 < 32; i0 += 8) {         // (out early: a token's code is 0.2 us if all 32 are passed)
+          for (int i0 = 0; i0 < 32; i0 += 8) {     // (1 x 4096 -> 6144: all 32 passed 7.2 us, out early 6.9)
             if (c * 32 + i0 >= t.valid) break;
 #pragma unroll
             for (int i = i0; i < i0 + 8; ++i)
@@ -981,14 +981,15 @@ struct Form {
   int cg, nt, split;
 };
 
-// The form of least estimated time.  A round of tiles costs its K steps, at least 0.28 us each (a stage's turn) and a little
-// for its tokens, whatever is between 8 and 256 of them; so as few rounds as can be, and in them the narrowest tiles.  With
+// The form of least estimated time.  A round of tiles costs its K steps, about 0.28 us each (the issuing warps' instructions)
+// and a little for its tokens, whatever is between 8 and 256 of them; so as few rounds as can be, and in them the narrowest tiles.  With
 // many CTAs a step takes what its bytes do: the weights from memory (6 TB/s), all operands from L2 (16 TB/s); and a round
 // never takes less than its outputs' way out.  The constants (us) are fitted to bf16 outputs of 1 to 512 tokens on
 // 4096 -> 6144, 4096 -> 14336, 14336 -> 4096, 4096 -> 4096, 1024 -> 1024 and 2048 -> 640, and of 521 to 8192 on K of 256 to
-// 7040, within 15 % of each time: one token, 4096 -> 6144: K in two 7.6, whole 8.6; 128 tokens, 14336 -> 4096: K in four
-// 13.8, in two (64-wide) 15.7, pairs 20.8; 200, 4096 -> 14336: pairs (one round) 12.2, single CTAs (two) 15.5; 512,
-// 4096 -> 4096: 128-wide 10.4, 256-wide 11.8; 3843, 2560 -> 3712: pairs 22.2, single CTAs 25.6.
+// 7040.  Of 90 other calls of 1 to 8192 tokens, 256 to 14336 -> 64 to 28672, the form taken is on average 1 % slower than the
+// best of 3 to 25 tried, at most 12 %.  One token, 4096 -> 6144: K in two 7.0 us, whole 7.9; 128 tokens, 14336 -> 4096: K in
+// four 13.6, in two (64-wide) 14.7, pairs 18.7; 200, 4096 -> 14336: pairs (one round) 11.8, single CTAs (two) 14.4; 512,
+// 4096 -> 4096: 128-wide 9.7, 256-wide 11.4; 3843, 2560 -> 3712: pairs 22.7, single CTAs 24.0.
 Form pick_form(int64_t groups, int64_t rows, int64_t d, int64_t d_out) {
   const int64_t sms = sm_count(), chunks = (d + kChunk - 1) / kChunk;
   const double steps = (double)((d + BK - 1) / BK);
