@@ -34,12 +34,14 @@ __device__ __forceinline__ float max_magnitude(float a, float b) {
 
 // silu(g) u: g / (1 + exp(-g)) u, by 2^x and the reciprocal, each within two units of the last place (and the rounding of
 // g log2 e, |g| 2^-24), without the steps that subnormal numbers take: 2^x below 2^-126 adds nothing to 1, and the reciprocal
-// of (1 + exp(-g)) / 16 is 2^-124 or more, or 0 of infinity (4096 x 14336 bf16: 40 us, 46 with those steps).
+// of (1 + exp(-g)) / 16 is 2^-124 or more, or 0 of infinity (4096 x 14336 bf16: 40 us, 46 with those steps).  The sixteenth goes
+// back into the reciprocal, not into g: of that it would take a subnormal gate's last bits, which a large u brings back.  (Below
+// g = -87.3 the factor is subnormal itself and rounded by up to 2^-22 of it.)
 __device__ __forceinline__ float swiglu(float g, float u) {
   float e, r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaf(e, 0.0625f, 0.0625f)));
-  return g * 0.0625f * r * u;
+  return g * (0.0625f * r) * u;
 }
 
 // 32 bytes from or to memory, at once where they lie on a 32-byte boundary (`wide`).
