@@ -350,8 +350,9 @@ __device__ __forceinline__ bool finish_half(const NormArgs& a, int64_t row, int 
     }
     float w[16];
     load_weights(static_cast<const W*>(a.weight) + (int64_t)half * 16, w);
+    // (h times the factor is at most sqrt(d); h times the weight could leave float32's range on the way to a value within it)
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v.r[k] = __float_as_uint(h[k] * w[k] * r);   // (bf16 times bf16 is mostly exact: one rounding, of the last product)
+    for (int k = 0; k < 16; ++k) v.r[k] = __float_as_uint(h[k] * r * w[k]);
   }
   uint32_t b;
   const uint2 c = quantize_half(v, &b);

@@ -29,3 +29,27 @@ def test_swiglu_of_gates_below_the_smallest_normal_number():
     assert np.array_equal(held[:, :d], g)
     near(*cat.cat_mx_swiglu_quantize(gu), held[:, :d] / (1 + np.exp(-held[:, :d])) * held[:, d:])
     assert cat.cat_device_status()[0] == 0
+
+
+# a row kernel each: a warp, a CTA with one and with two halves a thread, two readings
+WIDTHS = [96, 512, 4096, 9024, 14336, 40000]
+
+
+def check_norm(x, r, w, eps):
+    """The norm with the residual against float64: the sum exactly, the 4-bit form as near as `near` asks."""
+    for res in (r, None):
+        xq, xs, h = cat.cat_mx_rmsnorm_quantize(x, w, eps, residual=res)
+        total = host(x) + (host(res) if res is not None else 0.0)
+        assert torch.equal(h, (x.float() + res.float()).to(x.dtype) if res is not None else x)
+        near(xq, xs, total / np.sqrt((total ** 2).mean(-1, keepdims=True) + eps) * host(w))
+    assert cat.cat_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size,gain,eps", [(1e15, 1e30, 1e-5), (1e-15, 1e-30, 1e-35)])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_whose_gain_and_values_leave_the_range_together(d, size, gain, eps, dtype):
+    """Values times gain would overflow or vanish; the normalized value times gain is an ordinary number."""
+    rng = np.random.default_rng(d)
+    x, r = (dev(size * rng.standard_normal((5, d)), TYPES[dtype]) for _ in range(2))
+    check_norm(x, r, dev(gain * (1 + 0.2 * rng.standard_normal(d)), TYPES[dtype]), eps)
