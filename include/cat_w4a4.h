@@ -535,7 +535,8 @@ cat_status cat_mx_swiglu_quantize(const void* gu, cat_dtype dtype, int64_t n, in
 /*
  * cat_mx_rmsnorm_quantize -- residual addition, root-mean-square norm and quantization of its output:
  *   h = x + residual;   v = h / sqrt(mean_i h_i^2 + eps) * weight;   xq, xs = the 4-bit form of v
- * all in float32; v is of the sum before it is rounded to h's type.
+ * all in float32; v is of the sum before it is rounded to h's type.  Rows whose squares leave float32's range are normalized
+ * all the same (a row of zeros with eps = 0, and with eps = 0 one whose root mean square is below 2^-127, gets NaN scales).
  *   x, residual  device [n][d] in `dtype`; residual may be NULL (h = x).
  *   weight       device [d] in `weight_dtype`.
  *   h            out, device [n][d] in `dtype`; may be x or residual themselves, and may be NULL (not written).

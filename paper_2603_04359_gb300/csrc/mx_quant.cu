@@ -329,8 +329,25 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   return v;
 }
-__device__ __forceinline__ float row_factor(const NormArgs& a, float sum) {
-  return __frsqrt_rn(sum / (float)(a.halves * 16) + a.eps);
+__device__ __forceinline__ float mean_square(const NormArgs& a, float sum) { return sum / (float)(a.halves * 16) + a.eps; }
+__device__ __forceinline__ float row_factor(float mean) { return __frsqrt_rn(mean); }
+
+// Rows whose squares leave float32's range, though the norm does not (|h| from about 1e19 on, or below 1e-19 with an eps of
+// nothing): their sum is infinite, or has lost what was below 2^-126.  Such a row is summed again times a power of two that
+// brings it back: a mean of 2^110 or more (d is at most 2^18) to at most 2^106 and at least 2^-40, one below 2^-80 to at
+// most 2^100.  The factor of the scaled row times the power is the row's own.  (eps of 2^-80 or more keeps a mean from being small.)
+__device__ __forceinline__ bool out_of_range(float mean) { return mean < 0x1p-80f || mean == __int_as_float(0x7F800000); }
+__device__ __forceinline__ float back_in_range(float mean) { return mean < 1.f ? 0x1p90f : 0x1p-75f; }
+__device__ __forceinline__ float scaled_factor(const NormArgs& a, float sum, float by) {
+  return __frsqrt_rn(sum / (float)(a.halves * 16) + a.eps * by * by) * by;
+}
+__device__ __forceinline__ float scaled_squares(const float (&h)[16], float by, float sq) {
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const float v = h[k] * by;
+    sq = fmaf(v, v, sq);
+  }
+  return sq;
 }
 
 // The second half of a row's work for half a block (whole warps; lanes past the row's end hold nothing): h and the 4-bit
@@ -374,7 +391,13 @@ __global__ void __launch_bounds__(kThreads) mx_rmsnorm_warp_kernel(const __grid_
       p.load(a, row * a.halves + lane);
       sq = p.sum(a, h, 0.f);
     }
-    bad |= finish_half<T, W>(a, row, lane, h, row_factor(a, warp_sum(sq)));
+    const float mean = mean_square(a, warp_sum(sq));
+    float r = row_factor(mean);
+    if (out_of_range(mean)) {                            // (the same in all lanes)
+      const float by = back_in_range(mean);
+      r = scaled_factor(a, warp_sum(lane < a.halves ? scaled_squares(h, by, 0.f) : 0.f), by);
+    }
+    bad |= finish_half<T, W>(a, row, lane, h, r);
   }
   if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(a.status, kStatusNonFinite);
 }
@@ -406,7 +429,20 @@ __global__ void __launch_bounds__(kRowThreads, sizeof(T) * ITEMS == 2 ? 2 : 1)
     sq = warp_sum(sq);
     if (lane == 0) part[turn][warp] = sq;
     __syncthreads();                                     // (part[] has two turns, so one barrier a row will do)
-    const float r = row_factor(a, warp_sum(lane < warps ? part[turn][lane] : 0.f));
+    const float mean = mean_square(a, warp_sum(lane < warps ? part[turn][lane] : 0.f));
+    float r = row_factor(mean);
+    if (out_of_range(mean)) {                            // (the same in all threads)
+      const float by = back_in_range(mean);
+      sq = 0.f;
+#pragma unroll
+      for (int j = 0; j < ITEMS; ++j)
+        if (j * (int)blockDim.x + (int)threadIdx.x < a.halves) sq = scaled_squares(h[j], by, sq);
+      sq = warp_sum(sq);
+      __syncthreads();                                   // the first sums have been read
+      if (lane == 0) part[turn][warp] = sq;
+      __syncthreads();
+      r = scaled_factor(a, warp_sum(lane < warps ? part[turn][lane] : 0.f), by);
+    }
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
       const int half = j * blockDim.x + threadIdx.x;
@@ -416,7 +452,7 @@ __global__ void __launch_bounds__(kRowThreads, sizeof(T) * ITEMS == 2 ? 2 : 1)
   if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) report(a.status, kStatusNonFinite);
 }
 
-// Longer rows are read twice (before h is written).
+// Longer rows are read twice (before h is written), rows that leave the range three times.
 template <typename T, typename W>
 __global__ void __launch_bounds__(kRowThreads) mx_rmsnorm_long_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float part[32];
@@ -433,7 +469,22 @@ __global__ void __launch_bounds__(kRowThreads) mx_rmsnorm_long_kernel(const __gr
     sq = warp_sum(sq);
     if (lane == 0) part[warp] = sq;
     __syncthreads();
-    const float r = row_factor(a, warp_sum(lane < warps ? part[lane] : 0.f));
+    const float mean = mean_square(a, warp_sum(lane < warps ? part[lane] : 0.f));
+    float r = row_factor(mean);
+    if (out_of_range(mean)) {                            // (the same in all threads)
+      const float by = back_in_range(mean);
+      sq = 0.f;
+      for (int half = threadIdx.x; half < a.halves; half += blockDim.x) {
+        p.load(a, row * a.halves + half);
+        p.sum(a, h, 0.f);
+        sq = scaled_squares(h, by, sq);
+      }
+      sq = warp_sum(sq);
+      __syncthreads();                                   // the first sums have been read
+      if (lane == 0) part[warp] = sq;
+      __syncthreads();
+      r = scaled_factor(a, warp_sum(lane < warps ? part[lane] : 0.f), by);
+    }
     for (int half = threadIdx.x; half - lane < a.halves; half += blockDim.x) {
       if (half < a.halves) {
         p.load(a, row * a.halves + half);

@@ -53,3 +53,42 @@ def test_norm_whose_gain_and_values_leave_the_range_together(d, size, gain, eps,
     rng = np.random.default_rng(d)
     x, r = (dev(size * rng.standard_normal((5, d)), TYPES[dtype]) for _ in range(2))
     check_norm(x, r, dev(gain * (1 + 0.2 * rng.standard_normal(d)), TYPES[dtype]), eps)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size,eps", [(1e20, 1e-5), (1e28, 0.0), (1e37, 1e-5), (1e-21, 0.0), (1e-30, 0.0), (1e-22, 2.0 ** -149)])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_whose_squares_leave_the_range(d, size, eps, dtype):
+    """Squares overflow or vanish, the norm does not: rows of such values beside an ordinary row."""
+    rng = np.random.default_rng(d + 1)
+    rows = np.array([size, 1.0, size, 3 * size, size])[:, None]
+    x, r = (dev(rows * rng.standard_normal((5, d)), TYPES[dtype]) for _ in range(2))
+    check_norm(x, r, dev(1 + 0.2 * rng.standard_normal(d), TYPES[dtype]), eps)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_of_the_largest_numbers(d, dtype):
+    """Every value the largest of its type: the normalized ones are 1."""
+    largest = torch.finfo(TYPES[dtype]).max
+    x = torch.full((3, d), largest, dtype=TYPES[dtype], device="cuda")
+    x[1, ::2] = -largest
+    xq, xs, _ = cat.cat_mx_rmsnorm_quantize(x, torch.full((d,), 1.01, device="cuda"), 1e-5)
+    v = cat.cat_mx_dequantize(xq, xs)
+    assert torch.equal(v, torch.sign(x.float()))                    # 1.01 is nearest to 1
+    assert cat.cat_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_of_an_infinity_beside_rows_out_of_range(d):
+    """A row with an infinity still says so, with NaN in its block and zeros elsewhere; rows of zeros with eps = 0 are NaN."""
+    x = torch.full((4, d), 1e25, device="cuda")
+    x[1, 40] = float("inf")
+    x[2] = 0.0
+    xq, xs, _ = cat.cat_mx_rmsnorm_quantize(x, torch.ones(d, device="cuda"), 0.0)
+    v = cat.cat_mx_dequantize(xq, xs)
+    # 1 is a power of two: known to 1e-5, a block's largest value may be below it, under half the scale, and 6 / 8 the most there
+    assert bool(((v[0] == 1.0) | (v[0] == 0.75)).all()) and torch.equal(v[3], v[0])
+    assert torch.isnan(v[1, 32:64]).all() and not v[1, :32].any() and not v[1, 64:].any()
+    assert torch.isnan(v[2]).all()
+    assert cat.cat_device_status()[0] == 4
