@@ -3,7 +3,7 @@
 A thin ctypes binding of the C ABI in ``include/cat_w4a4.h``: every function below has the name
 of the C entry point it calls, takes torch tensors, allocates outputs with torch on the tensors'
 device when none are given, passes raw pointers and the current CUDA stream, and raises
-``CatError`` on a non-zero status.  All arithmetic runs in the library's CUDA kernels (or, for
+``CatError`` on a non-zero status.  Tensors have to be on the current device (ValueError).  All arithmetic runs in the library's CUDA kernels (or, for
 ``cat_build_transform_host``, in its host code); there is no fallback path.
 """
 from __future__ import annotations
@@ -136,6 +136,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream(device: torch.device) -> int:
+    """The current stream of the tensors' device, which has to be the current one: the library launches, and keeps its
+    status word, on the current device."""
+    current = torch._C._cuda_getDevice()
+    if device.index is not None and device.index != current:
+        raise ValueError(f"the tensors are on {device}, but the current device is cuda:{current}: make theirs current "
+                         f"(torch.cuda.device) for the call")
     if _raw_stream is None or device.index is None:
         return torch.cuda.current_stream(device).cuda_stream
     return _raw_stream(device.index)
