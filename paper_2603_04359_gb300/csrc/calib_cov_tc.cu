@@ -27,11 +27,11 @@
 // they take the longest chunks that leave three or four in flight: 256 tokens, 128 at k = 256.  16384 tokens x
 // 4096 channels: 41.5 us with 64-token chunks, 33.5 now.
 #include <cstring>
-#include <mutex>
 
 #include "common.cuh"
 #include "gemm_pair.cuh"
 #include "per_device.h"
+#include "tensor_map.h"
 
 namespace cat {
 namespace {
@@ -469,23 +469,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  });
-  return fn;
 }
 
 int num_sms() {

@@ -49,13 +49,13 @@
 // most half full is split along K (see the split-tail section below).  Every wait is bounded; a wait
 // that gives up raises the device status word and all roles drain and exit.
 #include <cstring>
-#include <mutex>
 #include <type_traits>
 
 #include "common.cuh"
 #include "gemm_pair.cuh"
 #include "per_device.h"
 #include "sqnr_slot.cuh"
+#include "tensor_map.h"
 
 namespace cat {
 namespace {
@@ -792,23 +792,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc_fence_after();
     tmem_dealloc_pair(tmem, L::kTmem);
   }
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  });
-  return fn;
 }
 
 // y [n][d_out] fp32, box 32 x 32, 128-byte swizzle (matches the epilogue staging layout).

@@ -24,11 +24,11 @@
 // TMEM: accumulators (two where they fit) from column 0, then the scale slots of 512 channels each.  Every wait is
 // bounded; a wait that gives up raises the device status word and all roles drain and exit.
 #include <cstring>
-#include <mutex>
 
 #include "gemm_pair.cuh"
 #include "mx_format.cuh"
 #include "per_device.h"
+#include "tensor_map.h"
 
 namespace cat {
 namespace {
@@ -844,23 +844,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     else
       tmem_dealloc(tmem, kTmemCols);
   }
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  });
-  return fn;
 }
 
 // Bytes [rows][row_bytes], box [box_rows][box_bytes] with a swizzle of its row, out-of-range reads zero.

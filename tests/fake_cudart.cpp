@@ -41,6 +41,8 @@ thread_local struct {
   cudaStream_t stream;
 } pushed;
 const int sms = 152;
+bool want_context = false;           // tensor maps are encoded as the driver does it: in threads that have a context
+thread_local bool has_context = false;
 
 // Clusters of one-CTA-per-SM kernels that are resident at once: a cluster stays in a group of SMs (76 of two CTAs, 36 of
 // four, 15 of eight and 7 of sixteen, as a GB300 answers).
@@ -69,6 +71,7 @@ bool backed(const void* p) { return (uintptr_t)p >> 40 != 0x10; }
 CUresult encode(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                 const cuuint32_t* box, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                 CUtensorMapFloatOOBfill) {
+  if (want_context && !has_context) return CUDA_ERROR_INVALID_CONTEXT;
   boxes.push_back((int)box[1]);
   return CUDA_SUCCESS;
 }
@@ -84,6 +87,7 @@ void fake_reset() {
   boxes.clear();
 }
 void fake_set_device(int d) { device = d; }
+void fake_want_context(int want) { want_context = want != 0; }
 void fake_record_arg(const char* kernel, int index) { wanted[kernel] = index; }
 int fake_boxes() { return (int)boxes.size(); }
 int fake_box_rows(int i) { return boxes[i]; }
@@ -146,6 +150,11 @@ cudaError_t cudaGetLastError() {
 const char* cudaGetErrorString(cudaError_t e) { return e == cudaSuccess ? "no error" : "refused by the fake runtime"; }
 cudaError_t cudaGetDevice(int* d) {
   *d = device;
+  return cudaSuccess;
+}
+cudaError_t cudaSetDevice(int d) {
+  device = d;
+  has_context = true;
   return cudaSuccess;
 }
 cudaError_t cudaDeviceGetAttribute(int* v, enum cudaDeviceAttr a, int) {
