@@ -75,6 +75,23 @@ PyObject* wrap(std::initializer_list<at::Tensor> out) {
   return tuple;
 }
 
+// What a call does behind its checks -- its outputs' allocation and the launch -- goes without the interpreter's lock: a thread
+// that waits for memory, or for room in the launch queue, does not stop the others.
+class Unlocked {
+ public:
+  Unlocked() : state_(PyEval_SaveThread()) {}
+  ~Unlocked() { PyEval_RestoreThread(state_); }
+  Unlocked(const Unlocked&) = delete;
+
+ private:
+  PyThreadState* state_;
+};
+template <typename F>
+cat_status unlocked(F&& call) {
+  const Unlocked here;
+  return call();
+}
+
 bool count(Py_ssize_t got, Py_ssize_t want) {
   if (got == want) return true;
   PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, got);
@@ -92,9 +109,12 @@ PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (args[1] != Py_None && (!(rows = dense(args[1], 1)) || rows->scalar_type() != at::kInt || rows->get_device() != x->get_device()))
     Py_RETURN_NONE;
   const int64_t m = rows ? rows->size(0) : n;
-  const at::Tensor xq = bytes(m, d / 2), xs = bytes(m, (d + 511) / 512 * 16);
-  const cat_status st = cat_mx_quantize(x->data_ptr(), code(*x), n, d, rows ? static_cast<const int32_t*>(rows->data_ptr()) : nullptr,
-                                        m, u8(xq), u8(xs), stream_of(*x));
+  at::Tensor xq, xs;
+  const cat_status st = unlocked([&] {
+    xq = bytes(m, d / 2), xs = bytes(m, (d + 511) / 512 * 16);
+    return cat_mx_quantize(x->data_ptr(), code(*x), n, d, rows ? static_cast<const int32_t*>(rows->data_ptr()) : nullptr, m, u8(xq),
+                           u8(xs), stream_of(*x));
+  });
   return st == CAT_OK ? wrap({xq, xs}) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }
@@ -106,8 +126,11 @@ PyObject* swiglu_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const at::Tensor* gu = dense(args[0], 2);
   if (!gu || !real(*gu) || gu->size(1) % 2 || !current(*gu)) Py_RETURN_NONE;
   const int64_t n = gu->size(0), d = gu->size(1) / 2;
-  const at::Tensor xq = bytes(n, d / 2), xs = bytes(n, (d + 511) / 512 * 16);
-  const cat_status st = cat_mx_swiglu_quantize(gu->data_ptr(), code(*gu), n, d, u8(xq), u8(xs), stream_of(*gu));
+  at::Tensor xq, xs;
+  const cat_status st = unlocked([&] {
+    xq = bytes(n, d / 2), xs = bytes(n, (d + 511) / 512 * 16);
+    return cat_mx_swiglu_quantize(gu->data_ptr(), code(*gu), n, d, u8(xq), u8(xs), stream_of(*gu));
+  });
   return st == CAT_OK ? wrap({xq, xs}) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }
@@ -125,10 +148,13 @@ PyObject* rmsnorm_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (args[3] != Py_None && (!(r = dense(args[3], 2)) || r->scalar_type() != x->scalar_type() || r->size(0) != n || r->size(1) != d ||
                              r->get_device() != x->get_device()))
     Py_RETURN_NONE;
-  const at::Tensor h = r ? make(n, d, x->scalar_type()) : *x;
-  const at::Tensor xq = bytes(n, d / 2), xs = bytes(n, (d + 511) / 512 * 16);
-  const cat_status st = cat_mx_rmsnorm_quantize(x->data_ptr(), r ? r->data_ptr() : nullptr, code(*x), w->data_ptr(), code(*w), n, d,
-                                                (float)eps, r ? h.data_ptr() : nullptr, u8(xq), u8(xs), stream_of(*x));
+  at::Tensor h = *x, xq, xs;
+  const cat_status st = unlocked([&] {
+    if (r) h = make(n, d, x->scalar_type());
+    xq = bytes(n, d / 2), xs = bytes(n, (d + 511) / 512 * 16);
+    return cat_mx_rmsnorm_quantize(x->data_ptr(), r ? r->data_ptr() : nullptr, code(*x), w->data_ptr(), code(*w), n, d, (float)eps,
+                                   r ? h.data_ptr() : nullptr, u8(xq), u8(xs), stream_of(*x));
+  });
   return st == CAT_OK ? wrap({xq, xs, h}) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }
@@ -141,8 +167,11 @@ PyObject* dequantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   at::ScalarType type;
   if (!form(q, s, q ? q->get_device() : -1) || !out_type(args[2], &type) || !current(*q)) Py_RETURN_NONE;
   const int64_t n = q->size(0), d = 2 * q->size(1);
-  const at::Tensor out = make(n, d, type);
-  const cat_status st = cat_mx_dequantize(u8(*q), u8(*s), n, d, code(out), out.data_ptr(), stream_of(*q));
+  at::Tensor out;
+  const cat_status st = unlocked([&] {
+    out = make(n, d, type);
+    return cat_mx_dequantize(u8(*q), u8(*s), n, d, code(out), out.data_ptr(), stream_of(*q));
+  });
   return st == CAT_OK ? THPVariable_Wrap(out) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }
@@ -157,8 +186,11 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (!form(q, s, device) || !form(wq, ws, device) || wq->size(1) != q->size(1) || !out_type(args[4], &type) || !current(*q))
     Py_RETURN_NONE;
   const int64_t n = q->size(0), d_out = wq->size(0);
-  const at::Tensor y = make(n, d_out, type);
-  const cat_status st = cat_mx_linear(u8(*q), u8(*s), u8(*wq), u8(*ws), n, 2 * q->size(1), d_out, code(y), y.data_ptr(), stream_of(*q));
+  at::Tensor y;
+  const cat_status st = unlocked([&] {
+    y = make(n, d_out, type);
+    return cat_mx_linear(u8(*q), u8(*s), u8(*wq), u8(*ws), n, 2 * q->size(1), d_out, code(y), y.data_ptr(), stream_of(*q));
+  });
   return st == CAT_OK ? THPVariable_Wrap(y) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }
@@ -175,9 +207,12 @@ PyObject* linear_grouped(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       o->size(0) != wq->size(0) + 1 || o->get_device() != device || !out_type(args[5], &type) || !current(*q))
     Py_RETURN_NONE;
   const int64_t m = q->size(0), d_out = wq->size(1);
-  const at::Tensor y = make(m, d_out, type);
-  const cat_status st = cat_mx_linear_grouped(u8(*q), u8(*s), u8(*wq), u8(*ws), static_cast<const int32_t*>(o->data_ptr()),
-                                              wq->size(0), m, 2 * q->size(1), d_out, code(y), y.data_ptr(), stream_of(*q));
+  at::Tensor y;
+  const cat_status st = unlocked([&] {
+    y = make(m, d_out, type);
+    return cat_mx_linear_grouped(u8(*q), u8(*s), u8(*wq), u8(*ws), static_cast<const int32_t*>(o->data_ptr()), wq->size(0), m,
+                                 2 * q->size(1), d_out, code(y), y.data_ptr(), stream_of(*q));
+  });
   return st == CAT_OK ? THPVariable_Wrap(y) : PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }
