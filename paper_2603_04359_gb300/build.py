@@ -3,7 +3,8 @@
 Every translation unit is compiled by ``nvcc`` in parallel, then linked into one shared library
 next to this file.  The CUDA runtime is linked statically; the driver API (tensor-map encoding)
 is reached through ``cudaGetDriverEntryPointByVersion``, so nothing links against libcuda.  The Python
-calls of the microscaled operators (``_mx_calls.so``, on torch's C++ headers) link against that library.
+calls of the microscaled operators (``_mx_calls``, an extension module of this interpreter on torch's C++ headers) link
+against that library, which is there without them: where they do not build, the build says so and fails behind it.
 """
 from __future__ import annotations
 
@@ -20,7 +21,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcatw4a4.so")
 SOURCES = ["api.cu", "calib_cov.cu", "calib_cov_tc.cu", "act_quant.cu", "act_quant_tc.cu", "act_quant_few.cu", "gemm_tc.cu", "gemm_decode.cu", "gemm_decode_tc.cu", "sqnr.cu", "diag.cu", "quant_dp.cu", "gemm_dp.cu", "transform_dev.cu", "mx_quant.cu", "mx_gemm.cu", "transform_host.cpp"]
-CALLS = os.path.join(HERE, "_mx_calls.so")
+CALLS = os.path.join(HERE, "_mx_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-O3,-pthread", "-I", os.path.join(ROOT, "include")]
 
@@ -67,7 +68,7 @@ def _link_calls(obj: str) -> None:
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = CALLS + ".tmp"
     _run(["g++", "-shared", "-pthread", "-o", tmp, obj, "-L", HERE, "-l:" + os.path.basename(LIB), "-L", libs, "-ltorch_python",
-          "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"], "linking _mx_calls.so")
+          "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"], "linking _mx_calls")
     os.replace(tmp, CALLS)
 
 
@@ -76,12 +77,11 @@ def build(verbose: bool = False) -> str:
     with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         calls = ex.submit(_compile_calls)
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
-        calls_obj = calls.result()
     tmp = LIB + ".tmp"
     cmd = [nvcc(), *ARCH, "-shared", "-Xcompiler", "-pthread", "-o", tmp, *objs]
     _run(cmd, "link")
     os.replace(tmp, LIB)
-    _link_calls(calls_obj)
+    _link_calls(calls.result())
     return LIB
 
 
