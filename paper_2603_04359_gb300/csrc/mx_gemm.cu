@@ -880,6 +880,18 @@ struct Call {
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
+// Tensor memory of tiles of up to nt tokens: accumulators, two where two slots of scales fit beside them (to 192 tokens).
+struct Columns {
+  int xcols, acc_bufs, slots;
+  explicit Columns(int nt) {
+    xcols = 2 * ((nt + 63) / 64);
+    const int npad = (nt + 31) / 32 * 32, slot_cols = 16 + 4 * xcols;
+    acc_bufs = 2 * npad + 2 * slot_cols <= (int)kTmemCols ? 2 : 1;
+    slots = ((int)kTmemCols - acc_bufs * npad) / slot_cols;
+    if (slots > kMaxSlots) slots = kMaxSlots;
+  }
+};
+
 template <int CG, typename T, bool WHOLE>
 cudaError_t launch_form(const Call& c, int nt, int split) {
   MxArgs a;
@@ -900,11 +912,10 @@ cudaError_t launch_form(const Call& c, int nt, int split) {
   constexpr int kGroupBox = 32 * CG;
   a.bx = c.offsets && nt / CG > kGroupBox ? kGroupBox : nt / CG;
   a.bxs = c.offsets && nt > kGroupBox ? kGroupBox : nt;
-  a.xcols = 2 * ((nt + 63) / 64);
-  const int npad = (nt + 31) / 32 * 32, slot_cols = 16 + 4 * a.xcols;
-  a.acc_bufs = 2 * npad + 2 * slot_cols <= (int)kTmemCols ? 2 : 1;
-  const int slots = ((int)kTmemCols - a.acc_bufs * npad) / slot_cols;
-  a.slots = slots < kMaxSlots ? slots : kMaxSlots;
+  const Columns columns(nt);
+  a.xcols = columns.xcols;
+  a.acc_bufs = columns.acc_bufs;
+  a.slots = columns.slots;
   a.stage_bytes = kStageW + (uint32_t)up(nt / CG, a.bx) * 128u;
   a.ring_bytes = kScalesW + (uint32_t)up(up(nt, a.bxs), 64) * kScaleRow;
   const size_t red = split > 1 ? (size_t)split * ((nt + split - 1) / split) * BM * 4 : 0;
@@ -970,7 +981,8 @@ struct Form {
 // 7040.  Of 90 other calls of 1 to 8192 tokens, 256 to 14336 -> 64 to 28672, the form taken is on average 1 % slower than the
 // best of 3 to 25 tried, at most 12 %.  One token, 4096 -> 6144: K in two 7.0 us, whole 7.9; 128 tokens, 14336 -> 4096: K in
 // four 13.6, in two (64-wide) 14.7, pairs 18.7; 200, 4096 -> 14336: pairs (one round) 11.8, single CTAs (two) 14.4; 512,
-// 4096 -> 4096: 128-wide 9.7, 256-wide 11.4; 3843, 2560 -> 3712: pairs 22.7, single CTAs 24.0.
+// 4096 -> 4096: 128-wide 9.7, 256-wide 11.4; 3843, 2560 -> 3712: pairs 22.7, single CTAs 24.0; 4674, 1440 -> 2176: pairs of 192
+// tokens (two accumulators) 16.9, single CTAs 20.1.
 Form pick_form(int64_t groups, int64_t rows, int64_t d, int64_t d_out) {
   const int64_t sms = sm_count(), chunks = (d + kChunk - 1) / kChunk;
   const double steps = (double)((d + BK - 1) / BK);
@@ -992,13 +1004,12 @@ Form pick_form(int64_t groups, int64_t rows, int64_t d, int64_t d_out) {
     double step = cg == 1 ? 0.28 + 0.0003 * nt : 0.29 + 0.0002 * nt;
     step = step < from_memory ? from_memory : step;
     step = step < from_l2 ? from_l2 : step;
-    double round = steps / split * step, us = cg == 1 ? 3.6 + 0.004 * nt : 4.6, out = 0.6 + 0.011 * nt;
-    if (cg == 2 && nt > 160) {                    // one accumulator: a tile's MMAs wait for the one before to be read
+    double round = steps / split * step, us = cg == 1 ? 3.6 + 0.004 * nt : 4.6, out = 0.6 + (nt > 160 ? 0.009 : 0.011) * nt;
+    if (cg == 2 && Columns((int)nt).acc_bufs == 1) {   // a tile's MMAs wait for the one before to be read
       round += 0.8 + 0.002 * nt;
-      out = 0.6 + 0.009 * nt;
       us += round < out ? out : round;
     } else {
-      us += round + (cg == 2 ? 1.0 + 0.003 * nt : 0.0);
+      us += round + (cg == 1 ? 0.0 : nt > 160 ? 0.8 + 0.002 * nt : 1.0 + 0.003 * nt);
     }
     us += (rounds - 1) * (round < out ? out : round) + (split > 1 ? 1.2 + 0.02 * nt : 0.0);
     if (us < least) {
