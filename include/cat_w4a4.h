@@ -527,7 +527,7 @@ cat_status cat_mx_dequantize(const uint8_t* xq, const uint8_t* xs, int64_t n, in
                              cat_stream_t stream);
 
 /* cat_mx_swiglu_quantize -- gu device [n][2d] in `dtype`, a row the gate g and then u: the 4-bit form of
- * silu(g) u = (g / (1 + exp(-g))) u, computed in float32 to within (4 + 1.2 |g|) 2^-23 of it (silu(g) of a subnormal
+ * silu(g) u = (g / (1 + exp(-g))) u, computed in float32 to within (5 + |g|) 2^-23 of it (silu(g) of a subnormal
  * g to float32's spacing there; 0 where exp(-g) overflows, g < -88.72) and rounded once.  For a down projection's input. */
 cat_status cat_mx_swiglu_quantize(const void* gu, cat_dtype dtype, int64_t n, int64_t d, uint8_t* xq, uint8_t* xs,
                                   cat_stream_t stream);

@@ -3,7 +3,8 @@
 A thin ctypes binding of the C ABI in ``include/cat_w4a4.h``: every function below has the name
 of the C entry point it calls, takes torch tensors, allocates outputs with torch on the tensors'
 device when none are given, passes raw pointers and the current CUDA stream, and raises
-``CatError`` on a non-zero status.  Tensors have to be on the current device (ValueError).  All arithmetic runs in the library's CUDA kernels (or, for
+``CatError`` on a non-zero status.  Tensors have to be on the current device (``ValueError``
+otherwise).  All arithmetic runs in the library's CUDA kernels (or, for
 ``cat_build_transform_host``, in its host code); there is no fallback path.
 """
 from __future__ import annotations

@@ -1,6 +1,6 @@
 // The Python calls of the microscaled 4-bit operators, without the interpreter's part of them: checks of the tensors,
 // outputs from torch's allocator, the current stream and the C entry point.  A decode call's kernels take a few
-// microseconds, so the host's time counts: a product took 10.8 us through ctypes and torch's Python, 3.8 here.
+// microseconds, so the host's time counts: a product took 10.8 us through ctypes and torch's Python, 3.7 here.
 //
 // A function takes what the Python function of the same operator takes, outputs excepted, and returns its result, or the
 // status of a call that the library refused, or None where the arguments are not the ordinary ones (other types, shapes,

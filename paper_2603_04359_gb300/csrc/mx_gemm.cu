@@ -973,10 +973,11 @@ struct Form {
   int cg, nt, split;
 };
 
-// The form of least estimated time.  A round of tiles costs its K steps, about 0.28 us each (the issuing warps' instructions)
-// and a little for its tokens, whatever is between 8 and 256 of them; so as few rounds as can be, and in them the narrowest tiles.  With
-// many CTAs a step takes what its bytes do: the weights from memory (6 TB/s), all operands from L2 (16 TB/s); and a round
-// never takes less than its outputs' way out.  The constants (us) are fitted to bf16 outputs of 1 to 512 tokens on
+// The form of least estimated time.  A round of tiles costs its K steps and a little for its tokens, whatever is between 8 and 256
+// of them; so as few rounds as can be, and in them the narrowest tiles.  A step is 0.28 us where the issuing warps' instructions
+// bound it (as fitted; since they look ahead, pairs take 0.24 and single CTAs 0.245: alike, so the constants stand); with
+// many CTAs it takes what its bytes do: the weights from memory (6 TB/s), all operands from L2 (16 TB/s: 201 x 4096 -> 6144, whose
+// weights three token tiles read, 0.23 us); and a round never takes less than its outputs' way out.  The constants (us) are fitted to bf16 outputs of 1 to 512 tokens on
 // 4096 -> 6144, 4096 -> 14336, 14336 -> 4096, 4096 -> 4096, 1024 -> 1024 and 2048 -> 640, and of 521 to 8192 on K of 256 to
 // 7040.  Of 90 other calls of 1 to 8192 tokens, 256 to 14336 -> 64 to 28672, the form taken is on average 1 % slower than the
 // best of 3 to 25 tried, at most 12 %.  One token, 4096 -> 6144: K in two 7.0 us, whole 7.9; 128 tokens, 14336 -> 4096: K in
@@ -1032,7 +1033,9 @@ cudaError_t launch_typed(const Call& c) {
   const int64_t rows = (c.m + groups - 1) / groups;                             // of each, on average
   Form f = pick_form(groups, rows, c.d, c.d_out);
   if (c.offsets) {
-    // the host knows no group's rows: tiles have room for four times the average (each takes what its group needs)
+    // the host knows no group's rows: tiles have room for four times the average (each takes what its group needs).  Of twelve
+    // calls of 4 to 64 experts, twice the average took 2.6 % longer (128 tokens to 4 of 64, a group of 122, 17.5 us against 15.3),
+    // eight times as long (1258 rows of 53, 28.5 against 30.3; 8192 of 8, 175 against 172)
     const int64_t room = up(c.m < 4 * rows ? c.m : 4 * rows, 8 * f.cg), widest = 128 * f.cg;
     f.nt = (int)(room < widest ? room : widest);
   }
