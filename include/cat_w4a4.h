@@ -17,6 +17,8 @@
  *    acting on channels b*k .. b*k+k-1, stored row-major ([d_in/k][k][k] float32).
  *  - Unless a parameter says "host", pointers are device pointers owned by the caller; the
  *    library never frees them.  Device pointers must be 16-byte aligned.
+ *  - A call works on the device that is current in the calling thread, whose pointers and stream it has to be
+ *    given; it may be the thread's first CUDA work.
  *  - Calls are asynchronous on `stream` (NULL = the legacy default stream) unless stated.
  *    Launch failures return CAT_ERR_CUDA.  Conditions detected on the device (a bounded wait
  *    that gave up, a non-finite input) are recorded in a device status word that

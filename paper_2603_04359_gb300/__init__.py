@@ -695,7 +695,7 @@ def cat_mx_quantize(x: torch.Tensor, rows: Optional[torch.Tensor] = None, xq: Op
     dev = x.device
     m = n
     if rows is not None:
-        m = rows.numel()
+        m = rows.numel() if isinstance(rows, torch.Tensor) else 0
         _expect(rows, "rows", torch.int32, (m,), dev)
     xq, xs = _mx_out(xq, xs, m, d, dev)
     _check("cat_mx_quantize", load_library().cat_mx_quantize(_ptr(x), _dtype(x), n, d, _ptr(rows), m, _ptr(xq), _ptr(xs),
