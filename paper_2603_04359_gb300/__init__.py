@@ -134,18 +134,19 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(device: torch.device) -> int:
     """The current stream of the tensors' device, which has to be the current one: the library launches, and keeps its
     status word, on the current device."""
-    current = torch._C._cuda_getDevice()
-    if device.index is not None and device.index != current:
-        raise ValueError(f"the tensors are on {device}, but the current device is cuda:{current}: make theirs current "
-                         f"(torch.cuda.device) for the call")
-    if _raw_stream is None or device.index is None:
+    index = device.index
+    if index is None:
         return torch.cuda.current_stream(device).cuda_stream
-    return _raw_stream(device.index)
+    if index != _raw_device():
+        raise ValueError(f"the tensors are on {device}, but the current device is cuda:{_raw_device()}: make theirs current "
+                         f"(torch.cuda.device) for the call")
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _dtype(t: torch.Tensor) -> int:

@@ -13,7 +13,7 @@ PRELUDE = """
 import ctypes, torch
 import paper_2603_04359_gb300 as cat
 
-torch._C._cuda_getDevice = lambda: 0          # (torch's own wants a driver first)
+cat._raw_device = lambda: 0                   # (torch's own wants a driver first)
 kept = []
 
 def on(device, dtype, *shape, stride=None):

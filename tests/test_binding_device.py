@@ -56,7 +56,7 @@ def test_compiled_calls_leave_them_to_the_binding(outcomes):
 
 
 def test_stream_of_the_current_device(monkeypatch):
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 3)
+    monkeypatch.setattr(cat, "_raw_device", lambda: 3)
     monkeypatch.setattr(cat, "_raw_stream", lambda index: 100 + index)
     assert cat._stream(torch.device("cuda", 3)) == 103
     with pytest.raises(ValueError, match="cuda:0.*current device is cuda:3"):
