@@ -1,4 +1,4 @@
-"""The products' checker itself: an output that lacks one step of K, one part of a split or one block is refused."""
+"""The products' exact comparison itself: an output that lacks one step of K, one part of a split or one block is refused."""
 import numpy as np
 import pytest
 import torch
@@ -9,7 +9,7 @@ import mx_reference as R
 
 @pytest.mark.parametrize("n,d,d_out", [(40, 131072, 64), (16, 65536, 64), (27, 14336, 64), (3, 512, 40)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_checker_refuses_what_is_lost(n, d, d_out, dtype):
+def test_what_is_lost_is_refused(n, d, d_out, dtype):
     rng = np.random.default_rng(d)
     xq, xs = M.operand(rng, n, d, M.binades(d))
     wq, ws = M.operand(rng, d_out, d, M.binades(d))
@@ -25,7 +25,7 @@ def test_checker_refuses_what_is_lost(n, d, d_out, dtype):
         M.check(one.float().to(dtype), want)
 
 
-def test_checker_wants_exact_sums():
+def test_sums_have_to_be_exact():
     rng = np.random.default_rng(0)
     xq, xs = M.operand(rng, 4, 4096, 9)
     with pytest.raises(AssertionError, match="other operands"):
