@@ -570,6 +570,87 @@ cat_status cat_mx_linear_grouped(const uint8_t* xq, const uint8_t* xs, const uin
                                  cat_dtype out_dtype, void* y, cat_stream_t stream);
 
 /*
+ * The paged key/value cache in the microscaled 4-bit form, and the attention that reads it: what lies between a block's
+ * fused projection (cat_mx_linear) and its output projection.
+ *
+ * A cache is uint8 [pages][2][hkv][page * (d/2 + d/32)]: keys (0) and values (1) of `page` tokens of each of hkv heads of
+ * d channels, d one of 64, 128, 256, page a power of two from 16 to 1024.  A head's part of a page is its tokens' codes
+ * (d/2 bytes each), then their scales (d/32 bytes each; quantization as above, a block 32 channels).  A token's codes are
+ * the bytes of the form above in another order: its blocks' 16 bytes are cut into pieces, 4 bytes of keys and 2 of values,
+ * and the first pieces of all blocks come first (block after block), then all second pieces, and so on: a lane of a matrix
+ * instruction finds what it needs of all blocks side by side.
+ * A row of a cache is numbered page * (its page) + (its place there); pages * page is at most 2^31 - 512.
+ */
+
+/* cat_mx_cache_page_bytes -- page * (d/2 + d/32), the bytes of a head's keys (or values) of a page; 0 for sizes that a
+ * cache cannot have. */
+int64_t cat_mx_cache_page_bytes(int64_t page, int64_t d);
+
+/*
+ * cat_mx_cache_write -- keys and values k, v device [n][hkv][d] in `dtype` to rows slots[0 .. n-1] (device int32) of the
+ * cache.  A token whose slot is outside the cache (a padded batch's -1) is not written.  Slots are to be distinct: of a
+ * row named twice, some bytes may be one token's and some the other's.  Non-finite values as in cat_mx_quantize.
+ */
+cat_status cat_mx_cache_write(const void* k, const void* v, cat_dtype dtype, int64_t n, const int32_t* slots,
+                              uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d, cat_stream_t stream);
+
+/* cat_mx_cache_read -- the values that rows slots[0 .. m-1] stand for, k and v device [m][hkv][d] in `out_dtype`, exact in
+ * both (NaN under a NaN scale); zeros for a slot outside the cache. */
+cat_status cat_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d, const int32_t* slots,
+                             int64_t m, cat_dtype out_dtype, void* k, void* v, cat_stream_t stream);
+
+/*
+ * cat_mx_rope_cache_write -- what a fused projection's output goes through on its way to attention, in one pass: per head of
+ * queries and keys a root-mean-square norm and the rotation by the token's position, then queries to q_out and keys and
+ * values to the cache.
+ *   qkv        device [n][(hq + 2 hkv) d] in `dtype`: query heads, then key heads, then value heads.
+ *   q_weight, k_weight  device [d] in `weight_dtype`, each may be NULL (no norm of those heads):
+ *              x / sqrt(mean_i x_i^2 + eps) * weight; eps >= 0 and finite.
+ *   cos, sin   device [table_rows][rot/2] float32, rot a multiple of 16 up to d: of channels 0 .. rot-1, pair i is turned,
+ *              (a, b) -> (a cos_i - b sin_i, b cos_i + a sin_i).  Pairs are channels (i, i + rot/2), or (2i, 2i + 1) if
+ *              `interleaved`.  Channels from rot on stay.
+ *   positions  device [n] int32, rows of cos and sin; outside [0, table_rows) a token's queries and keys become NaN (and the
+ *              non-finite bit of the status word is raised).
+ *   slots, cache  as in cat_mx_cache_write.
+ *   q_out      device [n][hq][d] bfloat16, computed in float32 (float64 where that could change a key's code) and rounded once.
+ * Keys are quantized as if computed exactly: where float32's error could change a code or a scale they are computed in
+ * float64, so a cache does not depend on how its tokens came to it.
+ */
+cat_status cat_mx_rope_cache_write(const void* qkv, cat_dtype dtype, int64_t n, int64_t hq, const void* q_weight,
+                                   const void* k_weight, cat_dtype weight_dtype, double eps, const int32_t* positions,
+                                   const float* cos, const float* sin, int64_t table_rows, int64_t rot, int interleaved,
+                                   const int32_t* slots, uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d,
+                                   void* q_out, cat_stream_t stream);
+
+/* cat_mx_attention_workspace -- bytes of the workspace of cat_mx_attention for n query rows of seqs sequences on the current
+ * device (0: none; -1: the device cannot be asked). */
+int64_t cat_mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv, int64_t d);
+
+/*
+ * cat_mx_attention -- causal attention of a ragged batch over its sequences' pages of a cache.
+ *   q        device [n][hq][d] bfloat16; hq a multiple of hkv, query head h reads head h / (hq / hkv) of the cache.
+ *   offsets  device [seqs + 1] int32: rows offsets[s] .. offsets[s+1]-1 of q are the last tokens of sequence s, in order;
+ *            NULL: one row a sequence (n == seqs).  Taken as the nearest that are within [0, n]; sequences may be empty.  Rows of
+ *            no sequence (before offsets[0], from offsets[seqs] on) are set to zero.
+ *   lens     device [seqs] int32: tokens of each sequence in the cache, those of the rows included.
+ *   table    device [seqs][width] int32: a sequence's pages, token t in page table[s][t / page].  Entries behind a sequence's
+ *            length are not read; a token on no page (an entry outside [0, pages), t >= width * page) is not attended.
+ *   window   0, or the number of tokens a row sees: itself and the window - 1 before it.
+ * Row j of a sequence with r rows and length L is token p = L - r + j and sees tokens max(0, p - window + 1) .. p:
+ *   out = sum_t softmax_t(scale q k_t) v_t, zero for a row that sees nothing (p < 0, a length of zero).
+ * Scores and sums in float32; a score's operands are exact (but for channels 2^-24 below a row's largest), weights are rounded
+ * to 11 bits (relative to the row's largest weight no smaller than 2^-24).  A NaN key or value of a token that a row does not see leaves it as it is.
+ *   out      device [n][hq][d] in `out_dtype`, rounded once.
+ *   workspace device, at least cat_mx_attention_workspace bytes, written and read by this call alone: calls that may run at the
+ *            same time need one each.  Its contents need not be kept or set.
+ * Nothing is read back to the host: lengths may change from one replay of a captured graph to the next.
+ */
+cat_status cat_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,
+                            int64_t d, const int32_t* table, int64_t width, const int32_t* lens, int64_t seqs,
+                            const int32_t* offsets, float scale, int64_t window, cat_dtype out_dtype, void* out, void* workspace,
+                            int64_t workspace_bytes, cat_stream_t stream);
+
+/*
  * cat_device_status -- synchronizes `stream`, then reads and clears the device status word.
  * Returns CAT_OK, CAT_ERR_TIMEOUT (a bounded wait in a kernel gave up and the kernel returned
  * early; its outputs are undefined) or CAT_ERR_NUMERIC (a kernel met a non-finite value; the

@@ -27,6 +27,8 @@ __all__ = [
     "cat_split_transform", "cat_split_transform_bytes", "cat_transform_quantize_act_split",
     "cat_mx_scale_pitch", "cat_mx_quantize", "cat_mx_dequantize", "cat_mx_swiglu_quantize", "cat_mx_rmsnorm_quantize",
     "cat_mx_linear", "cat_mx_linear_grouped",
+    "cat_mx_cache_page_bytes", "cat_mx_cache", "cat_mx_cache_write", "cat_mx_cache_read", "cat_mx_rope_cache_write",
+    "cat_mx_attention_workspace", "cat_mx_attention",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -100,6 +102,12 @@ def load_library() -> ctypes.CDLL:
         "cat_mx_rmsnorm_quantize": ([P, P, I, P, I, I64, I64, ctypes.c_float, P, P, P, P], I),
         "cat_mx_linear": ([P, P, P, P, I64, I64, I64, I, P, P], I),
         "cat_mx_linear_grouped": ([P, P, P, P, P, I64, I64, I64, I64, I, P, P], I),
+        "cat_mx_cache_page_bytes": ([I64, I64], I64),
+        "cat_mx_cache_write": ([P, P, I, I64, P, P, I64, I64, I64, I64, P], I),
+        "cat_mx_cache_read": ([P, I64, I64, I64, I64, P, I64, I, P, P, P], I),
+        "cat_mx_rope_cache_write": ([P, I, I64, I64, P, P, I, ctypes.c_double, P, P, P, I64, I64, I, P, P, I64, I64, I64, I64, P, P], I),
+        "cat_mx_attention_workspace": ([I64, I64, I64, I64, I64], I64),
+        "cat_mx_attention": ([P, I64, I64, P, I64, I64, I64, I64, P, I64, P, I64, P, ctypes.c_float, I64, I, P, P, I64, P], I),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -807,6 +815,174 @@ def cat_mx_linear_grouped(xq: torch.Tensor, xs: torch.Tensor, Wq: torch.Tensor, 
     _check("cat_mx_linear_grouped", load_library().cat_mx_linear_grouped(
         _ptr(xq), _ptr(xs), _ptr(Wq), _ptr(ws), _ptr(offsets), experts, m, 2 * half, d_out, _dtype(y), _ptr(y), _stream(dev)))
     return y
+
+
+# ---- the paged key/value cache in that form, and attention over it: uint8 [pages, 2, hkv, cat_mx_cache_page_bytes(page, d)]
+
+def cat_mx_cache_page_bytes(page: int, d: int) -> int:
+    """Bytes of the keys (or the values) of ``page`` tokens of a head of d channels: page * (d / 2 + d / 32); 0 for sizes that a
+    cache cannot have (d one of 64, 128, 256; page a power of two from 16 to 1024)."""
+    ok = d in (64, 128, 256) and 16 <= page <= 1024 and page & (page - 1) == 0
+    return page * (d // 2 + d // 32) if ok else 0
+
+
+def cat_mx_cache(pages: int, hkv: int, page: int, d: int, device=None) -> torch.Tensor:
+    """A cache of zeros."""
+    if cat_mx_cache_page_bytes(page, d) == 0:
+        raise ValueError(f"no cache has pages of {page} tokens and heads of {d} channels")
+    return torch.zeros((pages, 2, hkv, cat_mx_cache_page_bytes(page, d)), dtype=torch.uint8, device=device or torch.device("cuda"))
+
+
+def _mx_cache_sizes(cache: torch.Tensor, d: int) -> Tuple[int, int, int]:
+    """(pages, tokens a page, heads) of a cache of heads of d channels."""
+    if not isinstance(cache, torch.Tensor) or cache.dim() != 4 or cache.shape[1] != 2:
+        raise ValueError("cache must be a tensor [pages, 2, hkv, bytes of a page]")
+    if d not in (64, 128, 256):
+        raise ValueError(f"a head has 64, 128 or 256 channels, not {d}")
+    pages, _, hkv, part = cache.shape
+    page = part // (d // 2 + d // 32)
+    if cat_mx_cache_page_bytes(page, d) != part:
+        raise ValueError(f"cache has {part} bytes of a head a page: not those of 16 to 1024 (a power of two) tokens of {d} channels")
+    _expect(cache, "cache", torch.uint8, (pages, 2, hkv, part), cache.device)
+    return pages, page, hkv
+
+
+def _numbers(t: torch.Tensor, name: str, dev: torch.device) -> int:
+    """Checks an int32 tensor of one dimension; its length."""
+    m = t.numel() if isinstance(t, torch.Tensor) else 0
+    _expect(t, name, torch.int32, (m,), dev)
+    return m
+
+
+def cat_mx_cache_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor) -> torch.Tensor:
+    """Keys and values k, v [n, hkv, d] to rows ``slots`` (int32 [n]; page * its page + the place there; distinct, and those
+    outside the cache are left out) of ``cache``, which is returned."""
+    r = (_mx_native or _calls()).cache_write(k, v, slots, cache)
+    if r == 0:
+        return cache
+    if r is not None:
+        _check("cat_mx_cache_write", r)
+    _need(k, "k")
+    n, hkv, d = k.shape
+    dev = k.device
+    _expect(v, "v", k.dtype, (n, hkv, d), dev)
+    _expect(slots, "slots", torch.int32, (n,), dev)
+    pages, page, heads = _mx_cache_sizes(cache, d)
+    _expect(cache, "cache", torch.uint8, (pages, 2, hkv, cache.shape[3]), dev)
+    _check("cat_mx_cache_write", load_library().cat_mx_cache_write(_ptr(k), _ptr(v), _dtype(k), n, _ptr(slots), _ptr(cache), pages,
+                                                                   page, hkv, d, _stream(dev)))
+    return cache
+
+
+def cat_mx_cache_read(cache: torch.Tensor, slots: torch.Tensor, d: int, out_dtype: Optional[torch.dtype] = None,
+                      k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The keys and values [m, hkv, d] that rows ``slots`` (int32 [m]) of a cache stand for: float32 (default) or bfloat16, exact
+    in both; zeros for slots outside the cache."""
+    if k is None and v is None:
+        r = (_mx_native or _calls()).cache_read(cache, slots, d, out_dtype)
+        if type(r) is tuple:
+            return r
+        if r is not None:
+            _check("cat_mx_cache_read", r)
+    pages, page, hkv = _mx_cache_sizes(cache, d)
+    dev = cache.device
+    m = _numbers(slots, "slots", dev)
+    out_dtype = out_dtype or (k.dtype if k is not None else v.dtype if v is not None else None)
+    k = _mx_result(k, "k", out_dtype, (m, hkv, d), dev)
+    v = _mx_result(v, "v", k.dtype, (m, hkv, d), dev)
+    _check("cat_mx_cache_read", load_library().cat_mx_cache_read(_ptr(cache), pages, page, hkv, d, _ptr(slots), m, _dtype(k), _ptr(k),
+                                                                 _ptr(v), _stream(dev)))
+    return k, v
+
+
+def cat_mx_rope_cache_write(qkv: torch.Tensor, d: int, positions: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor,
+                            slots: torch.Tensor, cache: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+                            k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                            q: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A fused projection's output qkv [n, (hq + 2 hkv) d] through the norms of its query and key heads (``q_weight``,
+    ``k_weight`` [d]; none: no norm) and the rotation by ``positions`` (int32 [n], rows of the float32 tables cos and sin
+    [rows, rot / 2]; channels from rot on are not turned): keys and values to rows ``slots`` of the cache, queries
+    [n, hq, d] in bfloat16 returned.  Pairs are channels (i, i + rot / 2), or neighbours if ``interleaved``."""
+    if q is None:
+        r = (_mx_native or _calls()).rope_cache_write(qkv, d, positions, cos, sin, slots, cache, q_weight, k_weight, eps, interleaved)
+        if isinstance(r, torch.Tensor):
+            return r
+        if r is not None:
+            _check("cat_mx_rope_cache_write", r)
+    _need(qkv, "qkv")
+    n, row = qkv.shape
+    dev = qkv.device
+    pages, page, hkv = _mx_cache_sizes(cache, d)
+    if row % d or row // d <= 2 * hkv:
+        raise ValueError(f"qkv has {row} columns: not heads of {d} of which 2 x {hkv} are keys and values")
+    hq = row // d - 2 * hkv
+    _expect(cache, "cache", torch.uint8, tuple(cache.shape), dev)
+    _expect(positions, "positions", torch.int32, (n,), dev)
+    _expect(slots, "slots", torch.int32, (n,), dev)
+    _need(cos, "cos")
+    if cos.dim() != 2:
+        raise ValueError("cos must be [rows, rot / 2]")
+    _expect(cos, "cos", torch.float32, tuple(cos.shape), dev)
+    _expect(sin, "sin", torch.float32, tuple(cos.shape), dev)
+    weight = q_weight if q_weight is not None else k_weight
+    if weight is not None:
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None:
+                _expect(w, name, weight.dtype, (d,), dev)
+    q = _given(q, "q", torch.bfloat16, (n, hq, d), dev)
+    _check("cat_mx_rope_cache_write", load_library().cat_mx_rope_cache_write(
+        _ptr(qkv), _dtype(qkv), n, hq, _ptr(q_weight), _ptr(k_weight), 0 if weight is None else _dtype(weight), eps, _ptr(positions),
+        _ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)), _ptr(slots), _ptr(cache), pages, page, hkv, d,
+        _ptr(q), _stream(dev)))
+    return q
+
+
+def cat_mx_attention_workspace(n: int, seqs: int, hq: int, hkv: int, d: int) -> int:
+    """Bytes that cat_mx_attention needs beside its tensors, on the current device."""
+    return int(load_library().cat_mx_attention_workspace(n, seqs, hq, hkv, d))
+
+
+def cat_mx_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, scale: float,
+                     offsets: Optional[torch.Tensor] = None, window: int = 0, out_dtype: Optional[torch.dtype] = None,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention of the last tokens of each sequence, q [n, hq, d] bfloat16, over their pages of a cache: [n, hq, d],
+    bfloat16 (default) or float32.  ``table`` int32 [seqs, width]: a sequence's pages; ``lens`` int32 [seqs]: its tokens in the
+    cache, its rows of q included; ``offsets`` int32 [seqs + 1]: its rows of q (none: one each); ``window``: tokens a row sees
+    (0: all).  Rows of no sequence, and rows that see no token, are zero.  ``workspace`` (uint8, by default allocated) is one
+    call's own."""
+    if out is None and workspace is None:
+        r = (_mx_native or _calls()).attention(q, cache, table, lens, scale, offsets, window, out_dtype)
+        if isinstance(r, torch.Tensor):
+            return r
+        if r is not None:
+            _check("cat_mx_attention", r)
+    _need(q, "q")
+    n, hq, d = q.shape
+    dev = q.device
+    _expect(q, "q", torch.bfloat16, (n, hq, d), dev)
+    pages, page, hkv = _mx_cache_sizes(cache, d)
+    _expect(cache, "cache", torch.uint8, tuple(cache.shape), dev)
+    _need(table, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be [seqs, width]")
+    seqs, width = table.shape
+    _expect(table, "table", torch.int32, (seqs, width), dev)
+    _expect(lens, "lens", torch.int32, (seqs,), dev)
+    if offsets is not None:
+        _expect(offsets, "offsets", torch.int32, (seqs + 1,), dev)
+    if out is None:
+        out = torch.empty((n, hq, d), dtype=out_dtype or torch.bfloat16, device=dev)
+    else:
+        _expect(out, "out", out_dtype or out.dtype, (n, hq, d), dev)
+    kind, stream = _dtype(out), _stream(dev)
+    need = max(cat_mx_attention_workspace(n, seqs, hq, hkv, d), 0)
+    if workspace is None:
+        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+    _expect(workspace, "workspace", torch.uint8, (workspace.numel(),), dev)
+    _check("cat_mx_attention", load_library().cat_mx_attention(
+        _ptr(q), n, hq, _ptr(cache), pages, page, hkv, d, _ptr(table), width, _ptr(lens), seqs, _ptr(offsets), scale, window,
+        kind, _ptr(out), _ptr(workspace), workspace.numel(), stream))
+    return out
 
 
 def cat_set_wait_limit_ns(ns: int) -> None:

@@ -9,7 +9,7 @@
 
 #include "../../include/cat_w4a4.h"
 #include "common.cuh"
-#include "mx_format.cuh"
+#include "mx_cache.cuh"
 #include "transform_host.h"
 
 namespace cat {
@@ -61,6 +61,19 @@ cudaError_t launch_mx_rmsnorm_quantize(const void* x, const void* residual, cons
 cudaError_t launch_mx_gemm(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws,
                            const int32_t* offsets, int64_t experts, int64_t m, int64_t d, int64_t d_out, int out_dtype,
                            void* y, uint32_t* status, cudaStream_t stream);
+cudaError_t launch_mx_cache_write(const void* k, const void* v, int dtype, int64_t n, const int32_t* slots, uint8_t* cache,
+                                  int64_t pages, int64_t page, int64_t hkv, int64_t d, uint32_t* status, cudaStream_t stream);
+cudaError_t launch_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d, const int32_t* slots,
+                                 int64_t m, int dtype, void* k, void* v, cudaStream_t stream);
+cudaError_t launch_mx_rope(const void* qkv, int dtype, int64_t n, int64_t hq, const void* q_weight, const void* k_weight,
+                           int weight_dtype, double eps, const int32_t* positions, const float* cos, const float* sin,
+                           int64_t table_rows, int64_t rot, int interleaved, const int32_t* slots, uint8_t* cache, int64_t pages,
+                           int64_t page, int64_t hkv, int64_t d, void* q_out, uint32_t* status, cudaStream_t stream);
+int64_t mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv, int64_t d);
+cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,
+                                int64_t d, const int32_t* table, int64_t width, const int32_t* lens, int64_t seqs,
+                                const int32_t* offsets, float scale, int64_t window, int out_dtype, void* out, void* workspace,
+                                cudaStream_t stream);
 }  // namespace cat
 
 namespace {
@@ -1062,5 +1075,114 @@ cat_status cat_mx_linear_grouped(const uint8_t* xq, const uint8_t* xs, const uin
   return mx_launch("cat_mx_linear_grouped launch", [&](uint32_t* status) {
     return cat::launch_mx_gemm(xq, xs, Wq, ws, offsets, experts, m, d, d_out, (int)out_dtype, y, status,
                                (cudaStream_t)stream);
+  });
+}
+
+// ---- the 4-bit key/value cache
+
+static constexpr int64_t kMaxHeads = 65536;      // query and key heads of a call
+
+static cat_status check_cache(int64_t pages, int64_t page, int64_t hkv, int64_t d) {
+  if (d != 64 && d != 128 && d != 256) return fail(CAT_ERR_SHAPE, "a head has 64, 128 or 256 channels");
+  if (page < 16 || page > 1024 || (page & (page - 1)) != 0) return fail(CAT_ERR_SHAPE, "page must be a power of two from 16 to 1024");
+  if (hkv < 1 || hkv > kMaxHeads) return fail(CAT_ERR_SHAPE, "hkv must be in [1, 65536]");
+  if (pages < 0 || pages > kMaxMxRows / page) return fail(CAT_ERR_SHAPE, "a cache has at most 2^31 - 512 rows");
+  return CAT_OK;
+}
+static bool rows_fit(int64_t n) { return n >= 0 && n <= kMaxMxRows; }
+
+int64_t cat_mx_cache_page_bytes(int64_t page, int64_t d) {
+  const bool ok = (d == 64 || d == 128 || d == 256) && page >= 16 && page <= 1024 && (page & (page - 1)) == 0;
+  return ok ? cat::mx_page_bytes(page, d) : 0;
+}
+
+cat_status cat_mx_cache_write(const void* k, const void* v, cat_dtype dtype, int64_t n, const int32_t* slots, uint8_t* cache,
+                              int64_t pages, int64_t page, int64_t hkv, int64_t d, cat_stream_t stream) {
+  if (!known(dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_cache(pages, page, hkv, d);
+  if (st != CAT_OK) return st;
+  if (!rows_fit(n)) return fail(CAT_ERR_SHAPE, "n must be in [0, 2^31 - 512]");
+  if (n == 0) return ok();
+  if (!k || !v || !slots || (pages > 0 && !cache)) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(slots) || !aligned16(cache))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_cache_write launch", [&](uint32_t* status) {
+    return cat::launch_mx_cache_write(k, v, (int)dtype, n, slots, cache, pages, page, hkv, d, status, (cudaStream_t)stream);
+  });
+}
+
+cat_status cat_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d, const int32_t* slots,
+                             int64_t m, cat_dtype out_dtype, void* k, void* v, cat_stream_t stream) {
+  if (!known(out_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_cache(pages, page, hkv, d);
+  if (st != CAT_OK) return st;
+  if (!rows_fit(m)) return fail(CAT_ERR_SHAPE, "m must be in [0, 2^31 - 512]");
+  if (m == 0) return ok();
+  if (!k || !v || !slots || (pages > 0 && !cache)) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(slots) || !aligned16(cache))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_cache_read launch", [&](uint32_t*) {
+    return cat::launch_mx_cache_read(cache, pages, page, hkv, d, slots, m, (int)out_dtype, k, v, (cudaStream_t)stream);
+  });
+}
+
+cat_status cat_mx_rope_cache_write(const void* qkv, cat_dtype dtype, int64_t n, int64_t hq, const void* q_weight,
+                                   const void* k_weight, cat_dtype weight_dtype, double eps, const int32_t* positions,
+                                   const float* cos, const float* sin, int64_t table_rows, int64_t rot, int interleaved,
+                                   const int32_t* slots, uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d,
+                                   void* q_out, cat_stream_t stream) {
+  if (!known(dtype) || !known(weight_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  if (!(eps >= 0.0) || eps > 3e38) return fail(CAT_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+  if (interleaved != 0 && interleaved != 1) return fail(CAT_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  cat_status st = check_cache(pages, page, hkv, d);
+  if (st != CAT_OK) return st;
+  if (hq < 1 || hq > kMaxHeads) return fail(CAT_ERR_SHAPE, "hq must be in [1, 65536]");
+  if (rot < 16 || rot > d || rot % 16 != 0) return fail(CAT_ERR_SHAPE, "rot must be a multiple of 16 from 16 to d");
+  if (table_rows < 0 || !rows_fit(table_rows)) return fail(CAT_ERR_SHAPE, "table_rows must be in [0, 2^31 - 512]");
+  if (!rows_fit(n) || n > kMaxMxRows / ((hq + 2 * hkv + 7) / 8)) return fail(CAT_ERR_SHAPE, "too many tokens");
+  if (n == 0) return ok();
+  if (!qkv || !positions || (table_rows > 0 && (!cos || !sin)) || !slots || (pages > 0 && !cache) || !q_out)
+    return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(qkv) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(positions) || !aligned16(cos) ||
+      !aligned16(sin) || !aligned16(slots) || !aligned16(cache) || !aligned16(q_out))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  return mx_launch("cat_mx_rope_cache_write launch", [&](uint32_t* status) {
+    return cat::launch_mx_rope(qkv, (int)dtype, n, hq, q_weight, k_weight, (int)weight_dtype, eps, positions, cos, sin, table_rows,
+                               rot, interleaved, slots, cache, pages, page, hkv, d, q_out, status, (cudaStream_t)stream);
+  });
+}
+
+int64_t cat_mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv, int64_t d) {
+  if (n <= 0 || seqs <= 0 || hkv < 1 || hq < hkv || hq > kMaxHeads || hq % hkv != 0 || (d != 64 && d != 128 && d != 256)) return 0;
+  return cat::mx_attention_workspace(n, seqs, hq, hkv, d);
+}
+
+cat_status cat_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,
+                            int64_t d, const int32_t* table, int64_t width, const int32_t* lens, int64_t seqs,
+                            const int32_t* offsets, float scale, int64_t window, cat_dtype out_dtype, void* out, void* workspace,
+                            int64_t workspace_bytes, cat_stream_t stream) {
+  if (!known(out_dtype)) return fail(CAT_ERR_INVALID_ARG, "unknown dtype");
+  cat_status st = check_cache(pages, page, hkv, d);
+  if (st != CAT_OK) return st;
+  if (hq < hkv || hq > kMaxHeads || hq % hkv != 0) return fail(CAT_ERR_SHAPE, "hq must be a multiple of hkv, at most 65536");
+  if (!std::isfinite(scale)) return fail(CAT_ERR_INVALID_ARG, "scale must be finite");
+  if (window < 0 || window > kMaxMxRows) return fail(CAT_ERR_SHAPE, "window must be in [0, 2^31 - 512]");
+  if (seqs < 0 || seqs > 65536) return fail(CAT_ERR_SHAPE, "seqs must be in [0, 65536]");
+  if (width < 0 || width > kMaxMxRows / page) return fail(CAT_ERR_SHAPE, "a sequence has at most 2^31 - 512 tokens");
+  if (!rows_fit(n) || n > kMaxMxRows / hq) return fail(CAT_ERR_SHAPE, "too many query rows (n * hq is at most 2^31 - 512)");
+  if (!offsets && n != seqs) return fail(CAT_ERR_SHAPE, "without offsets, n must be seqs");
+  if (n == 0) return ok();
+  if (!q || (pages > 0 && !cache) || (seqs > 0 && width > 0 && !table) || (seqs > 0 && !lens) || !out)
+    return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
+  if (!aligned16(q) || !aligned16(cache) || !aligned16(table) || !aligned16(lens) || !aligned16(offsets) || !aligned16(out) ||
+      !aligned16(workspace))
+    return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  if ((st = check_device()) != CAT_OK) return st;
+  const int64_t need = cat::mx_attention_workspace(n, seqs, hq, hkv, d);
+  if (need < 0) return fail(CAT_ERR_CUDA, "the device's size cannot be asked");
+  if (workspace_bytes < need || (need > 0 && !workspace)) return fail(CAT_ERR_SHAPE, "the workspace is too small");
+  return mx_launch("cat_mx_attention launch", [&](uint32_t*) {
+    return cat::launch_mx_attention(q, n, hq, cache, pages, page, hkv, d, table, width, lens, seqs, offsets, scale, window,
+                                    (int)out_dtype, out, workspace, (cudaStream_t)stream);
   });
 }

@@ -217,9 +217,154 @@ PyObject* linear_grouped(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// A cache [pages][2][hkv][bytes of a page] of heads of d channels.
+struct Cache {
+  const at::Tensor* t;
+  int64_t pages, page, hkv;
+  Cache(PyObject* o, int64_t d) : t(dense(o, 4)), pages(0), page(0), hkv(0) {
+    if (!t) return;
+    const int64_t part = t->size(3), token = d / 2 + d / 32;
+    if (t->scalar_type() != at::kByte || t->size(1) != 2 || token <= 0 || part % token != 0 ||
+        cat_mx_cache_page_bytes(part / token, d) != part) {
+      t = nullptr;
+      return;
+    }
+    pages = t->size(0), page = part / token, hkv = t->size(2);
+  }
+  bool on(int64_t device) const { return t && t->get_device() == device; }
+};
+// int32 [n] of a device, any n for -1
+const at::Tensor* numbers(PyObject* o, int64_t n, int64_t device) {
+  const at::Tensor* t = dense(o, 1);
+  return t && t->scalar_type() == at::kInt && (n < 0 || t->size(0) == n) && t->get_device() == device ? t : nullptr;
+}
+const int32_t* i32(const at::Tensor* t) { return t ? static_cast<const int32_t*>(t->data_ptr()) : nullptr; }
+at::Tensor make3(int64_t a, int64_t b, int64_t c, at::ScalarType type) {
+  return at::detail::empty_generic({a, b, c}, c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                   type, c10::nullopt);
+}
+
+// (k, v, slots, cache): 0 once done
+PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (!count(nargs, 4)) return nullptr;
+  const at::Tensor *k = dense(args[0], 3), *v = dense(args[1], 3);
+  if (!k || !v || !real(*k) || v->scalar_type() != k->scalar_type() || v->sizes() != k->sizes() || v->get_device() != k->get_device() ||
+      !current(*k))
+    Py_RETURN_NONE;
+  const int64_t n = k->size(0), hkv = k->size(1), d = k->size(2);
+  const at::Tensor* slots = numbers(args[2], n, k->get_device());
+  const Cache c(args[3], d);
+  if (!slots || !c.on(k->get_device()) || c.hkv != hkv) Py_RETURN_NONE;
+  const cat_status st = unlocked([&] {
+    return cat_mx_cache_write(k->data_ptr(), v->data_ptr(), code(*k), n, i32(slots), u8(*c.t), c.pages, c.page, hkv, d, stream_of(*k));
+  });
+  return PyLong_FromLong(st);
+  END_HANDLE_TH_ERRORS
+}
+
+// An integer argument; false where it is none (or too large).
+bool integer(PyObject* o, int64_t* v) {
+  if (!PyLong_Check(o)) return false;
+  int over = 0;
+  *v = PyLong_AsLongLongAndOverflow(o, &over);
+  return over == 0;
+}
+
+// (cache, slots, d, out_dtype)
+PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (!count(nargs, 4)) return nullptr;
+  int64_t d;
+  at::ScalarType type;
+  if (!integer(args[2], &d) || !out_type(args[3], &type)) Py_RETURN_NONE;
+  const Cache c(args[0], d);
+  if (!c.t || !current(*c.t)) Py_RETURN_NONE;
+  const at::Tensor* slots = numbers(args[1], -1, c.t->get_device());
+  if (!slots) Py_RETURN_NONE;
+  const int64_t m = slots->size(0);
+  at::Tensor k, v;
+  const cat_status st = unlocked([&] {
+    k = make3(m, c.hkv, d, type), v = make3(m, c.hkv, d, type);
+    return cat_mx_cache_read(u8(*c.t), c.pages, c.page, c.hkv, d, i32(slots), m, code(k), k.data_ptr(), v.data_ptr(), stream_of(*c.t));
+  });
+  return st == CAT_OK ? wrap({k, v}) : PyLong_FromLong(st);
+  END_HANDLE_TH_ERRORS
+}
+
+// (qkv, d, positions, cos, sin, slots, cache, q_weight, k_weight, eps, interleaved)
+PyObject* rope_cache_write(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (!count(nargs, 11)) return nullptr;
+  const at::Tensor* x = dense(args[0], 2);
+  int64_t d;
+  if (!x || !real(*x) || !integer(args[1], &d) || d <= 0 || !current(*x)) Py_RETURN_NONE;
+  const int64_t device = x->get_device(), n = x->size(0), heads = x->size(1) / d;
+  const Cache c(args[6], d);
+  const at::Tensor *positions = numbers(args[2], n, device), *cos = dense(args[3], 2), *sin = dense(args[4], 2),
+                   *slots = numbers(args[5], n, device);
+  if (!c.on(device) || x->size(1) % d != 0 || heads <= 2 * c.hkv || !positions || !slots || !cos || !sin ||
+      cos->scalar_type() != at::kFloat || sin->scalar_type() != at::kFloat || cos->sizes() != sin->sizes() ||
+      cos->get_device() != device || sin->get_device() != device)
+    Py_RETURN_NONE;
+  const at::Tensor* w[2] = {nullptr, nullptr};
+  for (int i = 0; i < 2; ++i)
+    if (args[7 + i] != Py_None &&
+        (!(w[i] = dense(args[7 + i], 1)) || !real(*w[i]) || w[i]->size(0) != d || w[i]->get_device() != device))
+      Py_RETURN_NONE;
+  if (w[0] && w[1] && w[0]->scalar_type() != w[1]->scalar_type()) Py_RETURN_NONE;
+  const double eps = PyFloat_AsDouble(args[9]);
+  if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+  const int interleaved = PyObject_IsTrue(args[10]);
+  if (interleaved < 0) return nullptr;
+  const at::Tensor* weight = w[0] ? w[0] : w[1];
+  const int64_t hq = heads - 2 * c.hkv;
+  at::Tensor q;
+  const cat_status st = unlocked([&] {
+    q = make3(n, hq, d, at::kBFloat16);
+    return cat_mx_rope_cache_write(x->data_ptr(), code(*x), n, hq, w[0] ? w[0]->data_ptr() : nullptr,
+                                   w[1] ? w[1]->data_ptr() : nullptr, weight ? code(*weight) : CAT_F32, eps, i32(positions),
+                                   static_cast<const float*>(cos->data_ptr()), static_cast<const float*>(sin->data_ptr()),
+                                   cos->size(0), 2 * cos->size(1), interleaved, i32(slots), u8(*c.t), c.pages, c.page, c.hkv, d,
+                                   q.data_ptr(), stream_of(*x));
+  });
+  return st == CAT_OK ? THPVariable_Wrap(q) : PyLong_FromLong(st);
+  END_HANDLE_TH_ERRORS
+}
+
+// (q, cache, table, lens, scale, offsets, window, out_dtype)
+PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (!count(nargs, 8)) return nullptr;
+  const at::Tensor *q = dense(args[0], 3), *table = dense(args[2], 2), *offsets = nullptr;
+  if (!q || q->scalar_type() != at::kBFloat16 || !table || !current(*q)) Py_RETURN_NONE;
+  const int64_t device = q->get_device(), n = q->size(0), hq = q->size(1), d = q->size(2), seqs = table->size(0);
+  const Cache c(args[1], d);
+  const at::Tensor* lens = numbers(args[3], seqs, device);
+  at::ScalarType type = at::kBFloat16;
+  int64_t window;
+  if (!c.on(device) || !lens || table->scalar_type() != at::kInt || table->get_device() != device || !integer(args[6], &window) ||
+      (args[5] != Py_None && !(offsets = numbers(args[5], seqs + 1, device))) || (args[7] != Py_None && !out_type(args[7], &type)))
+    Py_RETURN_NONE;
+  const double scale = PyFloat_AsDouble(args[4]);
+  if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+  at::Tensor out, ws;
+  const cat_status st = unlocked([&] {
+    const int64_t need = cat_mx_attention_workspace(n, seqs, hq, c.hkv, d);
+    out = make3(n, hq, d, type);
+    if (need > 0) ws = bytes(1, need);
+    return cat_mx_attention(q->data_ptr(), n, hq, u8(*c.t), c.pages, c.page, c.hkv, d, i32(table), table->size(1), i32(lens), seqs,
+                            i32(offsets), (float)scale, window, code(out), out.data_ptr(), need > 0 ? ws.data_ptr() : nullptr,
+                            need > 0 ? need : 0, stream_of(*q));
+  });
+  return st == CAT_OK ? THPVariable_Wrap(out) : PyLong_FromLong(st);
+  END_HANDLE_TH_ERRORS
+}
+
 #define CAT_CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef calls[] = {CAT_CALL(quantize), CAT_CALL(swiglu_quantize), CAT_CALL(rmsnorm_quantize), CAT_CALL(dequantize),
-                       CAT_CALL(linear), CAT_CALL(linear_grouped), {nullptr, nullptr, 0, nullptr}};
+                       CAT_CALL(linear), CAT_CALL(linear_grouped), CAT_CALL(cache_write), CAT_CALL(cache_read),
+                       CAT_CALL(rope_cache_write), CAT_CALL(attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mx_calls", nullptr, -1, calls, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
