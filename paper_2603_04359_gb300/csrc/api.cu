@@ -73,7 +73,7 @@ int64_t mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv,
 cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,
                                 int64_t d, const int32_t* table, int64_t width, const int32_t* lens, int64_t seqs,
                                 const int32_t* offsets, float scale, int64_t window, int out_dtype, void* out, void* workspace,
-                                cudaStream_t stream);
+                                uint32_t* status, cudaStream_t stream);
 }  // namespace cat
 
 namespace {
@@ -1181,8 +1181,8 @@ cat_status cat_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t*
   const int64_t need = cat::mx_attention_workspace(n, seqs, hq, hkv, d);
   if (need < 0) return fail(CAT_ERR_CUDA, "the device's size cannot be asked");
   if (workspace_bytes < need || (need > 0 && !workspace)) return fail(CAT_ERR_SHAPE, "the workspace is too small");
-  return mx_launch("cat_mx_attention launch", [&](uint32_t*) {
+  return mx_launch("cat_mx_attention launch", [&](uint32_t* status) {
     return cat::launch_mx_attention(q, n, hq, cache, pages, page, hkv, d, table, width, lens, seqs, offsets, scale, window,
-                                    (int)out_dtype, out, workspace, (cudaStream_t)stream);
+                                    (int)out_dtype, out, workspace, status, (cudaStream_t)stream);
   });
 }

@@ -21,7 +21,7 @@ inline void note_launch() { g_kernel_launches.fetch_add(1, std::memory_order_rel
 enum : uint32_t {
   kStatusTimeout = 1u,     // a bounded wait gave up
   kStatusNonFinite = 2u,   // a non-finite value reached a quantizer
-  // with kStatusTimeout: the kernel (bits 8..14) and, in bits 16..31, the source line of the first
+  // with kStatusTimeout: the kernel (bits 8..15) and, in bits 16..31, the source line of the first
   // wait that gave up
   kWhereTransform2Pass = 1u << 8,
   kWhereTransformFused = 1u << 9,
@@ -30,6 +30,7 @@ enum : uint32_t {
   kWhereCalib = 1u << 12,
   kWhereGemmDp = 1u << 13,
   kWhereMxGemm = 1u << 14,
+  kWhereMxAttention = 1u << 15,
 };
 
 // The status bits a kernel raises when a wait gave up: abort holds the line of the first one.

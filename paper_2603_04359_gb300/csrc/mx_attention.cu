@@ -17,7 +17,7 @@
 // Scores leave with lane (g, t) having tokens g, g + 8 of rows 2 t, 2 t + 1; times the values' scales of its tokens they are
 // turned to the second product's operand by movmatrix.
 //
-// Work is cut evenly, whatever the lengths: units (sequence, row tile, head) lie one behind the other on a line of 16-token steps, and
+// Work is cut evenly, whatever the lengths: units (sequence, row tile, head) lie one behind the other on a line of 32-token steps, and
 // each CTA has an equal piece of it, found from the lengths on the device.  A unit in one piece is written at once; the others'
 // parts go through the workspace, and a second kernel joins them in the order of their tokens.
 #include <cuda_fp16.h>
@@ -29,8 +29,10 @@ namespace cat {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kUnitCost = 4;                // a unit's beginning and end, in steps
-constexpr int kLeastPiece = 8;              // steps a CTA is worth
+constexpr int kStep = 32;                   // tokens a warp takes at once (two of the products' 16)
+constexpr int kUnitCost = 2;                // a unit's beginning and end, in steps
+constexpr int kAhead = kStep * kWarps;      // tokens between a warp's steps
+constexpr int kLeastPiece = 4;              // steps a CTA is worth
 constexpr float kSlack = 6.f;               // a row's scores may exceed its running maximum by this (binary orders) before it follows
 constexpr int kLowR = 40;                   // least reference exponent of the values (below it they count less bits)
 
@@ -52,10 +54,11 @@ struct AttnArgs {
   int out_f32;
   float *parts, *ml;                        // [2 grid][rows][D], [2 grid][rows][2]
   Plan* plan;
+  uint32_t* status;
 };
 
 struct Seq {
-  int begin, ql, steps, tiles;              // first row, rows, 16-token steps and row tiles
+  int begin, ql, steps, tiles;              // first row, rows, steps and row tiles
   int64_t len, first, end;                  // tokens; the first a row sees; one past the last in the cache
   __device__ __forceinline__ int64_t cost(int hkv) const { return steps ? (int64_t)tiles * hkv * (steps + kUnitCost) : 0; }
 };
@@ -76,7 +79,7 @@ __device__ __forceinline__ Seq seq_at(const AttnArgs& a, int s) {
   const int64_t cap = a.width << a.c.page_log, p = q.len - q.ql;
   q.end = q.len < cap ? q.len : cap;
   q.first = a.window && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
-  q.steps = q.ql > 0 && q.end > q.first ? (int)((q.end + 15) / 16 - q.first / 16) : 0;
+  q.steps = q.ql > 0 && q.end > q.first ? (int)((q.end + kStep - 1) / kStep - q.first / kStep) : 0;
   q.tiles = (int)(((int64_t)q.ql * a.group + ROWS - 1) / ROWS);
   return q;
 }
@@ -92,130 +95,137 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t transpose(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// The float16 values of a byte's two codes, the first in the low half (byte i of w).
+// The float16 values of the two codes in byte I of w, the first in the low half.
 template <int I>
 __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
   uint32_t r;
-  asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %1; cvt.rn.f16x2.e2m1x2 %0, a; }" : "=r"(r) : "r"(I ? w >> (8 * I) : w));
+  if constexpr (I == 0)
+    asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %1; cvt.rn.f16x2.e2m1x2 %0, a; }" : "=r"(r) : "r"(w));
+  else if constexpr (I == 1)
+    asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %1; cvt.rn.f16x2.e2m1x2 %0, b; }" : "=r"(r) : "r"(w));
+  else if constexpr (I == 2)
+    asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %1; cvt.rn.f16x2.e2m1x2 %0, c; }" : "=r"(r) : "r"(w));
+  else
+    asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %1; cvt.rn.f16x2.e2m1x2 %0, d; }" : "=r"(r) : "r"(w));
   return r;
 }
 __device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// 2^(byte - 127) of byte i of w; 0 for a byte of 0 and infinity for 255.
-template <int I>
-__device__ __forceinline__ float byte_scale(uint32_t w) {
-  return __uint_as_float((I < 3 ? w << (23 - 8 * I) : w >> 1) & 0x7F800000u);
+// Four scale bytes as the powers of two (and NaN) that they stand for.
+__device__ __forceinline__ void scales4(uint32_t w, float* s) {
+  uint32_t lo, hi;
+  asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.rn.bf16x2.ue8m0x2 %0, a; cvt.rn.bf16x2.ue8m0x2 %1, b; }" : "=r"(lo), "=r"(hi) : "r"(w));
+  s[0] = __uint_as_float(lo << 16);
+  s[1] = __uint_as_float(lo & 0xFFFF0000u);
+  s[2] = __uint_as_float(hi << 16);
+  s[3] = __uint_as_float(hi & 0xFFFF0000u);
 }
-__device__ __forceinline__ float byte_scale_at(const uint32_t* w, int b) {
-  switch (b & 3) {
-    case 0: return byte_scale<0>(w[b / 4]);
-    case 1: return byte_scale<1>(w[b / 4]);
-    case 2: return byte_scale<2>(w[b / 4]);
-    default: return byte_scale<3>(w[b / 4]);
+template <int NB>
+__device__ __forceinline__ void scales_of(const uint32_t* w, float (&s)[NB]) {
+  if constexpr (NB == 2) {
+    uint32_t lo;
+    asm("{ .reg .b16 a, b; mov.b32 {a, b}, %1; cvt.rn.bf16x2.ue8m0x2 %0, a; }" : "=r"(lo) : "r"(w[0]));
+    s[0] = __uint_as_float(lo << 16);
+    s[1] = __uint_as_float(lo & 0xFFFF0000u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NB; i += 4) scales4(w[i / 4], s + i);
   }
 }
 __device__ __forceinline__ uint32_t byte_at(const uint32_t* w, int b) { return w[b / 4] >> (8 * (b & 3)) & 0xFFu; }
 
-// The largest byte of two words.
-__device__ __forceinline__ uint32_t most_byte(uint32_t a, uint32_t b) {
-  const uint32_t m = __vmaxu2(__vmaxu2(a & 0x00FF00FFu, (a >> 8) & 0x00FF00FFu), __vmaxu2(b & 0x00FF00FFu, (b >> 8) & 0x00FF00FFu));
+// The largest byte of a word.
+__device__ __forceinline__ uint32_t most_byte(uint32_t w) {
+  const uint32_t m = __vmaxu2(w & 0x00FF00FFu, (w >> 8) & 0x00FF00FFu);
   return max(m & 0xFFFFu, m >> 16);
 }
 
 template <int WORDS>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
   if constexpr (WORDS == 1) {
-    asm("ld.global.nc.L1::no_allocate.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   } else if constexpr (WORDS == 2) {
-    asm("ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    w[0] = v.x, w[1] = v.y;
   } else {
 #pragma unroll
-    for (int i = 0; i < WORDS; i += 4)
-      asm("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
-          : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3])
-          : "l"(p + 4 * i));
-  }
-}
-
-// A lane's part of 16 tokens, as it is in the cache.
-template <int NB>
-struct Step {
-  static constexpr int kScaleWords = (NB + 3) / 4;
-  uint32_t k[2][NB], v[4][NB / 2], ks[2][kScaleWords], vs[2][kScaleWords];
-  // r: the first token's place in its page
-  __device__ __forceinline__ void load(const uint8_t* kp, const uint8_t* vp, int page, int r, int g, int t) {
-    constexpr int kRow = 16 * NB;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      load_words<NB>(kp + (r + g + 8 * i) * kRow + t * (4 * NB), k[i]);
-      const int sc = page * kRow + (r + g + 8 * i) * NB;
-      if constexpr (NB == 2) {
-        uint16_t a, b;
-        asm("ld.global.nc.b16 %0, [%1];" : "=h"(a) : "l"(kp + sc));
-        asm("ld.global.nc.b16 %0, [%1];" : "=h"(b) : "l"(vp + sc));
-        ks[i][0] = a;
-        vs[i][0] = b;
-      } else {
-        load_words<kScaleWords>(kp + sc, ks[i]);
-        load_words<kScaleWords>(vp + sc, vs[i]);
-      }
+    for (int i = 0; i < WORDS; i += 4) {
+      const uint4 v = reinterpret_cast<const uint4*>(p)[i / 4];
+      w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load_words<NB / 2>(vp + (r + 2 * t + (i & 1) + 8 * (i >> 1)) * kRow + g * (2 * NB), v[i]);
   }
-  __device__ __forceinline__ uint32_t most_scale() const {
-    if constexpr (NB == 8) return max(most_byte(vs[0][0], vs[1][0]), most_byte(vs[0][1], vs[1][1]));
-    else return most_byte(vs[0][0], vs[1][0]);
-  }
-  // (all 255s left out)
-  __device__ __forceinline__ uint32_t most_real_scale() const {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const uint32_t s = byte_at(vs[i], b);
-        if (s != 255u) m = max(m, s);
-      }
-    return m;
-  }
-  __device__ __forceinline__ bool nan_key(int i) const {
-    bool any = false;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) any |= byte_at(ks[i], b) == 255u;
-    return any;
-  }
-};
-
-template <int NB, int NT>
-constexpr int smem_bytes() {
-  return 8 * NT * 32 * NB * 2 + kWarps * 8 * NT * (32 * NB + 4) * 4 + kWarps * 8 * NT * 8 + 8 * NT * 16;
 }
+// a token's NB scale bytes
+template <int NB>
+__device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t* w) {
+  if constexpr (NB == 2)
+    w[0] = *reinterpret_cast<const uint16_t*>(p);
+  else
+    load_words<NB / 4>(p, w);
+}
+
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{ .reg .pred q; elect.sync _|q, 0xFFFFFFFF; selp.u32 %0, 1, 0, q; }" : "=r"(p));
+  return p != 0;
+}
+// `bytes` (a multiple of 16) from memory to shared memory, counted on `bar`
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src),
+               "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
+// What a CTA keeps.  A warp's region is its ring of steps (the codes of 32 tokens' keys, of their values, their scales), and then what it
+// hands on of its rows.
+template <int NB, int NT, int RESIDENT>
+struct Layout {
+  static constexpr int D = 32 * NB, ROWS = 8 * NT, kPitch = D + 4;
+  static constexpr int kCodes = kStep * 16 * NB, kScales = kStep * NB, kStage = 2 * (kCodes + kScales);
+  static constexpr int kStages = NB == 2 ? 4 : NB == 4 ? (RESIDENT == 2 ? 4 : 3) : (RESIDENT == 3 ? 2 : 3);
+  static constexpr int kHanded = ROWS * kPitch * 4;
+  static constexpr int kRegion = kStages * kStage > kHanded ? kStages * kStage : kHanded;
+  static constexpr int kQ = kWarps * kRegion, kMl = kQ + ROWS * D * 2, kRows = kMl + kWarps * ROWS * 8, kBytes = kRows + ROWS * 12;
+  static_assert(kRegion % 16 == 0 && kQ % 16 == 0 && kMl % 16 == 0, "");
+};
 
 template <int NB, int NT, int RESIDENT>
 __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const __grid_constant__ AttnArgs a) {
-  constexpr int D = 32 * NB, ROWS = 8 * NT, kPitch = D + 4;
+  using L = Layout<NB, NT, RESIDENT>;
+  constexpr int D = L::D, ROWS = L::ROWS, kPitch = L::kPitch, kStages = L::kStages;
   constexpr bool kKeepQ = NT * NB <= 8;                  // queries in registers
-  extern __shared__ __align__(16) uint8_t smem[];
-  uint2* qs = reinterpret_cast<uint2*>(smem);                                   // [NT][NB][2][32 lanes] of four float16
-  float* os = reinterpret_cast<float*>(smem + ROWS * D * 2);                    // [warps][ROWS][kPitch]
-  float2* mls = reinterpret_cast<float2*>(os + kWarps * ROWS * kPitch);         // [warps][ROWS]
-  float* fac = reinterpret_cast<float*>(mls + kWarps * ROWS);                   // rows: what a product of codes is times,
+  extern __shared__ __align__(128) uint8_t smem[];
+  uint2* qs = reinterpret_cast<uint2*>(smem + L::kQ);                           // [NT][NB][2][32 lanes] of four float16
+  float2* mls = reinterpret_cast<float2*>(smem + L::kMl);                       // [warps][ROWS]
+  float* fac = reinterpret_cast<float*>(smem + L::kRows);                       // rows: what a product of codes is times,
   int* lim = reinterpret_cast<int*>(fac + ROWS);                                // the last token seen (-1: none),
   int* low = lim + ROWS;                                                        // and the first
   __shared__ int64_t scan[kWarps];
   __shared__ int found_s;
   __shared__ int64_t found_at;
+  __shared__ uint64_t full_bars[kWarps][kStages];
+  __shared__ int has[kWarps][kStages];                   // which halves of a step are there
+  __shared__ int abort_flag;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
   const int hkv = a.c.hkv, cta = blockIdx.x;
+  if (tid == 0) {
+    for (int i = 0; i < kWarps * kStages; ++i) mbar_init(&full_bars[0][0] + i, 1);
+    abort_flag = 0;
+    fence_mbar_init();
+  }
   pdl_wait_then_release();
 
   // ---- this CTA's piece of the line
@@ -282,6 +292,10 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
   int64_t at = found_at;                                 // place in the sequence's part of the line
   int64_t left = to - from;
   Seq sq = seq_at<ROWS>(a, s);
+  uint8_t* const ring = smem + warp * L::kRegion;
+  uint64_t* const full = full_bars[warp];
+  int put = 0, get = 0, flying = 0;                      // ring places, steps on their way
+  uint32_t get_round = 0;
   while (left > 0) {
     while (at >= sq.cost(hkv)) {                         // the next sequence with work
       at -= sq.cost(hkv);
@@ -306,9 +320,54 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
     if (starts && step1 == 0) continue;                  // (only the unit's beginning: the next CTA has its first step)
     const int slot = 2 * cta + (starts ? 1 : 0);
 
+    const int t_base = (int)(sq.first / kStep) * kStep, t_end = (int)sq.end;
+    const int32_t* pages = a.table + (int64_t)s * a.width;
+    const uint8_t* head = a.c.base + (int64_t)h * a.c.part;
+    const int64_t page_bytes = 2 * a.c.hkv * a.c.part, to_v = a.c.hkv * a.c.part;
+    const int page = a.c.page;
+    auto page_of = [&](int tk, bool in) {                // -1: none
+      if (!in || tk >= t_end) return -1;
+      const int pg = __ldg(pages + (tk >> a.c.page_log));
+      return pg < 0 || pg >= a.pages ? -1 : pg;
+    };
+    // The step at token tk into the ring, if it is one of this piece's; the pages of the one after are looked up.
+    int pg0 = page_of(t_base + kStep * (step0 + warp), step0 + warp < step1);
+    int pg1 = page_of(t_base + kStep * (step0 + warp) + 16, step0 + warp < step1);
+    auto issue = [&](int st, int tk) {
+      if (st < step1) {
+        if (elect_one()) {
+          uint8_t* to = ring + put * L::kStage;
+          has[warp][put] = (pg0 >= 0 ? 1 : 0) | (pg1 >= 0 ? 2 : 0);
+          const bool together = page >= kStep && pg0 >= 0 && pg1 >= 0;
+          mbar_arrive_expect_tx(&full[put], (uint32_t)((pg0 >= 0) + (pg1 >= 0)) * (L::kStage / 2));
+#pragma unroll 1
+          for (int half = 0; half < (together ? 1 : 2); ++half) {
+            const int pg = half ? pg1 : pg0, n = together ? kStep : kStep / 2, o = half * (kStep / 2);
+            if (pg < 0) continue;
+            const uint8_t* k = head + pg * page_bytes;
+            const int r = (tk + o) & (page - 1);
+            const uint8_t* sc = k + (page * 16 + r) * NB;
+            k += r * (16 * NB);
+            bulk_load(to + o * (16 * NB), k, n * 16 * NB, &full[put]);
+            bulk_load(to + 2 * L::kCodes + o * NB, sc, n * NB, &full[put]);
+            bulk_load(to + L::kCodes + o * (16 * NB), k + to_v, n * 16 * NB, &full[put]);
+            bulk_load(to + 2 * L::kCodes + L::kScales + o * NB, sc + to_v, n * NB, &full[put]);
+          }
+        }
+        if (++put == kStages) put = 0;
+        ++flying;
+        pg0 = page_of(tk + kAhead, st + kWarps < step1);
+        pg1 = page_of(tk + kAhead + 16, st + kWarps < step1);
+      }
+    };
+    int step = step0 + warp, tok = t_base + kStep * step;
+    fence_proxy_async_smem();                            // (the region was written and read otherwise)
+    __syncthreads();                                     // the unit before has been handed on
+#pragma unroll 1
+    for (int i = 0; i < kStages - 1; ++i) issue(step + i * kWarps, tok + i * kAhead);
+
     // ---- queries to float16, in the order of the operand
     const int rows = min(ROWS, sq.ql * a.group - rt * ROWS);
-    __syncthreads();                                     // (the unit before has been written)
     for (int r = warp; r < ROWS; r += kWarps) {
       constexpr int kPer = NB;                           // channels a lane: D / 32
       float x[kPer];
@@ -356,13 +415,15 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
 #pragma unroll
           for (int u = 0; u < 2; ++u) qf[j][b][u] = qs[((j * NB + b) * 2 + u) * 32 + lane];
     }
-    float f[NT][2], m[NT][2], l[NT][2], acc[NB][2][NT][4];
+    // A score times fac less its row's `base` is what the exponential takes: base = m - (136 - ref), the weights times 2^(136 - ref), so
+    // that with a value's scale, 2^(byte - 127) of a byte up to ref, they are at most 2^(9 + kSlack).
+    float f[NT][2], m[NT][2], base[NT][2], l[NT][2], acc[NB][2][NT][4];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         f[j][i] = fac[8 * j + 2 * t + i];
-        m[j][i] = -1e30f;
+        base[j][i] = m[j][i] = -1e30f;
         l[j][i] = 0.f;
       }
 #pragma unroll
@@ -374,90 +435,42 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
 #pragma unroll
           for (int k = 0; k < 4; ++k) acc[b][i][j][k] = 0.f;
     int ref = kLowR;                                     // largest scale byte of values so far
+    float most = kSlack + (float)(136 - kLowR);          // what a score may exceed its base by
     // tokens that all rows see
     const int64_t p_first = sq.len - sq.ql + (rt * ROWS) / a.group, p_last = sq.len - sq.ql + (rt * ROWS + rows - 1) / a.group;
-    const int64_t all_to = p_first < sq.end - 1 ? p_first : sq.end - 1, all_from = a.window ? p_last - a.window + 1 : 0;
+    const int all_to = (int)(p_first < sq.end - 1 ? p_first : sq.end - 1);
+    const int all_from = a.window && p_last - a.window + 1 > 0 ? (int)(p_last - a.window + 1) : 0;
 
-    const int64_t t_base = sq.first / 16 * 16;
-    const int32_t* pages = a.table + (int64_t)s * a.width;
-    auto page_of = [&](int step) { return step < step1 ? (int64_t)pages[(t_base + 16 * (int64_t)step) >> a.c.page_log] : -1; };
-    auto load = [&](Step<NB>& st, int64_t pg, int step) {
-      if (pg < 0 || pg >= a.pages) return;
-      const uint8_t* kp = a.c.at(pg, 0, h);
-      st.load(kp, kp + a.c.hkv * a.c.part, a.c.page, (int)((t_base + 16 * (int64_t)step) & (a.c.page - 1)), g, t);
-    };
-    int step = step0 + warp;
-    Step<NB> next;
-    int64_t pg = page_of(step), pg_next = page_of(step + kWarps);
-    load(next, pg, step);
-    for (; step < step1; step += kWarps) {
-      const Step<NB> cur = next;
-      const int64_t here = pg;
-      pg = pg_next;
-      pg_next = page_of(step + 2 * kWarps);
-      load(next, pg, step + kWarps);
-      if (here < 0 || here >= a.pages) continue;
+    for (; step < step1; step += kWarps, tok += kAhead) {
+      issue(step + (kStages - 1) * kWarps, tok + (kStages - 1) * kAhead);
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&full[get], get_round & 1, &abort_flag, __LINE__))) break;
+      const uint8_t* st = ring + get * L::kStage;
+      const int here = has[warp][get];
+      uint32_t own[(NB + 3) / 4];                        // a token's values' scales
+      load_scales<NB>(st + 2 * L::kCodes + L::kScales + lane * NB, own);
+      if (!(here >> (lane >> 4) & 1))
+#pragma unroll
+        for (int i = 0; i < (NB + 3) / 4; ++i) own[i] = 0u;
 
-      // ---- scores
-      float x[NT][4];
+      // ---- the values' reference
+      bool odd = false;
+      uint32_t big = most_byte(own[0]);
+      if constexpr (NB == 8) big = max(big, most_byte(own[NB / 4 - 1]));
+      if (__any_sync(0xFFFFFFFFu, big > (uint32_t)ref)) {
+        uint32_t real = 0;                               // NaN's 255 is none
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[j][k] = 0.f;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        float part[NT][4];
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) part[j][k] = 0.f;
-        const uint32_t lo[4] = {code_pair<0>(cur.k[0][b]), code_pair<0>(cur.k[1][b]), code_pair<1>(cur.k[0][b]), code_pair<1>(cur.k[1][b])};
-        const uint32_t hi[4] = {code_pair<2>(cur.k[0][b]), code_pair<2>(cur.k[1][b]), code_pair<3>(cur.k[0][b]), code_pair<3>(cur.k[1][b])};
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const uint2 q0 = kKeepQ ? qf[kKeepQ ? j : 0][b][0] : qs[((j * NB + b) * 2) * 32 + lane];
-          const uint2 q1 = kKeepQ ? qf[kKeepQ ? j : 0][b][1] : qs[((j * NB + b) * 2 + 1) * 32 + lane];
-          mma(part[j], lo, q0.x, q0.y);
-          mma(part[j], hi, q1.x, q1.y);
-        }
-        const float s0 = byte_scale_at(cur.ks[0], b), s1 = byte_scale_at(cur.ks[1], b);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          x[j][0] = fmaf(part[j][0], s0, x[j][0]);
-          x[j][1] = fmaf(part[j][1], s0, x[j][1]);
-          x[j][2] = fmaf(part[j][2], s1, x[j][2]);
-          x[j][3] = fmaf(part[j][3], s1, x[j][3]);
-        }
-      }
-      const bool nan0 = cur.nan_key(0), nan1 = cur.nan_key(1);
-      const int64_t t0 = t_base + 16 * (int64_t)step;
-      bool over = false;
-      const bool partial = t0 + 15 > all_to || t0 < all_from;
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[j][k] *= f[j][k & 1];
-          if (k < 2 ? nan0 : nan1) x[j][k] = __int_as_float(0x7FFFFFFF);
-          if (partial) {
-            const int tok = (int)t0 + g + 8 * (k >> 1), r = 8 * j + 2 * t + (k & 1);
-            if (tok > lim[r] || tok < low[r]) x[j][k] = __int_as_float(0xFF800000);
-          }
-          over |= x[j][k] > m[j][k & 1] + kSlack;
-        }
-
-      // ---- running maxima and the values' reference
-      if (__any_sync(0xFFFFFFFFu, over)) {
+        for (int b = 0; b < NB; ++b)
+          if (byte_at(own, b) != 255u) real = max(real, byte_at(own, b));
+        const int top = max((int)__reduce_max_sync(0xFFFFFFFFu, real), ref);
+        odd = __any_sync(0xFFFFFFFFu, big == 255u);
+        const float by = ex2((float)(ref - top));
+        ref = top;
+        most = kSlack + (float)(136 - ref);
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float top = fmaxf(x[j][i], x[j][2 + i]);
-#pragma unroll
-            for (int k = 4; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
-            top = fmaxf(top, m[j][i]);
-            const float by = ex2(m[j][i] - top);
-            m[j][i] = top;
+            base[j][i] = m[j][i] - (float)(136 - ref);
             l[j][i] *= by;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -468,69 +481,159 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
               }
           }
       }
-      bool odd = false;
-      if (__any_sync(0xFFFFFFFFu, cur.most_scale() > (uint32_t)ref)) {
-        const int top = max((int)__reduce_max_sync(0xFFFFFFFFu, cur.most_real_scale()), ref);
-        odd = __any_sync(0xFFFFFFFFu, cur.most_scale() == 255u);
-        const float by = ex2((float)(ref - top));
-        ref = top;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          l[j][0] *= by;
-          l[j][1] *= by;
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) acc[b][c][j][k] *= by;
-        }
-      }
 
-      // ---- weights times 2^(136 - ref): with a value's scale, 2^(byte - 127), at most 2^15
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[j][k] = ex2(x[j][k] - (m[j][k & 1] - (float)(136 - ref)));
-          l[j][k & 1] += x[j][k];
-        }
+      for (int half = 0; half < 2; ++half) {
+        if (!(here >> half & 1)) continue;
+        const int t0 = tok + 16 * half;
+        const uint8_t* kc = st + (16 * half + g) * (16 * NB) + t * (4 * NB);
+        const uint8_t* ks = st + 2 * L::kCodes + (16 * half + g) * NB;
+        const uint8_t* vc = st + L::kCodes + (16 * half + 2 * t) * (16 * NB) + g * (2 * NB);
 
-      // ---- values
+        // ---- scores
+        float x[NT][4];
+        {
+          float s0[NB], s1[NB];
+          uint32_t w0[(NB + 3) / 4], w1[(NB + 3) / 4], k0[NB], k1[NB];
+          load_scales<NB>(ks, w0);
+          load_scales<NB>(ks + 8 * NB, w1);
+          load_words<NB>(kc, k0);
+          load_words<NB>(kc + 8 * 16 * NB, k1);
+          scales_of<NB>(w0, s0);
+          scales_of<NB>(w1, s1);
 #pragma unroll
-      for (int i = 0; i < NB / 2; ++i) {
-        // even and odd channels of pairs of tokens: nibbles side by side
-        uint32_t ev[2], ov[2];
+          for (int b = 0; b < NB; ++b) {
+            const uint32_t lo[4] = {code_pair<0>(k0[b]), code_pair<0>(k1[b]), code_pair<1>(k0[b]), code_pair<1>(k1[b])};
+            const uint32_t hi[4] = {code_pair<2>(k0[b]), code_pair<2>(k1[b]), code_pair<3>(k0[b]), code_pair<3>(k1[b])};
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
-          const uint32_t A = cur.v[2 * h2][i], B = cur.v[2 * h2 + 1][i];
-          ev[h2] = (A & 0x0F0F0F0Fu) | ((B << 4) & 0xF0F0F0F0u);
-          ov[h2] = ((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u);
-        }
-        const uint32_t va[4][4] = {{code_pair<0>(ev[0]), code_pair<0>(ov[0]), code_pair<0>(ev[1]), code_pair<0>(ov[1])},
-                                   {code_pair<1>(ev[0]), code_pair<1>(ov[0]), code_pair<1>(ev[1]), code_pair<1>(ov[1])},
-                                   {code_pair<2>(ev[0]), code_pair<2>(ov[0]), code_pair<2>(ev[1]), code_pair<2>(ov[1])},
-                                   {code_pair<3>(ev[0]), code_pair<3>(ov[0]), code_pair<3>(ev[1]), code_pair<3>(ov[1])}};
-#pragma unroll
-        for (int o = 0; o < 2; ++o) {
-          const int b = 2 * i + o;
-          const float s0 = byte_scale_at(cur.vs[0], b), s1 = byte_scale_at(cur.vs[1], b);
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            float w[4] = {x[j][0] * s0, x[j][1] * s0, x[j][2] * s1, x[j][3] * s1};
-            if (odd) {                                   // a NaN scale counts for rows that see its token only
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                if (byte_at(cur.vs[k >> 1], b) == 255u) w[k] = __int_as_float(0x7FFFFFFF);
-                if (x[j][k] == 0.f) w[k] = 0.f;
+            for (int j = 0; j < NT; ++j) {
+              const uint2 q0 = kKeepQ ? qf[kKeepQ ? j : 0][b][0] : qs[((j * NB + b) * 2) * 32 + lane];
+              const uint2 q1 = kKeepQ ? qf[kKeepQ ? j : 0][b][1] : qs[((j * NB + b) * 2 + 1) * 32 + lane];
+              float part[4];
+              mma_first(part, lo, q0.x, q0.y);
+              mma(part, hi, q1.x, q1.y);
+              if (b == 0) {
+                x[j][0] = part[0] * s0[0], x[j][1] = part[1] * s0[0], x[j][2] = part[2] * s1[0], x[j][3] = part[3] * s1[0];
+              } else {
+                x[j][0] = fmaf(part[0], s0[b], x[j][0]), x[j][1] = fmaf(part[1], s0[b], x[j][1]);
+                x[j][2] = fmaf(part[2], s1[b], x[j][2]), x[j][3] = fmaf(part[3], s1[b], x[j][3]);
               }
             }
-            const uint32_t p0 = transpose(f16_pair(w[0], w[1])), p1 = transpose(f16_pair(w[2], w[3]));
-            mma(acc[b][0][j], va[2 * o], p0, p1);
-            mma(acc[b][1][j], va[2 * o + 1], p0, p1);
+          }
+        }
+        const bool partial = t0 + 15 > all_to || t0 < all_from;
+        auto hidden = [&](int j, int k) {
+          const int at_tok = t0 + g + 8 * (k >> 1), r = 8 * j + 2 * t + (k & 1);
+          return at_tok > lim[r] || at_tok < low[r];
+        };
+        float e[NT][4], top = -1e30f;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            e[j][k] = fmaf(x[j][k], f[j][k & 1], -base[j][k & 1]);
+            if (partial && hidden(j, k)) e[j][k] = __int_as_float(0xFF800000);
+            top = fmaxf(top, e[j][k]);
+          }
+
+        // ---- running maxima
+        if (__any_sync(0xFFFFFFFFu, top > most)) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float lo = partial && hidden(j, i) ? -1e30f : x[j][i] * f[j][i];
+              const float hi = partial && hidden(j, 2 + i) ? -1e30f : x[j][2 + i] * f[j][i];
+              float up = fmaxf(lo, hi);
+#pragma unroll
+              for (int k = 4; k < 32; k <<= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, k));
+              up = fmaxf(up, m[j][i]);
+              const float by = ex2(m[j][i] - up);
+              m[j][i] = up;
+              base[j][i] = up - (float)(136 - ref);
+              l[j][i] *= by;
+#pragma unroll
+              for (int k = i; k < 4; k += 2)
+                if (!(partial && hidden(j, k))) e[j][k] = fmaf(x[j][k], f[j][i], -base[j][i]);
+#pragma unroll
+              for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                  acc[b][c][j][i] *= by;
+                  acc[b][c][j][2 + i] *= by;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            x[j][k] = ex2(e[j][k]);
+            l[j][k & 1] += x[j][k];
+          }
+
+        // ---- values
+        float s0[NB], s1[NB];
+        uint32_t w0[(NB + 3) / 4], w1[(NB + 3) / 4], v[4][NB / 2];
+        load_scales<NB>(ks + L::kScales, w0);
+        load_scales<NB>(ks + L::kScales + 8 * NB, w1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_words<NB / 2>(vc + ((i & 1) + 8 * (i >> 1)) * (16 * NB), v[i]);
+        scales_of<NB>(w0, s0);
+        scales_of<NB>(w1, s1);
+#pragma unroll
+        for (int i = 0; i < NB / 2; ++i) {
+          // even and odd channels of pairs of tokens: nibbles side by side
+          uint32_t ev[2], ov[2];
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2) {
+            const uint32_t A = v[2 * h2][i], B = v[2 * h2 + 1][i];
+            ev[h2] = (A & 0x0F0F0F0Fu) | ((B << 4) & 0xF0F0F0F0u);
+            ov[h2] = ((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u);
+          }
+          const uint32_t va[4][4] = {{code_pair<0>(ev[0]), code_pair<0>(ov[0]), code_pair<0>(ev[1]), code_pair<0>(ov[1])},
+                                     {code_pair<1>(ev[0]), code_pair<1>(ov[0]), code_pair<1>(ev[1]), code_pair<1>(ov[1])},
+                                     {code_pair<2>(ev[0]), code_pair<2>(ov[0]), code_pair<2>(ev[1]), code_pair<2>(ov[1])},
+                                     {code_pair<3>(ev[0]), code_pair<3>(ov[0]), code_pair<3>(ev[1]), code_pair<3>(ov[1])}};
+#pragma unroll
+          for (int o = 0; o < 2; ++o) {
+            const int b = 2 * i + o;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              float w[4] = {x[j][0] * s0[b], x[j][1] * s0[b], x[j][2] * s1[b], x[j][3] * s1[b]};
+              if (odd) {                                 // a NaN scale counts for rows that see its token only
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (x[j][k] == 0.f) w[k] = 0.f;
+              }
+              const uint32_t p0 = transpose(f16_pair(w[0], w[1])), p1 = transpose(f16_pair(w[2], w[3]));
+              mma(acc[b][0][j], va[2 * o], p0, p1);
+              mma(acc[b][1][j], va[2 * o + 1], p0, p1);
+            }
           }
         }
       }
+      __syncwarp();                                      // all lanes have read the step
+      --flying;
+      if (++get == kStages) {
+        get = 0;
+        ++get_round;
+      }
+    }
+    if (abort_flag) {                                    // a wait gave up: the copies still on their way, then out
+      volatile int none = 0;
+      for (; flying > 0; --flying) {
+        mbar_wait_bounded(&full[get], get_round & 1, &none);
+        if (++get == kStages) {
+          get = 0;
+          ++get_round;
+        }
+      }
+    }
+    __syncthreads();                                     // (the warps' last reads of their rings, too)
+    if (abort_flag) {
+      if (tid == 0) report(a.status, timeout_bits(kWhereMxAttention, abort_flag));
+      return;
     }
 
     // ---- the warps' parts together
@@ -542,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) l[j][i] += __shfl_xor_sync(0xFFFFFFFFu, l[j][i], k);
         if (g == 0) mls[warp * ROWS + 8 * j + 2 * t + i] = make_float2(m[j][i], l[j][i] * unref);
-        float* o = os + (warp * ROWS + 8 * j + 2 * t + i) * kPitch;
+        float* o = reinterpret_cast<float*>(smem + warp * L::kRegion) + (8 * j + 2 * t + i) * kPitch;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
           *reinterpret_cast<float4*>(o + 32 * b + 4 * g) = make_float4(acc[b][0][j][i] * unref, acc[b][0][j][2 + i] * unref,
@@ -559,7 +662,7 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
       for (int w = 0; w < kWarps; ++w) {
         const float2 ml = mls[w * ROWS + r];
         const float by = ex2(ml.x - top);
-        const float4 v = *reinterpret_cast<const float4*>(os + (w * ROWS + r) * kPitch + 4 * c);
+        const float4 v = *reinterpret_cast<const float4*>(smem + w * L::kRegion + (r * kPitch + 4 * c) * 4);
         sum = fmaf(ml.y, by, sum);
         o.x = fmaf(v.x, by, o.x), o.y = fmaf(v.y, by, o.y), o.z = fmaf(v.z, by, o.z), o.w = fmaf(v.w, by, o.w);
       }
@@ -657,7 +760,7 @@ size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 template <int NB, int NT, int RESIDENT>
 cudaError_t run(AttnArgs a, int grid, cudaStream_t stream) {
   static PerDevice<cudaError_t> allowed;
-  constexpr int kSmem = smem_bytes<NB, NT>();
+  constexpr int kSmem = Layout<NB, NT, RESIDENT>::kBytes;
   cudaError_t e = allowed.get([] { return allow_smem(mx_attention_kernel<NB, NT, RESIDENT>, kSmem); });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -690,7 +793,7 @@ int64_t mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv,
 cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,
                                 int64_t d, const int32_t* table, int64_t width, const int32_t* lens, int64_t seqs,
                                 const int32_t* offsets, float scale, int64_t window, int out_dtype, void* out, void* workspace,
-                                cudaStream_t stream) {
+                                uint32_t* status, cudaStream_t stream) {
   if (seqs == 0) return cudaMemsetAsync(out, 0, (size_t)n * hq * d * (out_dtype == 0 ? 4 : 2), stream);
   const int sms = sm_count();
   if (sms < 0) return cudaErrorInvalidDevice;
@@ -705,7 +808,7 @@ cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint
   a.pages = pages, a.table = table, a.lens = lens, a.offsets = offsets, a.width = width;
   a.n = (int)n, a.hq = (int)hq, a.group = (int)(hq / hkv), a.seqs = (int)seqs;
   a.scale = scale * 1.44269504f;
-  a.window = window, a.out = out, a.out_f32 = out_dtype == 0;
+  a.status = status, a.window = window, a.out = out, a.out_f32 = out_dtype == 0;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.parts = reinterpret_cast<float*>(ws);
   a.ml = reinterpret_cast<float*>(ws + round_up(rows * d * 4));

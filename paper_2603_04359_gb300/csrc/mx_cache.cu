@@ -390,7 +390,7 @@ __device__ __noinline__ void exact_key(const RopeArgs& a, const T* x, const void
 constexpr float kMargin = 20.f * 0x1p-24f;
 
 template <typename T, int NB, int PAIRS>
-__global__ void __launch_bounds__(kThreads) mx_rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int D = 32 * NB;
   const int lane = threadIdx.x & 31, p = lane & 3;
   const int64_t item = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
