@@ -22,7 +22,7 @@
 // parts go through the workspace, and a second kernel joins them in the order of their tokens.
 #include <cuda_fp16.h>
 
-#include "mx_cache.cuh"
+#include "mx_attention.cuh"
 #include "per_device.h"
 
 namespace cat {
@@ -33,62 +33,22 @@ constexpr int kStep = 32;                   // tokens a warp takes at once (two 
 constexpr int kUnitCost = 2;                // a unit's beginning and end, in steps
 constexpr int kAhead = kStep * kWarps;      // tokens between a warp's steps
 constexpr int kLeastPiece = 4;              // steps a CTA is worth
-constexpr float kSlack = 6.f;               // a row's scores may exceed its running maximum by this (binary orders) before it follows
 constexpr int kLowR = 40;                   // least reference exponent of the values (below it they count less bits)
 
-// A CTA's piece that begins a unit which others go on with.
-struct Plan {
-  int s, h, rt, last;                       // last: the last CTA with a part of it; -1: none
-};
-
-struct AttnArgs {
-  const __nv_bfloat16* q;
-  MxCache c;
-  int64_t pages;
-  const int32_t *table, *lens, *offsets;
-  int64_t width;
-  int n, hq, group, seqs;
-  float scale;                              // scale log2 e
-  int64_t window;
-  void* out;
-  int out_f32;
-  float *parts, *ml;                        // [2 grid][rows][D], [2 grid][rows][2]
-  Plan* plan;
-  uint32_t* status;
-};
-
-struct Seq {
-  int begin, ql, steps, tiles;              // first row, rows, steps and row tiles
-  int64_t len, first, end;                  // tokens; the first a row sees; one past the last in the cache
+struct Seq : Rows {
+  int steps, tiles;                         // steps and row tiles; no steps: none, or the other kernel's
   __device__ __forceinline__ int64_t cost(int hkv) const { return steps ? (int64_t)tiles * hkv * (steps + kUnitCost) : 0; }
 };
-
 template <int ROWS>
 __device__ __forceinline__ Seq seq_at(const AttnArgs& a, int s) {
   Seq q;
-  int end;
-  if (a.offsets) {
-    q.begin = min(max(a.offsets[s], 0), a.n);
-    end = min(max(a.offsets[s + 1], q.begin), a.n);
-  } else {
-    q.begin = s;
-    end = s + 1;
-  }
-  q.ql = end - q.begin;
-  q.len = a.lens[s];
-  const int64_t cap = a.width << a.c.page_log, p = q.len - q.ql;
-  q.end = q.len < cap ? q.len : cap;
-  q.first = a.window && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
-  q.steps = q.ql > 0 && q.end > q.first ? (int)((q.end + kStep - 1) / kStep - q.first / kStep) : 0;
-  q.tiles = (int)(((int64_t)q.ql * a.group + ROWS - 1) / ROWS);
+  static_cast<Rows&>(q) = rows_of(a, s);
+  const int64_t rows = (int64_t)q.ql * a.group;
+  q.steps = q.any() && rows <= a.few ? (int)((q.end + kStep - 1) / kStep - q.first / kStep) : 0;
+  q.tiles = (int)((rows + ROWS - 1) / ROWS);
   return q;
 }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // 16 x 8 += 16 x 16 times 16 x 8, float16 operands
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -176,18 +136,6 @@ __device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t* w) {
     load_words<NB / 4>(p, w);
 }
 
-__device__ __forceinline__ bool elect_one() {
-  uint32_t p;
-  asm volatile("{ .reg .pred q; elect.sync _|q, 0xFFFFFFFF; selp.u32 %0, 1, 0, q; }" : "=r"(p));
-  return p != 0;
-}
-// `bytes` (a multiple of 16) from memory to shared memory, counted on `bar`
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src),
-               "r"(bytes), "r"(smem_u32(bar))
-               : "memory");
-}
-
 // What a CTA keeps.  A warp's region is its ring of steps (the codes of 32 tokens' keys, of their values, their scales), and then what it
 // hands on of its rows.
 template <int NB, int NT, int RESIDENT>
@@ -266,26 +214,9 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
     }
   }
 
-  // ---- rows that see nothing because their sequence has no tokens, and rows of no sequence
-  {
-    const int64_t row_words = (int64_t)a.hq * D / (a.out_f32 ? 4 : 8);
-    uint4* out = static_cast<uint4*>(a.out);
-    auto clear = [&](int64_t r0, int64_t r1, int64_t first, int64_t stride) {
-      for (int64_t i = r0 * row_words + first; i < r1 * row_words; i += stride) out[i] = make_uint4(0u, 0u, 0u, 0u);
-    };
-    for (int s = cta; s < a.seqs; s += gridDim.x) {
-      const Seq q = seq_at<ROWS>(a, s);
-      if (!q.steps && q.ql > 0) clear(q.begin, q.begin + q.ql, tid, kThreads);
-    }
-    if (a.offsets) {
-      const int64_t first = (int64_t)cta * kThreads + tid, stride = (int64_t)gridDim.x * kThreads;
-      const int head = min(max(a.offsets[0], 0), a.n), tail = min(max(a.offsets[a.seqs], 0), a.n);
-      clear(0, head, first, stride);
-      clear(max(tail, head), a.n, first, stride);
-    }
-  }
+  if (a.clears) clear_rows<D>(a);
   __syncthreads();
-  if (tid == 0 && a.plan) a.plan[cta].last = -1;
+  if (tid == 0) a.plan[cta].last = -1;
   if (cta >= ctas) return;
 
   int s = found_s;
@@ -440,6 +371,9 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
     const int64_t p_first = sq.len - sq.ql + (rt * ROWS) / a.group, p_last = sq.len - sq.ql + (rt * ROWS + rows - 1) / a.group;
     const int all_to = (int)(p_first < sq.end - 1 ? p_first : sq.end - 1);
     const int all_from = a.window && p_last - a.window + 1 > 0 ? (int)(p_last - a.window + 1) : 0;
+    // and that some row sees
+    const int some_to = (int)(p_last < sq.end - 1 ? p_last : sq.end - 1);
+    const int some_from = a.window && p_first - a.window + 1 > 0 ? (int)(p_first - a.window + 1) : 0;
 
     for (; step < step1; step += kWarps, tok += kAhead) {
       issue(step + (kStages - 1) * kWarps, tok + (kStages - 1) * kAhead);
@@ -457,10 +391,11 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
       uint32_t big = most_byte(own[0]);
       if constexpr (NB == 8) big = max(big, most_byte(own[NB / 4 - 1]));
       if (__any_sync(0xFFFFFFFFu, big > (uint32_t)ref)) {
-        uint32_t real = 0;                               // NaN's 255 is none
+        uint32_t real = 0;                               // NaN's 255 is none, nor is what no row sees, which may be anything
+        if (tok + lane >= some_from && tok + lane <= some_to)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-          if (byte_at(own, b) != 255u) real = max(real, byte_at(own, b));
+          for (int b = 0; b < NB; ++b)
+            if (byte_at(own, b) != 255u) real = max(real, byte_at(own, b));
         const int top = max((int)__reduce_max_sync(0xFFFFFFFFu, real), ref);
         odd = __any_sync(0xFFFFFFFFu, big == 255u);
         const float by = ex2((float)(ref - top));
@@ -671,13 +606,7 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
         const int64_t to_row = ((int64_t)(sq.begin + j) * a.hq + h * a.group + (rr - j * a.group)) * D + 4 * c;
         const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
         o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
-        if (a.out_f32) {
-          *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to_row) = o;
-        } else {
-          const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x, o.y), hi = __floats2bfloat162_rn(o.z, o.w);
-          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to_row) =
-              make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-        }
+        store4(a, to_row, o);
       } else {
         *reinterpret_cast<float4*>(a.parts + ((int64_t)slot * ROWS + r) * D + 4 * c) = o;
         if (c == 0) *reinterpret_cast<float2*>(a.ml + ((int64_t)slot * ROWS + r) * 2) = make_float2(top, sum);
@@ -686,79 +615,30 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
   }
 }
 
-// The parts of a unit, one row a CTA: blockIdx.x the CTA that began it.
-template <int NB, int NT>
-__global__ void __launch_bounds__(kThreads) mx_attention_join_kernel(const __grid_constant__ AttnArgs a) {
-  constexpr int D = 32 * NB, ROWS = 8 * NT, kLanes = D / 4, kGroups = kThreads / kLanes;   // lanes a row of four channels; parts at once
-  __shared__ float4 os[kThreads];
-  __shared__ float2 mls[kGroups];
-  pdl_wait_then_release();
-  const int cta = blockIdx.x, r = blockIdx.y;
-  const Plan p = a.plan[cta];
-  if (p.last < 0) return;
-  const Seq sq = seq_at<ROWS>(a, p.s);
-  if (r >= min(ROWS, sq.ql * a.group - p.rt * ROWS)) return;
-  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  float top = -1e30f, sum = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = cta + group; k <= p.last; k += kGroups) {
-    const int64_t slot = ((int64_t)2 * k + (k == cta ? 1 : 0)) * ROWS + r;
-    const float2 ml = *reinterpret_cast<const float2*>(a.ml + slot * 2);
-    const float4 v = *reinterpret_cast<const float4*>(a.parts + slot * D + 4 * lane);
-    const float now = fmaxf(top, ml.x), was = ex2(top - now), by = ex2(ml.x - now);
-    top = now;
-    sum = sum * was + ml.y * by;
-    o.x = o.x * was + v.x * by, o.y = o.y * was + v.y * by, o.z = o.z * was + v.z * by, o.w = o.w * was + v.w * by;
-  }
-  os[threadIdx.x] = o;
-  if (lane == 0) mls[group] = make_float2(top, sum);
-  __syncthreads();
-  if (group != 0) return;
-  for (int w = 1; w < kGroups; ++w) {
-    const float2 ml = mls[w];
-    const float4 v = os[w * kLanes + lane];
-    const float now = fmaxf(top, ml.x), was = ex2(top - now), by = ex2(ml.x - now);
-    top = now;
-    sum = sum * was + ml.y * by;
-    o.x = o.x * was + v.x * by, o.y = o.y * was + v.y * by, o.z = o.z * was + v.z * by, o.w = o.w * was + v.w * by;
-  }
-  const int rr = p.rt * ROWS + r, j = rr / a.group;
-  const int64_t to_row = ((int64_t)(sq.begin + j) * a.hq + p.h * a.group + (rr - j * a.group)) * D + 4 * lane;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
-  if (a.out_f32) {
-    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to_row) = o;
-  } else {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x, o.y), hi = __floats2bfloat162_rn(o.z, o.w);
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to_row) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-  }
-}
-
-int sm_count() {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return -1;
-  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) return -1;
-  return sms;
-}
-
-// Tiles of 8 rows that a call's units have, and CTAs an SM: by what a warp keeps in registers (NT 16-channel accumulators a block of
-// 32 channels, and two steps' codes).
+// Tiles of 8 rows that the units of sequences of few rows have, and CTAs an SM: by what a warp keeps in registers.
 struct Form {
   int nt, resident;
 };
-Form form_of(int64_t n, int64_t seqs, int64_t hq, int64_t hkv, int64_t d) {
-  const int64_t rows = (n + seqs - 1) / seqs * (hq / hkv);     // of a sequence, on average
-  const int most = d == 256 ? 2 : 4;
-  int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-  if (nt > most) nt = most;
-  return {nt, (int)(nt * d <= 128 ? 4 : nt * d <= 256 ? 3 : 2)};
+Form form_of(int64_t n, int64_t seqs, int64_t group, int64_t d) {
+  const int64_t rows = (n + seqs - 1) / seqs * group;    // of a sequence, on average
+  const int nt = rows <= 8 ? 1 : 2;
+  return {nt, nt * d <= 128 ? 4 : nt * d <= 256 ? 3 : 2};
 }
 
-size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
+// Which kernels a call takes.  Both can do any number of rows; with no more rows than sequences (a decode step, whatever its
+// offsets) the first does all, with one sequence or many heads on a key head it is known which is the better one for all, and else
+// either leaves the other's sequences out (an empty launch of the second costs a decode step some 5 us).
+struct Needs {
+  bool few, tiles;
+  Needs(int64_t n, int64_t seqs, int64_t group) {
+    tiles = group > kMostFewRows || (n > seqs && n * group > kMostFewRows);
+    few = !tiles || (group <= kMostFewRows && seqs > 1);
+  }
+  int most_few() const { return few ? tiles ? kMostFewRows : 0x7FFFFFFF : 0; }
+};
 
 template <int NB, int NT, int RESIDENT>
-cudaError_t run(AttnArgs a, int grid, cudaStream_t stream) {
+cudaError_t run(const AttnArgs& a, int grid, cudaStream_t stream) {
   static PerDevice<cudaError_t> allowed;
   constexpr int kSmem = Layout<NB, NT, RESIDENT>::kBytes;
   cudaError_t e = allowed.get([] { return allow_smem(mx_attention_kernel<NB, NT, RESIDENT>, kSmem); });
@@ -773,10 +653,14 @@ cudaError_t run(AttnArgs a, int grid, cudaStream_t stream) {
   cfg.numAttrs = 1;
   note_launch();
   if ((e = cudaLaunchKernelEx(&cfg, mx_attention_kernel<NB, NT, RESIDENT>, a)) != cudaSuccess) return e;
-  cfg.gridDim = dim3((unsigned)grid, 8 * NT);
-  cfg.dynamicSmemBytes = 0;
-  note_launch();
-  return cudaLaunchKernelEx(&cfg, mx_attention_join_kernel<NB, NT>, a);
+  return launch_join<32 * NB, 8 * NT>(a, grid, stream);
+}
+
+int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return -1;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) return -1;
+  return sms;
 }
 
 }  // namespace
@@ -785,9 +669,13 @@ int64_t mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv,
   if (seqs == 0) return 0;
   const int sms = sm_count();
   if (sms < 0) return -1;
-  const Form f = form_of(n, seqs, hq, hkv, d);
-  const size_t grid = (size_t)sms * f.resident, rows = 2 * grid * 8 * f.nt;
-  return (int64_t)(round_up(rows * d * 4) + round_up(rows * 8) + round_up(grid * sizeof(Plan)));
+  const int64_t group = hq / hkv;
+  const Form f = form_of(n, seqs, group, d);
+  const Needs needs(n, seqs, group);
+  size_t bytes = 0;
+  if (needs.few) bytes += Parts((size_t)sms * f.resident, 8 * f.nt, d).bytes;
+  if (needs.tiles) bytes += Parts(sms, attention_tile_rows(d), d).bytes;
+  return (int64_t)bytes;
 }
 
 cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,
@@ -797,9 +685,6 @@ cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint
   if (seqs == 0) return cudaMemsetAsync(out, 0, (size_t)n * hq * d * (out_dtype == 0 ? 4 : 2), stream);
   const int sms = sm_count();
   if (sms < 0) return cudaErrorInvalidDevice;
-  const Form f = form_of(n, seqs, hq, hkv, d);
-  const int grid = sms * f.resident;
-  const size_t rows = (size_t)2 * grid * 8 * f.nt;
   AttnArgs a = {};
   int log = 0;
   while ((int64_t(1) << log) < page) ++log;
@@ -809,12 +694,22 @@ cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint
   a.n = (int)n, a.hq = (int)hq, a.group = (int)(hq / hkv), a.seqs = (int)seqs;
   a.scale = scale * 1.44269504f;
   a.status = status, a.window = window, a.out = out, a.out_f32 = out_dtype == 0;
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  a.parts = reinterpret_cast<float*>(ws);
-  a.ml = reinterpret_cast<float*>(ws + round_up(rows * d * 4));
-  a.plan = reinterpret_cast<Plan*>(ws + round_up(rows * d * 4) + round_up(rows * 8));
-  if (d == 64) return f.nt == 1 ? run<2, 1, 4>(a, grid, stream) : f.nt == 2 ? run<2, 2, 4>(a, grid, stream) : run<2, 4, 3>(a, grid, stream);
-  if (d == 128) return f.nt == 1 ? run<4, 1, 4>(a, grid, stream) : f.nt == 2 ? run<4, 2, 3>(a, grid, stream) : run<4, 4, 2>(a, grid, stream);
+  const Form f = form_of(n, seqs, a.group, d);
+  const Needs needs(n, seqs, a.group);
+  a.few = needs.most_few();
+  const Parts parts((size_t)sms * f.resident, 8 * f.nt, d), tiles(sms, attention_tile_rows(d), d);
+  cudaError_t e = cudaSuccess;
+  a.clears = 1;
+  if (needs.tiles) {
+    tiles.place(&a, workspace);
+    if ((e = launch_attention_tiles(a, d, sms, stream)) != cudaSuccess || !needs.few) return e;
+    workspace = static_cast<uint8_t*>(workspace) + tiles.bytes;
+    a.clears = 0;
+  }
+  parts.place(&a, workspace);
+  const int grid = sms * f.resident;
+  if (d == 64) return f.nt == 1 ? run<2, 1, 4>(a, grid, stream) : run<2, 2, 4>(a, grid, stream);
+  if (d == 128) return f.nt == 1 ? run<4, 1, 4>(a, grid, stream) : run<4, 2, 3>(a, grid, stream);
   return f.nt == 1 ? run<8, 1, 3>(a, grid, stream) : run<8, 2, 2>(a, grid, stream);
 }
 

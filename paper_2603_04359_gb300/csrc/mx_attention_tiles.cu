@@ -1,0 +1,730 @@
+// Attention of tiles of query rows over pages of the 4-bit cache: prompts, and more rows than mx_attention.cu is for.
+//
+//   S = Q K^T (128 rows x KT tokens, float32 in tensor memory),  P = 2^(s - m),  O = O 2^(m' - m) + P V
+//
+// on 5th-generation tensor cores, float16 operands.  The tensor cores take the codes as numbers only after they are unpacked: each of
+// a step's keys and values to float16, code times 2^(byte - ref + 12) with ref the largest scale byte of a warp's tokens (keys;
+// the products of 32 tokens are times its power again) or of all values so far (O is scaled when it grows).  That is exact down to 2^-22
+// of the largest block, and to 2^-36 with fewer bits.  A step's unpacking is shared by 256 rows (two tiles of 128; d = 256: one):
+// queries of a key head's group lie together, row r is head r % group of token r / group.
+//
+// Per step of 128 tokens at d = 128 the MMAs take 2048 cycles of an SM, the exponentials of 2 x 16384 scores 1024, the
+// unpacking ~400 issue slots a scheduler: so what bounds it are the MMAs, if the others keep out of their way.
+//
+// Warps (576 threads, one CTA an SM):
+//   0..3, 4..7   a tile's rows each, one a thread: scores from tensor memory, weights back to it (over the scores; the A operand of P V
+//                is read there), the running maximum and sum, O's correction where the maximum grows by more than 2^6, output
+//   8..11        keys to float16, 12..15 values: a token's row a thread (d = 256: half of one)
+//   16           issues the MMAs: P V of a tile, then the tile's next scores, the other tile's behind them
+//   17           bulk copies of the codes as they are, a ring of three
+// MMAs of one thread are carried out in the order of their issue, so next scores may follow the product that reads the weights
+// in their place.  Every wait is bounded; one that gives up raises the device status word and all roles drain and leave.
+//
+// A CTA has an equal piece of a line of all units as mx_attention.cu's; a unit's length there is a straight line in its number (the
+// tokens that its last row sees, or the window), so that its place can be found without a list.
+#include <cuda_fp16.h>
+
+#include "mx_attention.cuh"
+#include "per_device.h"
+
+namespace cat {
+namespace {
+
+constexpr int kThreads = 576;
+constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
+constexpr int kUnitCost = 384;              // a unit's beginning and end, in tokens
+constexpr int kLeastPiece = 1024;           // tokens (with units' costs) that a CTA is worth
+constexpr int kLowR = 16;                   // least reference scale byte
+constexpr uint32_t kTmemCols = 512;
+
+template <int NB>
+struct Tc {
+  static constexpr int D = 32 * NB, QT = NB == 8 ? 1 : 2, KT = NB == 8 ? 64 : 128, ROWS = 128 * QT;
+  static constexpr int kQ = 128 * D * 2, kTile = KT * D * 2, kCodes = KT * 16 * NB, kRaw = kCodes + KT * NB, kRing = 3;
+  static constexpr int kOffK = QT * kQ, kOffV = kOffK + 2 * kTile, kOffRaw = kOffV + 2 * kTile, kOffBars = kOffRaw + kRing * kRaw;
+  static constexpr int kSmem = 1024 + kOffBars + 2048;
+  static constexpr uint32_t kO = QT * KT;                // tensor memory: a tile's scores, then O's
+  static_assert(kSmem <= 227 * 1024 && QT * (KT + D) <= (int)kTmemCols, "");
+};
+
+struct Bars {
+  uint64_t raw_full[3], raw_empty[3], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full, s_full[2], p_full[2], pv_done[2], most_full, mma_done;
+  // (of four steps: keys are unpacked two steps ahead of scores that are still read)
+  float k_factor[4][4];                     // 2^(ref - 139) of a warp's tokens' keys
+  uint32_t there[4];                        // which 16-token groups of a step are on pages
+  uint32_t raw_there[3];
+  int v_ref[2];                             // the values' reference
+  uint32_t v_odd[2][4];                     // whether a scale of a warp's tokens is NaN
+  uint32_t v_most[2][4];                    // their largest
+  uint8_t v_nan[2][128];                    // a token's blocks of NaN scales
+  int64_t scan[kThreads / 32];
+  int64_t found_at;
+  int found_s, abort;
+  uint32_t tmem_addr;
+};
+static_assert(sizeof(Bars) <= 2048, "barrier room");
+
+struct Seq : Rows {
+  int tiles;
+  int64_t a, b;                             // a unit of row tile i has a + b i of the line
+  __device__ __forceinline__ int64_t before(int64_t i) const { return a * i + b * (i * (i - 1) / 2); }     // tiles 0 .. i - 1
+};
+template <int ROWS>
+__device__ __forceinline__ Seq seq_at(const AttnArgs& a, int s) {
+  Seq q;
+  static_cast<Rows&>(q) = rows_of(a, s);
+  const int64_t rows = (int64_t)q.ql * a.group;
+  q.tiles = q.any() && rows > a.few ? (int)((rows + ROWS - 1) / ROWS) : 0;
+  const int64_t tokens = (ROWS + a.group - 1) / a.group, past = q.len > q.ql ? q.len - q.ql : 0;
+  q.a = kUnitCost + past + tokens;
+  q.b = tokens;
+  if (a.window && a.window + tokens < past + tokens * q.tiles) {
+    q.a = kUnitCost + a.window + tokens;
+    q.b = 0;
+  }
+  return q;
+}
+
+// A CTA's way along its piece, the same in all warps.
+struct Unit {
+  int s, h, rt, rows, j0, j1;               // the steps of KT tokens, from the sequence's beginning
+  bool starts, whole, nothing;              // nothing: no row sees a token
+  int64_t p0;                               // the token of the sequence's first row
+  int64_t t0, t1;                           // the tokens that some row sees
+};
+template <int NB>
+struct Walk {
+  using C = Tc<NB>;
+  const AttnArgs& a;
+  int s;
+  int64_t at, left, to;
+  Seq q;
+  __device__ __forceinline__ Walk(const AttnArgs& args, int s_, int64_t at_, int64_t from, int64_t to_)
+      : a(args), s(s_), at(at_), left(to_ - from), to(to_), q(seq_at<C::ROWS>(args, s_)) {}
+  // The next unit with something to do; place and length on the line by `end` (where the unit ends) for who plans
+  __device__ __forceinline__ bool next(Unit& u, int64_t* unit_end = nullptr) {
+    while (left > 0) {
+      int64_t all = a.c.hkv * q.before(q.tiles);
+      while (at >= all) {
+        at -= all;
+        q = seq_at<C::ROWS>(a, ++s);
+        all = a.c.hkv * q.before(q.tiles);
+      }
+      int lo = 0, hi = q.tiles - 1;                      // the last tile that begins at `at` or before
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (a.c.hkv * q.before(mid) <= at)
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      const int64_t length = q.a + q.b * lo, in = at - a.c.hkv * q.before(lo);
+      const int64_t h = in / length, place = in - h * length, end = place + left < length ? place + left : length;
+      u.s = s, u.h = (int)h, u.rt = lo;
+      u.rows = (int)min((int64_t)C::ROWS, (int64_t)q.ql * a.group - (int64_t)lo * C::ROWS);
+      const int64_t first_row = (int64_t)lo * C::ROWS / a.group, last_row = ((int64_t)lo * C::ROWS + u.rows - 1) / a.group;
+      u.p0 = q.len - q.ql;
+      const int64_t p_first = u.p0 + first_row, p_last = u.p0 + last_row;
+      const int64_t t1 = p_last + 1 < q.end ? p_last + 1 : q.end, t0 = a.window && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
+      u.t0 = t0, u.t1 = t1;
+      const int first = (int)(t0 / C::KT), steps = t1 > t0 ? (int)((t1 + C::KT - 1) / C::KT) - first : 0;
+      const int x0 = (int)(place * steps / length), x1 = (int)(end * steps / length);
+      u.j0 = first + x0, u.j1 = first + x1;
+      u.starts = x0 == 0;
+      u.whole = u.starts && x1 == steps;
+      u.nothing = steps == 0;
+      const bool cleared = u.nothing && place == 0;
+      // a unit's last piece may have no step (it lies in the last step's part of the line): its part is marked empty
+      const bool empty_part = x0 == x1 && x0 > 0;
+      at += end - place;
+      left -= end - place;
+      if (unit_end) *unit_end = to - left + (length - end);
+      if (x1 > x0 || cleared || empty_part) return true;
+    }
+    return false;
+  }
+};
+
+// ---- tensor memory
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
+  tmem_st16(taddr, v);
+  tmem_st16(taddr + 16, v + 16);
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Instruction descriptor of kind::f16: float16 operands, D float32, M = 128; A K-major, B K-major or (bit 16) MN-major.
+__host__ __device__ constexpr uint32_t idesc_f16(int n, bool b_mn) { return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
+// MN-major operand, 128-byte swizzle: a token a 128-byte row of 64 channels, 8 tokens 1 KiB apart, 64 channels `lbo` bytes.
+__device__ __forceinline__ uint64_t sdesc_mnmajor_sw128(uint32_t saddr, uint32_t lbo) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b),
+               "r"(idesc), "r"(accumulate)
+               : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b),
+               "r"(idesc), "r"(accumulate)
+               : "memory");
+}
+
+__device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The four pairs of a word's codes, times a scale.
+__device__ __forceinline__ void unpack8(uint32_t w, __half2 s, uint32_t (&r)[4]) {
+  asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %4; cvt.rn.f16x2.e2m1x2 %0, a; cvt.rn.f16x2.e2m1x2 %1, b; "
+      "cvt.rn.f16x2.e2m1x2 %2, c; cvt.rn.f16x2.e2m1x2 %3, d; }"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+      : "r"(w));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 v = __hmul2_rn(*reinterpret_cast<const __half2*>(&r[i]), s);
+    r[i] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+// 2^(byte - ref + 12) twice (byte <= ref), subnormal below 2^-14 and 0 below 2^-24.
+__device__ __forceinline__ __half2 half_scale(int byte, int ref) {
+  const int e = byte - ref + 27;
+  const uint32_t h = e > 0 ? (uint32_t)e << 10 : e > -10 ? 512u >> -e : 0u, two = h | h << 16;
+  return *reinterpret_cast<const __half2*>(&two);
+}
+
+// Two float32 operations at once.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t r;
+  asm("{ .reg .b64 x, y, z; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; mov.b64 z, {%5, %6}; fma.rn.f32x2 %0, x, y, z; }"
+      : "=l"(r)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  float2 o;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+  return o;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t r;
+  asm("{ .reg .b64 x, y; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; add.rn.f32x2 %0, x, y; }"
+      : "=l"(r)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  float2 o;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+  return o;
+}
+
+// A thread's row of keys or values (d = 256: half of one) to float16 operands: rows of 64 channels, 128 bytes each, 16-byte pieces at
+// piece ^ (row mod 8).  Quarters are taken in an order that differs from lane to lane, so that neither reads nor writes meet in banks.
+template <int NB, bool VALUES>
+__device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* tile, int tid, const __half2 (&scale)[NB < 4 ? NB : 4]) {
+  using C = Tc<NB>;
+  constexpr int kHere = NB < 4 ? NB : 4;                 // blocks of the row that are this thread's
+  const int row = NB == 8 ? tid >> 1 : tid, half = NB == 8 ? tid & 1 : 0;
+  const int turn = NB == 2 ? (row >> 2) & 3 : NB == 4 ? (row >> 1) & 3 : 0x78 >> (2 * (row & 3)) & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int p = i ^ turn;                              // the quarter: channels 8 p .. 8 p + 7 of every block
+    uint32_t w[kHere];
+    if constexpr (VALUES) {                              // halfwords [2][NB]
+      const uint8_t* at = raw + row * (16 * NB) + p * (4 * NB) + half * 8;
+      uint32_t lo[kHere / 2], hi[kHere / 2];
+      if constexpr (NB == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        lo[0] = v.x, hi[0] = v.y;
+      } else if constexpr (NB == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        lo[0] = v.x, lo[1] = v.y, hi[0] = v.z, hi[1] = v.w;
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(at), u = *reinterpret_cast<const uint2*>(at + 16);
+        lo[0] = v.x, lo[1] = v.y, hi[0] = u.x, hi[1] = u.y;
+      }
+#pragma unroll
+      for (int b = 0; b < kHere; b += 2) {
+        w[b] = __byte_perm(lo[b / 2], hi[b / 2], 0x5410);
+        w[b + 1] = __byte_perm(lo[b / 2], hi[b / 2], 0x7632);
+      }
+    } else {
+      const uint8_t* at = raw + row * (16 * NB) + p * (4 * NB) + half * 16;
+      if constexpr (NB == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        w[0] = v.x, w[1] = v.y;
+      } else {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < kHere; ++b) {
+      uint32_t r[4];
+      unpack8(w[b], scale[b], r);
+      const int block = half * 4 + b, piece = (block & 1) * 4 + p;
+      *reinterpret_cast<uint4*>(tile + (block >> 1) * (C::KT * 128) + row * 128 + ((piece ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+  }
+}
+
+template <int NB>
+__global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const __grid_constant__ AttnArgs a) {
+  using C = Tc<NB>;
+  constexpr int D = C::D, KT = C::KT, QT = C::QT, ROWS = C::ROWS, kHere = NB < 4 ? NB : 4;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Bars* bars = reinterpret_cast<Bars*>(smem + C::kOffBars);
+  volatile int* abort_flag = &bars->abort;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), cta = blockIdx.x, hkv = a.c.hkv;
+
+  if (tid == 0) {
+    for (int i = 0; i < 3; ++i) mbar_init(&bars->raw_full[i], 1), mbar_init(&bars->raw_empty[i], 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->k_full[i], 4), mbar_init(&bars->v_full[i], 4);
+      mbar_init(&bars->k_empty[i], 1), mbar_init(&bars->v_empty[i], 1);
+      mbar_init(&bars->s_full[i], 1), mbar_init(&bars->p_full[i], 4), mbar_init(&bars->pv_done[i], 1);
+    }
+    mbar_init(&bars->q_full, 4 * QT);
+    mbar_init(&bars->most_full, 4);
+    mbar_init(&bars->mma_done, 1);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  pdl_wait_then_release();
+
+  // ---- this CTA's piece of the line
+  const int per = (a.seqs + kThreads - 1) / kThreads, s_from = min(tid * per, a.seqs), s_to = min(s_from + per, a.seqs);
+  auto cost = [&](int s) {
+    const Seq q = seq_at<ROWS>(a, s);
+    return hkv * q.before(q.tiles);
+  };
+  int64_t mine = 0;
+  for (int s = s_from; s < s_to; ++s) mine += cost(s);
+  int64_t before = mine, total = 0;
+#pragma unroll
+  for (int k = 1; k < 32; k <<= 1) {
+    const int64_t v = __shfl_up_sync(0xFFFFFFFFu, before, k);
+    if (lane >= k) before += v;
+  }
+  if (lane == 31) bars->scan[warp] = before;
+  __syncthreads();
+  before -= mine;
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += bars->scan[w];
+    total += bars->scan[w];
+  }
+  int64_t ctas = (total + kLeastPiece - 1) / kLeastPiece;
+  if (ctas > gridDim.x) ctas = gridDim.x;
+  const int64_t each = ctas ? total / ctas : 0, rest = ctas ? total - each * ctas : 0;
+  auto cut = [&](int64_t k) { return each * k + (k < rest ? k : rest); };
+  const int64_t from = cut(cta), to = cut(cta + 1);
+  if (cta < ctas && mine > 0 && before <= from && from < before + mine) {
+    int64_t at = before;
+    for (int s = s_from; s < s_to; ++s) {
+      const int64_t c = cost(s);
+      if (from < at + c) {
+        bars->found_s = s;
+        bars->found_at = from - at;
+        break;
+      }
+      at += c;
+    }
+  }
+  if (a.clears) clear_rows<D>(a);
+  if (tid == 0) a.plan[cta].last = -1;
+  const bool works = cta < ctas;
+  if (warp == kMmaWarp && works) tmem_alloc(&bars->tmem_addr, kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (!works) return;
+  const uint32_t tmem = bars->tmem_addr;
+  Walk<NB> walk(a, bars->found_s, bars->found_at, from, to);
+  Unit u;
+  bool ok = true;
+  uint32_t jj = 0;                                       // steps so far
+#define CAT_WAIT(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort_flag, __LINE__)))
+
+  if (warp < 4 * QT) {
+    // ---------------------------------------------------------------- rows
+    const int tile = warp >> 2, r = tile * 128 + (warp & 3) * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + tile * KT, o_col = lanes + C::kO + tile * D;
+    int64_t unit_end;
+    uint32_t units = 0, tj = 0;                          // units and this tile's steps so far
+    while (ok && walk.next(u, &unit_end)) {
+      if (tid == 0 && u.starts && !u.whole) {
+        Plan p = {u.s, u.h, u.rt, 0};
+        const int64_t last = unit_end - 1;
+        p.last = (int)(last < rest * (each + 1) ? last / (each + 1) : rest + (last - rest * (each + 1)) / each);
+        a.plan[cta] = p;
+      }
+      const Seq& q = walk.q;
+      const int64_t rr = (int64_t)u.rt * ROWS + r;
+      const int j = (int)(rr / a.group);
+      const int64_t row = ((int64_t)(q.begin + j) * a.hq + u.h * a.group + (rr - (int64_t)j * a.group)) * D;
+      const bool real = r < u.rows;
+      const int slot = 2 * cta + (u.starts ? 1 : 0);
+      if (u.j0 == u.j1) {                                // no tokens: rows of zeros, or an empty part
+        if (real && u.nothing) {
+          for (int c = 0; c < D; c += 4) store4(a, row + c, make_float4(0.f, 0.f, 0.f, 0.f));
+        } else if (real) {
+          *reinterpret_cast<float2*>(a.ml + ((int64_t)slot * ROWS + r) * 2) = make_float2(-1e30f, 0.f);
+        }
+        continue;
+      }
+      // the row to float16, its largest channel in [2^13, 2^14); a negative scale goes into its sign
+      float fac;
+      {
+        const uint4* from_q = reinterpret_cast<const uint4*>(a.q + row);
+        uint32_t most = 0;
+        if (real)
+#pragma unroll 4
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 v = from_q[c];
+            const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+            most = max(most, max(m & 0xFFFFu, m >> 16));
+          }
+        const int e = max((int)(most >> 7), 1);
+        const float up = (e >= 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23)) * (a.scale < 0.f ? -1.f : 1.f);
+        auto half2_of = [&](uint32_t w) {
+          return e == 255 ? 0x7FFF7FFFu : f16_pair(__uint_as_float(w << 16) * up * 0x1p13f, __uint_as_float(w & 0xFFFF0000u) * up * 0x1p13f);
+        };
+        uint8_t* to_q = smem + tile * C::kQ + (r & 127) * 128;
+#pragma unroll 4
+        for (int c = 0; c < D / 8; ++c) {
+          const uint4 v = real ? from_q[c] : make_uint4(0u, 0u, 0u, 0u);
+          *reinterpret_cast<uint4*>(to_q + (c >> 3) * (128 * 128) + (((c & 7) ^ (r & 7)) << 4)) =
+              make_uint4(half2_of(v.x), half2_of(v.y), half2_of(v.z), half2_of(v.w));
+        }
+        fac = ldexpf(fabsf(a.scale), e - 140);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (elect_one()) mbar_arrive(&bars->q_full);
+      if (!CAT_WAIT(&bars->q_full, units & 1)) break;    // (nobody is at the next unit's queries before all are at this one's)
+      ++units;
+      const int64_t p = u.p0 + j;
+      const int lim = real ? (int)(p < q.end - 1 ? p : q.end - 1) : 0x7FFFFFFF;
+      const int low = real && a.window && p - a.window + 1 > 0 ? (int)(p - a.window + 1) : 0;
+      const bool tile_real = tile * 128 < u.rows, any_real = __any_sync(0xFFFFFFFFu, real);
+      float m = -1e30f;
+      float2 l2 = make_float2(0.f, 0.f);
+      int ref = 0;
+      uint32_t nan_blocks = 0;
+      for (int step = u.j0; step < u.j1; ++step, ++jj) {
+        if (!tile_real) continue;
+        const int b = jj & 1;
+        const float* k_factor = bars->k_factor[jj & 3];
+        if (!CAT_WAIT(&bars->s_full[tile], tj & 1)) break;
+        if (!CAT_WAIT(&bars->v_full[b], (jj >> 1) & 1)) break;       // (the values' reference)
+        tc_fence_after();
+        if (any_real) {
+          const int t0 = step * KT;
+          const uint32_t there = bars->there[jj & 3];
+          constexpr uint32_t kAll = (1u << (KT / 16)) - 1u;
+          const bool full = __all_sync(0xFFFFFFFFu, t0 + KT - 1 <= lim && t0 >= low) && there == kAll;
+          // ---- the step's largest score
+          float top = -1e30f;
+#pragma unroll
+          for (int c = 0; c < KT / 32; ++c) {
+            uint32_t v[32];
+            CAT_TMEM_LD32(s_col + 32 * c, v);
+            const float f0 = fac * k_factor[KT == 64 ? 2 * c : c], f1 = fac * k_factor[KT == 64 ? 2 * c + 1 : c];
+            tmem_ld_wait();
+            if (!full) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const int at = t0 + 32 * c + i;
+                if (at > lim || at < low || !(there >> (2 * c + i / 16) & 1)) v[i] = 0xFF800000u;
+              }
+            }
+            float m0 = __uint_as_float(v[0]), m1 = __uint_as_float(v[16]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) {
+              m0 = fmaxf(m0, __uint_as_float(v[i]));
+              m1 = fmaxf(m1, __uint_as_float(v[16 + i]));
+            }
+            // (of factors that are 0, an infinity of what is not seen makes NaN, which is not the larger)
+            top = fmaxf(top, fmaxf(m0 * f0, m1 * f1));
+          }
+          const int now = bars->v_ref[b];
+          const bool first = step == u.j0;
+          if (__any_sync(0xFFFFFFFFu, first || top > m + kSlack || now != ref)) {
+            const float up = top > m + kSlack || first ? fmaxf(top, m) : m;
+            const float by = ex2(m - up);
+            m = up;
+            l2.x *= by, l2.y *= by;
+            if (!first) {
+              if (!CAT_WAIT(&bars->pv_done[tile], (tj - 1) & 1)) break;
+              tc_fence_after();
+              const float scale_o = by * ex2((float)(ref - now));
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                uint32_t v[32];
+                CAT_TMEM_LD32(o_col + c, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * scale_o);
+                tmem_st32(o_col + c, v);
+              }
+            }
+            ref = now;
+          }
+          if (bars->v_odd[b][0] | bars->v_odd[b][1] | bars->v_odd[b][2] | bars->v_odd[b][3])
+            for (int i = 0; i < KT; ++i) {
+              const int at = t0 + i;
+              if (at <= lim && at >= low) nan_blocks |= bars->v_nan[b][i];
+            }
+          // ---- weights, times 2^8
+          const float2 base = make_float2(8.f - m, 8.f - m);
+#pragma unroll
+          for (int c = 0; c < KT / 32; ++c) {
+            uint32_t v[32], w[16];
+            CAT_TMEM_LD32(s_col + 32 * c, v);
+            const float f0 = fac * k_factor[KT == 64 ? 2 * c : c], f1 = fac * k_factor[KT == 64 ? 2 * c + 1 : c];
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const float f = i < 16 ? f0 : f1;
+              float2 x = fma2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(f, f), base);
+              if (!full) {
+                const int at = t0 + 32 * c + i;
+                const bool on = there >> (2 * c + i / 16) & 1;
+                if (at > lim || at < low || !on) x.x = __int_as_float(0xFF800000);
+                if (at + 1 > lim || at + 1 < low || !on) x.y = __int_as_float(0xFF800000);
+              }
+              x.x = ex2(x.x), x.y = ex2(x.y);
+              l2 = add2(l2, x);
+              w[i / 2] = f16_pair(x.x, x.y);
+            }
+            tmem_st16(s_col + 16 * c, w);
+          }
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&bars->p_full[tile]);
+        ++tj;
+      }
+      if (!ok) break;
+      if (!tile_real) continue;
+      // ---- out
+      if (!CAT_WAIT(&bars->pv_done[tile], (tj - 1) & 1)) break;
+      tc_fence_after();
+      if (any_real) {
+        const float l = l2.x + l2.y;
+        float unref = ldexpf(1.f, ref - 139);
+        if (u.whole) unref = l == 0.f ? 0.f : ldexpf(1.f / l, ref - 139);
+        float* part = a.parts + ((int64_t)slot * ROWS + r) * D;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t v[32];
+          CAT_TMEM_LD32(o_col + c, v);
+          tmem_ld_wait();
+          const bool nan = nan_blocks >> (c / 32) & 1;
+          if (real)
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              float4 o = make_float4(__uint_as_float(v[i]) * unref, __uint_as_float(v[i + 1]) * unref, __uint_as_float(v[i + 2]) * unref,
+                                     __uint_as_float(v[i + 3]) * unref);
+              if (nan) o.x = o.y = o.z = o.w = __int_as_float(0x7FFFFFFF);
+              if (u.whole)
+                store4(a, row + c + i, o);
+              else
+                *reinterpret_cast<float4*>(part + c + i) = o;
+            }
+        }
+        if (real && !u.whole) *reinterpret_cast<float2*>(a.ml + ((int64_t)slot * ROWS + r) * 2) = make_float2(m, l);
+      }
+      tc_fence_before();
+    }
+  } else if (warp >= kKeyWarp0 && warp < kMmaWarp) {
+    // ---------------------------------------------------------------- keys and values to float16
+    const bool values = warp >= kValueWarp0;
+    const int w = (warp - kKeyWarp0) & 3, t = w * 32 + lane, row = NB == 8 ? t >> 1 : t, first_block = NB == 8 ? (t & 1) * 4 : 0;
+    int ref = kLowR;
+    while (ok && walk.next(u)) {
+      if (values) ref = kLowR;                           // (O begins anew)
+      for (int step = u.j0; step < u.j1; ++step, ++jj) {
+        const uint32_t e = 2 * jj + (values ? 1 : 0), st = e % 3, b = jj & 1;
+        if (!CAT_WAIT(&bars->raw_full[st], (e / 3) & 1)) break;
+        const uint8_t* raw = smem + C::kOffRaw + st * C::kRaw;
+        const uint32_t there = bars->raw_there[st];
+        const int64_t token = (int64_t)step * KT + row;
+        const bool on = (there >> (row / 16) & 1) && token >= u.t0 && token < u.t1;      // (what no row sees is zeros, and no reference)
+        int bytes[kHere];
+        uint32_t most = 0, nan = 0;
+#pragma unroll
+        for (int i = 0; i < kHere; ++i) {
+          bytes[i] = on ? raw[C::kCodes + row * NB + first_block + i] : 0;
+          if (bytes[i] == 255)
+            nan |= 1u << (first_block + i);
+          else
+            most = max(most, (uint32_t)bytes[i]);
+        }
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        __half2 scale[kHere];
+        if (values) {
+          if (lane == 0) {
+            bars->v_most[b][w] = most;
+            mbar_arrive(&bars->most_full);
+          }
+          if (!CAT_WAIT(&bars->most_full, jj & 1)) break;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ref = max(ref, (int)bars->v_most[b][i]);
+          if (jj >= 2 && !CAT_WAIT(&bars->v_empty[b], ((jj >> 1) - 1) & 1)) break;
+          const bool odd = __any_sync(0xFFFFFFFFu, nan != 0);
+          if (NB == 8) nan |= __shfl_xor_sync(0xFFFFFFFFu, nan, 1);
+          bars->v_nan[b][row] = (uint8_t)nan;
+          if (lane == 0) bars->v_odd[b][w] = odd;
+          if (t == 0) bars->v_ref[b] = ref;
+#pragma unroll
+          for (int i = 0; i < kHere; ++i) scale[i] = on && bytes[i] != 255 ? half_scale(bytes[i], ref) : half_scale(-1000, 0);
+          unpack_row<NB, true>(raw, smem + C::kOffV + b * C::kTile, t, scale);
+        } else {
+          const int kref = max((int)most, kLowR);
+          if (jj >= 2 && !CAT_WAIT(&bars->k_empty[b], ((jj >> 1) - 1) & 1)) break;
+#pragma unroll
+          for (int i = 0; i < kHere; ++i) {
+            scale[i] = on ? half_scale(bytes[i], kref) : half_scale(-1000, 0);
+            if (bytes[i] == 255) scale[i] = __half2half2(__ushort_as_half(0x7FFF));
+          }
+          if (lane == 0) bars->k_factor[jj & 3][w] = __uint_as_float((uint32_t)(kref - 12) << 23);
+          if (t == 0) bars->there[jj & 3] = there;
+          unpack_row<NB, false>(raw, smem + C::kOffK + b * C::kTile, t, scale);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (elect_one()) {
+          mbar_arrive(&bars->raw_empty[st]);
+          mbar_arrive(values ? &bars->v_full[b] : &bars->k_full[b]);
+        }
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ---------------------------------------------------------------- MMAs
+    constexpr uint32_t kScores = idesc_f16(KT, false), kOut = idesc_f16(D, true);
+    uint32_t units = 0, tj[2] = {0, 0};
+    auto scores = [&](int tile, uint32_t j) {
+      const uint32_t qb = smem_u32(smem + tile * C::kQ), kb = smem_u32(smem + C::kOffK + (j & 1) * C::kTile);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+        mma_ss(tmem + tile * KT, sdesc_kmajor_sw128(qb + (kk >> 2) * (128 * 128) + (kk & 3) * 32),
+               sdesc_kmajor_sw128(kb + (kk >> 2) * (KT * 128) + (kk & 3) * 32), kScores, kk != 0);
+      mma_commit(&bars->s_full[tile]);
+    };
+    while (ok && walk.next(u)) {
+      if (u.j0 == u.j1) continue;
+      const int tiles = u.rows > 128 ? 2 : 1;
+      if (!CAT_WAIT(&bars->q_full, units & 1)) break;
+      ++units;
+      if (!CAT_WAIT(&bars->k_full[jj & 1], (jj >> 1) & 1)) break;
+      tc_fence_after();
+      if (elect_one()) {
+        for (int tile = 0; tile < tiles; ++tile) scores(tile, jj);
+        mma_commit(&bars->k_empty[jj & 1]);
+      }
+      __syncwarp();
+      for (int step = u.j0; step < u.j1 && ok; ++step, ++jj) {
+        const bool more = step + 1 < u.j1;
+        for (int tile = 0; tile < tiles; ++tile) {
+          if (tile == 0 && !CAT_WAIT(&bars->v_full[jj & 1], (jj >> 1) & 1)) break;
+          if (!CAT_WAIT(&bars->p_full[tile], tj[tile] & 1)) break;
+          ++tj[tile];
+          if (tile == 0 && more && !CAT_WAIT(&bars->k_full[(jj + 1) & 1], ((jj + 1) >> 1) & 1)) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t vb = smem_u32(smem + C::kOffV + (jj & 1) * C::kTile);
+#pragma unroll
+            for (int kk = 0; kk < KT / 16; ++kk)
+              mma_ts(tmem + C::kO + tile * D, tmem + tile * KT + kk * 8, sdesc_mnmajor_sw128(vb + kk * 2048, KT * 128), kOut,
+                     step > u.j0 || kk != 0);
+            mma_commit(&bars->pv_done[tile]);
+            if (tile == tiles - 1) mma_commit(&bars->v_empty[jj & 1]);
+            if (more) {
+              scores(tile, jj + 1);
+              if (tile == tiles - 1) mma_commit(&bars->k_empty[(jj + 1) & 1]);
+            }
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (elect_one()) mma_commit(&bars->mma_done);
+    __syncwarp();
+    volatile int none = 0;
+    mbar_wait_bounded(&bars->mma_done, 0, &none);        // (nothing is on its way to tensor memory any more)
+  } else if (warp == kLoadWarp) {
+    // ---------------------------------------------------------------- copies
+    const int most = a.c.page < KT ? a.c.page : KT, copies = KT / most;      // tokens a copy; copies a step, a lane each
+    uint32_t e = 0;
+    while (ok && walk.next(u)) {
+      const int32_t* pages = a.table + (int64_t)u.s * a.width;
+      const uint8_t* head = a.c.base + (int64_t)u.h * a.c.part;
+      for (int step = u.j0; step < u.j1 && ok; ++step, ++jj) {
+        const int t0 = step * KT + lane * most;
+        int64_t pg = -1;
+        if (lane < copies && t0 < walk.q.end) pg = __ldg(pages + (t0 >> a.c.page_log));
+        if (pg >= a.pages) pg = -1;
+        const uint32_t have = __ballot_sync(0xFFFFFFFFu, pg >= 0);
+        uint32_t groups = 0;                             // of 16 tokens
+        for (int i = 0; i < copies; ++i)
+          if (have >> i & 1) groups |= ((1u << (most / 16)) - 1u) << (i * (most / 16));
+        for (int kind = 0; kind < 2; ++kind, ++e) {
+          const uint32_t st = e % 3;
+          if (e >= 3 && !CAT_WAIT(&bars->raw_empty[st], (e / 3 - 1) & 1)) break;
+          uint8_t* raw = smem + C::kOffRaw + st * C::kRaw;
+          if (lane == 0) {
+            bars->raw_there[st] = groups;
+            mbar_arrive_expect_tx(&bars->raw_full[st], (uint32_t)(__popc(have) * most * 17 * NB));
+          }
+          __syncwarp();
+          if (pg >= 0) {
+            const uint8_t* part = head + (pg * 2 + kind) * a.c.hkv * a.c.part;
+            const int r = t0 & (a.c.page - 1), o = lane * most;
+            bulk_load(raw + o * (16 * NB), part + r * (16 * NB), most * 16 * NB, &bars->raw_full[st]);
+            bulk_load(raw + C::kCodes + o * NB, part + (a.c.page * 16 + r) * NB, most * NB, &bars->raw_full[st]);
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (!ok) {                                           // the copies still on their way
+      volatile int none = 0;
+      for (uint32_t i = e > 3 ? e - 3 : 0; i < e; ++i) mbar_wait_bounded(&bars->raw_full[i % 3], (i / 3) & 1, &none);
+    }
+  }
+#undef CAT_WAIT
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
+  if (tid == 0 && bars->abort) report(a.status, timeout_bits(kWhereMxAttention, bars->abort));
+}
+
+template <int NB>
+cudaError_t run(const AttnArgs& a, int grid, cudaStream_t stream) {
+  static PerDevice<cudaError_t> allowed;
+  constexpr int kSmem = Tc<NB>::kSmem < 120 * 1024 ? 120 * 1024 : Tc<NB>::kSmem;       // (one CTA an SM: tensor memory)
+  cudaError_t e = allowed.get([] { return allow_smem(mx_attention_tiles_kernel<NB>, kSmem); });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = pdl_attr();
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  note_launch();
+  if ((e = cudaLaunchKernelEx(&cfg, mx_attention_tiles_kernel<NB>, a)) != cudaSuccess) return e;
+  return launch_join<32 * NB, Tc<NB>::ROWS>(a, grid, stream);
+}
+
+}  // namespace
+
+int attention_tile_rows(int64_t d) { return d == 256 ? Tc<8>::ROWS : Tc<4>::ROWS; }
+
+cudaError_t launch_attention_tiles(const AttnArgs& a, int64_t d, int grid, cudaStream_t stream) {
+  return d == 64 ? run<2>(a, grid, stream) : d == 128 ? run<4>(a, grid, stream) : run<8>(a, grid, stream);
+}
+
+}  // namespace cat

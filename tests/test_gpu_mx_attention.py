@@ -33,7 +33,7 @@ def host(t):
 class Batch:
     """Sequences of `lens` tokens with `rows` queries each in a cache of poisoned pages (every scale NaN where no token is)."""
 
-    def __init__(self, seed, lens, rows, hq, hkv, d, page, spare=3, size=1.0):
+    def __init__(self, seed, lens, rows, hq, hkv, d, page, spare=3, size=1.0, fill=0xFF):
         rng = np.random.default_rng(seed)
         self.rng, self.d, self.page, self.hq, self.hkv = rng, d, page, hq, hkv
         self.lens, self.rows = np.array(lens, dtype=np.int32), np.array(rows)
@@ -46,7 +46,7 @@ class Batch:
         for s, c in enumerate(count):
             self.table[s, :c] = order[at:at + c]
             at += c
-        self.cache = dev(C.blank(pages, hkv, page, d, 0xFF))
+        self.cache = dev(C.blank(pages, hkv, page, d, fill))
         slots = np.concatenate([self.table[s, np.arange(n) // page] * page + np.arange(n) % page for s, n in enumerate(lens) if n > 0]
                                + [np.zeros(0, dtype=np.int64)]).astype(np.int32)
         k = rng.standard_normal((len(slots), hkv, d)) * (1 + 7 * (np.arange(d) < 2)) * size
@@ -114,6 +114,43 @@ def test_prompts(hq, hkv, d, q, length, window):
     b = Batch(q, [length], [q], hq, hkv, d, 64)
     b.check(b.run(window=window), window=window)
     b.check(b.run(window=window, out_dtype=torch.float32), window=window)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("hq,hkv,page,lens,rows,window", [
+    (4, 1, 64, [1000, 0, 333, 64, 2000], [500, 3, 333, 40, 1], 0), (40, 1, 16, [200, 90, 17], [1, 1, 1], 0), (3, 3, 128, [700, 650], [700, 128], 100),
+    (16, 2, 1024, [3000], [70], 0), (5, 1, 32, [400, 30], [257, 60], 0), (17, 1, 16, [5, 300], [9, 2], 33), (8, 2, 64, [129, 127, 128], [129, 127, 64], 0)])
+def test_tiles(hq, hkv, page, lens, rows, window, d):
+    """Sequences of many rows beside others: whole tiles and parts of them, rows that see nothing, groups that no tile's rows divide."""
+    b = Batch(d + hq, lens, rows, hq, hkv, d, page)
+    got = b.run(window=window)
+    b.check(got, window=window)
+    assert torch.equal(got, b.run(window=window))
+    b.check(b.run(window=window, out_dtype=torch.float32), window=window)
+    assert cat.cat_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 20.0])
+def test_tiles_scales_and_sizes(scale):
+    b = Batch(19, [500, 90], [200, 90], 4, 2, 128, 32)
+    b.check(b.run(scale=scale), scale=scale)
+    n = 500
+    for up in (1, -1):
+        v = b.rng.standard_normal((n, 2, 128)) * np.exp2(up * np.linspace(-20, 20, n))[:, None, None]
+        v[:, :, 32:64] *= 2.0 ** -12
+        k = b.rng.standard_normal((n, 2, 128)) * np.exp2(2 * np.sin(np.arange(n)))[:, None, None]
+        slots = b.table[0, np.arange(n) // 32] * 32 + np.arange(n) % 32
+        cat.cat_mx_cache_write(dev(k, torch.float32), dev(v, torch.float32), dev(slots.astype(np.int32)), b.cache)
+        b.check(b.run(scale=scale / 4), scale=scale / 4)
+
+
+def test_tiles_of_a_long_sequence():
+    """Units cut into parts, and pages that are none."""
+    b = Batch(21, [20000, 300], [70, 2], 8, 1, 128, 64)
+    b.table[0, 7], b.table[0, 150] = -1, 10 ** 6
+    got = b.run()
+    b.check(got)
+    assert torch.equal(got, b.run())
 
 
 def test_many_sequences():
@@ -212,6 +249,44 @@ def test_nan_of_tokens_that_are_not_seen():
     g = host(b.run(window=30))
     assert np.isfinite(g[:4]).all() and np.isnan(g[4:, 2:, 32:64]).all()
     assert np.isfinite(g[4:, :2]).all() and np.isfinite(g[4:, 2:, :32]).all() and np.isfinite(g[4:, 2:, 64:]).all()
+
+
+@pytest.mark.parametrize("rows", [[1, 1, 3], [40, 20, 33]])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_what_is_not_seen_may_be_anything(d, rows):
+    """Cache rows behind the lengths of the largest finite scales and codes; tokens behind the window of the largest values."""
+    b = Batch(17, [90, 40, 150], rows, 8, 2, d, 64, fill=0xFD)
+    b.check(b.run())
+    k = np.full((30, 2, d), 2.0 ** 120)
+    slots = (b.table[2, np.arange(30) // 64] * 64 + np.arange(30) % 64).astype(np.int32)
+    cat.cat_mx_cache_write(dev(k, torch.float32), dev(k, torch.float32), dev(slots), b.cache)
+    b.check(b.run(window=80), window=80)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_nan_of_tokens_that_a_prompts_rows_do_not_see(d):
+    b = Batch(18, [300, 70], [200, 70], 4, 2, d, 32)
+    t = np.array([20, 230])                                        # behind the windows of all; seen from row 130 on, to row 159
+    slots = (b.table[0, t // 32] * 32 + t % 32).astype(np.int32)
+    k, v = b.rng.standard_normal((2, 2, d)), np.ones((2, 2, d))
+    v[:, 1, 40] = np.inf
+    cat.cat_mx_cache_write(dev(k, torch.float32), dev(v, torch.float32), dev(slots), b.cache)
+    cat.cat_device_status()
+    want = C.attention(host(b.q), host(b.cache), b.page, b.table, b.lens, d ** -0.5, b.offsets, 30)
+    tol = C.tolerance(*want, d, True)
+    g = host(b.run(window=30))
+    odd = np.zeros(g.shape, dtype=bool)
+    odd[130:160, 2:, 32:64] = True
+    assert np.isnan(g[odd]).all() and np.isfinite(g[~odd]).all()
+    assert np.all(np.abs(g - want[0])[~odd] <= tol[~odd])
+    bad = np.full((2, 2, d), np.nan)                               # keys too
+    cat.cat_mx_cache_write(dev(bad, torch.float32), dev(v, torch.float32), dev(slots), b.cache)
+    cat.cat_device_status()
+    g = host(b.run(window=30))
+    odd[:] = False
+    odd[130:160] = True
+    assert np.isnan(g[odd]).all() and np.isfinite(g[~odd]).all()
+    assert np.all(np.abs(g - want[0])[~odd] <= tol[~odd])
 
 
 def test_queries_that_are_not_finite():
