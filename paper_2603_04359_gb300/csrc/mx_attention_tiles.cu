@@ -8,15 +8,18 @@
 // of the largest block, and to 2^-36 with fewer bits.  A step's unpacking is shared by 256 rows (two tiles of 128; d = 256: one):
 // queries of a key head's group lie together, row r is head r % group of token r / group.
 //
-// Per step of 128 tokens at d = 128 the MMAs take 2048 cycles of an SM, the exponentials of 2 x 16384 scores 1024, the
-// unpacking ~400 issue slots a scheduler: so what bounds it are the MMAs, if the others keep out of their way.
+// Per step of 64 tokens at d = 128 the MMAs take 1024 cycles of an SM, the exponentials of 2 x 8192 scores 512, the
+// unpacking ~200 issue slots a scheduler: what bounds it are the MMAs, if the others keep out of their way.  So scores have two
+// buffers a tile, and the next ones are there when a step's weights are done (with one buffer and steps of 128 tokens a tile's
+// weights, its two products and what lies between were one after the other: 5400 cycles a step for 2048 of MMAs).
 //
 // Warps (576 threads, one CTA an SM):
 //   0..3, 4..7   a tile's rows each, one a thread: scores from tensor memory, weights back to it (over the scores; the A operand of P V
 //                is read there), the running maximum and sum, O's correction where the maximum grows by more than 2^6, output
-//   8..11        keys to float16, 12..15 values: a token's row a thread (d = 256: half of one)
-//   16           issues the MMAs: P V of a tile, then the tile's next scores, the other tile's behind them
-//   17           bulk copies of the codes as they are, a ring of three
+//   8..11        keys to float16, 12..15 values: half of a token's row a thread
+//   16           issues the MMAs: P V of a tile, behind it the scores of the tile's step after the next, in the weights' place
+//   17           bulk copies of the codes as they are, a ring each of keys and values (one for both let values that wait for room keep
+//                keys back)
 // MMAs of one thread are carried out in the order of their issue, so next scores may follow the product that reads the weights
 // in their place.  Every wait is bounded; one that gives up raises the device status word and all roles drain and leave.
 //
@@ -31,38 +34,25 @@ namespace cat {
 namespace {
 
 constexpr int kThreads = 576;
+constexpr int KT = 64;                      // tokens a step
 constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kUnitCost = 384;              // a unit's beginning and end, in tokens
 constexpr int kLeastPiece = 1024;           // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
 constexpr uint32_t kTmemCols = 512;
+constexpr int kBarRoom = 6144;
 
 template <int NB>
 struct Tc {
-  static constexpr int D = 32 * NB, QT = NB == 8 ? 1 : 2, KT = NB == 8 ? 64 : 128, ROWS = 128 * QT;
-  static constexpr int kQ = 128 * D * 2, kTile = KT * D * 2, kCodes = KT * 16 * NB, kRaw = kCodes + KT * NB, kRing = 3;
-  static constexpr int kOffK = QT * kQ, kOffV = kOffK + 2 * kTile, kOffRaw = kOffV + 2 * kTile, kOffBars = kOffRaw + kRing * kRaw;
-  static constexpr int kSmem = 1024 + kOffBars + 2048;
-  static constexpr uint32_t kO = QT * KT;                // tensor memory: a tile's scores, then O's
-  static_assert(kSmem <= 227 * 1024 && QT * (KT + D) <= (int)kTmemCols, "");
+  static constexpr int D = 32 * NB, QT = NB == 8 ? 1 : 2, ROWS = 128 * QT;
+  static constexpr int kBufs = NB == 8 ? 2 : 4, kBufLog = NB == 8 ? 1 : 2;     // of unpacked keys, and of values
+  static constexpr int kQ = 128 * D * 2, kTile = KT * D * 2, kCodes = KT * 16 * NB, kRaw = kCodes + KT * NB;
+  static constexpr int kRingK = NB == 8 ? 2 : 3, kRingV = NB == 8 ? 1 : 3, kRing = kRingK + kRingV;      // codes as they are: of keys, of values
+  static constexpr int kOffK = QT * kQ, kOffV = kOffK + kBufs * kTile, kOffRaw = kOffV + kBufs * kTile, kOffBars = kOffRaw + kRing * kRaw;
+  static constexpr int kSmem = 1024 + kOffBars + kBarRoom;
+  static constexpr uint32_t kO = QT * 2 * KT;            // tensor memory: two buffers of scores a tile, then O's
+  static_assert(kSmem <= 227 * 1024 && QT * (2 * KT + D) <= (int)kTmemCols, "");
 };
-
-struct Bars {
-  uint64_t raw_full[3], raw_empty[3], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full, s_full[2], p_full[2], pv_done[2], most_full, mma_done;
-  // (of four steps: keys are unpacked two steps ahead of scores that are still read)
-  float k_factor[4][4];                     // 2^(ref - 139) of a warp's tokens' keys
-  uint32_t there[4];                        // which 16-token groups of a step are on pages
-  uint32_t raw_there[3];
-  int v_ref[2];                             // the values' reference
-  uint32_t v_odd[2][4];                     // whether a scale of a warp's tokens is NaN
-  uint32_t v_most[2][4];                    // their largest
-  uint8_t v_nan[2][128];                    // a token's blocks of NaN scales
-  int64_t scan[kThreads / 32];
-  int64_t found_at;
-  int found_s, abort;
-  uint32_t tmem_addr;
-};
-static_assert(sizeof(Bars) <= 2048, "barrier room");
 
 struct Seq : Rows {
   int tiles;
@@ -85,24 +75,37 @@ __device__ __forceinline__ Seq seq_at(const AttnArgs& a, int s) {
   return q;
 }
 
-// A CTA's way along its piece, the same in all warps.
+// A CTA's way along its piece, the same in all warps; each keeps its own in shared memory (registers are short).
 struct Unit {
   int s, h, rt, rows, j0, j1;               // the steps of KT tokens, from the sequence's beginning
   bool starts, whole, nothing;              // nothing: no row sees a token
   int64_t p0;                               // the token of the sequence's first row
   int64_t t0, t1;                           // the tokens that some row sees
+  int64_t end;                              // where the unit ends on the line
 };
-template <int NB>
 struct Walk {
-  using C = Tc<NB>;
-  const AttnArgs& a;
   int s;
   int64_t at, left, to;
   Seq q;
-  __device__ __forceinline__ Walk(const AttnArgs& args, int s_, int64_t at_, int64_t from, int64_t to_)
-      : a(args), s(s_), at(at_), left(to_ - from), to(to_), q(seq_at<C::ROWS>(args, s_)) {}
-  // The next unit with something to do; place and length on the line by `end` (where the unit ends) for who plans
-  __device__ __forceinline__ bool next(Unit& u, int64_t* unit_end = nullptr) {
+  Unit u;
+  template <int NB>
+  __device__ __forceinline__ void begin(const AttnArgs& a, int s_, int64_t at_, int64_t from, int64_t to_) {
+    s = s_, at = at_, left = to_ - from, to = to_;
+    q = seq_at<Tc<NB>::ROWS>(a, s_);
+  }
+  // A whole warp: the next unit with something to do.
+  template <int NB>
+  __device__ __forceinline__ bool next(const AttnArgs& a) {
+    __syncwarp();                                        // (all lanes are done with the unit before)
+    bool more = false;
+    if ((threadIdx.x & 31) == 0) more = advance<NB>(a);
+    more = __shfl_sync(0xFFFFFFFFu, more, 0);
+    __syncwarp();
+    return more;
+  }
+  template <int NB>
+  __device__ __forceinline__ bool advance(const AttnArgs& a) {
+    using C = Tc<NB>;
     while (left > 0) {
       int64_t all = a.c.hkv * q.before(q.tiles);
       while (at >= all) {
@@ -127,7 +130,7 @@ struct Walk {
       const int64_t p_first = u.p0 + first_row, p_last = u.p0 + last_row;
       const int64_t t1 = p_last + 1 < q.end ? p_last + 1 : q.end, t0 = a.window && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
       u.t0 = t0, u.t1 = t1;
-      const int first = (int)(t0 / C::KT), steps = t1 > t0 ? (int)((t1 + C::KT - 1) / C::KT) - first : 0;
+      const int first = (int)(t0 / KT), steps = t1 > t0 ? (int)((t1 + KT - 1) / KT) - first : 0;
       const int x0 = (int)(place * steps / length), x1 = (int)(end * steps / length);
       u.j0 = first + x0, u.j1 = first + x1;
       u.starts = x0 == 0;
@@ -138,12 +141,30 @@ struct Walk {
       const bool empty_part = x0 == x1 && x0 > 0;
       at += end - place;
       left -= end - place;
-      if (unit_end) *unit_end = to - left + (length - end);
+      u.end = to - left + (length - end);
       if (x1 > x0 || cleared || empty_part) return true;
     }
     return false;
   }
 };
+
+struct Bars {
+  uint64_t raw_full[6], raw_empty[6], k_full[4], k_empty[4], v_full[4], v_empty[4], q_full, s_full[2][2], p_full[2][2], pv_done[2][2], most_full,
+      mma_done;
+  // (of eight steps: keys are unpacked up to five steps ahead of scores that are still read)
+  float k_factor[8][2];                     // 2^(ref - 139) of 32 tokens' keys
+  uint32_t there[8];                        // which 16-token groups of a step are on pages
+  uint32_t raw_there[6];
+  uint32_t v_ref[4];                        // the values' reference, + 256 where a scale of the step's is NaN
+  uint32_t v_most[2][4];                    // the same of a warp's tokens
+  uint8_t v_nan[4][2][KT];                  // a token's blocks of NaN scales (d = 256: those of half of them)
+  int64_t scan[20];
+  int64_t found_at;
+  int found_s, abort;
+  uint32_t tmem_addr;
+  Walk walks[20];
+};
+static_assert(sizeof(Bars) <= kBarRoom, "barrier room");
 
 // ---- tensor memory
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
@@ -215,20 +236,19 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return o;
 }
 
-// A thread's row of keys or values (d = 256: half of one) to float16 operands: rows of 64 channels, 128 bytes each, 16-byte pieces at
-// piece ^ (row mod 8).  Quarters are taken in an order that differs from lane to lane, so that neither reads nor writes meet in banks.
+// Half of a token's row of keys or values to float16 operands: two quarters of it (d = 256: half of the blocks).  Operands are rows of
+// 64 channels, 128 bytes each, 16-byte pieces at piece ^ (row mod 8).  Quarters are taken in an order that differs from lane to lane, so that
+// writes never meet in a bank and reads in pairs at most.
 template <int NB, bool VALUES>
-__device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* tile, int tid, const __half2 (&scale)[NB < 4 ? NB : 4]) {
-  using C = Tc<NB>;
-  constexpr int kHere = NB < 4 ? NB : 4;                 // blocks of the row that are this thread's
-  const int row = NB == 8 ? tid >> 1 : tid, half = NB == 8 ? tid & 1 : 0;
-  const int turn = NB == 2 ? (row >> 2) & 3 : NB == 4 ? (row >> 1) & 3 : 0x78 >> (2 * (row & 3)) & 3;
+__device__ __forceinline__ void unpack_half(const uint8_t* raw, uint8_t* tile, int row, int half, const __half2 (&scale)[NB < 4 ? NB : 4]) {
+  constexpr int kHere = NB < 4 ? NB : 4, kQuarters = NB == 8 ? 4 : 2;
+  const int block0 = NB == 8 ? 4 * half : 0, turn = NB == 2 ? (row >> 2) & 1 : NB == 4 ? (row >> 1) & 1 : (row >> 1) & 3;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int p = i ^ turn;                              // the quarter: channels 8 p .. 8 p + 7 of every block
+  for (int i = 0; i < kQuarters; ++i) {
+    const int p = NB == 8 ? i ^ turn : 2 * half + (i ^ turn);          // the quarter: channels 8 p .. 8 p + 7 of every block
+    const uint8_t* at = raw + row * (16 * NB) + p * (4 * NB);
     uint32_t w[kHere];
     if constexpr (VALUES) {                              // halfwords [2][NB]
-      const uint8_t* at = raw + row * (16 * NB) + p * (4 * NB) + half * 8;
       uint32_t lo[kHere / 2], hi[kHere / 2];
       if constexpr (NB == 2) {
         const uint2 v = *reinterpret_cast<const uint2*>(at);
@@ -237,7 +257,7 @@ __device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* tile, in
         const uint4 v = *reinterpret_cast<const uint4*>(at);
         lo[0] = v.x, lo[1] = v.y, hi[0] = v.z, hi[1] = v.w;
       } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(at), u = *reinterpret_cast<const uint2*>(at + 16);
+        const uint2 v = *reinterpret_cast<const uint2*>(at + 8 * half), u = *reinterpret_cast<const uint2*>(at + 8 * half + 16);
         lo[0] = v.x, lo[1] = v.y, hi[0] = u.x, hi[1] = u.y;
       }
 #pragma unroll
@@ -245,30 +265,86 @@ __device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* tile, in
         w[b] = __byte_perm(lo[b / 2], hi[b / 2], 0x5410);
         w[b + 1] = __byte_perm(lo[b / 2], hi[b / 2], 0x7632);
       }
+    } else if constexpr (NB == 2) {
+      const uint2 v = *reinterpret_cast<const uint2*>(at);
+      w[0] = v.x, w[1] = v.y;
     } else {
-      const uint8_t* at = raw + row * (16 * NB) + p * (4 * NB) + half * 16;
-      if constexpr (NB == 2) {
-        const uint2 v = *reinterpret_cast<const uint2*>(at);
-        w[0] = v.x, w[1] = v.y;
-      } else {
-        const uint4 v = *reinterpret_cast<const uint4*>(at);
-        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-      }
+      const uint4 v = *reinterpret_cast<const uint4*>(at + (NB == 8 ? 16 * half : 0));
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
     }
 #pragma unroll
     for (int b = 0; b < kHere; ++b) {
       uint32_t r[4];
       unpack8(w[b], scale[b], r);
-      const int block = half * 4 + b, piece = (block & 1) * 4 + p;
-      *reinterpret_cast<uint4*>(tile + (block >> 1) * (C::KT * 128) + row * 128 + ((piece ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
+      const int block = block0 + b, piece = (block & 1) * 4 + p;
+      *reinterpret_cast<uint4*>(tile + (block >> 1) * (KT * 128) + row * 128 + ((piece ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
     }
   }
+}
+
+// 16 columns of this warp's 32 lanes
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                 "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+               : "r"(taddr));
+}
+
+// The same, there: what is done with them is behind this.
+__device__ __forceinline__ void tmem_have16(uint32_t (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+}
+
+// A row's weights 2^(score + base) of KT tokens, as float16 pairs; their sum, and the largest exponent.  16 scores come from tensor
+// memory while those before are worked on.
+template <bool FULL>
+__device__ __forceinline__ void some_weights(const uint32_t (&v)[16], float f, float base, int at, int lim, int low, bool on, uint32_t* w,
+                                             float2 (&sum)[2], float (&most)[2]) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    float2 x = fma2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(f, f), make_float2(base, base));
+    if (!FULL) {
+      if (!on || at + i > lim || at + i < low) x.x = __int_as_float(0xFF800000);
+      if (!on || at + i + 1 > lim || at + i + 1 < low) x.y = __int_as_float(0xFF800000);
+    }
+    asm("max.f32 %0, %0, %1, %2;" : "+f"(most[i / 2 & 1]) : "f"(x.x), "f"(x.y));
+    x.x = ex2(x.x), x.y = ex2(x.y);
+    sum[i / 2 & 1] = add2(sum[i / 2 & 1], x);
+    w[i / 2] = f16_pair(x.x, x.y);
+  }
+}
+template <bool FULL>
+__device__ __forceinline__ float all_weights(uint32_t s_col, const float* k_factor, float fac, float base, int t0, int lim, int low,
+                                             uint32_t there, uint32_t (&w)[KT / 2], float2& total) {
+  float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+  float most[2] = {-1e30f, -1e30f};
+  uint32_t a[16], b[16];
+  tmem_ld16(s_col, a);
+#pragma unroll
+  for (int c = 0; c < KT / 16; c += 2) {
+    const float f = fac * k_factor[c / 2];
+    tmem_have16(a);
+    tmem_ld16(s_col + 16 * c + 16, b);
+    some_weights<FULL>(a, f, base, t0 + 16 * c, lim, low, there >> c & 1, w + 8 * c, sum, most);
+    tmem_have16(b);
+    if (c + 2 < KT / 16) tmem_ld16(s_col + 16 * c + 32, a);
+    some_weights<FULL>(b, f, base, t0 + 16 * c + 16, lim, low, there >> (c + 1) & 1, w + 8 * c + 8, sum, most);
+  }
+  total = add2(sum[0], sum[1]);
+  return fmaxf(most[0], most[1]);
+}
+__device__ __forceinline__ float weights(uint32_t s_col, const float* k_factor, float fac, float base, bool full, int t0, int lim, int low,
+                                         uint32_t there, uint32_t (&w)[KT / 2], float2& total) {
+  if (full) return all_weights<true>(s_col, k_factor, fac, base, t0, lim, low, there, w, total);
+  return all_weights<false>(s_col, k_factor, fac, base, t0, lim, low, there, w, total);
 }
 
 template <int NB>
 __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const __grid_constant__ AttnArgs a) {
   using C = Tc<NB>;
-  constexpr int D = C::D, KT = C::KT, QT = C::QT, ROWS = C::ROWS, kHere = NB < 4 ? NB : 4;
+  constexpr int D = C::D, QT = C::QT, kBufs = C::kBufs, kBufLog = C::kBufLog, ROWS = C::ROWS, kHere = NB < 4 ? NB : 4;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Bars* bars = reinterpret_cast<Bars*>(smem + C::kOffBars);
@@ -276,11 +352,15 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), cta = blockIdx.x, hkv = a.c.hkv;
 
   if (tid == 0) {
-    for (int i = 0; i < 3; ++i) mbar_init(&bars->raw_full[i], 1), mbar_init(&bars->raw_empty[i], 4);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 6; ++i) mbar_init(&bars->raw_full[i], 1), mbar_init(&bars->raw_empty[i], 4);
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&bars->k_full[i], 4), mbar_init(&bars->v_full[i], 4);
       mbar_init(&bars->k_empty[i], 1), mbar_init(&bars->v_empty[i], 1);
-      mbar_init(&bars->s_full[i], 1), mbar_init(&bars->p_full[i], 4), mbar_init(&bars->pv_done[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->s_full[i][0], 1), mbar_init(&bars->s_full[i][1], 1);
+      mbar_init(&bars->p_full[i][0], 4), mbar_init(&bars->p_full[i][1], 4);
+      mbar_init(&bars->pv_done[i][0], 1), mbar_init(&bars->pv_done[i][1], 1);
     }
     mbar_init(&bars->q_full, 4 * QT);
     mbar_init(&bars->most_full, 4);
@@ -337,8 +417,9 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   tc_fence_after();
   if (!works) return;
   const uint32_t tmem = bars->tmem_addr;
-  Walk<NB> walk(a, bars->found_s, bars->found_at, from, to);
-  Unit u;
+  Walk& walk = bars->walks[warp];
+  const Unit& u = walk.u;
+  if (lane == 0) walk.begin<NB>(a, bars->found_s, bars->found_at, from, to);
   bool ok = true;
   uint32_t jj = 0;                                       // steps so far
 #define CAT_WAIT(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort_flag, __LINE__)))
@@ -346,13 +427,12 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   if (warp < 4 * QT) {
     // ---------------------------------------------------------------- rows
     const int tile = warp >> 2, r = tile * 128 + (warp & 3) * 32 + lane;
-    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + tile * KT, o_col = lanes + C::kO + tile * D;
-    int64_t unit_end;
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_cols = lanes + tile * (2 * KT), o_col = lanes + C::kO + tile * D;
     uint32_t units = 0, tj = 0;                          // units and this tile's steps so far
-    while (ok && walk.next(u, &unit_end)) {
+    while (ok && walk.next<NB>(a)) {
       if (tid == 0 && u.starts && !u.whole) {
         Plan p = {u.s, u.h, u.rt, 0};
-        const int64_t last = unit_end - 1;
+        const int64_t last = u.end - 1;
         p.last = (int)(last < rest * (each + 1) ? last / (each + 1) : rest + (last - rest * (each + 1)) / each);
         a.plan[cta] = p;
       }
@@ -405,55 +485,40 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       const int lim = real ? (int)(p < q.end - 1 ? p : q.end - 1) : 0x7FFFFFFF;
       const int low = real && a.window && p - a.window + 1 > 0 ? (int)(p - a.window + 1) : 0;
       const bool tile_real = tile * 128 < u.rows, any_real = __any_sync(0xFFFFFFFFu, real);
-      float m = -1e30f;
+      float m = 0.f;
+      bool seen = false;                                 // the maximum is one of scores
       float2 l2 = make_float2(0.f, 0.f);
       int ref = 0;
       uint32_t nan_blocks = 0;
       for (int step = u.j0; step < u.j1; ++step, ++jj) {
         if (!tile_real) continue;
-        const int b = jj & 1;
-        const float* k_factor = bars->k_factor[jj & 3];
-        if (!CAT_WAIT(&bars->s_full[tile], tj & 1)) break;
-        if (!CAT_WAIT(&bars->v_full[b], (jj >> 1) & 1)) break;       // (the values' reference)
+        const uint32_t b = jj & (kBufs - 1), s_col = s_cols + (tj & 1) * KT;
+        const float* k_factor = bars->k_factor[jj & 7];
+        if (!CAT_WAIT(&bars->s_full[tile][tj & 1], (tj >> 1) & 1)) break;
         tc_fence_after();
-        if (any_real) {
+        if (!any_real) {
+          if (!CAT_WAIT(&bars->v_full[b], (jj >> kBufLog) & 1)) break;       // (so that no step is left behind by two rounds)
+        } else {
           const int t0 = step * KT;
-          const uint32_t there = bars->there[jj & 3];
+          const uint32_t there = bars->there[jj & 7];
           constexpr uint32_t kAll = (1u << (KT / 16)) - 1u;
           const bool full = __all_sync(0xFFFFFFFFu, t0 + KT - 1 <= lim && t0 >= low) && there == kAll;
-          // ---- the step's largest score
-          float top = -1e30f;
-#pragma unroll
-          for (int c = 0; c < KT / 32; ++c) {
-            uint32_t v[32];
-            CAT_TMEM_LD32(s_col + 32 * c, v);
-            const float f0 = fac * k_factor[KT == 64 ? 2 * c : c], f1 = fac * k_factor[KT == 64 ? 2 * c + 1 : c];
-            tmem_ld_wait();
-            if (!full) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const int at = t0 + 32 * c + i;
-                if (at > lim || at < low || !(there >> (2 * c + i / 16) & 1)) v[i] = 0xFF800000u;
-              }
-            }
-            float m0 = __uint_as_float(v[0]), m1 = __uint_as_float(v[16]);
-#pragma unroll
-            for (int i = 1; i < 16; ++i) {
-              m0 = fmaxf(m0, __uint_as_float(v[i]));
-              m1 = fmaxf(m1, __uint_as_float(v[16 + i]));
-            }
-            // (of factors that are 0, an infinity of what is not seen makes NaN, which is not the larger)
-            top = fmaxf(top, fmaxf(m0 * f0, m1 * f1));
-          }
-          const int now = bars->v_ref[b];
+          // Weights, times 2^8, of the maximum so far; where that is too small by more than kSlack (a unit's first step), again.
+          uint32_t w[KT / 2];
+          float2 sum;
+          const float most = weights(s_col, k_factor, fac, 8.f - m, full, t0, lim, low, there, w, sum);
+          if (!CAT_WAIT(&bars->v_full[b], (jj >> kBufLog) & 1)) break;       // (the values' reference)
+          const uint32_t v_ref = bars->v_ref[b];
+          const int now = (int)(v_ref & 255u);
           const bool first = step == u.j0;
-          if (__any_sync(0xFFFFFFFFu, first || top > m + kSlack || now != ref)) {
-            const float up = top > m + kSlack || first ? fmaxf(top, m) : m;
-            const float by = ex2(m - up);
+          const bool grows = most > 8.f + kSlack || (!seen && most > -1e29f);
+          if (__any_sync(0xFFFFFFFFu, grows || now != ref)) {
+            const float up = grows ? m + (most - 8.f) : m, by = seen ? ex2(m - up) : 1.f;      // (nothing seen: all is 0)
             m = up;
+            seen |= grows;
             l2.x *= by, l2.y *= by;
             if (!first) {
-              if (!CAT_WAIT(&bars->pv_done[tile], (tj - 1) & 1)) break;
+              if (!CAT_WAIT(&bars->pv_done[tile][(tj - 1) & 1], ((tj - 1) >> 1) & 1)) break;
               tc_fence_after();
               const float scale_o = by * ex2((float)(ref - now));
 #pragma unroll 1
@@ -467,47 +532,27 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
               }
             }
             ref = now;
+            weights(s_col, k_factor, fac, 8.f - m, full, t0, lim, low, there, w, sum);
           }
-          if (bars->v_odd[b][0] | bars->v_odd[b][1] | bars->v_odd[b][2] | bars->v_odd[b][3])
+          l2 = add2(l2, sum);
+#pragma unroll
+          for (int c = 0; c < KT / 2; c += 16) tmem_st16(s_col + c, w + c);
+          if (v_ref & 256u)
             for (int i = 0; i < KT; ++i) {
               const int at = t0 + i;
-              if (at <= lim && at >= low) nan_blocks |= bars->v_nan[b][i];
+              if (at <= lim && at >= low) nan_blocks |= (uint32_t)bars->v_nan[b][0][i] | bars->v_nan[b][1][i];
             }
-          // ---- weights, times 2^8
-          const float2 base = make_float2(8.f - m, 8.f - m);
-#pragma unroll
-          for (int c = 0; c < KT / 32; ++c) {
-            uint32_t v[32], w[16];
-            CAT_TMEM_LD32(s_col + 32 * c, v);
-            const float f0 = fac * k_factor[KT == 64 ? 2 * c : c], f1 = fac * k_factor[KT == 64 ? 2 * c + 1 : c];
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const float f = i < 16 ? f0 : f1;
-              float2 x = fma2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(f, f), base);
-              if (!full) {
-                const int at = t0 + 32 * c + i;
-                const bool on = there >> (2 * c + i / 16) & 1;
-                if (at > lim || at < low || !on) x.x = __int_as_float(0xFF800000);
-                if (at + 1 > lim || at + 1 < low || !on) x.y = __int_as_float(0xFF800000);
-              }
-              x.x = ex2(x.x), x.y = ex2(x.y);
-              l2 = add2(l2, x);
-              w[i / 2] = f16_pair(x.x, x.y);
-            }
-            tmem_st16(s_col + 16 * c, w);
-          }
           tmem_st_wait();
         }
         tc_fence_before();
         __syncwarp();
-        if (elect_one()) mbar_arrive(&bars->p_full[tile]);
+        if (elect_one()) mbar_arrive(&bars->p_full[tile][tj & 1]);     // (a warp may be a step ahead of another: a barrier for each buffer)
         ++tj;
       }
       if (!ok) break;
       if (!tile_real) continue;
       // ---- out
-      if (!CAT_WAIT(&bars->pv_done[tile], (tj - 1) & 1)) break;
+      if (!CAT_WAIT(&bars->pv_done[tile][(tj - 1) & 1], ((tj - 1) >> 1) & 1)) break;
       tc_fence_after();
       if (any_real) {
         const float l = l2.x + l2.y;
@@ -539,13 +584,13 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   } else if (warp >= kKeyWarp0 && warp < kMmaWarp) {
     // ---------------------------------------------------------------- keys and values to float16
     const bool values = warp >= kValueWarp0;
-    const int w = (warp - kKeyWarp0) & 3, t = w * 32 + lane, row = NB == 8 ? t >> 1 : t, first_block = NB == 8 ? (t & 1) * 4 : 0;
+    const int w = (warp - kKeyWarp0) & 3, row = (w & 1) * 32 + lane, half = w >> 1, first_block = NB == 8 ? half * 4 : 0;
     int ref = kLowR;
-    while (ok && walk.next(u)) {
+    while (ok && walk.next<NB>(a)) {
       if (values) ref = kLowR;                           // (O begins anew)
       for (int step = u.j0; step < u.j1; ++step, ++jj) {
-        const uint32_t e = 2 * jj + (values ? 1 : 0), st = e % 3, b = jj & 1;
-        if (!CAT_WAIT(&bars->raw_full[st], (e / 3) & 1)) break;
+        const uint32_t ring = values ? C::kRingV : C::kRingK, st = (values ? C::kRingK : 0) + jj % ring, b = jj & (kBufs - 1);
+        if (!CAT_WAIT(&bars->raw_full[st], (jj / ring) & 1)) break;
         const uint8_t* raw = smem + C::kOffRaw + st * C::kRaw;
         const uint32_t there = bars->raw_there[st];
         const int64_t token = (int64_t)step * KT + row;
@@ -563,33 +608,47 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         most = __reduce_max_sync(0xFFFFFFFFu, most);
         __half2 scale[kHere];
         if (values) {
+          const bool odd = __any_sync(0xFFFFFFFFu, nan != 0);
           if (lane == 0) {
-            bars->v_most[b][w] = most;
+            bars->v_most[jj & 1][w] = most | (odd ? 256u : 0u);
             mbar_arrive(&bars->most_full);
           }
           if (!CAT_WAIT(&bars->most_full, jj & 1)) break;
+          uint32_t all = 0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) ref = max(ref, (int)bars->v_most[b][i]);
-          if (jj >= 2 && !CAT_WAIT(&bars->v_empty[b], ((jj >> 1) - 1) & 1)) break;
-          const bool odd = __any_sync(0xFFFFFFFFu, nan != 0);
-          if (NB == 8) nan |= __shfl_xor_sync(0xFFFFFFFFu, nan, 1);
-          bars->v_nan[b][row] = (uint8_t)nan;
-          if (lane == 0) bars->v_odd[b][w] = odd;
-          if (t == 0) bars->v_ref[b] = ref;
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t v = bars->v_most[jj & 1][i];
+            all |= v & 256u;
+            ref = max(ref, (int)(v & 255u));
+          }
+          if (jj >= kBufs && !CAT_WAIT(&bars->v_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
+          bars->v_nan[b][half][row] = (uint8_t)nan;
+          if (w == 0 && lane == 0) bars->v_ref[b] = (uint32_t)ref | all;
 #pragma unroll
           for (int i = 0; i < kHere; ++i) scale[i] = on && bytes[i] != 255 ? half_scale(bytes[i], ref) : half_scale(-1000, 0);
-          unpack_row<NB, true>(raw, smem + C::kOffV + b * C::kTile, t, scale);
+          unpack_half<NB, true>(raw, smem + C::kOffV + b * C::kTile, row, half, scale);
         } else {
-          const int kref = max((int)most, kLowR);
-          if (jj >= 2 && !CAT_WAIT(&bars->k_empty[b], ((jj >> 1) - 1) & 1)) break;
+          // (d = 256: the two halves' largest differ; the keys' reference is of all their blocks)
+          uint32_t whole = most;
+          if constexpr (NB == 8) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t o = on ? raw[C::kCodes + row * NB + (first_block ^ 4) + i] : 0u;
+              if (o != 255u) m = max(m, o);
+            }
+            whole = max(whole, __reduce_max_sync(0xFFFFFFFFu, m));
+          }
+          const int kref = max((int)whole, kLowR);
+          if (jj >= kBufs && !CAT_WAIT(&bars->k_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
 #pragma unroll
           for (int i = 0; i < kHere; ++i) {
             scale[i] = on ? half_scale(bytes[i], kref) : half_scale(-1000, 0);
             if (bytes[i] == 255) scale[i] = __half2half2(__ushort_as_half(0x7FFF));
           }
-          if (lane == 0) bars->k_factor[jj & 3][w] = __uint_as_float((uint32_t)(kref - 12) << 23);
-          if (t == 0) bars->there[jj & 3] = there;
-          unpack_row<NB, false>(raw, smem + C::kOffK + b * C::kTile, t, scale);
+          if (lane == 0 && half == 0) bars->k_factor[jj & 7][w & 1] = __uint_as_float((uint32_t)(kref - 12) << 23);
+          if (w == 0 && lane == 0) bars->there[jj & 7] = there;
+          unpack_half<NB, false>(raw, smem + C::kOffK + b * C::kTile, row, half, scale);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -603,48 +662,57 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
     // ---------------------------------------------------------------- MMAs
     constexpr uint32_t kScores = idesc_f16(KT, false), kOut = idesc_f16(D, true);
     uint32_t units = 0, tj[2] = {0, 0};
-    auto scores = [&](int tile, uint32_t j) {
-      const uint32_t qb = smem_u32(smem + tile * C::kQ), kb = smem_u32(smem + C::kOffK + (j & 1) * C::kTile);
+    auto scores = [&](int tile, uint32_t j, uint32_t buffer) {
+      const uint32_t qb = smem_u32(smem + tile * C::kQ), kb = smem_u32(smem + C::kOffK + (j & (kBufs - 1)) * C::kTile);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk)
-        mma_ss(tmem + tile * KT, sdesc_kmajor_sw128(qb + (kk >> 2) * (128 * 128) + (kk & 3) * 32),
+        mma_ss(tmem + (tile * 2 + buffer) * KT, sdesc_kmajor_sw128(qb + (kk >> 2) * (128 * 128) + (kk & 3) * 32),
                sdesc_kmajor_sw128(kb + (kk >> 2) * (KT * 128) + (kk & 3) * 32), kScores, kk != 0);
-      mma_commit(&bars->s_full[tile]);
+      mma_commit(&bars->s_full[tile][buffer]);
     };
-    while (ok && walk.next(u)) {
+    while (ok && walk.next<NB>(a)) {
       if (u.j0 == u.j1) continue;
       const int tiles = u.rows > 128 ? 2 : 1;
       if (!CAT_WAIT(&bars->q_full, units & 1)) break;
       ++units;
-      if (!CAT_WAIT(&bars->k_full[jj & 1], (jj >> 1) & 1)) break;
-      tc_fence_after();
-      if (elect_one()) {
-        for (int tile = 0; tile < tiles; ++tile) scores(tile, jj);
-        mma_commit(&bars->k_empty[jj & 1]);
+      for (int i = 0; i < 2 && u.j0 + i < u.j1; ++i) {   // the first two steps' scores
+        const uint32_t j = jj + i;
+        if (!CAT_WAIT(&bars->k_full[j & (kBufs - 1)], (j >> kBufLog) & 1)) break;
+        tc_fence_after();
+        if (elect_one()) {
+          for (int tile = 0; tile < tiles; ++tile) scores(tile, j, (tj[tile] + i) & 1);
+          mma_commit(&bars->k_empty[j & (kBufs - 1)]);
+        }
+        __syncwarp();
       }
-      __syncwarp();
       for (int step = u.j0; step < u.j1 && ok; ++step, ++jj) {
-        const bool more = step + 1 < u.j1;
+        const bool more = step + 2 < u.j1;
+        const uint32_t vb = jj & (kBufs - 1), ahead = jj + 2;
         for (int tile = 0; tile < tiles; ++tile) {
-          if (tile == 0 && !CAT_WAIT(&bars->v_full[jj & 1], (jj >> 1) & 1)) break;
-          if (!CAT_WAIT(&bars->p_full[tile], tj[tile] & 1)) break;
-          ++tj[tile];
-          if (tile == 0 && more && !CAT_WAIT(&bars->k_full[(jj + 1) & 1], ((jj + 1) >> 1) & 1)) break;
+          if (tile == 0 && !CAT_WAIT(&bars->v_full[vb], (jj >> kBufLog) & 1)) break;
+          const uint32_t buffer = tj[tile] & 1;
+          if (!CAT_WAIT(&bars->p_full[tile][buffer], (tj[tile] >> 1) & 1)) break;
           tc_fence_after();
           if (elect_one()) {
-            const uint32_t vb = smem_u32(smem + C::kOffV + (jj & 1) * C::kTile);
+            const uint32_t v = smem_u32(smem + C::kOffV + vb * C::kTile);
 #pragma unroll
             for (int kk = 0; kk < KT / 16; ++kk)
-              mma_ts(tmem + C::kO + tile * D, tmem + tile * KT + kk * 8, sdesc_mnmajor_sw128(vb + kk * 2048, KT * 128), kOut,
+              mma_ts(tmem + C::kO + tile * D, tmem + (tile * 2 + buffer) * KT + kk * 8, sdesc_mnmajor_sw128(v + kk * 2048, KT * 128), kOut,
                      step > u.j0 || kk != 0);
-            mma_commit(&bars->pv_done[tile]);
-            if (tile == tiles - 1) mma_commit(&bars->v_empty[jj & 1]);
-            if (more) {
-              scores(tile, jj + 1);
-              if (tile == tiles - 1) mma_commit(&bars->k_empty[(jj + 1) & 1]);
-            }
+            mma_commit(&bars->pv_done[tile][buffer]);
+            if (tile == tiles - 1) mma_commit(&bars->v_empty[vb]);
           }
           __syncwarp();
+          if (more) {
+            if (tile == 0 && !CAT_WAIT(&bars->k_full[ahead & (kBufs - 1)], (ahead >> kBufLog) & 1)) break;
+            tc_fence_after();
+            if (elect_one()) {
+              scores(tile, ahead, buffer);
+              if (tile == tiles - 1) mma_commit(&bars->k_empty[ahead & (kBufs - 1)]);
+            }
+            __syncwarp();
+          }
+          ++tj[tile];
         }
       }
     }
@@ -655,22 +723,28 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   } else if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- copies
     const int most = a.c.page < KT ? a.c.page : KT, copies = KT / most;      // tokens a copy; copies a step, a lane each
-    uint32_t e = 0;
-    while (ok && walk.next(u)) {
+    uint32_t sent[2] = {0, 0};
+    while (ok && walk.next<NB>(a)) {
       const int32_t* pages = a.table + (int64_t)u.s * a.width;
       const uint8_t* head = a.c.base + (int64_t)u.h * a.c.part;
-      for (int step = u.j0; step < u.j1 && ok; ++step, ++jj) {
+      const int64_t page_bytes = 2 * a.c.hkv * a.c.part;
+      auto page_of = [&](int step) {                     // of this lane's tokens, -1: none
         const int t0 = step * KT + lane * most;
-        int64_t pg = -1;
-        if (lane < copies && t0 < walk.q.end) pg = __ldg(pages + (t0 >> a.c.page_log));
-        if (pg >= a.pages) pg = -1;
+        if (lane >= copies || step >= u.j1 || t0 >= walk.q.end) return -1;
+        const int pg = __ldg(pages + (t0 >> a.c.page_log));
+        return pg < 0 || pg >= a.pages ? -1 : pg;
+      };
+      int pg_next = page_of(u.j0);
+      for (int step = u.j0; step < u.j1 && ok; ++step, ++jj) {
+        const int pg = pg_next, r = (step * KT + lane * most) & (a.c.page - 1), o = lane * most;
+        pg_next = page_of(step + 1);
         const uint32_t have = __ballot_sync(0xFFFFFFFFu, pg >= 0);
         uint32_t groups = 0;                             // of 16 tokens
         for (int i = 0; i < copies; ++i)
           if (have >> i & 1) groups |= ((1u << (most / 16)) - 1u) << (i * (most / 16));
-        for (int kind = 0; kind < 2; ++kind, ++e) {
-          const uint32_t st = e % 3;
-          if (e >= 3 && !CAT_WAIT(&bars->raw_empty[st], (e / 3 - 1) & 1)) break;
+        for (int kind = 0; kind < 2; ++kind) {
+          const uint32_t ring = kind ? C::kRingV : C::kRingK, st = (kind ? C::kRingK : 0) + jj % ring;
+          if (jj >= ring && !CAT_WAIT(&bars->raw_empty[st], (jj / ring - 1) & 1)) break;
           uint8_t* raw = smem + C::kOffRaw + st * C::kRaw;
           if (lane == 0) {
             bars->raw_there[st] = groups;
@@ -678,18 +752,22 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           }
           __syncwarp();
           if (pg >= 0) {
-            const uint8_t* part = head + (pg * 2 + kind) * a.c.hkv * a.c.part;
-            const int r = t0 & (a.c.page - 1), o = lane * most;
+            const uint8_t* part = head + pg * page_bytes + kind * a.c.hkv * a.c.part;
             bulk_load(raw + o * (16 * NB), part + r * (16 * NB), most * 16 * NB, &bars->raw_full[st]);
             bulk_load(raw + C::kCodes + o * NB, part + (a.c.page * 16 + r) * NB, most * NB, &bars->raw_full[st]);
           }
           __syncwarp();
+          ++sent[kind];
         }
       }
     }
     if (!ok) {                                           // the copies still on their way
       volatile int none = 0;
-      for (uint32_t i = e > 3 ? e - 3 : 0; i < e; ++i) mbar_wait_bounded(&bars->raw_full[i % 3], (i / 3) & 1, &none);
+      for (int kind = 0; kind < 2; ++kind) {
+        const uint32_t ring = kind ? C::kRingV : C::kRingK;
+        for (uint32_t i = sent[kind] > ring ? sent[kind] - ring : 0; i < sent[kind]; ++i)
+          mbar_wait_bounded(&bars->raw_full[(kind ? C::kRingK : 0) + i % ring], (i / ring) & 1, &none);
+      }
     }
   }
 #undef CAT_WAIT
