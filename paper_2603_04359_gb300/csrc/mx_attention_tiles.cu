@@ -34,7 +34,6 @@ namespace cat {
 namespace {
 
 constexpr int kThreads = 576;
-constexpr int KT = 64;                      // tokens a step
 constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kUnitCost = 384;              // a unit's beginning and end, in tokens
 constexpr int kLeastPiece = 1024;           // tokens (with units' costs) that a CTA is worth
@@ -45,13 +44,15 @@ constexpr int kBarRoom = 6144;
 template <int NB>
 struct Tc {
   static constexpr int D = 32 * NB, QT = NB == 8 ? 1 : 2, ROWS = 128 * QT;
-  static constexpr int kBufs = NB == 8 ? 2 : 4, kBufLog = NB == 8 ? 1 : 2;     // of unpacked keys, and of values
+  static constexpr int KT = NB == 8 ? 64 : 128;          // tokens a step
+  static constexpr int SB = NB == 8 ? 2 : 1;             // buffers of a tile's scores
+  static constexpr int kBufs = 2, kBufLog = 1;           // of unpacked keys, and of values
   static constexpr int kQ = 128 * D * 2, kTile = KT * D * 2, kCodes = KT * 16 * NB, kRaw = kCodes + KT * NB;
-  static constexpr int kRingK = NB == 8 ? 2 : 3, kRingV = NB == 8 ? 1 : 3, kRing = kRingK + kRingV;      // codes as they are: of keys, of values
+  static constexpr int kRingK = 2, kRingV = NB == 2 ? 2 : 1, kRing = kRingK + kRingV;      // codes as they are: of keys, of values
   static constexpr int kOffK = QT * kQ, kOffV = kOffK + kBufs * kTile, kOffRaw = kOffV + kBufs * kTile, kOffBars = kOffRaw + kRing * kRaw;
   static constexpr int kSmem = 1024 + kOffBars + kBarRoom;
-  static constexpr uint32_t kO = QT * 2 * KT;            // tensor memory: two buffers of scores a tile, then O's
-  static_assert(kSmem <= 227 * 1024 && QT * (2 * KT + D) <= (int)kTmemCols, "");
+  static constexpr uint32_t kO = QT * SB * KT;           // tensor memory: the scores, then O's
+  static_assert(kSmem <= 227 * 1024 && QT * (SB * KT + D) <= (int)kTmemCols, "");
 };
 
 struct Seq : Rows {
@@ -104,8 +105,9 @@ struct Walk {
     return more;
   }
   template <int NB>
-  __device__ __forceinline__ bool advance(const AttnArgs& a) {
+  __device__ __noinline__ bool advance(const AttnArgs& a) {
     using C = Tc<NB>;
+    constexpr int KT = C::KT;
     while (left > 0) {
       int64_t all = a.c.hkv * q.before(q.tiles);
       while (at >= all) {
@@ -152,12 +154,12 @@ struct Bars {
   uint64_t raw_full[6], raw_empty[6], k_full[4], k_empty[4], v_full[4], v_empty[4], q_full, s_full[2][2], p_full[2][2], pv_done[2][2], most_full,
       mma_done;
   // (of eight steps: keys are unpacked up to five steps ahead of scores that are still read)
-  float k_factor[8][2];                     // 2^(ref - 139) of 32 tokens' keys
+  float k_factor[8][4];                     // 2^(ref - 139) of 32 tokens' keys
   uint32_t there[8];                        // which 16-token groups of a step are on pages
   uint32_t raw_there[6];
   uint32_t v_ref[4];                        // the values' reference, + 256 where a scale of the step's is NaN
   uint32_t v_most[2][4];                    // the same of a warp's tokens
-  uint8_t v_nan[4][2][KT];                  // a token's blocks of NaN scales (d = 256: those of half of them)
+  uint8_t v_nan[2][2][128];                  // a token's blocks of NaN scales (d = 256: those of half of them)
   int64_t scan[20];
   int64_t found_at;
   int found_s, abort;
@@ -169,10 +171,6 @@ static_assert(sizeof(Bars) <= kBarRoom, "barrier room");
 // ---- tensor memory
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
-  tmem_st16(taddr, v);
-  tmem_st16(taddr + 16, v + 16);
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -236,41 +234,38 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return o;
 }
 
-// Half of a token's row of keys or values to float16 operands: two quarters of it (d = 256: half of the blocks).  Operands are rows of
+// A token's row of keys or values (d = 256: half of its blocks) to float16 operands.  Operands are rows of
 // 64 channels, 128 bytes each, 16-byte pieces at piece ^ (row mod 8).  Quarters are taken in an order that differs from lane to lane, so that
-// writes never meet in a bank and reads in pairs at most.
-template <int NB, bool VALUES>
-__device__ __forceinline__ void unpack_half(const uint8_t* raw, uint8_t* tile, int row, int half, const __half2 (&scale)[NB < 4 ? NB : 4]) {
-  constexpr int kHere = NB < 4 ? NB : 4, kQuarters = NB == 8 ? 4 : 2;
-  const int block0 = NB == 8 ? 4 * half : 0, turn = NB == 2 ? (row >> 2) & 1 : NB == 4 ? (row >> 1) & 1 : (row >> 1) & 3;
-#pragma unroll
-  for (int i = 0; i < kQuarters; ++i) {
-    const int p = NB == 8 ? i ^ turn : 2 * half + (i ^ turn);          // the quarter: channels 8 p .. 8 p + 7 of every block
+// neither reads nor writes meet in a bank (reads of d = 256 do in pairs).
+template <int NB>
+__device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* tile, int row, int half, bool values,
+                                            const __half2 (&scale)[NB < 4 ? NB : 4]) {
+  constexpr int KT = Tc<NB>::KT, kHere = NB < 4 ? NB : 4;
+  const int block0 = NB == 8 ? 4 * half : 0, turn = (NB == 2 ? row >> 2 : row >> 1) & 3;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    const int p = i ^ turn;                              // the quarter: channels 8 p .. 8 p + 7 of every block
     const uint8_t* at = raw + row * (16 * NB) + p * (4 * NB);
     uint32_t w[kHere];
-    if constexpr (VALUES) {                              // halfwords [2][NB]
-      uint32_t lo[kHere / 2], hi[kHere / 2];
-      if constexpr (NB == 2) {
-        const uint2 v = *reinterpret_cast<const uint2*>(at);
-        lo[0] = v.x, hi[0] = v.y;
-      } else if constexpr (NB == 4) {
-        const uint4 v = *reinterpret_cast<const uint4*>(at);
-        lo[0] = v.x, lo[1] = v.y, hi[0] = v.z, hi[1] = v.w;
-      } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(at + 8 * half), u = *reinterpret_cast<const uint2*>(at + 8 * half + 16);
-        lo[0] = v.x, lo[1] = v.y, hi[0] = u.x, hi[1] = u.y;
-      }
-#pragma unroll
-      for (int b = 0; b < kHere; b += 2) {
-        w[b] = __byte_perm(lo[b / 2], hi[b / 2], 0x5410);
-        w[b + 1] = __byte_perm(lo[b / 2], hi[b / 2], 0x7632);
-      }
-    } else if constexpr (NB == 2) {
+    if constexpr (NB == 2) {
       const uint2 v = *reinterpret_cast<const uint2*>(at);
       w[0] = v.x, w[1] = v.y;
-    } else {
-      const uint4 v = *reinterpret_cast<const uint4*>(at + (NB == 8 ? 16 * half : 0));
+    } else if constexpr (NB == 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(at);
       w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {                                             // (half of a quarter's words; of values, half of either row of halfwords)
+      const uint2 v = *reinterpret_cast<const uint2*>(at + (values ? 8 : 16) * half), n = *reinterpret_cast<const uint2*>(at + (values ? 8 * half + 16 : 16 * half + 8));
+      w[0] = v.x, w[1] = v.y, w[2] = n.x, w[3] = n.y;
+    }
+    if (values) {                                        // halfwords [2][blocks]
+      uint32_t t[kHere];
+#pragma unroll
+      for (int b = 0; b < kHere; b += 2) {
+        t[b] = __byte_perm(w[b / 2], w[kHere / 2 + b / 2], 0x5410);
+        t[b + 1] = __byte_perm(w[b / 2], w[kHere / 2 + b / 2], 0x7632);
+      }
+#pragma unroll
+      for (int b = 0; b < kHere; ++b) w[b] = t[b];
     }
 #pragma unroll
     for (int b = 0; b < kHere; ++b) {
@@ -291,60 +286,120 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
 }
 
 // The same, there: what is done with them is behind this.
+__device__ __forceinline__ void tmem_have32(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]),
+                 "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23])
+               :
+               : "memory");
+  asm volatile("" : "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float m;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  return m;
+}
 __device__ __forceinline__ void tmem_have16(uint32_t (&v)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
                : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
                  "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
-// A row's weights 2^(score + base) of KT tokens, as float16 pairs; their sum, and the largest exponent.  16 scores come from tensor
-// memory while those before are worked on.
-template <bool FULL>
-__device__ __forceinline__ void some_weights(const uint32_t (&v)[16], float f, float base, int at, int lim, int low, bool on, uint32_t* w,
-                                             float2 (&sum)[2], float (&most)[2]) {
+// What a product is times; never 0, which would make NaN of the infinity that stands for what is not seen.
+__device__ __forceinline__ float score_factor(float fac, float k_factor) { return fmaxf(fac * k_factor, 0x1p-126f); }
+
+// The largest score of a row's KT, times its factors.
+template <int KT>
+__device__ __forceinline__ float largest(uint32_t s_col, const float* k_factor, float fac) {
+  float most = -INFINITY;
+#pragma unroll 1
+  for (int c = 0; c < KT / 32; ++c) {
+    uint32_t v[32];
+    CAT_TMEM_LD32(s_col + 32 * c, v);
+    const float f = score_factor(fac, k_factor[c]);
+    tmem_have32(v);
+    float m[2] = {__uint_as_float(v[0]), __uint_as_float(v[1])};
 #pragma unroll
-  for (int i = 0; i < 16; i += 2) {
-    float2 x = fma2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(f, f), make_float2(base, base));
-    if (!FULL) {
-      if (!on || at + i > lim || at + i < low) x.x = __int_as_float(0xFF800000);
-      if (!on || at + i + 1 > lim || at + i + 1 < low) x.y = __int_as_float(0xFF800000);
+    for (int i = 2; i < 32; i += 4) {
+      m[0] = max3(m[0], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+      if (i + 2 < 32) m[1] = max3(m[1], __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
     }
-    asm("max.f32 %0, %0, %1, %2;" : "+f"(most[i / 2 & 1]) : "f"(x.x), "f"(x.y));
-    x.x = ex2(x.x), x.y = ex2(x.y);
-    sum[i / 2 & 1] = add2(sum[i / 2 & 1], x);
-    w[i / 2] = f16_pair(x.x, x.y);
+    most = fmaxf(most, fmaxf(m[0], m[1]) * f);
   }
+  return most;
 }
-template <bool FULL>
-__device__ __forceinline__ float all_weights(uint32_t s_col, const float* k_factor, float fac, float base, int t0, int lim, int low,
-                                             uint32_t there, uint32_t (&w)[KT / 2], float2& total) {
-  float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-  float most[2] = {-1e30f, -1e30f};
-  uint32_t a[16], b[16];
-  tmem_ld16(s_col, a);
+// A row's weights 2^(score + base), as float16 pairs in the scores' place; their sum is added to `sum`.
+template <int KT>
+__device__ __forceinline__ void weights(uint32_t s_col, const float* k_factor, float fac, float base, float2& sum) {
+  float2 part = make_float2(0.f, 0.f);
+#pragma unroll 1
+  for (int c = 0; c < KT / 32; ++c) {
+    uint32_t v[32], w[16];
+    CAT_TMEM_LD32(s_col + 32 * c, v);
+    const float f = score_factor(fac, k_factor[c]);
+    tmem_have32(v);
 #pragma unroll
-  for (int c = 0; c < KT / 16; c += 2) {
-    const float f = fac * k_factor[c / 2];
-    tmem_have16(a);
-    tmem_ld16(s_col + 16 * c + 16, b);
-    some_weights<FULL>(a, f, base, t0 + 16 * c, lim, low, there >> c & 1, w + 8 * c, sum, most);
-    tmem_have16(b);
-    if (c + 2 < KT / 16) tmem_ld16(s_col + 16 * c + 32, a);
-    some_weights<FULL>(b, f, base, t0 + 16 * c + 16, lim, low, there >> (c + 1) & 1, w + 8 * c + 8, sum, most);
+    for (int i = 0; i < 32; i += 2) {
+      float2 x = fma2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(f, f), make_float2(base, base));
+      x.x = ex2(x.x), x.y = ex2(x.y);
+      if (i & 2)
+        part = add2(part, x);
+      else
+        sum = add2(sum, x);
+      w[i / 2] = f16_pair(x.x, x.y);
+    }
+    tmem_st16(s_col + 16 * c, w);
   }
-  total = add2(sum[0], sum[1]);
-  return fmaxf(most[0], most[1]);
+  sum = add2(sum, part);
 }
-__device__ __forceinline__ float weights(uint32_t s_col, const float* k_factor, float fac, float base, bool full, int t0, int lim, int low,
-                                         uint32_t there, uint32_t (&w)[KT / 2], float2& total) {
-  if (full) return all_weights<true>(s_col, k_factor, fac, base, t0, lim, low, there, w, total);
-  return all_weights<false>(s_col, k_factor, fac, base, t0, lim, low, there, w, total);
+// Scores of tokens that a row does not see become -infinity where they are (steps at an end of what the rows see alone come here).
+template <int KT>
+__device__ __forceinline__ void hide(uint32_t s_col, int t0, int lim, int low, uint32_t there) {
+#pragma unroll 1
+  for (int c = 0; c < KT / 16; ++c) {
+    uint32_t v[16];
+    tmem_ld16(s_col + 16 * c, v);
+    tmem_have16(v);
+    const bool on = there >> c & 1;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int at = t0 + 16 * c + i;
+      if (!on || at > lim || at < low) v[i] = 0xFF800000u;
+    }
+    tmem_st16(s_col + 16 * c, v);
+  }
+  tmem_st_wait();
+}
+
+// A bounded wait in few instructions (the roles' loops have to stay in the instruction cache together: with the timed wait in line at
+// every place, and copies of the weights' code, 77 % of the cache's rate behind it went into fetching them again).  POLL: without
+// letting the hardware suspend the thread, whose waking takes longer; for the MMAs' warp, behind which all others are.
+constexpr int kTries = 1 << 20, kPolls = 1 << 24;      // (a try takes up to some microseconds, a poll some 50 ns)
+template <bool POLL>
+__device__ __forceinline__ bool short_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int site) {
+  auto over = [&] {
+    if constexpr (!POLL) return mbar_try_wait(bar, parity);
+    uint32_t p;
+    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(p)
+                 : "r"(smem_u32(bar)), "r"(parity)
+                 : "memory");
+    return p != 0;
+  };
+#pragma unroll 1
+  for (int n = 0; !over(); ++n)
+    if (n > (POLL ? kPolls : kTries) || *abort) {
+      if (*abort == 0) *abort = site;
+      return false;
+    }
+  return true;
 }
 
 template <int NB>
 __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const __grid_constant__ AttnArgs a) {
   using C = Tc<NB>;
-  constexpr int D = C::D, QT = C::QT, kBufs = C::kBufs, kBufLog = C::kBufLog, ROWS = C::ROWS, kHere = NB < 4 ? NB : 4;
+  constexpr int D = C::D, KT = C::KT, SB = C::SB, QT = C::QT, kBufs = C::kBufs, kBufLog = C::kBufLog, ROWS = C::ROWS, kHere = NB < 4 ? NB : 4;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Bars* bars = reinterpret_cast<Bars*>(smem + C::kOffBars);
@@ -422,12 +477,13 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   if (lane == 0) walk.begin<NB>(a, bars->found_s, bars->found_at, from, to);
   bool ok = true;
   uint32_t jj = 0;                                       // steps so far
-#define CAT_WAIT(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort_flag, __LINE__)))
+#define CAT_WAIT(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, short_wait<false>(bar, parity, abort_flag, __LINE__)))
+#define CAT_POLL(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, short_wait<true>(bar, parity, abort_flag, __LINE__)))
 
   if (warp < 4 * QT) {
     // ---------------------------------------------------------------- rows
     const int tile = warp >> 2, r = tile * 128 + (warp & 3) * 32 + lane;
-    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_cols = lanes + tile * (2 * KT), o_col = lanes + C::kO + tile * D;
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_cols = lanes + tile * (SB * KT), o_col = lanes + C::kO + tile * D;
     uint32_t units = 0, tj = 0;                          // units and this tile's steps so far
     while (ok && walk.next<NB>(a)) {
       if (tid == 0 && u.starts && !u.whole) {
@@ -453,14 +509,20 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       // the row to float16, its largest channel in [2^13, 2^14); a negative scale goes into its sign
       float fac;
       {
+        // (the row is read twice, the second time from L1; eight pieces on their way at once: a unit begins with this)
         const uint4* from_q = reinterpret_cast<const uint4*>(a.q + row);
         uint32_t most = 0;
         if (real)
-#pragma unroll 4
-          for (int c = 0; c < D / 8; ++c) {
-            const uint4 v = from_q[c];
-            const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-            most = max(most, max(m & 0xFFFFu, m >> 16));
+#pragma unroll 1
+          for (int c = 0; c < D / 8; c += 8) {
+            uint4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __ldg(from_q + c + i);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t m = __vmaxu2(__vmaxu2(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), __vmaxu2(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu));
+              most = max(most, max(m & 0xFFFFu, m >> 16));
+            }
           }
         const int e = max((int)(most >> 7), 1);
         const float up = (e >= 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23)) * (a.scale < 0.f ? -1.f : 1.f);
@@ -468,11 +530,15 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           return e == 255 ? 0x7FFF7FFFu : f16_pair(__uint_as_float(w << 16) * up * 0x1p13f, __uint_as_float(w & 0xFFFF0000u) * up * 0x1p13f);
         };
         uint8_t* to_q = smem + tile * C::kQ + (r & 127) * 128;
-#pragma unroll 4
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 v = real ? from_q[c] : make_uint4(0u, 0u, 0u, 0u);
-          *reinterpret_cast<uint4*>(to_q + (c >> 3) * (128 * 128) + (((c & 7) ^ (r & 7)) << 4)) =
-              make_uint4(half2_of(v.x), half2_of(v.y), half2_of(v.z), half2_of(v.w));
+#pragma unroll 1
+        for (int c = 0; c < D / 8; c += 4) {
+          uint4 v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = real ? __ldg(from_q + c + i) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(to_q + (c >> 3) * (128 * 128) + ((((c & 7) + i) ^ (r & 7)) << 4)) =
+                make_uint4(half2_of(v[i].x), half2_of(v[i].y), half2_of(v[i].z), half2_of(v[i].w));
         }
         fac = ldexpf(fabsf(a.scale), e - 140);
       }
@@ -492,9 +558,9 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       uint32_t nan_blocks = 0;
       for (int step = u.j0; step < u.j1; ++step, ++jj) {
         if (!tile_real) continue;
-        const uint32_t b = jj & (kBufs - 1), s_col = s_cols + (tj & 1) * KT;
+        const uint32_t b = jj & (kBufs - 1), s_col = s_cols + tj % SB * KT;
         const float* k_factor = bars->k_factor[jj & 7];
-        if (!CAT_WAIT(&bars->s_full[tile][tj & 1], (tj >> 1) & 1)) break;
+        if (!CAT_WAIT(&bars->s_full[tile][tj % SB], tj / SB & 1)) break;
         tc_fence_after();
         if (!any_real) {
           if (!CAT_WAIT(&bars->v_full[b], (jj >> kBufLog) & 1)) break;       // (so that no step is left behind by two rounds)
@@ -503,56 +569,49 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           const uint32_t there = bars->there[jj & 7];
           constexpr uint32_t kAll = (1u << (KT / 16)) - 1u;
           const bool full = __all_sync(0xFFFFFFFFu, t0 + KT - 1 <= lim && t0 >= low) && there == kAll;
-          // Weights, times 2^8, of the maximum so far; where that is too small by more than kSlack (a unit's first step), again.
-          uint32_t w[KT / 2];
-          float2 sum;
-          const float most = weights(s_col, k_factor, fac, 8.f - m, full, t0, lim, low, there, w, sum);
+          if (!full) hide<KT>(s_col, t0, lim, low, there);
+          const float most = largest<KT>(s_col, k_factor, fac);
           if (!CAT_WAIT(&bars->v_full[b], (jj >> kBufLog) & 1)) break;       // (the values' reference)
-          const uint32_t v_ref = bars->v_ref[b];
-          const int now = (int)(v_ref & 255u);
-          const bool first = step == u.j0;
-          const bool grows = most > 8.f + kSlack || (!seen && most > -1e29f);
+          const int now = (int)(bars->v_ref[b] & 255u);
+          const bool grows = seen ? most > m + kSlack : most > -INFINITY;
           if (__any_sync(0xFFFFFFFFu, grows || now != ref)) {
-            const float up = grows ? m + (most - 8.f) : m, by = seen ? ex2(m - up) : 1.f;      // (nothing seen: all is 0)
+            const float up = grows ? most : m, by = seen ? ex2(m - up) : 1.f;       // (nothing seen: all is 0)
             m = up;
             seen |= grows;
             l2.x *= by, l2.y *= by;
-            if (!first) {
-              if (!CAT_WAIT(&bars->pv_done[tile][(tj - 1) & 1], ((tj - 1) >> 1) & 1)) break;
+            if (step != u.j0) {
+              if (!CAT_WAIT(&bars->pv_done[tile][(tj - 1) % SB], (tj - 1) / SB & 1)) break;
               tc_fence_after();
               const float scale_o = by * ex2((float)(ref - now));
 #pragma unroll 1
-              for (int c = 0; c < D; c += 32) {
-                uint32_t v[32];
-                CAT_TMEM_LD32(o_col + c, v);
-                tmem_ld_wait();
+              for (int c = 0; c < D; c += 16) {
+                uint32_t v[16];
+                tmem_ld16(o_col + c, v);
+                tmem_have16(v);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * scale_o);
-                tmem_st32(o_col + c, v);
+                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * scale_o);
+                tmem_st16(o_col + c, v);
               }
             }
             ref = now;
-            weights(s_col, k_factor, fac, 8.f - m, full, t0, lim, low, there, w, sum);
           }
-          l2 = add2(l2, sum);
-#pragma unroll
-          for (int c = 0; c < KT / 2; c += 16) tmem_st16(s_col + c, w + c);
-          if (v_ref & 256u)
+          weights<KT>(s_col, k_factor, fac, 8.f - m, l2);    // (times 2^8)
+          if (bars->v_ref[b] & 256u)
             for (int i = 0; i < KT; ++i) {
               const int at = t0 + i;
-              if (at <= lim && at >= low) nan_blocks |= (uint32_t)bars->v_nan[b][0][i] | bars->v_nan[b][1][i];
+              if (at <= lim && at >= low) nan_blocks |= (uint32_t)bars->v_nan[b][0][i] | (NB == 8 ? bars->v_nan[b][1][i] : 0u);
             }
           tmem_st_wait();
         }
         tc_fence_before();
         __syncwarp();
-        if (elect_one()) mbar_arrive(&bars->p_full[tile][tj & 1]);     // (a warp may be a step ahead of another: a barrier for each buffer)
+        if (elect_one()) mbar_arrive(&bars->p_full[tile][tj % SB]);    // (a warp may be a step ahead of another: a barrier for each buffer)
         ++tj;
       }
       if (!ok) break;
       if (!tile_real) continue;
       // ---- out
-      if (!CAT_WAIT(&bars->pv_done[tile][(tj - 1) & 1], ((tj - 1) >> 1) & 1)) break;
+      if (!CAT_WAIT(&bars->pv_done[tile][(tj - 1) % SB], (tj - 1) / SB & 1)) break;
       tc_fence_after();
       if (any_real) {
         const float l = l2.x + l2.y;
@@ -584,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   } else if (warp >= kKeyWarp0 && warp < kMmaWarp) {
     // ---------------------------------------------------------------- keys and values to float16
     const bool values = warp >= kValueWarp0;
-    const int w = (warp - kKeyWarp0) & 3, row = (w & 1) * 32 + lane, half = w >> 1, first_block = NB == 8 ? half * 4 : 0;
+    const int w = (warp - kKeyWarp0) & 3, row = NB == 8 ? (w & 1) * 32 + lane : w * 32 + lane, half = NB == 8 ? w >> 1 : 0, first_block = NB == 8 ? half * 4 : 0;
     int ref = kLowR;
     while (ok && walk.next<NB>(a)) {
       if (values) ref = kLowR;                           // (O begins anew)
@@ -621,12 +680,11 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
             all |= v & 256u;
             ref = max(ref, (int)(v & 255u));
           }
+#pragma unroll
+          for (int i = 0; i < kHere; ++i) scale[i] = on && bytes[i] != 255 ? half_scale(bytes[i], ref) : half_scale(-1000, 0);
           if (jj >= kBufs && !CAT_WAIT(&bars->v_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
           bars->v_nan[b][half][row] = (uint8_t)nan;
           if (w == 0 && lane == 0) bars->v_ref[b] = (uint32_t)ref | all;
-#pragma unroll
-          for (int i = 0; i < kHere; ++i) scale[i] = on && bytes[i] != 255 ? half_scale(bytes[i], ref) : half_scale(-1000, 0);
-          unpack_half<NB, true>(raw, smem + C::kOffV + b * C::kTile, row, half, scale);
         } else {
           // (d = 256: the two halves' largest differ; the keys' reference is of all their blocks)
           uint32_t whole = most;
@@ -640,16 +698,16 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
             whole = max(whole, __reduce_max_sync(0xFFFFFFFFu, m));
           }
           const int kref = max((int)whole, kLowR);
-          if (jj >= kBufs && !CAT_WAIT(&bars->k_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
 #pragma unroll
           for (int i = 0; i < kHere; ++i) {
             scale[i] = on ? half_scale(bytes[i], kref) : half_scale(-1000, 0);
             if (bytes[i] == 255) scale[i] = __half2half2(__ushort_as_half(0x7FFF));
           }
-          if (lane == 0 && half == 0) bars->k_factor[jj & 7][w & 1] = __uint_as_float((uint32_t)(kref - 12) << 23);
+          if (jj >= kBufs && !CAT_WAIT(&bars->k_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
+          if (lane == 0 && half == 0) bars->k_factor[jj & 7][row / 32] = __uint_as_float((uint32_t)(kref - 12) << 23);
           if (w == 0 && lane == 0) bars->there[jj & 7] = there;
-          unpack_half<NB, false>(raw, smem + C::kOffK + b * C::kTile, row, half, scale);
         }
+        unpack_row<NB>(raw, smem + (values ? C::kOffV : C::kOffK) + b * C::kTile, row, half, values, scale);
         fence_proxy_async_smem();
         __syncwarp();
         if (elect_one()) {
@@ -662,49 +720,55 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
     // ---------------------------------------------------------------- MMAs
     constexpr uint32_t kScores = idesc_f16(KT, false), kOut = idesc_f16(D, true);
     uint32_t units = 0, tj[2] = {0, 0};
+    // (in loops, not in line: this warp's code is not in the instruction cache when its turn comes)
     auto scores = [&](int tile, uint32_t j, uint32_t buffer) {
-      const uint32_t qb = smem_u32(smem + tile * C::kQ), kb = smem_u32(smem + C::kOffK + (j & (kBufs - 1)) * C::kTile);
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk)
-        mma_ss(tmem + (tile * 2 + buffer) * KT, sdesc_kmajor_sw128(qb + (kk >> 2) * (128 * 128) + (kk & 3) * 32),
-               sdesc_kmajor_sw128(kb + (kk >> 2) * (KT * 128) + (kk & 3) * 32), kScores, kk != 0);
+      uint64_t qd = sdesc_kmajor_sw128(smem_u32(smem + tile * C::kQ)), kd = sdesc_kmajor_sw128(smem_u32(smem + C::kOffK + (j & (kBufs - 1)) * C::kTile));
+      const uint32_t to = tmem + (tile * SB + buffer) * KT;
+#pragma unroll 1
+      for (int kk = 0; kk < D / 16; ++kk) {              // (16 channels are 32 bytes of a row)
+        mma_ss(to, qd, kd, kScores, kk);
+        qd += (kk & 3) == 3 ? 128 * 128 / 16 - 6 : 2;
+        kd += (kk & 3) == 3 ? KT * 128 / 16 - 6 : 2;
+      }
       mma_commit(&bars->s_full[tile][buffer]);
     };
     while (ok && walk.next<NB>(a)) {
       if (u.j0 == u.j1) continue;
       const int tiles = u.rows > 128 ? 2 : 1;
-      if (!CAT_WAIT(&bars->q_full, units & 1)) break;
+      if (!CAT_POLL(&bars->q_full, units & 1)) break;
       ++units;
-      for (int i = 0; i < 2 && u.j0 + i < u.j1; ++i) {   // the first two steps' scores
+#pragma unroll 1
+      for (int i = 0; i < SB && u.j0 + i < u.j1; ++i) {  // the first scores
         const uint32_t j = jj + i;
-        if (!CAT_WAIT(&bars->k_full[j & (kBufs - 1)], (j >> kBufLog) & 1)) break;
+        if (!CAT_POLL(&bars->k_full[j & (kBufs - 1)], (j >> kBufLog) & 1)) break;
         tc_fence_after();
         if (elect_one()) {
-          for (int tile = 0; tile < tiles; ++tile) scores(tile, j, (tj[tile] + i) & 1);
+#pragma unroll 1
+          for (int tile = 0; tile < tiles; ++tile) scores(tile, j, (tj[tile] + i) % SB);
           mma_commit(&bars->k_empty[j & (kBufs - 1)]);
         }
         __syncwarp();
       }
       for (int step = u.j0; step < u.j1 && ok; ++step, ++jj) {
-        const bool more = step + 2 < u.j1;
-        const uint32_t vb = jj & (kBufs - 1), ahead = jj + 2;
+        const bool more = step + SB < u.j1;
+        const uint32_t vb = jj & (kBufs - 1), ahead = jj + SB;
+#pragma unroll 1
         for (int tile = 0; tile < tiles; ++tile) {
-          if (tile == 0 && !CAT_WAIT(&bars->v_full[vb], (jj >> kBufLog) & 1)) break;
-          const uint32_t buffer = tj[tile] & 1;
-          if (!CAT_WAIT(&bars->p_full[tile][buffer], (tj[tile] >> 1) & 1)) break;
+          if (tile == 0 && !CAT_POLL(&bars->v_full[vb], (jj >> kBufLog) & 1)) break;
+          const uint32_t buffer = tj[tile] % SB;
+          if (!CAT_POLL(&bars->p_full[tile][buffer], tj[tile] / SB & 1)) break;
           tc_fence_after();
           if (elect_one()) {
-            const uint32_t v = smem_u32(smem + C::kOffV + vb * C::kTile);
+            const uint64_t vd = sdesc_mnmajor_sw128(smem_u32(smem + C::kOffV + vb * C::kTile), KT * 128);
+            const uint32_t to = tmem + C::kO + tile * D, p = tmem + (tile * SB + buffer) * KT;
 #pragma unroll
-            for (int kk = 0; kk < KT / 16; ++kk)
-              mma_ts(tmem + C::kO + tile * D, tmem + (tile * 2 + buffer) * KT + kk * 8, sdesc_mnmajor_sw128(v + kk * 2048, KT * 128), kOut,
-                     step > u.j0 || kk != 0);
+            for (int kk = 0; kk < KT / 16; ++kk) mma_ts(to, p + kk * 8, vd + kk * (2048 / 16), kOut, step > u.j0 || kk != 0);
             mma_commit(&bars->pv_done[tile][buffer]);
             if (tile == tiles - 1) mma_commit(&bars->v_empty[vb]);
           }
           __syncwarp();
           if (more) {
-            if (tile == 0 && !CAT_WAIT(&bars->k_full[ahead & (kBufs - 1)], (ahead >> kBufLog) & 1)) break;
+            if (tile == 0 && !CAT_POLL(&bars->k_full[ahead & (kBufs - 1)], (ahead >> kBufLog) & 1)) break;
             tc_fence_after();
             if (elect_one()) {
               scores(tile, ahead, buffer);
@@ -742,6 +806,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         uint32_t groups = 0;                             // of 16 tokens
         for (int i = 0; i < copies; ++i)
           if (have >> i & 1) groups |= ((1u << (most / 16)) - 1u) << (i * (most / 16));
+#pragma unroll 1
         for (int kind = 0; kind < 2; ++kind) {
           const uint32_t ring = kind ? C::kRingV : C::kRingK, st = (kind ? C::kRingK : 0) + jj % ring;
           if (jj >= ring && !CAT_WAIT(&bars->raw_empty[st], (jj / ring - 1) & 1)) break;
@@ -771,6 +836,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
     }
   }
 #undef CAT_WAIT
+#undef CAT_POLL
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
