@@ -30,7 +30,7 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStep = 32;                   // tokens a warp takes at once (two of the products' 16)
-constexpr int kUnitCost = 2;                // a unit's beginning and end, in steps
+constexpr int kUnitCost = 10;                // a unit's beginning and end, in steps
 constexpr int kAhead = kStep * kWarps;      // tokens between a warp's steps
 constexpr int kLeastPiece = 4;              // steps a CTA is worth
 constexpr int kLowR = 40;                   // least reference exponent of the values (below it they count less bits)
@@ -136,6 +136,15 @@ __device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t* w) {
     load_words<NB / 4>(p, w);
 }
 
+__device__ __forceinline__ bool short_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int site) {
+#pragma unroll 1
+  for (int n = 0; !mbar_try_wait(bar, parity); ++n)
+    if (n > (1 << 20) || *abort) {
+      if (*abort == 0) *abort = site;
+      return false;
+    }
+  return true;
+}
 // What a CTA keeps.  A warp's region is its ring of steps (the codes of 32 tokens' keys, of their values, their scales), and then what it
 // hands on of its rows.
 template <int NB, int NT, int RESIDENT>
@@ -377,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
 
     for (; step < step1; step += kWarps, tok += kAhead) {
       issue(step + (kStages - 1) * kWarps, tok + (kStages - 1) * kAhead);
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&full[get], get_round & 1, &abort_flag, __LINE__))) break;
+      if (!__all_sync(0xFFFFFFFFu, short_wait(&full[get], get_round & 1, &abort_flag, __LINE__))) break;
       const uint8_t* st = ring + get * L::kStage;
       const int here = has[warp][get];
       uint32_t own[(NB + 3) / 4];                        // a token's values' scales
@@ -621,7 +630,7 @@ struct Form {
 };
 Form form_of(int64_t n, int64_t seqs, int64_t group, int64_t d) {
   const int64_t rows = (n + seqs - 1) / seqs * group;    // of a sequence, on average
-  const int nt = rows <= 8 ? 1 : 2;
+  const int nt = rows <= 8 ? 1 : rows <= 16 || d == 256 ? 2 : 3;
   return {nt, nt * d <= 128 ? 4 : nt * d <= 256 ? 3 : 2};
 }
 
@@ -629,12 +638,13 @@ Form form_of(int64_t n, int64_t seqs, int64_t group, int64_t d) {
 // offsets) the first does all, with one sequence or many heads on a key head it is known which is the better one for all, and else
 // either leaves the other's sequences out (an empty launch of the second costs a decode step some 5 us).
 struct Needs {
+  int most;                                 // rows of a sequence and key head up to which the first kernel is the faster
   bool few, tiles;
-  Needs(int64_t n, int64_t seqs, int64_t group) {
-    tiles = group > kMostFewRows || (n > seqs && n * group > kMostFewRows);
-    few = !tiles || (group <= kMostFewRows && seqs > 1);
+  Needs(int64_t n, int64_t seqs, int64_t group, int64_t d) : most(d == 256 ? 16 : 24) {
+    tiles = group > most || (n > seqs && n * group > most);
+    few = !tiles || (group <= most && seqs > 1);
   }
-  int most_few() const { return few ? tiles ? kMostFewRows : 0x7FFFFFFF : 0; }
+  int most_few() const { return few ? tiles ? most : 0x7FFFFFFF : 0; }
 };
 
 template <int NB, int NT, int RESIDENT>
@@ -671,7 +681,7 @@ int64_t mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv,
   if (sms < 0) return -1;
   const int64_t group = hq / hkv;
   const Form f = form_of(n, seqs, group, d);
-  const Needs needs(n, seqs, group);
+  const Needs needs(n, seqs, group, d);
   size_t bytes = 0;
   if (needs.few) bytes += Parts((size_t)sms * f.resident, 8 * f.nt, d).bytes;
   if (needs.tiles) bytes += Parts(sms, attention_tile_rows(d), d).bytes;
@@ -695,7 +705,7 @@ cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint
   a.scale = scale * 1.44269504f;
   a.status = status, a.window = window, a.out = out, a.out_f32 = out_dtype == 0;
   const Form f = form_of(n, seqs, a.group, d);
-  const Needs needs(n, seqs, a.group);
+  const Needs needs(n, seqs, a.group, d);
   a.few = needs.most_few();
   const Parts parts((size_t)sms * f.resident, 8 * f.nt, d), tiles(sms, attention_tile_rows(d), d);
   cudaError_t e = cudaSuccess;
@@ -708,8 +718,8 @@ cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint
   }
   parts.place(&a, workspace);
   const int grid = sms * f.resident;
-  if (d == 64) return f.nt == 1 ? run<2, 1, 4>(a, grid, stream) : run<2, 2, 4>(a, grid, stream);
-  if (d == 128) return f.nt == 1 ? run<4, 1, 4>(a, grid, stream) : run<4, 2, 3>(a, grid, stream);
+  if (d == 64) return f.nt == 1 ? run<2, 1, 4>(a, grid, stream) : f.nt == 2 ? run<2, 2, 4>(a, grid, stream) : run<2, 3, 3>(a, grid, stream);
+  if (d == 128) return f.nt == 1 ? run<4, 1, 4>(a, grid, stream) : f.nt == 2 ? run<4, 2, 3>(a, grid, stream) : run<4, 3, 2>(a, grid, stream);
   return f.nt == 1 ? run<8, 1, 3>(a, grid, stream) : run<8, 2, 2>(a, grid, stream);
 }
 

@@ -6,7 +6,6 @@
 namespace cat {
 
 constexpr float kSlack = 6.f;               // a row's scores may exceed its running maximum by this (binary orders) before it follows
-constexpr int kMostFewRows = 16;            // rows of a sequence and key head (tokens x group) up to which it is of few rows
 
 // A CTA's piece that begins a unit (sequence, row tile, head) which others go on with.
 struct Plan {

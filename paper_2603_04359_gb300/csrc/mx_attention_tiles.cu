@@ -35,7 +35,7 @@ namespace {
 
 constexpr int kThreads = 576;
 constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
-constexpr int kUnitCost = 384;              // a unit's beginning and end, in tokens
+constexpr int kUnitCost = 768;              // a unit's beginning and end, in tokens
 constexpr int kLeastPiece = 1024;           // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
 constexpr uint32_t kTmemCols = 512;
@@ -83,16 +83,28 @@ struct Unit {
   int64_t p0;                               // the token of the sequence's first row
   int64_t t0, t1;                           // the tokens that some row sees
   int64_t end;                              // where the unit ends on the line
+  int begin;                                // the sequence's first row,
+  int64_t tokens;                           // and one past its last token in the cache
 };
 struct Walk {
-  int s;
-  int64_t at, left, to;
+  int s, rt, h;                             // the next unit,
+  int64_t place, left, to;                  // where in it; what is left of the piece, and its end
   Seq q;
   Unit u;
   template <int NB>
-  __device__ __forceinline__ void begin(const AttnArgs& a, int s_, int64_t at_, int64_t from, int64_t to_) {
-    s = s_, at = at_, left = to_ - from, to = to_;
+  __device__ __forceinline__ void begin(const AttnArgs& a, int s_, int64_t at, int64_t from, int64_t to_) {
+    s = s_, left = to_ - from, to = to_;
     q = seq_at<Tc<NB>::ROWS>(a, s_);
+    int lo = 0, hi = q.tiles - 1;                        // the last tile that begins at `at` or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (a.c.hkv * q.before(mid) <= at)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    const int64_t in = at - a.c.hkv * q.before(lo), length = q.a + q.b * lo;
+    rt = lo, h = (int)(in / length), place = in - h * length;
   }
   // A whole warp: the next unit with something to do.
   template <int NB>
@@ -109,41 +121,39 @@ struct Walk {
     using C = Tc<NB>;
     constexpr int KT = C::KT;
     while (left > 0) {
-      int64_t all = a.c.hkv * q.before(q.tiles);
-      while (at >= all) {
-        at -= all;
-        q = seq_at<C::ROWS>(a, ++s);
-        all = a.c.hkv * q.before(q.tiles);
-      }
-      int lo = 0, hi = q.tiles - 1;                      // the last tile that begins at `at` or before
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (a.c.hkv * q.before(mid) <= at)
-          lo = mid;
-        else
-          hi = mid - 1;
-      }
-      const int64_t length = q.a + q.b * lo, in = at - a.c.hkv * q.before(lo);
-      const int64_t h = in / length, place = in - h * length, end = place + left < length ? place + left : length;
-      u.s = s, u.h = (int)h, u.rt = lo;
-      u.rows = (int)min((int64_t)C::ROWS, (int64_t)q.ql * a.group - (int64_t)lo * C::ROWS);
-      const int64_t first_row = (int64_t)lo * C::ROWS / a.group, last_row = ((int64_t)lo * C::ROWS + u.rows - 1) / a.group;
+      const int64_t length = q.a + q.b * rt, end = place + left < length ? place + left : length;
+      const uint32_t group = (uint32_t)a.group, row0 = (uint32_t)rt * C::ROWS;
+      u.s = s, u.h = h, u.rt = rt;
+      u.rows = (int)min((int64_t)C::ROWS, (int64_t)q.ql * a.group - (int64_t)row0);
       u.p0 = q.len - q.ql;
-      const int64_t p_first = u.p0 + first_row, p_last = u.p0 + last_row;
+      const int64_t p_first = u.p0 + row0 / group, p_last = u.p0 + (row0 + (uint32_t)u.rows - 1) / group;
       const int64_t t1 = p_last + 1 < q.end ? p_last + 1 : q.end, t0 = a.window && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
-      u.t0 = t0, u.t1 = t1;
+      u.t0 = t0, u.t1 = t1, u.begin = q.begin, u.tokens = q.end;
       const int first = (int)(t0 / KT), steps = t1 > t0 ? (int)((t1 + KT - 1) / KT) - first : 0;
-      const int x0 = (int)(place * steps / length), x1 = (int)(end * steps / length);
+      // (any growing map of the line to steps will do that is the same for all: in float32)
+      auto step_of = [&](int64_t x) { return x == length ? steps : min((int)((float)x / (float)length * (float)steps), steps); };
+      const int x0 = step_of(place), x1 = step_of(end);
       u.j0 = first + x0, u.j1 = first + x1;
       u.starts = x0 == 0;
       u.whole = u.starts && x1 == steps;
       u.nothing = steps == 0;
       const bool cleared = u.nothing && place == 0;
-      // a unit's last piece may have no step (it lies in the last step's part of the line): its part is marked empty
+      // a unit's later piece may have no step: its part is marked empty
       const bool empty_part = x0 == x1 && x0 > 0;
-      at += end - place;
       left -= end - place;
       u.end = to - left + (length - end);
+      place = end;
+      if (end == length) {                               // the next unit
+        place = 0;
+        if (++h == a.c.hkv) {
+          h = 0;
+          if (++rt == q.tiles && left > 0) {
+            rt = 0;
+            do q = seq_at<C::ROWS>(a, ++s);
+            while (q.tiles == 0);
+          }
+        }
+      }
       if (x1 > x0 || cleared || empty_part) return true;
     }
     return false;
@@ -492,10 +502,9 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         p.last = (int)(last < rest * (each + 1) ? last / (each + 1) : rest + (last - rest * (each + 1)) / each);
         a.plan[cta] = p;
       }
-      const Seq& q = walk.q;
-      const int64_t rr = (int64_t)u.rt * ROWS + r;
-      const int j = (int)(rr / a.group);
-      const int64_t row = ((int64_t)(q.begin + j) * a.hq + u.h * a.group + (rr - (int64_t)j * a.group)) * D;
+      const uint32_t rr = (uint32_t)u.rt * ROWS + r;     // (a sequence has less than 2^31 rows)
+      const int j = (int)(rr / (uint32_t)a.group);
+      const int64_t row = ((int64_t)(u.begin + j) * a.hq + u.h * a.group + (int)(rr - (uint32_t)j * (uint32_t)a.group)) * D;
       const bool real = r < u.rows;
       const int slot = 2 * cta + (u.starts ? 1 : 0);
       if (u.j0 == u.j1) {                                // no tokens: rows of zeros, or an empty part
@@ -506,41 +515,46 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         }
         continue;
       }
-      // the row to float16, its largest channel in [2^13, 2^14); a negative scale goes into its sign
+      // The warp's rows to float16, a row's largest channel in [2^13, 2^14); a negative scale goes into its sign.  All of them on their
+      // way at once, to where they are then rewritten; D / 8 lanes a row.
       float fac;
       {
-        // (the row is read twice, the second time from L1; eight pieces on their way at once: a unit begins with this)
-        const uint4* from_q = reinterpret_cast<const uint4*>(a.q + row);
-        uint32_t most = 0;
-        if (real)
+        constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+        const int piece = lane % kLanes, warp_row = tile * 128 + (warp & 3) * 32;
+        uint8_t* const to_q = smem + tile * C::kQ + (piece >> 3) * (128 * 128) + (warp & 3) * (32 * 128);
+        auto place = [&](int at) { return to_q + at * 128 + (((piece & 7) ^ (at & 7)) << 4); };
+        __syncwarp();                                    // (what was there has been read)
 #pragma unroll 1
-          for (int c = 0; c < D / 8; c += 8) {
-            uint4 v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __ldg(from_q + c + i);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t m = __vmaxu2(__vmaxu2(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), __vmaxu2(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu));
-              most = max(most, max(m & 0xFFFFu, m >> 16));
-            }
-          }
-        const int e = max((int)(most >> 7), 1);
-        const float up = (e >= 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23)) * (a.scale < 0.f ? -1.f : 1.f);
-        auto half2_of = [&](uint32_t w) {
-          return e == 255 ? 0x7FFF7FFFu : f16_pair(__uint_as_float(w << 16) * up * 0x1p13f, __uint_as_float(w & 0xFFFF0000u) * up * 0x1p13f);
-        };
-        uint8_t* to_q = smem + tile * C::kQ + (r & 127) * 128;
-#pragma unroll 1
-        for (int c = 0; c < D / 8; c += 4) {
-          uint4 v[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = real ? __ldg(from_q + c + i) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(to_q + (c >> 3) * (128 * 128) + ((((c & 7) + i) ^ (r & 7)) << 4)) =
-                make_uint4(half2_of(v[i].x), half2_of(v[i].y), half2_of(v[i].z), half2_of(v[i].w));
+        for (int i = 0; i < 32; i += kAtOnce) {
+          const int at = i + lane / kLanes;
+          const int64_t from_q = __shfl_sync(0xFFFFFFFFu, row, at);
+          const bool in = warp_row + at < u.rows;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(place(at))), "l"(a.q + (in ? from_q + piece * 8 : 0)), "r"(in ? 16 : 0)
+                       : "memory");
         }
-        fac = ldexpf(fabsf(a.scale), e - 140);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+        const float sign = a.scale < 0.f ? -1.f : 1.f;
+        int mine = 1;                                    // this thread's row's exponent
+#pragma unroll 1
+        for (int i = 0; i < 32; i += kAtOnce) {
+          const int at = i + lane / kLanes;
+          uint4* const p = reinterpret_cast<uint4*>(place(at));
+          const uint4 v = *p;
+          const uint32_t m2 = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+          uint32_t most = max(m2 & 0xFFFFu, m2 >> 16);
+#pragma unroll
+          for (int k = 1; k < kLanes; k <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, k));
+          const int e = max((int)(most >> 7), 1);
+          const int theirs = __shfl_sync(0xFFFFFFFFu, e, (lane % kAtOnce) * kLanes);
+          if (lane / kAtOnce == i / kAtOnce) mine = theirs;
+          const float up = (e >= 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23)) * sign;
+          auto half2_of = [&](uint32_t w) {
+            return e == 255 ? 0x7FFF7FFFu : f16_pair(__uint_as_float(w << 16) * up * 0x1p13f, __uint_as_float(w & 0xFFFF0000u) * up * 0x1p13f);
+          };
+          *p = make_uint4(half2_of(v.x), half2_of(v.y), half2_of(v.z), half2_of(v.w));
+        }
+        fac = ldexpf(fabsf(a.scale), mine - 140);
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -548,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       if (!CAT_WAIT(&bars->q_full, units & 1)) break;    // (nobody is at the next unit's queries before all are at this one's)
       ++units;
       const int64_t p = u.p0 + j;
-      const int lim = real ? (int)(p < q.end - 1 ? p : q.end - 1) : 0x7FFFFFFF;
+      const int lim = real ? (int)(p < u.tokens - 1 ? p : u.tokens - 1) : 0x7FFFFFFF;
       const int low = real && a.window && p - a.window + 1 > 0 ? (int)(p - a.window + 1) : 0;
       const bool tile_real = tile * 128 < u.rows, any_real = __any_sync(0xFFFFFFFFu, real);
       float m = 0.f;
@@ -617,24 +631,36 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         const float l = l2.x + l2.y;
         float unref = ldexpf(1.f, ref - 139);
         if (u.whole) unref = l == 0.f ? 0.f : ldexpf(1.f / l, ref - 139);
-        float* part = a.parts + ((int64_t)slot * ROWS + r) * D;
+        // 32 channels of the warp's rows at a time through the place of its queries, whose products are done: eight lanes a row
+        uint8_t* stage = smem + tile * C::kQ + (warp & 3) * (32 * 128);
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t v[32];
           CAT_TMEM_LD32(o_col + c, v);
-          tmem_ld_wait();
+          tmem_have32(v);
           const bool nan = nan_blocks >> (c / 32) & 1;
-          if (real)
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-              float4 o = make_float4(__uint_as_float(v[i]) * unref, __uint_as_float(v[i + 1]) * unref, __uint_as_float(v[i + 2]) * unref,
-                                     __uint_as_float(v[i + 3]) * unref);
-              if (nan) o.x = o.y = o.z = o.w = __int_as_float(0x7FFFFFFF);
-              if (u.whole)
-                store4(a, row + c + i, o);
-              else
-                *reinterpret_cast<float4*>(part + c + i) = o;
+          for (int i = 0; i < 32; i += 4) {
+            float4 o = make_float4(__uint_as_float(v[i]) * unref, __uint_as_float(v[i + 1]) * unref, __uint_as_float(v[i + 2]) * unref,
+                                   __uint_as_float(v[i + 3]) * unref);
+            if (nan) o.x = o.y = o.z = o.w = __int_as_float(0x7FFFFFFF);
+            *reinterpret_cast<float4*>(stage + lane * 128 + (((i / 4) ^ (lane & 7)) << 4)) = o;
+          }
+          __syncwarp();
+#pragma unroll 1
+          for (int i = lane >> 3; i < 32; i += 4) {
+            const int at = tile * 128 + (warp & 3) * 32 + i;
+            const float4 o = *reinterpret_cast<const float4*>(stage + i * 128 + (((lane & 7) ^ (i & 7)) << 4));
+            const int64_t to_out = __shfl_sync(0xFFFFFFFFu, row, i);
+            if (at < u.rows) {
+              if (u.whole) {
+                store4(a, to_out + c + 4 * (lane & 7), o);
+              } else {
+                *reinterpret_cast<float4*>(a.parts + ((int64_t)slot * ROWS + at) * D + c + 4 * (lane & 7)) = o;
+              }
             }
+          }
+          __syncwarp();
         }
         if (real && !u.whole) *reinterpret_cast<float2*>(a.ml + ((int64_t)slot * ROWS + r) * 2) = make_float2(m, l);
       }
@@ -794,7 +820,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       const int64_t page_bytes = 2 * a.c.hkv * a.c.part;
       auto page_of = [&](int step) {                     // of this lane's tokens, -1: none
         const int t0 = step * KT + lane * most;
-        if (lane >= copies || step >= u.j1 || t0 >= walk.q.end) return -1;
+        if (lane >= copies || step >= u.j1 || t0 >= u.tokens) return -1;
         const int pg = __ldg(pages + (t0 >> a.c.page_log));
         return pg < 0 || pg >= a.pages ? -1 : pg;
       };
