@@ -9,7 +9,7 @@
 namespace cat {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kFlatBlocks = 16;             // most blocks an SM of a grid-stride loop
 
 __device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
@@ -54,6 +54,24 @@ __device__ __forceinline__ float row_sum(float s) {
   return s + __shfl_xor_sync(0xFFFFFFFFu, s, 2);
 }
 
+// Two float32 operations at once.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void apart(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // A row's quarter in the 4-bit form: NB words, and the row's NB scale bytes (each lane has all).
 template <int NB>
 struct Codes {
@@ -61,6 +79,15 @@ struct Codes {
   __device__ __forceinline__ void set_scale(int b, uint32_t byte) {
     if (b % 4 == 0) s[b / 4] = 0u;
     s[b / 4] |= byte << (8 * (b & 3));
+  }
+  // (any b)
+  __device__ __forceinline__ void replace(int b, uint32_t codes, uint32_t byte) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+      if (i == b) {
+        w[i] = codes;
+        s[i / 4] = (s[i / 4] & ~(0xFFu << (8 * (i & 3)))) | byte << (8 * (i & 3));
+      }
   }
   __device__ __forceinline__ uint32_t scale(int b) const { return s[b / 4] >> (8 * (b & 3)) & 0xFFu; }
   // Values' pieces are halfwords: a quarter is the low halves of all words, then the high ones.
@@ -312,25 +339,57 @@ __device__ __forceinline__ float sticky(double v) {
   return (double)f == v || !isfinite(v) ? f : __uint_as_float(__float_as_uint(f) | 1u);
 }
 
-// A key's quarter in float64, all of it read again.  Whole warps; lanes without a key (on = false) take part in the shuffles only.
+// a + b as a sum and its error
+__device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
+  s = __fadd_rn(a, b);
+  const float t = __fsub_rn(s, a);
+  e = __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t));
+}
+
+// A key's quarter of the blocks in `blocks` (the same in all lanes) from its exact values, read again and computed in float64: some
+// hundred operations of it, whose rate is 1/64 of float32's, so that the squares are summed in pairs of float32 (to some 2^-45) and no
+// more blocks are done than have to be.  Whole warps; lanes without a key (on = false) take part in the shuffles only.
 template <typename T, int NB>
 __device__ __noinline__ void exact_key(const RopeArgs& a, const T* x, const void* weight, bool neighbours, int64_t pos, bool valid,
-                                       bool on, int p, Codes<NB>* out) {
+                                       bool on, int p, uint32_t blocks, Codes<NB>* out) {
   float f[8], w[8], g[8];
-  double r = 1.0, sq = 0.0;
-  if (on && weight)
+  double r = 1.0;
+  if (__any_sync(0xFFFFFFFFu, on && weight)) {
+    double sum = 0.0;
+    if (on && weight) {
+      float hi = 0.f, lo = 0.f;
+      bool odd = false;                                  // squares that leave the range where the errors are exact
 #pragma unroll 1
-    for (int b = 0; b < NB; ++b) {
-      load8(x + 32 * b + 8 * p, f);
+      for (int b = 0; b < NB; ++b) {
+        load8(x + 32 * b + 8 * p, f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sq += (double)f[i] * (double)f[i];
+        for (int i = 0; i < 8; ++i) {
+          const float sq = __fmul_rn(f[i], f[i]), low = __fmaf_rn(f[i], f[i], -sq);
+          float e;
+          odd |= f[i] != 0.f && !(sq > 0x1p-100f && sq < 0x1p100f);
+          two_sum(hi, sq, hi, e);
+          lo = __fadd_rn(lo, __fadd_rn(e, low));
+        }
+      }
+      sum = (double)hi + (double)lo;
+      if (odd) {
+        sum = 0.0;
+#pragma unroll 1
+        for (int b = 0; b < NB; ++b) {
+          load8(x + 32 * b + 8 * p, f);
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) sum += (double)f[i] * (double)f[i];
+        }
+      }
     }
-  sq = row_sum(sq);
-  if (weight) r = 1.0 / sqrt(sq / (32 * NB) + a.eps);
+    sum = row_sum(sum);
+    if (weight) r = 1.0 / sqrt(sum / (32 * NB) + a.eps);
+  }
 #pragma unroll 1
   for (int b = 0; b < NB; ++b) {
+    if (!(blocks >> b & 1u)) continue;
     const int c = 32 * b + 8 * p;
-    double y[8], most = 0.0;
+    double y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = 0.0;
     if (on) {
@@ -339,7 +398,7 @@ __device__ __noinline__ void exact_key(const RopeArgs& a, const T* x, const void
       for (int i = 0; i < 8; ++i) w[i] = 1.f;
       if (weight) load_weight8(a, weight, c, w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = (double)f[i] * r * (double)(weight ? w[i] : 1.f);
+      for (int i = 0; i < 8; ++i) y[i] = weight ? (double)f[i] * (double)w[i] : (double)f[i];
       if (c < a.rot && valid) {
         float co[8], si[8];
         double z[8];
@@ -353,32 +412,156 @@ __device__ __noinline__ void exact_key(const RopeArgs& a, const T* x, const void
           load8(x + o, g);
           if (weight) load_weight8(a, weight, o, w);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) z[i] = (double)g[i] * r * (double)(weight ? w[i] : 1.f);
+          for (int i = 0; i < 8; ++i) z[i] = weight ? (double)g[i] * (double)w[i] : (double)g[i];
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = y[i] * (double)co[i] + z[i] * (double)si[i];
       }
+      if (weight)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] *= r;
       if (!valid)
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = __longlong_as_double(0x7FF8000000000000ll);
     }
-    bool fine = true;
+    // magnitudes as integers compare like the numbers
+    int64_t big = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      fine &= isfinite(y[i]) != 0;
-      most = fmax(most, fabs(y[i]));
+      const int64_t m = __double_as_longlong(y[i]) & 0x7FFFFFFFFFFFFFFFll;
+      big = m > big ? m : big;
     }
-    most = fmax(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-    most = fmax(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-    const uint32_t odd = __ballot_sync(0xFFFFFFFFu, !fine) >> (threadIdx.x & 28) & 15u;
-    // floor(log2 most) + 125: of a double's exponent field 1023 + e
-    const int e = (int)(__double_as_longlong(most) >> 52) - 1023 + 125;
-    const uint32_t byte = odd || e > 254 ? 255u : e > 0 ? (uint32_t)e : 0u;
+    const int64_t o1 = __shfl_xor_sync(0xFFFFFFFFu, big, 1);
+    big = o1 > big ? o1 : big;
+    const int64_t o2 = __shfl_xor_sync(0xFFFFFFFFu, big, 2);
+    big = o2 > big ? o2 : big;
+    // floor(log2 most) + 125: of a double's exponent field 1023 + e (2047: not finite)
+    const int e = (int)(big >> 52) - 1023 + 125;
+    const uint32_t byte = e > 254 ? 255u : e > 0 ? (uint32_t)e : 0u;
     float u[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = byte == 255u ? 0.f : sticky(y[i] * __longlong_as_double((int64_t)(1150 - (int)byte) << 52));
-    out->w[b] = byte == 255u ? 0u : mx_pack8(u);
-    out->set_scale(b, byte);
+    const uint32_t codes = byte == 255u ? 0u : mx_pack8(u);
+    if (on) out->replace(b, codes, byte);
+  }
+}
+
+// A number as the sum of two float32, the second some units of the first at most.
+struct Pair {
+  float h, l;
+};
+__device__ __forceinline__ Pair product(float a, float b) {
+  const float h = __fmul_rn(a, b);
+  return {h, __fmaf_rn(a, b, -h)};
+}
+__device__ __forceinline__ Pair times(Pair a, float b) {
+  const float h = __fmul_rn(a.h, b);
+  return {h, __fmaf_rn(a.l, b, __fmaf_rn(a.h, b, -h))};
+}
+__device__ __forceinline__ Pair times(Pair a, Pair b) {
+  const float h = __fmul_rn(a.h, b.h);
+  return {h, __fmaf_rn(a.h, b.l, __fmaf_rn(a.l, b.h, __fmaf_rn(a.h, b.h, -h)))};
+}
+__device__ __forceinline__ Pair plus(Pair a, Pair b) {
+  Pair s;
+  float e;
+  two_sum(a.h, b.h, s.h, e);
+  e = __fadd_rn(e, __fadd_rn(a.l, b.l));
+  const float h = __fadd_rn(s.h, e);
+  return {h, __fsub_rn(e, __fsub_rn(h, s.h))};
+}
+// The float32 that rounds, and compares with powers of two, as the pair does: the nearest, moved by a unit toward the rest's side where
+// that could be a border (few bits of the significand are set).
+__device__ __forceinline__ float nudged(Pair v) {
+  const float h = __fadd_rn(v.h, v.l), l = __fsub_rn(v.l, __fsub_rn(h, v.h));
+  const uint32_t u = __float_as_uint(h);
+  if ((u & 0xFFFFu) != 0u || l == 0.f || h == 0.f) return h;
+  return __uint_as_float((l > 0.f) == (h > 0.f) ? u + 1u : u - 1u);
+}
+
+// exact_key for values of ordinary sizes, in pairs of float32: to some 2^-43 of |y co| + |y' si|, where float64's few and slow units
+// took 6 us for a key (999 tokens of 48 heads without a norm: 12 us with them, 6 without any such key).
+template <typename T, int NB>
+__device__ __noinline__ void near_key(const RopeArgs& a, const T* x, const void* weight, bool neighbours, int64_t pos, bool on, int p,
+                                      uint32_t blocks, Codes<NB>* out) {
+  float f[8], w[8];
+  Pair r = {1.f, 0.f};
+  if (__any_sync(0xFFFFFFFFu, on && weight)) {
+    Pair sum = {0.f, 0.f};
+    if (on && weight)
+#pragma unroll 1
+      for (int b = 0; b < NB; ++b) {
+        load8(x + 32 * b + 8 * p, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const Pair q = product(f[i], f[i]);
+          float e;
+          two_sum(sum.h, q.h, sum.h, e);
+          sum.l = __fadd_rn(sum.l, __fadd_rn(e, q.l));
+        }
+      }
+#pragma unroll
+    for (int k = 1; k < 4; k <<= 1) {
+      const Pair other = {__shfl_xor_sync(0xFFFFFFFFu, sum.h, k), __shfl_xor_sync(0xFFFFFFFFu, sum.l, k)};
+      sum = plus(sum, other);
+    }
+    if (weight) {
+      // m to the power -1/2: the rounded root, and a step of Newton's from it
+      const float eps = (float)a.eps;
+      const Pair m = plus({sum.h * (1.f / (32 * NB)), sum.l * (1.f / (32 * NB))}, {eps, (float)(a.eps - (double)eps)});
+      const float r0 = __frsqrt_rn(m.h);
+      const Pair t = times(product(r0, r0), m);
+      r = {r0, 0.5f * r0 * __fsub_rn(__fsub_rn(1.f, t.h), t.l)};
+    }
+  }
+#pragma unroll 1
+  for (int b = 0; b < NB; ++b) {
+    if (!(blocks >> b & 1u)) continue;
+    const int c = 32 * b + 8 * p;
+    Pair y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = {0.f, 0.f};
+    if (on) {
+      load8(x + c, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = 1.f;
+      if (weight) load_weight8(a, weight, c, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = product(f[i], weight ? w[i] : 1.f);
+      if (c < a.rot) {
+        float co[8], si[8];
+        if (neighbours) {
+          turn_factors<true>(a, pos, c, co, si);
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const Pair u = y[i], v = y[i + 1];
+            y[i] = plus(times(u, co[i]), times(v, si[i]));
+            y[i + 1] = plus(times(v, co[i + 1]), times(u, si[i + 1]));
+          }
+        } else {
+          turn_factors<false>(a, pos, c, co, si);
+          const int o = c < a.rot / 2 ? c + a.rot / 2 : c - a.rot / 2;
+          load8(x + o, f);
+          if (weight) load_weight8(a, weight, o, w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = plus(times(y[i], co[i]), times(product(f[i], weight ? w[i] : 1.f), si[i]));
+        }
+      }
+      if (weight)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = times(y[i], r);
+    }
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(nudged(y[i])));
+    m = row_max(m);
+    const uint32_t byte = mx_scale_byte(__float_as_uint(m));
+    const float inv = mx_inverse_scale(byte);            // (finite: of ordinary sizes)
+    float u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = nudged(y[i]) * inv;
+    const uint32_t codes = mx_pack8(u);
+    if (on) out->replace(b, codes, byte);
   }
 }
 
@@ -390,7 +573,7 @@ __device__ __noinline__ void exact_key(const RopeArgs& a, const T* x, const void
 constexpr float kMargin = 20.f * 0x1p-24f;
 
 template <typename T, int NB, int PAIRS>
-__global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kThreads, NB == 8 ? 4 : 7) mx_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int D = 32 * NB;
   const int lane = threadIdx.x & 31, p = lane & 3;
   const int64_t item = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
@@ -406,7 +589,8 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(cons
   if (in && !is_q) slot = a.slots[t];
   const T* x = static_cast<const T*>(a.qkv) + (t * a.heads + head) * D;
 
-  float y[NB][8], sq[4] = {0.f, 0.f, 0.f, 0.f};
+  float y[NB][8], sq[4];
+  uint64_t sq2[2] = {0ull, 0ull};
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     if (in) {
@@ -419,7 +603,12 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(cons
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sq[i & 3] = fmaf(y[b][i], y[b][i], sq[i & 3]);
+    for (int i = 0; i < 8; i += 2) {
+      const uint64_t v = two(y[b][i], y[b][i + 1]);
+      sq2[i / 2 & 1] = fma2(v, v, sq2[i / 2 & 1]);
+    }
+  apart(sq2[0], sq[0], sq[1]);
+  apart(sq2[1], sq[2], sq[3]);
   const float mean = row_sum((sq[0] + sq[1]) + (sq[2] + sq[3])) * (1.f / D) + (float)a.eps;
   float r = __frsqrt_rn(mean);
   // Squares that leave float32's range, though the norm does not: summed again in float64.
@@ -438,13 +627,15 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(cons
     for (int b = 0; b < NB; ++b) {
       float w[8];
       load_weight8(a, weight, 32 * b + 8 * p, w);
+      const uint64_t rr = two(r, r);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[b][i] = y[b][i] * r * w[i];
+      for (int i = 0; i < 8; i += 2) apart(mul2(mul2(two(y[b][i], y[b][i + 1]), rr), two(w[i], w[i + 1])), y[b][i], y[b][i + 1]);
     }
   }
-  float most[NB];                                        // of |y co| + |y' si|
+  float most[NB];                                        // keys: of |y co| + |y' si|
 #pragma unroll
   for (int b = 0; b < NB; ++b) most[b] = 0.f;
+  const bool keys = __any_sync(0xFFFFFFFFu, is_k);
   if (in && !is_v && valid) {
     if constexpr (PAIRS == kHalves || PAIRS == kQuarters) {
       constexpr int kApart = PAIRS == kHalves ? NB / 2 : NB / 4;
@@ -452,14 +643,20 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(cons
       for (int b = 0; b < kApart; ++b) {
         float co[8], si[8];
         turn_factors<false>(a, pos, 32 * b + 8 * p, co, si);     // (si is -sin here)
+        if (keys) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float u = y[b][i], v = y[b + kApart][i];
-          const float uc = u * co[i], vs = v * si[i], vc = v * co[i], us = u * si[i];
-          most[b] = fmaxf(most[b], fabsf(uc) + fabsf(vs));
-          most[b + kApart] = fmaxf(most[b + kApart], fabsf(vc) + fabsf(us));
-          y[b][i] = fmaf(v, si[i], uc);
-          y[b + kApart][i] = fmaf(-u, si[i], vc);
+          for (int i = 0; i < 8; ++i) {
+            const float u = y[b][i], v = y[b + kApart][i];
+            most[b] = fmaxf(most[b], fabsf(u * co[i]) + fabsf(v * si[i]));
+            most[b + kApart] = fmaxf(most[b + kApart], fabsf(v * co[i]) + fabsf(u * si[i]));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const uint64_t u = two(y[b][i], y[b][i + 1]), v = two(y[b + kApart][i], y[b + kApart][i + 1]);
+          const uint64_t c2 = two(co[i], co[i + 1]), s2 = two(si[i], si[i + 1]), n2 = two(-si[i], -si[i + 1]);
+          apart(fma2(v, s2, mul2(u, c2)), y[b][i], y[b][i + 1]);
+          apart(fma2(u, n2, mul2(v, c2)), y[b + kApart][i], y[b + kApart][i + 1]);
         }
       }
     } else {
@@ -485,16 +682,12 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(cons
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float yc = y[b][i] * co[i];
-            most[b] = fmaxf(most[b], fabsf(yc) + fabsf(z[i] * si[i]));
+            if (keys) most[b] = fmaxf(most[b], fabsf(yc) + fabsf(z[i] * si[i]));
             y[b][i] = fmaf(z[i], si[i], yc);
           }
         }
       }
     }
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) most[b] = fmaxf(most[b], fabsf(y[b][i]));
   }
   if (!valid) {
 #pragma unroll
@@ -511,34 +704,48 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 2 : 3) mx_rope_kernel(cons
   if (!__any_sync(0xFFFFFFFFu, writes)) return;
 
   Codes<NB> out;
-  bool near = odd && is_k;
+  uint32_t near = odd && is_k ? (1u << NB) - 1u : 0u;    // blocks whose codes float32's error could change
+  bool far = odd || !valid || (weight && !(mean < 0x1p100f));
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max_magnitude(m, y[b][i]);
     m = row_max(m);
-    const float all = row_max(most[b]);                  // (all lanes shuffle, whatever their heads are)
-    const float e = is_k ? all * kMargin : 0.f;
+    float e = 0.f;
+    if (keys) {                                          // (all lanes shuffle, whatever their heads are; channels that are not turned)
+      const float all = fmaxf(row_max(most[b]), m);
+      if (is_k) e = all * kMargin;
+    }
     const uint32_t byte = mx_scale_byte(__float_as_uint(m));
     const float inv = byte == 255u ? 0.f : mx_inverse_scale(byte);
-    float u[8], below[8], above[8];
+    float u[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      u[i] = y[b][i] * inv;
-      below[i] = (y[b][i] - e) * inv;
-      above[i] = (y[b][i] + e) * inv;
-    }
+    for (int i = 0; i < 8; ++i) u[i] = y[b][i] * inv;
     out.w[b] = byte == 255u ? 0u : mx_pack8(u);
     out.set_scale(b, byte);
-    // (codes that differ in their signs alone are 0 and -0)
-    near |= is_k && (byte == 255u || ((mx_pack8(below) ^ mx_pack8(above)) & 0x77777777u) != 0u ||
-                     mx_scale_byte(__float_as_uint(fmaxf(m - e, 0.f))) != byte || mx_scale_byte(__float_as_uint(m + e)) != byte);
+    if (keys) {
+      float below[8], above[8];
+      const float margin = e * inv;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        below[i] = u[i] - margin;
+        above[i] = u[i] + margin;
+      }
+      // (codes that differ in their signs alone are 0 and -0)
+      if (is_k && (byte == 255u || ((mx_pack8(below) ^ mx_pack8(above)) & 0x77777777u) != 0u ||
+                   mx_scale_byte(__float_as_uint(fmaxf(m - e, 0.f))) != byte || mx_scale_byte(__float_as_uint(m + e)) != byte))
+        near |= 1u << b;
+      // sizes at which pairs of float32 would lose bits (nothing tells what a NaN or an infinity is made of)
+      far |= is_k && !(m > 0x1p-40f && e < 0x1p40f && byte != 255u);
+    }
   }
-  if (__any_sync(0xFFFFFFFFu, near)) {
-    Codes<NB> exact;
-    exact_key<T, NB>(a, x, weight, PAIRS == kNeighbours, pos, valid, is_k, p, &exact);
-    if (is_k) out = exact;
+  const uint32_t blocks = __reduce_or_sync(0xFFFFFFFFu, near);
+  if (blocks) {
+    if (__any_sync(0xFFFFFFFFu, near && far))
+      exact_key<T, NB>(a, x, weight, PAIRS == kNeighbours, pos, valid, is_k, p, blocks, &out);
+    else
+      near_key<T, NB>(a, x, weight, PAIRS == kNeighbours, pos, is_k, p, blocks, &out);
   }
   bool bad = false;
 #pragma unroll

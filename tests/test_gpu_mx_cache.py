@@ -185,6 +185,22 @@ def test_rope_keys_next_to_borders():
         same_cache(host(cache), C.store(C.blank(n // page, 1, page, d), page, k, v, slots), page, d)
 
 
+@pytest.mark.parametrize("dtype,norm,interleaved", [("bf16", True, False), ("f32", True, True), ("f32", False, False), ("bf16", False, True)])
+def test_rope_many_keys(dtype, norm, interleaved):
+    """Some millions of keys, of which float32 would round some hundreds otherwise than their exact values."""
+    n, hkv, d, page = 6000, 4, 128, 64
+    rng = np.random.default_rng(11)
+    qkv, pages, cos, sin, pos, _, wk = rope_case(rng, n, 1, hkv, d, page, dtype, d, False, norm, "f32")
+    slots = np.arange(n, dtype=np.int32)
+    cache = cat.cat_mx_cache(pages, hkv, page, d)
+    cat.cat_mx_rope_cache_write(qkv, d, dev(pos), cos, sin, dev(slots), cache, k_weight=wk, interleaved=interleaved)
+    x = host(qkv).reshape(n, -1, d)[:, 1:1 + hkv]
+    k = C.turned(C.normed(x, None if wk is None else host(wk), 1e-6), host(cos)[pos], host(sin)[pos], interleaved)
+    codes, b = R.quantize(k.reshape(-1, d))
+    got, _ = cat.cat_mx_cache_read(cache, dev(slots), d)
+    np.testing.assert_array_equal(host(got).reshape(-1, d), R.values(codes, b))
+
+
 @pytest.mark.parametrize("size", [1e-30, 1e-15, 1e15, 1e30])
 def test_rope_rows_whose_squares_leave_float32(size):
     n, hq, hkv, d, page = 6, 2, 1, 128, 16
