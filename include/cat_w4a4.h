@@ -612,9 +612,9 @@ cat_status cat_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, 
  *   positions  device [n] int32, rows of cos and sin; outside [0, table_rows) a token's queries and keys become NaN (and the
  *              non-finite bit of the status word is raised).
  *   slots, cache  as in cat_mx_cache_write.
- *   q_out      device [n][hq][d] bfloat16, computed in float32 (float64 where that could change a key's code) and rounded once.
- * Keys are quantized as if computed exactly: where float32's error could change a code or a scale they are computed in
- * float64, so a cache does not depend on how its tokens came to it.
+ *   q_out      device [n][hq][d] bfloat16, computed in float32 and rounded once.
+ * Keys are quantized as if computed exactly: where float32's error could change a code or a scale they are computed again to some
+ * 2^-43, so a cache does not depend on how its tokens came to it.
  */
 cat_status cat_mx_rope_cache_write(const void* qkv, cat_dtype dtype, int64_t n, int64_t hq, const void* q_weight,
                                    const void* k_weight, cat_dtype weight_dtype, double eps, const int32_t* positions,
@@ -638,8 +638,10 @@ int64_t cat_mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t 
  *   window   0, or the number of tokens a row sees: itself and the window - 1 before it.
  * Row j of a sequence with r rows and length L is token p = L - r + j and sees tokens max(0, p - window + 1) .. p:
  *   out = sum_t softmax_t(scale q k_t) v_t, zero for a row that sees nothing (p < 0, a length of zero).
- * Scores and sums in float32; a score's operands are exact (but for channels 2^-24 below a row's largest), weights are rounded
- * to 11 bits (relative to the row's largest weight no smaller than 2^-24).  A NaN key or value of a token that a row does not see leaves it as it is.
+ * Scores and sums in float32.  A score's operands are exact, but for channels of a query 2^-24 below its row's largest and keys
+ * 2^-35 below the largest of their neighbours.  Weights are rounded to 11 bits (those 2^-22 and less of the row's largest, and those of
+ * values whose scale is below the largest seen by as much in all, to fewer).  A NaN key or value of a token that a row does not see
+ * leaves it as it is.
  *   out      device [n][hq][d] in `out_dtype`, rounded once.
  *   workspace device, at least cat_mx_attention_workspace bytes, written and read by this call alone: calls that may run at the
  *            same time need one each.  Its contents need not be kept or set.

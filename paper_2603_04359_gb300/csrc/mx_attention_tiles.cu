@@ -4,22 +4,24 @@
 //
 // on 5th-generation tensor cores, float16 operands.  The tensor cores take the codes as numbers only after they are unpacked: each of
 // a step's keys and values to float16, code times 2^(byte - ref + 12) with ref the largest scale byte of a warp's tokens (keys;
-// the products of 32 tokens are times its power again) or of all values so far (O is scaled when it grows).  That is exact down to 2^-22
-// of the largest block, and to 2^-36 with fewer bits.  A step's unpacking is shared by 256 rows (two tiles of 128; d = 256: one):
-// queries of a key head's group lie together, row r is head r % group of token r / group.
+// the products of 32 tokens are times its power again) or of all values so far (O is scaled when it grows).  That is exact down to 2^-35
+// of the largest block.  A step's unpacking is shared by 256 rows (two tiles of 128; d = 256: one): queries of a key head's group lie
+// together, row r is head r % group of token r / group.
 //
-// Per step of 64 tokens at d = 128 the MMAs take 1024 cycles of an SM, the exponentials of 2 x 8192 scores 512, the
-// unpacking ~200 issue slots a scheduler: what bounds it are the MMAs, if the others keep out of their way.  So scores have two
-// buffers a tile, and the next ones are there when a step's weights are done (with one buffer and steps of 128 tokens a tile's
-// weights, its two products and what lies between were one after the other: 5400 cycles a step for 2048 of MMAs).
+// Per step of 128 tokens at d = 128 the MMAs take 2080 cycles of an SM (32 of them, 65 each), the exponentials of 2 x 16384 scores 1024, the
+// unpacking ~400 issue slots a scheduler.  A step takes ~4750: a tile's weights (~3000: two passes over its scores, their way from and to
+// tensor memory), its two products and the waits between them follow one another, and two tiles in turn fill the tensor cores to 44 %.
+// 2048 tokens of 32 heads over 32768: 1132 us, 0.94 PFLOP/s.  What was slower: steps of 64 tokens with two buffers of scores a tile, whose
+// products of 64 columns take as long as those of 128 (1350 to 1530 us); the maximum found along with the weights, and these again where
+// it grew, whose code does not stay in the instruction cache beside the other roles' (1360 with steps of 64); one ring for the copies
+// of keys and of values, where values that wait for room keep keys back (1430).
 //
 // Warps (576 threads, one CTA an SM):
 //   0..3, 4..7   a tile's rows each, one a thread: scores from tensor memory, weights back to it (over the scores; the A operand of P V
 //                is read there), the running maximum and sum, O's correction where the maximum grows by more than 2^6, output
-//   8..11        keys to float16, 12..15 values: half of a token's row a thread
-//   16           issues the MMAs: P V of a tile, behind it the scores of the tile's step after the next, in the weights' place
-//   17           bulk copies of the codes as they are, a ring each of keys and values (one for both let values that wait for room keep
-//                keys back)
+//   8..11        keys to float16, 12..15 values: a token's row a thread (d = 256: half of one)
+//   16           issues the MMAs: P V of a tile, behind it the tile's next scores (d = 256: of the step after the next), in the weights' place
+//   17           bulk copies of the codes as they are, a ring each of keys and values
 // MMAs of one thread are carried out in the order of their issue, so next scores may follow the product that reads the weights
 // in their place.  Every wait is bounded; one that gives up raises the device status word and all roles drain and leave.
 //
@@ -35,8 +37,8 @@ namespace {
 
 constexpr int kThreads = 576;
 constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
-constexpr int kUnitCost = 768;              // a unit's beginning and end, in tokens
-constexpr int kLeastPiece = 1024;           // tokens (with units' costs) that a CTA is worth
+constexpr int kUnitCost = 768;              // a unit's beginning and end, in tokens (measured: 384 and 1536 were up to 37 and 9 % slower)
+constexpr int kLeastPiece = 256;            // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
 constexpr uint32_t kTmemCols = 512;
 constexpr int kBarRoom = 6144;
@@ -852,13 +854,11 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         }
       }
     }
-    if (!ok) {                                           // the copies still on their way
-      volatile int none = 0;
-      for (int kind = 0; kind < 2; ++kind) {
-        const uint32_t ring = kind ? C::kRingV : C::kRingK;
-        for (uint32_t i = sent[kind] > ring ? sent[kind] - ring : 0; i < sent[kind]; ++i)
-          mbar_wait_bounded(&bars->raw_full[(kind ? C::kRingK : 0) + i % ring], (i / ring) & 1, &none);
-      }
+    volatile int none = 0;                               // the last copies have come, whatever became of the others' waits
+    for (int kind = 0; kind < 2; ++kind) {
+      const uint32_t ring = kind ? C::kRingV : C::kRingK;
+      for (uint32_t i = sent[kind] > ring ? sent[kind] - ring : 0; i < sent[kind]; ++i)
+        mbar_wait_bounded(&bars->raw_full[(kind ? C::kRingK : 0) + i % ring], (i / ring) & 1, &none);
     }
   }
 #undef CAT_WAIT
@@ -873,7 +873,8 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
 template <int NB>
 cudaError_t run(const AttnArgs& a, int grid, cudaStream_t stream) {
   static PerDevice<cudaError_t> allowed;
-  constexpr int kSmem = Tc<NB>::kSmem < 120 * 1024 ? 120 * 1024 : Tc<NB>::kSmem;       // (one CTA an SM: tensor memory)
+  // No other kernel's CTA with tensor memory beside this one, which takes all of it.
+  constexpr int kSmem = Tc<NB>::kSmem < 216 * 1024 ? 216 * 1024 : Tc<NB>::kSmem;
   cudaError_t e = allowed.get([] { return allow_smem(mx_attention_tiles_kernel<NB>, kSmem); });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};

@@ -334,6 +334,49 @@ def test_streams_and_graphs():
     assert torch.equal(graphs[0][1], graphs[1][1])
 
 
+def test_prompts_on_streams_and_in_graphs():
+    """Both kernels of a mixed batch, on two streams at once and replayed with other lengths."""
+    a = Batch(22, [400, 700, 90], [200, 1, 2], 8, 2, 128, 64)
+    b = Batch(23, [900], [300], 4, 1, 64, 16)
+    wa, wb = a.run(), b.run()
+    a.check(wa)
+    table, lens, offsets = dev(a.table), dev(a.lens), dev(a.offsets)
+    bt, bl, bo = dev(b.table), dev(b.lens), dev(b.offsets)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for _ in range(8):
+        with torch.cuda.stream(s1):
+            outs.append((cat.cat_mx_attention(a.q, a.cache, table, lens, 128 ** -0.5, offsets=offsets), wa))
+        with torch.cuda.stream(s2):
+            outs.append((cat.cat_mx_attention(b.q, b.cache, bt, bl, 64 ** -0.5, offsets=bo), wb))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in outs)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        oa = cat.cat_mx_attention(a.q, a.cache, table, lens, 128 ** -0.5, offsets=offsets)
+        ob = cat.cat_mx_attention(b.q, b.cache, bt, bl, 64 ** -0.5, offsets=bo)
+    lens.copy_(torch.tensor([250, 64, 90], dtype=torch.int32))
+    offsets.copy_(torch.tensor([0, 130, 131, 203], dtype=torch.int32))
+    for _ in range(3):
+        g.replay()
+    torch.cuda.synchronize()
+    a.lens, a.offsets = np.array([250, 64, 90], dtype=np.int32), np.array([0, 130, 131, 203], dtype=np.int32)
+    a.check(oa)
+    assert torch.equal(ob, wb)
+    assert cat.cat_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("offsets", [[5, 2, 9, 300], [0, 400, -3, 7], [250, 240, 10, 0]])
+def test_offsets_out_of_order_stay_within_the_rows(offsets):
+    """(Which sequence a row named twice is of is not said; nothing outside is written, and the next call is right.)"""
+    b = Batch(24, [300, 50, 400], [100, 60, 100], 4, 2, 128, 32)
+    room = torch.full((262, 4, 128), 3.0, dtype=torch.bfloat16, device=DEV)
+    b.run(offsets=np.array(offsets, dtype=np.int32), out=room[1:261])
+    assert bool((room[0] == 3).all()) and bool((room[261] == 3).all())
+    b.check(b.run())
+
+
 def test_a_decode_loop():
     """Prompts and steps as a server runs them: projections' rows through norms and rotation into the cache, attention behind."""
     rng = np.random.default_rng(20)

@@ -247,3 +247,58 @@ def test_rope_equals_its_parts():
     v = qkv.view(n, -1, d)[:, hq + hkv:].contiguous()
     other = cat.cat_mx_cache_write(v, v, dev(slots), cat.cat_mx_cache(pages, hkv, page, d))
     assert torch.equal(other[:, 1], whole[:, 1])
+
+
+def test_streams_and_graphs():
+    """A captured rotation and read, replayed with other tokens, positions and slots beside calls on another stream."""
+    n, hq, hkv, d, page = 50, 4, 2, 128, 16
+    rng = np.random.default_rng(12)
+    qkv, pages, cos, sin, pos, wq, wk = rope_case(rng, n, hq, hkv, d, page, "bf16", d, True, True, "bf16")
+    slots = rng.permutation(pages * page)[:n].astype(np.int32)
+    other = rng.permutation(pages * page)[:n].astype(np.int32)
+    cache, aside = cat.cat_mx_cache(pages, hkv, page, d), cat.cat_mx_cache(pages, hkv, page, d)
+    x, p, s = qkv.clone(), dev(pos), dev(slots)
+    run = lambda c: cat.cat_mx_rope_cache_write(x, d, p, cos, sin, s, c, q_weight=wq, k_weight=wk)  # noqa: E731
+    run(cache)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        q = run(cache)
+        k, v = cat.cat_mx_cache_read(cache, s, d)
+    x.copy_(qkv.flip(0))
+    s.copy_(dev(other))
+    cache.zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(5):
+            q2 = run(aside)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(q, q2) and torch.equal(cache, aside)
+    wk_, wv_ = cat.cat_mx_cache_read(cache, s, d)
+    assert torch.equal(k, wk_) and torch.equal(v, wv_)
+    assert cat.cat_device_status()[0] == 0
+
+
+def test_rows_of_a_large_cache():
+    """Rows whose bytes lie behind 2^32 of the cache's first."""
+    page, hkv, d = 1024, 8, 256
+    pages = 4 * 2 ** 30 // (2 * hkv * C.page_bytes(page, d)) + 2
+    cache = cat.cat_mx_cache(pages, hkv, page, d)
+    rng = np.random.default_rng(13)
+    k, v = heads(rng, 20, hkv, d), heads(rng, 20, hkv, d)
+    slots = (pages * page - 1 - 7 * np.arange(20)).astype(np.int32)
+    cat.cat_mx_cache_write(dev(k, torch.float32), dev(v, torch.float32), dev(slots), cache)
+    gk, gv = cat.cat_mx_cache_read(cache, dev(slots), d)
+    for got, x in ((gk, k), (gv, v)):
+        np.testing.assert_array_equal(host(got).reshape(-1, d), R.values(*R.quantize(host(dev(x, torch.float32)).reshape(-1, d))))
+    assert not cache[:pages - 1].any()
+    table = torch.tensor([[pages - 1]], dtype=torch.int32, device=DEV)
+    q = torch.ones((2, hkv, d), dtype=torch.bfloat16, device=DEV)
+    small = cache[pages - 1:].clone()
+    for rows in (1, 2):
+        off = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+        lens = torch.tensor([1024], dtype=torch.int32, device=DEV)
+        far = cat.cat_mx_attention(q[:rows], cache, table, lens, 0.1, offsets=off)
+        assert torch.equal(far, cat.cat_mx_attention(q[:rows], small, table * 0, lens, 0.1, offsets=off)) and bool(far.any())
