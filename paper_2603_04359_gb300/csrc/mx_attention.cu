@@ -225,7 +225,8 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
 
   if (a.clears) clear_rows<D>(a);
   __syncthreads();
-  if (tid == 0) a.plan[cta].last = -1;
+  if (tid < 2) a.plan[2 * cta + tid].last = -1;
+  __syncwarp();
   if (cta >= ctas) return;
 
   int s = found_s;
@@ -247,13 +248,12 @@ __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const 
     const int64_t end_place = place + left < unit_cost ? place + left : unit_cost;
     const int step0 = max(place - kUnitCost, 0), step1 = max((int)end_place - kUnitCost, 0);
     const bool whole = step0 == 0 && step1 == sq.steps, starts = step0 == 0;
-    if (tid == 0 && starts && step1 > 0 && !whole) {
-      // the last CTA with a part: that of the unit's last step
-      const int64_t last_place = to - end_place + unit_cost - 1;         // on the line (`to` is where this piece ends)
-      Plan p = {s, h, rt, 0};
-      int64_t k = last_place < rest * (each + 1) ? last_place / (each + 1) : rest + (last_place - rest * (each + 1)) / each;
-      p.last = (int)k;
-      a.plan[cta] = p;
+    if (tid == 0 && step1 > 0 && !whole) {
+      // (`to` is where this piece ends on the line; a unit's parts begin with its first step)
+      const int64_t end = to - left + (unit_cost - place);
+      const int cta_first = starts ? cta : cta_of(end - sq.steps, each, rest), cta_last = cta_of(end - 1, each, rest);
+      const int row0 = rt * ROWS, n_rows = (int)min((int64_t)ROWS, (int64_t)sq.ql * a.group - row0);
+      a.plan[2 * cta + starts] = {cta_first, cta_last, sq.begin, h, row0, n_rows};
     }
     left -= end_place - place;
     at += end_place - place;

@@ -7,10 +7,16 @@ namespace cat {
 
 constexpr float kSlack = 6.f;               // a row's scores may exceed its running maximum by this (binary orders) before it follows
 
-// A CTA's piece that begins a unit (sequence, row tile, head) which others go on with.
-struct Plan {
-  int s, h, rt, last;                       // last: the last CTA with a part of it; -1: none
+// A unit (sequence, row tile, head) of which a CTA has a part and not the whole: it has two at most, that which it goes on with and
+// that which it begins.
+struct alignas(16) Plan {
+  int first, last;                          // the CTAs with a part of it; last = -1: no such unit
+  int begin, h, row0, rows;                 // its sequence's first row; its head, first row of the head's group, and rows
 };
+// The CTA that a place of the line is a piece of: `each` places a CTA, one more for the first `rest` of them.
+__device__ __forceinline__ int cta_of(int64_t place, int64_t each, int64_t rest) {
+  return (int)(place < rest * (each + 1) ? place / (each + 1) : rest + (place - rest * (each + 1)) / each);
+}
 
 struct AttnArgs {
   const __nv_bfloat16* q;
@@ -26,7 +32,7 @@ struct AttnArgs {
   void* out;
   int out_f32;
   float *parts, *ml;                        // [2 grid][rows][D], [2 grid][rows][2]: maximum and sum
-  Plan* plan;
+  Plan* plan;                               // [grid][2]
   uint32_t* status;
 };
 
@@ -37,7 +43,7 @@ struct Parts {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     ml = up(2 * grid * rows * d * 4);
     plan = ml + up(2 * grid * rows * 8);
-    bytes = plan + up(grid * sizeof(Plan));
+    bytes = plan + up(2 * grid * sizeof(Plan));
   }
   void place(AttnArgs* a, void* workspace) const {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -126,45 +132,123 @@ __device__ __forceinline__ void clear_rows(const AttnArgs& a) {
   }
 }
 
-constexpr int kJoinThreads = 128;
+constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps;
 
-// The parts of a unit, some of its rows a CTA: blockIdx.x the CTA that began it.
+// A row of a unit's output from some of its parts: D / 4 (64: 16) lanes have four channels each, or eight.
+template <int D>
+struct JoinRow {
+  static constexpr int kWide = D == 256 ? 2 : 1, kLanes = D == 64 ? 16 : 32;           // float4s a lane; lanes a part
+  float top, sum;                           // (of a lane's parts until `close`)
+  float4 o[kWide];
+  __device__ __forceinline__ void clear() {
+    top = -1e30f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWide; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void follow(float now) {
+    const float was = ex2(top - now);
+    top = now, sum *= was;
+#pragma unroll
+    for (int i = 0; i < kWide; ++i) o[i].x *= was, o[i].y *= was, o[i].z *= was, o[i].w *= was;
+  }
+  __device__ __forceinline__ void add(const float4 (&v)[kWide], float by) {
+#pragma unroll
+    for (int i = 0; i < kWide; ++i)
+      o[i].x = fmaf(v[i].x, by, o[i].x), o[i].y = fmaf(v[i].y, by, o[i].y), o[i].z = fmaf(v[i].z, by, o[i].z), o[i].w = fmaf(v[i].w, by, o[i].w);
+  }
+  // A warp: row r of the parts of CTAs from, from + stride, ..., last; `first` is the one that began the unit.
+  template <int ROWS>
+  __device__ __forceinline__ void parts(const AttnArgs& a, int r, int first, int from, int last, int stride) {
+    const int lane = threadIdx.x & 31;
+    for (int base = from; base <= last; base += 32 * stride) {
+      const int k = base + lane * stride;
+      auto slot_of = [&](int c) { return ((int64_t)2 * c + (c == first ? 1 : 0)) * ROWS + r; };
+      float2 ml = make_float2(-1e30f, 0.f);
+      if (k <= last) ml = *reinterpret_cast<const float2*>(a.ml + slot_of(k) * 2);
+      const bool some = ml.y != 0.f;                     // (a part of no tokens has no values)
+      float now = some ? fmaxf(top, ml.x) : top;
+#pragma unroll
+      for (int i = 1; i < 32; i <<= 1) now = fmaxf(now, __shfl_xor_sync(0xFFFFFFFFu, now, i));
+      follow(now);
+      const float mine = some ? ex2(ml.x - now) : 0.f;
+      if (some) sum = fmaf(ml.y, mine, sum);
+      const uint32_t which = __ballot_sync(0xFFFFFFFFu, some);
+      const int count = min(32, (last - base) / stride + 1);
+#pragma unroll 8
+      for (int i = 0; i < count; i += 32 / kLanes) {
+        const int j = i + lane / kLanes;                 // (< 32: `count` is even there or followed by one that is not `some`)
+        const float by = __shfl_sync(0xFFFFFFFFu, mine, j);
+        if (which >> j & 1) {
+          const float* at = a.parts + slot_of(base + j * stride) * D + 4 * (lane % kLanes);
+          float4 v[kWide];
+#pragma unroll
+          for (int w = 0; w < kWide; ++w) v[w] = *reinterpret_cast<const float4*>(at + 128 * w);
+          add(v, by);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 1; i < 32; i <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
+    if (kLanes == 16) {
+      o[0].x += __shfl_xor_sync(0xFFFFFFFFu, o[0].x, 16), o[0].y += __shfl_xor_sync(0xFFFFFFFFu, o[0].y, 16);
+      o[0].z += __shfl_xor_sync(0xFFFFFFFFu, o[0].z, 16), o[0].w += __shfl_xor_sync(0xFFFFFFFFu, o[0].w, 16);
+    }
+  }
+};
+
+// The parts of units, in the order of their tokens.  The CTAs with a part of a unit share its rows out among them (and among gridDim.y):
+// one launch of as many CTAs as the SMs hold at once, however many parts a unit has.  A row of few parts is a warp's; of many the
+// warps take every fourth part each, whose loads are independent of one another.  (One unit and row a CTA, its parts one behind the other,
+// and CTAs for all that could begin one: a step of 64 heads over 131000 tokens spent 10 us here, one of 27 short sequences 5.)
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads) mx_attention_join_kernel(const __grid_constant__ AttnArgs a) {
-  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;       // lanes a row of four channels; parts at once
-  __shared__ float4 os[kJoinThreads];
-  __shared__ float2 mls[kGroups];
+  using Row = JoinRow<D>;
+  __shared__ float4 os[kJoinWarps][D / 4];
+  __shared__ float2 mls[kJoinWarps];
   pdl_wait_then_release();
-  const int cta = blockIdx.x;
-  const Plan p = a.plan[cta];
+  const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const Plan p = a.plan[2 * cta + (blockIdx.y & 1)];
   if (p.last < 0) return;
-  const Rows sq = rows_of(a, p.s);
-  const int rows = (int)min((int64_t)ROWS, (int64_t)sq.ql * a.group - (int64_t)p.rt * ROWS);
-  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-    float top = -1e30f, sum = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](const float2& ml, const float4& v) {
-      const float now = fmaxf(top, ml.x), was = ex2(top - now), by = ex2(ml.x - now);
-      top = now;
-      sum = sum * was + ml.y * by;
-      o.x = o.x * was + v.x * by, o.y = o.y * was + v.y * by, o.z = o.z * was + v.z * by, o.w = o.w * was + v.w * by;
-    };
-    for (int k = cta + group; k <= p.last; k += kGroups) {
-      const int64_t slot = ((int64_t)2 * k + (k == cta ? 1 : 0)) * ROWS + r;
-      const float2 ml = *reinterpret_cast<const float2*>(a.ml + slot * 2);
-      if (ml.y != 0.f) add(ml, *reinterpret_cast<const float4*>(a.parts + slot * D + 4 * lane));       // (a part of no tokens has no values)
+  const int split = gridDim.y / 2, stride = (p.last - p.first + 1) * split, r0 = (cta - p.first) * split + blockIdx.y / 2;
+  auto store = [&](int r, float sum, int at, float4 o) {
+    const int rr = p.row0 + r, j = rr / a.group;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
+    store4(a, ((int64_t)(p.begin + j) * a.hq + p.h * a.group + (rr - j * a.group)) * D + at, o);
+  };
+  Row row;
+  if (p.last - p.first < 2 * kJoinWarps) {
+    for (int r = r0 + warp * stride; r < p.rows; r += kJoinWarps * stride) {
+      row.clear();
+      row.template parts<ROWS>(a, r, p.first, p.first, p.last, 1);
+#pragma unroll
+      for (int w = 0; w < Row::kWide; ++w)
+        if (lane < Row::kLanes) store(r, row.sum, 4 * lane + 128 * w, row.o[w]);
     }
+    return;
+  }
+  for (int r = r0; r < p.rows; r += stride) {
+    row.clear();
+    row.template parts<ROWS>(a, r, p.first, p.first + warp, p.last, kJoinWarps);
     __syncthreads();                                     // (the row before has been joined)
-    os[threadIdx.x] = o;
-    if (lane == 0) mls[group] = make_float2(top, sum);
+#pragma unroll
+    for (int w = 0; w < Row::kWide; ++w)
+      if (lane < Row::kLanes) os[warp][lane + 32 * w] = row.o[w];
+    if (lane == 0) mls[warp] = make_float2(row.top, row.sum);
     __syncthreads();
-    if (group == 0) {
-      for (int w = 1; w < kGroups; ++w) add(mls[w], os[w * kLanes + lane]);
-      const int rr = p.rt * ROWS + r, j = rr / a.group;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
-      store4(a, ((int64_t)(sq.begin + j) * a.hq + p.h * a.group + (rr - j * a.group)) * D + 4 * lane, o);
+    if (threadIdx.x < D / 4) {
+      float top = mls[0].x, sum = 0.f;
+#pragma unroll
+      for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, mls[w].x);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        const float by = ex2(mls[w].x - top);
+        const float4 v = os[w][threadIdx.x];
+        sum = fmaf(mls[w].y, by, sum);
+        o.x = fmaf(v.x, by, o.x), o.y = fmaf(v.y, by, o.y), o.z = fmaf(v.z, by, o.z), o.w = fmaf(v.w, by, o.w);
+      }
+      store(r, sum, 4 * threadIdx.x, o);
     }
   }
 }
@@ -172,12 +256,14 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attention_join_kernel(const _
 template <int D, int ROWS>
 cudaError_t launch_join(const AttnArgs& a, int grid, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid, ROWS < 32 ? ROWS : 32);
+  cfg.gridDim = dim3((unsigned)grid, 2 * (ROWS < 128 ? 1 : 8));
   cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = stream;
+  // Behind tiles its CTAs may wait while theirs still work.  Behind the kernel of few rows, 2 to 4 CTAs an SM, they are in the way of the
+  // next call's, which then come to lie unevenly (64 sequences of up to 8192 tokens in a row of calls: 98 us each, against 83).
   cudaLaunchAttribute attr = pdl_attr();
   cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = ROWS < 128 ? 0 : 1;
   note_launch();
   return cudaLaunchKernelEx(&cfg, mx_attention_join_kernel<D, ROWS>, a);
 }

@@ -84,7 +84,7 @@ struct Unit {
   bool starts, whole, nothing;              // nothing: no row sees a token
   int64_t p0;                               // the token of the sequence's first row
   int64_t t0, t1;                           // the tokens that some row sees
-  int64_t end;                              // where the unit ends on the line
+  int64_t from, end;                        // where the unit's first step ends on the line (of a later piece), and its end
   int begin;                                // the sequence's first row,
   int64_t tokens;                           // and one past its last token in the cache
 };
@@ -144,6 +144,12 @@ struct Walk {
       const bool empty_part = x0 == x1 && x0 > 0;
       left -= end - place;
       u.end = to - left + (length - end);
+      if (x0 > 0) {                                      // (the first end with a step; beside the quotient for rounding's sake)
+        int64_t x = length / steps;
+        while (step_of(x - 1) > 0) --x;
+        while (step_of(x) == 0) ++x;
+        u.from = u.end - length + x - 1;                 // (a piece's end counts for its steps)
+      }
       place = end;
       if (end == length) {                               // the next unit
         place = 0;
@@ -476,7 +482,8 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
     }
   }
   if (a.clears) clear_rows<D>(a);
-  if (tid == 0) a.plan[cta].last = -1;
+  if (tid < 2) a.plan[2 * cta + tid].last = -1;
+  __syncwarp();
   const bool works = cta < ctas;
   if (warp == kMmaWarp && works) tmem_alloc(&bars->tmem_addr, kTmemCols);
   tc_fence_before();
@@ -498,12 +505,8 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
     const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_cols = lanes + tile * (SB * KT), o_col = lanes + C::kO + tile * D;
     uint32_t units = 0, tj = 0;                          // units and this tile's steps so far
     while (ok && walk.next<NB>(a)) {
-      if (tid == 0 && u.starts && !u.whole) {
-        Plan p = {u.s, u.h, u.rt, 0};
-        const int64_t last = u.end - 1;
-        p.last = (int)(last < rest * (each + 1) ? last / (each + 1) : rest + (last - rest * (each + 1)) / each);
-        a.plan[cta] = p;
-      }
+      if (tid == 0 && !u.whole)
+        a.plan[2 * cta + u.starts] = {u.starts ? cta : cta_of(u.from, each, rest), cta_of(u.end - 1, each, rest), u.begin, u.h, u.rt * ROWS, u.rows};
       const uint32_t rr = (uint32_t)u.rt * ROWS + r;     // (a sequence has less than 2^31 rows)
       const int j = (int)(rr / (uint32_t)a.group);
       const int64_t row = ((int64_t)(u.begin + j) * a.hq + u.h * a.group + (int)(rr - (uint32_t)j * (uint32_t)a.group)) * D;
