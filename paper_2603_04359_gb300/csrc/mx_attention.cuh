@@ -27,6 +27,7 @@ struct AttnArgs {
   int n, hq, group, seqs;
   int few;                                  // sequences of at most this many rows are the first kernel's, others the second's
   int clears;                               // this launch clears the rows that see nothing
+  int beside;                               // this launch runs beside the one before it
   float scale;                              // scale log2 e
   int64_t window;
   void* out;
@@ -53,9 +54,9 @@ struct Parts {
   }
 };
 
-// Tiles of more rows: the grid, rows a tile, and the launch (with the joining of parts).
+// Tiles of more rows: rows a tile, and the launch (and that of its joining of parts).
 int attention_tile_rows(int64_t d);
-cudaError_t launch_attention_tiles(const AttnArgs& a, int64_t d, int grid, cudaStream_t stream);
+cudaError_t launch_attention_tiles(const AttnArgs& a, int64_t d, int grid, bool join, cudaStream_t stream);
 
 namespace {
 
@@ -134,11 +135,11 @@ __device__ __forceinline__ void clear_rows(const AttnArgs& a) {
 
 constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps;
 
-// A row of a unit's output from some of its parts: D / 4 (64: 16) lanes have four channels each, or eight.
+// A row of a unit's output from some of its parts: a lane has four channels, or two times four.
 template <int D>
 struct JoinRow {
   static constexpr int kWide = D == 256 ? 2 : 1, kLanes = D == 64 ? 16 : 32;           // float4s a lane; lanes a part
-  float top, sum;                           // (of a lane's parts until `close`)
+  float top, sum;
   float4 o[kWide];
   __device__ __forceinline__ void clear() {
     top = -1e30f, sum = 0.f;
@@ -196,20 +197,21 @@ struct JoinRow {
   }
 };
 
-// The parts of units, in the order of their tokens.  The CTAs with a part of a unit share its rows out among them (and among gridDim.y):
+// The parts of units, in the order of their tokens.  The CTAs with a part of a unit share its rows out among them (tiles': eight times):
 // one launch of as many CTAs as the SMs hold at once, however many parts a unit has.  A row of few parts is a warp's; of many the
 // warps take every fourth part each, whose loads are independent of one another.  (One unit and row a CTA, its parts one behind the other,
 // and CTAs for all that could begin one: a step of 64 heads over 131000 tokens spent 10 us here, one of 27 short sequences 5.)
+__host__ __device__ constexpr int join_split(int rows) { return rows < 128 ? 1 : 8; }
 template <int D, int ROWS>
-__global__ void __launch_bounds__(kJoinThreads) mx_attention_join_kernel(const __grid_constant__ AttnArgs a) {
+__device__ __forceinline__ void join(const AttnArgs& a, int index) {
   using Row = JoinRow<D>;
+  constexpr int split = join_split(ROWS);
   __shared__ float4 os[kJoinWarps][D / 4];
   __shared__ float2 mls[kJoinWarps];
-  pdl_wait_then_release();
-  const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const Plan p = a.plan[2 * cta + (blockIdx.y & 1)];
+  const int entry = index / split, cta = entry / 2, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const Plan p = a.plan[entry];
   if (p.last < 0) return;
-  const int split = gridDim.y / 2, stride = (p.last - p.first + 1) * split, r0 = (cta - p.first) * split + blockIdx.y / 2;
+  const int stride = (p.last - p.first + 1) * split, r0 = (cta - p.first) * split + index % split;
   auto store = [&](int r, float sum, int at, float4 o) {
     const int rr = p.row0 + r, j = rr / a.group;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -254,18 +256,27 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attention_join_kernel(const _
 }
 
 template <int D, int ROWS>
-cudaError_t launch_join(const AttnArgs& a, int grid, cudaStream_t stream) {
+__global__ void __launch_bounds__(kJoinThreads) mx_attention_join_kernel(const __grid_constant__ AttnArgs a) {
+  pdl_wait_then_release();
+  join<D, ROWS>(a, blockIdx.x);
+}
+// Those of both kernels.
+template <int D, int ROWS, int TILE_ROWS>
+__global__ void __launch_bounds__(kJoinThreads) mx_attention_join_both_kernel(const __grid_constant__ AttnArgs few, int few_grid,
+                                                                              const __grid_constant__ AttnArgs tiles) {
+  pdl_wait_then_release();
+  if ((int)blockIdx.x < few_grid)
+    join<D, ROWS>(few, blockIdx.x);
+  else
+    join<D, TILE_ROWS>(tiles, blockIdx.x - few_grid);
+}
+
+inline cudaLaunchConfig_t join_config(int grid, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid, 2 * (ROWS < 128 ? 1 : 8));
+  cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = stream;
-  // Behind tiles its CTAs may wait while theirs still work.  Behind the kernel of few rows, 2 to 4 CTAs an SM, they are in the way of the
-  // next call's, which then come to lie unevenly (64 sequences of up to 8192 tokens in a row of calls: 98 us each, against 83).
-  cudaLaunchAttribute attr = pdl_attr();
-  cfg.attrs = &attr;
-  cfg.numAttrs = ROWS < 128 ? 0 : 1;
-  note_launch();
-  return cudaLaunchKernelEx(&cfg, mx_attention_join_kernel<D, ROWS>, a);
+  return cfg;
 }
 
 }  // namespace

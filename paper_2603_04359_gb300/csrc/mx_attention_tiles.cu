@@ -874,7 +874,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
 }
 
 template <int NB>
-cudaError_t run(const AttnArgs& a, int grid, cudaStream_t stream) {
+cudaError_t run(const AttnArgs& a, int grid, bool join, cudaStream_t stream) {
   static PerDevice<cudaError_t> allowed;
   // No other kernel's CTA with tensor memory beside this one, which takes all of it.
   constexpr int kSmem = Tc<NB>::kSmem < 216 * 1024 ? 216 * 1024 : Tc<NB>::kSmem;
@@ -889,16 +889,21 @@ cudaError_t run(const AttnArgs& a, int grid, cudaStream_t stream) {
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   note_launch();
-  if ((e = cudaLaunchKernelEx(&cfg, mx_attention_tiles_kernel<NB>, a)) != cudaSuccess) return e;
-  return launch_join<32 * NB, Tc<NB>::ROWS>(a, grid, stream);
+  e = cudaLaunchKernelEx(&cfg, mx_attention_tiles_kernel<NB>, a);
+  if (e != cudaSuccess || !join) return e;
+  cfg = join_config(2 * grid * join_split(Tc<NB>::ROWS), stream);      // (its CTAs may wait while the tiles' still work)
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  note_launch();
+  return cudaLaunchKernelEx(&cfg, mx_attention_join_kernel<32 * NB, Tc<NB>::ROWS>, a);
 }
 
 }  // namespace
 
 int attention_tile_rows(int64_t d) { return d == 256 ? Tc<8>::ROWS : Tc<4>::ROWS; }
 
-cudaError_t launch_attention_tiles(const AttnArgs& a, int64_t d, int grid, cudaStream_t stream) {
-  return d == 64 ? run<2>(a, grid, stream) : d == 128 ? run<4>(a, grid, stream) : run<8>(a, grid, stream);
+cudaError_t launch_attention_tiles(const AttnArgs& a, int64_t d, int grid, bool join, cudaStream_t stream) {
+  return d == 64 ? run<2>(a, grid, join, stream) : d == 128 ? run<4>(a, grid, join, stream) : run<8>(a, grid, join, stream);
 }
 
 }  // namespace cat
