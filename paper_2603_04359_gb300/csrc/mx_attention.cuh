@@ -135,10 +135,10 @@ __device__ __forceinline__ void clear_rows(const AttnArgs& a) {
 
 constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps;
 
-// A row of a unit's output from some of its parts: a lane has four channels, or two times four.
-template <int D>
+// A row of a unit's output, or 4 kLanes kWide channels of it, from some of its parts: a lane has kWide times four channels.
+template <int D, int kLanes, int kWide>
 struct JoinRow {
-  static constexpr int kWide = D == 256 ? 2 : 1, kLanes = D == 64 ? 16 : 32;           // float4s a lane; lanes a part
+  static constexpr int lanes = kLanes, wide = kWide;
   float top, sum;
   float4 o[kWide];
   __device__ __forceinline__ void clear() {
@@ -159,7 +159,7 @@ struct JoinRow {
   }
   // A warp: row r of the parts of CTAs from, from + stride, ..., last; `first` is the one that began the unit.
   template <int ROWS>
-  __device__ __forceinline__ void parts(const AttnArgs& a, int r, int first, int from, int last, int stride) {
+  __device__ __forceinline__ void parts(const AttnArgs& a, int r, int first, int from, int last, int stride, int channel = 0) {
     const int lane = threadIdx.x & 31;
     for (int base = from; base <= last; base += 32 * stride) {
       const int k = base + lane * stride;
@@ -180,7 +180,7 @@ struct JoinRow {
         const int j = i + lane / kLanes;                 // (< 32: `count` is even there or followed by one that is not `some`)
         const float by = __shfl_sync(0xFFFFFFFFu, mine, j);
         if (which >> j & 1) {
-          const float* at = a.parts + slot_of(base + j * stride) * D + 4 * (lane % kLanes);
+          const float* at = a.parts + slot_of(base + j * stride) * D + channel + 4 * (lane % kLanes);
           float4 v[kWide];
 #pragma unroll
           for (int w = 0; w < kWide; ++w) v[w] = *reinterpret_cast<const float4*>(at + 128 * w);
@@ -190,21 +190,24 @@ struct JoinRow {
     }
 #pragma unroll
     for (int i = 1; i < 32; i <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
-    if (kLanes == 16) {
-      o[0].x += __shfl_xor_sync(0xFFFFFFFFu, o[0].x, 16), o[0].y += __shfl_xor_sync(0xFFFFFFFFu, o[0].y, 16);
-      o[0].z += __shfl_xor_sync(0xFFFFFFFFu, o[0].z, 16), o[0].w += __shfl_xor_sync(0xFFFFFFFFu, o[0].w, 16);
-    }
+#pragma unroll
+    for (int i = kLanes; i < 32; i <<= 1)
+#pragma unroll
+      for (int w = 0; w < kWide; ++w) {
+        o[w].x += __shfl_xor_sync(0xFFFFFFFFu, o[w].x, i), o[w].y += __shfl_xor_sync(0xFFFFFFFFu, o[w].y, i);
+        o[w].z += __shfl_xor_sync(0xFFFFFFFFu, o[w].z, i), o[w].w += __shfl_xor_sync(0xFFFFFFFFu, o[w].w, i);
+      }
   }
 };
 
 // The parts of units, in the order of their tokens.  The CTAs with a part of a unit share its rows out among them (tiles': eight times):
 // one launch of as many CTAs as the SMs hold at once, however many parts a unit has.  A row of few parts is a warp's; of many the
-// warps take every fourth part each, whose loads are independent of one another.  (One unit and row a CTA, its parts one behind the other,
+// warps of a CTA take every fourth part each, of all its channels or, where there are CTAs enough, of 32, all loads independent.  (One unit and row a CTA, its parts one behind the other,
 // and CTAs for all that could begin one: a step of 64 heads over 131000 tokens spent 10 us here, one of 27 short sequences 5.)
 __host__ __device__ constexpr int join_split(int rows) { return rows < 128 ? 1 : 8; }
 template <int D, int ROWS>
 __device__ __forceinline__ void join(const AttnArgs& a, int index) {
-  using Row = JoinRow<D>;
+  constexpr int kLanes = D == 64 ? 16 : 32, kWide = D == 256 ? 2 : 1;
   constexpr int split = join_split(ROWS);
   __shared__ float4 os[kJoinWarps][D / 4];
   __shared__ float2 mls[kJoinWarps];
@@ -218,41 +221,49 @@ __device__ __forceinline__ void join(const AttnArgs& a, int index) {
     o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
     store4(a, ((int64_t)(p.begin + j) * a.hq + p.h * a.group + (rr - j * a.group)) * D + at, o);
   };
-  Row row;
   if (p.last - p.first < 2 * kJoinWarps) {
+    JoinRow<D, kLanes, kWide> row;
     for (int r = r0 + warp * stride; r < p.rows; r += kJoinWarps * stride) {
       row.clear();
       row.template parts<ROWS>(a, r, p.first, p.first, p.last, 1);
 #pragma unroll
-      for (int w = 0; w < Row::kWide; ++w)
-        if (lane < Row::kLanes) store(r, row.sum, 4 * lane + 128 * w, row.o[w]);
+      for (int w = 0; w < kWide; ++w)
+        if (lane < kLanes) store(r, row.sum, 4 * lane + 128 * w, row.o[w]);
     }
     return;
   }
-  for (int r = r0; r < p.rows; r += stride) {
-    row.clear();
-    row.template parts<ROWS>(a, r, p.first, p.first + warp, p.last, kJoinWarps);
-    __syncthreads();                                     // (the row before has been joined)
+  auto shared = [&](auto row, int width) {               // all of a row's channels, or 32 of them
+    const int pieces = D / width;
+    for (int i = r0; i < p.rows * pieces; i += stride) {
+      const int r = i / pieces, channel = width * (i - r * pieces);
+      row.clear();
+      row.template parts<ROWS>(a, r, p.first, p.first + warp, p.last, kJoinWarps, channel);
+      __syncthreads();                                   // (the channels before have been joined)
 #pragma unroll
-    for (int w = 0; w < Row::kWide; ++w)
-      if (lane < Row::kLanes) os[warp][lane + 32 * w] = row.o[w];
-    if (lane == 0) mls[warp] = make_float2(row.top, row.sum);
-    __syncthreads();
-    if (threadIdx.x < D / 4) {
-      float top = mls[0].x, sum = 0.f;
+      for (int w = 0; w < row.wide; ++w)
+        if (lane < row.lanes) os[warp][lane + 32 * w] = row.o[w];
+      if (lane == 0) mls[warp] = make_float2(row.top, row.sum);
+      __syncthreads();
+      if (threadIdx.x < width / 4) {
+        float top = mls[0].x, sum = 0.f;
 #pragma unroll
-      for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, mls[w].x);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, mls[w].x);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) {
-        const float by = ex2(mls[w].x - top);
-        const float4 v = os[w][threadIdx.x];
-        sum = fmaf(mls[w].y, by, sum);
-        o.x = fmaf(v.x, by, o.x), o.y = fmaf(v.y, by, o.y), o.z = fmaf(v.z, by, o.z), o.w = fmaf(v.w, by, o.w);
+        for (int w = 0; w < kJoinWarps; ++w) {
+          const float by = ex2(mls[w].x - top);
+          const float4 v = os[w][threadIdx.x];
+          sum = fmaf(mls[w].y, by, sum);
+          o.x = fmaf(v.x, by, o.x), o.y = fmaf(v.y, by, o.y), o.z = fmaf(v.z, by, o.z), o.w = fmaf(v.w, by, o.w);
+        }
+        store(r, sum, channel + 4 * threadIdx.x, o);
       }
-      store(r, sum, 4 * threadIdx.x, o);
     }
-  }
+  };
+  if (p.rows * (D / 32) <= stride)
+    shared(JoinRow<D, 8, 1>(), 32);
+  else
+    shared(JoinRow<D, kLanes, kWide>(), D);
 }
 
 template <int D, int ROWS>
