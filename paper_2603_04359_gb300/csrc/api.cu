@@ -1089,6 +1089,11 @@ static cat_status check_cache(int64_t pages, int64_t page, int64_t hkv, int64_t 
   if (pages < 0 || pages > kMaxMxRows / page) return fail(CAT_ERR_SHAPE, "a cache has at most 2^31 - 512 rows");
   return CAT_OK;
 }
+static bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+static int64_t bytes_of(cat_dtype t) { return t == CAT_F32 ? 4 : 2; }
 static bool rows_fit(int64_t n) { return n >= 0 && n <= kMaxMxRows; }
 
 int64_t cat_mx_cache_page_bytes(int64_t page, int64_t d) {
@@ -1121,6 +1126,8 @@ cat_status cat_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, 
   if (!k || !v || !slots || (pages > 0 && !cache)) return fail(CAT_ERR_INVALID_ARG, "NULL pointer");
   if (!aligned16(k) || !aligned16(v) || !aligned16(slots) || !aligned16(cache))
     return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  if (overlap(k, m * hkv * d * bytes_of(out_dtype), v, m * hkv * d * bytes_of(out_dtype)))
+    return fail(CAT_ERR_INVALID_ARG, "k and v must not overlap");
   return mx_launch("cat_mx_cache_read launch", [&](uint32_t*) {
     return cat::launch_mx_cache_read(cache, pages, page, hkv, d, slots, m, (int)out_dtype, k, v, (cudaStream_t)stream);
   });
@@ -1146,6 +1153,8 @@ cat_status cat_mx_rope_cache_write(const void* qkv, cat_dtype dtype, int64_t n, 
   if (!aligned16(qkv) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(positions) || !aligned16(cos) ||
       !aligned16(sin) || !aligned16(slots) || !aligned16(cache) || !aligned16(q_out))
     return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  if (overlap(qkv, n * (hq + 2 * hkv) * d * bytes_of(dtype), q_out, n * hq * d * 2))
+    return fail(CAT_ERR_INVALID_ARG, "q_out must not overlap qkv");
   return mx_launch("cat_mx_rope_cache_write launch", [&](uint32_t* status) {
     return cat::launch_mx_rope(qkv, (int)dtype, n, hq, q_weight, k_weight, (int)weight_dtype, eps, positions, cos, sin, table_rows,
                                rot, interleaved, slots, cache, pages, page, hkv, d, q_out, status, (cudaStream_t)stream);
@@ -1177,6 +1186,8 @@ cat_status cat_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t*
   if (!aligned16(q) || !aligned16(cache) || !aligned16(table) || !aligned16(lens) || !aligned16(offsets) || !aligned16(out) ||
       !aligned16(workspace))
     return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
+  if (overlap(q, n * hq * d * 2, out, n * hq * d * bytes_of(out_dtype)))
+    return fail(CAT_ERR_INVALID_ARG, "out must not overlap q");
   if ((st = check_device()) != CAT_OK) return st;
   const int64_t need = cat::mx_attention_workspace(n, seqs, hq, hkv, d);
   if (need < 0) return fail(CAT_ERR_CUDA, "the device's size cannot be asked");

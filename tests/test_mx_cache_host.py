@@ -104,6 +104,18 @@ def test_refusals(lib):
     for i in (0, 3, 8, 10, 12, 16, 17):
         refused(a, good, 3, **{f"_{i}": BAD})
     refused(a, good, 0, _1=0, _11=0)
+    # outputs that overlap what is read while they are written, or one another
+    far, near = ctypes.c_void_p(0x10000 + 4 * 4 * 64 * 2), ctypes.c_void_p(0x10000 + 4 * 4 * 64 * 2 - 16)
+    for out in (P, near):
+        refused(a, good, 1, _16=out)
+        assert b"overlap" in lib.cat_last_error()
+    near_v = ctypes.c_void_p(0x10000 + 4 * 2 * 64 * 4 - 16)
+    for v in (P, near_v):
+        refused(r, [P, 2, 16, 2, 64, P, 4, 0, P, P, None], 1, _9=v)
+        assert b"overlap" in lib.cat_last_error()
+    refused(f, [P, 1, 4, 4, P, P, 0, 1e-6, P, P, P, 100, 64, 0, P, P, 2, 16, 2, 64, P, None], 1, _20=ctypes.c_void_p(0x10000 + 4 * 8 * 64 * 2 - 16))
+    if not torch.cuda.is_available():                    # (those beside one another are not refused for that)
+        assert a(*(good[:16] + [far] + good[17:])) != 1 or b"overlap" not in lib.cat_last_error()
     for bad in ((0, 1, 4, 2, 64), (1, 0, 4, 2, 64), (1, 1, 3, 2, 64), (1, 1, 4, 0, 64), (1, 1, 4, 2, 96)):
         assert lib.cat_mx_attention_workspace(*bad) == 0
 
@@ -191,21 +203,24 @@ def fake(tmp_path_factory):
     return FakeRuntime(tmp_path_factory.mktemp("fake_cache"))
 
 
+FAR = 1 << 46             # of outputs that must not overlap what is read
+
+
 def cache_calls(lib):
     for d in (64, 128, 256):
         for dtype in (0, 1):
             for n, hkv, page in ((1, 1, 16), (27, 8, 64), (100000, 5, 1024)):
                 yield "cat_mx_cache_write", A, A, dtype, n, A, A, 1000, page, hkv, d, None
-                yield "cat_mx_cache_read", A, 1000, page, hkv, d, A, n, dtype, A, A, None
+                yield "cat_mx_cache_read", A, 1000, page, hkv, d, A, n, dtype, A, FAR, None
                 for rot in (16, 32, 64):
                     for interleaved in (0, 1):
                         yield ("cat_mx_rope_cache_write", A, dtype, n, 4 * hkv, A, None, 1, 1e-6, A, A, A, 999, rot * (d // 64), interleaved,
-                               A, A, 1000, page, hkv, d, A, None)
+                               A, A, 1000, page, hkv, d, FAR, None)
             for n, seqs, hq, hkv in ((1, 1, 1, 1), (64, 64, 64, 8), (100, 20, 32, 8), (5000, 1, 16, 16), (300, 300, 128, 1)):
                 need = lib.cat_mx_attention_workspace(n, seqs, hq, hkv, d)
                 for offsets in (None, A):
                     if offsets or n == seqs:
-                        yield ("cat_mx_attention", A, n, hq, A, 1000, 64, hkv, d, A, 50, A, seqs, offsets, 0.1, 0, dtype, A, A, need, None)
+                        yield ("cat_mx_attention", A, n, hq, A, 1000, 64, hkv, d, A, 50, A, seqs, offsets, 0.1, 0, dtype, FAR, A, need, None)
 
 
 def test_every_launch_is_allowed_on_every_device(fake):
@@ -224,7 +239,7 @@ def test_every_launch_is_allowed_on_every_device(fake):
 def test_a_workspace_that_is_too_small_is_refused(fake):
     need = fake.lib.cat_mx_attention_workspace(4, 4, 8, 2, 128)
     assert need > 0
-    args = [A, 4, 8, A, 10, 64, 2, 128, A, 50, A, 4, None, 0.1, 0, 1, A]
+    args = [A, 4, 8, A, 10, 64, 2, 128, A, 50, A, 4, None, 0.1, 0, 1, FAR]
     assert fake.lib.cat_mx_attention(*args, A, need - 1, None) == 2
     assert fake.lib.cat_mx_attention(*args, None, need, None) == 2
     assert fake.lib.cat_mx_attention(*args, A, need, None) == 0
