@@ -22,6 +22,8 @@
 // parts go through the workspace, and a second kernel joins them in the order of their tokens.
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "mx_attention.cuh"
 #include "per_device.h"
 
@@ -644,14 +646,17 @@ Form form_of(int64_t n, int64_t seqs, int64_t group, int64_t d) {
   return {nt, nt * d <= 128 ? 4 : nt * d <= 256 ? 3 : 2};
 }
 
-// Which kernels a call takes.  Both can do any number of rows; with no more rows than sequences (a decode step, whatever its
-// offsets) the first does all, with one sequence or many heads on a key head it is known which is the better one for all, and else
-// either leaves the other's sequences out (an empty launch of the second costs a decode step some 5 us).
+// Which kernels a call takes.  Both can do any number of rows.  With no more rows than sequences (a decode step, whatever its offsets),
+// and where rows and the tokens that a table's width has room for are few, the first does all (tiles have a longer way from a unit's
+// beginning to its end: 48 rows a key head over 100 tokens 19 us against 24, 192 over 2000 30 against 41; 384 over 2000 42 against 35);
+// with one sequence or many heads on a key head it is known which is the better one for all, and else either leaves the other's sequences out.
+constexpr int64_t kFewWork = int64_t(1) << 22;           // rows of all heads times tokens
 struct Needs {
   int most;                                 // rows of a sequence and key head up to which the first kernel is the faster
   bool few, tiles;
-  Needs(int64_t n, int64_t seqs, int64_t group, int64_t d) : most(d == 256 ? 16 : 24) {
-    tiles = group > most || (n > seqs && n * group > most);
+  Needs(int64_t n, int64_t seqs, int64_t hq, int64_t hkv, int64_t d, int64_t room) : most(d == 256 ? 16 : 24) {
+    const int64_t group = hq / hkv;
+    tiles = (group > most || (n > seqs && n * group > most)) && (double)(n * hq) * (double)room > (double)kFewWork;
     few = !tiles || (group <= most && seqs > 1);
   }
   int most_few() const { return few ? tiles ? most : 0x7FFFFFFF : 0; }
@@ -701,11 +706,9 @@ int64_t mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv,
   if (sms < 0) return -1;
   const int64_t group = hq / hkv;
   const Form f = form_of(n, seqs, group, d);
-  const Needs needs(n, seqs, group, d);
-  size_t bytes = 0;
-  if (needs.few) bytes += Parts((size_t)sms * f.resident, 8 * f.nt, d).bytes;
-  if (needs.tiles) bytes += Parts(sms, attention_tile_rows(d), d).bytes;
-  return (int64_t)bytes;
+  const Needs needs(n, seqs, hq, hkv, d, INT64_MAX);       // (a table with little room may need the first's alone)
+  const size_t few = Parts((size_t)sms * f.resident, 8 * f.nt, d).bytes, tiles = needs.tiles ? Parts(sms, attention_tile_rows(d), d).bytes : 0;
+  return (int64_t)(needs.few ? few + tiles : std::max(few, tiles));
 }
 
 cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,
@@ -725,7 +728,7 @@ cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint
   a.scale = scale * 1.44269504f;
   a.status = status, a.window = window, a.out = out, a.out_f32 = out_dtype == 0;
   const Form f = form_of(n, seqs, a.group, d);
-  const Needs needs(n, seqs, a.group, d);
+  const Needs needs(n, seqs, hq, hkv, d, width * page);
   a.few = needs.most_few();
   const Parts parts((size_t)sms * f.resident, 8 * f.nt, d), tiles(sms, attention_tile_rows(d), d);
   a.clears = 1;

@@ -331,19 +331,26 @@ __device__ __forceinline__ float score_factor(float fac, float k_factor) { retur
 template <int KT>
 __device__ __forceinline__ float largest(uint32_t s_col, const float* k_factor, float fac) {
   float most = -INFINITY;
+  uint32_t a[16], b[16];
+  auto of = [](const uint32_t (&v)[16]) {
+    float m[2] = {fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1])), fmaxf(__uint_as_float(v[2]), __uint_as_float(v[3]))};
+#pragma unroll
+    for (int i = 4; i < 16; i += 4) {
+      m[0] = max3(m[0], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+      m[1] = max3(m[1], __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+    }
+    return fmaxf(m[0], m[1]);
+  };
+  tmem_ld16(s_col, a);
+  tmem_have16(a);
 #pragma unroll 1
   for (int c = 0; c < KT / 32; ++c) {
-    uint32_t v[32];
-    CAT_TMEM_LD32(s_col + 32 * c, v);
-    const float f = score_factor(fac, k_factor[c]);
-    tmem_have32(v);
-    float m[2] = {__uint_as_float(v[0]), __uint_as_float(v[1])};
-#pragma unroll
-    for (int i = 2; i < 32; i += 4) {
-      m[0] = max3(m[0], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
-      if (i + 2 < 32) m[1] = max3(m[1], __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
-    }
-    most = fmaxf(most, fmaxf(m[0], m[1]) * f);
+    tmem_ld16(s_col + 32 * c + 16, b);
+    const float f = score_factor(fac, k_factor[c]), m = of(a);
+    tmem_have16(b);
+    tmem_ld16(s_col + 32 * min(c + 1, KT / 32 - 1), a);
+    most = fmaxf(most, fmaxf(m, of(b)) * f);
+    tmem_have16(a);
   }
   return most;
 }

@@ -40,7 +40,11 @@ class Batch:
         count = [-(-max(int(n), 0) // page) for n in lens]
         pages = sum(count) + spare
         order = rng.permutation(pages).astype(np.int32)
+        # (few rows times a narrow table are all the first kernel's: ragged batches have room behind their sequences, `narrow` none)
         width = max(count + [1]) + 1
+        self.narrow = width
+        if sum(rows) > len(rows):
+            width += 2 ** 22 // (sum(rows) * hq * page)
         self.table = np.full((len(lens), width), -7, dtype=np.int32)           # (behind a length: not read)
         at = 0
         for s, c in enumerate(count):
@@ -59,7 +63,8 @@ class Batch:
     def run(self, scale=None, **more):
         scale = self.d ** -0.5 if scale is None else scale
         offsets = more.pop("offsets", self.offsets)
-        return cat.cat_mx_attention(self.q, self.cache, dev(self.table), dev(self.lens), scale,
+        table = self.table[:, :self.narrow] if more.pop("narrow", False) else self.table
+        return cat.cat_mx_attention(self.q, self.cache, dev(np.ascontiguousarray(table)), dev(self.lens), scale,
                                     offsets=None if offsets is None else dev(offsets), **more)
 
     def check(self, got, scale=None, window=0, offsets="own"):
@@ -93,6 +98,37 @@ def test_several_tokens(hq, hkv, d):
     assert not want[15:18].any()                     # tokens -3 .. -1 of a sequence of 3
     for window in (1, 7, 16, 33, 100000):
         b.check(b.run(window=window, out_dtype=torch.float32), window=window)
+
+
+@pytest.mark.parametrize("d", [64, 256])
+def test_a_length_behind_the_table(d):
+    """Tokens that no entry of the table is for are not attended, by either kernel."""
+    b = Batch(26 + d, [4500, 30, 4120], [200, 3, 2], 8, 2, d, 1024)
+    for width in (4, 3, 0):
+        b.table = np.ascontiguousarray(b.table[:, :width])
+        for window in (0, 300):
+            got = host(b.run(window=window, out_dtype=torch.float32))
+            if width == 0:
+                assert not got.any()
+            else:
+                want = C.attention(host(b.q), host(b.cache), b.page, b.table, b.lens, d ** -0.5, b.offsets, window)
+                assert np.all(np.abs(got - want[0]) <= C.tolerance(*want, d, False))
+    assert cat.cat_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("hq,hkv,lens,rows", [
+    (8, 2, [5, 40, 300, 3, 0, 17, 130, 16], [5, 3, 7, 6, 2, 0, 40, 1]), (20, 4, [7, 7, 5], [7, 6, 5]), (4, 4, [500], [300]),
+    (64, 1, [33, 100], [1, 2]), (5, 1, [1], [1]), (9, 3, [700, 20], [30, 20])])
+def test_many_rows_with_a_narrow_table(hq, hkv, lens, rows, d):
+    """(All of them the first kernel's, some of several tiles; beside them, with room in the table, the second's.)"""
+    b = Batch(25 + hq + d, lens, rows, hq, hkv, d, 16)
+    for window in (0, 1, 9, 64):
+        b.check(b.run(window=window, narrow=True), window=window)
+        b.check(b.run(window=window, out_dtype=torch.float32), window=window)
+    got = b.run(narrow=True)
+    assert torch.equal(got, b.run(narrow=True))
+    assert cat.cat_device_status()[0] == 0
 
 
 @pytest.mark.parametrize("hq,hkv,d,lens,rows", [
