@@ -1,7 +1,7 @@
 // Rows of the paged 4-bit key/value cache (mx_cache.cuh): keys and values in, values out, and a fused projection's output
 // through its heads' norms and rotation into the cache.
 //
-// All are bound by bytes: a value costs its input and 17/32 of a byte of the form.  A lane has quarter p of a head's row
+// All have little more to do than move bytes: a value costs its input and 17/32 of a byte of the form.  A lane has quarter p of a head's row
 // (channels 8 p .. 8 p + 7 of each block of 32), so four neighbouring lanes have a row: they read it in 16-byte pieces, 64 or 128
 // bytes side by side, find a block's largest magnitude in two shuffles, and write their quarter of the codes at once.
 #include "mx_cache.cuh"
@@ -187,7 +187,7 @@ struct Rows {
   }
 };
 
-// blockIdx.y: 0 keys, 1 values
+// blockIdx.y: 0 keys, 1 values.  Bound by memory: 8000 float32 tokens of 16 heads of 64 channels, 74 MB, 12.3 us (6.0 TB/s).
 template <typename T, int NB>
 __global__ void __launch_bounds__(kThreads) mx_cache_write_kernel(const T* __restrict__ k, const T* __restrict__ v, int64_t n,
                                                                   const int32_t* __restrict__ slots, MxCache c,
@@ -237,6 +237,7 @@ __device__ __forceinline__ void values8(uint32_t w, uint32_t byte, float (&v)[8]
   }
 }
 
+// Bound by memory: 32768 tokens of 8 heads of 128 channels to bf16, 170 MB, 27.7 us (6.1 TB/s).
 template <typename T, int NB>
 __global__ void __launch_bounds__(kThreads) mx_cache_read_kernel(MxCache c, const int32_t* __restrict__ slots, int64_t m,
                                                                  int64_t step_tokens, int step_heads, T* __restrict__ k,
@@ -572,6 +573,9 @@ __device__ __noinline__ void near_key(const RopeArgs& a, const T* x, const void*
 // the key's code is that of the exact value.
 constexpr float kMargin = 20.f * 0x1p-24f;
 
+// A warp has eight heads of a token, four lanes a head, its values in registers from the norm to the codes.  8192 tokens of 80 heads of 128 channels
+// in bf16, 311 MB, 78 us (4.0 TB/s): a warp's loads come at its beginning, and the 28 warps of an SM (72 registers) are too few to hide them
+// behind one another's arithmetic (2.2 instructions a cycle); with 24 warps, and a channel at a time instead of two, 118.
 template <typename T, int NB, int PAIRS>
 __global__ void __launch_bounds__(kThreads, NB == 8 ? 4 : 7) mx_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int D = 32 * NB;
