@@ -242,6 +242,19 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
   return o;
 }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t r;
+  asm("{ .reg .b64 x, y; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; mul.rn.f32x2 %0, x, y; }"
+      : "=l"(r)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  float2 o;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+  return o;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   uint64_t r;
   asm("{ .reg .b64 x, y; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; add.rn.f32x2 %0, x, y; }"
@@ -528,45 +541,49 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         continue;
       }
       // The warp's rows to float16, a row's largest channel in [2^13, 2^14); a negative scale goes into its sign.  All of them on their
-      // way at once, to where they are then rewritten; D / 8 lanes a row.
+      // way at once (D / 8 lanes a row), to where each thread then rewrites its own.
       float fac;
       {
         constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
-        const int piece = lane % kLanes, warp_row = tile * 128 + (warp & 3) * 32;
-        uint8_t* const to_q = smem + tile * C::kQ + (piece >> 3) * (128 * 128) + (warp & 3) * (32 * 128);
-        auto place = [&](int at) { return to_q + at * 128 + (((piece & 7) ^ (at & 7)) << 4); };
+        const int warp_row = tile * 128 + (warp & 3) * 32;
+        uint8_t* const to_q = smem + tile * C::kQ + (warp & 3) * (32 * 128);
+        auto place = [&](int at, int piece) { return to_q + (piece >> 3) * (128 * 128) + at * 128 + (((piece & 7) ^ (at & 7)) << 4); };
         __syncwarp();                                    // (what was there has been read)
-#pragma unroll 1
+#pragma unroll 4
         for (int i = 0; i < 32; i += kAtOnce) {
-          const int at = i + lane / kLanes;
+          const int at = i + lane / kLanes, piece = lane % kLanes;
           const int64_t from_q = __shfl_sync(0xFFFFFFFFu, row, at);
           const bool in = warp_row + at < u.rows;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(place(at))), "l"(a.q + (in ? from_q + piece * 8 : 0)), "r"(in ? 16 : 0)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(place(at, piece))),
+                       "l"(a.q + (in ? from_q + piece * 8 : 0)), "r"(in ? 16 : 0)
                        : "memory");
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncwarp();
-        const float sign = a.scale < 0.f ? -1.f : 1.f;
-        int mine = 1;                                    // this thread's row's exponent
-#pragma unroll 1
-        for (int i = 0; i < 32; i += kAtOnce) {
-          const int at = i + lane / kLanes;
-          uint4* const p = reinterpret_cast<uint4*>(place(at));
+        uint32_t m2[2] = {0u, 0u};
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4*>(place(lane, i));
+          m2[0] = __vmaxu2(m2[0], __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu));
+          m2[1] = __vmaxu2(m2[1], __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+        }
+        const uint32_t both = __vmaxu2(m2[0], m2[1]);
+        const int e = max((int)(max(both & 0xFFFFu, both >> 16) >> 7), 1);           // this thread's row's exponent
+        // (a row with an infinity or a NaN is NaN; the two factors together could leave float32's range)
+        const float up = (e == 255 ? __int_as_float(0x7FFFFFFF) : e == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23)) *
+                         (a.scale < 0.f ? -1.f : 1.f);
+        auto half2_of = [&](uint32_t w) {
+          const float2 x = mul2(mul2(make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)), make_float2(up, up)),
+                                make_float2(0x1p13f, 0x1p13f));
+          return f16_pair(x.x, x.y);
+        };
+#pragma unroll 2
+        for (int i = 0; i < D / 8; ++i) {
+          uint4* const p = reinterpret_cast<uint4*>(place(lane, i));
           const uint4 v = *p;
-          const uint32_t m2 = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-          uint32_t most = max(m2 & 0xFFFFu, m2 >> 16);
-#pragma unroll
-          for (int k = 1; k < kLanes; k <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, k));
-          const int e = max((int)(most >> 7), 1);
-          const int theirs = __shfl_sync(0xFFFFFFFFu, e, (lane % kAtOnce) * kLanes);
-          if (lane / kAtOnce == i / kAtOnce) mine = theirs;
-          const float up = (e >= 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23)) * sign;
-          auto half2_of = [&](uint32_t w) {
-            return e == 255 ? 0x7FFF7FFFu : f16_pair(__uint_as_float(w << 16) * up * 0x1p13f, __uint_as_float(w & 0xFFFF0000u) * up * 0x1p13f);
-          };
           *p = make_uint4(half2_of(v.x), half2_of(v.y), half2_of(v.z), half2_of(v.w));
         }
-        fac = ldexpf(fabsf(a.scale), mine - 140);
+        fac = ldexpf(fabsf(a.scale), e - 140);
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -643,33 +660,49 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         const float l = l2.x + l2.y;
         float unref = ldexpf(1.f, ref - 139);
         if (u.whole) unref = l == 0.f ? 0.f : ldexpf(1.f / l, ref - 139);
-        // 32 channels of the warp's rows at a time through the place of its queries, whose products are done: eight lanes a row
-        uint8_t* stage = smem + tile * C::kQ + (warp & 3) * (32 * 128);
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t v[32];
-          CAT_TMEM_LD32(o_col + c, v);
-          tmem_have32(v);
-          const bool nan = nan_blocks >> (c / 32) & 1;
+        // 128 bytes of each of the warp's rows at a time (32 channels in float32, 64 in bf16) through the place of its queries, whose
+        // products are done: eight lanes a row
+        const bool narrow = u.whole && !a.out_f32;
+        uint8_t* const mine = !real     ? nullptr
+                              : narrow  ? static_cast<uint8_t*>(a.out) + row * 2
+                              : u.whole ? static_cast<uint8_t*>(a.out) + row * 4
+                                        : reinterpret_cast<uint8_t*>(a.parts + ((int64_t)slot * ROWS + r) * D);
+        uint8_t* to[8];
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            float4 o = make_float4(__uint_as_float(v[i]) * unref, __uint_as_float(v[i + 1]) * unref, __uint_as_float(v[i + 2]) * unref,
-                                   __uint_as_float(v[i + 3]) * unref);
-            if (nan) o.x = o.y = o.z = o.w = __int_as_float(0x7FFFFFFF);
-            *reinterpret_cast<float4*>(stage + lane * 128 + (((i / 4) ^ (lane & 7)) << 4)) = o;
+        for (int k = 0; k < 8; ++k) {
+          const uint64_t base = __shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(mine), 4 * k + (lane >> 3));
+          to[k] = base ? reinterpret_cast<uint8_t*>(base) + 16 * (lane & 7) : nullptr;
+        }
+        uint8_t* const stage = smem + tile * C::kQ + (warp & 3) * (32 * 128);
+        auto staged = [&](int j) { return reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)); };
+#pragma unroll 1
+        for (int c = 0; c < D;) {
+#pragma unroll 1
+          for (int half = 0; half < (narrow ? 2 : 1); ++half, c += 32) {
+            uint32_t v[32];
+            CAT_TMEM_LD32(o_col + c, v);
+            tmem_have32(v);
+            const float by = nan_blocks >> (c / 32) & 1 ? __int_as_float(0x7FFFFFFF) : unref;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * by);
+            if (narrow) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) v[i / 2] = bf16_pair(__uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+#pragma unroll
+              for (int j = 0; j < 4; ++j) *staged(4 * half + j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) *staged(j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            }
           }
           __syncwarp();
-#pragma unroll 1
-          for (int i = lane >> 3; i < 32; i += 4) {
-            const int at = tile * 128 + (warp & 3) * 32 + i;
-            const float4 o = *reinterpret_cast<const float4*>(stage + i * 128 + (((lane & 7) ^ (i & 7)) << 4));
-            const int64_t to_out = __shfl_sync(0xFFFFFFFFu, row, i);
-            if (at < u.rows) {
-              if (u.whole) {
-                store4(a, to_out + c + 4 * (lane & 7), o);
-              } else {
-                *reinterpret_cast<float4*>(a.parts + ((int64_t)slot * ROWS + at) * D + c + 4 * (lane & 7)) = o;
-              }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int at = 4 * k + (lane >> 3);
+            const uint4 o = *reinterpret_cast<const uint4*>(stage + at * 128 + (((lane & 7) ^ (at & 7)) << 4));
+            if (to[k]) {
+              *reinterpret_cast<uint4*>(to[k]) = o;
+              to[k] += 128;
             }
           }
           __syncwarp();
