@@ -37,7 +37,7 @@ namespace {
 
 constexpr int kThreads = 576;
 constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
-constexpr int kUnitCost = 768;              // a unit's beginning and end, in tokens (measured: 384 and 1536 were up to 37 and 9 % slower)
+constexpr int kUnitCost = 448;              // a unit's beginning and end, in tokens (measured: 768 and 1024 were up to 4 and 7 % slower)
 constexpr int kLeastPiece = 256;            // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
 constexpr uint32_t kTmemCols = 512;
