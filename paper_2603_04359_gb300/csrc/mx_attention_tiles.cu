@@ -9,9 +9,9 @@
 // together, row r is head r % group of token r / group.
 //
 // Per step of 128 tokens at d = 128 the MMAs take 2080 cycles of an SM (32 of them, 65 each), the exponentials of 2 x 16384 scores 1024, the
-// unpacking ~400 issue slots a scheduler.  A step takes ~4750: a tile's weights (~3000: two passes over its scores, their way from and to
-// tensor memory), its two products and the waits between them follow one another, and two tiles in turn fill the tensor cores to 44 %.
-// 2048 tokens of 32 heads over 32768: 1132 us, 0.94 PFLOP/s.  What was slower: steps of 64 tokens with two buffers of scores a tile, whose
+// unpacking ~400 issue slots a scheduler.  A step takes ~4800: a tile's weights (~2900: two passes over its scores, their way from and to
+// tensor memory), its two products and the waits between them follow one another, and two tiles in turn fill the tensor cores to 42 %.
+// 2048 tokens of 32 heads over 32768: 1082 us, 0.98 PFLOP/s; a prompt of 4096: 211, a unit's beginning and end 12000 cycles of ~150000.  What was slower: steps of 64 tokens with two buffers of scores a tile, whose
 // products of 64 columns take as long as those of 128 (1350 to 1530 us); the maximum found along with the weights, and these again where
 // it grew, whose code does not stay in the instruction cache beside the other roles' (1360 with steps of 64); one ring for the copies
 // of keys and of values, where values that wait for room keep keys back (1430).
