@@ -10,7 +10,7 @@
 // A token's keys and values are 17/16 of a byte a channel for both, read once for all the query heads that share them: 152 SMs have
 // ~2.9 lane instructions a code in the time its bytes take from memory, and the unpacking is most of what there is to do: ~400 warp
 // instructions for 16 tokens of a head of 128 channels and 8 rows, 172 of them on the pipe that issues one every other cycle a scheduler.
-// 64 sequences of up to 8192 tokens, 8 key heads: 292 MB in 84 us (3.5 TB/s); one of 131000 tokens 46 us, 40 of them here; 2.3
+// 64 sequences of up to 8192 tokens, 8 key heads: 292 MB in 83 us (3.5 TB/s); one of 131000 tokens 45.5 us, 40 of them here; 2.3
 // instructions a cycle, from 16 warps an SM (128 registers; 12 and 20 warps were no faster).
 // Codes go from memory to registers in the layout of the matrix instructions' operands (which is what the cache's pieces are for) and
 // are unpacked in pairs there.  tcgen05 would want them unpacked into shared memory first, for 128 rows where there are 1 to 32.
@@ -313,21 +313,24 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
 
     // ---- queries to float16, in the order of the operand
     const int rows = min(ROWS, sq.ql * a.group - rt * ROWS);
-    for (int r = warp; r < ROWS; r += kWarps) {
-      constexpr int kPer = NB;                           // channels a lane: D / 32
+    constexpr int kPer = NB, kMine = ROWS / kWarps;      // channels a lane: D / 32; rows a warp, all on their way at once
+    uint32_t q_raw[kMine][kPer / 2];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      const int r = warp + k * kWarps, rr = rt * ROWS + r, j = rr / a.group;
+      const __nv_bfloat16* p = a.q + ((int64_t)(sq.begin + j) * a.hq + h * a.group + (rr - j * a.group)) * D + lane * kPer;
+#pragma unroll
+      for (int i = 0; i < kPer / 2; ++i) q_raw[k][i] = r < rows ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+    }
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      const int r = warp + k * kWarps, j = (rt * ROWS + r) / a.group;
       float x[kPer];
       float amax = 0.f;
-      const int rr = rt * ROWS + r, j = rr / a.group;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) x[i] = 0.f;
-      if (r < rows) {
-        const __nv_bfloat16* p = a.q + ((int64_t)(sq.begin + j) * a.hq + h * a.group + (rr - j * a.group)) * D + lane * kPer;
-#pragma unroll
-        for (int i = 0; i < kPer; i += 2) {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(p + i);
-          x[i] = __uint_as_float(w << 16);
-          x[i + 1] = __uint_as_float(w & 0xFFFF0000u);
-        }
+      for (int i = 0; i < kPer; i += 2) {
+        x[i] = __uint_as_float(q_raw[k][i / 2] << 16);
+        x[i + 1] = __uint_as_float(q_raw[k][i / 2] & 0xFFFF0000u);
       }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) amax = fmaxf(amax, __uint_as_float(min(__float_as_uint(x[i]) & 0x7FFFFFFFu, 0x7F800000u)));
@@ -339,8 +342,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       // channel c: block c / 32, lane's t = c % 32 / 8, then two halves u of four
 #pragma unroll
       for (int i = 0; i < kPer; i += 2) {
-        const int c = lane * kPer + i, b = c / 32, tt = c % 32 / 8, u = c % 8 / 4, k = c % 4 / 2;
-        reinterpret_cast<uint32_t*>(qs + (((r / 8) * NB + b) * 2 + u) * 32 + (r & 7) * 4 + tt)[k] = w[i / 2];
+        const int c = lane * kPer + i, b = c / 32, tt = c % 32 / 8, u = c % 8 / 4, two = c % 4 / 2;
+        reinterpret_cast<uint32_t*>(qs + (((r / 8) * NB + b) * 2 + u) * 32 + (r & 7) * 4 + tt)[two] = w[i / 2];
       }
       if (lane == 0) {
         const int64_t p = sq.len - sq.ql + j;
