@@ -150,6 +150,10 @@ __device__ __forceinline__ bool short_wait(uint64_t* bar, uint32_t parity, volat
     }
   return true;
 }
+template <bool B>
+struct Bool {
+  static constexpr bool value = B;
+};
 // What a CTA keeps.  A warp's region is its ring of steps (the codes of 32 tokens' keys, of their values, their scales), and then what it
 // hands on of its rows.
 template <int NB, int NT, int RESIDENT>
@@ -159,7 +163,7 @@ struct Layout {
   static constexpr int kStages = NB == 2 ? 4 : NB == 4 ? (RESIDENT == 2 ? 4 : 3) : (RESIDENT == 3 ? 2 : 3);
   static constexpr int kHanded = ROWS * kPitch * 4;
   static constexpr int kRegion = kStages * kStage > kHanded ? kStages * kStage : kHanded;
-  static constexpr int kQ = kWarps * kRegion, kMl = kQ + ROWS * D * 2, kRows = kMl + kWarps * ROWS * 8, kBytes = kRows + ROWS * 12;
+  static constexpr int kQ = kWarps * kRegion, kMl = kQ + ROWS * D * 2, kRows = kMl + kWarps * ROWS * 8, kBytes = kRows + (kWarps + 4) * ROWS * 4;
   static_assert(kRegion % 16 == 0 && kQ % 16 == 0 && kMl % 16 == 0, "");
 };
 
@@ -173,7 +177,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
   float2* mls = reinterpret_cast<float2*>(smem + L::kMl);                       // [warps][ROWS]
   float* fac = reinterpret_cast<float*>(smem + L::kRows);                       // rows: what a product of codes is times,
   int* lim = reinterpret_cast<int*>(fac + ROWS);                                // the last token seen (-1: none),
-  int* low = lim + ROWS;                                                        // and the first
+  int* low = lim + ROWS;                                                        // and the first,
+  int* power = low + ROWS;                                                      // fac over the scale, as a power of two
   __shared__ int64_t scan[kWarps];
   __shared__ int found_s;
   __shared__ int64_t found_at;
@@ -182,6 +187,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
   __shared__ int abort_flag;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
+  float* fac_step = reinterpret_cast<float*>(power + ROWS) + warp * ROWS;       // fac where a step's scales are relative to their largest
   const int hkv = a.c.hkv, cta = blockIdx.x;
   if (tid == 0) {
     for (int i = 0; i < kWarps * kStages; ++i) mbar_init(&full_bars[0][0] + i, 1);
@@ -334,7 +340,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) amax = fmaxf(amax, __uint_as_float(min(__float_as_uint(x[i]) & 0x7FFFFFFFu, 0x7F800000u)));
-      const int e = max((int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)) >> 23), 1);
+      const uint32_t largest = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
+      const int e = largest ? max((int)(largest >> 23), 1) : 127;
       const float up = e >= 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23);      // 2^(127 - e)
       uint32_t w[kPer / 2];
 #pragma unroll
@@ -348,6 +355,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       if (lane == 0) {
         const int64_t p = sq.len - sq.ql + j;
         fac[r] = ldexpf(a.scale, e - 140);
+        power[r] = e - 140;
         lim[r] = r < rows ? (int)(p < sq.end - 1 ? p : sq.end - 1) : -1;
         low[r] = a.window && p - a.window + 1 > 0 ? (int)(p - a.window + 1) : 0;
       }
@@ -363,14 +371,16 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
 #pragma unroll
           for (int u = 0; u < 2; ++u) qf[j][b][u] = qs[((j * NB + b) * 2 + u) * 32 + lane];
     }
-    // A score times fac less its row's `base` is what the exponential takes: base = m - (136 - ref), the weights times 2^(136 - ref), so
+    // A score, codes' product times fac, less its row's `base` is what the exponential takes: base = m - (136 - ref), the weights times 2^(136 - ref), so
     // that with a value's scale, 2^(byte - 127) of a byte up to ref, they are at most 2^(9 + kSlack).
     float f[NT][2], m[NT][2], base[NT][2], l[NT][2], acc[NB][2][NT][4];
+    bool odd_unit = false;                               // (uniform) what `steps` below goes on with in its other form
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         f[j][i] = fac[8 * j + 2 * t + i];
+        odd_unit |= !(fabsf(f[j][i]) < 0x1p100f);
         base[j][i] = m[j][i] = -1e30f;
         l[j][i] = 0.f;
       }
@@ -382,6 +392,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
         for (int j = 0; j < NT; ++j)
 #pragma unroll
           for (int k = 0; k < 4; ++k) acc[b][i][j][k] = 0.f;
+    odd_unit = __any_sync(0xFFFFFFFFu, odd_unit);
     int ref = kLowR;                                     // largest scale byte of values so far
     float most = kSlack + (float)(136 - kLowR);          // what a score may exceed its base by
     // tokens that all rows see
@@ -392,121 +403,68 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
     const int some_to = (int)(p_last < sq.end - 1 ? p_last : sq.end - 1);
     const int some_from = a.window && p_first - a.window + 1 > 0 ? (int)(p_first - a.window + 1) : 0;
 
-    for (; step < step1; step += kWarps, tok += kAhead) {
-      issue(step + (kStages - 1) * kWarps, tok + (kStages - 1) * kAhead);
-      if (!__all_sync(0xFFFFFFFFu, short_wait(&full[get], get_round & 1, &abort_flag, __LINE__))) break;
-      const uint8_t* st = ring + get * L::kStage;
-      const int here = has[warp][get];
-      uint32_t own[(NB + 3) / 4];                        // a token's values' scales
-      load_scales<NB>(st + 2 * L::kCodes + L::kScales + lane * NB, own);
-      if (!(here >> (lane >> 4) & 1))
+    // The steps that are left.  What is out of the ordinary has a copy of the code of its own, in which a warp does the rest of a unit (true:
+    // it is to go on there), and costs the other next to nothing (2 to 12 % where one code looked out for all of it).  A sum of codes times
+    // scales is at most 2^27 times the largest scale, and its row's factor comes after it: with keys' scales of 2^65 and more, factors far
+    // from one, scores of more than 2^16 (and values of NaN scales), scales are taken relative to the largest of those that some row sees, and a score is
+    // rounded to float32 before its base is taken off.
+    bool issued = false, large = false;
+    auto steps = [&](auto odd_form) -> bool {
+      constexpr bool kOdd = decltype(odd_form)::value;
+      for (; step < step1; step += kWarps, tok += kAhead) {
+        if (!issued) issue(step + (kStages - 1) * kWarps, tok + (kStages - 1) * kAhead);
+        issued = false;
+        if (!__all_sync(0xFFFFFFFFu, short_wait(&full[get], get_round & 1, &abort_flag, __LINE__))) return false;
+        const uint8_t* st = ring + get * L::kStage;
+        const int here = has[warp][get];
+        uint32_t own[(NB + 3) / 4], own_k[(NB + 3) / 4], high = 0u;      // a token's values' and keys' scales; keys' of 2^65 and more
+        load_scales<NB>(st + 2 * L::kCodes + L::kScales + lane * NB, own);
+        load_scales<NB>(st + 2 * L::kCodes + lane * NB, own_k);
+        if (!(here >> (lane >> 4) & 1))
 #pragma unroll
-        for (int i = 0; i < (NB + 3) / 4; ++i) own[i] = 0u;
+          for (int i = 0; i < (NB + 3) / 4; ++i) own[i] = own_k[i] = 0u;
+#pragma unroll
+        for (int i = 0; i < (NB + 3) / 4; ++i) high |= own_k[i] & (own_k[i] << 1) & 0x80808080u;
 
-      // ---- the values' reference
-      bool odd = false;
-      uint32_t big = most_byte(own[0]);
-      if constexpr (NB == 8) big = max(big, most_byte(own[NB / 4 - 1]));
-      if (__any_sync(0xFFFFFFFFu, big > (uint32_t)ref)) {
-        uint32_t real = 0;                               // NaN's 255 is none, nor is what no row sees, which may be anything
-        if (tok + lane >= some_from && tok + lane <= some_to)
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-            if (byte_at(own, b) != 255u) real = max(real, byte_at(own, b));
-        const int top = max((int)__reduce_max_sync(0xFFFFFFFFu, real), ref);
-        odd = __any_sync(0xFFFFFFFFu, big == 255u);
-        const float by = ex2((float)(ref - top));
-        ref = top;
-        most = kSlack + (float)(136 - ref);
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            base[j][i] = m[j][i] - (float)(136 - ref);
-            l[j][i] *= by;
+        float down = 1.f;                                  // (kOdd) the power of two that the keys' scales are multiplied by
+        if constexpr (kOdd) {
+          uint32_t real = 0;                               // (NaN's 255 is none, nor is what no row sees)
+          if (tok + lane >= some_from && tok + lane <= some_to)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                acc[b][c][j][i] *= by;
-                acc[b][c][j][2 + i] *= by;
-              }
-          }
-      }
-
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (!(here >> half & 1)) continue;
-        const int t0 = tok + 16 * half;
-        const uint8_t* kc = st + (16 * half + g) * (16 * NB) + t * (4 * NB);
-        const uint8_t* ks = st + 2 * L::kCodes + (16 * half + g) * NB;
-        const uint8_t* vc = st + L::kCodes + (16 * half + 2 * t) * (16 * NB) + g * (2 * NB);
-
-        // ---- scores
-        float x[NT][4];
-        {
-          float s0[NB], s1[NB];
-          uint32_t w0[(NB + 3) / 4], w1[(NB + 3) / 4], k0[NB], k1[NB];
-          load_scales<NB>(ks, w0);
-          load_scales<NB>(ks + 8 * NB, w1);
-          load_words<NB>(kc, k0);
-          load_words<NB>(kc + 8 * 16 * NB, k1);
-          scales_of<NB>(w0, s0);
-          scales_of<NB>(w1, s1);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            const uint32_t lo[4] = {code_pair<0>(k0[b]), code_pair<0>(k1[b]), code_pair<1>(k0[b]), code_pair<1>(k1[b])};
-            const uint32_t hi[4] = {code_pair<2>(k0[b]), code_pair<2>(k1[b]), code_pair<3>(k0[b]), code_pair<3>(k1[b])};
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-              const uint2 q0 = kKeepQ ? qf[kKeepQ ? j : 0][b][0] : qs[((j * NB + b) * 2) * 32 + lane];
-              const uint2 q1 = kKeepQ ? qf[kKeepQ ? j : 0][b][1] : qs[((j * NB + b) * 2 + 1) * 32 + lane];
-              float part[4];
-              mma_first(part, lo, q0.x, q0.y);
-              mma(part, hi, q1.x, q1.y);
-              if (b == 0) {
-                x[j][0] = part[0] * s0[0], x[j][1] = part[1] * s0[0], x[j][2] = part[2] * s1[0], x[j][3] = part[3] * s1[0];
-              } else {
-                x[j][0] = fmaf(part[0], s0[b], x[j][0]), x[j][1] = fmaf(part[1], s0[b], x[j][1]);
-                x[j][2] = fmaf(part[2], s1[b], x[j][2]), x[j][3] = fmaf(part[3], s1[b], x[j][3]);
-              }
-            }
-          }
+              if (byte_at(own_k, b) != 255u) real = max(real, byte_at(own_k, b));
+          const int kr = (int)__reduce_max_sync(0xFFFFFFFFu, real);
+          down = kr == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - kr) << 23);
+          __syncwarp();
+          if (lane < ROWS) fac_step[lane] = fminf(fmaxf(ldexpf(a.scale, power[lane] + kr - 127), -kMost), kMost);
+          __syncwarp();
         }
-        const bool partial = t0 + 15 > all_to || t0 < all_from;
-        auto hidden = [&](int j, int k) {
-          const int at_tok = t0 + g + 8 * (k >> 1), r = 8 * j + 2 * t + (k & 1);
-          return at_tok > lim[r] || at_tok < low[r];
-        };
-        float e[NT][4], top = -1e30f;
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            e[j][k] = fmaf(x[j][k], f[j][k & 1], -base[j][k & 1]);
-            if (partial && hidden(j, k)) e[j][k] = __int_as_float(0xFF800000);
-            top = fmaxf(top, e[j][k]);
-          }
 
-        // ---- running maxima
-        if (__any_sync(0xFFFFFFFFu, top > most)) {
+        // ---- the values' reference
+        bool nan = false;
+        uint32_t big = most_byte(own[0]);
+        if constexpr (NB == 8) big = max(big, most_byte(own[NB / 4 - 1]));
+        if (__any_sync(0xFFFFFFFFu, big > (uint32_t)ref || (!kOdd && high))) {
+          if (!kOdd && __any_sync(0xFFFFFFFFu, high || big == 255u)) {
+            issued = true;
+            return true;
+          }
+          uint32_t real = 0;                               // NaN's 255 is none, nor is what no row sees, which may be anything
+          if (tok + lane >= some_from && tok + lane <= some_to)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              if (byte_at(own, b) != 255u) real = max(real, byte_at(own, b));
+          const int top = max((int)__reduce_max_sync(0xFFFFFFFFu, real), ref);
+          nan = kOdd && __any_sync(0xFFFFFFFFu, big == 255u);
+          const float by = ex2((float)(ref - top));
+          ref = top;
+          most = kSlack + (float)(136 - ref);
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const float lo = partial && hidden(j, i) ? -1e30f : x[j][i] * f[j][i];
-              const float hi = partial && hidden(j, 2 + i) ? -1e30f : x[j][2 + i] * f[j][i];
-              float up = fmaxf(lo, hi);
-#pragma unroll
-              for (int k = 4; k < 32; k <<= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, k));
-              up = fmaxf(up, m[j][i]);
-              const float by = ex2(m[j][i] - up);
-              m[j][i] = up;
-              base[j][i] = up - (float)(136 - ref);
+              base[j][i] = m[j][i] - (float)(136 - ref);
               l[j][i] *= by;
-#pragma unroll
-              for (int k = i; k < 4; k += 2)
-                if (!(partial && hidden(j, k))) e[j][k] = fmaf(x[j][k], f[j][i], -base[j][i]);
 #pragma unroll
               for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -516,62 +474,164 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
                 }
             }
         }
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            x[j][k] = ex2(e[j][k]);
-            l[j][k & 1] += x[j][k];
-          }
 
-        // ---- values
-        float s0[NB], s1[NB];
-        uint32_t w0[(NB + 3) / 4], w1[(NB + 3) / 4], v[4][NB / 2];
-        load_scales<NB>(ks + L::kScales, w0);
-        load_scales<NB>(ks + L::kScales + 8 * NB, w1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_words<NB / 2>(vc + ((i & 1) + 8 * (i >> 1)) * (16 * NB), v[i]);
-        scales_of<NB>(w0, s0);
-        scales_of<NB>(w1, s1);
+        for (int half = 0; half < 2; ++half) {
+          if (!(here >> half & 1)) continue;
+          const int t0 = tok + 16 * half;
+          const uint8_t* kc = st + (16 * half + g) * (16 * NB) + t * (4 * NB);
+          const uint8_t* ks = st + 2 * L::kCodes + (16 * half + g) * NB;
+          const uint8_t* vc = st + L::kCodes + (16 * half + 2 * t) * (16 * NB) + g * (2 * NB);
+
+          // ---- scores
+          float x[NT][4];
+          {
+            float s0[NB], s1[NB];
+            uint32_t w0[(NB + 3) / 4], w1[(NB + 3) / 4], k0[NB], k1[NB];
+            load_scales<NB>(ks, w0);
+            load_scales<NB>(ks + 8 * NB, w1);
+            load_words<NB>(kc, k0);
+            load_words<NB>(kc + 8 * 16 * NB, k1);
+            scales_of<NB>(w0, s0);
+            scales_of<NB>(w1, s1);
+            if constexpr (kOdd)
 #pragma unroll
-        for (int i = 0; i < NB / 2; ++i) {
-          // even and odd channels of pairs of tokens: nibbles side by side
-          uint32_t ev[2], ov[2];
+              for (int b = 0; b < NB; ++b) s0[b] *= down, s1[b] *= down;
 #pragma unroll
-          for (int h2 = 0; h2 < 2; ++h2) {
-            const uint32_t A = v[2 * h2][i], B = v[2 * h2 + 1][i];
-            ev[h2] = (A & 0x0F0F0F0Fu) | ((B << 4) & 0xF0F0F0F0u);
-            ov[h2] = ((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u);
-          }
-          const uint32_t va[4][4] = {{code_pair<0>(ev[0]), code_pair<0>(ov[0]), code_pair<0>(ev[1]), code_pair<0>(ov[1])},
-                                     {code_pair<1>(ev[0]), code_pair<1>(ov[0]), code_pair<1>(ev[1]), code_pair<1>(ov[1])},
-                                     {code_pair<2>(ev[0]), code_pair<2>(ov[0]), code_pair<2>(ev[1]), code_pair<2>(ov[1])},
-                                     {code_pair<3>(ev[0]), code_pair<3>(ov[0]), code_pair<3>(ev[1]), code_pair<3>(ov[1])}};
+            for (int b = 0; b < NB; ++b) {
+              const uint32_t lo[4] = {code_pair<0>(k0[b]), code_pair<0>(k1[b]), code_pair<1>(k0[b]), code_pair<1>(k1[b])};
+              const uint32_t hi[4] = {code_pair<2>(k0[b]), code_pair<2>(k1[b]), code_pair<3>(k0[b]), code_pair<3>(k1[b])};
 #pragma unroll
-          for (int o = 0; o < 2; ++o) {
-            const int b = 2 * i + o;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-              float w[4] = {x[j][0] * s0[b], x[j][1] * s0[b], x[j][2] * s1[b], x[j][3] * s1[b]};
-              if (odd) {                                 // a NaN scale counts for rows that see its token only
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  if (x[j][k] == 0.f) w[k] = 0.f;
+              for (int j = 0; j < NT; ++j) {
+                const uint2 q0 = kKeepQ ? qf[kKeepQ ? j : 0][b][0] : qs[((j * NB + b) * 2) * 32 + lane];
+                const uint2 q1 = kKeepQ ? qf[kKeepQ ? j : 0][b][1] : qs[((j * NB + b) * 2 + 1) * 32 + lane];
+                float part[4];
+                mma_first(part, lo, q0.x, q0.y);
+                mma(part, hi, q1.x, q1.y);
+                if (b == 0) {
+                  x[j][0] = part[0] * s0[0], x[j][1] = part[1] * s0[0], x[j][2] = part[2] * s1[0], x[j][3] = part[3] * s1[0];
+                } else {
+                  x[j][0] = fmaf(part[0], s0[b], x[j][0]), x[j][1] = fmaf(part[1], s0[b], x[j][1]);
+                  x[j][2] = fmaf(part[2], s1[b], x[j][2]), x[j][3] = fmaf(part[3], s1[b], x[j][3]);
+                }
               }
-              const uint32_t p0 = transpose(f16_pair(w[0], w[1])), p1 = transpose(f16_pair(w[2], w[3]));
-              mma(acc[b][0][j], va[2 * o], p0, p1);
-              mma(acc[b][1][j], va[2 * o + 1], p0, p1);
+            }
+          }
+          const bool partial = t0 + 15 > all_to || t0 < all_from;
+          auto hidden = [&](int j, int k) {
+            const int at_tok = t0 + g + 8 * (k >> 1), r = 8 * j + 2 * t + (k & 1);
+            return at_tok > lim[r] || at_tok < low[r];
+          };
+          float e[NT][4], top = -1e30f;
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if constexpr (kOdd) {                        // (rounded before the base is taken off)
+                x[j][k] *= fac_step[8 * j + 2 * t + (k & 1)];
+                e[j][k] = x[j][k] - base[j][k & 1];
+              } else {
+                e[j][k] = fmaf(x[j][k], f[j][k & 1], -base[j][k & 1]);
+              }
+              if (partial && hidden(j, k)) e[j][k] = __int_as_float(0xFF800000);
+              top = fmaxf(top, e[j][k]);
+            }
+
+          // ---- running maxima
+          if (__any_sync(0xFFFFFFFFu, top > most || (!kOdd && large))) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                // (rounded here: what a product keeps beyond float32 would be a large difference of large scores)
+                if constexpr (!kOdd) x[j][i] *= f[j][i], x[j][2 + i] *= f[j][i];
+                const float lo = partial && hidden(j, i) ? -1e30f : x[j][i];
+                const float hi = partial && hidden(j, 2 + i) ? -1e30f : x[j][2 + i];
+                float up = fmaxf(lo, hi);
+#pragma unroll
+                for (int k = 4; k < 32; k <<= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, k));
+                up = fmaxf(up, m[j][i]);
+                const float by = ex2(m[j][i] - up);
+                if constexpr (!kOdd) large |= __any_sync(0xFFFFFFFFu, fabsf(up) > 0x1p16f && up != -1e30f);
+                m[j][i] = up;
+                base[j][i] = up - (float)(136 - ref);
+                l[j][i] *= by;
+#pragma unroll
+                for (int k = i; k < 4; k += 2)
+                  if (!(partial && hidden(j, k))) e[j][k] = x[j][k] - base[j][i];
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                  for (int c = 0; c < 2; ++c) {
+                    acc[b][c][j][i] *= by;
+                    acc[b][c][j][2 + i] *= by;
+                  }
+              }
+          }
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              x[j][k] = ex2(e[j][k]);
+              l[j][k & 1] += x[j][k];
+            }
+
+          // ---- values
+          float s0[NB], s1[NB];
+          uint32_t w0[(NB + 3) / 4], w1[(NB + 3) / 4], v[4][NB / 2];
+          load_scales<NB>(ks + L::kScales, w0);
+          load_scales<NB>(ks + L::kScales + 8 * NB, w1);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load_words<NB / 2>(vc + ((i & 1) + 8 * (i >> 1)) * (16 * NB), v[i]);
+          scales_of<NB>(w0, s0);
+          scales_of<NB>(w1, s1);
+#pragma unroll
+          for (int i = 0; i < NB / 2; ++i) {
+            // even and odd channels of pairs of tokens: nibbles side by side
+            uint32_t ev[2], ov[2];
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2) {
+              const uint32_t A = v[2 * h2][i], B = v[2 * h2 + 1][i];
+              ev[h2] = (A & 0x0F0F0F0Fu) | ((B << 4) & 0xF0F0F0F0u);
+              ov[h2] = ((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u);
+            }
+            const uint32_t va[4][4] = {{code_pair<0>(ev[0]), code_pair<0>(ov[0]), code_pair<0>(ev[1]), code_pair<0>(ov[1])},
+                                       {code_pair<1>(ev[0]), code_pair<1>(ov[0]), code_pair<1>(ev[1]), code_pair<1>(ov[1])},
+                                       {code_pair<2>(ev[0]), code_pair<2>(ov[0]), code_pair<2>(ev[1]), code_pair<2>(ov[1])},
+                                       {code_pair<3>(ev[0]), code_pair<3>(ov[0]), code_pair<3>(ev[1]), code_pair<3>(ov[1])}};
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+              const int b = 2 * i + o;
+#pragma unroll
+              for (int j = 0; j < NT; ++j) {
+                float w[4] = {x[j][0] * s0[b], x[j][1] * s0[b], x[j][2] * s1[b], x[j][3] * s1[b]};
+                if (kOdd && nan) {                         // a NaN scale counts for rows that see its token only
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+                    if (x[j][k] == 0.f) w[k] = 0.f;
+                }
+                const uint32_t p0 = transpose(f16_pair(w[0], w[1])), p1 = transpose(f16_pair(w[2], w[3]));
+                mma(acc[b][0][j], va[2 * o], p0, p1);
+                mma(acc[b][1][j], va[2 * o + 1], p0, p1);
+              }
             }
           }
         }
+        __syncwarp();                                      // all lanes have read the step
+        --flying;
+        if (++get == kStages) {
+          get = 0;
+          ++get_round;
+        }
+        if (!kOdd && large) {
+          step += kWarps, tok += kAhead;
+          return true;
+        }
       }
-      __syncwarp();                                      // all lanes have read the step
-      --flying;
-      if (++get == kStages) {
-        get = 0;
-        ++get_round;
-      }
-    }
+      return false;
+    };
+    if (!odd_unit) odd_unit = steps(Bool<false>());
+    if (odd_unit) steps(Bool<true>());
     if (abort_flag) {                                    // a wait gave up: the copies still on their way, then out
       volatile int none = 0;
       for (; flying > 0; --flying) {
@@ -731,7 +791,7 @@ cudaError_t launch_mx_attention(const void* q, int64_t n, int64_t hq, const uint
   a.c = {const_cast<uint8_t*>(cache), pages * page, (int)page, log, (int)hkv, mx_page_bytes(page, d)};
   a.pages = pages, a.table = table, a.lens = lens, a.offsets = offsets, a.width = width;
   a.n = (int)n, a.hq = (int)hq, a.group = (int)(hq / hkv), a.seqs = (int)seqs;
-  a.scale = scale * 1.44269504f;
+  a.scale = std::min(std::max(scale * 1.44269504f, -kMost), kMost);
   a.status = status, a.window = window, a.out = out, a.out_f32 = out_dtype == 0;
   const Form f = form_of(n, seqs, a.group, d);
   const Needs needs(n, seqs, hq, hkv, d, width * page);

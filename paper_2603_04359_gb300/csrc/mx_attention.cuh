@@ -5,6 +5,7 @@
 
 namespace cat {
 
+constexpr float kMost = 3.402823466e38f;    // the largest float32
 constexpr float kSlack = 6.f;               // a row's scores may exceed its running maximum by this (binary orders) before it follows
 
 // A unit (sequence, row tile, head) of which a CTA has a part and not the whole: it has two at most, that which it goes on with and
