@@ -172,7 +172,7 @@ struct Bars {
   uint64_t raw_full[6], raw_empty[6], k_full[4], k_empty[4], v_full[4], v_empty[4], q_full, s_full[2][2], p_full[2][2], pv_done[2][2], most_full,
       mma_done;
   // (of eight steps: keys are unpacked up to five steps ahead of scores that are still read)
-  float k_factor[8][4];                     // 2^(ref - 139) of 32 tokens' keys
+  int k_power[8][4];                        // 2^(ref - 139) of 32 tokens' keys, as a float32's exponent field
   uint32_t there[8];                        // which 16-token groups of a step are on pages
   uint32_t raw_there[6];
   uint32_t v_ref[4];                        // the values' reference, + 256 where a scale of the step's is NaN
@@ -189,6 +189,9 @@ static_assert(sizeof(Bars) <= kBarRoom, "barrier room");
 // ---- tensor memory
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -337,12 +340,19 @@ __device__ __forceinline__ void tmem_have16(uint32_t (&v)[16]) {
                  "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
-// What a product is times; never 0, which would make NaN of the infinity that stands for what is not seen.
-__device__ __forceinline__ float score_factor(float fac, float k_factor) { return fmaxf(fac * k_factor, 0x1p-126f); }
+// What a product of a row's query and keys is times: significand * 2^power of the row, times the keys' power of two.  Never 0, which would
+// make NaN of the infinity that stands for what is not seen, nor infinite, which would of a product that is 0.
+struct Factor {
+  uint32_t significand;                     // of [1, 2), its 23 bits
+  int power;
+  __device__ __forceinline__ float of(int k_power) const {
+    return __uint_as_float((uint32_t)min(max(power + k_power, 1), 254) << 23 | significand);
+  }
+};
 
 // The largest score of a row's KT, times its factors.
 template <int KT>
-__device__ __forceinline__ float largest(uint32_t s_col, const float* k_factor, float fac) {
+__device__ __forceinline__ float largest(uint32_t s_col, const int* k_power, Factor fac) {
   float most = -INFINITY;
   uint32_t a[16], b[16];
   auto of = [](const uint32_t (&v)[16]) {
@@ -359,7 +369,7 @@ __device__ __forceinline__ float largest(uint32_t s_col, const float* k_factor, 
 #pragma unroll 1
   for (int c = 0; c < KT / 32; ++c) {
     tmem_ld16(s_col + 32 * c + 16, b);
-    const float f = score_factor(fac, k_factor[c]), m = of(a);
+    const float f = fac.of(k_power[c]), m = of(a);
     tmem_have16(b);
     tmem_ld16(s_col + 32 * min(c + 1, KT / 32 - 1), a);
     most = fmaxf(most, fmaxf(m, of(b)) * f);
@@ -369,13 +379,13 @@ __device__ __forceinline__ float largest(uint32_t s_col, const float* k_factor, 
 }
 // A row's weights 2^(score + base), as float16 pairs in the scores' place; their sum is added to `sum`.
 template <int KT>
-__device__ __forceinline__ void weights(uint32_t s_col, const float* k_factor, float fac, float base, float2& sum) {
+__device__ __forceinline__ void weights(uint32_t s_col, const int* k_power, Factor fac, float base, float2& sum) {
   float2 part = make_float2(0.f, 0.f);
 #pragma unroll 1
   for (int c = 0; c < KT / 32; ++c) {
     uint32_t v[32], w[16];
     CAT_TMEM_LD32(s_col + 32 * c, v);
-    const float f = score_factor(fac, k_factor[c]);
+    const float f = fac.of(k_power[c]);
     tmem_have32(v);
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
@@ -390,6 +400,26 @@ __device__ __forceinline__ void weights(uint32_t s_col, const float* k_factor, f
     tmem_st16(s_col + 16 * c, w);
   }
   sum = add2(sum, part);
+}
+// The same of scores that are rounded before m is taken off: what a product keeps beyond float32 would be a large difference of large scores.
+template <int KT>
+__device__ __forceinline__ float weights_apart(uint32_t s_col, const int* k_power, Factor fac, float m) {
+  float sum = 0.f;
+#pragma unroll 1
+  for (int c = 0; c < KT / 16; ++c) {
+    uint32_t v[16], w[8];
+    tmem_ld16(s_col + 16 * c, v);
+    const float f = fac.of(k_power[c / 2]);
+    tmem_have16(v);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float x = ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[i]), f), -m) + 8.f), y = ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[i + 1]), f), -m) + 8.f);
+      sum += x + y;
+      w[i / 2] = f16_pair(x, y);
+    }
+    tmem_st8(s_col + 8 * c, w);
+  }
+  return sum;
 }
 // Scores of tokens that a row does not see become -infinity where they are (steps at an end of what the rows see alone come here).
 template <int KT>
@@ -542,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       }
       // The warp's rows to float16, a row's largest channel in [2^13, 2^14); a negative scale goes into its sign.  All of them on their
       // way at once (D / 8 lanes a row), to where each thread then rewrites its own.
-      float fac;
+      Factor fac;
       {
         constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
         const int warp_row = tile * 128 + (warp & 3) * 32;
@@ -583,7 +613,9 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           const uint4 v = *p;
           *p = make_uint4(half2_of(v.x), half2_of(v.y), half2_of(v.z), half2_of(v.w));
         }
-        fac = ldexpf(fabsf(a.scale), e - 140);
+        int power;
+        const float scale = 2.f * frexpf(fabsf(a.scale), &power);      // (of [1, 2), or 0)
+        fac = {__float_as_uint(scale) & 0x7FFFFFu, a.scale == 0.f ? -1000 : power - 1 + e - 140};
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -595,14 +627,14 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       const int low = real && a.window && p - a.window + 1 > 0 ? (int)(p - a.window + 1) : 0;
       const bool tile_real = tile * 128 < u.rows, any_real = __any_sync(0xFFFFFFFFu, real);
       float m = 0.f;
-      bool seen = false;                                 // the maximum is one of scores
+      bool seen = false, apart = false;                  // the maximum is one of scores; some row's is more than 2^16
       float2 l2 = make_float2(0.f, 0.f);
       int ref = 0;
       uint32_t nan_blocks = 0;
       for (int step = u.j0; step < u.j1; ++step, ++jj) {
         if (!tile_real) continue;
         const uint32_t b = jj & (kBufs - 1), s_col = s_cols + tj % SB * KT;
-        const float* k_factor = bars->k_factor[jj & 7];
+        const int* k_power = bars->k_power[jj & 7];
         if (!CAT_WAIT(&bars->s_full[tile][tj % SB], tj / SB & 1)) break;
         tc_fence_after();
         if (!any_real) {
@@ -613,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           constexpr uint32_t kAll = (1u << (KT / 16)) - 1u;
           const bool full = __all_sync(0xFFFFFFFFu, t0 + KT - 1 <= lim && t0 >= low) && there == kAll;
           if (!full) hide<KT>(s_col, t0, lim, low, there);
-          const float most = largest<KT>(s_col, k_factor, fac);
+          const float most = largest<KT>(s_col, k_power, fac);
           if (!CAT_WAIT(&bars->v_full[b], (jj >> kBufLog) & 1)) break;       // (the values' reference)
           const int now = (int)(bars->v_ref[b] & 255u);
           const bool grows = seen ? most > m + kSlack : most > -INFINITY;
@@ -621,6 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
             const float up = grows ? most : m, by = seen ? ex2(m - up) : 1.f;       // (nothing seen: all is 0)
             m = up;
             seen |= grows;
+            apart = __any_sync(0xFFFFFFFFu, fabsf(m) > 0x1p16f);
             l2.x *= by, l2.y *= by;
             if (step != u.j0) {
               if (!CAT_WAIT(&bars->pv_done[tile][(tj - 1) % SB], (tj - 1) / SB & 1)) break;
@@ -638,7 +671,10 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
             }
             ref = now;
           }
-          weights<KT>(s_col, k_factor, fac, 8.f - m, l2);    // (times 2^8)
+          if (__builtin_expect(apart, 0))
+            l2.x += weights_apart<KT>(s_col, k_power, fac, m);
+          else
+            weights<KT>(s_col, k_power, fac, 8.f - m, l2);   // (times 2^8)
           if (bars->v_ref[b] & 256u)
             for (int i = 0; i < KT; ++i) {
               const int at = t0 + i;
@@ -775,7 +811,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
             if (bytes[i] == 255) scale[i] = __half2half2(__ushort_as_half(0x7FFF));
           }
           if (jj >= kBufs && !CAT_WAIT(&bars->k_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
-          if (lane == 0 && half == 0) bars->k_factor[jj & 7][row / 32] = __uint_as_float((uint32_t)(kref - 12) << 23);
+          if (lane == 0 && half == 0) bars->k_power[jj & 7][row / 32] = kref - 12;
           if (w == 0 && lane == 0) bars->there[jj & 7] = there;
         }
         unpack_row<NB>(raw, smem + (values ? C::kOffV : C::kOffK) + b * C::kTile, row, half, values, scale);

@@ -59,8 +59,56 @@ def test_keys_far_from_one(size, d, rows):
     check(b, scale=d ** -0.5 / size)
 
 
+@pytest.mark.parametrize("rows", [FEW, TILES])
+@pytest.mark.parametrize("size,key", [(2.0 ** -120, 2.0 ** 4), (2.0 ** 120, 2.0 ** -4), (2.0 ** -60, 2.0 ** -58), (2.0 ** 100, 2.0 ** -100),
+                                      (2.0 ** -100, 2.0 ** 110)])
+def test_queries_and_keys_far_from_one(size, key, rows):
+    b = Batch(32, [300, 90, 150], rows, 4, 2, 128, 32, size=key)
+    b.q = b.q * size
+    b.q[0] = 0.0
+    b.q[3:5] = b.q[3:5] / size
+    scale = np.sqrt(1 / 128) / size / key
+    with np.errstate(over="ignore"):
+        ok = abs(np.float32(scale * 2)) < np.finfo(np.float32).max
+    check(b, scale=scale if ok else 2.0 ** 127)
+
+
 def grown(b, s, at, size, kind):
     """The token's keys or values a size larger."""
     t = np.array([at])
     x = b.rng.standard_normal((1, b.cache.shape[2], b.d)) * size
     rewrite(b, s, t, **{kind: x})
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_tiles_queries_far_from_one_and_not_finite(d):
+    """The tiles' way of a query to float16: zero rows, the largest and smallest, NaN and infinity, and the rows beside them."""
+    b = Batch(38 + d, [300, 70], [200, 40], 4, 2, d, 32)
+    up = torch.ones((240, 4, 1), dtype=torch.float32, device=b.q.device)
+    up[3], up[70, 1], up[150, 2], up[239, 3] = 0.0, 2.0 ** 120, 2.0 ** -110, 2.0 ** 123
+    b.q = (b.q.float() * up).to(torch.bfloat16)
+    for scale in (d ** -0.5, -0.2, 0.0):
+        check(b, scale=scale)
+    small = 2.0 ** 100
+    b.q = (b.q.float() * torch.where(up > 1, 1 / small, 1.0)).to(torch.bfloat16)
+    check(b, scale=2.0 ** -20)
+    b.q[20, 1, 5], b.q[129, 3, 0] = float("nan"), float("inf")
+    g = host(b.run())
+    odd = np.zeros((240, 4), dtype=bool)
+    odd[20, 1] = odd[129, 3] = True
+    assert np.isnan(g[odd]).all() and np.isfinite(g[~odd]).all()
+    b.q[20, 1, 5], b.q[129, 3, 0] = 0.0, 0.0
+    again = host(b.run())
+    assert np.array_equal(g[~odd], again[~odd])
+
+
+def test_many_sequences_some_of_many_rows():
+    """More sequences than the tiles' block has threads, prompts among them."""
+    rng = np.random.default_rng(2)
+    lens, rows = rng.integers(0, 40, 1300), np.ones(1300, dtype=int)
+    rows[::7] = 0
+    for s in (0, 575, 576, 577, 900, 1299):
+        lens[s], rows[s] = 60 + s % 7, 30 + s % 5
+    b = Batch(39, lens.tolist(), rows.tolist(), 4, 2, 64, 16)
+    check(b)
+    check(b, window=17)
