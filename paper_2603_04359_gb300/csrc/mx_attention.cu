@@ -381,7 +381,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       for (int i = 0; i < 2; ++i) {
         f[j][i] = fac[8 * j + 2 * t + i];
         odd_unit |= !(fabsf(f[j][i]) < 0x1p100f);
-        base[j][i] = m[j][i] = -1e30f;
+        base[j][i] = m[j][i] = kNone;
         l[j][i] = 0.f;
       }
 #pragma unroll
@@ -522,14 +522,14 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
             const int at_tok = t0 + g + 8 * (k >> 1), r = 8 * j + 2 * t + (k & 1);
             return at_tok > lim[r] || at_tok < low[r];
           };
-          float e[NT][4], top = -1e30f;
+          float e[NT][4], top = kNone;
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              if constexpr (kOdd) {                        // (rounded before the base is taken off)
+              if constexpr (kOdd) {                        // (rounded before the maximum is taken off, and that before what the base has beside it)
                 x[j][k] *= fac_step[8 * j + 2 * t + (k & 1)];
-                e[j][k] = x[j][k] - base[j][k & 1];
+                e[j][k] = (x[j][k] - m[j][k & 1]) + (float)(136 - ref);
               } else {
                 e[j][k] = fmaf(x[j][k], f[j][k & 1], -base[j][k & 1]);
               }
@@ -545,20 +545,20 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
               for (int i = 0; i < 2; ++i) {
                 // (rounded here: what a product keeps beyond float32 would be a large difference of large scores)
                 if constexpr (!kOdd) x[j][i] *= f[j][i], x[j][2 + i] *= f[j][i];
-                const float lo = partial && hidden(j, i) ? -1e30f : x[j][i];
-                const float hi = partial && hidden(j, 2 + i) ? -1e30f : x[j][2 + i];
+                const float lo = partial && hidden(j, i) ? kNone : x[j][i];
+                const float hi = partial && hidden(j, 2 + i) ? kNone : x[j][2 + i];
                 float up = fmaxf(lo, hi);
 #pragma unroll
                 for (int k = 4; k < 32; k <<= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, k));
                 up = fmaxf(up, m[j][i]);
                 const float by = ex2(m[j][i] - up);
-                if constexpr (!kOdd) large |= __any_sync(0xFFFFFFFFu, fabsf(up) > 0x1p16f && up != -1e30f);
+                if constexpr (!kOdd) large |= __any_sync(0xFFFFFFFFu, fabsf(up) > 0x1p16f && up != kNone);
                 m[j][i] = up;
                 base[j][i] = up - (float)(136 - ref);
                 l[j][i] *= by;
 #pragma unroll
                 for (int k = i; k < 4; k += 2)
-                  if (!(partial && hidden(j, k))) e[j][k] = x[j][k] - base[j][i];
+                  if (!(partial && hidden(j, k))) e[j][k] = (x[j][k] - up) + (float)(136 - ref);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll

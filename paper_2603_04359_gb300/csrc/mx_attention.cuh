@@ -6,6 +6,7 @@
 namespace cat {
 
 constexpr float kMost = 3.402823466e38f;    // the largest float32
+constexpr float kNone = -kMost;             // the maximum of no scores: none is less, but one that float32 does not hold
 constexpr float kSlack = 6.f;               // a row's scores may exceed its running maximum by this (binary orders) before it follows
 
 // A unit (sequence, row tile, head) of which a CTA has a part and not the whole: it has two at most, that which it goes on with and
@@ -143,7 +144,7 @@ struct JoinRow {
   float top, sum;
   float4 o[kWide];
   __device__ __forceinline__ void clear() {
-    top = -1e30f, sum = 0.f;
+    top = kNone, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kWide; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
@@ -165,7 +166,7 @@ struct JoinRow {
     for (int base = from; base <= last; base += 32 * stride) {
       const int k = base + lane * stride;
       auto slot_of = [&](int c) { return ((int64_t)2 * c + (c == first ? 1 : 0)) * ROWS + r; };
-      float2 ml = make_float2(-1e30f, 0.f);
+      float2 ml = make_float2(kNone, 0.f);
       if (k <= last) ml = *reinterpret_cast<const float2*>(a.ml + slot_of(k) * 2);
       const bool some = ml.y != 0.f;                     // (a part of no tokens has no values)
       float now = some ? fmaxf(top, ml.x) : top;

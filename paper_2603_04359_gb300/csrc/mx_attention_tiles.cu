@@ -566,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         if (real && u.nothing) {
           for (int c = 0; c < D; c += 4) store4(a, row + c, make_float4(0.f, 0.f, 0.f, 0.f));
         } else if (real) {
-          *reinterpret_cast<float2*>(a.ml + ((int64_t)slot * ROWS + r) * 2) = make_float2(-1e30f, 0.f);
+          *reinterpret_cast<float2*>(a.ml + ((int64_t)slot * ROWS + r) * 2) = make_float2(kNone, 0.f);
         }
         continue;
       }

@@ -80,6 +80,28 @@ def grown(b, s, at, size, kind):
     rewrite(b, s, t, **{kind: x})
 
 
+@pytest.mark.parametrize("rows,lens", [([1, 1, 1], [1, 40, 5000]), ([200, 40], [300, 3000])])
+@pytest.mark.parametrize("size", [-1.0, 1.0])
+def test_scores_of_any_size(size, rows, lens):
+    """Equal scores are equal weights, whatever they are: here 2^112 and -2^112."""
+    d = 128
+    b = Batch(36, lens, rows, 8, 2, d, 32)
+    b.q = torch.ones_like(b.q)
+    for s, n in enumerate(lens):
+        rewrite(b, s, np.arange(n), k=np.full((n, 2, d), 2.0 ** 50))
+    got = host(b.run(scale=size * 2.0 ** 55, out_dtype=torch.float32))
+    at = 0
+    for s, (n, r) in enumerate(zip(lens, rows)):
+        t = np.arange(n)
+        v = C.load(host(b.cache), b.page, d, b.table[s, t // b.page] * b.page + t % b.page, 1)
+        for j in range(r):
+            p = n - r + j + 1
+            # (weights of 1 exactly; a sum of p values in float32)
+            bound = (p / 16 + 64) * 2.0 ** -23 * np.abs(v[:p]).mean(0)
+            assert np.all(np.abs(got[at] - np.repeat(v[:p].mean(0), 4, 0)) <= np.repeat(bound, 4, 0)), (s, j)
+            at += 1
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_tiles_queries_far_from_one_and_not_finite(d):
     """The tiles' way of a query to float16: zero rows, the largest and smallest, NaN and infinity, and the rows beside them."""
