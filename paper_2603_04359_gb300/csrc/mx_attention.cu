@@ -648,7 +648,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       return;
     }
 
-    // ---- the warps' parts together
+    // ---- the warps' parts together: means of values each, as everywhere from here on (sums of many large values could leave float32)
     const float unref = ex2((float)(ref - 136));
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -656,33 +656,37 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) l[j][i] += __shfl_xor_sync(0xFFFFFFFFu, l[j][i], k);
+        const float by = l[j][i] == 0.f ? 0.f : 1.f / l[j][i];
         if (g == 0) mls[warp * ROWS + 8 * j + 2 * t + i] = make_float2(m[j][i], l[j][i] * unref);
         float* o = reinterpret_cast<float*>(smem + warp * L::kRegion) + (8 * j + 2 * t + i) * kPitch;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-          *reinterpret_cast<float4*>(o + 32 * b + 4 * g) = make_float4(acc[b][0][j][i] * unref, acc[b][0][j][2 + i] * unref,
-                                                                       acc[b][1][j][i] * unref, acc[b][1][j][2 + i] * unref);
+          *reinterpret_cast<float4*>(o + 32 * b + 4 * g) = make_float4(acc[b][0][j][i] * by, acc[b][0][j][2 + i] * by,
+                                                                       acc[b][1][j][i] * by, acc[b][1][j][2 + i] * by);
       }
     __syncthreads();
     for (int i = tid; i < rows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), c = i - r * (D / 4);
-      float top = mls[r].x, sum = 0.f;
+      float top = mls[r].x, sum = 0.f, share[kWarps];
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) top = fmaxf(top, mls[w * ROWS + r].x);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float2 ml = mls[w * ROWS + r];
-        const float by = ex2(ml.x - top);
+        share[w] = ml.y * ex2(ml.x - top);
+        sum += share[w];
+      }
+      const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float by = share[w] * inv;
         const float4 v = *reinterpret_cast<const float4*>(smem + w * L::kRegion + (r * kPitch + 4 * c) * 4);
-        sum = fmaf(ml.y, by, sum);
         o.x = fmaf(v.x, by, o.x), o.y = fmaf(v.y, by, o.y), o.z = fmaf(v.z, by, o.z), o.w = fmaf(v.w, by, o.w);
       }
       if (whole) {
         const int rr = rt * ROWS + r, j = rr / a.group;
         const int64_t to_row = ((int64_t)(sq.begin + j) * a.hq + h * a.group + (rr - j * a.group)) * D + 4 * c;
-        const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
-        o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
         store4(a, to_row, o);
       } else {
         *reinterpret_cast<float4*>(a.parts + ((int64_t)slot * ROWS + r) * D + 4 * c) = o;

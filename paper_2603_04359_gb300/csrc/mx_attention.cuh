@@ -137,7 +137,8 @@ __device__ __forceinline__ void clear_rows(const AttnArgs& a) {
 
 constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps;
 
-// A row of a unit's output, or 4 kLanes kWide channels of it, from some of its parts: a lane has kWide times four channels.
+// A row of a unit's output, or 4 kLanes kWide channels of it, from some of its parts: a lane has kWide times four channels.  Parts are means
+// of values with the sums of their weights, and so is what is made of them: a sum of many large values could leave float32.
 template <int D, int kLanes, int kWide>
 struct JoinRow {
   static constexpr int lanes = kLanes, wide = kWide;
@@ -148,11 +149,14 @@ struct JoinRow {
 #pragma unroll
     for (int i = 0; i < kWide; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  __device__ __forceinline__ void follow(float now) {
-    const float was = ex2(top - now);
-    top = now, sum *= was;
+  // Weights that add up to `more`, relative to 2^now, are to be added: what they are times is returned.
+  __device__ __forceinline__ float follow(float now, float more) {
+    const float had = sum * ex2(top - now);
+    top = now, sum = had + more;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum, was = had * inv;
 #pragma unroll
     for (int i = 0; i < kWide; ++i) o[i].x *= was, o[i].y *= was, o[i].z *= was, o[i].w *= was;
+    return inv;
   }
   __device__ __forceinline__ void add(const float4 (&v)[kWide], float by) {
 #pragma unroll
@@ -172,9 +176,10 @@ struct JoinRow {
       float now = some ? fmaxf(top, ml.x) : top;
 #pragma unroll
       for (int i = 1; i < 32; i <<= 1) now = fmaxf(now, __shfl_xor_sync(0xFFFFFFFFu, now, i));
-      follow(now);
-      const float mine = some ? ex2(ml.x - now) : 0.f;
-      if (some) sum = fmaf(ml.y, mine, sum);
+      float mine = some ? ml.y * ex2(ml.x - now) : 0.f, more = mine;
+#pragma unroll
+      for (int i = 1; i < 32; i <<= 1) more += __shfl_xor_sync(0xFFFFFFFFu, more, i);
+      mine *= follow(now, more);
       const uint32_t which = __ballot_sync(0xFFFFFFFFu, some);
       const int count = min(32, (last - base) / stride + 1);
 #pragma unroll 8
@@ -190,8 +195,6 @@ struct JoinRow {
         }
       }
     }
-#pragma unroll
-    for (int i = 1; i < 32; i <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
 #pragma unroll
     for (int i = kLanes; i < 32; i <<= 1)
 #pragma unroll
@@ -217,10 +220,8 @@ __device__ __forceinline__ void join(const AttnArgs& a, int index) {
   const Plan p = a.plan[entry];
   if (p.last < 0) return;
   const int stride = (p.last - p.first + 1) * split, r0 = (cta - p.first) * split + index % split;
-  auto store = [&](int r, float sum, int at, float4 o) {
+  auto store = [&](int r, int at, float4 o) {
     const int rr = p.row0 + r, j = rr / a.group;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
     store4(a, ((int64_t)(p.begin + j) * a.hq + p.h * a.group + (rr - j * a.group)) * D + at, o);
   };
   if (p.last - p.first < 2 * kJoinWarps) {
@@ -230,7 +231,7 @@ __device__ __forceinline__ void join(const AttnArgs& a, int index) {
       row.template parts<ROWS>(a, r, p.first, p.first, p.last, 1);
 #pragma unroll
       for (int w = 0; w < kWide; ++w)
-        if (lane < kLanes) store(r, row.sum, 4 * lane + 128 * w, row.o[w]);
+        if (lane < kLanes) store(r, 4 * lane + 128 * w, row.o[w]);
     }
     return;
   }
@@ -247,18 +248,23 @@ __device__ __forceinline__ void join(const AttnArgs& a, int index) {
       if (lane == 0) mls[warp] = make_float2(row.top, row.sum);
       __syncthreads();
       if (threadIdx.x < width / 4) {
-        float top = mls[0].x, sum = 0.f;
+        float top = mls[0].x, sum = 0.f, share[kJoinWarps];
 #pragma unroll
         for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, mls[w].x);
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) {
+          share[w] = mls[w].y * ex2(mls[w].x - top);
+          sum += share[w];
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kJoinWarps; ++w) {
-          const float by = ex2(mls[w].x - top);
+          const float by = share[w] * inv;
           const float4 v = os[w][threadIdx.x];
-          sum = fmaf(mls[w].y, by, sum);
           o.x = fmaf(v.x, by, o.x), o.y = fmaf(v.y, by, o.y), o.z = fmaf(v.z, by, o.z), o.w = fmaf(v.w, by, o.w);
         }
-        store(r, sum, channel + 4 * threadIdx.x, o);
+        store(r, channel + 4 * threadIdx.x, o);
       }
     }
   };

@@ -694,8 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
       tc_fence_after();
       if (any_real) {
         const float l = l2.x + l2.y;
-        float unref = ldexpf(1.f, ref - 139);
-        if (u.whole) unref = l == 0.f ? 0.f : ldexpf(1.f / l, ref - 139);
+        const float unref = l == 0.f ? 0.f : ldexpf(1.f / l, ref - 139);           // (parts are means, too)
         // 128 bytes of each of the warp's rows at a time (32 channels in float32, 64 in bf16) through the place of its queries, whose
         // products are done: eight lanes a row
         const bool narrow = u.whole && !a.out_f32;

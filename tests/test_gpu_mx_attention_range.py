@@ -73,6 +73,21 @@ def test_queries_and_keys_far_from_one(size, key, rows):
     check(b, scale=scale if ok else 2.0 ** 127)
 
 
+@pytest.mark.parametrize("lens,rows,hq", [([1, 200, 90], [1, 2, 1], 8), ([300, 90], [200, 40], 8), ([9000], [1], 8), ([9000, 20], [3, 1], 8),
+                                          ([20000], [70], 8), ([5000, 4000], [150, 1], 4)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("size", [2.0 ** -80, 2.0 ** 112])
+def test_values_far_from_one(size, d, lens, rows, hq):
+    """(Long sequences' units are cut in parts.)"""
+    if d == 256 and lens[0] > 9000:
+        lens = [9000]
+    b = Batch(33 + d, lens, rows, hq, 1, d, 64)
+    b.q = b.q * 0.25                                               # (many weights of a size)
+    for s, n in enumerate(lens):
+        rewrite(b, s, np.arange(n), v=(b.rng.uniform(-1.0, 1.0, (n, 1, d)) + 0.5) * size)
+    check(b)
+
+
 def grown(b, s, at, size, kind):
     """The token's keys or values a size larger."""
     t = np.array([at])
