@@ -38,7 +38,10 @@ constexpr int kStep = 32;                   // tokens a warp takes at once (two 
 constexpr int kUnitCost = 10;               // a unit's beginning and end, in steps (measured: 2 and 24 were up to 11 and 8 % slower)
 constexpr int kAhead = kStep * kWarps;      // tokens between a warp's steps
 constexpr int kLeastPiece = 4;              // steps a CTA is worth
-constexpr int kLowR = 40;                   // least reference exponent of the values (below it they count less bits)
+// The values' reference, a scale byte, as the weights have it: 2^(136 - ref) is what they are times, and within these float32 holds both their
+// sums and those that count little.
+constexpr int kLowR = 80, kHighR = 200;
+__device__ __forceinline__ int within(int ref) { return min(max(ref, kLowR), kHighR); }
 
 struct Seq : Rows {
   int steps, tiles;                         // steps and row tiles; no steps: none, or the other kernel's
@@ -372,7 +375,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
           for (int u = 0; u < 2; ++u) qf[j][b][u] = qs[((j * NB + b) * 2 + u) * 32 + lane];
     }
     // A score, codes' product times fac, less its row's `base` is what the exponential takes: base = m - (136 - ref), the weights times 2^(136 - ref), so
-    // that with a value's scale, 2^(byte - 127) of a byte up to ref, they are at most 2^(9 + kSlack).
+    // that with a value's scale, 2^(byte - 127) of a byte up to ref, they are at most 2^(9 + kSlack).  (A reference outside kLowR .. kHighR: the
+    // nearest one that is within, and `adjust` for the rest.)
     float f[NT][2], m[NT][2], base[NT][2], l[NT][2], acc[NB][2][NT][4];
     bool odd_unit = false;                               // (uniform) what `steps` below goes on with in its other form
 #pragma unroll
@@ -393,8 +397,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) acc[b][i][j][k] = 0.f;
     odd_unit = __any_sync(0xFFFFFFFFu, odd_unit);
-    int ref = kLowR;                                     // largest scale byte of values so far
-    float most = kSlack + (float)(136 - kLowR);          // what a score may exceed its base by
+    int ref = -1;                                        // largest scale byte of values so far
+    float most = kSlack + (float)(136 - within(-1));     // what a score may exceed its base by
     // tokens that all rows see
     const int64_t p_first = sq.len - sq.ql + (rt * ROWS) / a.group, p_last = sq.len - sq.ql + (rt * ROWS + rows - 1) / a.group;
     const int all_to = (int)(p_first < sq.end - 1 ? p_first : sq.end - 1);
@@ -409,6 +413,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
     // from one, scores of more than 2^16 (and values of NaN scales), scales are taken relative to the largest of those that some row sees, and a score is
     // rounded to float32 before its base is taken off.
     bool issued = false, large = false;
+    float adjust = 1.f;
     auto steps = [&](auto odd_form) -> bool {
       constexpr bool kOdd = decltype(odd_form)::value;
       for (; step < step1; step += kWarps, tok += kAhead) {
@@ -444,27 +449,28 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
         bool nan = false;
         uint32_t big = most_byte(own[0]);
         if constexpr (NB == 8) big = max(big, most_byte(own[NB / 4 - 1]));
-        if (__any_sync(0xFFFFFFFFu, big > (uint32_t)ref || (!kOdd && high))) {
-          if (!kOdd && __any_sync(0xFFFFFFFFu, high || big == 255u)) {
+        if (__any_sync(0xFFFFFFFFu, (int)big > ref || (!kOdd && high))) {
+          int real = -1;                                   // NaN's 255 is none, nor is what no row sees, which may be anything
+          if (tok + lane >= some_from && tok + lane <= some_to && (here >> (lane >> 4) & 1))
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              if (byte_at(own, b) != 255u) real = max(real, (int)byte_at(own, b));
+          const int top = max(__reduce_max_sync(0xFFFFFFFFu, real), ref);
+          if (!kOdd && (__any_sync(0xFFFFFFFFu, high || big == 255u) || (top >= 0 && top != within(top)))) {
             issued = true;
             return true;
           }
-          uint32_t real = 0;                               // NaN's 255 is none, nor is what no row sees, which may be anything
-          if (tok + lane >= some_from && tok + lane <= some_to)
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-              if (byte_at(own, b) != 255u) real = max(real, byte_at(own, b));
-          const int top = max((int)__reduce_max_sync(0xFFFFFFFFu, real), ref);
           nan = kOdd && __any_sync(0xFFFFFFFFu, big == 255u);
-          const float by = ex2((float)(ref - top));
+          const float by = ex2((float)(ref - top)), by_l = kOdd ? ex2((float)(within(ref) - within(top))) : by;
           ref = top;
-          most = kSlack + (float)(136 - ref);
+          if constexpr (kOdd) adjust = ref < 0 ? 1.f : __uint_as_float((uint32_t)(127 + within(ref) - ref) << 23);
+          most = kSlack + (float)(136 - within(ref));
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              base[j][i] = m[j][i] - (float)(136 - ref);
-              l[j][i] *= by;
+              base[j][i] = m[j][i] - (float)(136 - within(ref));
+              l[j][i] *= by_l;
 #pragma unroll
               for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -529,7 +535,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
             for (int k = 0; k < 4; ++k) {
               if constexpr (kOdd) {                        // (rounded before the maximum is taken off, and that before what the base has beside it)
                 x[j][k] *= fac_step[8 * j + 2 * t + (k & 1)];
-                e[j][k] = (x[j][k] - m[j][k & 1]) + (float)(136 - ref);
+                e[j][k] = (x[j][k] - m[j][k & 1]) + (float)(136 - within(ref));
               } else {
                 e[j][k] = fmaf(x[j][k], f[j][k & 1], -base[j][k & 1]);
               }
@@ -554,11 +560,11 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
                 const float by = ex2(m[j][i] - up);
                 if constexpr (!kOdd) large |= __any_sync(0xFFFFFFFFu, fabsf(up) > 0x1p16f && up != kNone);
                 m[j][i] = up;
-                base[j][i] = up - (float)(136 - ref);
+                base[j][i] = up - (float)(136 - within(ref));
                 l[j][i] *= by;
 #pragma unroll
                 for (int k = i; k < 4; k += 2)
-                  if (!(partial && hidden(j, k))) e[j][k] = (x[j][k] - up) + (float)(136 - ref);
+                  if (!(partial && hidden(j, k))) e[j][k] = (x[j][k] - up) + (float)(136 - within(ref));
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -605,6 +611,9 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
 #pragma unroll
               for (int j = 0; j < NT; ++j) {
                 float w[4] = {x[j][0] * s0[b], x[j][1] * s0[b], x[j][2] * s1[b], x[j][3] * s1[b]};
+                if constexpr (kOdd)
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) w[k] *= adjust;
                 if (kOdd && nan) {                         // a NaN scale counts for rows that see its token only
 #pragma unroll
                   for (int k = 0; k < 4; ++k)
@@ -649,20 +658,20 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
     }
 
     // ---- the warps' parts together: means of values each, as everywhere from here on (sums of many large values could leave float32)
-    const float unref = ex2((float)(ref - 136));
+    const float unref = ex2((float)(within(ref) - 136));
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) l[j][i] += __shfl_xor_sync(0xFFFFFFFFu, l[j][i], k);
-        const float by = l[j][i] == 0.f ? 0.f : 1.f / l[j][i];
+        const float by = l[j][i] == 0.f ? 0.f : 1.f / l[j][i], back = 1.f / adjust;
         if (g == 0) mls[warp * ROWS + 8 * j + 2 * t + i] = make_float2(m[j][i], l[j][i] * unref);
         float* o = reinterpret_cast<float*>(smem + warp * L::kRegion) + (8 * j + 2 * t + i) * kPitch;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-          *reinterpret_cast<float4*>(o + 32 * b + 4 * g) = make_float4(acc[b][0][j][i] * by, acc[b][0][j][2 + i] * by,
-                                                                       acc[b][1][j][i] * by, acc[b][1][j][2 + i] * by);
+          *reinterpret_cast<float4*>(o + 32 * b + 4 * g) = make_float4(acc[b][0][j][i] * by * back, acc[b][0][j][2 + i] * by * back,
+                                                                       acc[b][1][j][i] * by * back, acc[b][1][j][2 + i] * by * back);
       }
     __syncthreads();
     for (int i = tid; i < rows * (D / 4); i += kThreads) {

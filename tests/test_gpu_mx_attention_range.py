@@ -76,7 +76,7 @@ def test_queries_and_keys_far_from_one(size, key, rows):
 @pytest.mark.parametrize("lens,rows,hq", [([1, 200, 90], [1, 2, 1], 8), ([300, 90], [200, 40], 8), ([9000], [1], 8), ([9000, 20], [3, 1], 8),
                                           ([20000], [70], 8), ([5000, 4000], [150, 1], 4)])
 @pytest.mark.parametrize("d", [64, 128, 256])
-@pytest.mark.parametrize("size", [2.0 ** -80, 2.0 ** 112])
+@pytest.mark.parametrize("size", [2.0 ** -108, 2.0 ** -80, 2.0 ** 112, 2.0 ** 124])
 def test_values_far_from_one(size, d, lens, rows, hq):
     """(Long sequences' units are cut in parts.)"""
     if d == 256 and lens[0] > 9000:
