@@ -41,6 +41,7 @@ constexpr int kLeastPiece = 4;              // steps a CTA is worth
 // The values' reference, a scale byte, as the weights have it: 2^(136 - ref) is what they are times, and within these float32 holds both their
 // sums and those that count little.
 constexpr int kLowR = 80, kHighR = 200;
+constexpr int kBeyond = 8;                  // what a row's reference may be above the largest that the row sees
 __device__ __forceinline__ int within(int ref) { return min(max(ref, kLowR), kHighR); }
 
 struct Seq : Rows {
@@ -397,23 +398,39 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) acc[b][i][j][k] = 0.f;
     odd_unit = __any_sync(0xFFFFFFFFu, odd_unit);
-    int ref = -1;                                        // largest scale byte of values so far
+    int ref = -1;                                        // largest scale byte of values so far,
+    int sure = -1;                                       // and one that all rows have seen
     float most = kSlack + (float)(136 - within(-1));     // what a score may exceed its base by
     // tokens that all rows see
     const int64_t p_first = sq.len - sq.ql + (rt * ROWS) / a.group, p_last = sq.len - sq.ql + (rt * ROWS + rows - 1) / a.group;
     const int all_to = (int)(p_first < sq.end - 1 ? p_first : sq.end - 1);
     const int all_from = a.window && p_last - a.window + 1 > 0 ? (int)(p_last - a.window + 1) : 0;
+    const int sure_to = max(all_to, 0);                  // (rows before a sequence's beginning see nothing)
+    odd_unit |= all_from > sure_to;
     // and that some row sees
     const int some_to = (int)(p_last < sq.end - 1 ? p_last : sq.end - 1);
     const int some_from = a.window && p_first - a.window + 1 > 0 ? (int)(p_first - a.window + 1) : 0;
 
     // The steps that are left.  What is out of the ordinary has a copy of the code of its own, in which a warp does the rest of a unit (true:
-    // it is to go on there), and costs the other next to nothing (2 to 12 % where one code looked out for all of it).  A sum of codes times
-    // scales is at most 2^27 times the largest scale, and its row's factor comes after it: with keys' scales of 2^65 and more, factors far
-    // from one, scores of more than 2^16 (and values of NaN scales), scales are taken relative to the largest of those that some row sees, and a score is
-    // rounded to float32 before its base is taken off.
+    // it is to go on there), and costs the other next to nothing (2 to 12 % where one code looked out for all of it):
+    // keys' scales of 2^65 and more, factors far from one, scores of more than 2^16 (a sum of codes times scales is at most 2^27 times
+    // the largest scale, and its row's factor comes after it: scales are taken relative to the largest of those that some row sees, and a
+    // score is rounded to float32 before its maximum is taken off); values of NaN scales, of references that are not within kLowR ..
+    // kHighR, and of tokens that some rows see and others do not and that are larger than all that these see: a reference a row.
     bool issued = false, large = false;
-    float adjust = 1.f;
+    int refs[NT][2];                                     // a reference a row, in that form
+    auto adjust = [](int r) { return r < 0 ? 1.f : __uint_as_float((uint32_t)(127 + within(r) - r) << 23); };
+    // A row's sums, relative to another reference.
+    auto follow = [&](int j, int i, float by, float by_l) {
+      l[j][i] *= by_l;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          acc[b][c][j][i] *= by;
+          acc[b][c][j][2 + i] *= by;
+        }
+    };
     auto steps = [&](auto odd_form) -> bool {
       constexpr bool kOdd = decltype(odd_form)::value;
       for (; step < step1; step += kWarps, tok += kAhead) {
@@ -449,36 +466,46 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
         bool nan = false;
         uint32_t big = most_byte(own[0]);
         if constexpr (NB == 8) big = max(big, most_byte(own[NB / 4 - 1]));
-        if (__any_sync(0xFFFFFFFFu, (int)big > ref || (!kOdd && high))) {
+        if (__any_sync(0xFFFFFFFFu, (int)big > (sure < 0 ? -1 : ref) || (!kOdd && high))) {
           int real = -1;                                   // NaN's 255 is none, nor is what no row sees, which may be anything
           if (tok + lane >= some_from && tok + lane <= some_to && (here >> (lane >> 4) & 1))
 #pragma unroll
             for (int b = 0; b < NB; ++b)
               if (byte_at(own, b) != 255u) real = max(real, (int)byte_at(own, b));
-          const int top = max(__reduce_max_sync(0xFFFFFFFFu, real), ref);
-          if (!kOdd && (__any_sync(0xFFFFFFFFu, high || big == 255u) || (top >= 0 && top != within(top)))) {
-            issued = true;
-            return true;
-          }
-          nan = kOdd && __any_sync(0xFFFFFFFFu, big == 255u);
-          const float by = ex2((float)(ref - top)), by_l = kOdd ? ex2((float)(within(ref) - within(top))) : by;
-          ref = top;
-          if constexpr (kOdd) adjust = ref < 0 ? 1.f : __uint_as_float((uint32_t)(127 + within(ref) - ref) << 23);
-          most = kSlack + (float)(136 - within(ref));
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              base[j][i] = m[j][i] - (float)(136 - within(ref));
-              l[j][i] *= by_l;
-#pragma unroll
-              for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                  acc[b][c][j][i] *= by;
-                  acc[b][c][j][2 + i] *= by;
-                }
+          const int now = __reduce_max_sync(0xFFFFFFFFu, real), top = max(now, ref);
+          if constexpr (!kOdd) {
+            int all = now;
+            if (tok < all_from || tok + kStep - 1 > all_to)
+              all = __reduce_max_sync(0xFFFFFFFFu, tok + lane >= all_from && tok + lane <= sure_to ? real : -1);
+            sure = max(sure, all);
+            if (__any_sync(0xFFFFFFFFu, high || big == 255u) || (sure >= 0 && top > sure + kBeyond) || (top >= 0 && top != within(top))) {
+              issued = true;
+              return true;
             }
+            const float by = ex2((float)(ref - top));
+            ref = top;
+            most = kSlack + (float)(136 - within(ref));
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                base[j][i] = m[j][i] - (float)(136 - within(ref));
+                follow(j, i, by, by);
+              }
+          } else {
+            nan = __any_sync(0xFFFFFFFFu, big == 255u);
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int r = 8 * j + k, own_top = __reduce_max_sync(0xFFFFFFFFu, tok + lane >= low[r] && tok + lane <= lim[r] ? real : -1);
+                if (k / 2 == t) {
+                  const int was = refs[j][k & 1], need = max(was, own_top), to = now <= need + kBeyond ? max(now, was) : need;
+                  refs[j][k & 1] = to;
+                  follow(j, k & 1, ex2((float)(was - to)), ex2((float)(within(was) - within(to))));
+                }
+              }
+          }
         }
 
 #pragma unroll
@@ -535,7 +562,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
             for (int k = 0; k < 4; ++k) {
               if constexpr (kOdd) {                        // (rounded before the maximum is taken off, and that before what the base has beside it)
                 x[j][k] *= fac_step[8 * j + 2 * t + (k & 1)];
-                e[j][k] = (x[j][k] - m[j][k & 1]) + (float)(136 - within(ref));
+                e[j][k] = x[j][k] - m[j][k & 1];
               } else {
                 e[j][k] = fmaf(x[j][k], f[j][k & 1], -base[j][k & 1]);
               }
@@ -544,7 +571,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
             }
 
           // ---- running maxima
-          if (__any_sync(0xFFFFFFFFu, top > most || (!kOdd && large))) {
+          if (__any_sync(0xFFFFFFFFu, top > (kOdd ? kSlack : most) || (!kOdd && large))) {
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -560,11 +587,11 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
                 const float by = ex2(m[j][i] - up);
                 if constexpr (!kOdd) large |= __any_sync(0xFFFFFFFFu, fabsf(up) > 0x1p16f && up != kNone);
                 m[j][i] = up;
-                base[j][i] = up - (float)(136 - within(ref));
+                if constexpr (!kOdd) base[j][i] = up - (float)(136 - within(ref));
                 l[j][i] *= by;
 #pragma unroll
                 for (int k = i; k < 4; k += 2)
-                  if (!(partial && hidden(j, k))) e[j][k] = (x[j][k] - up) + (float)(136 - within(ref));
+                  if (!(partial && hidden(j, k))) e[j][k] = (x[j][k] - up) + (kOdd ? 0.f : (float)(136 - within(ref)));
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -578,6 +605,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+              if constexpr (kOdd) e[j][k] += (float)(136 - within(refs[j][k & 1]));
               x[j][k] = ex2(e[j][k]);
               l[j][k & 1] += x[j][k];
             }
@@ -613,7 +641,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
                 float w[4] = {x[j][0] * s0[b], x[j][1] * s0[b], x[j][2] * s1[b], x[j][3] * s1[b]};
                 if constexpr (kOdd)
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) w[k] *= adjust;
+                  for (int k = 0; k < 4; ++k) w[k] *= adjust(refs[j][k & 1]);
                 if (kOdd && nan) {                         // a NaN scale counts for rows that see its token only
 #pragma unroll
                   for (int k = 0; k < 4; ++k)
@@ -640,6 +668,10 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       return false;
     };
     if (!odd_unit) odd_unit = steps(Bool<false>());
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) refs[j][i] = odd_unit && low[8 * j + 2 * t + i] >= tok ? -1 : ref;      // (none yet: nothing seen)
     if (odd_unit) steps(Bool<true>());
     if (abort_flag) {                                    // a wait gave up: the copies still on their way, then out
       volatile int none = 0;
@@ -657,21 +689,26 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       return;
     }
 
+    if (odd_unit) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) follow(j, i, 1.f / adjust(refs[j][i]), 1.f);
+    }
     // ---- the warps' parts together: means of values each, as everywhere from here on (sums of many large values could leave float32)
-    const float unref = ex2((float)(within(ref) - 136));
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) l[j][i] += __shfl_xor_sync(0xFFFFFFFFu, l[j][i], k);
-        const float by = l[j][i] == 0.f ? 0.f : 1.f / l[j][i], back = 1.f / adjust;
-        if (g == 0) mls[warp * ROWS + 8 * j + 2 * t + i] = make_float2(m[j][i], l[j][i] * unref);
+        const float by = l[j][i] == 0.f ? 0.f : __fdividef(1.f, l[j][i]);
+        if (g == 0) mls[warp * ROWS + 8 * j + 2 * t + i] = make_float2(m[j][i], l[j][i] * ex2((float)(within(refs[j][i]) - 136)));
         float* o = reinterpret_cast<float*>(smem + warp * L::kRegion) + (8 * j + 2 * t + i) * kPitch;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-          *reinterpret_cast<float4*>(o + 32 * b + 4 * g) = make_float4(acc[b][0][j][i] * by * back, acc[b][0][j][2 + i] * by * back,
-                                                                       acc[b][1][j][i] * by * back, acc[b][1][j][2 + i] * by * back);
+          *reinterpret_cast<float4*>(o + 32 * b + 4 * g) = make_float4(acc[b][0][j][i] * by, acc[b][0][j][2 + i] * by,
+                                                                       acc[b][1][j][i] * by, acc[b][1][j][2 + i] * by);
       }
     __syncthreads();
     for (int i = tid; i < rows * (D / 4); i += kThreads) {

@@ -95,6 +95,19 @@ def grown(b, s, at, size, kind):
     rewrite(b, s, t, **{kind: x})
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("size", [2.0 ** 14, 2.0 ** 26, 2.0 ** 60, 2.0 ** 110])
+@pytest.mark.parametrize("rows,window", [([6, 3, 2], 0), ([6, 3, 2], 40), ([6, 3, 2], 2), ([6, 3, 6], 32)])
+def test_values_that_some_rows_see(rows, window, size, d):
+    """A value of another size ahead of a batch's early rows, and one behind its late rows' windows."""
+    b = Batch(34 + d, [300, 90, 150], rows, 4, 2, d, 32)
+    for s, (n, r) in enumerate(zip(b.lens, rows)):
+        grown(b, s, n - r + r // 2, size, "v")
+        if window:
+            grown(b, s, max(n - window - r // 2, 0), size, "v")
+    check(b, window=window)
+
+
 @pytest.mark.parametrize("rows,lens", [([1, 1, 1], [1, 40, 5000]), ([200, 40], [300, 3000])])
 @pytest.mark.parametrize("size", [-1.0, 1.0])
 def test_scores_of_any_size(size, rows, lens):
