@@ -645,7 +645,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
                 if (kOdd && nan) {                         // a NaN scale counts for rows that see its token only
 #pragma unroll
                   for (int k = 0; k < 4; ++k)
-                    if (x[j][k] == 0.f) w[k] = 0.f;
+                    if (partial && hidden(j, k)) w[k] = 0.f;
                 }
                 const uint32_t p0 = transpose(f16_pair(w[0], w[1])), p1 = transpose(f16_pair(w[2], w[3]));
                 mma(acc[b][0][j], va[2 * o], p0, p1);

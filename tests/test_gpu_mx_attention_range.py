@@ -130,6 +130,26 @@ def test_scores_of_any_size(size, rows, lens):
             at += 1
 
 
+@pytest.mark.parametrize("rows", [[1, 3], [200, 40]])
+def test_a_nan_value_of_the_smallest_weight(rows):
+    """A token that a row sees counts, though its weight is below float32."""
+    d = 64
+    b = Batch(37, [300, 90], rows, 4, 2, d, 32)
+    b.q = torch.ones_like(b.q)
+    for s in range(2):
+        n = int(b.lens[s])
+        k = np.ones((n, 2, d))
+        k[7] = -6.0
+        v = C.load(host(b.cache), b.page, d, b.table[s, np.arange(n) // b.page] * b.page + np.arange(n) % b.page, 1)
+        v[7, 1, 40] = np.nan
+        rewrite(b, s, np.arange(n), k=k, v=v)
+    cat.cat_device_status()
+    g = host(b.run(scale=1.0))
+    odd = np.zeros(g.shape, dtype=bool)
+    odd[:, 2:, 32:64] = True
+    assert np.isnan(g[odd]).all() and np.isfinite(g[~odd]).all()
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_tiles_queries_far_from_one_and_not_finite(d):
     """The tiles' way of a query to float16: zero rows, the largest and smallest, NaN and infinity, and the rows beside them."""
