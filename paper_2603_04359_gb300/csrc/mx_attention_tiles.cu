@@ -40,8 +40,9 @@ constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kUnitCost = 448;              // a unit's beginning and end, in tokens (measured: 768 and 1024 were up to 4 and 7 % slower)
 constexpr int kLeastPiece = 256;            // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
+constexpr int kBeyond = 4;                  // what a step's tokens may lie apart, or below the reference, before each has its own
 constexpr uint32_t kTmemCols = 512;
-constexpr int kBarRoom = 6144;
+constexpr int kBarRoom = 8192;
 
 template <int NB>
 struct Tc {
@@ -83,7 +84,8 @@ struct Unit {
   int s, h, rt, rows, j0, j1;               // the steps of KT tokens, from the sequence's beginning
   bool starts, whole, nothing;              // nothing: no row sees a token
   int64_t p0;                               // the token of the sequence's first row
-  int64_t t0, t1;                           // the tokens that some row sees
+  int64_t t0, t1;                           // the tokens that some row sees,
+  int64_t a0, a1;                           // and that all rows see (but those before the sequence's beginning, which see nothing)
   int64_t from, end;                        // where the unit's first step ends on the line (of a later piece), and its end
   int begin;                                // the sequence's first row,
   int64_t tokens;                           // and one past its last token in the cache
@@ -130,6 +132,8 @@ struct Walk {
       u.p0 = q.len - q.ql;
       const int64_t p_first = u.p0 + row0 / group, p_last = u.p0 + (row0 + (uint32_t)u.rows - 1) / group;
       const int64_t t1 = p_last + 1 < q.end ? p_last + 1 : q.end, t0 = a.window && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
+      u.a0 = a.window && p_last - a.window + 1 > 0 ? p_last - a.window + 1 : 0;
+      u.a1 = (p_first > 0 ? p_first : 0) + 1;
       u.t0 = t0, u.t1 = t1, u.begin = q.begin, u.tokens = q.end;
       const int first = (int)(t0 / KT), steps = t1 > t0 ? (int)((t1 + KT - 1) / KT) - first : 0;
       // (any growing map of the line to steps will do that is the same for all: in float32)
@@ -175,8 +179,9 @@ struct Bars {
   int k_power[8][4];                        // 2^(ref - 139) of 32 tokens' keys, as a float32's exponent field
   uint32_t there[8];                        // which 16-token groups of a step are on pages
   uint32_t raw_there[6];
-  uint32_t v_ref[4];                        // the values' reference, + 256 where a scale of the step's is NaN
-  uint32_t v_most[2][4];                    // the same of a warp's tokens
+  uint32_t v_ref[2];                        // the values' reference, + 256 where a scale of the step's is NaN, + 512 where each token has its own
+  uint32_t v_most[2][4];                    // the largest of a warp's tokens, + 256 the same, + 65536 times the least of its tokens' largest
+  uint8_t v_own[2][128];                    // a token's own reference
   uint8_t v_nan[2][2][128];                  // a token's blocks of NaN scales (d = 256: those of half of them)
   int64_t scan[20];
   int64_t found_at;
@@ -401,9 +406,10 @@ __device__ __forceinline__ void weights(uint32_t s_col, const int* k_power, Fact
   }
   sum = add2(sum, part);
 }
-// The same of scores that are rounded before m is taken off: what a product keeps beyond float32 would be a large difference of large scores.
+// The same of scores that are rounded before m is taken off (what a product keeps beyond float32 would be a large difference of large
+// scores), times 2^(own - ref) of each token's own reference where there are such.
 template <int KT>
-__device__ __forceinline__ float weights_apart(uint32_t s_col, const int* k_power, Factor fac, float m) {
+__device__ __forceinline__ float weights_apart(uint32_t s_col, const int* k_power, Factor fac, float m, const uint8_t* own, int ref) {
   float sum = 0.f;
 #pragma unroll 1
   for (int c = 0; c < KT / 16; ++c) {
@@ -415,7 +421,9 @@ __device__ __forceinline__ float weights_apart(uint32_t s_col, const int* k_powe
     for (int i = 0; i < 16; i += 2) {
       const float x = ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[i]), f), -m) + 8.f), y = ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[i + 1]), f), -m) + 8.f);
       sum += x + y;
-      w[i / 2] = f16_pair(x, y);
+      // (what is not seen, 0, may be of any size)
+      const float up = own ? ex2((float)min((int)own[16 * c + i] - ref, 0)) : 1.f, up2 = own ? ex2((float)min((int)own[16 * c + i + 1] - ref, 0)) : 1.f;
+      w[i / 2] = f16_pair(x * up, y * up2);
     }
     tmem_st8(s_col + 8 * c, w);
   }
@@ -647,7 +655,17 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           if (!full) hide<KT>(s_col, t0, lim, low, there);
           const float most = largest<KT>(s_col, k_power, fac);
           if (!CAT_WAIT(&bars->v_full[b], (jj >> kBufLog) & 1)) break;       // (the values' reference)
-          const int now = (int)(bars->v_ref[b] & 255u);
+          // The row's reference: at least that of the values that it sees, and no more above them than 2^(2 kBeyond), so that what it does not
+          // see, which may be anything, costs it no bits.
+          const uint32_t v_ref = bars->v_ref[b];
+          const bool own = v_ref & 512u;
+          int now = t0 <= lim && t0 + KT > low ? max(ref, (int)(v_ref & 255u)) : ref;
+          if (own) {
+            now = ref;
+#pragma unroll 1
+            for (int i = 0; i < KT; ++i)
+              if (t0 + i <= lim && t0 + i >= low) now = max(now, (int)bars->v_own[b][i]);
+          }
           const bool grows = seen ? most > m + kSlack : most > -INFINITY;
           if (__any_sync(0xFFFFFFFFu, grows || now != ref)) {
             const float up = grows ? most : m, by = seen ? ex2(m - up) : 1.f;       // (nothing seen: all is 0)
@@ -671,11 +689,11 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
             }
             ref = now;
           }
-          if (__builtin_expect(apart, 0))
-            l2.x += weights_apart<KT>(s_col, k_power, fac, m);
+          if (__builtin_expect(apart || own, 0))
+            l2.x += weights_apart<KT>(s_col, k_power, fac, m, own ? bars->v_own[b] : nullptr, ref);
           else
             weights<KT>(s_col, k_power, fac, 8.f - m, l2);   // (times 2^8)
-          if (bars->v_ref[b] & 256u)
+          if (v_ref & 256u)
             for (int i = 0; i < KT; ++i) {
               const int at = t0 + i;
               if (at <= lim && at >= low) nan_blocks |= (uint32_t)bars->v_nan[b][0][i] | (NB == 8 ? bars->v_nan[b][1][i] : 0u);
@@ -773,24 +791,48 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
         most = __reduce_max_sync(0xFFFFFFFFu, most);
         __half2 scale[kHere];
         if (values) {
+          // The reference is the largest scale so far; tokens have their own instead where some rows see others than others do and those
+          // differ, or where what was larger is seen no more, perhaps.
           const bool odd = __any_sync(0xFFFFFFFFu, nan != 0);
+          const int64_t t = (int64_t)step * KT;
+          const bool partial = max(t, u.t0) < u.a0 || min(t + KT, u.t1) > u.a1;
+          auto token_most = [&] {
+            int m = 0;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const int o = on ? raw[C::kCodes + row * NB + i] : 0;
+              if (o != 255) m = max(m, o);
+            }
+            return m;
+          };
+          uint32_t least = 255u;
+          if (partial) {
+            const uint32_t m = (uint32_t)token_most();
+            least = __reduce_min_sync(0xFFFFFFFFu, m ? m : 255u);
+          }
           if (lane == 0) {
-            bars->v_most[jj & 1][w] = most | (odd ? 256u : 0u);
+            bars->v_most[jj & 1][w] = most | (odd ? 256u : 0u) | least << 16;
             mbar_arrive(&bars->most_full);
           }
           if (!CAT_WAIT(&bars->most_full, jj & 1)) break;
           uint32_t all = 0;
+          int now = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t v = bars->v_most[jj & 1][i];
             all |= v & 256u;
-            ref = max(ref, (int)(v & 255u));
+            now = max(now, (int)(v & 255u));
+            least = min(least, v >> 16);
           }
+          ref = max(ref, now);
+          const bool own = now < ref - kBeyond || (int)least < now - kBeyond;
+          const int to = own ? token_most() : ref;
 #pragma unroll
-          for (int i = 0; i < kHere; ++i) scale[i] = on && bytes[i] != 255 ? half_scale(bytes[i], ref) : half_scale(-1000, 0);
+          for (int i = 0; i < kHere; ++i) scale[i] = on && bytes[i] != 255 ? half_scale(bytes[i], to) : half_scale(-1000, 0);
           if (jj >= kBufs && !CAT_WAIT(&bars->v_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
           bars->v_nan[b][half][row] = (uint8_t)nan;
-          if (w == 0 && lane == 0) bars->v_ref[b] = (uint32_t)ref | all;
+          if (own && half == 0) bars->v_own[b][row] = (uint8_t)to;
+          if (w == 0 && lane == 0) bars->v_ref[b] = (uint32_t)ref | all | (own ? 512u : 0u);
         } else {
           // (d = 256: the two halves' largest differ; the keys' reference is of all their blocks)
           uint32_t whole = most;

@@ -97,7 +97,8 @@ def grown(b, s, at, size, kind):
 
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("size", [2.0 ** 14, 2.0 ** 26, 2.0 ** 60, 2.0 ** 110])
-@pytest.mark.parametrize("rows,window", [([6, 3, 2], 0), ([6, 3, 2], 40), ([6, 3, 2], 2), ([6, 3, 6], 32)])
+@pytest.mark.parametrize("rows,window", [([6, 3, 2], 0), ([6, 3, 2], 40), ([6, 3, 2], 2), ([6, 3, 6], 32), ([200, 40, 70], 0),
+                                         ([200, 40, 70], 40), ([200, 1, 8], 33), ([200, 30, 70], 2)])
 def test_values_that_some_rows_see(rows, window, size, d):
     """A value of another size ahead of a batch's early rows, and one behind its late rows' windows."""
     b = Batch(34 + d, [300, 90, 150], rows, 4, 2, d, 32)
