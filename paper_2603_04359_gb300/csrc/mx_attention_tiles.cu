@@ -40,6 +40,7 @@ constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kUnitCost = 448;              // a unit's beginning and end, in tokens (measured: 768 and 1024 were up to 4 and 7 % slower)
 constexpr int kLeastPiece = 256;            // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
+constexpr int kKeysApart = 20;              // what 32 tokens' keys may lie apart before each has its own reference
 constexpr int kBeyond = 4;                  // what a step's tokens may lie apart, or below the reference, before each has its own
 constexpr uint32_t kTmemCols = 512;
 constexpr int kBarRoom = 8192;
@@ -177,6 +178,8 @@ struct Bars {
       mma_done;
   // (of eight steps: keys are unpacked up to five steps ahead of scores that are still read)
   int k_power[8][4];                        // 2^(ref - 139) of 32 tokens' keys, as a float32's exponent field
+  uint32_t k_apart[8];                      // a byte for 32 tokens: whether their products are times 2^(k_own - ref) each
+  uint8_t k_own[8][128];
   uint32_t there[8];                        // which 16-token groups of a step are on pages
   uint32_t raw_there[6];
   uint32_t v_ref[2];                        // the values' reference, + 256 where a scale of the step's is NaN, + 512 where each token has its own
@@ -429,14 +432,20 @@ __device__ __forceinline__ float weights_apart(uint32_t s_col, const int* k_powe
   }
   return sum;
 }
-// Scores of tokens that a row does not see become -infinity where they are (steps at an end of what the rows see alone come here).
+// Scores of tokens that a row does not see become -infinity where they are, and products of keys with references of their own get them
+// (steps at an end of what the rows see, and such, alone come here).
 template <int KT>
-__device__ __forceinline__ void hide(uint32_t s_col, int t0, int lim, int low, uint32_t there) {
+__device__ __forceinline__ void hide(uint32_t s_col, int t0, int lim, int low, uint32_t there, uint32_t apart, const uint8_t* own, const int* k_power) {
 #pragma unroll 1
   for (int c = 0; c < KT / 16; ++c) {
     uint32_t v[16];
     tmem_ld16(s_col + 16 * c, v);
     tmem_have16(v);
+    if (apart >> (8 * (c / 2)) & 1u) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        v[i] = __float_as_uint(__uint_as_float(v[i]) * ex2((float)((int)own[16 * c + i] - (k_power[c / 2] + 12))));
+    }
     const bool on = there >> c & 1;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -484,6 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
 
   if (tid == 0) {
     for (int i = 0; i < 6; ++i) mbar_init(&bars->raw_full[i], 1), mbar_init(&bars->raw_empty[i], 4);
+    for (int i = 0; i < 8; ++i) bars->k_apart[i] = 0u;
     for (int i = 0; i < 4; ++i) {
       mbar_init(&bars->k_full[i], 4), mbar_init(&bars->v_full[i], 4);
       mbar_init(&bars->k_empty[i], 1), mbar_init(&bars->v_empty[i], 1);
@@ -651,8 +661,9 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           const int t0 = step * KT;
           const uint32_t there = bars->there[jj & 7];
           constexpr uint32_t kAll = (1u << (KT / 16)) - 1u;
-          const bool full = __all_sync(0xFFFFFFFFu, t0 + KT - 1 <= lim && t0 >= low) && there == kAll;
-          if (!full) hide<KT>(s_col, t0, lim, low, there);
+          const uint32_t keys_apart = bars->k_apart[jj & 7];
+          const bool full = __all_sync(0xFFFFFFFFu, t0 + KT - 1 <= lim && t0 >= low) && there == kAll && keys_apart == 0u;
+          if (!full) hide<KT>(s_col, t0, lim, low, there, keys_apart, bars->k_own[jj & 7], k_power);
           const float most = largest<KT>(s_col, k_power, fac);
           if (!CAT_WAIT(&bars->v_full[b], (jj >> kBufLog) & 1)) break;       // (the values' reference)
           // The row's reference: at least that of the values that it sees, and no more above them than 2^(2 kBeyond), so that what it does not
@@ -835,24 +846,35 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
           if (w == 0 && lane == 0) bars->v_ref[b] = (uint32_t)ref | all | (own ? 512u : 0u);
         } else {
           // (d = 256: the two halves' largest differ; the keys' reference is of all their blocks)
-          uint32_t whole = most;
+          uint32_t mine = 0;
+#pragma unroll
+          for (int i = 0; i < kHere; ++i)
+            if (bytes[i] != 255) mine = max(mine, (uint32_t)bytes[i]);
           if constexpr (NB == 8) {
-            uint32_t m = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const uint32_t o = on ? raw[C::kCodes + row * NB + (first_block ^ 4) + i] : 0u;
-              if (o != 255u) m = max(m, o);
+              if (o != 255u) mine = max(mine, o);
             }
-            whole = max(whole, __reduce_max_sync(0xFFFFFFFFu, m));
+            most = __reduce_max_sync(0xFFFFFFFFu, mine);
           }
-          const int kref = max((int)whole, kLowR);
+          const int kref = max((int)most, kLowR);
+          // (a row may see none of the largest, or nothing of what it is large in)
+          const bool apart = __any_sync(0xFFFFFFFFu, mine && (int)mine < kref - kKeysApart);
+          const int to = apart ? (int)mine : kref;
 #pragma unroll
           for (int i = 0; i < kHere; ++i) {
-            scale[i] = on ? half_scale(bytes[i], kref) : half_scale(-1000, 0);
+            scale[i] = on ? half_scale(bytes[i], to) : half_scale(-1000, 0);
             if (bytes[i] == 255) scale[i] = __half2half2(__ushort_as_half(0x7FFF));
           }
           if (jj >= kBufs && !CAT_WAIT(&bars->k_empty[b], ((jj >> kBufLog) - 1) & 1)) break;
-          if (lane == 0 && half == 0) bars->k_power[jj & 7][row / 32] = kref - 12;
+          if (half == 0) {
+            if (apart) bars->k_own[jj & 7][row] = (uint8_t)to;
+            if (lane == 0) {
+              bars->k_power[jj & 7][row / 32] = kref - 12;
+              reinterpret_cast<uint8_t*>(&bars->k_apart[jj & 7])[row / 32] = apart;
+            }
+          }
           if (w == 0 && lane == 0) bars->there[jj & 7] = there;
         }
         unpack_row<NB>(raw, smem + (values ? C::kOffV : C::kOffK) + b * C::kTile, row, half, values, scale);

@@ -109,6 +109,18 @@ def test_values_that_some_rows_see(rows, window, size, d):
     check(b, window=window)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("size", [2.0 ** 26, 2.0 ** 60])
+@pytest.mark.parametrize("rows,window", [([6, 3, 2], 0), ([200, 40, 70], 0), ([200, 40, 70], 40)])
+def test_keys_that_some_rows_see(rows, window, size, d):
+    b = Batch(35 + d, [300, 90, 150], rows, 8, 2, d, 32)
+    for s, (n, r) in enumerate(zip(b.lens, rows)):
+        grown(b, s, n - r + r // 2, size, "k")
+        if window:
+            grown(b, s, max(n - window - r // 2, 0), size, "k")
+    check(b, window=window)
+
+
 @pytest.mark.parametrize("rows,lens", [([1, 1, 1], [1, 40, 5000]), ([200, 40], [300, 3000])])
 @pytest.mark.parametrize("size", [-1.0, 1.0])
 def test_scores_of_any_size(size, rows, lens):
