@@ -421,11 +421,11 @@ cat_status cat_linear_dp(const uint8_t* x_planes, int32_t bits_x, int32_t asym_x
 /*
  * cat_set_wait_limit_ns -- testing aid, no counterpart in the paper.  Sets, on the current device, the
  * bound of the pipeline waits of the weight-streaming W4A4 GEMM (cat_w4a4_linear, n <= 32), of the
- * digit-plane GEMM (cat_linear_dp) and of the microscaled products (cat_mx_linear, cat_mx_linear_grouped); 0 restores the default of 1 s (1e9 ns, also the largest value
- * accepted).  A wait that exceeds its bound gives up: the kernel drains its copies and MMAs in flight
+ * digit-plane GEMM (cat_linear_dp), of the microscaled products (cat_mx_linear, cat_mx_linear_grouped) and of cat_mx_attention;
+ * 0 restores the default of 1 s (1e9 ns, also the largest value accepted).  A wait that exceeds its bound gives up: the kernel drains its copies and MMAs in flight
  * (those waits keep the 1 s bound), frees its tensor memory, returns, and raises CAT_ERR_TIMEOUT in the
  * device status word with the kernel's bit (1 << 11 weight-streaming GEMM, 1 << 13 digit-plane GEMM,
- * 1 << 14 microscaled products) and the source line of the first wait that gave up in bits 16..31.  Its outputs are then undefined.
+ * 1 << 14 microscaled products, 1 << 15 attention) and the source line of the first wait that gave up in bits 16..31.  Its outputs are then undefined.
  * Synchronous (a blocking copy to the device); not for use while those kernels run.
  */
 cat_status cat_set_wait_limit_ns(uint64_t ns);

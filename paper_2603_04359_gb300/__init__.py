@@ -986,8 +986,8 @@ def cat_mx_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, 
 
 
 def cat_set_wait_limit_ns(ns: int) -> None:
-    """Testing aid: bound (ns) of the pipeline waits of the weight-streaming, digit-plane and microscaled GEMMs on
-    the current device; 0 restores the default (1 s)."""
+    """Testing aid: bound (ns) of the pipeline waits of the weight-streaming, digit-plane and microscaled GEMMs and of
+    attention on the current device; 0 restores the default (1 s)."""
     _check("cat_set_wait_limit_ns", load_library().cat_set_wait_limit_ns(int(ns)))
 
 

@@ -44,6 +44,8 @@ cudaError_t launch_gram_f32(const void* X, int dtype, int64_t n, int64_t d, floa
 cudaError_t set_decode_wait_limit(uint64_t ns);
 cudaError_t set_dp_wait_limit(uint64_t ns);
 cudaError_t set_mx_wait_limit(uint64_t ns);
+cudaError_t set_attention_wait_limit(uint64_t ns);
+cudaError_t set_attention_tiles_wait_limit(uint64_t ns);
 size_t dp_l24_work_bytes(int64_t n);
 cudaError_t launch_transform_quantize_dp(const void* x, int dtype, int64_t n, int64_t d, int k, const float* A, int bits,
                                          int asym, int l24, uint8_t* planes, float* scale, int32_t* zero,
@@ -813,6 +815,8 @@ cat_status cat_set_wait_limit_ns(uint64_t ns) {
   cudaError_t e = cat::set_decode_wait_limit(v);
   if (e == cudaSuccess) e = cat::set_dp_wait_limit(v);
   if (e == cudaSuccess) e = cat::set_mx_wait_limit(v);
+  if (e == cudaSuccess) e = cat::set_attention_wait_limit(v);
+  if (e == cudaSuccess) e = cat::set_attention_tiles_wait_limit(v);
   if (e != cudaSuccess) return cuda_fail(e, "cat_set_wait_limit_ns");
   return ok();
 }

@@ -145,15 +145,6 @@ __device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t* w) {
     load_words<NB / 4>(p, w);
 }
 
-__device__ __forceinline__ bool short_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int site) {
-#pragma unroll 1
-  for (int n = 0; !mbar_try_wait(bar, parity); ++n)
-    if (n > (1 << 20) || *abort) {
-      if (*abort == 0) *abort = site;
-      return false;
-    }
-  return true;
-}
 template <bool B>
 struct Bool {
   static constexpr bool value = B;
@@ -188,14 +179,14 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
   __shared__ int64_t found_at;
   __shared__ uint64_t full_bars[kWarps][kStages];
   __shared__ int has[kWarps][kStages];                   // which halves of a step are there
-  __shared__ int abort_flag;
+  __shared__ Waits waits;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
   float* fac_step = reinterpret_cast<float*>(power + ROWS) + warp * ROWS;       // fac where a step's scales are relative to their largest
   const int hkv = a.c.hkv, cta = blockIdx.x;
   if (tid == 0) {
     for (int i = 0; i < kWarps * kStages; ++i) mbar_init(&full_bars[0][0] + i, 1);
-    abort_flag = 0;
+    waits.init();
     fence_mbar_init();
   }
   if (!a.beside) pdl_wait_then_release();
@@ -436,7 +427,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       for (; step < step1; step += kWarps, tok += kAhead) {
         if (!issued) issue(step + (kStages - 1) * kWarps, tok + (kStages - 1) * kAhead);
         issued = false;
-        if (!__all_sync(0xFFFFFFFFu, short_wait(&full[get], get_round & 1, &abort_flag, __LINE__))) return false;
+        if (!__all_sync(0xFFFFFFFFu, short_wait<false, true>(&full[get], get_round & 1, &waits, __LINE__))) return false;
         const uint8_t* st = ring + get * L::kStage;
         const int here = has[warp][get];
         uint32_t own[(NB + 3) / 4], own_k[(NB + 3) / 4], high = 0u;      // a token's values' and keys' scales; keys' of 2^65 and more
@@ -607,6 +598,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
             for (int k = 0; k < 4; ++k) {
               if constexpr (kOdd) e[j][k] += (float)(136 - within(refs[j][k & 1]));
               x[j][k] = ex2(e[j][k]);
+              if constexpr (kOdd)
+                if (e[j][k] == __int_as_float(0xFF800000)) x[j][k] = -0.f;       // (not seen: told from weights below float32)
               l[j][k & 1] += x[j][k];
             }
 
@@ -645,7 +638,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
                 if (kOdd && nan) {                         // a NaN scale counts for rows that see its token only
 #pragma unroll
                   for (int k = 0; k < 4; ++k)
-                    if (partial && hidden(j, k)) w[k] = 0.f;
+                    if (__float_as_uint(x[j][k]) == 0x80000000u) w[k] = 0.f;
                 }
                 const uint32_t p0 = transpose(f16_pair(w[0], w[1])), p1 = transpose(f16_pair(w[2], w[3]));
                 mma(acc[b][0][j], va[2 * o], p0, p1);
@@ -673,7 +666,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) refs[j][i] = odd_unit && low[8 * j + 2 * t + i] >= tok ? -1 : ref;      // (none yet: nothing seen)
     if (odd_unit) steps(Bool<true>());
-    if (abort_flag) {                                    // a wait gave up: the copies still on their way, then out
+    if (waits.abort) {                                   // a wait gave up: the copies still on their way, then out
       volatile int none = 0;
       for (; flying > 0; --flying) {
         mbar_wait_bounded(&full[get], get_round & 1, &none);
@@ -684,8 +677,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
       }
     }
     __syncthreads();                                     // (the warps' last reads of their rings, too)
-    if (abort_flag) {
-      if (tid == 0) report(a.status, timeout_bits(kWhereMxAttention, abort_flag));
+    if (waits.abort) {
+      if (tid == 0) report(a.status, timeout_bits(kWhereMxAttention, waits.abort));
       return;
     }
 
@@ -815,6 +808,8 @@ int sm_count() {
 }
 
 }  // namespace
+
+cudaError_t set_attention_wait_limit(uint64_t ns) { return cudaMemcpyToSymbol(g_wait_limit, &ns, sizeof(ns)); }
 
 int64_t mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t hkv, int64_t d) {
   if (seqs == 0) return 0;

@@ -92,6 +92,57 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Bound of the pipeline waits (ns; of each kernel's own): kWaitLimitNs unless a test shortens it (cat_set_wait_limit_ns).
+__device__ uint64_t g_wait_limit = kWaitLimitNs;
+
+// What a CTA's waits have in common, in shared memory.
+struct Waits {
+  int abort;                                // the line of the first wait that gave up
+  int patience;                             // tries before a wait looks at the clock: 0 with a short limit, and once a wait has given up
+  uint32_t limit;                           // (1 s at most, of a clock's low word)
+  __device__ __forceinline__ void init() {
+    limit = (uint32_t)g_wait_limit;
+    patience = limit < kWaitLimitNs ? 0 : 64;
+    abort = 0;
+  }
+};
+__device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
+  uint32_t p;
+  asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+               : "=r"(p)
+               : "r"(smem_u32(bar)), "r"(parity)
+               : "memory");
+  return p != 0;
+}
+// A wait whose first try has failed.  The clock is looked at every `patience` tries only (of up to some microseconds; polls of some 50 ns: 64
+// times as many).  Out of line: one copy of it for all waits stays in the instruction cache.
+template <bool POLL>
+__device__ __noinline__ bool long_wait(uint64_t* bar, uint32_t parity, volatile Waits* w, int site) {
+  uint32_t since = 0;
+#pragma unroll 1
+  for (int n = 0;; ++n) {
+    if (n >= (POLL ? w->patience << 6 : w->patience)) {
+      if (w->abort) return false;
+      n = 0;
+      const uint32_t now = (uint32_t)globaltimer_ns();
+      if (since == 0) since = now ? now : 1u;            // (0: not looked at yet)
+      if ((int32_t)(now - since) + 1 >= (int32_t)w->limit) {
+        w->abort = site;
+        w->patience = 0;
+        return false;
+      }
+    }
+    if (POLL ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+  }
+}
+// A bounded wait.  POLL: without letting the hardware suspend the thread, whose waking takes longer.  TEST: the first try alone (what
+// is there at once needs no more, and with a short limit what is not gives up there).
+template <bool POLL, bool TEST = POLL>
+__device__ __forceinline__ bool short_wait(uint64_t* bar, uint32_t parity, volatile Waits* w, int site) {
+  if (TEST ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+  return long_wait<POLL>(bar, parity, w, site);
+}
+
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
   asm volatile("{ .reg .pred q; elect.sync _|q, 0xFFFFFFFF; selp.u32 %0, 1, 0, q; }" : "=r"(p));

@@ -188,7 +188,8 @@ struct Bars {
   uint8_t v_nan[2][2][128];                  // a token's blocks of NaN scales (d = 256: those of half of them)
   int64_t scan[20];
   int64_t found_at;
-  int found_s, abort;
+  int found_s;
+  Waits waits;
   uint32_t tmem_addr;
   Walk walks[20];
 };
@@ -457,30 +458,6 @@ __device__ __forceinline__ void hide(uint32_t s_col, int t0, int lim, int low, u
   tmem_st_wait();
 }
 
-// A bounded wait in few instructions (the roles' loops have to stay in the instruction cache together: with the timed wait in line at
-// every place, and copies of the weights' code, 77 % of the cache's rate behind it went into fetching them again).  POLL: without
-// letting the hardware suspend the thread, whose waking takes longer; for the MMAs' warp, behind which all others are.
-constexpr int kTries = 1 << 20, kPolls = 1 << 24;      // (a try takes up to some microseconds, a poll some 50 ns)
-template <bool POLL>
-__device__ __forceinline__ bool short_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int site) {
-  auto over = [&] {
-    if constexpr (!POLL) return mbar_try_wait(bar, parity);
-    uint32_t p;
-    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-                 : "=r"(p)
-                 : "r"(smem_u32(bar)), "r"(parity)
-                 : "memory");
-    return p != 0;
-  };
-#pragma unroll 1
-  for (int n = 0; !over(); ++n)
-    if (n > (POLL ? kPolls : kTries) || *abort) {
-      if (*abort == 0) *abort = site;
-      return false;
-    }
-  return true;
-}
-
 template <int NB>
 __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const __grid_constant__ AttnArgs a) {
   using C = Tc<NB>;
@@ -488,7 +465,6 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Bars* bars = reinterpret_cast<Bars*>(smem + C::kOffBars);
-  volatile int* abort_flag = &bars->abort;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), cta = blockIdx.x, hkv = a.c.hkv;
 
   if (tid == 0) {
@@ -506,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
     mbar_init(&bars->q_full, 4 * QT);
     mbar_init(&bars->most_full, 4);
     mbar_init(&bars->mma_done, 1);
-    bars->abort = 0;
+    bars->waits.init();
     fence_mbar_init();
   }
   pdl_wait_then_release();
@@ -564,8 +540,10 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   if (lane == 0) walk.begin<NB>(a, bars->found_s, bars->found_at, from, to);
   bool ok = true;
   uint32_t jj = 0;                                       // steps so far
-#define CAT_WAIT(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, short_wait<false>(bar, parity, abort_flag, __LINE__)))
-#define CAT_POLL(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, short_wait<true>(bar, parity, abort_flag, __LINE__)))
+// (The roles' loops have to stay in the instruction cache together: with the timed wait in line at every place, and copies of the weights' code, 77 %
+// of the cache's rate behind it went into fetching them again.  Polls are for the MMAs' warp, behind which all others are.)
+#define CAT_WAIT(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, short_wait<false>(bar, parity, &bars->waits, __LINE__)))
+#define CAT_POLL(bar, parity) (ok = ok && (bool)__all_sync(0xFFFFFFFFu, short_wait<true>(bar, parity, &bars->waits, __LINE__)))
 
   if (warp < 4 * QT) {
     // ---------------------------------------------------------------- rows
@@ -1009,7 +987,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_attention_tiles_kernel(const _
   __syncthreads();
   tc_fence_after();
   if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
-  if (tid == 0 && bars->abort) report(a.status, timeout_bits(kWhereMxAttention, bars->abort));
+  if (tid == 0 && bars->waits.abort) report(a.status, timeout_bits(kWhereMxAttention, bars->waits.abort));
 }
 
 template <int NB>
@@ -1038,6 +1016,8 @@ cudaError_t run(const AttnArgs& a, int grid, bool join, cudaStream_t stream) {
 }
 
 }  // namespace
+
+cudaError_t set_attention_tiles_wait_limit(uint64_t ns) { return cudaMemcpyToSymbol(g_wait_limit, &ns, sizeof(ns)); }
 
 int attention_tile_rows(int64_t d) { return d == 256 ? Tc<8>::ROWS : Tc<4>::ROWS; }
 
