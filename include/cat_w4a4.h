@@ -588,14 +588,14 @@ int64_t cat_mx_cache_page_bytes(int64_t page, int64_t d);
 
 /*
  * cat_mx_cache_write -- keys and values k, v device [n][hkv][d] in `dtype` to rows slots[0 .. n-1] (device int32) of the
- * cache.  A token whose slot is outside the cache (a padded batch's -1) is not written.  Slots are to be distinct: of a
+ * cache, which lies apart from them.  A token whose slot is outside the cache (a padded batch's -1) is not written.  Slots are to be distinct: of a
  * row named twice, some bytes may be one token's and some the other's.  Non-finite values as in cat_mx_quantize.
  */
 cat_status cat_mx_cache_write(const void* k, const void* v, cat_dtype dtype, int64_t n, const int32_t* slots,
                               uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d, cat_stream_t stream);
 
 /* cat_mx_cache_read -- the values that rows slots[0 .. m-1] stand for, k and v device [m][hkv][d] in `out_dtype`, exact in
- * both (NaN under a NaN scale); zeros for a slot outside the cache.  k and v must not overlap. */
+ * both (NaN under a NaN scale); zeros for a slot outside the cache.  k and v must not overlap one another, the cache or slots. */
 cat_status cat_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv, int64_t d, const int32_t* slots,
                              int64_t m, cat_dtype out_dtype, void* k, void* v, cat_stream_t stream);
 
@@ -611,8 +611,8 @@ cat_status cat_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, 
  *              `interleaved`.  Channels from rot on stay.
  *   positions  device [n] int32, rows of cos and sin; outside [0, table_rows) a token's queries and keys become NaN (and the
  *              non-finite bit of the status word is raised).
- *   slots, cache  as in cat_mx_cache_write.
- *   q_out      device [n][hq][d] bfloat16, computed in float32 and rounded once; not within qkv.
+ *   slots, cache  as in cat_mx_cache_write; the cache lies apart from all that is read.
+ *   q_out      device [n][hq][d] bfloat16, computed in float32 and rounded once; apart from all others.
  * Keys are quantized as if computed exactly: where float32's error could change a code or a scale they are computed again to some
  * 2^-43, so a cache does not depend on how its tokens came to it.
  */
@@ -642,9 +642,9 @@ int64_t cat_mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t 
  * 2^-35 below the largest of their neighbours.  Weights are rounded to 11 bits (those 2^-22 and less of the row's largest, and those of
  * values whose scale is below the largest seen by as much in all, to fewer).  A NaN key or value of a token that a row does not see
  * leaves it as it is.
- *   out      device [n][hq][d] in `out_dtype`, rounded once; not within q.
+ *   out      device [n][hq][d] in `out_dtype`, rounded once; apart from all others.
  *   workspace device, at least cat_mx_attention_workspace bytes, written and read by this call alone: calls that may run at the
- *            same time need one each.  Its contents need not be kept or set.
+ *            same time need one each.  Apart from all others.  Its contents need not be kept or set.
  * Nothing is read back to the host: lengths may change from one replay of a captured graph to the next.
  */
 cat_status cat_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t* cache, int64_t pages, int64_t page, int64_t hkv,

@@ -847,6 +847,17 @@ def _mx_cache_sizes(cache: torch.Tensor, d: int) -> Tuple[int, int, int]:
     return pages, page, hkv
 
 
+def _apart(written: dict, read: dict) -> None:
+    """Refuses memory that is written while it is read, or written twice: {name: tensor or None} each."""
+    def ends(t):
+        return t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()
+    pairs = [(a, b) for a in written for b in read] + [(a, b) for i, a in enumerate(written) for b in list(written)[:i]]
+    for a, b in pairs:
+        x, y = written[a], read.get(b, written.get(b))
+        if x is not None and y is not None and ends(x)[0] < ends(y)[1] and ends(y)[0] < ends(x)[1]:
+            raise ValueError(f"{a} must not share memory with {b}")
+
+
 def _numbers(t: torch.Tensor, name: str, dev: torch.device) -> int:
     """Checks an int32 tensor of one dimension; its length."""
     m = t.numel() if isinstance(t, torch.Tensor) else 0
@@ -869,6 +880,7 @@ def cat_mx_cache_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, ca
     _expect(slots, "slots", torch.int32, (n,), dev)
     pages, page, heads = _mx_cache_sizes(cache, d)
     _expect(cache, "cache", torch.uint8, (pages, 2, hkv, cache.shape[3]), dev)
+    _apart({"cache": cache}, {"k": k, "v": v, "slots": slots})
     _check("cat_mx_cache_write", load_library().cat_mx_cache_write(_ptr(k), _ptr(v), _dtype(k), n, _ptr(slots), _ptr(cache), pages,
                                                                    page, hkv, d, _stream(dev)))
     return cache
@@ -890,6 +902,7 @@ def cat_mx_cache_read(cache: torch.Tensor, slots: torch.Tensor, d: int, out_dtyp
     out_dtype = out_dtype or (k.dtype if k is not None else v.dtype if v is not None else None)
     k = _mx_result(k, "k", out_dtype, (m, hkv, d), dev)
     v = _mx_result(v, "v", k.dtype, (m, hkv, d), dev)
+    _apart({"k": k, "v": v}, {"cache": cache, "slots": slots})
     _check("cat_mx_cache_read", load_library().cat_mx_cache_read(_ptr(cache), pages, page, hkv, d, _ptr(slots), m, _dtype(k), _ptr(k),
                                                                  _ptr(v), _stream(dev)))
     return k, v
@@ -930,6 +943,8 @@ def cat_mx_rope_cache_write(qkv: torch.Tensor, d: int, positions: torch.Tensor, 
             if w is not None:
                 _expect(w, name, weight.dtype, (d,), dev)
     q = _given(q, "q", torch.bfloat16, (n, hq, d), dev)
+    _apart({"q": q, "cache": cache}, {"qkv": qkv, "positions": positions, "slots": slots, "cos": cos, "sin": sin, "q_weight": q_weight,
+                                      "k_weight": k_weight})
     _check("cat_mx_rope_cache_write", load_library().cat_mx_rope_cache_write(
         _ptr(qkv), _dtype(qkv), n, hq, _ptr(q_weight), _ptr(k_weight), 0 if weight is None else _dtype(weight), eps, _ptr(positions),
         _ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)), _ptr(slots), _ptr(cache), pages, page, hkv, d,
@@ -974,11 +989,13 @@ def cat_mx_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, 
         out = torch.empty((n, hq, d), dtype=out_dtype or torch.bfloat16, device=dev)
     else:
         _expect(out, "out", out_dtype or out.dtype, (n, hq, d), dev)
+    if workspace is not None:
+        _expect(workspace, "workspace", torch.uint8, (workspace.numel(),), dev)
+    _apart({"out": out, "workspace": workspace}, {"q": q, "cache": cache, "table": table, "lens": lens, "offsets": offsets})
     kind, stream = _dtype(out), _stream(dev)
     need = max(cat_mx_attention_workspace(n, seqs, hq, hkv, d), 0)
     if workspace is None:
         workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
-    _expect(workspace, "workspace", torch.uint8, (workspace.numel(),), dev)
     _check("cat_mx_attention", load_library().cat_mx_attention(
         _ptr(q), n, hq, _ptr(cache), pages, page, hkv, d, _ptr(table), width, _ptr(lens), seqs, _ptr(offsets), scale, window,
         kind, _ptr(out), _ptr(workspace), workspace.numel(), stream))

@@ -1097,6 +1097,7 @@ static bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_byt
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
+static int64_t cache_bytes(int64_t pages, int64_t page, int64_t hkv, int64_t d) { return pages * 2 * hkv * cat::mx_page_bytes(page, d); }
 static int64_t bytes_of(cat_dtype t) { return t == CAT_F32 ? 4 : 2; }
 static bool rows_fit(int64_t n) { return n >= 0 && n <= kMaxMxRows; }
 
@@ -1159,6 +1160,11 @@ cat_status cat_mx_rope_cache_write(const void* qkv, cat_dtype dtype, int64_t n, 
     return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
   if (overlap(qkv, n * (hq + 2 * hkv) * d * bytes_of(dtype), q_out, n * hq * d * 2))
     return fail(CAT_ERR_INVALID_ARG, "q_out must not overlap qkv");
+  const int64_t q_bytes = n * hq * d * 2, table_bytes = table_rows * (rot / 2) * 4, w_bytes = d * bytes_of(weight_dtype);
+  if (overlap(q_out, q_bytes, cache, cache_bytes(pages, page, hkv, d)) || overlap(q_out, q_bytes, cos, table_bytes) ||
+      overlap(q_out, q_bytes, sin, table_bytes) || overlap(q_out, q_bytes, positions, n * 4) || overlap(q_out, q_bytes, slots, n * 4) ||
+      (q_weight && overlap(q_out, q_bytes, q_weight, w_bytes)) || (k_weight && overlap(q_out, q_bytes, k_weight, w_bytes)))
+    return fail(CAT_ERR_INVALID_ARG, "q_out must not share memory with the cache, the tables, positions, slots or weights");
   return mx_launch("cat_mx_rope_cache_write launch", [&](uint32_t* status) {
     return cat::launch_mx_rope(qkv, (int)dtype, n, hq, q_weight, k_weight, (int)weight_dtype, eps, positions, cos, sin, table_rows,
                                rot, interleaved, slots, cache, pages, page, hkv, d, q_out, status, (cudaStream_t)stream);
@@ -1192,6 +1198,11 @@ cat_status cat_mx_attention(const void* q, int64_t n, int64_t hq, const uint8_t*
     return fail(CAT_ERR_ALIGNMENT, "pointers must be 16-byte aligned");
   if (overlap(q, n * hq * d * 2, out, n * hq * d * bytes_of(out_dtype)))
     return fail(CAT_ERR_INVALID_ARG, "out must not overlap q");
+  const int64_t out_bytes = n * hq * d * bytes_of(out_dtype);
+  if (overlap(out, out_bytes, cache, cache_bytes(pages, page, hkv, d)) || overlap(out, out_bytes, table, seqs * width * 4) ||
+      overlap(out, out_bytes, lens, seqs * 4) || (offsets && overlap(out, out_bytes, offsets, (seqs + 1) * 4)) ||
+      (workspace && workspace_bytes > 0 && overlap(out, out_bytes, workspace, workspace_bytes)))
+    return fail(CAT_ERR_INVALID_ARG, "out must not share memory with the cache, table, lens, offsets or the workspace");
   if ((st = check_device()) != CAT_OK) return st;
   const int64_t need = cat::mx_attention_workspace(n, seqs, hq, hkv, d);
   if (need < 0) return fail(CAT_ERR_CUDA, "the device's size cannot be asked");

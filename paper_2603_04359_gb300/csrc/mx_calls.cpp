@@ -238,6 +238,11 @@ const at::Tensor* numbers(PyObject* o, int64_t n, int64_t device) {
   const at::Tensor* t = dense(o, 1);
   return t && t->scalar_type() == at::kInt && (n < 0 || t->size(0) == n) && t->get_device() == device ? t : nullptr;
 }
+// Whether two tensors share memory.
+bool shared(const at::Tensor& a, const at::Tensor& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.data_ptr()), y = reinterpret_cast<uintptr_t>(b.data_ptr());
+  return x < y + b.nbytes() && y < x + a.nbytes();
+}
 const int32_t* i32(const at::Tensor* t) { return t ? static_cast<const int32_t*>(t->data_ptr()) : nullptr; }
 at::Tensor make3(int64_t a, int64_t b, int64_t c, at::ScalarType type) {
   return at::detail::empty_generic({a, b, c}, c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA),
@@ -255,7 +260,7 @@ PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t n = k->size(0), hkv = k->size(1), d = k->size(2);
   const at::Tensor* slots = numbers(args[2], n, k->get_device());
   const Cache c(args[3], d);
-  if (!slots || !c.on(k->get_device()) || c.hkv != hkv) Py_RETURN_NONE;
+  if (!slots || !c.on(k->get_device()) || c.hkv != hkv || shared(*k, *c.t) || shared(*v, *c.t) || shared(*slots, *c.t)) Py_RETURN_NONE;
   const cat_status st = unlocked([&] {
     return cat_mx_cache_write(k->data_ptr(), v->data_ptr(), code(*k), n, i32(slots), u8(*c.t), c.pages, c.page, hkv, d, stream_of(*k));
   });
@@ -305,7 +310,8 @@ PyObject* rope_cache_write(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                    *slots = numbers(args[5], n, device);
   if (!c.on(device) || x->size(1) % d != 0 || heads <= 2 * c.hkv || !positions || !slots || !cos || !sin ||
       cos->scalar_type() != at::kFloat || sin->scalar_type() != at::kFloat || cos->sizes() != sin->sizes() ||
-      cos->get_device() != device || sin->get_device() != device)
+      cos->get_device() != device || sin->get_device() != device || shared(*x, *c.t) || shared(*positions, *c.t) || shared(*slots, *c.t) ||
+      shared(*cos, *c.t) || shared(*sin, *c.t))
     Py_RETURN_NONE;
   const at::Tensor* w[2] = {nullptr, nullptr};
   for (int i = 0; i < 2; ++i)
@@ -313,6 +319,7 @@ PyObject* rope_cache_write(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         (!(w[i] = dense(args[7 + i], 1)) || !real(*w[i]) || w[i]->size(0) != d || w[i]->get_device() != device))
       Py_RETURN_NONE;
   if (w[0] && w[1] && w[0]->scalar_type() != w[1]->scalar_type()) Py_RETURN_NONE;
+  if ((w[0] && shared(*w[0], *c.t)) || (w[1] && shared(*w[1], *c.t))) Py_RETURN_NONE;
   const double eps = PyFloat_AsDouble(args[9]);
   if (eps == -1.0 && PyErr_Occurred()) return nullptr;
   const int interleaved = PyObject_IsTrue(args[10]);
