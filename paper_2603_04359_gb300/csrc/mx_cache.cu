@@ -716,9 +716,9 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 4 : 7) mx_rope_kernel(cons
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max_magnitude(m, y[b][i]);
     m = row_max(m);
-    float e = 0.f;
+    float e = 0.f, all = 0.f;
     if (keys) {                                          // (all lanes shuffle, whatever their heads are; channels that are not turned)
-      const float all = fmaxf(row_max(most[b]), m);
+      all = fmaxf(row_max(most[b]), m);
       if (is_k) e = all * kMargin;
     }
     const uint32_t byte = mx_scale_byte(__float_as_uint(m));
@@ -741,12 +741,12 @@ __global__ void __launch_bounds__(kThreads, NB == 8 ? 4 : 7) mx_rope_kernel(cons
                    mx_scale_byte(__float_as_uint(fmaxf(m - e, 0.f))) != byte || mx_scale_byte(__float_as_uint(m + e)) != byte))
         near |= 1u << b;
       // sizes at which pairs of float32 would lose bits (nothing tells what a NaN or an infinity is made of)
-      far |= is_k && !(m > 0x1p-40f && e < 0x1p40f && byte != 255u);
+      far |= is_k && !((m > 0x1p-40f || all == 0.f) && e < 0x1p40f && byte != 255u);
     }
   }
   const uint32_t blocks = __reduce_or_sync(0xFFFFFFFFu, near);
   if (blocks) {
-    if (__any_sync(0xFFFFFFFFu, near && far))
+    if (__any_sync(0xFFFFFFFFu, is_k && far))            // (all of the warp's keys get these blocks anew)
       exact_key<T, NB>(a, x, weight, PAIRS == kNeighbours, pos, valid, is_k, p, blocks, &out);
     else
       near_key<T, NB>(a, x, weight, PAIRS == kNeighbours, pos, is_k, p, blocks, &out);
