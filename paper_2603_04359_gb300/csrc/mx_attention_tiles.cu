@@ -40,7 +40,7 @@ constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kUnitCost = 448;              // a unit's beginning and end, in tokens (measured: 768 and 1024 were up to 4 and 7 % slower)
 constexpr int kLeastPiece = 256;            // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
-constexpr int kKeysApart = 20;              // what 32 tokens' keys may lie apart before each has its own reference
+constexpr int kKeysApart = 8;               // what 32 tokens' keys may lie apart before each has its own reference
 constexpr int kBeyond = 4;                  // what a step's tokens may lie apart, or below the reference, before each has its own
 constexpr uint32_t kTmemCols = 512;
 constexpr int kBarRoom = 8192;
