@@ -614,7 +614,8 @@ cat_status cat_mx_cache_read(const uint8_t* cache, int64_t pages, int64_t page, 
  *   slots, cache  as in cat_mx_cache_write; the cache lies apart from all that is read.
  *   q_out      device [n][hq][d] bfloat16, computed in float32 and rounded once; apart from all others.
  * Keys are quantized as if computed exactly: where float32's error could change a code or a scale they are computed again to some
- * 2^-43, so a cache does not depend on how its tokens came to it.
+ * 2^-43, so a cache does not depend on how its tokens came to it.  (But for channels that the norm takes below 2^-126 and a weight of
+ * more than 2^26 brings back.)
  */
 cat_status cat_mx_rope_cache_write(const void* qkv, cat_dtype dtype, int64_t n, int64_t hq, const void* q_weight,
                                    const void* k_weight, cat_dtype weight_dtype, double eps, const int32_t* positions,
@@ -630,18 +631,19 @@ int64_t cat_mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t 
  * cat_mx_attention -- causal attention of a ragged batch over its sequences' pages of a cache.
  *   q        device [n][hq][d] bfloat16; hq a multiple of hkv, query head h reads head h / (hq / hkv) of the cache.
  *   offsets  device [seqs + 1] int32: rows offsets[s] .. offsets[s+1]-1 of q are the last tokens of sequence s, in order;
- *            NULL: one row a sequence (n == seqs).  Taken as the nearest that are within [0, n]; sequences may be empty.  Rows of
- *            no sequence (before offsets[0], from offsets[seqs] on) are set to zero.
+ *            NULL: one row a sequence (n == seqs).  In ascending order; taken as the nearest that are within [0, n]; sequences may be
+ *            empty.  Rows of no sequence (before offsets[0], from offsets[seqs] on) are set to zero.
  *   lens     device [seqs] int32: tokens of each sequence in the cache, those of the rows included.
  *   table    device [seqs][width] int32: a sequence's pages, token t in page table[s][t / page].  Entries behind a sequence's
  *            length are not read; a token on no page (an entry outside [0, pages), t >= width * page) is not attended.
  *   window   0, or the number of tokens a row sees: itself and the window - 1 before it.
  * Row j of a sequence with r rows and length L is token p = L - r + j and sees tokens max(0, p - window + 1) .. p:
  *   out = sum_t softmax_t(scale q k_t) v_t, zero for a row that sees nothing (p < 0, a length of zero).
- * Scores and sums in float32.  A score's operands are exact, but for channels of a query 2^-24 below its row's largest and keys
- * 2^-35 below the largest of their neighbours.  Weights are rounded to 11 bits (those 2^-22 and less of the row's largest, and those of
- * values whose scale is below the largest seen by as much in all, to fewer).  A NaN key or value of a token that a row does not see
- * leaves it as it is.
+ * Scores and sums in float32.  A score's operands are exact, but for channels of a query 2^-24 below its row's largest and blocks of a
+ * key 2^-27 below its token's largest.  Weights are rounded to 11 bits (those 2^-14 and less of the row's largest, and those of values
+ * whose scale is below the largest that the row sees by as much in all, to fewer: off by 2^-26 of the largest at most).  What a row does
+ * not see, NaN among it, leaves it as it is, but for such roundings.  Scores beyond float32 are not defined; all others are, of queries, keys, values and
+ * scales of any size.
  *   out      device [n][hq][d] in `out_dtype`, rounded once; apart from all others.
  *   workspace device, at least cat_mx_attention_workspace bytes, written and read by this call alone: calls that may run at the
  *            same time need one each.  Apart from all others.  Its contents need not be kept or set.

@@ -10,7 +10,7 @@
 // A token's keys and values are 17/16 of a byte a channel for both, read once for all the query heads that share them: 152 SMs have
 // ~2.9 lane instructions a code in the time its bytes take from memory, and the unpacking is most of what there is to do: ~400 warp
 // instructions for 16 tokens of a head of 128 channels and 8 rows, 172 of them on the pipe that issues one every other cycle a scheduler.
-// 64 sequences of up to 8192 tokens, 8 key heads: 292 MB in 83 us (3.5 TB/s); one of 131000 tokens 45.5 us, 40 of them here; 2.3
+// 64 sequences of up to 8192 tokens, 8 key heads: 292 MB in 85 us (3.4 TB/s); one of 131000 tokens 46.5 us, 41 of them here; 2.3
 // instructions a cycle, from 16 warps an SM (128 registers; 12 and 20 warps were no faster).
 // Codes go from memory to registers in the layout of the matrix instructions' operands (which is what the cache's pieces are for) and
 // are unpacked in pairs there.  tcgen05 would want them unpacked into shared memory first, for 128 rows where there are 1 to 32.
@@ -737,7 +737,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, uint8_t* smem) {
 
 // Beside the tiles of the same call (which have waited for what was before them, and share nothing with this) it waits for them at its
 // end, so that what comes after it comes after both: 16 sequences of 5 drafted tokens, where the tiles have nothing to do, 54 us
-// instead of 57.
+// instead of 57.  Where the tiles have work, their shared memory leaves no room for this kernel's CTAs, which start on an SM when its
+// tiles' CTA leaves: 64 sequences of 4000 tokens beside 2048 rows over 8192, 430 us, apart 79 and 284.
 template <int NB, int NT, int RESIDENT>
 __global__ void __launch_bounds__(kThreads, RESIDENT) mx_attention_kernel(const __grid_constant__ AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
@@ -750,7 +751,9 @@ struct Form {
   int nt, resident;
 };
 Form form_of(int64_t n, int64_t seqs, int64_t group, int64_t d) {
-  const int64_t rows = (n + seqs - 1) / seqs * group;    // of a sequence, on average
+  // Of a sequence, on average, the tiles' among them, as the host does not know which those are: beside a long chunk, sequences of one row
+  // go by the form for 24 (63 of them and 2048 rows, 64 / 8 heads: 673 us, apart 79 and 532).
+  const int64_t rows = (n + seqs - 1) / seqs * group;
   const int nt = rows <= 8 ? 1 : rows <= 16 || d == 256 ? 2 : 3;
   return {nt, nt * d <= 128 ? 4 : nt * d <= 256 ? 3 : 2};
 }
@@ -789,7 +792,7 @@ cudaError_t run(const AttnArgs& a, int grid, const AttnArgs& tiles, int tile_gri
   note_launch();
   if ((e = cudaLaunchKernelEx(&cfg, mx_attention_kernel<NB, NT, RESIDENT>, a)) != cudaSuccess) return e;
   // Launched when all is done: CTAs that wait beside this kernel's, 2 to 4 an SM, are in the way of the next call's, which then come
-  // to lie unevenly (64 sequences of up to 8192 tokens in a row of calls: 98 us each, against 83).
+  // to lie unevenly (64 sequences of up to 8192 tokens in a row of calls: 98 us each, against 83 as it was then).
   note_launch();
   const int entries = 2 * grid;
   if (!tile_grid) {

@@ -29,7 +29,7 @@ struct AttnArgs {
   int n, hq, group, seqs;
   int few;                                  // sequences of at most this many rows are the first kernel's, others the second's
   int clears;                               // this launch clears the rows that see nothing
-  int beside;                               // this launch runs beside the one before it
+  int beside;                               // this launch does not wait for the one before it until its end
   float scale;                              // scale log2 e
   int64_t window;
   void* out;

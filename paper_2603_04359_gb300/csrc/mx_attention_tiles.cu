@@ -5,13 +5,16 @@
 // on 5th-generation tensor cores, float16 operands.  The tensor cores take the codes as numbers only after they are unpacked: each of
 // a step's keys and values to float16, code times 2^(byte - ref + 12) with ref the largest scale byte of a warp's tokens (keys;
 // the products of 32 tokens are times its power again) or of all values so far (O is scaled when it grows).  That is exact down to 2^-35
-// of the largest block.  A step's unpacking is shared by 256 rows (two tiles of 128; d = 256: one): queries of a key head's group lie
-// together, row r is head r % group of token r / group.
+// of the largest block.  A row may see other tokens than its neighbours, and its result does not depend on the size of the others: where
+// tokens lie apart (keys by 2^8; values by 2^4 at an edge of what rows see, or below the reference) each has a reference of its own,
+// which its scores get back where they are, and its weights carry.  A step's unpacking is shared by 256 rows (two tiles of 128; d = 256:
+// one): queries of a key head's group lie together, row r is head r % group of token r / group.
 //
 // Per step of 128 tokens at d = 128 the MMAs take 2080 cycles of an SM (32 of them, 65 each), the exponentials of 2 x 16384 scores 1024, the
 // unpacking ~400 issue slots a scheduler.  A step takes ~4800: a tile's weights (~2900: two passes over its scores, their way from and to
 // tensor memory), its two products and the waits between them follow one another, and two tiles in turn fill the tensor cores to 42 %.
-// 2048 tokens of 32 heads over 32768: 1082 us, 0.98 PFLOP/s; a prompt of 4096: 211, a unit's beginning and end 12000 cycles of ~150000.  What was slower: steps of 64 tokens with two buffers of scores a tile, whose
+// 2048 tokens of 32 heads over 32768: 1099 us, 0.97 PFLOP/s; a prompt of 4096: 217, a unit's beginning and end 12000 cycles of ~150000
+// (1082 and 211 before scores and values of any size were looked out for).  What was slower: steps of 64 tokens with two buffers of scores a tile, whose
 // products of 64 columns take as long as those of 128 (1350 to 1530 us); the maximum found along with the weights, and these again where
 // it grew, whose code does not stay in the instruction cache beside the other roles' (1360 with steps of 64); one ring for the copies
 // of keys and of values, where values that wait for room keep keys back (1430).
@@ -23,7 +26,8 @@
 //   16           issues the MMAs: P V of a tile, behind it the tile's next scores (d = 256: of the step after the next), in the weights' place
 //   17           bulk copies of the codes as they are, a ring each of keys and values
 // MMAs of one thread are carried out in the order of their issue, so next scores may follow the product that reads the weights
-// in their place.  Every wait is bounded; one that gives up raises the device status word and all roles drain and leave.
+// in their place.  Every wait is bounded; one that gives up raises the device status word and all roles drain and leave.  (One copy of the
+// wait out of line, for all places: in line at each, a prompt of 4096 took 226 us, of heads of 64 203 instead of 180.)
 //
 // A CTA has an equal piece of a line of all units as mx_attention.cu's; a unit's length there is a straight line in its number (the
 // tokens that its last row sees, or the window), so that its place can be found without a list.
