@@ -640,8 +640,8 @@ int64_t cat_mx_attention_workspace(int64_t n, int64_t seqs, int64_t hq, int64_t 
  * Row j of a sequence with r rows and length L is token p = L - r + j and sees tokens max(0, p - window + 1) .. p:
  *   out = sum_t softmax_t(scale q k_t) v_t, zero for a row that sees nothing (p < 0, a length of zero).
  * Scores and sums in float32.  A score's operands are exact, but for channels of a query 2^-24 below its row's largest and blocks of a
- * key 2^-27 below its token's largest.  Weights are rounded to 11 bits (those 2^-14 and less of the row's largest, and those of values
- * whose scale is below the largest that the row sees by as much in all, to fewer: off by 2^-26 of the largest at most).  What a row does
+ * key 2^-27 below its token's largest.  Weights are rounded to 11 bits (those 2^-20 and less of the row's largest, and those of values
+ * whose scale is below the largest that the row sees by as much in all, to fewer: off by 2^-31 of the largest at most).  What a row does
  * not see, NaN among it, leaves it as it is, but for such roundings.  Scores beyond float32 are not defined; all others are, of queries, keys, values and
  * scales of any size.
  *   out      device [n][hq][d] in `out_dtype`, rounded once; apart from all others.

@@ -41,7 +41,7 @@ constexpr int kLeastPiece = 4;              // steps a CTA is worth
 // The values' reference, a scale byte, as the weights have it: 2^(136 - ref) is what they are times, and within these float32 holds both their
 // sums and those that count little.
 constexpr int kLowR = 80, kHighR = 200;
-constexpr int kBeyond = 8;                  // what a row's reference may be above the largest that the row sees
+constexpr int kBeyond = 2;                  // what a row's reference may be above the largest that the row sees
 __device__ __forceinline__ int within(int ref) { return min(max(ref, kLowR), kHighR); }
 
 struct Seq : Rows {

@@ -6,7 +6,7 @@
 // a step's keys and values to float16, code times 2^(byte - ref + 12) with ref the largest scale byte of a warp's tokens (keys;
 // the products of 32 tokens are times its power again) or of all values so far (O is scaled when it grows).  That is exact down to 2^-35
 // of the largest block.  A row may see other tokens than its neighbours, and its result does not depend on the size of the others: where
-// tokens lie apart (keys by 2^8; values by 2^4 at an edge of what rows see, or below the reference) each has a reference of its own,
+// tokens lie apart (keys by more than 2^8; values by more than 2^2 at an edge of what rows see, or below the reference) each has a reference of its own,
 // which its scores get back where they are, and its weights carry.  A step's unpacking is shared by 256 rows (two tiles of 128; d = 256:
 // one): queries of a key head's group lie together, row r is head r % group of token r / group.
 //
@@ -45,7 +45,7 @@ constexpr int kUnitCost = 448;              // a unit's beginning and end, in to
 constexpr int kLeastPiece = 256;            // tokens (with units' costs) that a CTA is worth
 constexpr int kLowR = 16;                   // least reference scale byte
 constexpr int kKeysApart = 8;               // what 32 tokens' keys may lie apart before each has its own reference
-constexpr int kBeyond = 4;                  // what a step's tokens may lie apart, or below the reference, before each has its own
+constexpr int kBeyond = 2;                  // what a step's tokens may lie apart, or below the reference, before each has its own
 constexpr uint32_t kTmemCols = 512;
 constexpr int kBarRoom = 8192;
 

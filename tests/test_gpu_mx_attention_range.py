@@ -195,3 +195,55 @@ def test_many_sequences_some_of_many_rows():
     b = Batch(39, lens.tolist(), rows.tolist(), 4, 2, 64, 16)
     check(b)
     check(b, window=17)
+
+
+def random_batch(seed):
+    """A batch of any kind: prompts, drafted tokens, decode steps; keys and values of sizes that go along, jump or lie far from one."""
+    rng = np.random.default_rng(seed)
+    d, hkv, group = int(rng.choice([64, 128, 256])), int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 4, 5, 8, 17]))
+    page, seqs, kind = int(rng.choice([16, 32, 64, 128])), int(rng.integers(1, 6)), rng.choice(["decode", "draft", "prompt", "mixed"])
+    lens = [int(np.exp(rng.uniform(0, np.log(700)))) for _ in range(seqs)]
+    if rng.random() < 0.2:
+        lens[0] = 3000
+    rows = []
+    for n in lens:
+        k = kind if kind != "mixed" else rng.choice(["decode", "draft", "prompt"])
+        rows.append(1 if k == "decode" else int(rng.integers(1, 12)) if k == "draft" else int(rng.integers(1, min(n, 300) + 1)))
+    if rng.random() < 0.3:
+        rows[0] = min(lens[0] + int(rng.integers(0, 4)), 300)
+    b = Batch(seed, lens, rows, hkv * group, hkv, d, page, fill=int(rng.choice([0xFF, 0xFD, 0x00])))
+    sizes = {"plain": lambda n, up: np.ones(n), "spread": lambda n, up: np.exp2(rng.uniform(-30, up, n)),
+             "jumps": lambda n, up: np.where(rng.random(n) < 0.02, 2.0 ** rng.uniform(0, 2 * up + 1), 1.0),
+             "walk": lambda n, up: np.exp2(np.cumsum(rng.normal(0, 1.0, n)).clip(-60, up)),
+             "tiny": lambda n, up: np.exp2(rng.uniform(-100, -90, n)),
+             "huge": lambda n, up: np.exp2(rng.uniform(90, 118, n)) if up > 5 else np.ones(n)}
+    for s, n in enumerate(lens):
+        k, v = (rng.standard_normal((n, hkv, d)) * sizes[rng.choice(list(sizes))](n, up)[:, None, None] for up in (2, 60))
+        if rng.random() < 0.3:
+            v[:, :, 32:64] *= 2.0 ** -20
+        if rng.random() < 0.2:
+            v[rng.integers(0, n)] = 0.0
+            k[rng.integers(0, n)] = 0.0
+        rewrite(b, s, np.arange(n), k=k, v=v)
+    window = int(np.exp(rng.uniform(0, np.log(800)))) if rng.random() < 0.5 else 0
+    return b, dict(window=window, narrow=bool(rng.random() < 0.3), scale=float(d ** -0.5 * rng.choice([1, 1, -1, 4, 0.01])))
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_random_batches(seed):
+    b, how = random_batch(1000 + seed)
+    check(b, **how)
+
+
+@pytest.mark.parametrize("rows", [[2, 40], [100, 40]])
+def test_a_rows_values_below_ones_that_it_does_not_see(rows):
+    """The largest that a row sees has a weight of 2^-20, and its result is of values as much below that; the next token's are up to 2^10 above."""
+    n = rows[0] + 2
+    for up in range(1, 11):
+        b = Batch(61, [n, 300], rows, 4, 2, 128, 32)
+        b.q = torch.ones_like(b.q)
+        size, k = np.full((n, 1, 1), 2.0 ** -20), 0.5 * b.rng.standard_normal((n, 2, 128))
+        size[0], k[0] = 1.0, -1.0
+        size[n - 1], k[n - 1] = 2.0 ** up, -1.0
+        rewrite(b, 0, np.arange(n), k=k, v=b.rng.uniform(0.5, 1.0, (n, 2, 128)) * size)
+        check(b, scale=14 / 128)
