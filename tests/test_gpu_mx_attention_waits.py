@@ -30,12 +30,12 @@ def call(lens, rows, hq, hkv, d, page=64, seed=51):
     return lambda: cat.cat_mx_attention(q, cache, table, length, d ** -0.5, offsets=offsets)
 
 
-CALLS = {"decode": ([16384] * 16, [1] * 16, 64, 8), "drafted": ([9000] * 16, [5] * 16, 32, 8), "prompts": ([2000, 1500], [2000, 700], 8, 2),
+CALLS = {"decode": ([16384] * 16, [1] * 16, 64, 8), "prompts": ([2000, 1500], [2000, 700], 8, 2),
          "parts": ([60000], [70], 8, 1), "mixed": ([2000] + [9000] * 20, [700] + [1] * 20, 32, 8)}
 
 
-# (other sizes of the first two leave copies time enough: none is waited for)
-@pytest.mark.parametrize("kind,d", [("decode", 64), ("decode", 128), ("drafted", 256)] + [(k, d) for k in ("prompts", "parts", "mixed") for d in (64, 128, 256)])
+# (at their start decode's CTAs ask for 85 MB at once; with wider heads or more rows copies may have time enough, and none is waited for)
+@pytest.mark.parametrize("kind,d", [("decode", 64), ("decode", 128)] + [(k, d) for k in ("prompts", "parts", "mixed") for d in (64, 128, 256)])
 def test_bounded_wait_gives_up_then_library_recovers(kind, d):
     run = call(*CALLS[kind], d)
     want = run()
